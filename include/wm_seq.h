@@ -63,6 +63,12 @@ const char *wm_seq_last_error(const wm_seq *h);
 /* Kernels that the last call launched. */
 int wm_seq_last_launches(const wm_seq *h);
 
+/* Failure injection for tests of the timeout path: every wait inside a kernel is bounded.
+ * With polls > 0 the next scan call that joins spans across CTAs (few channels, many
+ * steps) makes its first CTA poll, at most that often, for something that nothing sets; it
+ * records WM_ERR_TIMEOUT, as a real bounded wait does, and goes on.  One shot. */
+wm_status wm_seq_inject_wait_timeout(wm_seq *h, unsigned int polls);
+
 /* Frees what the handle owns (after the device has finished).  NULL is a no-op. */
 void wm_seq_destroy(wm_seq *h);
 

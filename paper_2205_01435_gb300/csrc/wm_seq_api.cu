@@ -162,21 +162,27 @@ extern "C" wm_status wm_seq_sync(wm_seq *h) {
     if (!h) return WM_ERR_INVALID_ARG;
     h->err[0] = 0;
     OnDevice on(h);
-    int st = 0;
+    int st[2] = {};
     cudaError_t e = on.e;
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
-    if (e == cudaSuccess) e = cudaMemcpy(&st, h->status, sizeof st, cudaMemcpyDeviceToHost);
-    if (e == cudaSuccess && st) e = cudaMemset(h->status, 0, sizeof st);
+    if (e == cudaSuccess) e = cudaMemcpy(st, h->status, sizeof st, cudaMemcpyDeviceToHost);
+    if (e == cudaSuccess && (st[0] || st[1])) e = cudaMemset(h->status, 0, sizeof st);
     if (e != cudaSuccess) return cuda_fail(h, e, "wm_seq_sync");
-    if (st == WM_ERR_INVALID_ARG)
-        return fail(h, WM_ERR_INVALID_ARG, "wm_seq_sync", "a token or a length of an earlier call was out of range");
-    if (st) return fail(h, (wm_status)st, "wm_seq_sync", "a wait inside a kernel gave up");
+    if (st[1]) return fail(h, (wm_status)st[1], "wm_seq_sync", "a wait inside a kernel gave up");
+    if (st[0]) return fail(h, (wm_status)st[0], "wm_seq_sync", "a token or a length of an earlier call was out of range");
     return WM_OK;
 }
 
 extern "C" const char *wm_seq_last_error(const wm_seq *h) { return h ? h->err : "null handle"; }
 
 extern "C" int wm_seq_last_launches(const wm_seq *h) { return h ? h->last_launches : 0; }
+
+extern "C" wm_status wm_seq_inject_wait_timeout(wm_seq *h, unsigned int polls) {
+    if (!h) return WM_ERR_INVALID_ARG;
+    h->err[0] = 0;
+    h->test_wait = polls;
+    return WM_OK;
+}
 
 #define SEQ_BEGIN(what)                                            \
     if (!h) return WM_ERR_INVALID_ARG;                             \

@@ -16,8 +16,9 @@ struct wm_seq {
     bool ws_captured = false;   // a captured graph may hold ws: it is kept when ws grows
     void *retired[64] = {};     // such earlier workspaces (each at least doubles)
     int n_retired = 0;
-    int *status = nullptr;      // device status word
+    int *status = nullptr;      // device status words: [0] arguments, [1] a wait gave up
     int last_launches = 0;
+    uint32_t test_wait = 0;     // wm_seq_inject_wait_timeout: polls of the next call's injected wait
     char err[256] = "";
 };
 

@@ -115,6 +115,21 @@ def test_scan_resets_and_lengths(ops, dtype, T, N, H, reset, lengths):
     check_scan(ops, scan_inputs(T, N, H, DT[dtype], seed=5 + T, reset=reset, lengths=lengths))
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,N,H,layout", [(9, 90, 512, "plain"), (33, 160, 301, "plain"), (70, 100, 512, "columns"),
+                                          (40, 48, 1000, "batch"), (11, 95, 514, "plain")])
+@pytest.mark.parametrize("masks", [False, True])
+def test_scan_many_channels(ops, dtype, T, N, H, layout, masks):
+    check_scan(ops, scan_inputs(T, N, H, DT[dtype], layout, seed=T, reset=masks, lengths=masks))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,N,H", [(5000, 1, 20), (3000, 2, 130), (6000, 1, 66), (2500, 1, 33), (1500, 3, 700)])
+def test_scan_long(ops, dtype, T, N, H):
+    """Several stretches of time, one channel tile to many, resets and padding across their borders."""
+    check_scan(ops, scan_inputs(T, N, H, DT[dtype], seed=T, reset=True, lengths=N > 1))
+
+
 @pytest.mark.parametrize("T,N,H", [(600, 1, 64), (20, 2, 32)])
 def test_scan_slow_gates(ops, T, N, H):
     """Gates that keep nearly everything: errors must not grow beyond the bound that follows them."""
@@ -568,3 +583,16 @@ def test_refusals_of_the_c_entries(ops, seq):
     assert lib.wm_seq_last_error(h)
     assert lib.wm_seq_layer_norm(h, 0, 1, 8, p, 8, None, None, 0.1, p, 8, None, None, None) == 0
     assert lib.wm_seq_last_error(h) == b""
+
+
+def test_wait_gives_up(seq):
+    """A wait that nothing completes ends by its limit, is reported once, and leaves the handle usable."""
+    ops = seq.SequenceOps()
+    s = scan_inputs(3000, 1, 64, torch.float32, seed=1)
+    ops.inject_wait_timeout(1000)
+    run_scan(ops, s)
+    with pytest.raises(seq.WMError) as e:
+        ops.sync()
+    assert e.value.status == 4
+    ops.sync()
+    check_scan(ops, s)
