@@ -91,6 +91,34 @@ template <class T, int VEC>
 __device__ __forceinline__ seq_vec<T, VEC> seq_load(const T *p) {
     return *reinterpret_cast<const seq_vec<T, VEC> *>(p);
 }
+// The values of a vector as floats, and back; bf16 in pairs (one instruction a value, or two values).
+template <class T, int VEC>
+__device__ __forceinline__ void seq_unpack(const seq_vec<T, VEC> &v, float (&f)[VEC]) {
+    if constexpr (sizeof(T) == 2 && VEC % 2 == 0) {
+        const uint32_t *w = reinterpret_cast<const uint32_t *>(&v);
+#pragma unroll
+        for (int k = 0; k < VEC / 2; ++k) {
+            f[2 * k] = __uint_as_float(w[k] << 16);
+            f[2 * k + 1] = __uint_as_float(w[k] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) f[k] = seq_to_float(v.v[k]);
+    }
+}
+template <class T, int VEC>
+__device__ __forceinline__ seq_vec<T, VEC> seq_pack(const float (&f)[VEC]) {
+    seq_vec<T, VEC> v;
+    if constexpr (sizeof(T) == 2 && VEC % 2 == 0) {
+        __nv_bfloat162 *w = reinterpret_cast<__nv_bfloat162 *>(&v);
+#pragma unroll
+        for (int k = 0; k < VEC / 2; ++k) w[k] = __floats2bfloat162_rn(f[2 * k], f[2 * k + 1]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < VEC; ++k) v.v[k] = seq_from_float<T>(f[k]);
+    }
+    return v;
+}
 template <class T, int VEC>
 __device__ __forceinline__ void seq_store(T *p, const seq_vec<T, VEC> &v) {
     *reinterpret_cast<seq_vec<T, VEC> *>(p) = v;

@@ -6,8 +6,9 @@
 //
 // Both are st -> A st + B per step (A = keep; B = write x, or keep dh), so a span of steps is
 // st -> P st + S with P the product of its keeps and S its result from 0.  A span that holds a
-// reset ignores what enters it, whatever that is: P = SEQ_CUT, and the state is selected, not
-// multiplied by 0 (which would keep an inf or NaN).  States, P and S are fp32.
+// reset ignores what enters it, whatever that is: its P carries a minus sign, which products
+// with keeps leave there, and the state is selected, not multiplied by 0 (which would keep an
+// inf or NaN).  States, P and S are fp32.
 //
 // Bound by memory: forward reads gate and x and writes h (6 bytes a value in bf16, about 15
 // instructions), backward reads gate, x, h and dh and writes two gradients (12 bytes).  Three
@@ -26,7 +27,6 @@
 
 namespace {
 
-constexpr float SEQ_CUT = -1.f;  // P of a span with a reset inside (products of keeps are >= 0)
 constexpr int kThreads = 128;
 
 template <class T>
@@ -66,29 +66,36 @@ __device__ __forceinline__ long long live_steps(const int32_t *lengths, int n, l
 template <class T, int VEC>
 __device__ __forceinline__ seq_vec<T, VEC> step_fwd(const seq_vec<T, VEC> &g, const seq_vec<T, VEC> &x, bool cut,
                                                     float (&st)[VEC]) {
-    seq_vec<T, VEC> o;
+    float fg[VEC], fx[VEC];
+    seq_unpack(g, fg);
+    seq_unpack(x, fx);
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
         float keep, write;
-        gates<T>(seq_to_float(g.v[k]), keep, write);
-        st[k] = fmaf(keep, cut ? 0.f : st[k], write * seq_to_float(x.v[k]));
-        o.v[k] = seq_from_float<T>(st[k]);
+        gates<T>(fg[k], keep, write);
+        st[k] = fmaf(keep, cut ? 0.f : st[k], write * fx[k]);
     }
-    return o;
+    return seq_pack<T, VEC>(st);
 }
 template <class T, int VEC>
 __device__ __forceinline__ void step_bwd(const seq_vec<T, VEC> &g, const seq_vec<T, VEC> &x, const seq_vec<T, VEC> &dh,
                                          const float (&before)[VEC], bool cut, float (&c)[VEC], seq_vec<T, VEC> &dgate,
                                          seq_vec<T, VEC> &dx) {
+    float fg[VEC], fx[VEC], fd[VEC];
+    seq_unpack(g, fg);
+    seq_unpack(x, fx);
+    seq_unpack(dh, fd);
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
         float keep, write;
-        gates<T>(seq_to_float(g.v[k]), keep, write);
-        const float L = seq_to_float(dh.v[k]) + c[k];
-        dgate.v[k] = seq_from_float<T>(L * ((cut ? 0.f : before[k]) - seq_to_float(x.v[k])) * keep * write);
-        dx.v[k] = seq_from_float<T>(L * write);
+        gates<T>(fg[k], keep, write);
+        const float L = fd[k] + c[k], lw = L * write;
+        fg[k] = lw * ((cut ? 0.f : before[k]) - fx[k]) * keep;
+        fx[k] = lw;
         c[k] = cut ? 0.f : keep * L;
     }
+    dgate = seq_pack<T, VEC>(fg);
+    dx = seq_pack<T, VEC>(fx);
 }
 
 template <int VEC>
@@ -155,11 +162,8 @@ __global__ void __launch_bounds__(kThreads) k_scan_walk(const ScanParams<T> a) {
                 seq_store(a.h.row(t, n) + j, step_fwd<T, VEC>(vg[u], vx[u], cut[u], st));
             } else {
                 float before[VEC];
-                if (t > 0)
-#pragma unroll
-                    for (int k = 0; k < VEC; ++k) before[k] = seq_to_float(vh[u].v[k]);
-                else
-                    read_state<VEC>(before, a.h_init, c);
+                if (t > 0) seq_unpack(vh[u], before);
+                else read_state<VEC>(before, a.h_init, c);
                 V dgate, dx;
                 step_bwd<T, VEC>(vg[u], vx[u], vd[u], before, cut[u], st, dgate, dx);
                 seq_store(a.dgate.row(t, n) + j, dgate);
@@ -260,13 +264,8 @@ __global__ void __launch_bounds__(kThreads) k_scan_stream(const ScanParams<T> a)
                 o0 += a.h.st;
             } else {
                 float before[VEC];
-                if (i + u + 1 < live) {
-                    const V vh = r[3 * kThreads];
-#pragma unroll
-                    for (int k = 0; k < VEC; ++k) before[k] = seq_to_float(vh.v[k]);
-                } else {
-                    read_state<VEC>(before, a.h_init, c);
-                }
+                if (i + u + 1 < live) seq_unpack(r[3 * kThreads], before);
+                else read_state<VEC>(before, a.h_init, c);
                 V dgate, dx;
                 step_bwd<T, VEC>(r[0], r[kThreads], r[2 * kThreads], before, ct, st, dgate, dx);
                 seq_store(o0, dgate);
@@ -291,11 +290,10 @@ __global__ void __launch_bounds__(kThreads) k_scan_stream(const ScanParams<T> a)
 // chunks by a ticket, so a chunk waits only for chunks that are running or done.
 constexpr int kSpanThreads = 256, SUBS = kSpanThreads / 32;
 constexpr unsigned kPolls = 1u << 20;  // a wait's limit: about a second
-constexpr unsigned long long kUnset = ~0ull;
 
 struct SpanWork {
     unsigned *ticket;
-    unsigned long long *chunk_ps, *group_ps;  // [tile][groups][W][32], [tile][sections][W][32]
+    unsigned long long *chunk_ps, *group_ps;  // [tile][groups][32][W], [tile][sections][32][W]
     unsigned long long *section;              // [tile][sections][W]: the state entering it
     int chunks, groups, sections, tiles;      // chunks, groups, sections of a tile; tiles in all
     int tiles_per_n;
@@ -303,7 +301,7 @@ struct SpanWork {
 };
 
 __device__ __forceinline__ void publish(unsigned long long *p, float2 v) {
-    const unsigned x = isnan(v.x) ? 0x7fffffffu : __float_as_uint(v.x);  // (never kUnset)
+    const unsigned x = isnan(v.x) ? 0x7fffffffu : __float_as_uint(v.x);  // (never the ones of an empty place)
     const unsigned long long b = (unsigned long long)__float_as_uint(v.y) << 32 | x;
     asm volatile("st.relaxed.gpu.global.b64 [%0], %1;" ::"l"(p), "l"(b) : "memory");
 }
@@ -317,45 +315,48 @@ __device__ __forceinline__ float2 unpack(unsigned long long b) {
     return make_float2(__uint_as_float((unsigned)b), __uint_as_float((unsigned)(b >> 32)));
 }
 
+// Whether the span holds a reset (the sign of P, also of -0).
+__device__ __forceinline__ bool cuts_off(float p) { return __float_as_int(p) < 0; }
 // Span a, then span b.
 __device__ __forceinline__ float2 join(float2 a, float2 b) {
-    if (b.x < 0.f) return b;
-    return make_float2(a.x < 0.f ? a.x : a.x * b.x, fmaf(b.x, a.y, b.y));
+    return cuts_off(b.x) ? b : make_float2(a.x * b.x, fmaf(b.x, a.y, b.y));
 }
 // The state after a span.
-__device__ __forceinline__ float through(float2 ps, float st) { return ps.x < 0.f ? ps.y : fmaf(ps.x, st, ps.y); }
+__device__ __forceinline__ float through(float2 ps, float st) { return cuts_off(ps.x) ? ps.y : fmaf(ps.x, st, ps.y); }
 
-// Lanes' spans joined in lane order; lane 0 has the result.
-__device__ __forceinline__ float2 join_lanes(float2 v) {
+// Joins spans [0, count) of this thread's at p, p + stride, ...: polls each until it is there.
+// Bounded: the first wait that gives up says so in status[1], which the others look at now and
+// then, and the value counts as a span of nothing.
+template <int MOST>
+__device__ __forceinline__ float2 join_published(const unsigned long long *p, int stride, int count, int *status) {
+    unsigned long long b[MOST];
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const float2 w = make_float2(__shfl_down_sync(0xffffffffu, v.x, o), __shfl_down_sync(0xffffffffu, v.y, o));
-        v = join(v, w);
+    for (int q = 0; q < MOST; ++q) b[q] = q < count ? peek(p + q * stride) : 0;
+    float2 v = make_float2(1.f, 0.f);
+    unsigned polls = 0;
+#pragma unroll
+    for (int q = 0; q < MOST; ++q) {
+        if (q >= count) break;
+        while (!is_set(b[q])) {
+            ++polls;
+            if (polls >= kPolls || (polls % 8192 == 0 && *(volatile int *)(status + 1))) {
+                seq_record(status + 1, WM_ERR_TIMEOUT);
+                b[q] = 0x3f800000ull;
+                break;
+            }
+            b[q] = peek(p + q * stride);
+        }
+        v = join(v, unpack(b[q]));
     }
     return v;
 }
 
-// Polls until every lane's value is there.  Bounded: the first wait that gives up says so in
-// status[1], which the others look at now and then, and the value counts as a span of nothing.
-__device__ __forceinline__ float2 wait_for(unsigned long long b, const unsigned long long *p, bool want, int *status) {
-    unsigned polls = 0;
-    while (!__all_sync(0xffffffffu, !want || is_set(b))) {
-        ++polls;
-        if (polls == kPolls || (polls % 8192 == 0 && *(volatile int *)(status + 1))) {
-            if (threadIdx.x % 32 == 0) seq_record(status + 1, WM_ERR_TIMEOUT);
-            break;
-        }
-        if (want) b = peek(p);
-    }
-    return want && is_set(b) ? unpack(b) : make_float2(1.f, 0.f);
-}
-
-// SPANS > 1 chunk per tile: DEEP.  Logical step i is t = i, or T - 1 - i backward.
+// DEEP: more than one chunk per tile.  Logical step i is t = i, or T - 1 - i backward.
 template <class T, int VEC, int L, bool BWD, bool RESET, bool DEEP>
 __global__ void __launch_bounds__(kSpanThreads, 2) k_scan_spans(const ScanParams<T> a, const SpanWork wk) {
     using V = seq_vec<T, VEC>;
-    constexpr int W = 32 * VEC, PER_WARP = W / SUBS;
-    __shared__ float2 spans[SUBS][W], whole[W];
+    constexpr int W = 32 * VEC, PARTS = kSpanThreads / W, EACH = 32 / PARTS;
+    __shared__ float2 spans[SUBS][W], near[DEEP ? PARTS : 1][W], far[DEEP ? PARTS : 1][W];
     __shared__ float enter[W];
     __shared__ unsigned s_ticket;
     unsigned ticket = blockIdx.x;
@@ -372,12 +373,19 @@ __global__ void __launch_bounds__(kSpanThreads, 2) k_scan_spans(const ScanParams
     const long long live = live_steps(a.lengths, n, T_, a.status);
     const long long i0 = ((long long)chunk * SUBS + sub) * L, t0 = BWD ? T_ - 1 - i0 : i0;
     const int dir = BWD ? -1 : 1;
+    // the span's steps u in [0, steps) exist, and those in [skip, count) are not padding
+    const int steps = (int)max(0ll, min((long long)L, T_ - i0));
+    const int skip = BWD ? (int)max(0ll, min((long long)L, t0 - live + 1)) : 0;
+    const int count = BWD ? steps : (int)max(0ll, min((long long)L, live - i0));
 
     // per step: A and B, and what the second pass takes besides
     float A[L][VEC], B[L][VEC], wr[BWD ? L : 1][VEC], df[BWD ? L : 1][VEC];
-    float2 ps[VEC];
+    float P[VEC], S[VEC];
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) ps[k] = make_float2(1.f, 0.f);
+    for (int k = 0; k < VEC; ++k) {
+        P[k] = 1.f;
+        S[k] = 0.f;
+    }
     unsigned cuts = 0;
     {
         V rg[L], rx[L], rd[BWD ? L : 1], rh[BWD ? L : 1];
@@ -385,12 +393,11 @@ __global__ void __launch_bounds__(kSpanThreads, 2) k_scan_spans(const ScanParams
         const T *pd = BWD ? a.dh.row(t0, n) + j : nullptr, *ph = BWD ? a.h_in.row(t0 - 1, n) + j : nullptr;
 #pragma unroll
         for (int u = 0; u < L; ++u) {
-            const long long t = BWD ? t0 - u : t0 + u;
-            if (mine && t >= 0 && t < live) {
+            if (mine && u >= skip && u < count) {
                 rg[u] = seq_load<T, VEC>(pg);
                 rx[u] = seq_load<T, VEC>(px);
                 if (BWD) rd[u] = seq_load<T, VEC>(pd);
-                if (BWD && t > 0) rh[u] = seq_load<T, VEC>(ph);
+                if (BWD && t0 > u) rh[u] = seq_load<T, VEC>(ph);
             }
             pg += dir * a.gate.st;
             px += dir * a.x.st;
@@ -399,131 +406,128 @@ __global__ void __launch_bounds__(kSpanThreads, 2) k_scan_spans(const ScanParams
                 ph -= a.h_in.st;
             }
         }
-        if (RESET) {  // lane u has step u's
-            const long long t = BWD ? t0 - lane : t0 + lane;
-            cuts = __ballot_sync(0xffffffffu, lane < L && t >= 0 && t < live && a.reset[t * a.N + n] != 0);
-        }
+        if (RESET)  // lane u has step u's
+            cuts = __ballot_sync(0xffffffffu, lane >= skip && lane < count && a.reset[(t0 + dir * lane) * a.N + n] != 0);
 #pragma unroll
         for (int u = 0; u < L; ++u) {
-            const long long t = BWD ? t0 - u : t0 + u;
-            const bool in = mine && t >= 0 && t < live, cut = RESET && (cuts >> u & 1);
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                float keep = 1.f, write = 0.f;
-                if (in) gates<T>(seq_to_float(rg[u].v[k]), keep, write);
-                if (!BWD) {
-                    B[u][k] = in ? write * seq_to_float(rx[u].v[k]) : 0.f;
-                } else {
-                    float before = 0.f;
-                    if (in && !cut) before = t > 0 ? seq_to_float(rh[u].v[k]) : a.h_init ? a.h_init[c + k] : 0.f;
-                    B[u][k] = in ? seq_to_float(rd[u].v[k]) : 0.f;
-                    wr[u][k] = write;
-                    df[u][k] = in ? (before - seq_to_float(rx[u].v[k])) * keep * write : 0.f;
+            const bool cut = RESET && (cuts >> u & 1);
+            if (mine && u >= skip && u < count) {
+                float g[VEC], x[VEC], d[VEC], hb[VEC];
+                seq_unpack(rg[u], g);
+                seq_unpack(rx[u], x);
+                if (BWD) {
+                    seq_unpack(rd[u], d);
+                    if (t0 > u) seq_unpack(rh[u], hb);
+                    else read_state<VEC>(hb, a.h_init, c);
                 }
-                A[u][k] = keep;
-                if (RESET && cut) {
-                    ps[k] = make_float2(SEQ_CUT, BWD ? 0.f : B[u][k]);
-                    if (!BWD) A[u][k] = SEQ_CUT;
-                } else {
-                    if (!RESET || ps[k].x >= 0.f) ps[k].x *= keep;
-                    ps[k].y = BWD ? keep * (B[u][k] + ps[k].y) : fmaf(keep, ps[k].y, B[u][k]);
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) {
+                    float keep, write;
+                    gates<T>(g[k], keep, write);
+                    A[u][k] = keep;
+                    if (!BWD) {
+                        B[u][k] = write * x[k];
+                        S[k] = fmaf(keep, cut ? 0.f : S[k], B[u][k]);
+                    } else {
+                        B[u][k] = d[k];
+                        wr[u][k] = write;
+                        df[u][k] = ((cut ? 0.f : hb[k]) - x[k]) * keep;  // times dx gives dgate
+                        S[k] = cut ? 0.f : keep * (d[k] + S[k]);
+                    }
+                    P[k] = cut ? -1.f : P[k] * keep;
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) {
+                    A[u][k] = 1.f;
+                    B[u][k] = 0.f;
+                    if (BWD) wr[u][k] = df[u][k] = 0.f;
                 }
             }
         }
     }
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) spans[sub][lane * VEC + k] = ps[k];
+    for (int k = 0; k < VEC; ++k) spans[sub][lane * VEC + k] = make_float2(P[k], S[k]);
     __syncthreads();
-    float2 before[VEC];  // the chunk's spans before this one
+    // a thread per channel and part from here on
+    const int ch = threadIdx.x % W, part = threadIdx.x / W;
+    const int group = chunk >> 5, in_group = chunk & 31, section = group >> 5, in_section = group & 31;
+    const bool more = chunk + 1 < wk.chunks;
+    float2 own = make_float2(1.f, 0.f);
+    if (part == 0) {
+        own = spans[0][ch];
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) {
-        float2 v[SUBS];
-#pragma unroll
-        for (int q = 0; q < SUBS; ++q) v[q] = spans[q][lane * VEC + k];
-        float2 all = v[0];
-        before[k] = make_float2(1.f, 0.f);
-#pragma unroll
-        for (int q = 1; q < SUBS; ++q) {
-            if (q == sub) before[k] = all;
-            all = join(all, v[q]);
-        }
-        if (sub == 0) whole[lane * VEC + k] = all;
+        for (int q = 1; q < SUBS; ++q) own = join(own, spans[q][ch]);
     }
-    __syncthreads();
-    // the state entering the chunk, PER_WARP channels a warp
-    {
-        const int group = chunk >> 5, in_group = chunk & 31, section = group >> 5, in_section = group & 31;
-        const int ch0 = sub * PER_WARP;
-        unsigned long long *cp = DEEP ? wk.chunk_ps + (((long long)tile * wk.groups + group) * W + ch0) * 32 : nullptr;
-        unsigned long long *gp = DEEP ? wk.group_ps + (((long long)tile * wk.sections + section) * W + ch0) * 32 : nullptr;
-        unsigned long long *sp = DEEP ? wk.section + ((long long)tile * wk.sections + section) * W + ch0 : nullptr;
-        const bool more = chunk + 1 < wk.chunks;
-        if (DEEP && more && lane < PER_WARP) publish(cp + lane * 32 + in_group, whole[ch0 + lane]);
-        if (DEEP && wk.test_wait && ticket == 0 && sub == 0) {
+    if (DEEP) {
+        unsigned long long *cp = wk.chunk_ps + ((long long)tile * wk.groups + group) * 32 * W + ch;
+        unsigned long long *gp = wk.group_ps + ((long long)tile * wk.sections + section) * 32 * W + ch;
+        unsigned long long *sp = wk.section + ((long long)tile * wk.sections + section) * W + ch;
+        if (more && part == 0) publish(cp + in_group * W, own);
+        if (wk.test_wait && ticket == 0 && threadIdx.x == 0) {
             unsigned left = wk.test_wait;
             while (!is_set(peek(sp)) && left-- > 0) {}  // (nothing enters the first section)
-            if (lane == 0) seq_record(a.status + 1, WM_ERR_TIMEOUT);
+            seq_record(a.status + 1, WM_ERR_TIMEOUT);
         }
-        // the group's chunks before this one; the group's (P, S) goes out before anything else is waited for
-        float2 near[PER_WARP];
-        if (DEEP && in_group) {
-            unsigned long long p[PER_WARP];
+        const int from = part * EACH;
+        near[part][ch] = join_published<EACH>(cp + from * W, W, min(EACH, in_group - from), a.status);
+        if (in_group == 31 && more) {  // the group's (P, S) goes out before anything else is waited for
+            __syncthreads();
+            if (part == 0) {
+                float2 v = near[0][ch];
 #pragma unroll
-            for (int q = 0; q < PER_WARP; ++q) p[q] = lane < in_group ? peek(cp + q * 32 + lane) : 0;
-#pragma unroll
-            for (int q = 0; q < PER_WARP; ++q) {
-                near[q] = join_lanes(wait_for(p[q], cp + q * 32 + lane, lane < in_group, a.status));
-                if (in_group == 31 && more && lane == 0) publish(gp + q * 32 + in_section, join(near[q], whole[ch0 + q]));
-            }
-        }
-#pragma unroll
-        for (int q = 0; q < PER_WARP; ++q) {
-            const int ch = ch0 + q;
-            float st = 0.f;
-            if (!DEEP || section == 0) {
-                if (j0 + ch < a.H && a.h0) st = a.h0[(long long)n * a.H + j0 + ch];
-            } else {
-                st = wait_for(peek(sp + q), sp + q, true, a.status).y;
-            }
-            if (DEEP && in_section) {
-                const unsigned long long *p = gp + q * 32 + lane;
-                st = through(join_lanes(wait_for(lane < in_section ? peek(p) : 0, p, lane < in_section, a.status)), st);
-            }
-            if (DEEP && in_group) st = through(near[q], st);
-            if (lane == 0) {
-                enter[ch] = st;
-                st = through(whole[ch], st);
-                if (DEEP && more && (chunk & 1023) == 1023) publish(sp + W + q, make_float2(0.f, st));
-                if (!more && a.last && j0 + ch < a.H) a.last[(long long)n * a.H + j0 + ch] = st;
+                for (int q = 1; q < PARTS; ++q) v = join(v, near[q][ch]);
+                publish(gp + in_section * W, join(v, own));
             }
         }
+        far[part][ch] = join_published<EACH>(gp + from * W, W, min(EACH, in_section - from), a.status);
+        __syncthreads();
+        if (part == 0) {
+            float st;
+            if (section == 0) st = j0 + ch < a.H && a.h0 ? a.h0[(long long)n * a.H + j0 + ch] : 0.f;
+            else st = join_published<1>(sp, 0, 1, a.status).y;
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) st = through(far[q][ch], st);
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) st = through(near[q][ch], st);
+            enter[ch] = st;
+            st = through(own, st);
+            if (more && (chunk & 1023) == 1023) publish(sp + W, make_float2(0.f, st));
+            if (!more && a.last && j0 + ch < a.H) a.last[(long long)n * a.H + j0 + ch] = st;
+        }
+    } else if (part == 0) {
+        const float st = j0 + ch < a.H && a.h0 ? a.h0[(long long)n * a.H + j0 + ch] : 0.f;
+        enter[ch] = st;
+        if (a.last && j0 + ch < a.H) a.last[(long long)n * a.H + j0 + ch] = through(own, st);
     }
     __syncthreads();
     // the outputs, from the state entering the span
     float mid[VEC];
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) mid[k] = sub ? through(before[k], enter[lane * VEC + k]) : enter[lane * VEC + k];
+    for (int k = 0; k < VEC; ++k) {
+        mid[k] = enter[lane * VEC + k];
+        for (int q = 0; q < sub; ++q) mid[k] = through(spans[q][lane * VEC + k], mid[k]);
+    }
     T *o0 = (BWD ? a.dgate.row(t0, n) : a.h.row(t0, n)) + j, *o1 = BWD ? a.dx.row(t0, n) + j : nullptr;
 #pragma unroll
     for (int u = 0; u < L; ++u) {
-        const long long t = BWD ? t0 - u : t0 + u;
-        const bool in = t < live, cut = RESET && (cuts >> u & 1);
-        V out0, out1;
+        const bool cut = RESET && (cuts >> u & 1);
+        float f0[VEC], f1[VEC];
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
             if (!BWD) {
-                mid[k] = RESET && A[u][k] < 0.f ? B[u][k] : fmaf(A[u][k], mid[k], B[u][k]);
-                out0.v[k] = seq_from_float<T>(in ? mid[k] : 0.f);
+                mid[k] = fmaf(A[u][k], cut ? 0.f : mid[k], B[u][k]);
+                f0[k] = u < count ? mid[k] : 0.f;
             } else {
                 const float dL = B[u][k] + mid[k];
-                out0.v[k] = seq_from_float<T>(in ? dL * df[u][k] : 0.f);
-                out1.v[k] = seq_from_float<T>(in ? dL * wr[u][k] : 0.f);
+                f1[k] = u >= skip ? dL * wr[u][k] : 0.f;
+                f0[k] = u >= skip ? dL * wr[u][k] * df[u][k] : 0.f;
                 mid[k] = cut ? 0.f : A[u][k] * dL;
             }
         }
-        if (mine && t >= 0 && t < T_) {
-            seq_store(o0, out0);
-            if (BWD) seq_store(o1, out1);
+        if (mine && u < steps) {
+            seq_store(o0, seq_pack<T, VEC>(f0));
+            if (BWD) seq_store(o1, seq_pack<T, VEC>(f1));
         }
         o0 += dir * (BWD ? a.dgate.st : a.h.st);
         if (BWD) o1 -= a.dx.st;
@@ -621,14 +625,13 @@ Plan plan(const wm_seq *h, const seq_scan_args &a, bool bwd) {
         p.kind = Plan::STREAM;
     } else {
         p.kind = Plan::SPANS;
-        if (p.vec > w4) p.vec = w4;
         const int W = 32 * p.vec;
         SpanWork &k = p.wk;
         k.tiles_per_n = (a.H + W - 1) / W;
         k.tiles = a.N * k.tiles_per_n;
-        // spans of 16 values a thread (backward 8); of 4 when the longer ones leave SMs idle
-        p.len = (bwd ? 8 : 16);
-        if ((a.T + SUBS * p.len - 1) / (SUBS * p.len) * k.tiles < h->sms) p.len = 4;
+        // spans of 32 values a thread (backward 16); a quarter of that when the longer ones leave SMs idle
+        p.len = (bwd ? 16 : 32) / p.vec;
+        if ((a.T + SUBS * p.len - 1) / (SUBS * p.len) * k.tiles < h->sms) p.len /= 4;
         k.chunks = (int)((a.T + SUBS * p.len - 1) / (SUBS * p.len));
         k.groups = (k.chunks + 31) / 32;
         k.sections = (k.groups + 31) / 32;
@@ -665,13 +668,20 @@ cudaError_t spans(wm_seq *h, const seq_scan_args &a, const Plan &p, cudaStream_t
 
 template <class T, bool BWD>
 cudaError_t dispatch(wm_seq *h, const seq_scan_args &a, cudaStream_t s) {
-    constexpr int W4 = 4 / sizeof(T), LONG = BWD ? 8 : 16;
+    constexpr int W4 = 4 / sizeof(T);
     const Plan p = plan(h, a, BWD);
     if (p.kind == Plan::WALK)
         return p.vec == 2 * W4 ? walk<T, 2 * W4, BWD>(h, a, s) : p.vec == W4 ? walk<T, W4, BWD>(h, a, s) : walk<T, 1, BWD>(h, a, s);
     if (p.kind == Plan::STREAM) return p.vec == 2 * W4 ? stream<T, 2 * W4, BWD>(h, a, s) : stream<T, W4, BWD>(h, a, s);
-    if (p.vec == W4) return p.len == 4 ? spans<T, W4, 4, BWD>(h, a, p, s) : spans<T, W4, LONG, BWD>(h, a, p, s);
-    return p.len == 4 ? spans<T, 1, 4, BWD>(h, a, p, s) : spans<T, 1, LONG, BWD>(h, a, p, s);
+    constexpr int LONG = BWD ? 16 : 32;
+    auto go = [&](auto vec) {
+        constexpr int VEC = decltype(vec)::value;
+        return p.len == LONG / VEC ? spans<T, VEC, LONG / VEC, BWD>(h, a, p, s) : spans<T, VEC, LONG / VEC / 4, BWD>(h, a, p, s);
+    };
+    if (p.vec == 2 * W4) return go(std::integral_constant<int, 2 * W4>{});
+    if constexpr (W4 == 2)
+        if (p.vec == 2) return go(std::integral_constant<int, 2>{});
+    return go(std::integral_constant<int, 1>{});
 }
 
 }  // namespace
