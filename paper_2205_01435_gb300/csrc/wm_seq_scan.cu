@@ -324,32 +324,36 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
 // The state after a span.
 __device__ __forceinline__ float through(float2 ps, float st) { return cuts_off(ps.x) ? ps.y : fmaf(ps.x, st, ps.y); }
 
-// Joins spans [0, count) of this thread's at p, p + stride, ...: polls each until it is there.
-// Bounded: the first wait that gives up says so in status[1], which the others look at now and
-// then, and the value counts as a span of nothing.
+// Up to MOST published spans of this thread's channel: `ask` issues the reads, `join` waits for
+// what was not there yet and joins them.  Bounded: the first wait that gives up says so in
+// status[1], which the others look at now and then, and the value counts as a span of nothing.
 template <int MOST>
-__device__ __forceinline__ float2 join_published(const unsigned long long *p, int stride, int count, int *status) {
+struct Published {
     unsigned long long b[MOST];
+    __device__ __forceinline__ void ask(const unsigned long long *p, int stride, int count) {
 #pragma unroll
-    for (int q = 0; q < MOST; ++q) b[q] = q < count ? peek(p + q * stride) : 0;
-    float2 v = make_float2(1.f, 0.f);
-    unsigned polls = 0;
-#pragma unroll
-    for (int q = 0; q < MOST; ++q) {
-        if (q >= count) break;
-        while (!is_set(b[q])) {
-            ++polls;
-            if (polls >= kPolls || (polls % 8192 == 0 && *(volatile int *)(status + 1))) {
-                seq_record(status + 1, WM_ERR_TIMEOUT);
-                b[q] = 0x3f800000ull;
-                break;
-            }
-            b[q] = peek(p + q * stride);
-        }
-        v = join(v, unpack(b[q]));
+        for (int q = 0; q < MOST; ++q) b[q] = q < count ? peek(p + q * stride) : 0;
     }
-    return v;
-}
+    __device__ __forceinline__ float2 joined(const unsigned long long *p, int stride, int count, int *status) {
+        float2 v = make_float2(1.f, 0.f);
+        unsigned polls = 0;
+#pragma unroll
+        for (int q = 0; q < MOST; ++q) {
+            if (q >= count) break;
+            while (!is_set(b[q])) {
+                ++polls;
+                if (polls >= kPolls || (polls % 8192 == 0 && *(volatile int *)(status + 1))) {
+                    seq_record(status + 1, WM_ERR_TIMEOUT);
+                    b[q] = 0x3f800000ull;
+                    break;
+                }
+                b[q] = peek(p + q * stride);
+            }
+            v = join(v, unpack(b[q]));
+        }
+        return v;
+    }
+};
 
 // DEEP: more than one chunk per tile.  Logical step i is t = i, or T - 1 - i backward.
 template <class T, int VEC, int L, bool BWD, bool RESET, bool DEEP>
@@ -379,7 +383,8 @@ __global__ void __launch_bounds__(kSpanThreads, 2) k_scan_spans(const ScanParams
     const int count = BWD ? steps : (int)max(0ll, min((long long)L, live - i0));
 
     // per step: A and B, and what the second pass takes besides
-    float A[L][VEC], B[L][VEC], wr[BWD ? L : 1][VEC], df[BWD ? L : 1][VEC];
+    float A[L][VEC], B[BWD ? 1 : L][VEC], wr[BWD ? L : 1][VEC], df[BWD ? L : 1][VEC];
+    V rd[BWD ? L : 1];  // backward: B is dh, as it came
     float P[VEC], S[VEC];
 #pragma unroll
     for (int k = 0; k < VEC; ++k) {
@@ -388,7 +393,7 @@ __global__ void __launch_bounds__(kSpanThreads, 2) k_scan_spans(const ScanParams
     }
     unsigned cuts = 0;
     {
-        V rg[L], rx[L], rd[BWD ? L : 1], rh[BWD ? L : 1];
+        V rg[L], rx[L], rh[BWD ? L : 1];
         const T *pg = a.gate.row(t0, n) + j, *px = a.x.row(t0, n) + j;
         const T *pd = BWD ? a.dh.row(t0, n) + j : nullptr, *ph = BWD ? a.h_in.row(t0 - 1, n) + j : nullptr;
 #pragma unroll
@@ -429,7 +434,6 @@ __global__ void __launch_bounds__(kSpanThreads, 2) k_scan_spans(const ScanParams
                         B[u][k] = write * x[k];
                         S[k] = fmaf(keep, cut ? 0.f : S[k], B[u][k]);
                     } else {
-                        B[u][k] = d[k];
                         wr[u][k] = write;
                         df[u][k] = ((cut ? 0.f : hb[k]) - x[k]) * keep;  // times dx gives dgate
                         S[k] = cut ? 0.f : keep * (d[k] + S[k]);
@@ -440,8 +444,12 @@ __global__ void __launch_bounds__(kSpanThreads, 2) k_scan_spans(const ScanParams
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) {
                     A[u][k] = 1.f;
-                    B[u][k] = 0.f;
-                    if (BWD) wr[u][k] = df[u][k] = 0.f;
+                    if (BWD) {
+                        wr[u][k] = df[u][k] = 0.f;
+                        rd[u].v[k] = seq_from_float<T>(0.f);
+                    } else {
+                        B[u][k] = 0.f;
+                    }
                 }
             }
         }
@@ -469,8 +477,17 @@ __global__ void __launch_bounds__(kSpanThreads, 2) k_scan_spans(const ScanParams
             while (!is_set(peek(sp)) && left-- > 0) {}  // (nothing enters the first section)
             seq_record(a.status + 1, WM_ERR_TIMEOUT);
         }
-        const int from = part * EACH;
-        near[part][ch] = join_published<EACH>(cp + from * W, W, min(EACH, in_group - from), a.status);
+        const int from = part * EACH, n_near = min(EACH, in_group - from), n_far = min(EACH, in_section - from);
+        Published<EACH> pub;
+        pub.ask(cp + from * W, W, n_near);
+        unsigned long long s0 = 0;
+        float st = 0.f;
+        if (part == 0) {
+            if (section > 0) s0 = peek(sp);
+            else if (j0 + ch < a.H && a.h0) st = a.h0[(long long)n * a.H + j0 + ch];
+        }
+        near[part][ch] = pub.joined(cp + from * W, W, n_near, a.status);
+        pub.ask(gp + from * W, W, n_far);
         if (in_group == 31 && more) {  // the group's (P, S) goes out before anything else is waited for
             __syncthreads();
             if (part == 0) {
@@ -480,12 +497,13 @@ __global__ void __launch_bounds__(kSpanThreads, 2) k_scan_spans(const ScanParams
                 publish(gp + in_section * W, join(v, own));
             }
         }
-        far[part][ch] = join_published<EACH>(gp + from * W, W, min(EACH, in_section - from), a.status);
+        far[part][ch] = pub.joined(gp + from * W, W, n_far, a.status);
         __syncthreads();
         if (part == 0) {
-            float st;
-            if (section == 0) st = j0 + ch < a.H && a.h0 ? a.h0[(long long)n * a.H + j0 + ch] : 0.f;
-            else st = join_published<1>(sp, 0, 1, a.status).y;
+            if (section > 0) {
+                Published<1> left{{s0}};
+                st = left.joined(sp, 0, 1, a.status).y;
+            }
 #pragma unroll
             for (int q = 0; q < PARTS; ++q) st = through(far[q][ch], st);
 #pragma unroll
@@ -512,14 +530,15 @@ __global__ void __launch_bounds__(kSpanThreads, 2) k_scan_spans(const ScanParams
 #pragma unroll
     for (int u = 0; u < L; ++u) {
         const bool cut = RESET && (cuts >> u & 1);
-        float f0[VEC], f1[VEC];
+        float f0[VEC], f1[VEC], d[VEC];
+        if (BWD) seq_unpack(rd[u], d);
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
             if (!BWD) {
                 mid[k] = fmaf(A[u][k], cut ? 0.f : mid[k], B[u][k]);
                 f0[k] = u < count ? mid[k] : 0.f;
             } else {
-                const float dL = B[u][k] + mid[k];
+                const float dL = d[k] + mid[k];
                 f1[k] = u >= skip ? dL * wr[u][k] : 0.f;
                 f0[k] = u >= skip ? dL * wr[u][k] * df[u][k] : 0.f;
                 mid[k] = cut ? 0.f : A[u][k] * dL;
@@ -607,6 +626,7 @@ cudaError_t stream(const wm_seq *h, const seq_scan_args &a, cudaStream_t s) {
 
 // What a call does: its kernel, the values per access, the steps per span and the layout of the
 // workspace.
+constexpr int kLenFwd = 16, kLenBwd16 = 12, kLenBwd32 = 12, kLenShort = 4;
 struct Plan {
     enum Kind { WALK, STREAM, SPANS } kind;
     int vec, len;
@@ -625,13 +645,14 @@ Plan plan(const wm_seq *h, const seq_scan_args &a, bool bwd) {
         p.kind = Plan::STREAM;
     } else {
         p.kind = Plan::SPANS;
+        if (p.vec > w4) p.vec = w4;  // rows of 128 bytes: wider tiles have shorter spans for the same registers
         const int W = 32 * p.vec;
         SpanWork &k = p.wk;
         k.tiles_per_n = (a.H + W - 1) / W;
         k.tiles = a.N * k.tiles_per_n;
-        // spans of 32 values a thread (backward 16); a quarter of that when the longer ones leave SMs idle
-        p.len = (bwd ? 16 : 32) / p.vec;
-        if ((a.T + SUBS * p.len - 1) / (SUBS * p.len) * k.tiles < h->sms) p.len /= 4;
+        // the longest spans that the registers hold; short ones when those leave SMs idle
+        p.len = bwd ? (w4 == 2 ? kLenBwd16 : kLenBwd32) : kLenFwd;
+        if ((a.T + SUBS * p.len - 1) / (SUBS * p.len) * k.tiles < h->sms) p.len = kLenShort;
         k.chunks = (int)((a.T + SUBS * p.len - 1) / (SUBS * p.len));
         k.groups = (k.chunks + 31) / 32;
         k.sections = (k.groups + 31) / 32;
@@ -673,15 +694,9 @@ cudaError_t dispatch(wm_seq *h, const seq_scan_args &a, cudaStream_t s) {
     if (p.kind == Plan::WALK)
         return p.vec == 2 * W4 ? walk<T, 2 * W4, BWD>(h, a, s) : p.vec == W4 ? walk<T, W4, BWD>(h, a, s) : walk<T, 1, BWD>(h, a, s);
     if (p.kind == Plan::STREAM) return p.vec == 2 * W4 ? stream<T, 2 * W4, BWD>(h, a, s) : stream<T, W4, BWD>(h, a, s);
-    constexpr int LONG = BWD ? 16 : 32;
-    auto go = [&](auto vec) {
-        constexpr int VEC = decltype(vec)::value;
-        return p.len == LONG / VEC ? spans<T, VEC, LONG / VEC, BWD>(h, a, p, s) : spans<T, VEC, LONG / VEC / 4, BWD>(h, a, p, s);
-    };
-    if (p.vec == 2 * W4) return go(std::integral_constant<int, 2 * W4>{});
-    if constexpr (W4 == 2)
-        if (p.vec == 2) return go(std::integral_constant<int, 2>{});
-    return go(std::integral_constant<int, 1>{});
+    constexpr int LONG = !BWD ? kLenFwd : sizeof(T) == 2 ? kLenBwd16 : kLenBwd32;
+    if (p.vec == W4) return p.len == LONG ? spans<T, W4, LONG, BWD>(h, a, p, s) : spans<T, W4, kLenShort, BWD>(h, a, p, s);
+    return p.len == LONG ? spans<T, 1, LONG, BWD>(h, a, p, s) : spans<T, 1, kLenShort, BWD>(h, a, p, s);
 }
 
 }  // namespace
