@@ -123,4 +123,15 @@ template <class T, int VEC>
 __device__ __forceinline__ void seq_store(T *p, const seq_vec<T, VEC> &v) {
     *reinterpret_cast<seq_vec<T, VEC> *>(p) = v;
 }
+
+// ---- asynchronous copies into a thread's own places of shared memory (4, 8 or 16 bytes) ----
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void *src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
 #endif

@@ -16,31 +16,107 @@ namespace {
 // Rows longer than this many values per thread x threads go through the looping kernels.
 constexpr int kFwdMax = 16384, kBwdMax = 8192;
 
-template <class T, int VEC, int E>
-struct Row {
-    seq_vec<T, VEC> v[E / VEC];
+// A thread holds vectors lane, lane + TPR, ... of its row.  Rows on their way: a ring of RING
+// rows in shared memory, every thread copying and reading its own vectors (no barrier, and no
+// registers held by loads in flight).  bf16 rows that are not aligned to 4 bytes cannot be
+// copied so: their threads load a row when they come to it.
+template <int E>
+constexpr int ring_rows() {  // two rows and more on their way: 24 KB and more an SM in every variant
+    return E == 8 ? 6 : E == 16 ? 4 : 3;
+}
+
+template <class T, int VEC>
+constexpr bool ring_fits() {
+    return VEC * sizeof(T) >= 4;
+}
+
+template <class T, int VEC, int E, int TPR, int ARRAYS, int THREADS>
+struct Rows {
+    using V = seq_vec<T, VEC>;
+    static constexpr bool ASYNC = ring_fits<T, VEC>();
+    static constexpr int RING = ring_rows<E>();
+    V *mine;
+    const T *p[ARRAYS];  // the next row to copy (ASYNC), or to load
+    long long left;      // rows not copied yet
+    int slot = 0;
+    static constexpr size_t bytes() { return ASYNC ? (size_t)RING * ARRAYS * THREADS * E * sizeof(T) : 0; }
+    __device__ __forceinline__ V *place(int s, int a, int i) const { return mine + ((s * ARRAYS + a) * (E / VEC) + i) * THREADS; }
+    __device__ __forceinline__ void issue(int s, const long long (&step)[ARRAYS], int D, int lane) {
+        if (left > 0) {
+#pragma unroll
+            for (int a = 0; a < ARRAYS; ++a) {
+#pragma unroll
+                for (int i = 0; i < E / VEC; ++i) {
+                    const int j = (i * TPR + lane) * VEC;
+                    if (j < D)
+                        copy_async<ASYNC ? (int)sizeof(V) : 4>((uint32_t)__cvta_generic_to_shared(place(s, a, i)), p[a] + j);
+                }
+                p[a] += step[a];
+            }
+        }
+        --left;
+        copy_commit();
+    }
+    __device__ __forceinline__ void start(const long long (&step)[ARRAYS], int D, int lane) {
+        if constexpr (ASYNC)
+#pragma unroll
+            for (int q = 0; q < RING - 1; ++q) issue(q, step, D, lane);
+    }
+    // makes the next row readable
+    __device__ __forceinline__ void arrive(const long long (&step)[ARRAYS], int D, int lane) {
+        if constexpr (ASYNC) {
+            issue(slot == 0 ? RING - 1 : slot - 1, step, D, lane);
+            copy_wait<RING - 1>();
+        }
+    }
+    __device__ __forceinline__ V read(int a, int i, int lane) const {
+        if constexpr (ASYNC) return *place(slot, a, i);
+        else return seq_load<T, VEC>(p[a] + (i * TPR + lane) * VEC);
+    }
+    __device__ __forceinline__ void next(const long long (&step)[ARRAYS]) {
+        if constexpr (ASYNC) {
+            slot = slot + 1 == RING ? 0 : slot + 1;
+        } else {
+#pragma unroll
+            for (int a = 0; a < ARRAYS; ++a) p[a] += step[a];
+        }
+    }
 };
 
-// Lane l of TPR holds vectors l, l + TPR, ... of the row.
-template <class T, int VEC, int E, int TPR>
-__device__ __forceinline__ void load_row(Row<T, VEC, E> &r, const T *p, int D, int lane) {
-#pragma unroll
-    for (int i = 0; i < E / VEC; ++i) {
-        const int j = (i * TPR + lane) * VEC;
-        if (j < D) r.v[i] = seq_load<T, VEC>(p + j);
-    }
+// Rows of 1024 values in one warp: the weights come from shared memory, in the order the lanes
+// read them (they would fill the registers); else they stay in registers.
+template <int E, int TPR>
+constexpr bool shared_weights() {
+    return TPR == 32 && E == 32;
 }
 
 template <int VEC, int E, int TPR>
-__device__ __forceinline__ void load_param(float (&w)[E], const float *p, float fill, int D, int lane) {
+struct Weights {
+    static constexpr bool SHARED = shared_weights<E, TPR>();
+    float r[SHARED ? 1 : E];
+    const float *s;
+    __device__ __forceinline__ void load(const float *p, float fill, int D, int lane, float *smem) {
+        if constexpr (SHARED) {  // [E / 4][32] quads: quad q of lane l holds its values 4q ... 4q + 3
+            for (int o = threadIdx.x; o < 1024; o += blockDim.x) {
+                const int e = o / 128 * 4 + o % 4, l = o / 4 % 32, j = (e / VEC * TPR + l) * VEC + e % VEC;
+                smem[o] = p && j < D ? p[j] : fill;
+            }
+            s = smem + lane * 4;
+        } else {
 #pragma unroll
-    for (int i = 0; i < E / VEC; ++i)
+            for (int i = 0; i < E / VEC; ++i)
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) {
-            const int j = (i * TPR + lane) * VEC + k;
-            w[i * VEC + k] = p && j < D ? p[j] : fill;
+                for (int k = 0; k < VEC; ++k) {
+                    const int j = (i * TPR + lane) * VEC + k;
+                    r[i * VEC + k] = p && j < D ? p[j] : fill;
+                }
         }
-}
+    }
+    __device__ __forceinline__ float operator[](int e) const {
+        if constexpr (SHARED) return s[e / 4 * 128 + e % 4];
+        else return r[e];
+    }
+};
 
 // Sums over the TPR threads of a row; every thread gets the result.  One barrier a call:
 // the buffers alternate, and a thread writes one again only after a barrier that all
@@ -76,38 +152,51 @@ constexpr int cta_threads() {
     return TPR < 128 ? 128 : TPR;
 }
 
+// CTAs of an SM at once: what the registers of the largest variants allow.
+template <int TPR>
+constexpr int fwd_ctas() {
+    return TPR == 32 ? 6 : TPR == 128 ? 4 : TPR == 256 ? 2 : 1;
+}
+template <int TPR>
+constexpr int bwd_ctas() {
+    return TPR == 32 ? 4 : TPR == 128 ? 3 : 1;
+}
+
 template <class T, int VEC, int E, int TPR>
-__global__ void __launch_bounds__(cta_threads<TPR>()) k_norm_fwd(long long rows, int D, const T *__restrict__ x,
-                                                                 long long ldx, const float *__restrict__ w,
-                                                                 const float *__restrict__ b, float eps, T *y,
-                                                                 long long ldy, float *__restrict__ mean,
-                                                                 float *__restrict__ rstd) {
-    constexpr int RPC = cta_threads<TPR>() / TPR;
+__global__ void __launch_bounds__(cta_threads<TPR>(), fwd_ctas<TPR>())
+    k_norm_fwd(long long rows, int D, const T *__restrict__ x, long long ldx, const float *__restrict__ w,
+               const float *__restrict__ b, float eps, T *y, long long ldy, float *__restrict__ mean, float *__restrict__ rstd) {
+    constexpr int THREADS = cta_threads<TPR>(), RPC = THREADS / TPR;
+    constexpr bool SHARED = shared_weights<E, TPR>();
+    extern __shared__ __align__(16) unsigned char ring[];
     __shared__ float2 red[2 * (TPR / 32)];
+    __shared__ __align__(16) float ws[SHARED ? 2 : 1][SHARED ? 1024 : 1];
     RowSum<TPR> sum{red, 0};
     const int lane = threadIdx.x % TPR;
-    const long long step = (long long)gridDim.x * RPC;
+    const long long step = (long long)gridDim.x * RPC, steps[1] = {step * ldx};
     long long r = (long long)blockIdx.x * RPC + threadIdx.x / TPR;
-    if (r >= rows) return;  // TPR > 32: the whole CTA
-    Row<T, VEC, E> next;
-    load_row<T, VEC, E, TPR>(next, x + r * ldx, D, lane);
-    float ww[E], bb[E];
-    load_param<VEC, E, TPR>(ww, w, 1.f, D, lane);
-    load_param<VEC, E, TPR>(bb, b, 0.f, D, lane);
+    Rows<T, VEC, E, TPR, 1, THREADS> in{reinterpret_cast<seq_vec<T, VEC> *>(ring) + threadIdx.x, {x + r * ldx},
+                                        r < rows ? (rows - r + step - 1) / step : 0};
+    in.start(steps, D, lane);
+    Weights<VEC, E, TPR> ww, bb;
+    ww.load(w, 1.f, D, lane, ws[0]);
+    bb.load(b, 0.f, D, lane, ws[SHARED ? 1 : 0]);
+    if (SHARED) __syncthreads();
     const float inv = 1.f / (float)D;
-    for (; r < rows; r += step) {
-        float v[E];
+    T *out = y + r * ldy;
+    for (; r < rows; r += step, out += step * ldy) {
+        in.arrive(steps, D, lane);
+        float v[E / VEC][VEC];
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < E / VEC; ++i) {
-            const bool in = (i * TPR + lane) * VEC < D;
+            if ((i * TPR + lane) * VEC < D) {
+                seq_unpack(in.read(0, i, lane), v[i]);
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                v[i * VEC + k] = in ? seq_to_float(next.v[i].v[k]) : 0.f;
-                s += v[i * VEC + k];
+                for (int k = 0; k < VEC; ++k) s += v[i][k];
             }
         }
-        if (r + step < rows) load_row<T, VEC, E, TPR>(next, x + (r + step) * ldx, D, lane);
+        in.next(steps);
         const float mu = sum(make_float2(s, 0.f)).x * inv;
         float q = 0.f;
 #pragma unroll
@@ -115,8 +204,8 @@ __global__ void __launch_bounds__(cta_threads<TPR>()) k_norm_fwd(long long rows,
             if ((i * TPR + lane) * VEC < D)
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) {
-                    v[i * VEC + k] -= mu;
-                    q = fmaf(v[i * VEC + k], v[i * VEC + k], q);
+                    v[i][k] -= mu;
+                    q = fmaf(v[i][k], v[i][k], q);
                 }
         const float rs = rsqrtf(sum(make_float2(q, 0.f)).x * inv + eps);
         if (mean && lane == 0) {
@@ -126,84 +215,93 @@ __global__ void __launch_bounds__(cta_threads<TPR>()) k_norm_fwd(long long rows,
 #pragma unroll
         for (int i = 0; i < E / VEC; ++i) {
             const int j = (i * TPR + lane) * VEC;
-            if (j >= D) continue;
-            seq_vec<T, VEC> o;
+            if (j < D) {
 #pragma unroll
-            for (int k = 0; k < VEC; ++k)
-                o.v[k] = seq_from_float<T>(fmaf(v[i * VEC + k] * rs, ww[i * VEC + k], bb[i * VEC + k]));
-            seq_store(y + r * ldy + j, o);
+                for (int k = 0; k < VEC; ++k) v[i][k] = fmaf(v[i][k] * rs, ww[i * VEC + k], bb[i * VEC + k]);
+                seq_store(out + j, seq_pack<T, VEC>(v[i]));
+            }
         }
     }
 }
 
 // part: [gridDim.x][2][D] sums of dw and db over the CTA's rows (null: not wanted)
 template <class T, int VEC, int E, int TPR>
-__global__ void __launch_bounds__(cta_threads<TPR>()) k_norm_bwd(long long rows, int D, const T *__restrict__ x,
-                                                                 long long ldx, const float *__restrict__ w,
-                                                                 const float *__restrict__ mean,
-                                                                 const float *__restrict__ rstd, const T *dy,
-                                                                 long long lddy, T *dx, long long lddx,
-                                                                 float *__restrict__ part) {
-    constexpr int RPC = cta_threads<TPR>() / TPR;
+__global__ void __launch_bounds__(cta_threads<TPR>(), bwd_ctas<TPR>())
+    k_norm_bwd(long long rows, int D, const T *__restrict__ x, long long ldx, const float *__restrict__ w,
+               const float *__restrict__ mean, const float *__restrict__ rstd, const T *dy, long long lddy, T *dx, long long lddx,
+               float *__restrict__ part) {
+    constexpr int THREADS = cta_threads<TPR>(), RPC = THREADS / TPR;
+    constexpr bool SHARED = shared_weights<E, TPR>();
+    extern __shared__ __align__(16) unsigned char ring[];  // the rows' ring; after the rows (RPC > 1) sums [RPC][2][D]
     __shared__ float2 red[2 * (TPR / 32)];
-    extern __shared__ float cols[];  // RPC > 1: [RPC][2][D]
+    __shared__ __align__(16) float ws[SHARED ? 1024 : 1];
     RowSum<TPR> sum{red, 0};
     const int lane = threadIdx.x % TPR, sub = threadIdx.x / TPR;
-    const long long step = (long long)gridDim.x * RPC;
-    float ww[E], dw[E], db[E];
-    load_param<VEC, E, TPR>(ww, w, 1.f, D, lane);
-#pragma unroll
-    for (int e = 0; e < E; ++e) dw[e] = db[e] = 0.f;
-    const float inv = 1.f / (float)D;
+    const long long step = (long long)gridDim.x * RPC, steps[2] = {step * ldx, step * lddy};
     long long r = (long long)blockIdx.x * RPC + sub;
-    Row<T, VEC, E> nx, ny;
+    Rows<T, VEC, E, TPR, 2, THREADS> in{reinterpret_cast<seq_vec<T, VEC> *>(ring) + threadIdx.x, {x + r * ldx, dy + r * lddy},
+                                        r < rows ? (rows - r + step - 1) / step : 0};
+    in.start(steps, D, lane);
     float nmu = 0.f, nrs = 0.f;
     if (r < rows) {
-        load_row<T, VEC, E, TPR>(nx, x + r * ldx, D, lane);
-        load_row<T, VEC, E, TPR>(ny, dy + r * lddy, D, lane);
         nmu = mean[r];
         nrs = rstd[r];
     }
-    for (; r < rows; r += step) {
-        const Row<T, VEC, E> cx = nx, cy = ny;
+    Weights<VEC, E, TPR> ww;
+    ww.load(w, 1.f, D, lane, ws);
+    if (SHARED) __syncthreads();
+    float dw[E], db[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) dw[e] = db[e] = 0.f;
+    const float inv = 1.f / (float)D;
+    T *out = dx + r * lddx;
+    for (; r < rows; r += step, out += step * lddx) {
         const float mu = nmu, rs = nrs;
+        in.arrive(steps, D, lane);
         if (r + step < rows) {
-            load_row<T, VEC, E, TPR>(nx, x + (r + step) * ldx, D, lane);
-            load_row<T, VEC, E, TPR>(ny, dy + (r + step) * lddy, D, lane);
             nmu = mean[r + step];
             nrs = rstd[r + step];
         }
         float2 s = make_float2(0.f, 0.f);
 #pragma unroll
         for (int i = 0; i < E / VEC; ++i)
-            if ((i * TPR + lane) * VEC < D)
+            if ((i * TPR + lane) * VEC < D) {
+                float fx[VEC], fd[VEC];
+                seq_unpack(in.read(0, i, lane), fx);
+                seq_unpack(in.read(1, i, lane), fd);
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) {
                     const int e = i * VEC + k;
-                    const float xh = (seq_to_float(cx.v[i].v[k]) - mu) * rs, d = seq_to_float(cy.v[i].v[k]);
-                    dw[e] = fmaf(d, xh, dw[e]);
-                    db[e] += d;
-                    s.x = fmaf(d, ww[e], s.x);
-                    s.y = fmaf(d * ww[e], xh, s.y);
+                    const float xh = (fx[k] - mu) * rs, g = fd[k] * ww[e];
+                    dw[e] = fmaf(fd[k], xh, dw[e]);
+                    db[e] += fd[k];
+                    s.x += g;
+                    s.y = fmaf(g, xh, s.y);
                 }
+            }
         s = sum(s);
         const float m1 = s.x * inv, m2 = s.y * inv;
 #pragma unroll
         for (int i = 0; i < E / VEC; ++i) {
             const int j = (i * TPR + lane) * VEC;
-            if (j >= D) continue;
-            seq_vec<T, VEC> o;
+            if (j < D) {
+                float fx[VEC], fd[VEC];
+                seq_unpack(in.read(0, i, lane), fx);
+                seq_unpack(in.read(1, i, lane), fd);
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                const float xh = (seq_to_float(cx.v[i].v[k]) - mu) * rs;
-                const float g = seq_to_float(cy.v[i].v[k]) * ww[i * VEC + k];
-                o.v[k] = seq_from_float<T>(rs * (g - m1 - xh * m2));
+                for (int k = 0; k < VEC; ++k) {
+                    const float xh = (fx[k] - mu) * rs;
+                    fd[k] = rs * (fmaf(fd[k], ww[i * VEC + k], -m1) - xh * m2);
+                }
+                seq_store(out + j, seq_pack<T, VEC>(fd));
             }
-            seq_store(dx + r * lddx + j, o);
         }
+        in.next(steps);
     }
     if (!part) return;
     part += (long long)blockIdx.x * 2 * D;
+    if (RPC > 1) __syncthreads();  // the ring is done with: the sums take its place
+    float *cols = reinterpret_cast<float *>(ring);
     float *to = RPC > 1 ? cols + sub * 2 * D : part;
 #pragma unroll
     for (int i = 0; i < E / VEC; ++i)
@@ -337,72 +435,84 @@ Shape shape(int D) {
     return {512, 32};
 }
 
-int bwd_ctas(const wm_seq *h, long long rows, int D) {
-    const int rpc = D <= 1024 ? 4 : 1;
-    const long long need = (rows + rpc - 1) / rpc, most = (long long)h->sms * (D > 4096 ? 1 : 3);
+int bwd_grid(const wm_seq *h, long long rows, int D) {
+    const int rpc = D <= 1024 ? 4 : 1, per_sm = D <= 1024 ? bwd_ctas<32>() : D <= 4096 ? bwd_ctas<128>() : bwd_ctas<256>();
+    const long long need = (rows + rpc - 1) / rpc, most = (long long)h->sms * per_sm;
     return (int)(need < most ? need : most);
 }
 
-#define NORM_SHAPES(CALL)                       \
-    if (sh.tpr == 32 && sh.e == 8) CALL(8, 32)  \
-    else if (sh.tpr == 32 && sh.e == 16) CALL(16, 32) \
-    else if (sh.tpr == 32) CALL(32, 32)         \
-    else if (sh.tpr == 128 && sh.e == 16) CALL(16, 128) \
-    else if (sh.tpr == 128) CALL(32, 128)       \
-    else if (sh.tpr == 256) CALL(32, 256)
+// Launches with its dynamic shared memory (above 48 KB a kernel has to be told).
+template <class... P, class... A>
+cudaError_t launch(void (*k)(P...), int grid, int threads, size_t smem, cudaStream_t s, A... args) {
+    if (smem > 40 << 10) {
+        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    k<<<grid, threads, smem, s>>>(args...);
+    return cudaGetLastError();
+}
+
+#define NORM_SHAPES(CALL)                          \
+    if (sh.tpr == 32 && sh.e == 8) CALL(8, 32)     \
+    if (sh.tpr == 32 && sh.e == 16) CALL(16, 32)   \
+    if (sh.tpr == 32) CALL(32, 32)                 \
+    if (sh.tpr == 128 && sh.e == 16) CALL(16, 128) \
+    if (sh.tpr == 128) CALL(32, 128)               \
+    if (sh.tpr == 256) CALL(32, 256)
 
 template <class T, int VEC>
-void fwd(const wm_seq *h, long long rows, int D, const T *x, long long ldx, const float *w, const float *b, float eps,
-         T *y, long long ldy, float *mean, float *rstd, cudaStream_t s) {
+cudaError_t fwd(const wm_seq *h, long long rows, int D, const T *x, long long ldx, const float *w, const float *b, float eps,
+                T *y, long long ldy, float *mean, float *rstd, cudaStream_t s) {
     const Shape sh = shape(D);
-#define CALL(E, TPR)                                                                                                  \
-    {                                                                                                                 \
-        constexpr int rpc = cta_threads<TPR>() / TPR;                                                                 \
-        const long long need = (rows + rpc - 1) / rpc, most = (long long)h->sms * (TPR > 128 ? 4 : 8);                \
-        k_norm_fwd<T, VEC, E, TPR><<<(unsigned)(need < most ? need : most), cta_threads<TPR>(), 0, s>>>(              \
-            rows, D, x, ldx, w, b, eps, y, ldy, mean, rstd);                                                          \
+#define CALL(E, TPR)                                                                                                     \
+    {                                                                                                                    \
+        constexpr int threads = cta_threads<TPR>(), rpc = threads / TPR;                                                 \
+        const long long need = (rows + rpc - 1) / rpc, most = (long long)h->sms * fwd_ctas<TPR>();                       \
+        return launch(k_norm_fwd<T, VEC, E, TPR>, (int)(need < most ? need : most), threads,                             \
+                      Rows<T, VEC, E, TPR, 1, threads>::bytes(), s, rows, D, x, ldx, w, b, eps, y, ldy, mean, rstd);     \
     }
-    NORM_SHAPES(CALL) else CALL(32, 512)
+    NORM_SHAPES(CALL)
+    CALL(32, 512)
 #undef CALL
 }
 
 template <class T, int VEC>
-void bwd(const wm_seq *h, long long rows, int D, const T *x, long long ldx, const float *w, const float *mean,
-         const float *rstd, const T *dy, long long lddy, T *dx, long long lddx, float *part, int ctas, cudaStream_t s) {
+cudaError_t bwd(long long rows, int D, const T *x, long long ldx, const float *w, const float *mean, const float *rstd,
+                const T *dy, long long lddy, T *dx, long long lddx, float *part, int grid, cudaStream_t s) {
     const Shape sh = shape(D);
-#define CALL(E, TPR)                                                                                            \
-    {                                                                                                           \
-        constexpr int rpc = cta_threads<TPR>() / TPR;                                                           \
-        k_norm_bwd<T, VEC, E, TPR><<<ctas, cta_threads<TPR>(), part && rpc > 1 ? (size_t)rpc * 2 * D * 4 : 0, s>>>( \
-            rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part);                                          \
+#define CALL(E, TPR)                                                                                             \
+    {                                                                                                            \
+        constexpr int threads = cta_threads<TPR>(), rpc = threads / TPR;                                         \
+        const size_t ring = Rows<T, VEC, E, TPR, 2, threads>::bytes(), cols = rpc > 1 ? (size_t)rpc * 2 * D * 4 : 0; \
+        return launch(k_norm_bwd<T, VEC, E, TPR>, grid, threads, ring > cols ? ring : cols, s, rows, D, x, ldx,   \
+                      w, mean, rstd, dy, lddy, dx, lddx, part);                                                  \
     }
     NORM_SHAPES(CALL)
 #undef CALL
+    return cudaErrorInvalidValue;  // (rows above kBwdMax take the looping kernel)
 }
 
 template <class T>
-void fwd_any(const wm_seq *h, long long rows, int D, const T *x, long long ldx, const float *w, const float *b,
-             float eps, T *y, long long ldy, float *mean, float *rstd, cudaStream_t s) {
+cudaError_t fwd_any(const wm_seq *h, long long rows, int D, const T *x, long long ldx, const float *w, const float *b,
+                    float eps, T *y, long long ldy, float *mean, float *rstd, cudaStream_t s) {
     if (D > kFwdMax) {
         const long long most = (long long)h->sms * 4;
-        k_norm_fwd_long<T><<<(unsigned)(rows < most ? rows : most), kLong, 0, s>>>(rows, D, x, ldx, w, b, eps, y, ldy, mean, rstd);
-        return;
+        return launch(k_norm_fwd_long<T>, (int)(rows < most ? rows : most), kLong, 0, s, rows, D, x, ldx, w, b, eps, y, ldy, mean,
+                      rstd);
     }
     if (vec_ok(x, ldx, D, sizeof(T)) && vec_ok(y, ldy, D, sizeof(T)))
-        fwd<T, 16 / sizeof(T)>(h, rows, D, x, ldx, w, b, eps, y, ldy, mean, rstd, s);
-    else
-        fwd<T, 1>(h, rows, D, x, ldx, w, b, eps, y, ldy, mean, rstd, s);
+        return fwd<T, 16 / sizeof(T)>(h, rows, D, x, ldx, w, b, eps, y, ldy, mean, rstd, s);
+    return fwd<T, 1>(h, rows, D, x, ldx, w, b, eps, y, ldy, mean, rstd, s);
 }
 
 template <class T>
-void bwd_any(const wm_seq *h, long long rows, int D, const T *x, long long ldx, const float *w, const float *mean,
-             const float *rstd, const T *dy, long long lddy, T *dx, long long lddx, float *part, int ctas, cudaStream_t s) {
+cudaError_t bwd_any(long long rows, int D, const T *x, long long ldx, const float *w, const float *mean, const float *rstd,
+                    const T *dy, long long lddy, T *dx, long long lddx, float *part, int grid, cudaStream_t s) {
     if (D > kBwdMax)
-        k_norm_bwd_long<T><<<ctas, kLong, 0, s>>>(rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part);
-    else if (vec_ok(x, ldx, D, sizeof(T)) && vec_ok(dy, lddy, D, sizeof(T)) && vec_ok(dx, lddx, D, sizeof(T)))
-        bwd<T, 16 / sizeof(T)>(h, rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part, ctas, s);
-    else
-        bwd<T, 1>(h, rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part, ctas, s);
+        return launch(k_norm_bwd_long<T>, grid, kLong, 0, s, rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part);
+    if (vec_ok(x, ldx, D, sizeof(T)) && vec_ok(dy, lddy, D, sizeof(T)) && vec_ok(dx, lddx, D, sizeof(T)))
+        return bwd<T, 16 / sizeof(T)>(rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part, grid, s);
+    return bwd<T, 1>(rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part, grid, s);
 }
 
 }  // namespace
@@ -410,35 +520,34 @@ void bwd_any(const wm_seq *h, long long rows, int D, const T *x, long long ldx, 
 cudaError_t wm_seq_norm_launch(wm_seq *h, int dtype, long long rows, int D, const void *x, long long ldx,
                                const float *w, const float *b, float eps, void *y, long long ldy, float *mean,
                                float *rstd, cudaStream_t s) {
-    if (dtype == WM_BF16)
-        fwd_any(h, rows, D, (const __nv_bfloat16 *)x, ldx, w, b, eps, (__nv_bfloat16 *)y, ldy, mean, rstd, s);
-    else
-        fwd_any(h, rows, D, (const float *)x, ldx, w, b, eps, (float *)y, ldy, mean, rstd, s);
+    using bf16 = __nv_bfloat16;
     h->last_launches = 1;
-    return cudaGetLastError();
+    if (dtype == WM_BF16) return fwd_any(h, rows, D, (const bf16 *)x, ldx, w, b, eps, (bf16 *)y, ldy, mean, rstd, s);
+    return fwd_any(h, rows, D, (const float *)x, ldx, w, b, eps, (float *)y, ldy, mean, rstd, s);
 }
 
 size_t wm_seq_norm_backward_ws(const wm_seq *h, long long rows, int D) {
-    return (size_t)bwd_ctas(h, rows, D) * 2 * D * sizeof(float);
+    return (size_t)bwd_grid(h, rows, D) * 2 * D * sizeof(float);
 }
 
 cudaError_t wm_seq_norm_backward_launch(wm_seq *h, int dtype, long long rows, int D, const void *x, long long ldx,
                                         const float *w, const float *mean, const float *rstd, const void *dy,
                                         long long lddy, void *dx, long long lddx, float *dw, float *db,
                                         cudaStream_t s) {
-    const int ctas = bwd_ctas(h, rows, D);
+    using bf16 = __nv_bfloat16;
+    const int grid = bwd_grid(h, rows, D);
     float *part = dw || db ? (float *)h->ws : nullptr;
     h->last_launches = 0;
-    if (ctas > 0) {
-        if (dtype == WM_BF16)
-            bwd_any(h, rows, D, (const __nv_bfloat16 *)x, ldx, w, mean, rstd, (const __nv_bfloat16 *)dy, lddy,
-                    (__nv_bfloat16 *)dx, lddx, part, ctas, s);
-        else
-            bwd_any(h, rows, D, (const float *)x, ldx, w, mean, rstd, (const float *)dy, lddy, (float *)dx, lddx, part, ctas, s);
+    if (grid > 0) {
+        const cudaError_t e =
+            dtype == WM_BF16
+                ? bwd_any(rows, D, (const bf16 *)x, ldx, w, mean, rstd, (const bf16 *)dy, lddy, (bf16 *)dx, lddx, part, grid, s)
+                : bwd_any(rows, D, (const float *)x, ldx, w, mean, rstd, (const float *)dy, lddy, (float *)dx, lddx, part, grid, s);
+        if (e != cudaSuccess) return e;
         h->last_launches = 1;
     }
     if (dw || db) {  // no rows: zeros
-        k_norm_cols<<<(2 * D + 31) / 32, 512, 0, s>>>(ctas, D, part, dw, db);
+        k_norm_cols<<<(2 * D + 31) / 32, 512, 0, s>>>(grid, D, part, dw, db);
         ++h->last_launches;
     }
     return cudaGetLastError();

@@ -179,16 +179,6 @@ __global__ void __launch_bounds__(kThreads) k_scan_walk(const ScanParams<T> a) {
 // The ring holds GROUPS groups of kGroup steps; a group is one set of asynchronous copies.
 constexpr int kGroup = 2;
 
-template <int BYTES>
-__device__ __forceinline__ void copy_async(uint32_t dst, const void *src) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
-}
-__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void copy_wait() {
-    asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
 template <class T, int VEC, bool BWD, bool RESET, int GROUPS>
 __global__ void __launch_bounds__(kThreads) k_scan_stream(const ScanParams<T> a) {
     using V = seq_vec<T, VEC>;
