@@ -5,12 +5,14 @@
 // Both are bound by memory: the lookup by writing its output, the gradient by reading dout
 // once and writing the table once.  The gradient sorts (token, position) pairs by token,
 // stably, so that a row's terms are neighbours and always come in the order of their
-// positions: no floating-point atomics, the same bits every time.  A warp then sums BLOCK
-// sorted positions over a slice of columns in fp32, whatever tokens they hold, so that a
-// token that fills half of a batch costs no more than tokens that come once.  A run of one
-// token that lies inside a block is written at once; of a run that crosses blocks each block
-// leaves a partial row, and a second launch adds these in order.  Rows that no token took
-// are found by binary search in the sorted tokens and filled with zeros.
+// positions: no floating-point atomics, the same bits every time.  Up to 12,288 tokens a CTA
+// the sort is one launch of one cluster, with the pairs in shared memory; more go through
+// global memory.  A warp then sums a block of sorted positions over a slice of columns in
+// fp32, whatever tokens they hold, so that a token that fills half of a batch costs no more
+// than tokens that come once.  A run of one token that lies inside a block is written at
+// once; of a run that crosses blocks each block leaves a partial row, and a third launch adds
+// these in order.  Rows that no token took (the sort marks those that one did) are filled
+// with zeros by warps of the second.
 #include "wm_seq_internal.h"
 
 namespace {
@@ -53,9 +55,139 @@ __global__ void __launch_bounds__(kLookup) k_embed(long long n, int V, int D, co
     }
 }
 
-// ---- the sort: least significant digit first, 8 bits a pass -----------------------------
-// A pass: every tile's digit counts; their exclusive prefix, digits first; every pair to its
-// place.  Keys are tokens, V for those outside the table (they sort last and are left out).
+// ---- the sort: least significant digit first -----------------------------------------------
+// Keys are tokens, V for those outside the table (they sort last and are left out).
+//
+// In one cluster: CTA r holds places [r * per, (r + 1) * per) of the order in its shared memory.
+// A pass ranks its pairs by digit (warps over contiguous pieces, so ranks follow the places),
+// gives its digit counts to every CTA, and puts every pair to its place of the next order, in
+// whichever CTA that is.
+constexpr int kCluster = 16, kSortThreads = 1024, kPerCta = 12288, kSortItems = kPerCta / kSortThreads;
+constexpr int kMaxDigits = 256;
+
+struct ClusterSort {
+    int n, V, per, passes, bits;  // pairs of a CTA; digit width
+    const int32_t *tokens;
+    int *key, *pos;
+    uint8_t *present;  // [V]
+    int *status;
+};
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t peer(const void *p, uint32_t rank) {
+    uint32_t at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    return at;
+}
+
+__global__ void __launch_bounds__(kSortThreads, 1) k_sort_cluster(const ClusterSort a) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    unsigned long long *order[2] = {reinterpret_cast<unsigned long long *>(smem),
+                                    reinterpret_cast<unsigned long long *>(smem) + a.per};  // pos << 32 | key
+    __shared__ unsigned short cnt[kSortThreads / 32][kMaxDigits];  // pairs of a digit per warp, then before it
+    __shared__ int all[kCluster][kMaxDigits], base[kMaxDigits], scan[8];
+    const int tid = threadIdx.x, lane = tid & 31, w = tid / 32;
+    const int rank = (int)cluster_rank(), ranks = (int)cluster_size();
+    const int lo = rank * a.per, m = max(0, min(a.per, a.n - lo));
+    const int digits = 1 << a.bits;
+    // the sums may be launched now: they wait for this grid's end before they read anything
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    for (int v = rank * kSortThreads + tid; v < a.V; v += ranks * kSortThreads) a.present[v] = 0;
+    for (int i = tid; i < m; i += kSortThreads) {
+        const int t = token_row(a.tokens[lo + i], a.V, a.status);
+        order[0][i] = (unsigned long long)(lo + i) << 32 | (unsigned)(t < 0 ? a.V : t);
+    }
+    cluster_barrier();  // every CTA has started: their shared memory may be written
+    // a warp's piece of the CTA's places
+    const int piece = ((a.per + 31) / 32 + 31) / 32 * 32;
+    for (int pass = 0; pass < a.passes; ++pass) {
+        const unsigned long long *from = order[pass & 1];
+        unsigned long long *to = order[(pass & 1) ^ 1];
+        for (int d = lane; d < digits; d += 32) cnt[w][d] = 0;
+        __syncthreads();
+        // (kSortItems + 1: a piece is rounded up to whole warps)
+        unsigned long long item[kSortItems + 1];
+        unsigned short before[kSortItems + 1];
+#pragma unroll
+        for (int q = 0; q <= kSortItems; ++q) {
+            const int i = w * piece + q * 32 + lane;
+            if (q * 32 >= piece || w * piece + q * 32 >= m) break;  // the same for the whole warp
+            const bool in = i < m && q * 32 + lane < piece;
+            item[q] = in ? from[i] : 0;
+            const int d = in ? ((unsigned)item[q] >> (pass * a.bits)) & (digits - 1) : digits;
+            const unsigned same = __match_any_sync(0xffffffffu, d);
+            const int r = __popc(same & ((1u << lane) - 1));
+            const int have = in ? cnt[w][d] : 0;
+            before[q] = (unsigned short)(have + r);
+            __syncwarp();
+            if (in && r == 0) cnt[w][d] = (unsigned short)(have + __popc(same));
+            __syncwarp();
+        }
+        __syncthreads();
+        for (int d = tid; d < digits; d += kSortThreads) {
+            int sum = 0;
+            for (int q = 0; q < kSortThreads / 32; ++q) {
+                const int c = cnt[q][d];
+                cnt[q][d] = (unsigned short)sum;
+                sum += c;
+            }
+            for (int q = 0; q < ranks; ++q)
+                asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(peer(&all[rank][d], q)), "r"(sum) : "memory");
+        }
+        cluster_barrier();
+        // places of smaller digits, and of this digit in the CTAs before
+        if (tid < kMaxDigits) {
+            int total = 0, mine = 0;
+            if (tid < digits)
+                for (int q = 0; q < ranks; ++q) {
+                    if (q == rank) mine = total;
+                    total += all[q][tid];
+                }
+            int s = total;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int up = __shfl_up_sync(0xffffffffu, s, o);
+                if (lane >= o) s += up;
+            }
+            if (lane == 31) scan[w] = s;
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            for (int q = 0; q < w; ++q) s += scan[q];
+            base[tid] = s - total + mine;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q <= kSortItems; ++q) {
+            const int i = w * piece + q * 32 + lane;
+            if (q * 32 >= piece || i >= m) break;
+            const int d = ((unsigned)item[q] >> (pass * a.bits)) & (digits - 1);
+            const int at = base[d] + cnt[w][d] + before[q], r = at / a.per;
+            asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(peer(to + (at - r * a.per), r)), "l"(item[q]) : "memory");
+        }
+        cluster_barrier();
+    }
+    const unsigned long long *done = order[a.passes & 1];
+    for (int i = tid; i < m; i += kSortThreads) {
+        const int k = (int)(unsigned)done[i];
+        a.key[lo + i] = k;
+        a.pos[lo + i] = (int)(done[i] >> 32);
+        if (k < a.V) a.present[k] = 1;
+    }
+}
+
+// Through global memory, 8 bits a pass.  A pass: every tile's digit counts; their exclusive
+// prefix, digits first; every pair to its place.
 constexpr int kTile = 4096, kSort = 256, kDigits = 256;
 
 struct SortPass {
@@ -63,7 +195,8 @@ struct SortPass {
     const int32_t *tokens;  // first pass: the tokens; else null
     const int *key_in, *pos_in;
     int *key_out, *pos_out;
-    int *count;  // [kDigits][tiles]
+    int *count;        // [kDigits][tiles]
+    uint8_t *present;  // last pass: marked; else null
     int *status;
 };
 
@@ -140,204 +273,248 @@ __global__ void __launch_bounds__(kSort) k_sort_scatter(const SortPass a) {
             const int to = cnt[w][d] + rank;
             a.key_out[to] = key;
             a.pos_out[to] = a.tokens ? i : a.pos_in[i];
+            if (a.present && key < a.V) a.present[key] = 1;
         }
         __syncthreads();
     }
 }
 
 // ---- sums over the sorted positions -------------------------------------------------------
-constexpr int kBlock = 32, kSum = 128;
+constexpr int kSum = 128;
 
 template <class T>
 struct SumArgs {
-    int n, V, D, blocks, slices;  // slices of 32 * VEC columns
-    long long zero_warps;         // warps that look for absent rows (32 rows each)
+    int n, V, D, block, blocks, slices;  // sorted positions a block (a multiple of 32); slices of 32 * VEC columns
+    int zero_warps;                      // warps that look for absent rows (32 rows each)
     const int *key, *pos;
+    const uint8_t *present;
     const T *dout;
     T *dtable;
     float scale;
     float *part;  // [blocks][2][D]: a run that came in from the block before; one that goes on
 };
 
-template <class T, int VEC>
+template <int VEC>
 __device__ __forceinline__ void put(float *p, const float (&v)[VEC]) {
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) p[k] = v[k];
+    *reinterpret_cast<seq_vec<float, VEC> *>(p) = *reinterpret_cast<const seq_vec<float, VEC> *>(v);
 }
 template <class T, int VEC>
 __device__ __forceinline__ void put_row(T *p, const float (&v)[VEC], float scale) {
-    seq_vec<T, VEC> o;
+    float f[VEC];
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) o.v[k] = seq_from_float<T>(v[k] * scale);
-    seq_store(p, o);
+    for (int k = 0; k < VEC; ++k) f[k] = v[k] * scale;
+    seq_store(p, seq_pack<T, VEC>(f));
 }
 
 template <class T, int VEC>
 __global__ void __launch_bounds__(kSum) k_embed_sum(const SumArgs<T> a) {
     const int lane = threadIdx.x & 31;
     long long unit = (long long)blockIdx.x * (kSum / 32) + threadIdx.x / 32;
-    const long long units = (long long)a.blocks * a.slices;
-    if (unit >= units) {  // rows without tokens
-        unit -= units;
-        if (unit >= a.zero_warps) return;
-        const int v = (int)unit * 32 + lane;
-        int lo = 0, hi = a.n;
-        while (lo < hi) {
-            const int mid = lo + (hi - lo) / 2;
-            if (a.key[mid] < v) lo = mid + 1;
-            else hi = mid;
-        }
-        unsigned absent = __ballot_sync(0xffffffffu, v < a.V && (lo == a.n || a.key[lo] != v));
-        float zero[VEC] = {};
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (unit < a.zero_warps) {  // rows without tokens
+        const long long v = unit * 32 + lane;
+        unsigned absent = __ballot_sync(0xffffffffu, v < a.V && !a.present[v]);
+        const float zero[VEC] = {};
         for (; absent; absent &= absent - 1) {
             const long long row = unit * 32 + __ffs(absent) - 1;
             for (int j = lane * VEC; j < a.D; j += 32 * VEC) put_row<T, VEC>(a.dtable + row * a.D + j, zero, 1.f);
         }
         return;
     }
+    unit -= a.zero_warps;
+    if (unit >= (long long)a.blocks * a.slices) return;
     const int b = (int)(unit / a.slices), j = ((int)(unit % a.slices) * 32 + lane) * VEC;
-    const int lo = b * kBlock, m = min(kBlock, a.n - lo);
-    const int key = lane < m ? a.key[lo + lane] : a.V, pos = lane < m ? a.pos[lo + lane] : 0;
-    const int prev = lo > 0 ? a.key[lo - 1] : -1, next = lo + m < a.n ? a.key[lo + m] : -1;
+    const int lo = b * a.block, hi = min(a.n, lo + a.block);
     const bool mine = j < a.D;
+    // the key before the current run began, and whether that run is the block's first
+    const int prev = lo > 0 ? a.key[lo - 1] : -1;
+    bool head = true;
     float acc[VEC] = {};
     constexpr int U = 8;
-    bool head = true;  // the current run is the block's first
+    int key = lo + lane < hi ? a.key[lo + lane] : a.V, pos = lo + lane < hi ? a.pos[lo + lane] : 0;
+    for (int at = lo; at < hi; at += 32) {
+        // the next 32 keys are here before this one's rows are summed (-1: after the last)
+        const int ni = at + 32 + lane;
+        const int nkey = ni < a.n && ni <= hi ? a.key[ni] : -1, npos = ni < hi ? a.pos[ni] : 0;
+        const int first_next = __shfl_sync(0xffffffffu, nkey, 0), m = min(32, hi - at);
+        // (a block's last 32 may be fewer only at the end of all: nothing follows then)
 #pragma unroll 1
-    for (int q0 = 0; q0 < m; q0 += U) {
-        seq_vec<T, VEC> v[U];
+        for (int q0 = 0; q0 < m; q0 += U) {
+            seq_vec<T, VEC> v[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int q = q0 + u;
-            const int k = __shfl_sync(0xffffffffu, key, q & 31), p = __shfl_sync(0xffffffffu, pos, q & 31);
-            if (q < m && k < a.V && mine) v[u] = seq_load<T, VEC>(a.dout + (long long)p * a.D + j);
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int q = q0 + u;
-            const int k = __shfl_sync(0xffffffffu, key, q & 31);
-            const int after = __shfl_sync(0xffffffffu, key, (q + 1) & 31);
-            if (q >= m || k >= a.V) continue;
-            if (mine)
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) acc[e] += seq_to_float(v[u].v[e]);
-            const bool end = q + 1 == m;
-            if (!end && after == k) continue;
-            // the run ends here, or leaves the block
-            if (mine) {
-                const bool came = head && k == prev, goes = end && k == next;
-                if (came) put<T, VEC>(a.part + ((long long)b * 2) * a.D + j, acc);
-                else if (goes) put<T, VEC>(a.part + ((long long)b * 2 + 1) * a.D + j, acc);
-                else put_row<T, VEC>(a.dtable + (long long)k * a.D + j, acc, a.scale);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+            for (int u = 0; u < U; ++u) {
+                const int k = __shfl_sync(0xffffffffu, key, (q0 + u) & 31), p = __shfl_sync(0xffffffffu, pos, (q0 + u) & 31);
+                if (q0 + u < m && k < a.V && mine) v[u] = seq_load<T, VEC>(a.dout + (long long)p * a.D + j);
             }
-            head = false;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int q = q0 + u;
+                const int k = __shfl_sync(0xffffffffu, key, q & 31);
+                int after = __shfl_sync(0xffffffffu, key, (q + 1) & 31);
+                if (q >= m || k >= a.V) continue;
+                if (q == 31) after = first_next;
+                else if (q + 1 == m) after = -1;
+                if (mine) {
+                    float f[VEC];
+                    seq_unpack(v[u], f);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) acc[e] += f[e];
+                }
+                const bool end = at + q + 1 == hi;  // of the block
+                if (!end && after == k) continue;
+                // the run ends here, or leaves the block
+                if (mine) {
+                    const bool came = head && k == prev, goes = end && k == after;
+                    if (came) put<VEC>(a.part + ((long long)b * 2) * a.D + j, acc);
+                    else if (goes) put<VEC>(a.part + ((long long)b * 2 + 1) * a.D + j, acc);
+                    else put_row<T, VEC>(a.dtable + (long long)k * a.D + j, acc, a.scale);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+                }
+                head = false;
+            }
         }
+        key = ni < hi ? nkey : a.V;
+        pos = npos;
     }
 }
 
-// A run that crosses blocks: the CTA of the block where it starts adds its parts, each warp a
-// stretch of the blocks, then the stretches in order.
+// A run that crosses blocks: the CTA of the block where it starts (and of a slice of columns) adds
+// its parts, each warp a stretch of the blocks, then the stretches in order.
 template <class T, int VEC>
 __global__ void __launch_bounds__(256) k_embed_join(const SumArgs<T> a) {
     constexpr int W = 8;
     __shared__ float s[W][32 * VEC];
-    const int b = blockIdx.x, hi = (b + 1) * kBlock;
+    const int b = blockIdx.x / a.slices, sl = blockIdx.x % a.slices, lo = b * a.block, hi = lo + a.block;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     if (hi >= a.n) return;
-    const int k = a.key[hi - 1];
-    if (k >= a.V || a.key[hi] != k) return;
-    const int lo = b * kBlock;
-    if (a.key[lo] == k && lo > 0 && a.key[lo - 1] == k) return;  // it started in a block before
-    // the end of the run
-    int l = hi, r = a.n;
-    while (l < r) {
-        const int mid = l + (r - l) / 2;
-        if (a.key[mid] <= k) l = mid + 1;
-        else r = mid;
-    }
-    const int last = (l - 1) / kBlock;  // its last block
+    const int k = a.key[hi - 1], k_next = a.key[hi], k_lo = a.key[lo], k_prev = lo > 0 ? a.key[lo - 1] : -1;
+    if (k >= a.V || k_next != k || (k_lo == k && k_prev == k)) return;  // no run leaves, or it started before
     const int lane = threadIdx.x & 31, w = threadIdx.x / 32;
+    // its last block: the last whose first key is k (32 blocks a look)
+    int last = b + 1;
+    for (int q = b + 2;; q += 32) {
+        const bool on = q + lane < a.blocks && a.key[(q + lane) * a.block] == k;
+        const unsigned off = ~__ballot_sync(0xffffffffu, on);
+        last = q - 1 + (off ? __ffs(off) - 1 : 32);
+        if (off) break;
+    }
     const int count = last - b, per = (count + W - 1) / W;  // blocks after this one
     const int from = b + 1 + w * per, to = min(last + 1, from + per);
-    for (int sl = 0; sl < a.slices; ++sl) {
-        const int j = (sl * 32 + lane) * VEC;
-        float acc[VEC] = {};
-        if (j < a.D) {
-            if (w == 0)
+    const int j = (sl * 32 + lane) * VEC;
+    float acc[VEC] = {};
+    if (j < a.D) {
+        using F = seq_vec<float, VEC>;
+        if (w == 0) {
+            const F v = *reinterpret_cast<const F *>(a.part + ((long long)b * 2 + 1) * a.D + j);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) acc[e] = a.part[((long long)b * 2 + 1) * a.D + j + e];
+            for (int e = 0; e < VEC; ++e) acc[e] = v.v[e];
+        }
 #pragma unroll 4
-            for (int q = from; q < to; ++q)
+        for (int q = from; q < to; ++q) {
+            const F v = *reinterpret_cast<const F *>(a.part + ((long long)q * 2) * a.D + j);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) acc[e] += a.part[((long long)q * 2) * a.D + j + e];
+            for (int e = 0; e < VEC; ++e) acc[e] += v.v[e];
         }
+    }
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) s[w][lane * VEC + e] = acc[e];
-        __syncthreads();
-        if (w == 0 && j < a.D) {
-            for (int q = 1; q < W; ++q)
+    for (int e = 0; e < VEC; ++e) s[w][lane * VEC + e] = acc[e];
+    __syncthreads();
+    if (w == 0 && j < a.D) {
+        for (int q = 1; q < W; ++q)
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) acc[e] += s[q][lane * VEC + e];
-            put_row<T, VEC>(a.dtable + (long long)k * a.D + j, acc, a.scale);
-        }
-        __syncthreads();
+            for (int e = 0; e < VEC; ++e) acc[e] += s[q][lane * VEC + e];
+        put_row<T, VEC>(a.dtable + (long long)k * a.D + j, acc, a.scale);
     }
 }
 
 size_t up(size_t b) { return (b + 255) & ~(size_t)255; }
 
-int passes(int V) {
+int key_bits(int V) {  // keys 0 ... V
     int bits = 1;
     while (bits < 31 && (V >> bits)) ++bits;
-    return (bits + 7) / 8;
+    return bits;
 }
 
 struct Layout {
-    int tiles, blocks;
-    size_t key[2], pos[2], count, part, total;
+    bool cluster;
+    int tiles, block, blocks;
+    size_t key[2], pos[2], count, present, part, total;
 };
-Layout layout(long long n, int D) {
+Layout layout(const wm_seq *h, long long n, int V, int D, size_t es) {
     Layout l{};
+    l.cluster = n <= (long long)kCluster * kPerCta;
     l.tiles = (int)((n + kTile - 1) / kTile);
-    l.blocks = (int)((n + kBlock - 1) / kBlock);
+    // Positions per block: long blocks leave fewer partial rows of tokens that are common, short ones
+    // keep 16 warps an SM busy.
+    const long long slices = (D * es + 511) / 512;
+    l.block = 32;
+    while (l.block < 256 && n * slices / (2 * l.block) >= h->sms * 16ll) l.block *= 2;
+    l.blocks = (int)((n + l.block - 1) / l.block);
     size_t o = 0;
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < (l.cluster ? 1 : 2); ++i) {
         l.key[i] = o;
         o += up((size_t)n * 4);
         l.pos[i] = o;
         o += up((size_t)n * 4);
     }
     l.count = o;
-    o += up((size_t)l.tiles * kDigits * 4);
+    if (!l.cluster) o += up((size_t)l.tiles * kDigits * 4);
+    l.present = o;
+    o += up((size_t)V);
     l.part = o;
     o += up((size_t)l.blocks * 2 * D * 4);
     l.total = o;
     return l;
 }
 
+// Launches that may start while the one before still runs (they wait for it themselves).
+template <class P>
+cudaError_t follow(void (*k)(P), unsigned grid, int threads, cudaStream_t s, const P &p) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(threads);
+    cfg.stream = s;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, k, p);
+}
+
 template <class T, int VEC>
-void sums(wm_seq *h, SumArgs<T> a, cudaStream_t s) {
+cudaError_t sums(wm_seq *h, SumArgs<T> a, cudaStream_t s) {
     a.slices = (a.D + 32 * VEC - 1) / (32 * VEC);
     const long long warps = (long long)a.blocks * a.slices + a.zero_warps;
-    k_embed_sum<T, VEC><<<(unsigned)((warps + kSum / 32 - 1) / (kSum / 32)), kSum, 0, s>>>(a);
+    cudaError_t e = follow(k_embed_sum<T, VEC>, (unsigned)((warps + kSum / 32 - 1) / (kSum / 32)), kSum, s, a);
+    if (e != cudaSuccess) return e;
     ++h->last_launches;
     if (a.blocks > 1) {
-        k_embed_join<T, VEC><<<a.blocks - 1, 256, 0, s>>>(a);
+        e = follow(k_embed_join<T, VEC>, (unsigned)((a.blocks - 1) * a.slices), 256, s, a);
         ++h->last_launches;
     }
+    return e;
 }
 
 template <class T>
-void backward(wm_seq *h, int n, int V, int D, const int *key, const int *pos, const T *dout, float scale, T *dtable,
-              float *part, int blocks, cudaStream_t s) {
-    SumArgs<T> a{};
-    a.n = n; a.V = V; a.D = D; a.blocks = blocks;
-    a.zero_warps = ((long long)V + 31) / 32;
-    a.key = key; a.pos = pos; a.dout = dout; a.dtable = dtable; a.scale = scale; a.part = part;
+cudaError_t backward(wm_seq *h, SumArgs<T> a, const void *dout, void *dtable, cudaStream_t s) {
+    a.dout = (const T *)dout;
+    a.dtable = (T *)dtable;
     constexpr int VEC = 16 / sizeof(T);
-    if (D % VEC == 0 && (uintptr_t)dout % 16 == 0 && (uintptr_t)dtable % 16 == 0) sums<T, VEC>(h, a, s);
-    else sums<T, 1>(h, a, s);
+    if (a.D % VEC == 0 && (uintptr_t)dout % 16 == 0 && (uintptr_t)dtable % 16 == 0) return sums<T, VEC>(h, a, s);
+    return sums<T, 1>(h, a, s);
+}
+
+template <class T>
+SumArgs<T> sum_args(int n, int V, int D, const Layout &l, char *ws, int at, float scale) {
+    SumArgs<T> a{};
+    a.n = n; a.V = V; a.D = D; a.block = l.block; a.blocks = l.blocks;
+    a.zero_warps = (int)(((long long)V + 31) / 32);
+    a.key = (const int *)(ws + l.key[at]); a.pos = (const int *)(ws + l.pos[at]);
+    a.present = (const uint8_t *)(ws + l.present);
+    a.scale = scale; a.part = (float *)(ws + l.part);
+    return a;
 }
 
 template <class T>
@@ -364,29 +541,66 @@ cudaError_t wm_seq_embed_launch(wm_seq *h, int dtype, long long n, int V, int D,
     return cudaGetLastError();
 }
 
-size_t wm_seq_embed_backward_ws(const wm_seq *, long long n, int, int D) { return n ? layout(n, D).total : 0; }
+size_t wm_seq_embed_backward_ws(const wm_seq *h, int dtype, long long n, int V, int D) {
+    return n ? layout(h, n, V, D, dtype == WM_BF16 ? 2 : 4).total : 0;
+}
 
 cudaError_t wm_seq_embed_backward_launch(wm_seq *h, int dtype, long long n, int V, int D, const int32_t *tokens,
                                          const void *dout, float scale, void *dtable, cudaStream_t s) {
-    h->last_launches = 0;
-    const Layout l = layout(n, D);
-    char *ws = (char *)h->ws;
-    int *key[2], *pos[2];
-    for (int i = 0; i < 2; ++i) {
-        key[i] = (int *)(ws + l.key[i]);
-        pos[i] = (int *)(ws + l.pos[i]);
+    const size_t es = dtype == WM_BF16 ? 2 : 4;
+    if (n == 0) {
+        h->last_launches = 1;
+        return cudaMemsetAsync(dtable, 0, (size_t)V * D * es, s);
     }
+    h->last_launches = 0;
+    const Layout l = layout(h, n, V, D, es);
+    char *ws = (char *)h->ws;
+    const int bits = key_bits(V);
     int at = 0;
-    if (n > 0) {
-        const int np = passes(V);
+    if (l.cluster) {
+        ClusterSort a{};
+        a.n = (int)n; a.V = V;
+        // CTAs: 1024 tokens each, as far as the cluster goes
+        int ranks = 1;
+        while (ranks < kCluster && (long long)ranks * kSortThreads < n) ranks *= 2;
+        a.per = (int)((n + ranks - 1) / ranks);
+        a.passes = (bits + 7) / 8;
+        a.bits = (bits + a.passes - 1) / a.passes;
+        a.tokens = tokens;
+        a.key = (int *)(ws + l.key[0]); a.pos = (int *)(ws + l.pos[0]);
+        a.present = (uint8_t *)(ws + l.present);
+        a.status = h->status;
+        const size_t smem = (size_t)a.per * 16;
+        cudaError_t e = cudaFuncSetAttribute(k_sort_cluster, cudaFuncAttributeMaxDynamicSharedMemorySize, kPerCta * 16);
+        if (e == cudaSuccess && ranks > 8) e = cudaFuncSetAttribute(k_sort_cluster, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return e;
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3((unsigned)ranks);
+        cfg.blockDim = dim3(kSortThreads);
+        cfg.dynamicSmemBytes = smem;
+        cfg.stream = s;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim.x = (unsigned)ranks;
+        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        if ((e = cudaLaunchKernelEx(&cfg, k_sort_cluster, a)) != cudaSuccess) return e;
+        h->last_launches = 1;
+    } else {
+        const cudaError_t e = cudaMemsetAsync(ws + l.present, 0, (size_t)V, s);
+        if (e != cudaSuccess) return e;
+        h->last_launches = 1;
+        const int np = (bits + 7) / 8;
         for (int p = 0; p < np; ++p) {
             SortPass a{};
             a.n = (int)n; a.V = V; a.shift = 8 * p; a.tiles = l.tiles;
             a.tokens = p == 0 ? tokens : nullptr;
-            a.key_in = key[at]; a.pos_in = pos[at];
+            a.key_in = (const int *)(ws + l.key[at]); a.pos_in = (const int *)(ws + l.pos[at]);
             at ^= p > 0;
-            a.key_out = key[at]; a.pos_out = pos[at];
+            a.key_out = (int *)(ws + l.key[at]); a.pos_out = (int *)(ws + l.pos[at]);
             a.count = (int *)(ws + l.count);
+            a.present = p + 1 == np ? (uint8_t *)(ws + l.present) : nullptr;
             a.status = h->status;
             k_sort_count<<<l.tiles, kSort, 0, s>>>(a);
             k_sort_prefix<<<1, 1024, 0, s>>>(l.tiles * kDigits, a.count);
@@ -395,9 +609,6 @@ cudaError_t wm_seq_embed_backward_launch(wm_seq *h, int dtype, long long n, int 
         }
     }
     if (dtype == WM_BF16)
-        backward(h, (int)n, V, D, key[at], pos[at], (const __nv_bfloat16 *)dout, scale, (__nv_bfloat16 *)dtable,
-                 (float *)(ws + l.part), l.blocks, s);
-    else
-        backward(h, (int)n, V, D, key[at], pos[at], (const float *)dout, scale, (float *)dtable, (float *)(ws + l.part), l.blocks, s);
-    return cudaGetLastError();
+        return backward(h, sum_args<__nv_bfloat16>((int)n, V, D, l, ws, at, scale), dout, dtable, s);
+    return backward(h, sum_args<float>((int)n, V, D, l, ws, at, scale), dout, dtable, s);
 }

@@ -376,6 +376,17 @@ def test_embed(ops, dtype, n, V, D):
     ops.sync()
 
 
+@pytest.mark.parametrize("n,V", [(1023, 255), (1025, 256), (16384, 30000), (70001, 513), (196608, 100), (196609, 300), (250000, 70000)])
+def test_embed_backward_sort_sizes(ops, n, V):
+    """One CTA, a cluster, its last size, and beyond it; one digit to three."""
+    g = torch.Generator().manual_seed(V)
+    t = (float(V) ** torch.rand(n, generator=g, dtype=torch.float64)).long() - torch.randint(0, 2, (n,), generator=g)
+    t = torch.randperm(V + 1, generator=g)[t.clamp(0, V)] - 1
+    dout = rnd(n, 16, seed=2)
+    got = ops.embed_backward(t.to(torch.int32).cuda(), dout, V)
+    ref.check(got, *ref.embed_backward(t, dout, V, 1.0), "dtable")
+
+
 @pytest.mark.parametrize("kind", ["one token", "none", "sorted", "reversed", "common"])
 def test_embed_token_orders(ops, kind):
     n, V, D = 9000, 1000, 48
