@@ -4,10 +4,10 @@
 //
 // Bound by memory: every value is read for the norm, and read and written again where the
 // clip applies.  The tensors go to the kernels as tables in their parameters (no copy to the
-// device, no synchronisation), cut into tiles that CTAs take by a fixed stride, so that a
-// thousand small tensors load the GPU as evenly as one large one and the order of the sum
-// is fixed.  The second launch takes the tiles from the last to the first: what the first
-// read last is still in L2.
+// device, no synchronisation), cut into tiles, every CTA a run of them, so that a thousand
+// small tensors load the GPU as evenly as one large one and the order of the sum is fixed.
+// A tile's loads are issued before the one before it is worked on.  The second launch goes
+// through the runs backwards: what the first read last is still in L2.
 //
 // Squares are summed in fp32 within a 16-byte vector (4 or 8 values) and from there on
 // without rounding error that matters: a thread adds the vectors' sums into an fp32 pair
@@ -56,8 +56,9 @@ struct Sum {
 };
 
 template <int N>
-__device__ __noinline__ double squares64(const float (&v)[N]) {
+__device__ __forceinline__ double squares64(const float (&v)[N]) {
     double s = 0.0;
+#pragma unroll
     for (int i = 0; i < N; ++i) s += (double)v[i] * (double)v[i];
     return s;
 }
@@ -65,8 +66,18 @@ __device__ __noinline__ double squares64(const float (&v)[N]) {
 template <int N>
 __device__ __forceinline__ void add_squares(const float (&v)[N], Sum &sum) {
     float s = 0.f, any = 0.f;
+    if constexpr (N > 2) {  // two chains
+        float r = v[1] * v[1];
+        s = v[0] * v[0];
 #pragma unroll
-    for (int i = 0; i < N; ++i) s = fmaf(v[i], v[i], s);
+        for (int i = 2; i < N; i += 2) {
+            s = fmaf(v[i], v[i], s);
+            r = fmaf(v[i + 1], v[i + 1], r);
+        }
+        s += r;
+    } else {
+        s = v[0] * v[0];
+    }
     // below 1e-25 squares lose bits to fp32's range, above 1e34 a sum of them could pass it
     if (s > 1e-25f && s < 1e34f) {
         sum.add(s);
@@ -77,71 +88,103 @@ __device__ __forceinline__ void add_squares(const float (&v)[N], Sum &sum) {
     if (any != 0.f || s != 0.f) sum.wide += squares64(v);  // (NaN: s is)
 }
 
-template <class T>
-__device__ __forceinline__ void tile_squares(const T *p, int n, Sum &sum) {
-    constexpr int VEC = 16 / sizeof(T), EACH = kTileBytes / 16 / kThreads;
-    int done = 0;
-    if ((uintptr_t)p % 16 == 0) {
-        const int vecs = n / VEC;
-        seq_vec<T, VEC> v[EACH];
-#pragma unroll
-        for (int q = 0; q < EACH; ++q)
-            if (threadIdx.x + q * kThreads < vecs) v[q] = seq_load<T, VEC>(p + (threadIdx.x + q * kThreads) * VEC);
-#pragma unroll
-        for (int q = 0; q < EACH; ++q)
-            if (threadIdx.x + q * kThreads < vecs) {
-                float f[VEC];
-                seq_unpack(v[q], f);
-                add_squares(f, sum);
-            }
-        done = vecs * VEC;
+constexpr int kEach = kTileBytes / 16 / kThreads;  // 16-byte vectors of a tile per thread
+
+// The tile that a CTA is at, and its tensor.
+template <int SIZE>
+struct Cursor {
+    const Table<SIZE> &t;
+    int i, tile;
+    int lo, hi;  // the tensor's tiles
+    const char *src;
+    char *dst;
+    long long n;
+    bool bf16;
+    __device__ __forceinline__ Cursor(const Table<SIZE> &table, int first) : t(table), tile(first) {
+        int a = 0, b = t.count - 1;
+        while (a < b) {
+            const int mid = (a + b) / 2;
+            if (tile < t.tile_end[mid]) b = mid;
+            else a = mid + 1;
+        }
+        at(a);
     }
-    for (int i = done + threadIdx.x; i < n; i += kThreads) {
-        const float f[1] = {seq_to_float(p[i])};
+    __device__ __forceinline__ void at(int tensor) {
+        i = tensor;
+        lo = i ? t.tile_end[i - 1] : 0;
+        hi = t.tile_end[i];
+        src = (const char *)t.src[i];
+        dst = (char *)t.dst[i];
+        n = (long long)(t.n[i] >> 1);
+        bf16 = t.n[i] & 1;
+    }
+    __device__ __forceinline__ void step(int by) {  // 1 or -1
+        tile += by;
+        if (tile >= hi && i + 1 < t.count) at(i + 1);
+        else if (tile < lo && i > 0) at(i - 1);
+    }
+};
+// A tile: its place, and (aligned) its vectors.
+struct Tile {
+    const char *src;
+    char *dst;
+    int n;        // values
+    bool bf16, wide;  // wide: 16-byte accesses
+    uint4 v[kEach];
+    template <int SIZE>
+    __device__ __forceinline__ void load(const Cursor<SIZE> &c, bool with_dst) {
+        bf16 = c.bf16;
+        const long long at = (long long)(c.tile - c.lo) * kTileBytes;
+        const int shift = bf16 ? 1 : 2;
+        n = (int)min((long long)(kTileBytes >> shift), c.n - (at >> shift));
+        src = c.src + at;
+        dst = c.dst + at;
+        wide = (uintptr_t)src % 16 == 0 && (!with_dst || (uintptr_t)dst % 16 == 0);
+        const int vecs = wide ? n / (bf16 ? 8 : 4) : 0;
+#pragma unroll
+        for (int q = 0; q < kEach; ++q)
+            if ((int)threadIdx.x + q * kThreads < vecs) v[q] = reinterpret_cast<const uint4 *>(src)[threadIdx.x + q * kThreads];
+    }
+    __device__ __forceinline__ int vecs() const { return wide ? n / (bf16 ? 8 : 4) : 0; }
+};
+
+template <class T>
+__device__ __forceinline__ void tile_squares(const Tile &t, Sum &sum) {
+    constexpr int VEC = 16 / sizeof(T);
+    const int vecs = t.vecs();
+#pragma unroll
+    for (int q = 0; q < kEach; ++q)
+        if ((int)threadIdx.x + q * kThreads < vecs) {
+            float f[VEC];
+            seq_unpack(reinterpret_cast<const seq_vec<T, VEC> &>(t.v[q]), f);
+            add_squares(f, sum);
+        }
+    for (int i = vecs * VEC + threadIdx.x; i < t.n; i += kThreads) {
+        const float f[1] = {seq_to_float(reinterpret_cast<const T *>(t.src)[i])};
         add_squares(f, sum);
     }
 }
 
 template <class T>
-__device__ __forceinline__ void tile_scale(const T *p, T *q, int n, float scale) {
-    constexpr int VEC = 16 / sizeof(T), EACH = kTileBytes / 16 / kThreads;
-    int done = 0;
-    if ((uintptr_t)p % 16 == 0 && (uintptr_t)q % 16 == 0) {
-        const int vecs = n / VEC;
-        seq_vec<T, VEC> v[EACH];
+__device__ __forceinline__ void tile_scale(const Tile &t, float scale) {
+    constexpr int VEC = 16 / sizeof(T);
+    const int vecs = t.vecs();
+    T *to = reinterpret_cast<T *>(t.dst);
 #pragma unroll
-        for (int u = 0; u < EACH; ++u)
-            if (threadIdx.x + u * kThreads < vecs) v[u] = seq_load<T, VEC>(p + (threadIdx.x + u * kThreads) * VEC);
+    for (int q = 0; q < kEach; ++q)
+        if ((int)threadIdx.x + q * kThreads < vecs) {
+            float f[VEC];
+            seq_unpack(reinterpret_cast<const seq_vec<T, VEC> &>(t.v[q]), f);
 #pragma unroll
-        for (int u = 0; u < EACH; ++u)
-            if (threadIdx.x + u * kThreads < vecs) {
-                float f[VEC];
-                seq_unpack(v[u], f);
-#pragma unroll
-                for (int k = 0; k < VEC; ++k) f[k] *= scale;
-                seq_store(q + (threadIdx.x + u * kThreads) * VEC, seq_pack<T, VEC>(f));
-            }
-        done = vecs * VEC;
-    }
-    for (int i = done + threadIdx.x; i < n; i += kThreads) q[i] = seq_from_float<T>(seq_to_float(p[i]) * scale);
+            for (int k = 0; k < VEC; ++k) f[k] *= scale;
+            seq_store(to + (threadIdx.x + q * kThreads) * VEC, seq_pack<T, VEC>(f));
+        }
+    for (int i = vecs * VEC + threadIdx.x; i < t.n; i += kThreads)
+        to[i] = seq_from_float<T>(seq_to_float(reinterpret_cast<const T *>(t.src)[i]) * scale);
 }
 
-// The tensor that holds a tile, and the tile's first value and size.
-template <int SIZE>
-__device__ __forceinline__ int find(const Table<SIZE> &t, int tile, long long &first, int &n, bool &bf16) {
-    int lo = 0, hi = t.count - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi) / 2;
-        if (tile < t.tile_end[mid]) hi = mid;
-        else lo = mid + 1;
-    }
-    const int start = lo ? t.tile_end[lo - 1] : 0;
-    bf16 = t.n[lo] & 1;
-    const long long all = (long long)(t.n[lo] >> 1), per = kTileBytes / (bf16 ? 2 : 4);
-    first = (long long)(tile - start) * per;
-    n = (int)min(per, all - first);
-    return lo;
-}
+// CTA b's tiles: [first, last) of an even split.
+__device__ __forceinline__ int split(int tiles, int b) { return (int)((long long)tiles * b / gridDim.x); }
 
 // part[0, parts): sums of the launches before this one and of this one's CTAs.  The last CTA of the
 // last launch adds them, always in the same order, and leaves the norm and the scale.
@@ -152,14 +195,19 @@ __global__ void __launch_bounds__(kThreads) k_clip_squares(const __grid_constant
     __shared__ double red[kThreads / 32];
     __shared__ bool s_last;
     Sum sum;
+    const int first = split(t.tiles, blockIdx.x), end = split(t.tiles, blockIdx.x + 1);
+    Cursor<SIZE> c(t, first);
+    Tile next;
+    next.load(c, false);
     int vecs = 0;
-    for (int tile = blockIdx.x; tile < t.tiles; tile += gridDim.x) {
-        long long first;
-        int n;
-        bool bf16;
-        const int i = find(t, tile, first, n, bf16);
-        if (bf16) tile_squares((const __nv_bfloat16 *)t.src[i] + first, n, sum);
-        else tile_squares((const float *)t.src[i] + first, n, sum);
+    for (int tile = first; tile < end; ++tile) {
+        const Tile now = next;
+        if (tile + 1 < end) {
+            c.step(1);
+            next.load(c, false);
+        }
+        if (now.bf16) tile_squares<__nv_bfloat16>(now, sum);
+        else tile_squares<float>(now, sum);
         if ((vecs += kTileBytes / 2 / kThreads) >= kFlush) {  // (an unaligned tile: a value a vector)
             sum.flush();
             vecs = 0;
@@ -211,22 +259,25 @@ __global__ void __launch_bounds__(kThreads) k_clip_squares(const __grid_constant
 }
 
 template <int SIZE>
-__global__ void __launch_bounds__(kThreads) k_clip_scale(const __grid_constant__ Table<SIZE> t, const Result *result) {
-    long long first;
-    int n;
-    bool bf16;
-    int tile = t.tiles - 1 - (int)blockIdx.x, i = find(t, tile, first, n, bf16);
+__global__ void __launch_bounds__(kThreads) k_clip_scale(const __grid_constant__ Table<SIZE> t, const Result *result,
+                                                         int copies) {
+    const int first = split(t.tiles, blockIdx.x), end = split(t.tiles, blockIdx.x + 1);
+    Cursor<SIZE> c(t, end - 1);
     // launched while the first kernel still runs: its result is there after this
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const float scale = __ldcg(&result->scale);
-    for (;;) {
-        if (scale != 1.f || t.src[i] != t.dst[i]) {
-            if (bf16) tile_scale((const __nv_bfloat16 *)t.src[i] + first, (__nv_bfloat16 *)t.dst[i] + first, n, scale);
-            else tile_scale((const float *)t.src[i] + first, (float *)t.dst[i] + first, n, scale);
+    if (scale == 1.f && !copies) return;  // (copies: some dst is not its src)
+    Tile next;
+    next.load(c, true);
+    for (int tile = end - 1; tile >= first; --tile) {
+        const Tile now = next;
+        if (tile > first) {
+            c.step(-1);
+            next.load(c, true);
         }
-        tile -= gridDim.x;
-        if (tile < 0) return;
-        i = find(t, tile, first, n, bf16);
+        if (scale == 1.f && now.src == now.dst) continue;
+        if (now.bf16) tile_scale<__nv_bfloat16>(now, scale);
+        else tile_scale<float>(now, scale);
     }
 }
 
@@ -285,7 +336,7 @@ cudaError_t clip(wm_seq *h, int count, const wm_seq_grad *grads, float max_norm,
         cfg.stream = s;
         cfg.attrs = at;
         cfg.numAttrs = one;  // later tables follow a scale launch, whose end says nothing of the norm
-        const cudaError_t e = cudaLaunchKernelEx(&cfg, k_clip_scale<SIZE>, (const Table<SIZE>)t, (const Result *)result);
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, k_clip_scale<SIZE>, (const Table<SIZE>)t, (const Result *)result, (int)copies);
         if (e != cudaSuccess) return e;
         ++h->last_launches;
     }

@@ -46,10 +46,11 @@ __global__ void __launch_bounds__(kLookup) k_embed(long long n, int V, int D, co
             for (int u = 0; u < U; ++u) {
                 const int j = j0 + u * 32 * VEC;
                 if (j >= D) break;
+                float f[VEC];
+                seq_unpack(v[u], f);
 #pragma unroll
-                for (int k = 0; k < VEC; ++k)
-                    v[u].v[k] = seq_from_float<T>(row < 0 ? 0.f : seq_to_float(v[u].v[k]) * scale);
-                seq_store(out + i * D + j, v[u]);
+                for (int k = 0; k < VEC; ++k) f[k] = row < 0 ? 0.f : f[k] * scale;
+                seq_store(out + i * D + j, seq_pack<T, VEC>(f));
             }
         }
     }
@@ -284,7 +285,7 @@ constexpr int kSum = 128;
 
 template <class T>
 struct SumArgs {
-    int n, V, D, block, blocks, slices;  // sorted positions a block (a multiple of 32); slices of 32 * VEC columns
+    int n, V, D, block, blocks, slices;  // sorted positions a block; slices of 32 * VEC columns
     int zero_warps;                      // warps that look for absent rows (32 rows each)
     const int *key, *pos;
     const uint8_t *present;
@@ -307,7 +308,7 @@ __device__ __forceinline__ void put_row(T *p, const float (&v)[VEC], float scale
 }
 
 template <class T, int VEC>
-__global__ void __launch_bounds__(kSum) k_embed_sum(const SumArgs<T> a) {
+__global__ void __launch_bounds__(kSum, 6) k_embed_sum(const SumArgs<T> a) {
     const int lane = threadIdx.x & 31;
     long long unit = (long long)blockIdx.x * (kSum / 32) + threadIdx.x / 32;
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -326,105 +327,106 @@ __global__ void __launch_bounds__(kSum) k_embed_sum(const SumArgs<T> a) {
     const int b = (int)(unit / a.slices), j = ((int)(unit % a.slices) * 32 + lane) * VEC;
     const int lo = b * a.block, hi = min(a.n, lo + a.block);
     const bool mine = j < a.D;
-    // the key before the current run began, and whether that run is the block's first
+    const T *col = a.dout + (mine ? j : 0);
+    // the key before the block, and whether the current run is the block's first
     const int prev = lo > 0 ? a.key[lo - 1] : -1;
     bool head = true;
     float acc[VEC] = {};
     constexpr int U = 8;
-    int key = lo + lane < hi ? a.key[lo + lane] : a.V, pos = lo + lane < hi ? a.pos[lo + lane] : 0;
+    // 32 keys at a time, and the one after the block (-1: after the last)
+    auto key_at = [&](int i) { return i <= hi && i < a.n ? a.key[i] : -1; };
+    auto pos_at = [&](int i) { return i < hi ? a.pos[i] : 0; };
+    int key = key_at(lo + lane), pos = pos_at(lo + lane);
     for (int at = lo; at < hi; at += 32) {
-        // the next 32 keys are here before this one's rows are summed (-1: after the last)
-        const int ni = at + 32 + lane;
-        const int nkey = ni < a.n && ni <= hi ? a.key[ni] : -1, npos = ni < hi ? a.pos[ni] : 0;
-        const int first_next = __shfl_sync(0xffffffffu, nkey, 0), m = min(32, hi - at);
-        // (a block's last 32 may be fewer only at the end of all: nothing follows then)
+        // the next 32 are here before this one's rows are summed
+        const int nkey = key_at(at + 32 + lane), npos = pos_at(at + 32 + lane);
+        const int in_next = __shfl_down_sync(0xffffffffu, key, 1), first_next = __shfl_sync(0xffffffffu, nkey, 0);
+        const int after = lane == 31 ? first_next : in_next;
+        // tokens outside the table come last of all: m positions count, and runs end (in the block) where a bit is set
+        const int m = __popc(__ballot_sync(0xffffffffu, at + lane < hi && key < a.V));
+        const unsigned ends = __ballot_sync(0xffffffffu, after != key || at + lane + 1 == hi);
 #pragma unroll 1
         for (int q0 = 0; q0 < m; q0 += U) {
             seq_vec<T, VEC> v[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int k = __shfl_sync(0xffffffffu, key, (q0 + u) & 31), p = __shfl_sync(0xffffffffu, pos, (q0 + u) & 31);
-                if (q0 + u < m && k < a.V && mine) v[u] = seq_load<T, VEC>(a.dout + (long long)p * a.D + j);
+            for (int u = 0; u < U; ++u) {  // (past m: row 0, or a row that is not used)
+                const int p = __shfl_sync(0xffffffffu, pos, (q0 + u) & 31);
+                v[u] = seq_load<T, VEC>(col + (long long)p * a.D);
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int q = q0 + u;
-                const int k = __shfl_sync(0xffffffffu, key, q & 31);
-                int after = __shfl_sync(0xffffffffu, key, (q + 1) & 31);
-                if (q >= m || k >= a.V) continue;
-                if (q == 31) after = first_next;
-                else if (q + 1 == m) after = -1;
-                if (mine) {
-                    float f[VEC];
-                    seq_unpack(v[u], f);
+                if (q >= m) break;
+                float f[VEC];
+                seq_unpack(v[u], f);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) acc[e] += f[e];
-                }
-                const bool end = at + q + 1 == hi;  // of the block
-                if (!end && after == k) continue;
+                for (int e = 0; e < VEC; ++e) acc[e] += f[e];
+                if (!(ends >> q & 1)) continue;
                 // the run ends here, or leaves the block
+                const int k = __shfl_sync(0xffffffffu, key, q), nk = __shfl_sync(0xffffffffu, after, q);
                 if (mine) {
-                    const bool came = head && k == prev, goes = end && k == after;
+                    const bool came = head && k == prev, goes = nk == k;
                     if (came) put<VEC>(a.part + ((long long)b * 2) * a.D + j, acc);
                     else if (goes) put<VEC>(a.part + ((long long)b * 2 + 1) * a.D + j, acc);
                     else put_row<T, VEC>(a.dtable + (long long)k * a.D + j, acc, a.scale);
-#pragma unroll
-                    for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
                 }
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
                 head = false;
             }
         }
-        key = ni < hi ? nkey : a.V;
+        key = nkey;
         pos = npos;
     }
 }
 
-// A run that crosses blocks: the CTA of the block where it starts (and of a slice of columns) adds
-// its parts, each warp a stretch of the blocks, then the stretches in order.
+// A run that crosses blocks: the CTA of the block where it starts adds its parts.  A warp takes a
+// slice of columns and all blocks; of a run of many blocks the warps take a stretch each, slice by
+// slice, and the stretches are added in order.
 template <class T, int VEC>
 __global__ void __launch_bounds__(256) k_embed_join(const SumArgs<T> a) {
-    constexpr int W = 8;
-    __shared__ float s[W][32 * VEC];
-    const int b = blockIdx.x / a.slices, sl = blockIdx.x % a.slices, lo = b * a.block, hi = lo + a.block;
+    constexpr int W = 8, kMany = 16;
+    using F = seq_vec<float, VEC>;
+    __shared__ F s[W][32];
+    const int b = blockIdx.x, lo = b * a.block, hi = lo + a.block;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (hi >= a.n) return;
     const int k = a.key[hi - 1], k_next = a.key[hi], k_lo = a.key[lo], k_prev = lo > 0 ? a.key[lo - 1] : -1;
     if (k >= a.V || k_next != k || (k_lo == k && k_prev == k)) return;  // no run leaves, or it started before
     const int lane = threadIdx.x & 31, w = threadIdx.x / 32;
     // its last block: the last whose first key is k (32 blocks a look)
-    int last = b + 1;
+    int last;
     for (int q = b + 2;; q += 32) {
         const bool on = q + lane < a.blocks && a.key[(q + lane) * a.block] == k;
         const unsigned off = ~__ballot_sync(0xffffffffu, on);
         last = q - 1 + (off ? __ffs(off) - 1 : 32);
         if (off) break;
     }
-    const int count = last - b, per = (count + W - 1) / W;  // blocks after this one
-    const int from = b + 1 + w * per, to = min(last + 1, from + per);
-    const int j = (sl * 32 + lane) * VEC;
-    float acc[VEC] = {};
-    if (j < a.D) {
-        using F = seq_vec<float, VEC>;
-        if (w == 0) {
-            const F v = *reinterpret_cast<const F *>(a.part + ((long long)b * 2 + 1) * a.D + j);
+    auto add = [&](F &acc, long long row, int j) {
+        const F v = *reinterpret_cast<const F *>(a.part + row * a.D + j);
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) acc[e] = v.v[e];
-        }
+        for (int e = 0; e < VEC; ++e) acc.v[e] += v.v[e];
+    };
+    const bool many = last - b > kMany;
+    const int per = many ? (last - b + W - 1) / W : last - b;  // blocks after this one, a warp's share
+    const int from = b + 1 + (many ? w * per : 0), to = min(last + 1, from + per);
+    for (int sl = many ? 0 : w; sl < a.slices; sl += many ? 1 : W) {
+        const int j = (sl * 32 + lane) * VEC;
+        F acc = {};
+        if (j < a.D) {
+            if (!many || w == 0) add(acc, (long long)b * 2 + 1, j);
 #pragma unroll 4
-        for (int q = from; q < to; ++q) {
-            const F v = *reinterpret_cast<const F *>(a.part + ((long long)q * 2) * a.D + j);
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) acc[e] += v.v[e];
+            for (int q = from; q < to; ++q) add(acc, (long long)q * 2, j);
         }
-    }
+        if (many) {
+            __syncthreads();  // (the slice before is read)
+            s[w][lane] = acc;
+            __syncthreads();
+            if (w == 0)
+                for (int q = 1; q < W; ++q)
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) s[w][lane * VEC + e] = acc[e];
-    __syncthreads();
-    if (w == 0 && j < a.D) {
-        for (int q = 1; q < W; ++q)
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) acc[e] += s[q][lane * VEC + e];
-        put_row<T, VEC>(a.dtable + (long long)k * a.D + j, acc, a.scale);
+                    for (int e = 0; e < VEC; ++e) acc.v[e] += s[q][lane].v[e];
+        }
+        if ((!many || w == 0) && j < a.D) put_row<T, VEC>(a.dtable + (long long)k * a.D + j, acc.v, a.scale);
     }
 }
 
@@ -445,11 +447,11 @@ Layout layout(const wm_seq *h, long long n, int V, int D, size_t es) {
     Layout l{};
     l.cluster = n <= (long long)kCluster * kPerCta;
     l.tiles = (int)((n + kTile - 1) / kTile);
-    // Positions per block: long blocks leave fewer partial rows of tokens that are common, short ones
-    // keep 16 warps an SM busy.
-    const long long slices = (D * es + 511) / 512;
-    l.block = 32;
-    while (l.block < 256 && n * slices / (2 * l.block) >= h->sms * 16ll) l.block *= 2;
+    // Positions per block: all blocks' warps run at once (22 of 24 an SM), in blocks of 16 to 256 positions:
+    // a second round of warps would run alone, short blocks leave more partial rows.
+    const long long slices = (D * (long long)es + 511) / 512, warps = h->sms * 22ll;
+    const long long b = (n * slices + warps - 1) / warps;
+    l.block = (int)(b < 16 ? 16 : b > 256 ? 256 : (b + 7) / 8 * 8);
     l.blocks = (int)((n + l.block - 1) / l.block);
     size_t o = 0;
     for (int i = 0; i < (l.cluster ? 1 : 2); ++i) {
@@ -491,7 +493,7 @@ cudaError_t sums(wm_seq *h, SumArgs<T> a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     ++h->last_launches;
     if (a.blocks > 1) {
-        e = follow(k_embed_join<T, VEC>, (unsigned)((a.blocks - 1) * a.slices), 256, s, a);
+        e = follow(k_embed_join<T, VEC>, (unsigned)(a.blocks - 1), 256, s, a);
         ++h->last_launches;
     }
     return e;
