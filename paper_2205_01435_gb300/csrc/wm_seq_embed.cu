@@ -138,12 +138,15 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_sort_cluster(const ClusterS
         }
         __syncthreads();
         for (int d = tid; d < digits; d += kSortThreads) {
-            int sum = 0;
+            int c[kSortThreads / 32], sum = 0;
+#pragma unroll
+            for (int q = 0; q < kSortThreads / 32; ++q) c[q] = cnt[q][d];
+#pragma unroll
             for (int q = 0; q < kSortThreads / 32; ++q) {
-                const int c = cnt[q][d];
                 cnt[q][d] = (unsigned short)sum;
-                sum += c;
+                sum += c[q];
             }
+#pragma unroll 4
             for (int q = 0; q < ranks; ++q)
                 asm volatile("st.shared::cluster.b32 [%0], %1;" ::"r"(peer(&all[rank][d], q)), "r"(sum) : "memory");
         }
@@ -152,9 +155,10 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_sort_cluster(const ClusterS
         if (tid < kMaxDigits) {
             int total = 0, mine = 0;
             if (tid < digits)
-                for (int q = 0; q < ranks; ++q) {
+#pragma unroll
+                for (int q = 0; q < kCluster; ++q) {
                     if (q == rank) mine = total;
-                    total += all[q][tid];
+                    if (q < ranks) total += all[q][tid];
                 }
             int s = total;
 #pragma unroll
@@ -380,12 +384,14 @@ __global__ void __launch_bounds__(kSum, 6) k_embed_sum(const SumArgs<T> a) {
     }
 }
 
-// A run that crosses blocks: the CTA of the block where it starts adds its parts.  A warp takes a
-// slice of columns and all blocks; of a run of many blocks the warps take a stretch each, slice by
-// slice, and the stretches are added in order.
+// A run that crosses blocks: the CTA of the block where it starts adds its parts.  Slices of
+// columns go to groups of warps, whose warps take a stretch of the blocks each; the stretches are
+// added in order.
+constexpr int kJoin = 512;
+
 template <class T, int VEC>
-__global__ void __launch_bounds__(256) k_embed_join(const SumArgs<T> a) {
-    constexpr int W = 8, kMany = 16;
+__global__ void __launch_bounds__(kJoin) k_embed_join(const SumArgs<T> a) {
+    constexpr int W = kJoin / 32;
     using F = seq_vec<float, VEC>;
     __shared__ F s[W][32];
     const int b = blockIdx.x, lo = b * a.block, hi = lo + a.block;
@@ -401,32 +407,32 @@ __global__ void __launch_bounds__(256) k_embed_join(const SumArgs<T> a) {
         last = q - 1 + (off ? __ffs(off) - 1 : 32);
         if (off) break;
     }
+    const int per_slice = a.slices < W ? W / a.slices : 1, share = (last - b + per_slice - 1) / per_slice;
+    const int part = w % per_slice, from = b + 1 + part * share, to = min(last + 1, from + share);
     auto add = [&](F &acc, long long row, int j) {
         const F v = *reinterpret_cast<const F *>(a.part + row * a.D + j);
 #pragma unroll
         for (int e = 0; e < VEC; ++e) acc.v[e] += v.v[e];
     };
-    const bool many = last - b > kMany;
-    const int per = many ? (last - b + W - 1) / W : last - b;  // blocks after this one, a warp's share
-    const int from = b + 1 + (many ? w * per : 0), to = min(last + 1, from + per);
-    for (int sl = many ? 0 : w; sl < a.slices; sl += many ? 1 : W) {
-        const int j = (sl * 32 + lane) * VEC;
+    for (int sl0 = 0; sl0 < a.slices; sl0 += W / per_slice) {
+        const int sl = sl0 + w / per_slice, j = (sl * 32 + lane) * VEC;
+        const bool mine = w / per_slice < W / per_slice && sl < a.slices && j < a.D;  // (some warps may be left over)
         F acc = {};
-        if (j < a.D) {
-            if (!many || w == 0) add(acc, (long long)b * 2 + 1, j);
-#pragma unroll 4
+        if (mine) {
+            if (part == 0) add(acc, (long long)b * 2 + 1, j);
+#pragma unroll 8
             for (int q = from; q < to; ++q) add(acc, (long long)q * 2, j);
         }
-        if (many) {
-            __syncthreads();  // (the slice before is read)
+        if (per_slice > 1) {
+            __syncthreads();  // (the slices before are read)
             s[w][lane] = acc;
             __syncthreads();
-            if (w == 0)
-                for (int q = 1; q < W; ++q)
+            if (mine && part == 0)
+                for (int q = 1; q < per_slice; ++q)
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) acc.v[e] += s[q][lane].v[e];
+                    for (int e = 0; e < VEC; ++e) acc.v[e] += s[w + q][lane].v[e];
         }
-        if ((!many || w == 0) && j < a.D) put_row<T, VEC>(a.dtable + (long long)k * a.D + j, acc.v, a.scale);
+        if (mine && part == 0) put_row<T, VEC>(a.dtable + (long long)k * a.D + j, acc.v, a.scale);
     }
 }
 
@@ -493,7 +499,7 @@ cudaError_t sums(wm_seq *h, SumArgs<T> a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     ++h->last_launches;
     if (a.blocks > 1) {
-        e = follow(k_embed_join<T, VEC>, (unsigned)(a.blocks - 1), 256, s, a);
+        e = follow(k_embed_join<T, VEC>, (unsigned)(a.blocks - 1), kJoin, s, a);
         ++h->last_launches;
     }
     return e;

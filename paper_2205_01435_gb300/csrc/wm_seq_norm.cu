@@ -96,12 +96,13 @@ struct Weights {
     float r[SHARED ? 1 : E];
     const float *s;
     __device__ __forceinline__ void load(const float *p, float fill, int D, int lane, float *smem) {
-        if constexpr (SHARED) {  // [E / 4][32] quads: quad q of lane l holds its values 4q ... 4q + 3
+        if constexpr (SHARED) {  // [E / Q][32] of Q values: what lanes read together lies side by side
+            constexpr int Q = VEC % 4 == 0 ? 4 : 1;
             for (int o = threadIdx.x; o < 1024; o += blockDim.x) {
-                const int e = o / 128 * 4 + o % 4, l = o / 4 % 32, j = (e / VEC * TPR + l) * VEC + e % VEC;
+                const int e = o / (32 * Q) * Q + o % Q, l = o / Q % 32, j = (e / VEC * TPR + l) * VEC + e % VEC;
                 smem[o] = p && j < D ? p[j] : fill;
             }
-            s = smem + lane * 4;
+            s = smem + lane * Q;
         } else {
 #pragma unroll
             for (int i = 0; i < E / VEC; ++i)
@@ -112,9 +113,23 @@ struct Weights {
                 }
         }
     }
-    __device__ __forceinline__ float operator[](int e) const {
-        if constexpr (SHARED) return s[e / 4 * 128 + e % 4];
-        else return r[e];
+    // the weights of vector i
+    __device__ __forceinline__ void get(int i, float (&w)[VEC]) const {
+        if constexpr (!SHARED) {
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) w[k] = r[i * VEC + k];
+        } else if constexpr (VEC % 4 == 0) {
+#pragma unroll
+            for (int k = 0; k < VEC; k += 4) {
+                const float4 q = *reinterpret_cast<const float4 *>(s + (i * VEC + k) * 32);
+                w[k] = q.x;
+                w[k + 1] = q.y;
+                w[k + 2] = q.z;
+                w[k + 3] = q.w;
+            }
+        } else {  // one value a vector: [E][32]
+            w[0] = s[i * 32];
+        }
     }
 };
 
@@ -216,8 +231,11 @@ __global__ void __launch_bounds__(cta_threads<TPR>(), fwd_ctas<TPR>())
         for (int i = 0; i < E / VEC; ++i) {
             const int j = (i * TPR + lane) * VEC;
             if (j < D) {
+                float fw[VEC], fb[VEC];
+                ww.get(i, fw);
+                bb.get(i, fb);
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) v[i][k] = fmaf(v[i][k] * rs, ww[i * VEC + k], bb[i * VEC + k]);
+                for (int k = 0; k < VEC; ++k) v[i][k] = fmaf(v[i][k] * rs, fw[k], fb[k]);
                 seq_store(out + j, seq_pack<T, VEC>(v[i]));
             }
         }
@@ -266,13 +284,14 @@ __global__ void __launch_bounds__(cta_threads<TPR>(), bwd_ctas<TPR>())
 #pragma unroll
         for (int i = 0; i < E / VEC; ++i)
             if ((i * TPR + lane) * VEC < D) {
-                float fx[VEC], fd[VEC];
+                float fx[VEC], fd[VEC], fw[VEC];
                 seq_unpack(in.read(0, i, lane), fx);
                 seq_unpack(in.read(1, i, lane), fd);
+                ww.get(i, fw);
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) {
                     const int e = i * VEC + k;
-                    const float xh = (fx[k] - mu) * rs, g = fd[k] * ww[e];
+                    const float xh = (fx[k] - mu) * rs, g = fd[k] * fw[k];
                     dw[e] = fmaf(fd[k], xh, dw[e]);
                     db[e] += fd[k];
                     s.x += g;
@@ -285,13 +304,14 @@ __global__ void __launch_bounds__(cta_threads<TPR>(), bwd_ctas<TPR>())
         for (int i = 0; i < E / VEC; ++i) {
             const int j = (i * TPR + lane) * VEC;
             if (j < D) {
-                float fx[VEC], fd[VEC];
+                float fx[VEC], fd[VEC], fw[VEC];
                 seq_unpack(in.read(0, i, lane), fx);
                 seq_unpack(in.read(1, i, lane), fd);
+                ww.get(i, fw);
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) {
                     const float xh = (fx[k] - mu) * rs;
-                    fd[k] = rs * (fmaf(fd[k], ww[i * VEC + k], -m1) - xh * m2);
+                    fd[k] = rs * (fmaf(fd[k], fw[k], -m1) - xh * m2);
                 }
                 seq_store(out + j, seq_pack<T, VEC>(fd));
             }

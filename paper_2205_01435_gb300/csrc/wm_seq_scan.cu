@@ -46,13 +46,23 @@ struct ScanParams {
 };
 
 // keep and write without cancellation in either.
+//   fp32: from exp(-|p|), which neither overflows nor cancels; the selects make saturated gates exact.
+//   bf16: from exp(-p), p held at -80 where write rounds to 1 (NaN stays): six instructions of the
+//   forward's 20 a value.  The hardware's exponential and reciprocal (2^-21, 2^-23) are far
+//   below the inputs' precision; results below fp32's normal range are 0.
 template <class T>
 __device__ __forceinline__ void gates(float p, float &keep, float &write) {
-    // bf16 inputs: the hardware exponential's relative error (about 2^-21) is far below the inputs'
-    const float e = sizeof(T) == 2 ? __expf(-fabsf(p)) : expf(-fabsf(p));
-    const float s = __fdividef(1.f, 1.f + e), es = e * s;
-    keep = p >= 0.f ? s : es;
-    write = p >= 0.f ? es : s;
+    if constexpr (sizeof(T) == 2) {
+        float e;
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(p) : "f"(p), "f"(-80.f));
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(p * -1.4426950408889634f));
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(keep) : "f"(1.f + e));
+        write = e * keep;
+    } else {
+        const float e = expf(-fabsf(p)), s = __fdividef(1.f, 1.f + e), es = e * s;
+        keep = p >= 0.f ? s : es;
+        write = p >= 0.f ? es : s;
+    }
 }
 
 __device__ __forceinline__ long long live_steps(const int32_t *lengths, int n, long long T, int *status) {
@@ -188,19 +198,19 @@ __global__ void __launch_bounds__(kThreads) k_scan_stream(const ScanParams<T> a)
     if (grp >= a.groups) return;  // (no barrier below)
     const int n = (int)(grp / a.gpr), j = (int)(grp - (long long)n * a.gpr) * VEC;
     const long long c = (long long)n * a.H + j;
-    const long long live = live_steps(a.lengths, n, a.steps, a.status);
+    const int live = (int)live_steps(a.lengths, n, a.steps, a.status);
     float st[VEC];
     read_state<VEC>(st, a.h0, c);
     V *const mine = reinterpret_cast<V *>(ring) + threadIdx.x;
     const uint32_t base = (uint32_t)__cvta_generic_to_shared(mine);
     // the rows of the next step to copy and of the next to write, moved by one step at a time
-    const long long first = BWD ? live - 1 : 0;
+    const long long first = BWD ? live - 1ll : 0;
     const int dir = BWD ? -1 : 1;
     const T *pg = a.gate.row(first, n) + j, *px = a.x.row(first, n) + j;
     const T *pd = BWD ? a.dh.row(first, n) + j : nullptr, *ph = BWD ? a.h_in.row(first - 1, n) + j : nullptr;
     T *o0 = (BWD ? a.dgate.row(first, n) : a.h.row(first, n)) + j, *o1 = BWD ? a.dx.row(first, n) + j : nullptr;
     const uint8_t *pr = RESET ? a.reset + first * a.N + n : nullptr;
-    long long ahead = 0;  // steps whose copies were issued
+    int ahead = 0;  // steps whose copies were issued
     auto issue = [&](int slot) {
 #pragma unroll
         for (int u = 0; u < kGroup; ++u) {
@@ -232,7 +242,7 @@ __global__ void __launch_bounds__(kThreads) k_scan_stream(const ScanParams<T> a)
 #pragma unroll
         for (int u = 0; u < kGroup; ++u)
             if (u < live) cut_next[u] = pr[u * dir * (long long)a.N];
-    for (long long i = 0; i < live; i += kGroup) {
+    for (int i = 0; i < live; i += kGroup) {
         uint8_t cut[kGroup];
 #pragma unroll
         for (int u = 0; u < kGroup; ++u) cut[u] = cut_next[u];
