@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(kSum, 6) k_embed_sum(const SumArgs<T> a) {
 // A run that crosses blocks: the CTA of the block where it starts adds its parts.  Slices of
 // columns go to groups of warps, whose warps take a stretch of the blocks each; the stretches are
 // added in order.
-constexpr int kJoin = 512;
+constexpr int kJoin = 256;
 
 template <class T, int VEC>
 __global__ void __launch_bounds__(kJoin) k_embed_join(const SumArgs<T> a) {

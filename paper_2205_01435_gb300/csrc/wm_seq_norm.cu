@@ -342,17 +342,21 @@ __global__ void __launch_bounds__(cta_threads<TPR>(), bwd_ctas<TPR>())
     }
 }
 
-// dw, db: column sums of the CTAs' partial sums, in a fixed order (32 columns x 16 slices a CTA).
-__global__ void __launch_bounds__(512) k_norm_cols(int parts, int D, const float *__restrict__ part, float *dw, float *db) {
-    __shared__ float s[16][33];
+// dw, db: column sums of the CTAs' partial sums, in a fixed order (32 columns x 32 slices a CTA).
+constexpr int kSlices = 32;
+__global__ void __launch_bounds__(32 * kSlices) k_norm_cols(int parts, int D, const float *__restrict__ part, float *dw, float *db) {
+    __shared__ float s[kSlices][33];
     const int c = blockIdx.x * 32 + threadIdx.x % 32, q = threadIdx.x / 32;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     float v = 0.f;
     if (c < 2 * D)
-        for (int i = q; i < parts; i += 16) v += part[(long long)i * 2 * D + c];
+#pragma unroll 8
+        for (int i = q; i < parts; i += kSlices) v += part[(long long)i * 2 * D + c];
     s[q][threadIdx.x % 32] = v;
     __syncthreads();
     if (q || c >= 2 * D) return;
-    for (int i = 1; i < 16; ++i) v += s[i][threadIdx.x];
+#pragma unroll
+    for (int i = 1; i < kSlices; ++i) v += s[i][threadIdx.x];
     if (c < D) {
         if (dw) dw[c] = v;
     } else if (db) {
@@ -444,7 +448,8 @@ bool vec_ok(const void *p, long long ld, int D, size_t es) {
 }
 
 // Threads per row and values per thread: the fewest of each that hold the row (a warp up to 1024
-// values, so that its sums need no barrier).
+// values, so that its sums need no barrier: 65536 x 1024 bf16 backward took 80 us so, and 90 us with
+// 128 threads a row).
 struct Shape {
     int tpr, e;
 };
@@ -567,7 +572,18 @@ cudaError_t wm_seq_norm_backward_launch(wm_seq *h, int dtype, long long rows, in
         h->last_launches = 1;
     }
     if (dw || db) {  // no rows: zeros
-        k_norm_cols<<<(2 * D + 31) / 32, 512, 0, s>>>(grid, D, part, dw, db);
+        // (may start while the rows' kernel still runs: it waits for it itself)
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3((unsigned)((2 * (long long)D + 31) / 32));
+        cfg.blockDim = dim3(32 * kSlices);
+        cfg.stream = s;
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        at[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 1;
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, k_norm_cols, grid, D, (const float *)part, dw, db);
+        if (e != cudaSuccess) return e;
         ++h->last_launches;
     }
     return cudaGetLastError();
