@@ -186,21 +186,21 @@ __global__ void __launch_bounds__(kThreads) k_scan_walk(const ScanParams<T> a) {
 }
 
 // ---- many channels: a thread's inputs stream through a ring of its own -------------------
-// The ring holds GROUPS groups of kGroup steps; a group is one set of asynchronous copies.
-constexpr int kGroup = 2;
-
-template <class T, int VEC, bool BWD, bool RESET, int GROUPS>
+// The ring holds GROUPS groups of KG steps; a group is one set of asynchronous copies, and its
+// steps are worked on together: their gates do not wait for one another, only the state does.
+template <class T, int VEC, bool BWD, bool RESET, int KG, int GROUPS>
 __global__ void __launch_bounds__(kThreads) k_scan_stream(const ScanParams<T> a) {
     using V = seq_vec<T, VEC>;
     constexpr int ARRAYS = BWD ? 4 : 2, BYTES = sizeof(V);
-    extern __shared__ __align__(16) unsigned char ring[];  // [GROUPS * kGroup][ARRAYS][kThreads] of V
+    extern __shared__ __align__(16) unsigned char ring[];  // [GROUPS * KG][ARRAYS][kThreads] of V
     const long long grp = (long long)blockIdx.x * kThreads + threadIdx.x;
     if (grp >= a.groups) return;  // (no barrier below)
     const int n = (int)(grp / a.gpr), j = (int)(grp - (long long)n * a.gpr) * VEC;
     const long long c = (long long)n * a.H + j;
     const int live = (int)live_steps(a.lengths, n, a.steps, a.status);
-    float st[VEC];
+    float st[VEC], init[VEC];
     read_state<VEC>(st, a.h0, c);
+    if (BWD) read_state<VEC>(init, a.h_init, c);
     V *const mine = reinterpret_cast<V *>(ring) + threadIdx.x;
     const uint32_t base = (uint32_t)__cvta_generic_to_shared(mine);
     // the rows of the next step to copy and of the next to write, moved by one step at a time
@@ -210,12 +210,13 @@ __global__ void __launch_bounds__(kThreads) k_scan_stream(const ScanParams<T> a)
     const T *pd = BWD ? a.dh.row(first, n) + j : nullptr, *ph = BWD ? a.h_in.row(first - 1, n) + j : nullptr;
     T *o0 = (BWD ? a.dgate.row(first, n) : a.h.row(first, n)) + j, *o1 = BWD ? a.dx.row(first, n) + j : nullptr;
     const uint8_t *pr = RESET ? a.reset + first * a.N + n : nullptr;
+    const long long rn = dir * (long long)a.N;
     int ahead = 0;  // steps whose copies were issued
     auto issue = [&](int slot) {
 #pragma unroll
-        for (int u = 0; u < kGroup; ++u) {
+        for (int u = 0; u < KG; ++u) {
             if (ahead < live) {
-                const uint32_t to = base + (uint32_t)(slot * kGroup + u) * (ARRAYS * kThreads * BYTES);
+                const uint32_t to = base + (uint32_t)(slot * KG + u) * (ARRAYS * kThreads * BYTES);
                 copy_async<BYTES>(to, pg);
                 copy_async<BYTES>(to + kThreads * BYTES, px);
                 if (BWD) {
@@ -237,42 +238,55 @@ __global__ void __launch_bounds__(kThreads) k_scan_stream(const ScanParams<T> a)
 #pragma unroll
     for (int q = 0; q < GROUPS - 1; ++q) issue(q);
     int slot = 0;
-    uint8_t cut_next[kGroup] = {};
-    if (RESET)
-#pragma unroll
-        for (int u = 0; u < kGroup; ++u)
-            if (u < live) cut_next[u] = pr[u * dir * (long long)a.N];
-    for (int i = 0; i < live; i += kGroup) {
-        uint8_t cut[kGroup];
-#pragma unroll
-        for (int u = 0; u < kGroup; ++u) cut[u] = cut_next[u];
+    uint8_t cut_next[KG] = {};
+    auto marks = [&](int i) {  // the group's that starts at step i
         if (RESET) {
-            pr += kGroup * dir * (long long)a.N;
 #pragma unroll
-            for (int u = 0; u < kGroup; ++u)
-                if (i + kGroup + u < live) cut_next[u] = pr[u * dir * (long long)a.N];
+            for (int u = 0; u < KG; ++u)
+                if (i + u < live) cut_next[u] = pr[u * rn];
+            pr += KG * rn;
         }
+    };
+    marks(0);
+    for (int i = 0; i < live; i += KG) {
+        bool cut[KG];
+#pragma unroll
+        for (int u = 0; u < KG; ++u) cut[u] = RESET && cut_next[u];
+        marks(i + KG);
         issue(slot == 0 ? GROUPS - 1 : slot - 1);
         copy_wait<GROUPS - 1>();
-#pragma unroll
-        for (int u = 0; u < kGroup; ++u) {
-            if (i + u >= live) break;
-            const V *r = mine + (slot * kGroup + u) * (ARRAYS * kThreads);
-            const bool ct = RESET && cut[u];
+        const V *r = mine + slot * KG * (ARRAYS * kThreads);
+        auto step = [&](const V &g, const V &x, const V &d, const V &h, int u) {
             if (!BWD) {
-                seq_store(o0, step_fwd<T, VEC>(r[0], r[kThreads], ct, st));
+                seq_store(o0, step_fwd<T, VEC>(g, x, cut[u], st));
                 o0 += a.h.st;
             } else {
                 float before[VEC];
-                if (i + u + 1 < live) seq_unpack(r[3 * kThreads], before);
-                else read_state<VEC>(before, a.h_init, c);
+                seq_unpack(h, before);
+                if (i + u + 1 == live)
+#pragma unroll
+                    for (int k = 0; k < VEC; ++k) before[k] = init[k];
                 V dgate, dx;
-                step_bwd<T, VEC>(r[0], r[kThreads], r[2 * kThreads], before, ct, st, dgate, dx);
+                step_bwd<T, VEC>(g, x, d, before, cut[u], st, dgate, dx);
                 seq_store(o0, dgate);
                 seq_store(o1, dx);
                 o0 -= a.dgate.st;
                 o1 -= a.dx.st;
             }
+        };
+        auto read = [&](int u, int array) { return r[(u * ARRAYS + (BWD ? array : min(array, 1))) * kThreads]; };
+        if (i + KG <= live) {
+            V v[KG][ARRAYS];
+#pragma unroll
+            for (int u = 0; u < KG; ++u)
+#pragma unroll
+                for (int q = 0; q < ARRAYS; ++q) v[u][q] = read(u, q);
+#pragma unroll
+            for (int u = 0; u < KG; ++u) step(v[u][0], v[u][1], v[u][ARRAYS - 2], v[u][ARRAYS - 1], u);
+        } else {
+#pragma unroll
+            for (int u = 0; u < KG - 1; ++u)
+                if (i + u < live) step(read(u, 0), read(u, 1), read(u, 2), read(u, 3), u);
         }
         slot = slot + 1 == GROUPS ? 0 : slot + 1;
     }
@@ -599,16 +613,19 @@ cudaError_t walk(const wm_seq *h, const seq_scan_args &a, cudaStream_t s) {
     return cudaGetLastError();
 }
 
-template <class T, int VEC, bool BWD, bool RESET, int GROUPS>
-cudaError_t stream_launch(const ScanParams<T> &q, size_t smem, cudaStream_t s) {
-    auto *k = k_scan_stream<T, VEC, BWD, RESET, GROUPS>;
-    cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-    if (e != cudaSuccess) return e;
+template <class T, int VEC, bool BWD, bool RESET, int KG, int GROUPS>
+cudaError_t stream_launch(const ScanParams<T> &q, size_t step, cudaStream_t s) {
+    auto *k = k_scan_stream<T, VEC, BWD, RESET, KG, GROUPS>;
+    const size_t smem = KG * GROUPS * step;
+    if (smem > 40 << 10) {
+        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
     k<<<blocks(q.groups), kThreads, smem, s>>>(q);
     return cudaGetLastError();
 }
 
-// The deepest ring with which all CTAs run at once; 6 steps when there are more CTAs than that.
+// The deepest ring with which all CTAs run at once; the smallest when there are more CTAs than that.
 template <class T, int VEC, bool BWD>
 cudaError_t stream(const wm_seq *h, const seq_scan_args &a, cudaStream_t s) {
     const ScanParams<T> q = params<T>(h, a, VEC, BWD);
@@ -617,9 +634,9 @@ cudaError_t stream(const wm_seq *h, const seq_scan_args &a, cudaStream_t s) {
     const size_t room = (size_t)(220 << 10) / per_sm;
     auto go = [&](auto reset) {
         constexpr bool R = decltype(reset)::value;
-        if (room >= 12 * kGroup * step + 1024) return stream_launch<T, VEC, BWD, R, 12>(q, 12 * kGroup * step, s);
-        if (room >= 6 * kGroup * step + 1024) return stream_launch<T, VEC, BWD, R, 6>(q, 6 * kGroup * step, s);
-        return stream_launch<T, VEC, BWD, R, 3>(q, 3 * kGroup * step, s);
+        if (room >= 24 * step + 1024) return stream_launch<T, VEC, BWD, R, 4, 6>(q, step, s);
+        if (room >= 12 * step + 1024) return stream_launch<T, VEC, BWD, R, 4, 3>(q, step, s);
+        return stream_launch<T, VEC, BWD, R, 2, 3>(q, step, s);
     };
     return a.reset ? go(std::true_type{}) : go(std::false_type{});
 }
