@@ -19,8 +19,8 @@
 //                  that hold no registers; every thread waits for its own copies only.
 //   k_scan_spans   few channels: time is cut into spans of L steps, one per warp and all at once;
 //                  a CTA joins its spans in shared memory and finds the state entering them from
-//                  the (P, S) that the CTAs before it publish.  The spans' gates and values stay
-//                  in registers between the two passes.
+//                  the (P, S) that the CTAs before it publish.  The spans' inputs stay in shared
+//                  memory between the two passes.
 #include <type_traits>
 
 #include "wm_seq_internal.h"
@@ -370,10 +370,19 @@ struct Published {
 };
 
 // DEEP: more than one chunk per tile.  Logical step i is t = i, or T - 1 - i backward.
+//
+// The inputs wait in shared memory, every thread's in places of its own, while the chunk's (P, S)
+// goes out and the state entering it comes in, and the gates are formed again for the outputs:
+// six more instructions a value, but 64 registers a thread and so twice the CTAs.  (With the
+// gates kept in registers, 2 CTAs an SM, a chunk took 9,300 cycles, two thirds of it spent
+// waiting; 65,536 x 256 forward took 50 us.)
 template <class T, int VEC, int L, bool BWD, bool RESET, bool DEEP>
-__global__ void __launch_bounds__(kSpanThreads, 2) k_scan_spans(const ScanParams<T> a, const SpanWork wk) {
+__global__ void __launch_bounds__(kSpanThreads, 4) k_scan_spans(const ScanParams<T> a, const SpanWork wk) {
     using V = seq_vec<T, VEC>;
-    constexpr int W = 32 * VEC, PARTS = kSpanThreads / W, EACH = 32 / PARTS;
+    constexpr int W = 32 * VEC, PARTS = kSpanThreads / W, EACH = 32 / PARTS, ARRAYS = BWD ? 4 : 2;
+    constexpr int GATE = 0, X = 1, DH = 2, HB = 3;
+    constexpr bool ASYNC = sizeof(V) >= 4;
+    extern __shared__ __align__(16) unsigned char held[];  // [L][ARRAYS][kSpanThreads] of V
     __shared__ float2 spans[SUBS][W], near[DEEP ? PARTS : 1][W], far[DEEP ? PARTS : 1][W];
     __shared__ float enter[W];
     __shared__ unsigned s_ticket;
@@ -384,39 +393,34 @@ __global__ void __launch_bounds__(kSpanThreads, 2) k_scan_spans(const ScanParams
         ticket = s_ticket;
     }
     const int chunk = DEEP ? (int)(ticket / (unsigned)wk.tiles) : 0, tile = (int)(ticket - (unsigned)chunk * (unsigned)wk.tiles);
-    const int lane = threadIdx.x % 32, sub = threadIdx.x / 32;
+    const int lane = threadIdx.x % 32, sub = threadIdx.x / 32, dir = BWD ? -1 : 1;
     const int n = tile / wk.tiles_per_n, j0 = (tile - n * wk.tiles_per_n) * W, j = j0 + lane * VEC;
     const bool mine = j < a.H;
-    const long long c = (long long)n * a.H + j, T_ = a.steps;
-    const long long live = live_steps(a.lengths, n, T_, a.status);
+    const long long c = (long long)n * a.H + j;
+    const int T_ = (int)a.steps, live = (int)live_steps(a.lengths, n, a.steps, a.status);
     const long long i0 = ((long long)chunk * SUBS + sub) * L, t0 = BWD ? T_ - 1 - i0 : i0;
-    const int dir = BWD ? -1 : 1;
     // the span's steps u in [0, steps) exist, and those in [skip, count) are not padding
     const int steps = (int)max(0ll, min((long long)L, T_ - i0));
     const int skip = BWD ? (int)max(0ll, min((long long)L, t0 - live + 1)) : 0;
-    const int count = BWD ? steps : (int)max(0ll, min((long long)L, live - i0));
-
-    // per step: A and B, and what the second pass takes besides
-    float A[L][VEC], B[BWD ? 1 : L][VEC], wr[BWD ? L : 1][VEC], df[BWD ? L : 1][VEC];
-    V rd[BWD ? L : 1];  // backward: B is dh, as it came
-    float P[VEC], S[VEC];
-#pragma unroll
-    for (int k = 0; k < VEC; ++k) {
-        P[k] = 1.f;
-        S[k] = 0.f;
-    }
-    unsigned cuts = 0;
+    const int count = mine ? BWD ? steps : (int)max(0ll, min((long long)L, live - i0)) : 0;
+    V *const own_v = reinterpret_cast<V *>(held) + threadIdx.x;
+    auto at = [&](int u, int array) -> V & { return own_v[(u * ARRAYS + array) * kSpanThreads]; };
     {
-        V rg[L], rx[L], rh[BWD ? L : 1];
         const T *pg = a.gate.row(t0, n) + j, *px = a.x.row(t0, n) + j;
         const T *pd = BWD ? a.dh.row(t0, n) + j : nullptr, *ph = BWD ? a.h_in.row(t0 - 1, n) + j : nullptr;
+        auto bring = [&](int u, int array, const T *p) {
+            if constexpr (ASYNC) copy_async<(int)sizeof(V)>((uint32_t)__cvta_generic_to_shared(&at(u, array)), p);
+            else at(u, array) = seq_load<T, VEC>(p);
+        };
 #pragma unroll
         for (int u = 0; u < L; ++u) {
-            if (mine && u >= skip && u < count) {
-                rg[u] = seq_load<T, VEC>(pg);
-                rx[u] = seq_load<T, VEC>(px);
-                if (BWD) rd[u] = seq_load<T, VEC>(pd);
-                if (BWD && t0 > u) rh[u] = seq_load<T, VEC>(ph);
+            if (u >= skip && u < count) {
+                bring(u, GATE, pg);
+                bring(u, X, px);
+                if (BWD) {
+                    bring(u, DH, pd);
+                    if (t0 > u) bring(u, HB, ph);
+                }
             }
             pg += dir * a.gate.st;
             px += dir * a.x.st;
@@ -425,47 +429,33 @@ __global__ void __launch_bounds__(kSpanThreads, 2) k_scan_spans(const ScanParams
                 ph -= a.h_in.st;
             }
         }
-        if (RESET)  // lane u has step u's
-            cuts = __ballot_sync(0xffffffffu, lane >= skip && lane < count && a.reset[(t0 + dir * lane) * a.N + n] != 0);
+        if (ASYNC) copy_commit();
+    }
+    unsigned cuts = 0;
+    if (RESET) {  // lane u has step u's
+        const bool in = lane >= skip && lane < (BWD ? steps : (int)min((long long)L, live - i0));
+        cuts = __ballot_sync(0xffffffffu, in && a.reset[(t0 + dir * lane) * a.N + n] != 0);
+    }
+    float P[VEC], S[VEC];
 #pragma unroll
-        for (int u = 0; u < L; ++u) {
-            const bool cut = RESET && (cuts >> u & 1);
-            if (mine && u >= skip && u < count) {
-                float g[VEC], x[VEC], d[VEC], hb[VEC];
-                seq_unpack(rg[u], g);
-                seq_unpack(rx[u], x);
-                if (BWD) {
-                    seq_unpack(rd[u], d);
-                    if (t0 > u) seq_unpack(rh[u], hb);
-                    else read_state<VEC>(hb, a.h_init, c);
-                }
+    for (int k = 0; k < VEC; ++k) {
+        P[k] = 1.f;
+        S[k] = 0.f;
+    }
+    if (ASYNC) copy_wait<0>();
+#pragma unroll 4
+    for (int u = skip; u < count; ++u) {
+        const bool cut = RESET && (cuts >> u & 1);
+        float g[VEC], y[VEC];
+        seq_unpack(at(u, GATE), g);
+        seq_unpack(at(u, BWD ? DH : X), y);
 #pragma unroll
-                for (int k = 0; k < VEC; ++k) {
-                    float keep, write;
-                    gates<T>(g[k], keep, write);
-                    A[u][k] = keep;
-                    if (!BWD) {
-                        B[u][k] = write * x[k];
-                        S[k] = fmaf(keep, cut ? 0.f : S[k], B[u][k]);
-                    } else {
-                        wr[u][k] = write;
-                        df[u][k] = ((cut ? 0.f : hb[k]) - x[k]) * keep;  // times dx gives dgate
-                        S[k] = cut ? 0.f : keep * (d[k] + S[k]);
-                    }
-                    P[k] = cut ? -1.f : P[k] * keep;
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < VEC; ++k) {
-                    A[u][k] = 1.f;
-                    if (BWD) {
-                        wr[u][k] = df[u][k] = 0.f;
-                        rd[u].v[k] = seq_from_float<T>(0.f);
-                    } else {
-                        B[u][k] = 0.f;
-                    }
-                }
-            }
+        for (int k = 0; k < VEC; ++k) {
+            float keep, write;
+            gates<T>(g[k], keep, write);
+            if (!BWD) S[k] = fmaf(keep, cut ? 0.f : S[k], write * y[k]);
+            else S[k] = cut ? 0.f : keep * (y[k] + S[k]);
+            P[k] = cut ? -1.f : P[k] * keep;
         }
     }
 #pragma unroll
@@ -473,15 +463,18 @@ __global__ void __launch_bounds__(kSpanThreads, 2) k_scan_spans(const ScanParams
     __syncthreads();
     // a thread per channel and part from here on
     const int ch = threadIdx.x % W, part = threadIdx.x / W;
-    const int group = chunk >> 5, in_group = chunk & 31, section = group >> 5, in_section = group & 31;
     const bool more = chunk + 1 < wk.chunks;
     float2 own = make_float2(1.f, 0.f);
     if (part == 0) {
-        own = spans[0][ch];
+        float2 v[SUBS];
 #pragma unroll
-        for (int q = 1; q < SUBS; ++q) own = join(own, spans[q][ch]);
+        for (int q = 0; q < SUBS; ++q) v[q] = spans[q][ch];
+        own = v[0];
+#pragma unroll
+        for (int q = 1; q < SUBS; ++q) own = join(own, v[q]);
     }
     if (DEEP) {
+        const int group = chunk >> 5, in_group = chunk & 31, section = group >> 5, in_section = group & 31;
         unsigned long long *cp = wk.chunk_ps + ((long long)tile * wk.groups + group) * 32 * W + ch;
         unsigned long long *gp = wk.group_ps + ((long long)tile * wk.sections + section) * 32 * W + ch;
         unsigned long long *sp = wk.section + ((long long)tile * wk.sections + section) * W + ch;
@@ -541,30 +534,41 @@ __global__ void __launch_bounds__(kSpanThreads, 2) k_scan_spans(const ScanParams
         for (int q = 0; q < sub; ++q) mid[k] = through(spans[q][lane * VEC + k], mid[k]);
     }
     T *o0 = (BWD ? a.dgate.row(t0, n) : a.h.row(t0, n)) + j, *o1 = BWD ? a.dx.row(t0, n) + j : nullptr;
+    const long long d0 = dir * (BWD ? a.dgate.st : a.h.st);
+    const V zero = [] {
+        V z;
 #pragma unroll
-    for (int u = 0; u < L; ++u) {
-        const bool cut = RESET && (cuts >> u & 1);
-        float f0[VEC], f1[VEC], d[VEC];
-        if (BWD) seq_unpack(rd[u], d);
-#pragma unroll
-        for (int k = 0; k < VEC; ++k) {
-            if (!BWD) {
-                mid[k] = fmaf(A[u][k], cut ? 0.f : mid[k], B[u][k]);
-                f0[k] = u < count ? mid[k] : 0.f;
-            } else {
-                const float dL = d[k] + mid[k];
-                f1[k] = u >= skip ? dL * wr[u][k] : 0.f;
-                f0[k] = u >= skip ? dL * wr[u][k] * df[u][k] : 0.f;
-                mid[k] = cut ? 0.f : A[u][k] * dL;
-            }
-        }
-        if (mine && u < steps) {
-            seq_store(o0, seq_pack<T, VEC>(f0));
-            if (BWD) seq_store(o1, seq_pack<T, VEC>(f1));
-        }
-        o0 += dir * (BWD ? a.dgate.st : a.h.st);
-        if (BWD) o1 -= a.dx.st;
+        for (int k = 0; k < VEC; ++k) z.v[k] = seq_from_float<T>(0.f);
+        return z;
+    }();
+    for (int u = 0; u < (mine ? skip : 0); ++u) {  // (backward only)
+        seq_store(o0, zero);
+        seq_store(o1, zero);
+        o0 += d0;
+        o1 -= a.dx.st;
     }
+#pragma unroll 4
+    for (int u = skip; u < count; ++u) {
+        const bool cut = RESET && (cuts >> u & 1);
+        if (!BWD) {
+            seq_store(o0, step_fwd<T, VEC>(at(u, GATE), at(u, X), cut, mid));
+        } else {
+            float before[VEC];
+            if (t0 > u) seq_unpack(at(u, HB), before);
+            else read_state<VEC>(before, a.h_init, c);
+            V dgate, dx;
+            step_bwd<T, VEC>(at(u, GATE), at(u, X), at(u, DH), before, cut, mid, dgate, dx);
+            seq_store(o0, dgate);
+            seq_store(o1, dx);
+            o1 -= a.dx.st;
+        }
+        o0 += d0;
+    }
+    if (!BWD)
+        for (int u = count; u < (mine ? steps : 0); ++u) {
+            seq_store(o0, zero);
+            o0 += d0;
+        }
 }
 
 __global__ void k_scan_state(long long C, const float *h0, float *last) {
@@ -643,7 +647,7 @@ cudaError_t stream(const wm_seq *h, const seq_scan_args &a, cudaStream_t s) {
 
 // What a call does: its kernel, the values per access, the steps per span and the layout of the
 // workspace.
-constexpr int kLenFwd = 16, kLenBwd16 = 12, kLenBwd32 = 12, kLenShort = 4;
+constexpr int kLenFwd = 16, kLenBwd = 8, kLenShort = 4;
 struct Plan {
     enum Kind { WALK, STREAM, SPANS } kind;
     int vec, len;
@@ -662,13 +666,13 @@ Plan plan(const wm_seq *h, const seq_scan_args &a, bool bwd) {
         p.kind = Plan::STREAM;
     } else {
         p.kind = Plan::SPANS;
-        if (p.vec > w4) p.vec = w4;  // rows of 128 bytes: wider tiles have shorter spans for the same registers
+        if (p.vec > w4) p.vec = w4;  // rows of 128 bytes: wider tiles have shorter spans for the same room
         const int W = 32 * p.vec;
         SpanWork &k = p.wk;
         k.tiles_per_n = (a.H + W - 1) / W;
         k.tiles = a.N * k.tiles_per_n;
-        // the longest spans that the registers hold; short ones when those leave SMs idle
-        p.len = bwd ? (w4 == 2 ? kLenBwd16 : kLenBwd32) : kLenFwd;
+        // spans as long as four CTAs an SM have room for; short ones when those leave SMs idle
+        p.len = bwd ? kLenBwd : kLenFwd;
         if ((a.T + SUBS * p.len - 1) / (SUBS * p.len) * k.tiles < h->sms) p.len = kLenShort;
         k.chunks = (int)((a.T + SUBS * p.len - 1) / (SUBS * p.len));
         k.groups = (k.chunks + 31) / 32;
@@ -700,7 +704,13 @@ cudaError_t spans(wm_seq *h, const seq_scan_args &a, const Plan &p, cudaStream_t
     }
     auto *k = a.reset ? (deep ? k_scan_spans<T, VEC, L, BWD, true, true> : k_scan_spans<T, VEC, L, BWD, true, false>)
                       : (deep ? k_scan_spans<T, VEC, L, BWD, false, true> : k_scan_spans<T, VEC, L, BWD, false, false>);
-    k<<<(unsigned)((long long)wk.tiles * wk.chunks), kSpanThreads, 0, s>>>(q, wk);
+    using V = seq_vec<T, VEC>;
+    const size_t smem = (size_t)L * (BWD ? 4 : 2) * kSpanThreads * sizeof(V);
+    if (smem > 24 << 10) {
+        const cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    k<<<(unsigned)((long long)wk.tiles * wk.chunks), kSpanThreads, smem, s>>>(q, wk);
     return cudaGetLastError();
 }
 
@@ -711,7 +721,7 @@ cudaError_t dispatch(wm_seq *h, const seq_scan_args &a, cudaStream_t s) {
     if (p.kind == Plan::WALK)
         return p.vec == 2 * W4 ? walk<T, 2 * W4, BWD>(h, a, s) : p.vec == W4 ? walk<T, W4, BWD>(h, a, s) : walk<T, 1, BWD>(h, a, s);
     if (p.kind == Plan::STREAM) return p.vec == 2 * W4 ? stream<T, 2 * W4, BWD>(h, a, s) : stream<T, W4, BWD>(h, a, s);
-    constexpr int LONG = !BWD ? kLenFwd : sizeof(T) == 2 ? kLenBwd16 : kLenBwd32;
+    constexpr int LONG = BWD ? kLenBwd : kLenFwd;
     if (p.vec == W4) return p.len == LONG ? spans<T, W4, LONG, BWD>(h, a, p, s) : spans<T, W4, kLenShort, BWD>(h, a, p, s);
     return p.len == LONG ? spans<T, 1, LONG, BWD>(h, a, p, s) : spans<T, 1, kLenShort, BWD>(h, a, p, s);
 }
