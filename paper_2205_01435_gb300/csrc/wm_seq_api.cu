@@ -221,7 +221,7 @@ extern "C" wm_status wm_seq_embed_backward(wm_seq *h, int dtype, long long n, in
     c.array(dout, esize(dtype), n > 0, "dout is NULL");
     c.array(dtable, esize(dtype), true, "dtable is NULL");
     SEQ_CHECKED();
-    const wm_status st = reserve(h, wm_seq_embed_backward_ws(h, dtype, n, V, D), s, kWhat);
+    const wm_status st = reserve(h, wm_seq_embed_backward_ws(h, dtype, n, V, D, dout, dtable), s, kWhat);
     if (st != WM_OK) return st;
     return launched(h, wm_seq_embed_backward_launch(h, dtype, n, V, D, tokens, dout, scale, dtable, s), kWhat);
 }

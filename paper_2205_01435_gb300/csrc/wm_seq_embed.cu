@@ -13,6 +13,8 @@
 // once; of a run that crosses blocks each block leaves a partial row, and a third launch adds
 // these in order.  Rows that no token took (the sort marks those that one did) are filled
 // with zeros by warps of the second.
+#include <type_traits>
+
 #include "wm_seq_internal.h"
 
 namespace {
@@ -289,7 +291,7 @@ constexpr int kSum = 128;
 
 template <class T>
 struct SumArgs {
-    int n, V, D, block, blocks, slices;  // sorted positions a block; slices of 32 * VEC columns
+    int n, V, D, block, blocks, slices;  // sorted positions a block; slices of 32 * VEC * lane_vectors columns
     int zero_warps;                      // warps that look for absent rows (32 rows each)
     const int *key, *pos;
     const uint8_t *present;
@@ -298,6 +300,13 @@ struct SumArgs {
     float scale;
     float *part;  // [blocks][2][D]: a run that came in from the block before; one that goes on
 };
+
+// Vectors of a slice per lane: narrow accesses take more of them, so that a warp's share of a row is
+// 256 bytes and more.
+template <class T, int VEC>
+constexpr int lane_vectors() {
+    return VEC * sizeof(T) >= 8 ? 1 : VEC * sizeof(T) == 4 ? 2 : 4;
+}
 
 template <int VEC>
 __device__ __forceinline__ void put(float *p, const float (&v)[VEC]) {
@@ -328,15 +337,14 @@ __global__ void __launch_bounds__(kSum, 6) k_embed_sum(const SumArgs<T> a) {
     }
     unit -= a.zero_warps;
     if (unit >= (long long)a.blocks * a.slices) return;
-    const int b = (int)(unit / a.slices), j = ((int)(unit % a.slices) * 32 + lane) * VEC;
+    constexpr int R = lane_vectors<T, VEC>(), U = 8 / R < 4 ? 4 : 8 / R;  // vectors of a row per lane; rows in flight
+    const int b = (int)(unit / a.slices), j0 = ((int)(unit % a.slices) * 32 * R + lane) * VEC;  // columns j0 + r * 32 * VEC
     const int lo = b * a.block, hi = min(a.n, lo + a.block);
-    const bool mine = j < a.D;
-    const T *col = a.dout + (mine ? j : 0);
+    auto mine = [&](int r) { return j0 + r * 32 * VEC < a.D; };
     // the key before the block, and whether the current run is the block's first
     const int prev = lo > 0 ? a.key[lo - 1] : -1;
     bool head = true;
-    float acc[VEC] = {};
-    constexpr int U = 8;
+    float acc[R][VEC] = {};
     // 32 keys at a time, and the one after the block (-1: after the last)
     auto key_at = [&](int i) { return i <= hi && i < a.n ? a.key[i] : -1; };
     auto pos_at = [&](int i) { return i < hi ? a.pos[i] : 0; };
@@ -351,31 +359,40 @@ __global__ void __launch_bounds__(kSum, 6) k_embed_sum(const SumArgs<T> a) {
         const unsigned ends = __ballot_sync(0xffffffffu, after != key || at + lane + 1 == hi);
 #pragma unroll 1
         for (int q0 = 0; q0 < m; q0 += U) {
-            seq_vec<T, VEC> v[U];
+            seq_vec<T, VEC> v[U][R];
 #pragma unroll
             for (int u = 0; u < U; ++u) {  // (past m: row 0, or a row that is not used)
                 const int p = __shfl_sync(0xffffffffu, pos, (q0 + u) & 31);
-                v[u] = seq_load<T, VEC>(col + (long long)p * a.D);
+                const T *row = a.dout + (long long)p * a.D;
+#pragma unroll
+                for (int r = 0; r < R; ++r) v[u][r] = seq_load<T, VEC>(row + (mine(r) ? j0 + r * 32 * VEC : 0));
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int q = q0 + u;
                 if (q >= m) break;
-                float f[VEC];
-                seq_unpack(v[u], f);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) acc[e] += f[e];
+                for (int r = 0; r < R; ++r) {
+                    float f[VEC];
+                    seq_unpack(v[u][r], f);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) acc[r][e] += f[e];
+                }
                 if (!(ends >> q & 1)) continue;
                 // the run ends here, or leaves the block
                 const int k = __shfl_sync(0xffffffffu, key, q), nk = __shfl_sync(0xffffffffu, after, q);
-                if (mine) {
-                    const bool came = head && k == prev, goes = nk == k;
-                    if (came) put<VEC>(a.part + ((long long)b * 2) * a.D + j, acc);
-                    else if (goes) put<VEC>(a.part + ((long long)b * 2 + 1) * a.D + j, acc);
-                    else put_row<T, VEC>(a.dtable + (long long)k * a.D + j, acc, a.scale);
-                }
+                const bool came = head && k == prev, goes = nk == k;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+                for (int r = 0; r < R; ++r) {
+                    const int j = j0 + r * 32 * VEC;
+                    if (mine(r)) {
+                        if (came) put<VEC>(a.part + ((long long)b * 2) * a.D + j, acc[r]);
+                        else if (goes) put<VEC>(a.part + ((long long)b * 2 + 1) * a.D + j, acc[r]);
+                        else put_row<T, VEC>(a.dtable + (long long)k * a.D + j, acc[r], a.scale);
+                    }
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) acc[r][e] = 0.f;
+                }
                 head = false;
             }
         }
@@ -384,16 +401,16 @@ __global__ void __launch_bounds__(kSum, 6) k_embed_sum(const SumArgs<T> a) {
     }
 }
 
-// A run that crosses blocks: the CTA of the block where it starts adds its parts.  Slices of
-// columns go to groups of warps, whose warps take a stretch of the blocks each; the stretches are
-// added in order.
-constexpr int kJoin = 256;
+// A run that crosses blocks: the CTAs of the block where it starts add its parts, a CTA four slices of
+// 128 columns.  A slice goes to a group of warps, whose warps take a stretch of the blocks each;
+// the stretches are added in order.
+constexpr int kJoin = 256, kJoinColumns = 128, kJoinSlices = 4;
 
 template <class T, int VEC>
 __global__ void __launch_bounds__(kJoin) k_embed_join(const SumArgs<T> a) {
-    constexpr int W = kJoin / 32;
-    using F = seq_vec<float, VEC>;
-    __shared__ F s[W][32];
+    constexpr int W = kJoin / 32, JV = VEC >= 4 ? 4 : 1, R = 4 / JV;  // a lane's columns: R times JV
+    using F = seq_vec<float, JV>;
+    __shared__ float s[W][R * JV][32];
     const int b = blockIdx.x, lo = b * a.block, hi = lo + a.block;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int k = a.key[hi - 1], k_next = a.key[hi], k_lo = a.key[lo], k_prev = lo > 0 ? a.key[lo - 1] : -1;
@@ -407,33 +424,50 @@ __global__ void __launch_bounds__(kJoin) k_embed_join(const SumArgs<T> a) {
         last = q - 1 + (off ? __ffs(off) - 1 : 32);
         if (off) break;
     }
-    const int per_slice = a.slices < W ? W / a.slices : 1, share = (last - b + per_slice - 1) / per_slice;
-    const int part = w % per_slice, from = b + 1 + part * share, to = min(last + 1, from + share);
-    auto add = [&](F &acc, long long row, int j) {
-        const F v = *reinterpret_cast<const F *>(a.part + row * a.D + j);
+    const int all = (a.D + kJoinColumns - 1) / kJoinColumns, first = blockIdx.y * kJoinSlices, slices = min(kJoinSlices, all - first);
+    const int warps = W / slices, share = (last - b + warps - 1) / warps;  // warps a slice; blocks a warp
+    const int sl = w / warps, part = w % warps, from = b + 1 + part * share, to = min(last + 1, from + share);
+    const int j0 = (first + sl) * kJoinColumns + lane * JV;
+    float acc[R * JV] = {};
+    if (sl < slices) {
+        // eight partial rows at a time: the run's first, then this warp's stretch (past its end: row 0, not added)
+        const bool own = part == 0;
+        const int rows = max(0, to - from) + own;
+        for (int q0 = 0; q0 < rows; q0 += 8) {
+            F v[8][R];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) acc.v[e] += v.v[e];
-    };
-    for (int sl0 = 0; sl0 < a.slices; sl0 += W / per_slice) {
-        const int sl = sl0 + w / per_slice, j = (sl * 32 + lane) * VEC;
-        const bool mine = w / per_slice < W / per_slice && sl < a.slices && j < a.D;  // (some warps may be left over)
-        F acc = {};
-        if (mine) {
-            if (part == 0) add(acc, (long long)b * 2 + 1, j);
-#pragma unroll 8
-            for (int q = from; q < to; ++q) add(acc, (long long)q * 2, j);
-        }
-        if (per_slice > 1) {
-            __syncthreads();  // (the slices before are read)
-            s[w][lane] = acc;
-            __syncthreads();
-            if (mine && part == 0)
-                for (int q = 1; q < per_slice; ++q)
+            for (int u = 0; u < 8; ++u) {
+                const int q = q0 + u - own;
+                const long long row = q0 + u >= rows ? 0 : q < 0 ? (long long)b * 2 + 1 : (from + q) * 2ll;
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) acc.v[e] += s[w + q][lane].v[e];
+                for (int r = 0; r < R; ++r)
+                    v[u][r] = *reinterpret_cast<const F *>(a.part + row * a.D + (j0 + r * 32 < a.D ? j0 + r * 32 : 0));
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (q0 + u < rows)
+#pragma unroll
+                    for (int r = 0; r < R; ++r)
+#pragma unroll
+                        for (int e = 0; e < JV; ++e) acc[r * JV + e] += v[u][r].v[e];
         }
-        if (mine && part == 0) put_row<T, VEC>(a.dtable + (long long)k * a.D + j, acc.v, a.scale);
+#pragma unroll
+        for (int e = 0; e < R * JV; ++e) s[w][e][lane] = acc[e];
     }
+    __syncthreads();
+    if (sl >= slices || part) return;
+    for (int q = 1; q < warps; ++q)
+#pragma unroll
+        for (int e = 0; e < R * JV; ++e) acc[e] += s[w + q][e][lane];
+    T *to_row = a.dtable + (long long)k * a.D;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if (j0 + r * 32 < a.D) {
+            float f[JV];
+#pragma unroll
+            for (int e = 0; e < JV; ++e) f[e] = acc[r * JV + e];
+            put_row<T, JV>(to_row + j0 + r * 32, f, a.scale);
+        }
 }
 
 size_t up(size_t b) { return (b + 255) & ~(size_t)255; }
@@ -449,13 +483,13 @@ struct Layout {
     int tiles, block, blocks;
     size_t key[2], pos[2], count, present, part, total;
 };
-Layout layout(const wm_seq *h, long long n, int V, int D, size_t es) {
+Layout layout(const wm_seq *h, long long n, int V, int D, int cols) {  // cols: of a slice
     Layout l{};
     l.cluster = n <= (long long)kCluster * kPerCta;
     l.tiles = (int)((n + kTile - 1) / kTile);
     // Positions per block: all blocks' warps run at once (22 of 24 an SM), in blocks of 16 to 256 positions:
     // a second round of warps would run alone, short blocks leave more partial rows.
-    const long long slices = (D * (long long)es + 511) / 512, warps = h->sms * 22ll;
+    const long long slices = (D + cols - 1) / cols, warps = h->sms * 22ll;
     const long long b = (n * slices + warps - 1) / warps;
     l.block = (int)(b < 16 ? 16 : b > 256 ? 256 : (b + 7) / 8 * 8);
     l.blocks = (int)((n + l.block - 1) / l.block);
@@ -478,9 +512,9 @@ Layout layout(const wm_seq *h, long long n, int V, int D, size_t es) {
 
 // Launches that may start while the one before still runs (they wait for it themselves).
 template <class P>
-cudaError_t follow(void (*k)(P), unsigned grid, int threads, cudaStream_t s, const P &p) {
+cudaError_t follow(void (*k)(P), dim3 grid, int threads, cudaStream_t s, const P &p) {
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
     cfg.stream = s;
     cudaLaunchAttribute at[1];
@@ -492,26 +526,42 @@ cudaError_t follow(void (*k)(P), unsigned grid, int threads, cudaStream_t s, con
 }
 
 template <class T, int VEC>
+constexpr int slice_columns() {
+    return 32 * VEC * lane_vectors<T, VEC>();
+}
+
+template <class T, int VEC>
 cudaError_t sums(wm_seq *h, SumArgs<T> a, cudaStream_t s) {
-    a.slices = (a.D + 32 * VEC - 1) / (32 * VEC);
+    a.slices = (a.D + slice_columns<T, VEC>() - 1) / slice_columns<T, VEC>();
     const long long warps = (long long)a.blocks * a.slices + a.zero_warps;
     cudaError_t e = follow(k_embed_sum<T, VEC>, (unsigned)((warps + kSum / 32 - 1) / (kSum / 32)), kSum, s, a);
     if (e != cudaSuccess) return e;
     ++h->last_launches;
     if (a.blocks > 1) {
-        e = follow(k_embed_join<T, VEC>, (unsigned)(a.blocks - 1), kJoin, s, a);
+        const unsigned columns = (unsigned)((a.D + kJoinColumns * kJoinSlices - 1) / (kJoinColumns * kJoinSlices));
+        e = follow(k_embed_join<T, VEC>, dim3((unsigned)(a.blocks - 1), columns), kJoin, s, a);
         ++h->last_launches;
     }
     return e;
+}
+
+// Calls f with the widest access, as an integral constant, that D and the addresses allow.
+template <class T, class F>
+auto by_width(int D, const void *p, const void *q, F f) {
+    constexpr int VEC = 16 / sizeof(T);
+    auto ok = [&](int v) { return D % v == 0 && (uintptr_t)p % (v * sizeof(T)) == 0 && (uintptr_t)q % (v * sizeof(T)) == 0; };
+    if (ok(VEC)) return f(std::integral_constant<int, VEC>{});
+    if constexpr (VEC == 8)
+        if (ok(4)) return f(std::integral_constant<int, 4>{});
+    if (ok(2)) return f(std::integral_constant<int, 2>{});
+    return f(std::integral_constant<int, 1>{});
 }
 
 template <class T>
 cudaError_t backward(wm_seq *h, SumArgs<T> a, const void *dout, void *dtable, cudaStream_t s) {
     a.dout = (const T *)dout;
     a.dtable = (T *)dtable;
-    constexpr int VEC = 16 / sizeof(T);
-    if (a.D % VEC == 0 && (uintptr_t)dout % 16 == 0 && (uintptr_t)dtable % 16 == 0) return sums<T, VEC>(h, a, s);
-    return sums<T, 1>(h, a, s);
+    return by_width<T>(a.D, dout, dtable, [&](auto v) { return sums<T, decltype(v)::value>(h, a, s); });
 }
 
 template <class T>
@@ -528,13 +578,18 @@ SumArgs<T> sum_args(int n, int V, int D, const Layout &l, char *ws, int at, floa
 template <class T>
 void lookup(const wm_seq *h, long long n, int V, int D, const T *table, const int32_t *tokens, float scale, T *out,
             cudaStream_t s) {
-    constexpr int VEC = 16 / sizeof(T);
     const long long need = (n + kLookup / 32 - 1) / (kLookup / 32), most = (long long)h->sms * 16;
     const unsigned grid = (unsigned)(need < most ? need : most);
-    if (D % VEC == 0 && (uintptr_t)table % 16 == 0 && (uintptr_t)out % 16 == 0)
-        k_embed<T, VEC><<<grid, kLookup, 0, s>>>(n, V, D, table, tokens, scale, out, h->status);
-    else
-        k_embed<T, 1><<<grid, kLookup, 0, s>>>(n, V, D, table, tokens, scale, out, h->status);
+    by_width<T>(D, table, out, [&](auto v) {
+        k_embed<T, decltype(v)::value><<<grid, kLookup, 0, s>>>(n, V, D, table, tokens, scale, out, h->status);
+        return 0;
+    });
+}
+
+int columns(int dtype, int D, const void *dout, const void *dtable) {
+    if (dtype == WM_BF16)
+        return by_width<__nv_bfloat16>(D, dout, dtable, [](auto v) { return slice_columns<__nv_bfloat16, decltype(v)::value>(); });
+    return by_width<float>(D, dout, dtable, [](auto v) { return slice_columns<float, decltype(v)::value>(); });
 }
 
 }  // namespace
@@ -549,8 +604,8 @@ cudaError_t wm_seq_embed_launch(wm_seq *h, int dtype, long long n, int V, int D,
     return cudaGetLastError();
 }
 
-size_t wm_seq_embed_backward_ws(const wm_seq *h, int dtype, long long n, int V, int D) {
-    return n ? layout(h, n, V, D, dtype == WM_BF16 ? 2 : 4).total : 0;
+size_t wm_seq_embed_backward_ws(const wm_seq *h, int dtype, long long n, int V, int D, const void *dout, const void *dtable) {
+    return n ? layout(h, n, V, D, columns(dtype, D, dout, dtable)).total : 0;
 }
 
 cudaError_t wm_seq_embed_backward_launch(wm_seq *h, int dtype, long long n, int V, int D, const int32_t *tokens,
@@ -561,7 +616,7 @@ cudaError_t wm_seq_embed_backward_launch(wm_seq *h, int dtype, long long n, int 
         return cudaMemsetAsync(dtable, 0, (size_t)V * D * es, s);
     }
     h->last_launches = 0;
-    const Layout l = layout(h, n, V, D, es);
+    const Layout l = layout(h, n, V, D, columns(dtype, D, dout, dtable));
     char *ws = (char *)h->ws;
     const int bits = key_bits(V);
     int at = 0;

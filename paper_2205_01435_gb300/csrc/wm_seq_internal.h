@@ -56,7 +56,7 @@ cudaError_t wm_seq_norm_backward_launch(wm_seq *h, int dtype, long long rows, in
 
 cudaError_t wm_seq_embed_launch(wm_seq *h, int dtype, long long n, int V, int D, const void *table,
                                 const int32_t *tokens, float scale, void *out, cudaStream_t s);
-size_t wm_seq_embed_backward_ws(const wm_seq *h, int dtype, long long n, int V, int D);
+size_t wm_seq_embed_backward_ws(const wm_seq *h, int dtype, long long n, int V, int D, const void *dout, const void *dtable);
 cudaError_t wm_seq_embed_backward_launch(wm_seq *h, int dtype, long long n, int V, int D, const int32_t *tokens,
                                          const void *dout, float scale, void *dtable, cudaStream_t s);
 

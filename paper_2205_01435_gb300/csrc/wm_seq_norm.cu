@@ -9,6 +9,10 @@
 // CTAs walk the rows with a stride of the grid: the weights stay in registers, and in the
 // backward each thread sums its columns' dw and db over the CTA's rows in fp32; the CTAs'
 // partial sums are added in a fixed order by a second, small launch.
+#include <algorithm>
+#include <initializer_list>
+#include <utility>
+
 #include "wm_seq_internal.h"
 
 namespace {
@@ -22,7 +26,7 @@ constexpr int kFwdMax = 16384, kBwdMax = 8192;
 // copied so: their threads load a row when they come to it.
 template <int E>
 constexpr int ring_rows() {  // two rows and more on their way: 24 KB and more an SM in every variant
-    return E == 8 ? 6 : E == 16 ? 4 : 3;
+    return E == 8 ? 6 : E <= 16 ? 4 : 3;
 }
 
 template <class T, int VEC>
@@ -127,8 +131,9 @@ struct Weights {
                 w[k + 2] = q.z;
                 w[k + 3] = q.w;
             }
-        } else {  // one value a vector: [E][32]
-            w[0] = s[i * 32];
+        } else {  // [E][32]
+#pragma unroll
+            for (int k = 0; k < VEC; ++k) w[k] = s[(i * VEC + k) * 32];
         }
     }
 };
@@ -443,8 +448,15 @@ __global__ void __launch_bounds__(kLong) k_norm_bwd_long(long long rows, int D, 
     }
 }
 
-bool vec_ok(const void *p, long long ld, int D, size_t es) {
-    return (uintptr_t)p % 16 == 0 && (ld * es) % 16 == 0 && (D * es) % 16 == 0;
+// The widest access of `vec`, `vec` / 2, ... values that the arrays' addresses and strides and the
+// rows' length allow.
+int width(int vec, size_t es, int D, std::initializer_list<std::pair<const void *, long long>> arrays) {
+    for (; vec > 1; vec /= 2) {
+        bool ok = D % vec == 0;
+        for (const auto &a : arrays) ok &= (uintptr_t)a.first % (vec * es) == 0 && a.second % vec == 0;
+        if (ok) break;
+    }
+    return vec;
 }
 
 // Threads per row and values per thread: the fewest of each that hold the row (a warp up to 1024
@@ -453,8 +465,8 @@ bool vec_ok(const void *p, long long ld, int D, size_t es) {
 struct Shape {
     int tpr, e;
 };
-Shape shape(int D) {
-    if (D <= 1024) return {32, D <= 256 ? 8 : D <= 512 ? 16 : 32};
+Shape shape(int D, int vec) {
+    if (D <= 1024) return {32, D <= 256 ? 8 : D <= 384 && vec <= 4 ? 12 : D <= 512 ? 16 : 32};
     if (D <= 4096) return {128, D <= 2048 ? 16 : 32};
     if (D <= 8192) return {256, 32};
     return {512, 32};
@@ -479,6 +491,8 @@ cudaError_t launch(void (*k)(P...), int grid, int threads, size_t smem, cudaStre
 
 #define NORM_SHAPES(CALL)                          \
     if (sh.tpr == 32 && sh.e == 8) CALL(8, 32)     \
+    if constexpr (VEC <= 4)                        \
+        if (sh.tpr == 32 && sh.e == 12) CALL(12, 32) \
     if (sh.tpr == 32 && sh.e == 16) CALL(16, 32)   \
     if (sh.tpr == 32) CALL(32, 32)                 \
     if (sh.tpr == 128 && sh.e == 16) CALL(16, 128) \
@@ -488,7 +502,7 @@ cudaError_t launch(void (*k)(P...), int grid, int threads, size_t smem, cudaStre
 template <class T, int VEC>
 cudaError_t fwd(const wm_seq *h, long long rows, int D, const T *x, long long ldx, const float *w, const float *b, float eps,
                 T *y, long long ldy, float *mean, float *rstd, cudaStream_t s) {
-    const Shape sh = shape(D);
+    const Shape sh = shape(D, VEC);
 #define CALL(E, TPR)                                                                                                     \
     {                                                                                                                    \
         constexpr int threads = cta_threads<TPR>(), rpc = threads / TPR;                                                 \
@@ -504,12 +518,12 @@ cudaError_t fwd(const wm_seq *h, long long rows, int D, const T *x, long long ld
 template <class T, int VEC>
 cudaError_t bwd(long long rows, int D, const T *x, long long ldx, const float *w, const float *mean, const float *rstd,
                 const T *dy, long long lddy, T *dx, long long lddx, float *part, int grid, cudaStream_t s) {
-    const Shape sh = shape(D);
+    const Shape sh = shape(D, VEC);
 #define CALL(E, TPR)                                                                                             \
     {                                                                                                            \
         constexpr int threads = cta_threads<TPR>(), rpc = threads / TPR;                                         \
-        const size_t ring = Rows<T, VEC, E, TPR, 2, threads>::bytes(), cols = rpc > 1 ? (size_t)rpc * 2 * D * 4 : 0; \
-        return launch(k_norm_bwd<T, VEC, E, TPR>, grid, threads, ring > cols ? ring : cols, s, rows, D, x, ldx,   \
+        const long long ring = Rows<T, VEC, E, TPR, 2, threads>::bytes(), cols = rpc > 1 ? rpc * 8ll * D : 0;     \
+        return launch(k_norm_bwd<T, VEC, E, TPR>, grid, threads, (size_t)std::max(ring, cols), s, rows, D, x, ldx, \
                       w, mean, rstd, dy, lddy, dx, lddx, part);                                                  \
     }
     NORM_SHAPES(CALL)
@@ -525,8 +539,11 @@ cudaError_t fwd_any(const wm_seq *h, long long rows, int D, const T *x, long lon
         return launch(k_norm_fwd_long<T>, (int)(rows < most ? rows : most), kLong, 0, s, rows, D, x, ldx, w, b, eps, y, ldy, mean,
                       rstd);
     }
-    if (vec_ok(x, ldx, D, sizeof(T)) && vec_ok(y, ldy, D, sizeof(T)))
-        return fwd<T, 16 / sizeof(T)>(h, rows, D, x, ldx, w, b, eps, y, ldy, mean, rstd, s);
+    constexpr int VEC = 16 / sizeof(T);
+    const int v = width(VEC, sizeof(T), D, {{x, ldx}, {y, ldy}});
+    if (v == VEC) return fwd<T, VEC>(h, rows, D, x, ldx, w, b, eps, y, ldy, mean, rstd, s);
+    if (v == 4) return fwd<T, 4>(h, rows, D, x, ldx, w, b, eps, y, ldy, mean, rstd, s);
+    if (v == 2) return fwd<T, 2>(h, rows, D, x, ldx, w, b, eps, y, ldy, mean, rstd, s);
     return fwd<T, 1>(h, rows, D, x, ldx, w, b, eps, y, ldy, mean, rstd, s);
 }
 
@@ -535,8 +552,11 @@ cudaError_t bwd_any(long long rows, int D, const T *x, long long ldx, const floa
                     const T *dy, long long lddy, T *dx, long long lddx, float *part, int grid, cudaStream_t s) {
     if (D > kBwdMax)
         return launch(k_norm_bwd_long<T>, grid, kLong, 0, s, rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part);
-    if (vec_ok(x, ldx, D, sizeof(T)) && vec_ok(dy, lddy, D, sizeof(T)) && vec_ok(dx, lddx, D, sizeof(T)))
-        return bwd<T, 16 / sizeof(T)>(rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part, grid, s);
+    constexpr int VEC = 16 / sizeof(T);
+    const int v = width(VEC, sizeof(T), D, {{x, ldx}, {dy, lddy}, {dx, lddx}});
+    if (v == VEC) return bwd<T, VEC>(rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part, grid, s);
+    if (v == 4) return bwd<T, 4>(rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part, grid, s);
+    if (v == 2) return bwd<T, 2>(rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part, grid, s);
     return bwd<T, 1>(rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part, grid, s);
 }
 

@@ -297,17 +297,18 @@ __global__ void __launch_bounds__(kThreads) k_scan_stream(const ScanParams<T> a)
 // ---- few channels: spans of time side by side ----------------------------------------------
 // A tile is W = 32 * VEC channels of one sequence, a chunk SUBS spans of L steps of it; a CTA
 // takes one (chunk, tile).  Lane l of warp q holds VEC channels of span q.  Chunks are numbered
-// in the order of the recurrence; 32 make a group, 32 groups a section.  Every chunk publishes
+// in the order of the recurrence; 16 make a group, 16 groups a section.  Every chunk publishes
 // its (P, S), the last of a group the group's, the last of a section the state that leaves it,
 // and a chunk's entering state is the section's state through the groups and then the chunks
 // before it, always joined in the same tree: the same bits every time.  CTAs take their
 // chunks by a ticket, so a chunk waits only for chunks that are running or done.
 constexpr int kSpanThreads = 256, SUBS = kSpanThreads / 32;
+constexpr int kGroupBits = 4, kGroupOf = 1 << kGroupBits;
 constexpr unsigned kPolls = 1u << 20;  // a wait's limit: about a second
 
 struct SpanWork {
     unsigned *ticket;
-    unsigned long long *chunk_ps, *group_ps;  // [tile][groups][32][W], [tile][sections][32][W]
+    unsigned long long *chunk_ps, *group_ps;  // [tile][groups][kGroupOf][W], [tile][sections][kGroupOf][W]
     unsigned long long *section;              // [tile][sections][W]: the state entering it
     int chunks, groups, sections, tiles;      // chunks, groups, sections of a tile; tiles in all
     int tiles_per_n;
@@ -379,7 +380,7 @@ struct Published {
 template <class T, int VEC, int L, bool BWD, bool RESET, bool DEEP>
 __global__ void __launch_bounds__(kSpanThreads, 4) k_scan_spans(const ScanParams<T> a, const SpanWork wk) {
     using V = seq_vec<T, VEC>;
-    constexpr int W = 32 * VEC, PARTS = kSpanThreads / W, EACH = 32 / PARTS, ARRAYS = BWD ? 4 : 2;
+    constexpr int W = 32 * VEC, PARTS = kSpanThreads / W, EACH = kGroupOf / PARTS, ARRAYS = BWD ? 4 : 2;
     constexpr int GATE = 0, X = 1, DH = 2, HB = 3;
     constexpr bool ASYNC = sizeof(V) >= 4;
     extern __shared__ __align__(16) unsigned char held[];  // [L][ARRAYS][kSpanThreads] of V
@@ -469,14 +470,17 @@ __global__ void __launch_bounds__(kSpanThreads, 4) k_scan_spans(const ScanParams
         float2 v[SUBS];
 #pragma unroll
         for (int q = 0; q < SUBS; ++q) v[q] = spans[q][ch];
-        own = v[0];
 #pragma unroll
-        for (int q = 1; q < SUBS; ++q) own = join(own, v[q]);
+        for (int q = 0; q < SUBS; ++q) {
+            spans[q][ch] = own;  // from here on: what comes before the span
+            own = join(own, v[q]);
+        }
     }
     if (DEEP) {
-        const int group = chunk >> 5, in_group = chunk & 31, section = group >> 5, in_section = group & 31;
-        unsigned long long *cp = wk.chunk_ps + ((long long)tile * wk.groups + group) * 32 * W + ch;
-        unsigned long long *gp = wk.group_ps + ((long long)tile * wk.sections + section) * 32 * W + ch;
+        const int group = chunk >> kGroupBits, in_group = chunk & (kGroupOf - 1);
+        const int section = group >> kGroupBits, in_section = group & (kGroupOf - 1);
+        unsigned long long *cp = wk.chunk_ps + ((long long)tile * wk.groups + group) * kGroupOf * W + ch;
+        unsigned long long *gp = wk.group_ps + ((long long)tile * wk.sections + section) * kGroupOf * W + ch;
         unsigned long long *sp = wk.section + ((long long)tile * wk.sections + section) * W + ch;
         if (more && part == 0) publish(cp + in_group * W, own);
         if (wk.test_wait && ticket == 0 && threadIdx.x == 0) {
@@ -486,38 +490,44 @@ __global__ void __launch_bounds__(kSpanThreads, 4) k_scan_spans(const ScanParams
         }
         const int from = part * EACH, n_near = min(EACH, in_group - from), n_far = min(EACH, in_section - from);
         Published<EACH> pub;
-        pub.ask(cp + from * W, W, n_near);
         unsigned long long s0 = 0;
         float st = 0.f;
+        if (in_group) pub.ask(cp + from * W, W, n_near);
         if (part == 0) {
             if (section > 0) s0 = peek(sp);
             else if (j0 + ch < a.H && a.h0) st = a.h0[(long long)n * a.H + j0 + ch];
         }
-        near[part][ch] = pub.joined(cp + from * W, W, n_near, a.status);
-        pub.ask(gp + from * W, W, n_far);
-        if (in_group == 31 && more) {  // the group's (P, S) goes out before anything else is waited for
-            __syncthreads();
-            if (part == 0) {
-                float2 v = near[0][ch];
+        if (in_group) {
+            near[part][ch] = pub.joined(cp + from * W, W, n_near, a.status);
+            if (in_group == kGroupOf - 1 && more) {  // the group's (P, S) goes out before anything else is waited for
+                __syncthreads();
+                if (part == 0) {
+                    float2 v = near[0][ch];
 #pragma unroll
-                for (int q = 1; q < PARTS; ++q) v = join(v, near[q][ch]);
-                publish(gp + in_section * W, join(v, own));
+                    for (int q = 1; q < PARTS; ++q) v = join(v, near[q][ch]);
+                    publish(gp + in_section * W, join(v, own));
+                }
             }
         }
-        far[part][ch] = pub.joined(gp + from * W, W, n_far, a.status);
+        if (in_section) {
+            pub.ask(gp + from * W, W, n_far);
+            far[part][ch] = pub.joined(gp + from * W, W, n_far, a.status);
+        }
         __syncthreads();
         if (part == 0) {
             if (section > 0) {
                 Published<1> left{{s0}};
                 st = left.joined(sp, 0, 1, a.status).y;
             }
+            if (in_section)
 #pragma unroll
-            for (int q = 0; q < PARTS; ++q) st = through(far[q][ch], st);
+                for (int q = 0; q < PARTS; ++q) st = through(far[q][ch], st);
+            if (in_group)
 #pragma unroll
-            for (int q = 0; q < PARTS; ++q) st = through(near[q][ch], st);
+                for (int q = 0; q < PARTS; ++q) st = through(near[q][ch], st);
             enter[ch] = st;
             st = through(own, st);
-            if (more && (chunk & 1023) == 1023) publish(sp + W, make_float2(0.f, st));
+            if (more && in_group == kGroupOf - 1 && in_section == kGroupOf - 1) publish(sp + W, make_float2(0.f, st));
             if (!more && a.last && j0 + ch < a.H) a.last[(long long)n * a.H + j0 + ch] = st;
         }
     } else if (part == 0) {
@@ -529,10 +539,7 @@ __global__ void __launch_bounds__(kSpanThreads, 4) k_scan_spans(const ScanParams
     // the outputs, from the state entering the span
     float mid[VEC];
 #pragma unroll
-    for (int k = 0; k < VEC; ++k) {
-        mid[k] = enter[lane * VEC + k];
-        for (int q = 0; q < sub; ++q) mid[k] = through(spans[q][lane * VEC + k], mid[k]);
-    }
+    for (int k = 0; k < VEC; ++k) mid[k] = through(spans[sub][lane * VEC + k], enter[lane * VEC + k]);
     T *o0 = (BWD ? a.dgate.row(t0, n) : a.h.row(t0, n)) + j, *o1 = BWD ? a.dx.row(t0, n) + j : nullptr;
     const long long d0 = dir * (BWD ? a.dgate.st : a.h.st);
     const V zero = [] {
@@ -675,11 +682,11 @@ Plan plan(const wm_seq *h, const seq_scan_args &a, bool bwd) {
         p.len = bwd ? kLenBwd : kLenFwd;
         if ((a.T + SUBS * p.len - 1) / (SUBS * p.len) * k.tiles < h->sms) p.len = kLenShort;
         k.chunks = (int)((a.T + SUBS * p.len - 1) / (SUBS * p.len));
-        k.groups = (k.chunks + 31) / 32;
-        k.sections = (k.groups + 31) / 32;
+        k.groups = (k.chunks + kGroupOf - 1) / kGroupOf;
+        k.sections = (k.groups + kGroupOf - 1) / kGroupOf;
         if (k.chunks > 1) {
             const size_t t = (size_t)k.tiles * W * 8;
-            p.ws = 256 + t * k.groups * 32 + t * k.sections * 32 + t * k.sections;
+            p.ws = 256 + t * kGroupOf * (k.groups + k.sections) + t * k.sections;
         }
     }
     return p;
@@ -694,8 +701,8 @@ cudaError_t spans(wm_seq *h, const seq_scan_args &a, const Plan &p, cudaStream_t
         const size_t t = (size_t)wk.tiles * 32 * VEC;
         wk.ticket = (unsigned *)h->ws;
         wk.chunk_ps = (unsigned long long *)((char *)h->ws + 256);
-        wk.group_ps = wk.chunk_ps + t * wk.groups * 32;
-        wk.section = wk.group_ps + t * wk.sections * 32;
+        wk.group_ps = wk.chunk_ps + t * wk.groups * kGroupOf;
+        wk.section = wk.group_ps + t * wk.sections * kGroupOf;
         wk.test_wait = h->test_wait;
         h->test_wait = 0;
         const cudaError_t e = cudaMemsetAsync(h->ws, 0xff, p.ws, s);

@@ -376,6 +376,29 @@ def test_embed(ops, dtype, n, V, D):
     ops.sync()
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n,V,D", [(700, 40, 300), (700, 40, 302), (900, 1000, 1001), (3000, 9, 516), (300, 2, 2050)])
+def test_embed_widths(ops, dtype, n, V, D):
+    """Rows whose length allows 16-, 8-, 4- and 2-byte accesses, in one slice of columns and several."""
+    t = torch.randint(-1, V, (n,), generator=torch.Generator().manual_seed(D), dtype=torch.int32).cuda()
+    table, dout = rnd(V, D, seed=1, dtype=DT[dtype]), rnd(n, D, seed=2, dtype=DT[dtype])
+    ref.check(ops.embed(table, t, scale=0.3), *ref.embed(table, t, 0.3), "out")
+    ref.check(ops.embed_backward(t, dout, V, scale=0.3), *ref.embed_backward(t, dout, V, 0.3), "dtable")
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("D", [12, 258, 302, 380, 516, 700, 1002, 2050, 4100, 8194])
+def test_norm_widths(ops, dtype, D):
+    rows = 50
+    x, dy = rnd(rows, D, seed=D, dtype=DT[dtype], std=2.0), rnd(rows, D, seed=D + 3, dtype=DT[dtype])
+    w, b = rnd(D, seed=D + 1, mean=1.0), rnd(D, seed=D + 2)
+    y, mean, rstd = ops.layer_norm(x, w, b, want_stats=True)
+    ref.check(y, *ref.norm(x, w, b, 1e-5)["y"], "y")
+    g = ref.norm_backward(x, w, mean, rstd, dy)
+    for k, v in zip(("dx", "dw", "db"), ops.layer_norm_backward(x, w, mean, rstd, dy)):
+        ref.check(v, *g[k], k)
+
+
 @pytest.mark.parametrize("n,V", [(1023, 255), (1025, 256), (16384, 30000), (70001, 513), (196608, 100), (196609, 300), (250000, 70000)])
 def test_embed_backward_sort_sizes(ops, n, V):
     """One CTA, a cluster, its last size, and beyond it; one digit to three."""
