@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_sort_cluster(const ClusterS
     extern __shared__ __align__(16) unsigned char smem[];
     unsigned long long *order[2] = {reinterpret_cast<unsigned long long *>(smem),
                                     reinterpret_cast<unsigned long long *>(smem) + a.per};  // pos << 32 | key
-    __shared__ unsigned short cnt[kSortThreads / 32][kMaxDigits];  // pairs of a digit per warp, then before it
+    __shared__ __align__(4) unsigned short cnt[kSortThreads / 32][kMaxDigits];  // pairs of a digit per warp, then before it
     __shared__ int all[kCluster][kMaxDigits], base[kMaxDigits], scan[8];
     const int tid = threadIdx.x, lane = tid & 31, w = tid / 32;
     const int rank = (int)cluster_rank(), ranks = (int)cluster_size();
@@ -107,6 +107,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_sort_cluster(const ClusterS
     const int digits = 1 << a.bits;
     // the sums may be launched now: they wait for this grid's end before they read anything
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    for (int i = tid; i < kCluster * kMaxDigits; i += kSortThreads) all[i / kMaxDigits][i % kMaxDigits] = 0;
     for (int v = rank * kSortThreads + tid; v < a.V; v += ranks * kSortThreads) a.present[v] = 0;
     for (int i = tid; i < m; i += kSortThreads) {
         const int t = token_row(a.tokens[lo + i], a.V, a.status);
@@ -118,7 +119,7 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_sort_cluster(const ClusterS
     for (int pass = 0; pass < a.passes; ++pass) {
         const unsigned long long *from = order[pass & 1];
         unsigned long long *to = order[(pass & 1) ^ 1];
-        for (int d = lane; d < digits; d += 32) cnt[w][d] = 0;
+        for (int d = lane; d < digits / 2; d += 32) reinterpret_cast<int *>(cnt[w])[d] = 0;
         __syncthreads();
         // (kSortItems + 1: a piece is rounded up to whole warps)
         unsigned long long item[kSortItems + 1];
@@ -155,13 +156,14 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_sort_cluster(const ClusterS
         cluster_barrier();
         // places of smaller digits, and of this digit in the CTAs before
         if (tid < kMaxDigits) {
-            int total = 0, mine = 0;
-            if (tid < digits)
+            int v[kCluster], total = 0, mine = 0;
 #pragma unroll
-                for (int q = 0; q < kCluster; ++q) {
-                    if (q == rank) mine = total;
-                    if (q < ranks) total += all[q][tid];
-                }
+            for (int q = 0; q < kCluster; ++q) v[q] = all[q][tid];  // (0 past the digits and the CTAs there are)
+#pragma unroll
+            for (int q = 0; q < kCluster; ++q) {
+                mine += q < rank ? v[q] : 0;
+                total += v[q];
+            }
             int s = total;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
