@@ -64,9 +64,11 @@ const char *wm_seq_last_error(const wm_seq *h);
 int wm_seq_last_launches(const wm_seq *h);
 
 /* Failure injection for tests of the timeout path: every wait inside a kernel is bounded.
- * With polls > 0 the next scan call that joins spans across CTAs (few channels, many
- * steps) makes its first CTA poll, at most that often, for something that nothing sets; it
- * records WM_ERR_TIMEOUT, as a real bounded wait does, and goes on.  One shot. */
+ * With polls > 0 the next call whose CTAs wait for one another (a scan of few channels and
+ * many steps, or wm_seq_clip of up to 30 MB) makes its first CTA poll, at most that often,
+ * for something that nothing sets; it records WM_ERR_TIMEOUT, as a real bounded wait does,
+ * and goes on.  One shot.  After WM_ERR_TIMEOUT outputs are undefined until wm_seq_sync has
+ * returned it. */
 wm_status wm_seq_inject_wait_timeout(wm_seq *h, unsigned int polls);
 
 /* Frees what the handle owns (after the device has finished).  NULL is a no-op. */

@@ -166,7 +166,8 @@ extern "C" wm_status wm_seq_sync(wm_seq *h) {
     cudaError_t e = on.e;
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e == cudaSuccess) e = cudaMemcpy(st, h->status, sizeof st, cudaMemcpyDeviceToHost);
-    if (e == cudaSuccess && (st[0] || st[1])) e = cudaMemset(h->status, 0, sizeof st);
+    // (with a wait that gave up, the counters that calls meet at are reset too)
+    if (e == cudaSuccess && (st[0] || st[1])) e = cudaMemset(h->status, 0, st[1] ? 256 : sizeof st);
     if (e != cudaSuccess) return cuda_fail(h, e, "wm_seq_sync");
     if (st[1]) return fail(h, (wm_status)st[1], "wm_seq_sync", "a wait inside a kernel gave up");
     if (st[0]) return fail(h, (wm_status)st[0], "wm_seq_sync", "a token or a length of an earlier call was out of range");

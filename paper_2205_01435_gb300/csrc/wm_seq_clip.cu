@@ -7,7 +7,8 @@
 // device, no synchronisation), cut into tiles, every CTA a run of them, so that a thousand
 // small tensors load the GPU as evenly as one large one and the order of the sum is fixed.
 // A tile's loads are issued before the one before it is worked on.  The second launch goes
-// through the runs backwards: what the first read last is still in L2.
+// through the runs backwards: what the first read last is still in L2.  Gradients of up to 30 MB
+// take one launch, which holds them in shared memory between the norm and the clipping.
 //
 // Squares are summed in fp32 within a 16-byte vector (4 or 8 values) and from there on
 // without rounding error that matters: a thread adds the vectors' sums into an fp32 pair
@@ -37,7 +38,6 @@ struct Table {
 // What the first launches leave for the second ones.
 struct Result {
     float scale;  // 1: leave the gradients as they are
-    float norm;
 };
 
 // A sum of fp32 values as hi + lo, and in fp64 what does not fit fp32.
@@ -124,95 +124,84 @@ struct Cursor {
         else if (tile < lo && i > 0) at(i - 1);
     }
 };
-// A tile: its place, and (aligned) its vectors.
-struct Tile {
+// A tile's place.
+struct Spot {
     const char *src;
     char *dst;
-    int n;        // values
-    bool bf16, wide;  // wide: 16-byte accesses
-    uint4 v[kEach];
+    int n, vecs;  // values; 16-byte vectors among them (0: not aligned)
+    bool bf16;
     template <int SIZE>
-    __device__ __forceinline__ void load(const Cursor<SIZE> &c, bool with_dst) {
+    __device__ __forceinline__ void find(const Cursor<SIZE> &c, bool with_dst) {
         bf16 = c.bf16;
         const long long at = (long long)(c.tile - c.lo) * kTileBytes;
         const int shift = bf16 ? 1 : 2;
         n = (int)min((long long)(kTileBytes >> shift), c.n - (at >> shift));
         src = c.src + at;
         dst = c.dst + at;
-        wide = (uintptr_t)src % 16 == 0 && (!with_dst || (uintptr_t)dst % 16 == 0);
-        const int vecs = wide ? n / (bf16 ? 8 : 4) : 0;
+        vecs = (uintptr_t)src % 16 == 0 && (!with_dst || (uintptr_t)dst % 16 == 0) ? n >> (bf16 ? 3 : 2) : 0;
+    }
+};
+// And its vectors in registers.
+struct Tile : Spot {
+    uint4 v[kEach];
+    template <int SIZE>
+    __device__ __forceinline__ void load(const Cursor<SIZE> &c, bool with_dst) {
+        find(c, with_dst);
 #pragma unroll
         for (int q = 0; q < kEach; ++q)
             if ((int)threadIdx.x + q * kThreads < vecs) v[q] = reinterpret_cast<const uint4 *>(src)[threadIdx.x + q * kThreads];
     }
-    __device__ __forceinline__ int vecs() const { return wide ? n / (bf16 ? 8 : 4) : 0; }
 };
 
-template <class T>
-__device__ __forceinline__ void tile_squares(const Tile &t, Sum &sum) {
+// v(q): the thread's vector q of the tile.
+template <class T, class F>
+__device__ __forceinline__ void tile_squares(const Spot &t, F v, Sum &sum) {
     constexpr int VEC = 16 / sizeof(T);
-    const int vecs = t.vecs();
 #pragma unroll
     for (int q = 0; q < kEach; ++q)
-        if ((int)threadIdx.x + q * kThreads < vecs) {
+        if ((int)threadIdx.x + q * kThreads < t.vecs) {
+            const uint4 w = v(q);
             float f[VEC];
-            seq_unpack(reinterpret_cast<const seq_vec<T, VEC> &>(t.v[q]), f);
+            seq_unpack(reinterpret_cast<const seq_vec<T, VEC> &>(w), f);
             add_squares(f, sum);
         }
-    for (int i = vecs * VEC + threadIdx.x; i < t.n; i += kThreads) {
+    for (int i = t.vecs * VEC + threadIdx.x; i < t.n; i += kThreads) {
         const float f[1] = {seq_to_float(reinterpret_cast<const T *>(t.src)[i])};
         add_squares(f, sum);
     }
 }
+template <class F>
+__device__ __forceinline__ void add_tile(const Spot &t, F v, Sum &sum) {
+    if (t.bf16) tile_squares<__nv_bfloat16>(t, v, sum);
+    else tile_squares<float>(t, v, sum);
+}
 
-template <class T>
-__device__ __forceinline__ void tile_scale(const Tile &t, float scale) {
+template <class T, class F>
+__device__ __forceinline__ void tile_scale(const Spot &t, F v, float scale) {
     constexpr int VEC = 16 / sizeof(T);
-    const int vecs = t.vecs();
     T *to = reinterpret_cast<T *>(t.dst);
 #pragma unroll
     for (int q = 0; q < kEach; ++q)
-        if ((int)threadIdx.x + q * kThreads < vecs) {
+        if ((int)threadIdx.x + q * kThreads < t.vecs) {
+            const uint4 w = v(q);
             float f[VEC];
-            seq_unpack(reinterpret_cast<const seq_vec<T, VEC> &>(t.v[q]), f);
+            seq_unpack(reinterpret_cast<const seq_vec<T, VEC> &>(w), f);
 #pragma unroll
             for (int k = 0; k < VEC; ++k) f[k] *= scale;
             seq_store(to + (threadIdx.x + q * kThreads) * VEC, seq_pack<T, VEC>(f));
         }
-    for (int i = vecs * VEC + threadIdx.x; i < t.n; i += kThreads)
+    for (int i = t.vecs * VEC + threadIdx.x; i < t.n; i += kThreads)
         to[i] = seq_from_float<T>(seq_to_float(reinterpret_cast<const T *>(t.src)[i]) * scale);
 }
+template <class F>
+__device__ __forceinline__ void scale_tile(const Spot &t, F v, float scale) {
+    if (scale == 1.f && t.src == t.dst) return;
+    if (t.bf16) tile_scale<__nv_bfloat16>(t, v, scale);
+    else tile_scale<float>(t, v, scale);
+}
 
-// CTA b's tiles: [first, last) of an even split.
-__device__ __forceinline__ int split(int tiles, int b) { return (int)((long long)tiles * b / gridDim.x); }
-
-// part[0, parts): sums of the launches before this one and of this one's CTAs.  The last CTA of the
-// last launch adds them, always in the same order, and leaves the norm and the scale.
-template <int SIZE>
-__global__ void __launch_bounds__(kThreads) k_clip_squares(const __grid_constant__ Table<SIZE> t, double *part, int parts_before,
-                                                           int last, float max_norm, Result *result, float *norm,
-                                                           unsigned *arrived) {
-    __shared__ double red[kThreads / 32];
-    __shared__ bool s_last;
-    Sum sum;
-    const int first = split(t.tiles, blockIdx.x), end = split(t.tiles, blockIdx.x + 1);
-    Cursor<SIZE> c(t, first);
-    Tile next;
-    next.load(c, false);
-    int vecs = 0;
-    for (int tile = first; tile < end; ++tile) {
-        const Tile now = next;
-        if (tile + 1 < end) {
-            c.step(1);
-            next.load(c, false);
-        }
-        if (now.bf16) tile_squares<__nv_bfloat16>(now, sum);
-        else tile_squares<float>(now, sum);
-        if ((vecs += kTileBytes / 2 / kThreads) >= kFlush) {  // (an unaligned tile: a value a vector)
-            sum.flush();
-            vecs = 0;
-        }
-    }
+// The CTA's sum in fp64, in thread 0.
+__device__ __forceinline__ double cta_sum(Sum sum, double *red) {
     // over the warp: pairs in fp32, the wide parts only where there are any
     const bool wide = __any_sync(0xffffffffu, sum.wide != 0.0);
 #pragma unroll
@@ -227,9 +216,66 @@ __global__ void __launch_bounds__(kThreads) k_clip_squares(const __grid_constant
         red[threadIdx.x / 32] = sum.wide;
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-        double s = 0.0;
+    double s = 0.0;
+    if (threadIdx.x == 0)
         for (int i = 0; i < kThreads / 32; ++i) s += red[i];
+    return s;
+}
+// The norm from the CTAs' sums, always added in the same order; in every thread.
+__device__ __forceinline__ float norm_of(const double *part, int parts, double *red, float *out) {
+    double s = 0.0;
+    for (int i = threadIdx.x; i < parts; i += kThreads) s += __ldcg(part + i);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x / 32] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s = 0.0;
+        for (int i = 0; i < kThreads / 32; ++i) s += red[i];
+        // (the fp64 root takes a microsecond: only where the sum is out of fp32's range)
+        *out = s > 1e-30 && s < 1e38 ? sqrtf((float)s) : (float)sqrt(s);
+    }
+    __syncthreads();
+    return *out;
+}
+// min(1, max_norm / norm); 1 where the norm is not finite.
+__device__ __forceinline__ float scale_of(float norm, float max_norm) {
+    return norm > max_norm && isfinite(norm) ? __fdiv_rn(max_norm, norm) : 1.f;
+}
+
+// CTA b's tiles: [first, last) of an even split.
+__device__ __forceinline__ int split(int tiles, int b) { return (int)((long long)tiles * b / gridDim.x); }
+
+// part[0, parts): sums of the launches before this one and of this one's CTAs.  The last CTA of the
+// last launch adds them, always in the same order, and leaves the norm and the scale.
+template <int SIZE>
+__global__ void __launch_bounds__(kThreads) k_clip_squares(const __grid_constant__ Table<SIZE> t, double *part, int parts_before,
+                                                           int last, float max_norm, Result *result, float *norm,
+                                                           unsigned *arrived) {
+    __shared__ double red[kThreads / 32];
+    __shared__ float s_norm;
+    __shared__ bool s_last;
+    Sum sum;
+    const int first = split(t.tiles, blockIdx.x), end = split(t.tiles, blockIdx.x + 1);
+    Cursor<SIZE> c(t, first);
+    Tile next;
+    next.load(c, false);
+    int vecs = 0;
+    for (int tile = first; tile < end; ++tile) {
+        const Tile now = next;
+        if (tile + 1 < end) {
+            c.step(1);
+            next.load(c, false);
+        }
+        add_tile(now, [&](int q) { return now.v[q]; }, sum);
+        if ((vecs += kTileBytes / 2 / kThreads) >= kFlush) {  // (an unaligned tile: a value a vector)
+            sum.flush();
+            vecs = 0;
+        }
+    }
+    const double s = cta_sum(sum, red);
+    if (threadIdx.x == 0) {
         part[parts_before + blockIdx.x] = s;
         s_last = false;
         if (last) {
@@ -240,20 +286,10 @@ __global__ void __launch_bounds__(kThreads) k_clip_squares(const __grid_constant
     __syncthreads();
     if (!s_last) return;
     __threadfence();
-    const int parts = parts_before + gridDim.x;
-    double s = 0.0;
-    for (int i = threadIdx.x; i < parts; i += kThreads) s += __ldcg(part + i);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    if ((threadIdx.x & 31) == 0) red[threadIdx.x / 32] = s;
-    __syncthreads();
+    const float nrm = norm_of(part, parts_before + gridDim.x, red, &s_norm);
     if (threadIdx.x == 0) {
-        s = 0.0;
-        for (int i = 0; i < kThreads / 32; ++i) s += red[i];
-        s = sqrt(s);
-        *norm = result->norm = (float)s;
-        const bool clip = s > (double)max_norm && isfinite((float)s);
-        result->scale = clip ? (float)((double)max_norm / s) : 1.f;
+        *norm = nrm;
+        result->scale = scale_of(nrm, max_norm);
         *arrived = 0;
     }
 }
@@ -275,9 +311,81 @@ __global__ void __launch_bounds__(kThreads) k_clip_scale(const __grid_constant__
             c.step(-1);
             next.load(c, true);
         }
-        if (scale == 1.f && now.src == now.dst) continue;
-        if (now.bf16) tile_scale<__nv_bfloat16>(now, scale);
-        else tile_scale<float>(now, scale);
+        scale_tile(now, [&](int q) { return now.v[q]; }, scale);
+    }
+}
+
+// ---- gradients that fit the SMs' shared memory: one launch, every value read once -----------
+// All CTAs run at once (a cooperative launch), hold their tiles in shared memory, and wait for
+// one another's sums.  8.8 MB took 10 us so, and 14 us in the two launches above.
+constexpr int kHeld = 6;                  // tiles a CTA holds
+constexpr unsigned kPolls = 1u << 20;     // the wait's limit: about a second
+
+struct Meet {
+    unsigned arrived, left;
+};
+
+template <int SIZE>
+__global__ void __launch_bounds__(kThreads, 2) k_clip_once(const __grid_constant__ Table<SIZE> t, double *part, float max_norm,
+                                                           float *norm, int copies, Meet *meet, int *status, uint32_t test_wait) {
+    extern __shared__ uint4 held[];  // [kHeld][kEach][kThreads]
+    __shared__ double red[kThreads / 32];
+    __shared__ float s_norm;
+    const int first = split(t.tiles, blockIdx.x), end = split(t.tiles, blockIdx.x + 1);
+    auto vector = [&](int tile, int q) -> uint4 & { return held[((tile - first) * kEach + q) * kThreads + threadIdx.x]; };
+    {
+        Cursor<SIZE> c(t, first);
+        for (int tile = first; tile < end; ++tile, c.step(1)) {
+            Spot p;
+            p.find(c, true);
+#pragma unroll
+            for (int q = 0; q < kEach; ++q)
+                if ((int)threadIdx.x + q * kThreads < p.vecs)
+                    copy_async<16>((uint32_t)__cvta_generic_to_shared(&vector(tile, q)), p.src + (threadIdx.x + q * kThreads) * 16);
+        }
+        copy_commit();
+    }
+    Sum sum;
+    {
+        Cursor<SIZE> c(t, first);
+        copy_wait<0>();  // (its own copies are all that a thread reads)
+        for (int tile = first; tile < end; ++tile, c.step(1)) {
+            Spot p;
+            p.find(c, true);
+            add_tile(p, [&](int q) { return vector(tile, q); }, sum);
+        }
+    }
+    const double s = cta_sum(sum, red);
+    if (threadIdx.x == 0) {
+        part[blockIdx.x] = s;
+        __threadfence();
+        atomicAdd(&meet->arrived, 1u);
+        // (test_wait: one more than there are never arrives)
+        const unsigned want = gridDim.x + (test_wait && blockIdx.x == 0), most = test_wait && blockIdx.x == 0 ? test_wait : kPolls;
+        unsigned polls = 0;
+        while (*(volatile unsigned *)&meet->arrived < want)
+            if (++polls >= most) {
+                seq_record(status + 1, WM_ERR_TIMEOUT);
+                break;
+            }
+        __threadfence();
+    }
+    __syncthreads();
+    const float nrm = norm_of(part, gridDim.x, red, &s_norm);
+    if (threadIdx.x == 0) {
+        if (blockIdx.x == 0) *norm = nrm;
+        if (atomicAdd(&meet->left, 1u) == gridDim.x - 1) {  // the last to have waited: ready for the next call
+            meet->arrived = 0;
+            meet->left = 0;
+        }
+    }
+    const float scale = scale_of(nrm, max_norm);
+    if (scale == 1.f && !copies) return;
+    Cursor<SIZE> c(t, first);
+    for (int tile = first; tile < end; ++tile, c.step(1)) {
+        Spot p;
+        p.find(c, true);
+        scale_tile(p, [&](int q) { return vector(tile, q); }, scale);
     }
 }
 
@@ -315,6 +423,27 @@ cudaError_t clip(wm_seq *h, int count, const wm_seq_grad *grads, float max_norm,
     int left = 0;  // the last tensor that is not empty
     for (int i = 0; i < count; ++i)
         if (grads[i].n) left = i;
+    if (fill(t, grads, count, 0) > left && t.tiles <= 2 * h->sms * kHeld) {
+        auto *k = k_clip_once<SIZE>;
+        const int smem = kHeld * kTileBytes;
+        cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return e;
+        cudaLaunchConfig_t cfg{};
+        cfg.gridDim = dim3((unsigned)(t.tiles < 2 * h->sms ? t.tiles : 2 * h->sms));
+        cfg.blockDim = dim3(kThreads);
+        cfg.dynamicSmemBytes = (size_t)smem;
+        cfg.stream = s;
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeCooperative;
+        at[0].val.cooperative = 1;
+        cfg.attrs = at;
+        cfg.numAttrs = 1;
+        const uint32_t test_wait = h->test_wait;
+        h->test_wait = 0;
+        h->last_launches = 1;
+        return cudaLaunchKernelEx(&cfg, k, (const Table<SIZE>)t, part, max_norm, norm, (int)copies, (Meet *)(h->status + 16), h->status,
+                                  test_wait);
+    }
     int parts = 0;
     for (int i = 0; i <= left;) {
         i += fill(t, grads, count, i);

@@ -16,7 +16,9 @@ struct wm_seq {
     bool ws_captured = false;   // a captured graph may hold ws: it is kept when ws grows
     void *retired[64] = {};     // such earlier workspaces (each at least doubles)
     int n_retired = 0;
-    int *status = nullptr;      // device status words: [0] arguments, [1] a wait gave up
+    // 64 device words: [0] status: arguments, [1] status: a wait gave up; [8] and [16, 17] counters
+    // that the clipping's CTAs meet at (0 between calls)
+    int *status = nullptr;
     int last_launches = 0;
     uint32_t test_wait = 0;     // wm_seq_inject_wait_timeout: polls of the next call's injected wait
     char err[256] = "";

@@ -171,7 +171,8 @@ class SequenceOps:
         self._check(_lib.wm_seq_sync(self.h), "wm_seq_sync")
 
     def inject_wait_timeout(self, polls: int):
-        """wm_seq_inject_wait_timeout: a wait of the next long scan gives up (tests of the timeout path)."""
+        """wm_seq_inject_wait_timeout: a wait of the next long scan or small clipping gives up (tests of
+        the timeout path)."""
         self._check(_lib.wm_seq_inject_wait_timeout(self.h, int(polls)), "wm_seq_inject_wait_timeout")
 
     @property

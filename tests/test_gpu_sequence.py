@@ -484,6 +484,33 @@ def test_clip_unaligned_and_shaped(ops):
         ref.check(o, v, e, "out")
 
 
+@pytest.mark.parametrize("total", [100, 8_400_000, 8_700_000, 20_000_000])
+def test_clip_one_launch_and_two(ops, total):
+    """Around the size up to which the gradients are held on the SMs, and beyond it."""
+    grads = grads_of([total // 2, 3, total // 4 + 1], ["fp32", "bf16", "bf16"], seed=5)
+    grads.append(grads[0].new_zeros(total // 4))
+    norm, ne, want = ref.clip(grads, 100.0)
+    for _ in range(2):
+        out = [torch.empty_like(g) for g in grads]
+        ref.check(ops.clip_grads(grads, 100.0, out=out), norm, ne, "norm")
+        for o, (v, e) in zip(out, want):
+            ref.check(o, v, e, "out")
+    assert ops.last_launches == (1 if total <= 8_400_000 else 2)
+
+
+def test_clip_wait_gives_up(seq):
+    ops = seq.SequenceOps()
+    g = grads_of([3_000_000], ["fp32"])
+    ops.inject_wait_timeout(1000)
+    ops.clip_grads(g, 1e9)
+    with pytest.raises(seq.WMError) as e:
+        ops.sync()
+    assert e.value.status == 4
+    ops.sync()
+    norm, ne, _ = ref.clip(g, 1.0)
+    ref.check(ops.clip_grads(g, 1e9), norm, ne, "norm")
+
+
 @pytest.mark.parametrize("std", [1e-30, 1e-20, 1e18, 1e25])
 def test_clip_range(ops, std):
     """Values whose squares leave fp32's range, with zeros between them."""
@@ -536,12 +563,20 @@ def test_graph_capture(seq):
     s = scan_inputs(400, 1, 64, torch.bfloat16, seed=2)
     t = (torch.arange(3000, device="cuda") % 50).to(torch.int32)
     dout = rnd(3000, 32, seed=1)
-    want = run_scan(ops, s) + (ops.embed_backward(t, dout, 50),)
+    def calls():
+        clipped = [torch.empty_like(dout), torch.empty_like(big_grad)]
+        norms = [ops.clip_grads([dout], 1.0, out=clipped[:1]), ops.clip_grads([big_grad], 1.0, out=clipped[1:])]
+        _, mean, rstd = ops.layer_norm(dout, want_stats=True)
+        return run_scan(ops, s) + (ops.embed_backward(t, dout, 50), *clipped, *norms,
+                                   *ops.layer_norm_backward(dout, None, mean, rstd, dout))
+
+    big_grad = rnd(9_000_000, seed=3)
+    want = calls()
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph, stream=side):
-        got = run_scan(ops, s) + (ops.embed_backward(t, dout, 50),)
+        got = calls()
     graph.replay()
     assert all(torch.equal(a, b) for a, b in zip(want, got))
     # the workspace grows; the graph still has its own
