@@ -665,3 +665,57 @@ def test_wait_gives_up(seq):
     assert e.value.status == 4
     ops.sync()
     check_scan(ops, s)
+
+
+# ------------------------------------------------------------------ the operators together
+def block_module():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "gated_block.py")
+    spec = importlib.util.spec_from_file_location("gated_block", path)
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    return m
+
+
+def test_block_gradients_against_autograd():
+    """A training step's gradients, every operator in it, against torch's derivative of the plain block in 64 bits."""
+    m = block_module()
+    T, N, Z, A, D, H = 37, 6, 8, 11, 40, 24
+    z, actions = m.recordings(T, N, Z, A, "fp32")
+    block = m.GatedBlock(Z, A, D, H)
+    g = torch.Generator().manual_seed(3)
+    starts = (torch.rand(T, N, generator=g) < 0.1).to(torch.uint8).cuda()
+    lengths = torch.tensor([T, 0, 5, T, 20, 1], dtype=torch.int32, device="cuda")
+    pred, saved = block.forward(z[:-1], actions, starts, lengths)
+    dpred = torch.randn(T, N, Z, generator=g).cuda()
+    dpred = dpred * (torch.arange(T, device="cuda")[:, None] < lengths[None, :])[..., None]
+    got = block.backward(saved, dpred)
+    p = {k: v.double().cpu().requires_grad_() for k, v in block.p.items()}
+    e = torch.nn.functional.embedding(actions.cpu().long(), p["embed"]) * block.scale
+    y = torch.nn.functional.layer_norm(e + z[:-1].double().cpu() @ p["w_in"], (D,), p["ln_weight"], p["ln_bias"], 1e-5)
+    proj = y @ p["w_proj"] + p["b_proj"]
+    h = ref.scan(proj[..., :H], proj[..., H:], None, starts, lengths)["h"][0]
+    want = h @ p["w_out"]
+    # fp32 through five operators and six products (torch's products in fp32: tf32 is off)
+    assert float((pred.double().cpu() - want).abs().max()) <= 1e-4 * float(want.abs().max())
+    (want * dpred.double().cpu()).sum().backward()
+    for k, v in p.items():
+        assert float((got[k].double().cpu() - v.grad).norm()) <= 1e-4 * float(v.grad.norm()), k
+
+
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+def test_block_trains_and_dreams(precision):
+    m = block_module()
+    T, N, Z, A, H = 64, 32, 16, 20, 64
+    z, actions = m.recordings(T, N, Z, A, precision)
+    block = m.GatedBlock(Z, A, 64, H, precision)
+    losses = [float(block.train_step(z, actions, lr=1.0)[0]) for _ in range(60)]
+    assert losses[-1] < 0.5 * losses[0], losses[::10]
+    # step by step, the state in hand, the block predicts what the scan over the recording does
+    pred, _ = block.forward(z[:-1], actions)
+    state = torch.zeros(N, H, device="cuda")
+    steps = torch.stack([block.dream(z[t], actions[t], state) for t in range(T)])
+    tol = 1e-4 if precision == "fp32" else 3e-2
+    assert float((steps.float() - pred.float()).abs().max()) <= tol * float(pred.float().abs().max())
+    block.ops.sync()
