@@ -60,7 +60,7 @@ wm_status wm_seq_sync(wm_seq *h);
 /* Message of the last failing call on h (never NULL; "" if none). */
 const char *wm_seq_last_error(const wm_seq *h);
 
-/* Kernels that the last call launched. */
+/* Kernels that the last call launched (memory sets not counted). */
 int wm_seq_last_launches(const wm_seq *h);
 
 /* Failure injection for tests of the timeout path: every wait inside a kernel is bounded.
@@ -155,7 +155,7 @@ wm_status wm_seq_gated_scan_backward(wm_seq *h, int dtype, long long T, int N, i
                                      void *cuda_stream);
 
 /* One gradient of a clipping call: n values at src, written (scaled) to dst, which may
- * be src. */
+ * be src.  Gradients must not overlap one another. */
 typedef struct {
     const void *src;
     void *dst;

@@ -285,6 +285,7 @@ extern "C" wm_status wm_seq_gated_scan(wm_seq *h, int dtype, long long T, int N,
     SEQ_BEGIN("wm_seq_gated_scan");
     SEQ_DTYPE();
     c.that(T >= 0 && T < (1ll << 31) && N >= 0 && H >= 1, "0 <= T < 2^31, N >= 0 and H >= 1 are needed");
+    c.that((long long)N * ((H + 31ll) / 32) < (1ll << 31), "N * ceil(H / 32) must be below 2^31");
     SEQ_CHECKED();
     const bool any = T > 0 && N > 0;
     const size_t es = esize(dtype);
@@ -318,6 +319,7 @@ extern "C" wm_status wm_seq_gated_scan_backward(wm_seq *h, int dtype, long long 
     SEQ_BEGIN("wm_seq_gated_scan_backward");
     SEQ_DTYPE();
     c.that(T >= 0 && T < (1ll << 31) && N >= 0 && H >= 1, "0 <= T < 2^31, N >= 0 and H >= 1 are needed");
+    c.that((long long)N * ((H + 31ll) / 32) < (1ll << 31), "N * ceil(H / 32) must be below 2^31");
     SEQ_CHECKED();
     const bool any = T > 0 && N > 0;
     const size_t es = esize(dtype);

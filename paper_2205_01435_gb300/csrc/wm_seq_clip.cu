@@ -482,10 +482,7 @@ cudaError_t wm_seq_clip_launch(wm_seq *h, int count, const wm_seq_grad *grads, f
     h->last_launches = 0;
     int some = 0;
     for (int i = 0; i < count; ++i) some += grads[i].n > 0;
-    if (!some) {
-        h->last_launches = 1;
-        return cudaMemsetAsync(norm, 0, 4, s);
-    }
+    if (!some) return cudaMemsetAsync(norm, 0, 4, s);
     if (some <= 16) return clip<16>(h, count, grads, max_norm, norm, s);
     if (some <= 128) return clip<128>(h, count, grads, max_norm, norm, s);
     return clip<kTable>(h, count, grads, max_norm, norm, s);

@@ -613,11 +613,8 @@ size_t wm_seq_embed_backward_ws(const wm_seq *h, int dtype, long long n, int V, 
 cudaError_t wm_seq_embed_backward_launch(wm_seq *h, int dtype, long long n, int V, int D, const int32_t *tokens,
                                          const void *dout, float scale, void *dtable, cudaStream_t s) {
     const size_t es = dtype == WM_BF16 ? 2 : 4;
-    if (n == 0) {
-        h->last_launches = 1;
-        return cudaMemsetAsync(dtable, 0, (size_t)V * D * es, s);
-    }
     h->last_launches = 0;
+    if (n == 0) return cudaMemsetAsync(dtable, 0, (size_t)V * D * es, s);
     const Layout l = layout(h, n, V, D, columns(dtype, D, dout, dtable));
     char *ws = (char *)h->ws;
     const int bits = key_bits(V);
@@ -655,7 +652,6 @@ cudaError_t wm_seq_embed_backward_launch(wm_seq *h, int dtype, long long n, int 
     } else {
         const cudaError_t e = cudaMemsetAsync(ws + l.present, 0, (size_t)V, s);
         if (e != cudaSuccess) return e;
-        h->last_launches = 1;
         const int np = (bits + 7) / 8;
         for (int p = 0; p < np; ++p) {
             SortPass a{};

@@ -85,14 +85,16 @@ long long row_stride(const at::Tensor &t, const char *what) {
     const auto st = t.strides();
     const auto sz = t.sizes();
     if (sz[n - 1] > 1 && st[n - 1] != 1) throw Refuse{std::string(what) + ": its last axis must be dense"};
-    long long row = 0, span = 0;  // of the axes seen so far, from the last
+    bool any = false;
+    long long row = sz[n - 1], span = 0;  // the rows' stride; the next axis's, of the axes seen so far from the last
     for (int64_t i = n - 2; i >= 0; --i) {
         if (sz[i] == 1) continue;
-        if (!span) row = st[i];
+        if (!any) row = st[i];
         else if (st[i] != span) throw Refuse{std::string(what) + ": its leading axes must be one run of rows with a fixed stride"};
+        any = true;
         span = st[i] * sz[i];
     }
-    return span ? row : sz[n - 1];
+    return row;
 }
 
 struct Call {

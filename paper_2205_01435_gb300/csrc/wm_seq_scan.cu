@@ -482,7 +482,16 @@ __global__ void __launch_bounds__(kSpanThreads, 4) k_scan_spans(const ScanParams
         unsigned long long *cp = wk.chunk_ps + ((long long)tile * wk.groups + group) * kGroupOf * W + ch;
         unsigned long long *gp = wk.group_ps + ((long long)tile * wk.sections + section) * kGroupOf * W + ch;
         unsigned long long *sp = wk.section + ((long long)tile * wk.sections + section) * W + ch;
-        if (more && part == 0) publish(cp + in_group * W, own);
+        // h0 is read before the chunk publishes: `last` may be the same array, and the last chunk writes it
+        // once all have published
+        float st = 0.f;
+        if (part == 0) {
+            if (section == 0 && j0 + ch < a.H && a.h0) {
+                st = *(const volatile float *)(a.h0 + (long long)n * a.H + j0 + ch);
+                if (a.h0 == a.last) __threadfence();
+            }
+            if (more) publish(cp + in_group * W, own);
+        }
         if (wk.test_wait && ticket == 0 && threadIdx.x == 0) {
             unsigned left = wk.test_wait;
             while (!is_set(peek(sp)) && left-- > 0) {}  // (nothing enters the first section)
@@ -491,12 +500,8 @@ __global__ void __launch_bounds__(kSpanThreads, 4) k_scan_spans(const ScanParams
         const int from = part * EACH, n_near = min(EACH, in_group - from), n_far = min(EACH, in_section - from);
         Published<EACH> pub;
         unsigned long long s0 = 0;
-        float st = 0.f;
         if (in_group) pub.ask(cp + from * W, W, n_near);
-        if (part == 0) {
-            if (section > 0) s0 = peek(sp);
-            else if (j0 + ch < a.H && a.h0) st = a.h0[(long long)n * a.H + j0 + ch];
-        }
+        if (part == 0 && section > 0) s0 = peek(sp);
         if (in_group) {
             near[part][ch] = pub.joined(cp + from * W, W, n_near, a.status);
             if (in_group == kGroupOf - 1 && more) {  // the group's (P, S) goes out before anything else is waited for
@@ -707,7 +712,6 @@ cudaError_t spans(wm_seq *h, const seq_scan_args &a, const Plan &p, cudaStream_t
         h->test_wait = 0;
         const cudaError_t e = cudaMemsetAsync(h->ws, 0xff, p.ws, s);
         if (e != cudaSuccess) return e;
-        ++h->last_launches;
     }
     auto *k = a.reset ? (deep ? k_scan_spans<T, VEC, L, BWD, true, true> : k_scan_spans<T, VEC, L, BWD, true, false>)
                       : (deep ? k_scan_spans<T, VEC, L, BWD, false, true> : k_scan_spans<T, VEC, L, BWD, false, false>);

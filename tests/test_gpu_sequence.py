@@ -227,6 +227,17 @@ def test_step_is_the_scan(ops, dtype):
     assert ops.last_launches == 1
 
 
+@pytest.mark.parametrize("T,N,H", [(3, 2, 8), (40, 100, 512), (100, 2, 40), (20000, 1, 96), (5000, 4, 33)])
+def test_scan_state_in_place(ops, T, N, H):
+    """h_last may be h0, whichever kernel runs and however many CTAs read the state entering the call."""
+    s = scan_inputs(T, N, H, torch.bfloat16, seed=6)
+    want, last = ops.gated_scan(s["gate"], s["x"], h0=s["h0"])
+    for _ in range(3):
+        state = s["h0"].clone()
+        h, got = ops.gated_scan(s["gate"], s["x"], h0=state, h_last=state)
+        assert got is state and torch.equal(h, want) and torch.equal(state, last)
+
+
 def test_scan_offsets_past_32_bits(ops):
     """Steps 2^32 bytes and more apart: 64-bit offsets in every array."""
     T, N, H, far = 5, 2, 64, 2 ** 31 + 64
@@ -333,6 +344,28 @@ def test_norm_hard_rows(ops):
     ref.check(y[ok], *f["y"], "y")
     assert torch.isnan(y[3:5]).all()
     assert torch.equal(y[2], torch.zeros_like(y[2]))
+
+
+def test_norm_rows_of_any_stride(ops):
+    """Rows that are one row repeated, every other row, and runs of rows within wider arrays."""
+    row, dy = rnd(64, seed=1), rnd(5, 64, seed=2)
+    base = rnd(6, 4, 128, seed=3)
+    for x in (row.expand(5, 64), rnd(10, 64, seed=4)[::2], base[1:, 2, 32:96], base[:, :, 64:].flatten(0, 1)[:5], base[2:3, 1:2, :64].expand(5, 1, 64)):
+        y, mean, rstd = ops.layer_norm(x, want_stats=True)
+        ref.check(y, *ref.norm(x, None, None, 1e-5)["y"], str(x.stride()))
+        d = dy.view(x.shape)
+        got = ops.layer_norm_backward(x, None, mean, rstd, d)
+        for k, v in zip(("dx", "dw", "db"), got):
+            ref.check(v, *ref.norm_backward(x, None, mean, rstd, d)[k], k)
+    with pytest.raises(ValueError):  # not one run of rows
+        ops.layer_norm(base[:, :3, :64])
+    with pytest.raises(seq_error()):  # an output's rows may not be one row
+        ops.layer_norm(rnd(5, 64, seed=1), out=row.clone().expand(5, 64))
+
+
+def seq_error():
+    import paper_2205_01435_gb300 as pkg
+    return pkg.load().WMError
 
 
 def test_norm_empty(ops):
