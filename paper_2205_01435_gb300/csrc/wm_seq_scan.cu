@@ -641,24 +641,21 @@ cudaError_t stream_launch(const ScanParams<T> &q, size_t step, cudaStream_t s) {
     return cudaGetLastError();
 }
 
-// The deepest ring with which all CTAs run at once; the smallest when there are more CTAs than that.
+// A ring of 24 steps where all CTAs run at once with it, else of 12.  (512 x 1024 channels, bf16,
+// backward: 125 us with 12 steps and two CTAs an SM, 129 us with 6 steps and all at once.)
 template <class T, int VEC, bool BWD>
 cudaError_t stream(const wm_seq *h, const seq_scan_args &a, cudaStream_t s) {
     const ScanParams<T> q = params<T>(h, a, VEC, BWD);
     const size_t step = (BWD ? 4 : 2) * VEC * sizeof(T) * kThreads;
-    const int per_sm = (int)((blocks(q.groups) + h->sms - 1) / h->sms);
-    const size_t room = (size_t)(220 << 10) / per_sm;
+    const size_t per_sm = (blocks(q.groups) + h->sms - 1) / h->sms;
+    const bool deep = per_sm * (24 * step + 1024) <= (size_t)224 << 10;
     auto go = [&](auto reset) {
         constexpr bool R = decltype(reset)::value;
-        if (room >= 24 * step + 1024) return stream_launch<T, VEC, BWD, R, 4, 6>(q, step, s);
-        if (room >= 12 * step + 1024) return stream_launch<T, VEC, BWD, R, 4, 3>(q, step, s);
-        return stream_launch<T, VEC, BWD, R, 2, 3>(q, step, s);
+        return deep ? stream_launch<T, VEC, BWD, R, 4, 6>(q, step, s) : stream_launch<T, VEC, BWD, R, 4, 3>(q, step, s);
     };
     return a.reset ? go(std::true_type{}) : go(std::false_type{});
 }
 
-// What a call does: its kernel, the values per access, the steps per span and the layout of the
-// workspace.
 constexpr int kLenFwd = 16, kLenBwd = 8, kLenShort = 4;
 struct Plan {
     enum Kind { WALK, STREAM, SPANS } kind;
@@ -670,8 +667,10 @@ struct Plan {
 Plan plan(const wm_seq *h, const seq_scan_args &a, bool bwd) {
     Plan p{};
     const int w4 = a.dtype == WM_BF16 ? 2 : 1;  // values in 4 bytes
-    p.vec = width(a, bwd, 2 * w4);
     const long long C = (long long)a.N * a.H;
+    // 16-byte accesses where they leave an SM's 8 warps and more (512 x 1024, bf16: 66 and 125 us against 76
+    // and 145 with 8 bytes; 200 x 512: 78 and 151 against 70 and 128)
+    p.vec = width(a, bwd, C >= h->sms * 1200ll && a.T > kWalk ? 4 * w4 : 2 * w4);
     if (a.T <= kWalk) {
         p.kind = Plan::WALK;
     } else if (p.vec >= w4 && C >= (long long)h->sms * 300) {
@@ -731,7 +730,8 @@ cudaError_t dispatch(wm_seq *h, const seq_scan_args &a, cudaStream_t s) {
     const Plan p = plan(h, a, BWD);
     if (p.kind == Plan::WALK)
         return p.vec == 2 * W4 ? walk<T, 2 * W4, BWD>(h, a, s) : p.vec == W4 ? walk<T, W4, BWD>(h, a, s) : walk<T, 1, BWD>(h, a, s);
-    if (p.kind == Plan::STREAM) return p.vec == 2 * W4 ? stream<T, 2 * W4, BWD>(h, a, s) : stream<T, W4, BWD>(h, a, s);
+    if (p.kind == Plan::STREAM)
+        return p.vec == 4 * W4 ? stream<T, 4 * W4, BWD>(h, a, s) : p.vec == 2 * W4 ? stream<T, 2 * W4, BWD>(h, a, s) : stream<T, W4, BWD>(h, a, s);
     constexpr int LONG = BWD ? kLenBwd : kLenFwd;
     if (p.vec == W4) return p.len == LONG ? spans<T, W4, LONG, BWD>(h, a, p, s) : spans<T, W4, kLenShort, BWD>(h, a, p, s);
     return p.len == LONG ? spans<T, 1, LONG, BWD>(h, a, p, s) : spans<T, 1, kLenShort, BWD>(h, a, p, s);

@@ -117,7 +117,8 @@ def test_scan_resets_and_lengths(ops, dtype, T, N, H, reset, lengths):
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
 @pytest.mark.parametrize("T,N,H,layout", [(9, 90, 512, "plain"), (33, 160, 301, "plain"), (70, 100, 512, "columns"),
-                                          (40, 48, 1000, "batch"), (11, 95, 514, "plain")])
+                                          (40, 48, 1000, "batch"), (11, 95, 514, "plain"), (14, 200, 1024, "plain"),
+                                          (9, 365, 504, "columns")])
 @pytest.mark.parametrize("masks", [False, True])
 def test_scan_many_channels(ops, dtype, T, N, H, layout, masks):
     check_scan(ops, scan_inputs(T, N, H, DT[dtype], layout, seed=T, reset=masks, lengths=masks))
