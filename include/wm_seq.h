@@ -71,7 +71,8 @@ int wm_seq_last_launches(const wm_seq *h);
  * returned it. */
 wm_status wm_seq_inject_wait_timeout(wm_seq *h, unsigned int polls);
 
-/* Frees what the handle owns (after the device has finished).  NULL is a no-op. */
+/* Frees what the handle owns (after the device has finished); graphs that hold its calls
+ * must not be launched any more.  NULL is a no-op. */
 void wm_seq_destroy(wm_seq *h);
 
 /* Embedding lookup: out[i, :] = scale * table[tokens[i], :].
@@ -85,7 +86,7 @@ wm_status wm_seq_embed(wm_seq *h, int dtype, long long n, int V, int D, const vo
  *   tokens [n] int32;  dout [n, D] dtype, dense;  dtable [V, D] dtype, dense, overwritten
  * The tokens are sorted (stably, so the sums run in a fixed order) and every row is
  * written once; rows that no token took are 0.  Tokens outside [0, V) as above.
- * n < 2^31. */
+ * n <= 2^31 - 65536. */
 wm_status wm_seq_embed_backward(wm_seq *h, int dtype, long long n, int V, int D, const int32_t *tokens, const void *dout,
                                 float scale, void *dtable, void *cuda_stream);
 

@@ -136,6 +136,8 @@ extern "C" wm_status wm_seq_create(wm_seq **out) {
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, h->device);
     if (e == cudaSuccess) e = cudaMalloc((void **)&h->status, 256);
     if (e == cudaSuccess) e = cudaMemset(h->status, 0, 256);
+    if (e == cudaSuccess) e = wm_seq_embed_prepare(h);
+    if (e == cudaSuccess) e = wm_seq_clip_prepare(h);
     if (e != cudaSuccess) {
         cudaGetLastError();
         if (h->status) cudaFree(h->status);
@@ -216,7 +218,7 @@ extern "C" wm_status wm_seq_embed_backward(wm_seq *h, int dtype, long long n, in
                                            const void *dout, float scale, void *dtable, void *cuda_stream) {
     SEQ_BEGIN("wm_seq_embed_backward");
     SEQ_DTYPE();
-    c.that(n >= 0 && n < (1ll << 31) && V >= 1 && D >= 1, "0 <= n < 2^31, V >= 1 and D >= 1 are needed");
+    c.that(n >= 0 && n <= (1ll << 31) - 65536 && V >= 1 && D >= 1, "0 <= n <= 2^31 - 65536, V >= 1 and D >= 1 are needed");
     SEQ_CHECKED();
     c.array(tokens, 4, n > 0, "tokens is NULL");
     c.array(dout, esize(dtype), n > 0, "dout is NULL");

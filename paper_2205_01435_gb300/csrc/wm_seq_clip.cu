@@ -423,15 +423,12 @@ cudaError_t clip(wm_seq *h, int count, const wm_seq_grad *grads, float max_norm,
     int left = 0;  // the last tensor that is not empty
     for (int i = 0; i < count; ++i)
         if (grads[i].n) left = i;
-    if (fill(t, grads, count, 0) > left && t.tiles <= 2 * h->sms * kHeld) {
+    if (fill(t, grads, count, 0) > left && t.tiles <= h->clip_ctas * kHeld) {
         auto *k = k_clip_once<SIZE>;
-        const int smem = kHeld * kTileBytes;
-        cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-        if (e != cudaSuccess) return e;
         cudaLaunchConfig_t cfg{};
-        cfg.gridDim = dim3((unsigned)(t.tiles < 2 * h->sms ? t.tiles : 2 * h->sms));
+        cfg.gridDim = dim3((unsigned)(t.tiles < h->clip_ctas ? t.tiles : h->clip_ctas));
         cfg.blockDim = dim3(kThreads);
-        cfg.dynamicSmemBytes = (size_t)smem;
+        cfg.dynamicSmemBytes = kHeld * kTileBytes;
         cfg.stream = s;
         cudaLaunchAttribute at[1];
         at[0].id = cudaLaunchAttributeCooperative;
@@ -472,7 +469,25 @@ cudaError_t clip(wm_seq *h, int count, const wm_seq_grad *grads, float max_norm,
     return cudaGetLastError();
 }
 
+template <int SIZE>
+cudaError_t prepare_once(wm_seq *h) {
+    int per_sm = 0;
+    cudaError_t e = cudaFuncSetAttribute(k_clip_once<SIZE>, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeld * kTileBytes);
+    if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, k_clip_once<SIZE>, kThreads, kHeld * kTileBytes);
+    if (e == cudaSuccess && per_sm * h->sms < h->clip_ctas) h->clip_ctas = per_sm * h->sms;
+    return e;
+}
+
 }  // namespace
+
+// The kernels' attributes, and the CTAs that run at once (at most two an SM).
+cudaError_t wm_seq_clip_prepare(wm_seq *h) {
+    h->clip_ctas = 2 * h->sms;
+    cudaError_t e = prepare_once<16>(h);
+    if (e == cudaSuccess) e = prepare_once<128>(h);
+    if (e == cudaSuccess) e = prepare_once<kTable>(h);
+    return e;
+}
 
 // Room for the result and the partial sums of up to 65 tables.
 size_t wm_seq_clip_ws(const wm_seq *h) { return 256 + (size_t)most_ctas(h) * 65 * sizeof(double); }

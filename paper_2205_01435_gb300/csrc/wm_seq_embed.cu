@@ -487,7 +487,7 @@ struct Layout {
 };
 Layout layout(const wm_seq *h, long long n, int V, int D, int cols) {  // cols: of a slice
     Layout l{};
-    l.cluster = n <= (long long)kCluster * kPerCta;
+    l.cluster = n <= (long long)h->sort_ranks * kPerCta;
     l.tiles = (int)((n + kTile - 1) / kTile);
     // Positions per block: all blocks' warps run at once (22 of 24 an SM), in blocks of 16 to 256 positions:
     // a second round of warps would run alone, short blocks leave more partial rows.
@@ -594,7 +594,35 @@ int columns(int dtype, int D, const void *dout, const void *dtable) {
     return by_width<float>(D, dout, dtable, [](auto v) { return slice_columns<float, decltype(v)::value>(); });
 }
 
+cudaLaunchConfig_t sort_config(int ranks, size_t smem, cudaLaunchAttribute *attr) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)ranks);
+    cfg.blockDim = dim3(kSortThreads);
+    cfg.dynamicSmemBytes = smem;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)ranks;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cfg;
+}
+
 }  // namespace
+
+// The kernel's attributes, and the largest cluster that the device takes (it has to find the SMs in
+// one of its GPCs).
+cudaError_t wm_seq_embed_prepare(wm_seq *h) {
+    cudaError_t e = cudaFuncSetAttribute(k_sort_cluster, cudaFuncAttributeMaxDynamicSharedMemorySize, kPerCta * 16);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(k_sort_cluster, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    for (h->sort_ranks = kCluster; e == cudaSuccess && h->sort_ranks > 1; h->sort_ranks /= 2) {
+        cudaLaunchAttribute attr[1];
+        const cudaLaunchConfig_t cfg = sort_config(h->sort_ranks, kPerCta * 16, attr);
+        int clusters = 0;
+        e = cudaOccupancyMaxActiveClusters(&clusters, k_sort_cluster, &cfg);
+        if (e == cudaSuccess && clusters > 0) break;
+    }
+    return e;
+}
 
 cudaError_t wm_seq_embed_launch(wm_seq *h, int dtype, long long n, int V, int D, const void *table,
                                 const int32_t *tokens, float scale, void *out, cudaStream_t s) {
@@ -624,7 +652,7 @@ cudaError_t wm_seq_embed_backward_launch(wm_seq *h, int dtype, long long n, int 
         a.n = (int)n; a.V = V;
         // CTAs: 1024 tokens each, as far as the cluster goes
         int ranks = 1;
-        while (ranks < kCluster && (long long)ranks * kSortThreads < n) ranks *= 2;
+        while (ranks < h->sort_ranks && (long long)ranks * kSortThreads < n) ranks *= 2;
         a.per = (int)((n + ranks - 1) / ranks);
         a.passes = (bits + 7) / 8;
         a.bits = (bits + a.passes - 1) / a.passes;
@@ -633,21 +661,11 @@ cudaError_t wm_seq_embed_backward_launch(wm_seq *h, int dtype, long long n, int 
         a.present = (uint8_t *)(ws + l.present);
         a.status = h->status;
         const size_t smem = (size_t)a.per * 16;
-        cudaError_t e = cudaFuncSetAttribute(k_sort_cluster, cudaFuncAttributeMaxDynamicSharedMemorySize, kPerCta * 16);
-        if (e == cudaSuccess && ranks > 8) e = cudaFuncSetAttribute(k_sort_cluster, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        if (e != cudaSuccess) return e;
-        cudaLaunchConfig_t cfg{};
-        cfg.gridDim = dim3((unsigned)ranks);
-        cfg.blockDim = dim3(kSortThreads);
-        cfg.dynamicSmemBytes = smem;
-        cfg.stream = s;
         cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = (unsigned)ranks;
-        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        if ((e = cudaLaunchKernelEx(&cfg, k_sort_cluster, a)) != cudaSuccess) return e;
+        cudaLaunchConfig_t cfg = sort_config(ranks, smem, attr);
+        cfg.stream = s;
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, k_sort_cluster, a);
+        if (e != cudaSuccess) return e;
         h->last_launches = 1;
     } else {
         const cudaError_t e = cudaMemsetAsync(ws + l.present, 0, (size_t)V, s);

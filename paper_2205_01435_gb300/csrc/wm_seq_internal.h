@@ -11,6 +11,8 @@
 struct wm_seq {
     int device = 0;
     int sms = 0;
+    int sort_ranks = 0;  // CTAs of the embedding gradient's sorting cluster, at most
+    int clip_ctas = 0;   // CTAs of the one-launch clipping, at most
     void *ws = nullptr;  // workspace (grows on demand)
     size_t ws_bytes = 0;
     bool ws_captured = false;   // a captured graph may hold ws: it is kept when ws grows
@@ -42,6 +44,10 @@ struct seq_scan_args {
     const int32_t *lengths;
     float *h_last, *dh0;
 };
+
+// What the launchers ask the device for, once a handle.
+cudaError_t wm_seq_embed_prepare(wm_seq *h);
+cudaError_t wm_seq_clip_prepare(wm_seq *h);
 
 // ---- launchers.  *_ws: bytes of workspace a call takes ------------------------------
 size_t wm_seq_scan_ws(const wm_seq *h, const seq_scan_args &a, bool backward);

@@ -239,16 +239,49 @@ def test_scan_state_in_place(ops, T, N, H):
         assert got is state and torch.equal(h, want) and torch.equal(state, last)
 
 
-def test_scan_offsets_past_32_bits(ops):
-    """Steps 2^32 bytes and more apart: 64-bit offsets in every array."""
-    T, N, H, far = 5, 2, 64, 2 ** 31 + 64
-    big = torch.empty(4 * far + 8 * N * H, dtype=torch.bfloat16, device="cuda")
+@pytest.mark.parametrize("T,N,H,far", [(5, 2, 64, 2 ** 31 + 64), (12, 2, 64, 2 ** 29 + 64), (12, 90, 512, 2 ** 29 + 64)])
+def test_scan_offsets_past_32_bits(ops, T, N, H, far):
+    """Arrays whose last steps begin past 2^32 values: 64-bit offsets in every kernel."""
+    big = torch.empty((T - 1) * far + 6 * N * H, dtype=torch.bfloat16, device="cuda")
     s = scan_inputs(T, N, H, torch.bfloat16, seed=9)
     views = [torch.as_strided(big, (T, N, H), (far, H, 1), i * N * H) for i in range(6)]
     for v, k in zip(views, ("gate", "x", "dh")):
         v.copy_(s[k])
         s[k] = v
     check_scan(ops, s, out=views[3], dgate=views[4], dx=views[5])
+
+
+def test_norm_offsets_past_32_bits(ops):
+    far = 2 ** 31 + 24
+    big = torch.empty(2 * far + 3 * 64, dtype=torch.bfloat16, device="cuda")
+    x, y, dx = (torch.as_strided(big, (3, 64), (far, 1), i * 64) for i in range(3))
+    x.copy_(rnd(3, 64, seed=1, dtype=torch.bfloat16))
+    _, mean, rstd = ops.layer_norm(x, out=y, want_stats=True)
+    ref.check(y, *ref.norm(x, None, None, 1e-5)["y"], "y")
+    g = ref.norm_backward(x, None, mean, rstd, y)
+    ops.layer_norm_backward(x, None, mean, rstd, y, dx=dx)
+    ref.check(dx, *g["dx"], "dx")
+
+
+def test_embed_and_clip_past_32_bits(ops):
+    """More than 2^31 values: lookup, gradient (whole numbers, so that the sums are exact) and norm."""
+    n, V, D = 4_300_000, 1000, 512
+    t = ((torch.arange(n, device="cuda") * 7919) % (V + 1) - 1).to(torch.int32)
+    table = rnd(V, D, seed=1, dtype=torch.bfloat16)
+    out = ops.embed(table, t, scale=2.0)
+    at = torch.arange(n - 3000, n, 7, device="cuda")
+    assert torch.equal(out[at], torch.where((t[at] >= 0)[:, None], table[t[at].clamp(min=0).long()] * 2, 0))
+    part = torch.arange(n, device="cuda") % 3
+    out.copy_(part[:, None].expand(n, D))
+    got = ops.embed_backward(t, out, V, scale=0.25)
+    want = torch.zeros(V + 1, dtype=torch.float64, device="cuda").index_add_(0, (t + 1).long(), part.double())[1:] * 0.25
+    assert torch.equal(got, want.to(torch.bfloat16)[:, None].expand(V, D))
+    flat = out.view(-1)
+    flat.fill_(1.0)
+    norm = ops.clip_grads([flat], 1.0)
+    assert abs(float(norm) - math.sqrt(n * D)) <= 1e-6 * math.sqrt(n * D)
+    assert torch.equal(flat[-5:], torch.full_like(flat[-5:], 1.0 / float(norm)))
+    ops.sync()
 
 
 def test_scan_gradient_against_differences(ops):
