@@ -247,12 +247,13 @@ __global__ void __launch_bounds__(cta_threads<TPR>(), fwd_ctas<TPR>())
     }
 }
 
-// part: [gridDim.x][2][D] sums of dw and db over the CTA's rows (null: not wanted)
+// part: [gridDim.x][2][D] sums of dw and db over the CTA's rows (null: not wanted); of a single CTA
+// they go to dw and db at once
 template <class T, int VEC, int E, int TPR>
 __global__ void __launch_bounds__(cta_threads<TPR>(), bwd_ctas<TPR>())
     k_norm_bwd(long long rows, int D, const T *__restrict__ x, long long ldx, const float *__restrict__ w,
                const float *__restrict__ mean, const float *__restrict__ rstd, const T *dy, long long lddy, T *dx, long long lddx,
-               float *__restrict__ part) {
+               float *__restrict__ part, float *dw_out, float *db_out) {
     constexpr int THREADS = cta_threads<TPR>(), RPC = THREADS / TPR;
     constexpr bool SHARED = shared_weights<E, TPR>();
     extern __shared__ __align__(16) unsigned char ring[];  // the rows' ring; after the rows (RPC > 1) sums [RPC][2][D]
@@ -324,26 +325,32 @@ __global__ void __launch_bounds__(cta_threads<TPR>(), bwd_ctas<TPR>())
         in.next(steps);
     }
     if (!part) return;
-    part += (long long)blockIdx.x * 2 * D;
+    const bool single = gridDim.x == 1;
+    float *to_w = single ? dw_out : part + (long long)blockIdx.x * 2 * D, *to_b = single ? db_out : to_w + D;
     if (RPC > 1) __syncthreads();  // the ring is done with: the sums take its place
-    float *cols = reinterpret_cast<float *>(ring);
-    float *to = RPC > 1 ? cols + sub * 2 * D : part;
+    float *cols = reinterpret_cast<float *>(ring) + sub * 2 * D;
+    float *w_at = RPC > 1 ? cols : to_w, *b_at = RPC > 1 ? cols + D : to_b;
 #pragma unroll
     for (int i = 0; i < E / VEC; ++i)
 #pragma unroll
         for (int k = 0; k < VEC; ++k) {
             const int j = (i * TPR + lane) * VEC + k;
             if (j < D) {
-                to[j] = dw[i * VEC + k];
-                to[D + j] = db[i * VEC + k];
+                if (w_at) w_at[j] = dw[i * VEC + k];
+                if (b_at) b_at[j] = db[i * VEC + k];
             }
         }
     if (RPC == 1) return;
     __syncthreads();
+    const float *all = reinterpret_cast<const float *>(ring);
     for (int j = threadIdx.x; j < 2 * D; j += blockDim.x) {
-        float v = cols[j];
-        for (int q = 1; q < RPC; ++q) v += cols[q * 2 * D + j];
-        part[j] = v;
+        float v = all[j];
+        for (int q = 1; q < RPC; ++q) v += all[q * 2 * D + j];
+        if (j < D) {
+            if (to_w) to_w[j] = v;
+        } else if (to_b) {
+            to_b[j - D] = v;
+        }
     }
 }
 
@@ -475,6 +482,8 @@ Shape shape(int D, int vec) {
 int bwd_grid(const wm_seq *h, long long rows, int D) {
     const int rpc = D <= 1024 ? 4 : 1, per_sm = D <= 1024 ? bwd_ctas<32>() : D <= 4096 ? bwd_ctas<128>() : bwd_ctas<256>();
     const long long need = (rows + rpc - 1) / rpc, most = (long long)h->sms * per_sm;
+    // a few rows a warp: one CTA, which needs no second launch
+    if (need <= 4 && D <= 1024) return need > 0;
     return (int)(need < most ? need : most);
 }
 
@@ -517,14 +526,14 @@ cudaError_t fwd(const wm_seq *h, long long rows, int D, const T *x, long long ld
 
 template <class T, int VEC>
 cudaError_t bwd(long long rows, int D, const T *x, long long ldx, const float *w, const float *mean, const float *rstd,
-                const T *dy, long long lddy, T *dx, long long lddx, float *part, int grid, cudaStream_t s) {
+                const T *dy, long long lddy, T *dx, long long lddx, float *part, float *dw, float *db, int grid, cudaStream_t s) {
     const Shape sh = shape(D, VEC);
 #define CALL(E, TPR)                                                                                             \
     {                                                                                                            \
         constexpr int threads = cta_threads<TPR>(), rpc = threads / TPR;                                         \
         const long long ring = Rows<T, VEC, E, TPR, 2, threads>::bytes(), cols = rpc > 1 ? rpc * 8ll * D : 0;     \
         return launch(k_norm_bwd<T, VEC, E, TPR>, grid, threads, (size_t)std::max(ring, cols), s, rows, D, x, ldx, \
-                      w, mean, rstd, dy, lddy, dx, lddx, part);                                                  \
+                      w, mean, rstd, dy, lddy, dx, lddx, part, dw, db);                                          \
     }
     NORM_SHAPES(CALL)
 #undef CALL
@@ -549,15 +558,15 @@ cudaError_t fwd_any(const wm_seq *h, long long rows, int D, const T *x, long lon
 
 template <class T>
 cudaError_t bwd_any(long long rows, int D, const T *x, long long ldx, const float *w, const float *mean, const float *rstd,
-                    const T *dy, long long lddy, T *dx, long long lddx, float *part, int grid, cudaStream_t s) {
+                    const T *dy, long long lddy, T *dx, long long lddx, float *part, float *dw, float *db, int grid, cudaStream_t s) {
     if (D > kBwdMax)
         return launch(k_norm_bwd_long<T>, grid, kLong, 0, s, rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part);
     constexpr int VEC = 16 / sizeof(T);
     const int v = width(VEC, sizeof(T), D, {{x, ldx}, {dy, lddy}, {dx, lddx}});
-    if (v == VEC) return bwd<T, VEC>(rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part, grid, s);
-    if (v == 4) return bwd<T, 4>(rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part, grid, s);
-    if (v == 2) return bwd<T, 2>(rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part, grid, s);
-    return bwd<T, 1>(rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part, grid, s);
+    if (v == VEC) return bwd<T, VEC>(rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part, dw, db, grid, s);
+    if (v == 4) return bwd<T, 4>(rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part, dw, db, grid, s);
+    if (v == 2) return bwd<T, 2>(rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part, dw, db, grid, s);
+    return bwd<T, 1>(rows, D, x, ldx, w, mean, rstd, dy, lddy, dx, lddx, part, dw, db, grid, s);
 }
 
 }  // namespace
@@ -586,12 +595,12 @@ cudaError_t wm_seq_norm_backward_launch(wm_seq *h, int dtype, long long rows, in
     if (grid > 0) {
         const cudaError_t e =
             dtype == WM_BF16
-                ? bwd_any(rows, D, (const bf16 *)x, ldx, w, mean, rstd, (const bf16 *)dy, lddy, (bf16 *)dx, lddx, part, grid, s)
-                : bwd_any(rows, D, (const float *)x, ldx, w, mean, rstd, (const float *)dy, lddy, (float *)dx, lddx, part, grid, s);
+                ? bwd_any(rows, D, (const bf16 *)x, ldx, w, mean, rstd, (const bf16 *)dy, lddy, (bf16 *)dx, lddx, part, dw, db, grid, s)
+                : bwd_any(rows, D, (const float *)x, ldx, w, mean, rstd, (const float *)dy, lddy, (float *)dx, lddx, part, dw, db, grid, s);
         if (e != cudaSuccess) return e;
         h->last_launches = 1;
     }
-    if (dw || db) {  // no rows: zeros
+    if ((dw || db) && (grid != 1 || D > kBwdMax)) {  // no rows: zeros
         // (may start while the rows' kernel still runs: it waits for it itself)
         cudaLaunchConfig_t cfg{};
         cfg.gridDim = dim3((unsigned)((2 * (long long)D + 31) / 32));

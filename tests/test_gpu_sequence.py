@@ -477,6 +477,19 @@ def test_embed_backward_sort_sizes(ops, n, V):
     ref.check(got, *ref.embed_backward(t, dout, V, 1.0), "dtable")
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("n", [31, 255, 256, 257])
+@pytest.mark.parametrize("V,D", [(3, 1000), (5000, 301), (1, 64)])
+def test_embed_backward_few_tokens(ops, dtype, n, V, D):
+    """Up to 256 tokens go without a sort: rows that nearly all tokens took, and none."""
+    g = torch.Generator().manual_seed(n)
+    t = torch.where(torch.rand(n, generator=g) < 0.7, 0, torch.randint(-1, V, (n,), generator=g)).to(torch.int32).cuda()
+    dout = rnd(n, D, seed=2, dtype=DT[dtype])
+    out = torch.full((V, D), 5.0, dtype=DT[dtype], device="cuda")
+    ref.check(ops.embed_backward(t, dout, V, scale=3.0, out=out), *ref.embed_backward(t, dout, V, 3.0), "dtable")
+    assert ops.last_launches == (1 if n <= 256 else 3)
+
+
 @pytest.mark.parametrize("kind", ["one token", "none", "sorted", "reversed", "common"])
 def test_embed_token_orders(ops, kind):
     n, V, D = 9000, 1000, 48
