@@ -11,8 +11,9 @@
 // fp32, whatever tokens they hold, so that a token that fills half of a batch costs no more
 // than tokens that come once.  A run of one token that lies inside a block is written at
 // once; of a run that crosses blocks each block leaves a partial row, and a third launch adds
-// these in order.  Rows that no token took (the sort marks those that one did) are filled
-// with zeros by warps of the second.  A handful of tokens takes one launch without a sort.
+// these in order.  The table is filled with zeros meanwhile, by the SMs that the sort leaves
+// idle.  A handful of tokens takes one launch without a sort.
+#include <algorithm>
 #include <type_traits>
 
 #include "wm_seq_internal.h"
@@ -70,11 +71,23 @@ constexpr int kMaxDigits = 256;
 
 struct ClusterSort {
     int n, V, per, passes, bits;  // pairs of a CTA; digit width
+    unsigned per_inverse;         // floor(2^32 / per) + 1: place / per is its high product, exactly, while place * per < 2^32
     const int32_t *tokens;
     int *key, *pos;
-    uint8_t *present;  // [V]
     int *status;
+    char *zero;  // filled with zeros by the launch's other clusters
+    unsigned long long zero_bytes;
 };
+
+// What CTA `cta` of `ctas` fills.
+__device__ __forceinline__ void fill_zeros(char *p, unsigned long long bytes, unsigned cta, unsigned ctas) {
+    const unsigned long long head = min(bytes, (unsigned long long)(-(uintptr_t)p & 15)), vecs = (bytes - head) / 16;
+    const unsigned long long at = (unsigned long long)cta * kSortThreads + threadIdx.x, step = (unsigned long long)ctas * kSortThreads;
+    const uint4 z = make_uint4(0, 0, 0, 0);
+    for (unsigned long long i = at; i < vecs; i += step) reinterpret_cast<uint4 *>(p + head)[i] = z;
+    if (at < head) p[at] = 0;
+    if (at < bytes - head - vecs * 16) p[head + vecs * 16 + at] = 0;
+}
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -107,12 +120,9 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_sort_cluster(const ClusterS
     const int digits = 1 << a.bits;
     // the sums may be launched now: they wait for this grid's end before they read anything
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if ((int)blockIdx.x >= ranks) return fill_zeros(a.zero, a.zero_bytes, blockIdx.x - ranks, gridDim.x - ranks);
     for (int i = tid; i < kCluster * kMaxDigits; i += kSortThreads) all[i / kMaxDigits][i % kMaxDigits] = 0;
-    for (int v = rank * kSortThreads + tid; v < a.V; v += ranks * kSortThreads) a.present[v] = 0;
-    for (int i = tid; i < m; i += kSortThreads) {
-        const int t = token_row(a.tokens[lo + i], a.V, a.status);
-        order[0][i] = (unsigned long long)(lo + i) << 32 | (unsigned)(t < 0 ? a.V : t);
-    }
+    if ((int)gridDim.x == ranks) fill_zeros(a.zero, a.zero_bytes, rank, ranks);
     cluster_barrier();  // every CTA has started: their shared memory may be written
     // a warp's piece of the CTA's places
     const int piece = ((a.per + 31) / 32 + 31) / 32 * 32;
@@ -124,12 +134,24 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_sort_cluster(const ClusterS
         // (kSortItems + 1: a piece is rounded up to whole warps)
         unsigned long long item[kSortItems + 1];
         unsigned short before[kSortItems + 1];
+        auto mine = [&](int q) { return q * 32 < piece && w * piece + q * 32 + lane < m; };
+        if (pass == 0) {  // all loads in flight together
+            int t[kSortItems + 1];
+#pragma unroll
+            for (int q = 0; q <= kSortItems; ++q) t[q] = mine(q) ? a.tokens[lo + w * piece + q * 32 + lane] : 0;
+#pragma unroll
+            for (int q = 0; q <= kSortItems; ++q) {
+                const int k = token_row(t[q], a.V, a.status);
+                item[q] = (unsigned long long)(lo + w * piece + q * 32 + lane) << 32 | (unsigned)(k < 0 ? a.V : k);
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q <= kSortItems; ++q) item[q] = mine(q) ? from[w * piece + q * 32 + lane] : 0;
+        }
 #pragma unroll
         for (int q = 0; q <= kSortItems; ++q) {
-            const int i = w * piece + q * 32 + lane;
             if (q * 32 >= piece || w * piece + q * 32 >= m) break;  // the same for the whole warp
-            const bool in = i < m && q * 32 + lane < piece;
-            item[q] = in ? from[i] : 0;
+            const bool in = mine(q);
             const int d = in ? ((unsigned)item[q] >> (pass * a.bits)) & (digits - 1) : digits;
             const unsigned same = __match_any_sync(0xffffffffu, d);
             const int r = __popc(same & ((1u << lane) - 1));
@@ -178,20 +200,17 @@ __global__ void __launch_bounds__(kSortThreads, 1) k_sort_cluster(const ClusterS
         __syncthreads();
 #pragma unroll
         for (int q = 0; q <= kSortItems; ++q) {
-            const int i = w * piece + q * 32 + lane;
-            if (q * 32 >= piece || i >= m) break;
+            if (!mine(q)) break;
             const int d = ((unsigned)item[q] >> (pass * a.bits)) & (digits - 1);
-            const int at = base[d] + cnt[w][d] + before[q], r = at / a.per;
+            const int at = base[d] + cnt[w][d] + before[q], r = __umulhi((unsigned)at, a.per_inverse);
             asm volatile("st.shared::cluster.b64 [%0], %1;" ::"r"(peer(to + (at - r * a.per), r)), "l"(item[q]) : "memory");
         }
         cluster_barrier();
     }
     const unsigned long long *done = order[a.passes & 1];
     for (int i = tid; i < m; i += kSortThreads) {
-        const int k = (int)(unsigned)done[i];
-        a.key[lo + i] = k;
+        a.key[lo + i] = (int)(unsigned)done[i];
         a.pos[lo + i] = (int)(done[i] >> 32);
-        if (k < a.V) a.present[k] = 1;
     }
 }
 
@@ -204,8 +223,7 @@ struct SortPass {
     const int32_t *tokens;  // first pass: the tokens; else null
     const int *key_in, *pos_in;
     int *key_out, *pos_out;
-    int *count;        // [kDigits][tiles]
-    uint8_t *present;  // last pass: marked; else null
+    int *count;  // [kDigits][tiles]
     int *status;
 };
 
@@ -282,7 +300,6 @@ __global__ void __launch_bounds__(kSort) k_sort_scatter(const SortPass a) {
             const int to = cnt[w][d] + rank;
             a.key_out[to] = key;
             a.pos_out[to] = a.tokens ? i : a.pos_in[i];
-            if (a.present && key < a.V) a.present[key] = 1;
         }
         __syncthreads();
     }
@@ -294,9 +311,7 @@ constexpr int kSum = 128;
 template <class T>
 struct SumArgs {
     int n, V, D, block, blocks, slices;  // sorted positions a block; slices of 32 * VEC * lane_vectors columns
-    int zero_warps;                      // warps that look for absent rows (32 rows each)
     const int *key, *pos;
-    const uint8_t *present;
     const T *dout;
     T *dtable;
     float scale;
@@ -325,19 +340,8 @@ __device__ __forceinline__ void put_row(T *p, const float (&v)[VEC], float scale
 template <class T, int VEC>
 __global__ void __launch_bounds__(kSum, 6) k_embed_sum(const SumArgs<T> a) {
     const int lane = threadIdx.x & 31;
-    long long unit = (long long)blockIdx.x * (kSum / 32) + threadIdx.x / 32;
+    const long long unit = (long long)blockIdx.x * (kSum / 32) + threadIdx.x / 32;
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    if (unit < a.zero_warps) {  // rows without tokens
-        const long long v = unit * 32 + lane;
-        unsigned absent = __ballot_sync(0xffffffffu, v < a.V && !a.present[v]);
-        const float zero[VEC] = {};
-        for (; absent; absent &= absent - 1) {
-            const long long row = unit * 32 + __ffs(absent) - 1;
-            for (int j = lane * VEC; j < a.D; j += 32 * VEC) put_row<T, VEC>(a.dtable + row * a.D + j, zero, 1.f);
-        }
-        return;
-    }
-    unit -= a.zero_warps;
     if (unit >= (long long)a.blocks * a.slices) return;
     constexpr int R = lane_vectors<T, VEC>(), U = 8 / R < 4 ? 4 : 8 / R;  // vectors of a row per lane; rows in flight
     const int b = (int)(unit / a.slices), j0 = ((int)(unit % a.slices) * 32 * R + lane) * VEC;  // columns j0 + r * 32 * VEC
@@ -542,9 +546,9 @@ int key_bits(int V) {  // keys 0 ... V
 struct Layout {
     bool cluster;
     int tiles, block, blocks;
-    size_t key[2], pos[2], count, present, part, total;
+    size_t key[2], pos[2], count, part, total;
 };
-Layout layout(const wm_seq *h, long long n, int V, int D, int cols) {  // cols: of a slice
+Layout layout(const wm_seq *h, long long n, int D, int cols) {  // cols: of a slice
     Layout l{};
     l.cluster = n <= (long long)h->sort_ranks * kPerCta;
     l.tiles = (int)((n + kTile - 1) / kTile);
@@ -563,8 +567,6 @@ Layout layout(const wm_seq *h, long long n, int V, int D, int cols) {  // cols: 
     }
     l.count = o;
     if (!l.cluster) o += up((size_t)l.tiles * kDigits * 4);
-    l.present = o;
-    o += up((size_t)V);
     l.part = o;
     o += up((size_t)l.blocks * 2 * D * 4);
     l.total = o;
@@ -594,7 +596,7 @@ constexpr int slice_columns() {
 template <class T, int VEC>
 cudaError_t sums(wm_seq *h, SumArgs<T> a, cudaStream_t s) {
     a.slices = (a.D + slice_columns<T, VEC>() - 1) / slice_columns<T, VEC>();
-    const long long warps = (long long)a.blocks * a.slices + a.zero_warps;
+    const long long warps = (long long)a.blocks * a.slices;
     cudaError_t e = follow(k_embed_sum<T, VEC>, (unsigned)((warps + kSum / 32 - 1) / (kSum / 32)), kSum, s, a);
     if (e != cudaSuccess) return e;
     ++h->last_launches;
@@ -629,9 +631,7 @@ template <class T>
 SumArgs<T> sum_args(int n, int V, int D, const Layout &l, char *ws, int at, float scale) {
     SumArgs<T> a{};
     a.n = n; a.V = V; a.D = D; a.block = l.block; a.blocks = l.blocks;
-    a.zero_warps = (int)(((long long)V + 31) / 32);
     a.key = (const int *)(ws + l.key[at]); a.pos = (const int *)(ws + l.pos[at]);
-    a.present = (const uint8_t *)(ws + l.present);
     a.scale = scale; a.part = (float *)(ws + l.part);
     return a;
 }
@@ -706,7 +706,7 @@ cudaError_t wm_seq_embed_launch(wm_seq *h, int dtype, long long n, int V, int D,
 }
 
 size_t wm_seq_embed_backward_ws(const wm_seq *h, int dtype, long long n, int V, int D, const void *dout, const void *dtable) {
-    return n > kFew || (D + 31) / 32 > 65535 ? layout(h, n, V, D, columns(dtype, D, dout, dtable)).total : 0;
+    return n > kFew || (D + 31) / 32 > 65535 ? layout(h, n, D, columns(dtype, D, dout, dtable)).total : 0;
 }
 
 cudaError_t wm_seq_embed_backward_launch(wm_seq *h, int dtype, long long n, int V, int D, const int32_t *tokens,
@@ -719,7 +719,7 @@ cudaError_t wm_seq_embed_backward_launch(wm_seq *h, int dtype, long long n, int 
             return few(h, (int)n, V, D, tokens, (const __nv_bfloat16 *)dout, scale, (__nv_bfloat16 *)dtable, s);
         return few(h, (int)n, V, D, tokens, (const float *)dout, scale, (float *)dtable, s);
     }
-    const Layout l = layout(h, n, V, D, columns(dtype, D, dout, dtable));
+    const Layout l = layout(h, n, D, columns(dtype, D, dout, dtable));
     char *ws = (char *)h->ws;
     const int bits = key_bits(V);
     int at = 0;
@@ -730,21 +730,26 @@ cudaError_t wm_seq_embed_backward_launch(wm_seq *h, int dtype, long long n, int 
         int ranks = 1;
         while (ranks < h->sort_ranks && (long long)ranks * kSortThreads < n) ranks *= 2;
         a.per = (int)((n + ranks - 1) / ranks);
+        a.per = a.per < 2 ? 2 : a.per;
+        a.per_inverse = (unsigned)((1ull << 32) / a.per + 1);
         a.passes = (bits + 7) / 8;
         a.bits = (bits + a.passes - 1) / a.passes;
         a.tokens = tokens;
         a.key = (int *)(ws + l.key[0]); a.pos = (int *)(ws + l.pos[0]);
-        a.present = (uint8_t *)(ws + l.present);
         a.status = h->status;
-        const size_t smem = (size_t)a.per * 16;
+        a.zero = (char *)dtable;
+        a.zero_bytes = (unsigned long long)V * D * es;
         cudaLaunchAttribute attr[1];
-        cudaLaunchConfig_t cfg = sort_config(ranks, smem, attr);
+        cudaLaunchConfig_t cfg = sort_config(ranks, (size_t)a.per * 16, attr);
+        // clusters that fill, a CTA for every 64 KB as far as the SMs go; a small table the sorting one fills
+        const unsigned long long ctas = std::min((a.zero_bytes >> 16) + 1, (unsigned long long)(h->sms - ranks));
+        if (a.zero_bytes > (unsigned long long)ranks << 17) cfg.gridDim = dim3((unsigned)(ranks + (ctas + ranks - 1) / ranks * ranks));
         cfg.stream = s;
         const cudaError_t e = cudaLaunchKernelEx(&cfg, k_sort_cluster, a);
         if (e != cudaSuccess) return e;
         h->last_launches = 1;
     } else {
-        const cudaError_t e = cudaMemsetAsync(ws + l.present, 0, (size_t)V, s);
+        const cudaError_t e = cudaMemsetAsync(dtable, 0, (size_t)V * D * es, s);
         if (e != cudaSuccess) return e;
         const int np = (bits + 7) / 8;
         for (int p = 0; p < np; ++p) {
@@ -755,7 +760,6 @@ cudaError_t wm_seq_embed_backward_launch(wm_seq *h, int dtype, long long n, int 
             at ^= p > 0;
             a.key_out = (int *)(ws + l.key[at]); a.pos_out = (int *)(ws + l.pos[at]);
             a.count = (int *)(ws + l.count);
-            a.present = p + 1 == np ? (uint8_t *)(ws + l.present) : nullptr;
             a.status = h->status;
             k_sort_count<<<l.tiles, kSort, 0, s>>>(a);
             k_sort_prefix<<<1, 1024, 0, s>>>(l.tiles * kDigits, a.count);
