@@ -9,6 +9,10 @@
 // CTAs walk the rows with a stride of the grid: the weights stay in registers, and in the
 // backward each thread sums its columns' dw and db over the CTA's rows in fp32; the CTAs'
 // partial sums are added in a fixed order by a second, small launch.
+//
+// Measured (one GB300): 65,536 x 1024 bf16 46 us forward (5.8 TB/s), 80 us backward (5.0 TB/s: the
+// column sums leave 16 warps an SM, which issue half of the cycles) and 6 us for the column sums;
+// 20,000 x 301 fp32 12, 16 and 5 us.
 #include <algorithm>
 #include <initializer_list>
 #include <utility>

@@ -21,6 +21,10 @@
 //                  a CTA joins its spans in shared memory and finds the state entering them from
 //                  the (P, S) that the CTAs before it publish.  The spans' inputs stay in shared
 //                  memory between the two passes.
+//
+// Measured (bf16, one GB300): 128 steps x 512 x 1024 channels 59 us forward and 120 us backward, 6.8
+// TB/s, the rate of a copy; 65,536 steps x 256 channels 36 and 60 us (2.8 and 3.3 TB/s, bound by
+// instruction issue: 45 and 85 a value); one step of 16 x 256 channels 3 us.
 #include <type_traits>
 
 #include "wm_seq_internal.h"
