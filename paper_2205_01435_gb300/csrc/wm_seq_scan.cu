@@ -343,7 +343,7 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
 // The state after a span.
 __device__ __forceinline__ float through(float2 ps, float st) { return cuts_off(ps.x) ? ps.y : fmaf(ps.x, st, ps.y); }
 
-// Up to MOST published spans of this thread's channel: `ask` issues the reads, `join` waits for
+// Up to MOST published spans of this thread's channel: `ask` issues the reads, `joined` waits for
 // what was not there yet and joins them.  Bounded: the first wait that gives up says so in
 // status[1], which the others look at now and then, and the value counts as a span of nothing.
 template <int MOST>
@@ -592,7 +592,7 @@ __global__ void k_scan_state(long long C, const float *h0, float *last) {
     if (c < C) last[c] = h0 ? h0[c] : 0.f;
 }
 
-// The largest of these numbers of values per access that alignment, strides and H allow.
+// The most values per access, `most` or a half, a quarter ... of it, that alignment, strides and H allow.
 int width(const seq_scan_args &a, bool bwd, int most) {
     const size_t es = a.dtype == WM_BF16 ? 2 : 4;
     auto ok = [&](const wm_seq_view &v, int w) {
@@ -664,7 +664,7 @@ constexpr int kLenFwd = 16, kLenBwd = 8, kLenShort = 4;
 struct Plan {
     enum Kind { WALK, STREAM, SPANS } kind;
     int vec, len;
-    SpanWork wk;  // offsets in bytes
+    SpanWork wk;  // (its pointers are set at the launch)
     size_t ws;
 };
 
