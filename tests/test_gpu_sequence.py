@@ -342,6 +342,21 @@ def test_norm_many_rows(ops, dtype, rows, D):
     assert all(torch.equal(a, b) for a, b in zip(got, again))
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("rows,D", [(1, 9001), (3, 8200), (333, 9000), (333, 9002), (200, 9001), (310, 12288), (310, 12289)])
+def test_norm_long_rows(ops, dtype, rows, D):
+    """Around the longest rows that a CTA's registers hold, of every width, with more rows than CTAs; dx over dy."""
+    x, dy, w = rnd(rows, D, seed=1, dtype=DT[dtype], mean=0.2), rnd(rows, D, seed=2, dtype=DT[dtype]), rnd(D, seed=3, mean=1.0)
+    y, mean, rstd = ops.layer_norm(x, w, None, want_stats=True)
+    ref.check(y, *ref.norm(x, w, None, 1e-5)["y"], "y")
+    g = ref.norm_backward(x, w, mean, rstd, dy)
+    got = ops.layer_norm_backward(x, w, mean, rstd, dy)
+    for k, v in zip(("dx", "dw", "db"), got):
+        ref.check(v, *g[k], k)
+    again = ops.layer_norm_backward(x, w, mean, rstd, dy, dx=dy)
+    assert again[0] is dy and all(torch.equal(a, b) for a, b in zip(got, again))
+
+
 def test_norm_strides_and_in_place(ops):
     wide = rnd(40, 3 * 96 + 1, seed=1)
     for at in (0, 96, 97):  # aligned and not
