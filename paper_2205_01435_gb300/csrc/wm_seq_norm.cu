@@ -29,9 +29,9 @@ constexpr int kFwdMax = 16384, kBwdMax = 12288;
 // rows in shared memory, every thread copying and reading its own vectors (no barrier, and no
 // registers held by loads in flight).  bf16 rows that are not aligned to 4 bytes cannot be
 // copied so: their threads load a row when they come to it.
-template <int E>
+template <int E, int ARRAYS>
 constexpr int ring_rows() {  // two rows and more on their way: 24 KB and more an SM in every variant
-    return E == 8 ? 6 : E <= 16 ? 4 : E == 24 ? 2 : 3;  // (24: 512 threads, 192 KB for two arrays in fp32)
+    return E == 8 ? 6 : E <= 16 ? 4 : E == 24 ? 4 / ARRAYS : 3;  // (24: 512 threads, 192 KB in fp32)
 }
 
 template <class T, int VEC>
@@ -43,7 +43,7 @@ template <class T, int VEC, int E, int TPR, int ARRAYS, int THREADS>
 struct Rows {
     using V = seq_vec<T, VEC>;
     static constexpr bool ASYNC = ring_fits<T, VEC>();
-    static constexpr int RING = ring_rows<E>();
+    static constexpr int RING = ring_rows<E, ARRAYS>();
     V *mine;
     const T *p[ARRAYS];  // the next row to copy (ASYNC), or to load
     long long left;      // rows not copied yet
@@ -211,12 +211,21 @@ __global__ void __launch_bounds__(cta_threads<TPR>(), fwd_ctas<TPR>())
     T *out = y + r * ldy;
     for (; r < rows; r += step, out += step * ldy) {
         in.arrive(steps, D, lane);
+        // without a ring all of a row's loads go out before the first is used (4000 x 9001 bf16: 80 us,
+        // 184 one by one); from the ring they would only hold registers (6000 x 8192 fp32: 63 us, 74 so)
+        constexpr bool AHEAD = !ring_fits<T, VEC>();
+        seq_vec<T, VEC> raw[AHEAD ? E / VEC : 1];
+        if constexpr (AHEAD)
+#pragma unroll
+            for (int i = 0; i < E / VEC; ++i)
+                if ((i * TPR + lane) * VEC < D) raw[i] = in.read(0, i, lane);
         float v[E / VEC][VEC];
         float s = 0.f;
 #pragma unroll
         for (int i = 0; i < E / VEC; ++i) {
             if ((i * TPR + lane) * VEC < D) {
-                seq_unpack(in.read(0, i, lane), v[i]);
+                if constexpr (AHEAD) seq_unpack(raw[i], v[i]);
+                else seq_unpack(in.read(0, i, lane), v[i]);
 #pragma unroll
                 for (int k = 0; k < VEC; ++k) s += v[i][k];
             }
@@ -481,7 +490,7 @@ Shape shape(int D, int vec) {
     if (D <= 1024) return {32, D <= 256 ? 8 : D <= 384 && vec <= 4 ? 12 : D <= 512 ? 16 : 32};
     if (D <= 4096) return {128, D <= 2048 ? 16 : 32};
     if (D <= 8192) return {256, 32};
-    return {512, 32};
+    return {512, D <= 12288 ? 24 : 32};
 }
 
 int bwd_grid(const wm_seq *h, long long rows, int D) {
@@ -525,6 +534,7 @@ cudaError_t fwd(const wm_seq *h, long long rows, int D, const T *x, long long ld
                       Rows<T, VEC, E, TPR, 1, threads>::bytes(), s, rows, D, x, ldx, w, b, eps, y, ldy, mean, rstd);     \
     }
     NORM_SHAPES(CALL)
+    if (sh.e == 24) CALL(24, 512)
     CALL(32, 512)
 #undef CALL
 }
