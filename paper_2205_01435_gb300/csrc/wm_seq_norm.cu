@@ -29,9 +29,10 @@ constexpr int kFwdMax = 16384, kBwdMax = 12288;
 // rows in shared memory, every thread copying and reading its own vectors (no barrier, and no
 // registers held by loads in flight).  bf16 rows that are not aligned to 4 bytes cannot be
 // copied so: their threads load a row when they come to it.
-template <int E, int ARRAYS>
-constexpr int ring_rows() {  // two rows and more on their way: 24 KB and more an SM in every variant
-    return E == 8 ? 6 : E <= 16 ? 4 : E == 24 ? 4 / ARRAYS : 3;  // (24: 512 threads, 192 KB in fp32)
+template <int E, int ARRAYS, int THREADS>
+constexpr int ring_rows() {  // two rows and more on their way: 24 KB and more an SM in every variant, 192 KB at most
+    const int rows = E == 8 ? 6 : E < 32 ? 4 : 3, room = (192 << 10) / (ARRAYS * THREADS * E * 4);
+    return rows < room ? rows : room;
 }
 
 template <class T, int VEC>
@@ -43,7 +44,7 @@ template <class T, int VEC, int E, int TPR, int ARRAYS, int THREADS>
 struct Rows {
     using V = seq_vec<T, VEC>;
     static constexpr bool ASYNC = ring_fits<T, VEC>();
-    static constexpr int RING = ring_rows<E, ARRAYS>();
+    static constexpr int RING = ring_rows<E, ARRAYS, THREADS>();
     V *mine;
     const T *p[ARRAYS];  // the next row to copy (ASYNC), or to load
     long long left;      // rows not copied yet
@@ -482,19 +483,21 @@ int width(int vec, size_t es, int D, std::initializer_list<std::pair<const void 
 
 // Threads per row and values per thread: the fewest of each that hold the row (a warp up to 1024
 // values, so that its sums need no barrier: 65536 x 1024 bf16 backward took 80 us so, and 90 us with
-// 128 threads a row).
+// 128 threads a row).  From 4097 values the backward takes 512 threads where the forward takes 256: its column sums
+// would leave 256 threads an SM (8000 x 6001: fp32 144 us against 178, bf16 124 against 157; forward 84 against 80,
+// 106 against 92).
 struct Shape {
     int tpr, e;
 };
-Shape shape(int D, int vec) {
+Shape shape(int D, int vec, bool bwd) {
     if (D <= 1024) return {32, D <= 256 ? 8 : D <= 384 && vec <= 4 ? 12 : D <= 512 ? 16 : 32};
     if (D <= 4096) return {128, D <= 2048 ? 16 : 32};
-    if (D <= 8192) return {256, 32};
-    return {512, D <= 12288 ? 24 : 32};
+    if (D <= 8192 && !bwd) return {256, 32};
+    return {512, D <= 6144 && vec <= 4 ? 12 : D <= 8192 ? 16 : D <= 12288 ? 24 : 32};
 }
 
 int bwd_grid(const wm_seq *h, long long rows, int D) {
-    const int rpc = D <= 1024 ? 4 : 1, per_sm = D <= 1024 ? bwd_ctas<32>() : D <= 4096 ? bwd_ctas<128>() : bwd_ctas<256>();
+    const int rpc = D <= 1024 ? 4 : 1, per_sm = D <= 1024 ? bwd_ctas<32>() : D <= 4096 ? bwd_ctas<128>() : bwd_ctas<512>();
     const long long need = (rows + rpc - 1) / rpc, most = (long long)h->sms * per_sm;
     // a few rows a warp: one CTA, which needs no second launch
     if (need <= 4 && D <= 1024) return need > 0;
@@ -519,13 +522,12 @@ cudaError_t launch(void (*k)(P...), int grid, int threads, size_t smem, cudaStre
     if (sh.tpr == 32 && sh.e == 16) CALL(16, 32)   \
     if (sh.tpr == 32) CALL(32, 32)                 \
     if (sh.tpr == 128 && sh.e == 16) CALL(16, 128) \
-    if (sh.tpr == 128) CALL(32, 128)               \
-    if (sh.tpr == 256) CALL(32, 256)
+    if (sh.tpr == 128) CALL(32, 128)
 
 template <class T, int VEC>
 cudaError_t fwd(const wm_seq *h, long long rows, int D, const T *x, long long ldx, const float *w, const float *b, float eps,
                 T *y, long long ldy, float *mean, float *rstd, cudaStream_t s) {
-    const Shape sh = shape(D, VEC);
+    const Shape sh = shape(D, VEC, false);
 #define CALL(E, TPR)                                                                                                     \
     {                                                                                                                    \
         constexpr int threads = cta_threads<TPR>(), rpc = threads / TPR;                                                 \
@@ -534,6 +536,7 @@ cudaError_t fwd(const wm_seq *h, long long rows, int D, const T *x, long long ld
                       Rows<T, VEC, E, TPR, 1, threads>::bytes(), s, rows, D, x, ldx, w, b, eps, y, ldy, mean, rstd);     \
     }
     NORM_SHAPES(CALL)
+    if (sh.tpr == 256) CALL(32, 256)
     if (sh.e == 24) CALL(24, 512)
     CALL(32, 512)
 #undef CALL
@@ -542,7 +545,7 @@ cudaError_t fwd(const wm_seq *h, long long rows, int D, const T *x, long long ld
 template <class T, int VEC>
 cudaError_t bwd(long long rows, int D, const T *x, long long ldx, const float *w, const float *mean, const float *rstd,
                 const T *dy, long long lddy, T *dx, long long lddx, float *part, float *dw, float *db, int grid, cudaStream_t s) {
-    const Shape sh = shape(D, VEC);
+    const Shape sh = shape(D, VEC, true);
 #define CALL(E, TPR)                                                                                             \
     {                                                                                                            \
         constexpr int threads = cta_threads<TPR>(), rpc = threads / TPR;                                         \
@@ -551,6 +554,9 @@ cudaError_t bwd(long long rows, int D, const T *x, long long ldx, const float *w
                       w, mean, rstd, dy, lddy, dx, lddx, part, dw, db);                                          \
     }
     NORM_SHAPES(CALL)
+    if constexpr (VEC <= 4)
+        if (sh.e == 12) CALL(12, 512)
+    if (sh.e == 16) CALL(16, 512)
     CALL(24, 512)  // (rows above kBwdMax take the looping kernel)
 #undef CALL
 }
