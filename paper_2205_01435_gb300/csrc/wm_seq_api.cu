@@ -121,6 +121,13 @@ wm_status reserve(wm_seq *h, size_t need, cudaStream_t s, const char *what) {
     return WM_OK;
 }
 
+// Clears the first `bytes` of the status words, and waits for it: a memset of device memory returns before it
+// has run, and nothing orders it before the caller's next launch on a stream that does not wait for the default one.
+cudaError_t clear_status(wm_seq *h, size_t bytes) {
+    const cudaError_t e = cudaMemset(h->status, 0, bytes);
+    return e == cudaSuccess ? cudaStreamSynchronize(cudaStreamLegacy) : e;
+}
+
 wm_status launched(wm_seq *h, cudaError_t e, const char *what) {
     return e == cudaSuccess ? WM_OK : cuda_fail(h, e, what);
 }
@@ -135,7 +142,7 @@ extern "C" wm_status wm_seq_create(wm_seq **out) {
     cudaError_t e = cudaGetDevice(&h->device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->sms, cudaDevAttrMultiProcessorCount, h->device);
     if (e == cudaSuccess) e = cudaMalloc((void **)&h->status, 256);
-    if (e == cudaSuccess) e = cudaMemset(h->status, 0, 256);
+    if (e == cudaSuccess) e = clear_status(h, 256);
     if (e == cudaSuccess) e = wm_seq_embed_prepare(h);
     if (e == cudaSuccess) e = wm_seq_clip_prepare(h);
     if (e != cudaSuccess) {
@@ -169,7 +176,7 @@ extern "C" wm_status wm_seq_sync(wm_seq *h) {
     if (e == cudaSuccess) e = cudaDeviceSynchronize();
     if (e == cudaSuccess) e = cudaMemcpy(st, h->status, sizeof st, cudaMemcpyDeviceToHost);
     // (with a wait that gave up, the counters that calls meet at are reset too)
-    if (e == cudaSuccess && (st[0] || st[1])) e = cudaMemset(h->status, 0, st[1] ? 256 : sizeof st);
+    if (e == cudaSuccess && (st[0] || st[1])) e = clear_status(h, st[1] ? 256 : sizeof st);
     if (e != cudaSuccess) return cuda_fail(h, e, "wm_seq_sync");
     if (st[1]) return fail(h, (wm_status)st[1], "wm_seq_sync", "a wait inside a kernel gave up");
     if (st[0]) return fail(h, (wm_status)st[0], "wm_seq_sync", "a token or a length of an earlier call was out of range");
