@@ -17,6 +17,9 @@
  * arithmetic, states, statistics and sums are fp32 (or wider), rounded once when an
  * output is written.
  *
+ * Sizes: D, H, T and the tokens of a gradient are at most 2^31 - 65536; what a declaration
+ * gives as long long may be larger.
+ *
  * Memory: every array is device or managed memory of the handle's device; host memory
  * is an argument error (nothing is staged).  Outputs must not overlap inputs or each
  * other except where a declaration says so.  Arrays of zero elements may be NULL.
@@ -85,8 +88,7 @@ wm_status wm_seq_embed(wm_seq *h, int dtype, long long n, int V, int D, const vo
 /* Its gradient: dtable[v, :] = scale * sum over i with tokens[i] = v of dout[i, :].
  *   tokens [n] int32;  dout [n, D] dtype, dense;  dtable [V, D] dtype, dense, overwritten
  * The tokens are sorted (stably, so the sums run in a fixed order) and every row is
- * written once; rows that no token took are 0.  Tokens outside [0, V) as above.
- * n <= 2^31 - 65536. */
+ * written once; rows that no token took are 0.  Tokens outside [0, V) as above. */
 wm_status wm_seq_embed_backward(wm_seq *h, int dtype, long long n, int V, int D, const int32_t *tokens, const void *dout,
                                 float scale, void *dtable, void *cuda_stream);
 

@@ -82,6 +82,9 @@ struct Check {
 
 size_t esize(int dtype) { return dtype == WM_BF16 ? 2 : 4; }
 
+// The longest rows, and the most tokens: the kernels' 32-bit indices go past the end by less than 65,536.
+constexpr long long kMostInt = (1ll << 31) - 65536;
+
 // Room for `need` bytes of scratch on the handle, for a call on stream s.
 wm_status reserve(wm_seq *h, size_t need, cudaStream_t s, const char *what) {
     if (need == 0) return WM_OK;
@@ -210,7 +213,7 @@ extern "C" wm_status wm_seq_embed(wm_seq *h, int dtype, long long n, int V, int 
                                   const int32_t *tokens, float scale, void *out, void *cuda_stream) {
     SEQ_BEGIN("wm_seq_embed");
     SEQ_DTYPE();
-    c.that(n >= 0 && V >= 1 && D >= 1, "n >= 0, V >= 1 and D >= 1 are needed");
+    c.that(n >= 0 && V >= 1 && D >= 1 && D <= kMostInt, "n >= 0, V >= 1 and 1 <= D <= 2^31 - 65536 are needed");
     SEQ_CHECKED();
     c.array(table, esize(dtype), n > 0, "table is NULL");
     c.array(tokens, 4, n > 0, "tokens is NULL");
@@ -225,7 +228,8 @@ extern "C" wm_status wm_seq_embed_backward(wm_seq *h, int dtype, long long n, in
                                            const void *dout, float scale, void *dtable, void *cuda_stream) {
     SEQ_BEGIN("wm_seq_embed_backward");
     SEQ_DTYPE();
-    c.that(n >= 0 && n <= (1ll << 31) - 65536 && V >= 1 && D >= 1, "0 <= n <= 2^31 - 65536, V >= 1 and D >= 1 are needed");
+    c.that(n >= 0 && n <= kMostInt && V >= 1 && D >= 1 && D <= kMostInt,
+           "0 <= n <= 2^31 - 65536, V >= 1 and 1 <= D <= 2^31 - 65536 are needed");
     SEQ_CHECKED();
     c.array(tokens, 4, n > 0, "tokens is NULL");
     c.array(dout, esize(dtype), n > 0, "dout is NULL");
@@ -241,7 +245,7 @@ extern "C" wm_status wm_seq_layer_norm(wm_seq *h, int dtype, long long rows, int
                                        float *mean, float *rstd, void *cuda_stream) {
     SEQ_BEGIN("wm_seq_layer_norm");
     SEQ_DTYPE();
-    c.that(rows >= 0 && D >= 1, "rows >= 0 and D >= 1 are needed");
+    c.that(rows >= 0 && D >= 1 && D <= kMostInt, "rows >= 0 and 1 <= D <= 2^31 - 65536 are needed");
     c.that(eps >= 0.f && !isinf(eps), "eps must be finite and >= 0");
     c.that(ldx >= 0, "ldx must be >= 0");
     c.that(rows <= 1 || ldy >= D, "ldy must be >= D");
@@ -266,7 +270,7 @@ extern "C" wm_status wm_seq_layer_norm_backward(wm_seq *h, int dtype, long long 
                                                 long long lddx, float *dweight, float *dbias, void *cuda_stream) {
     SEQ_BEGIN("wm_seq_layer_norm_backward");
     SEQ_DTYPE();
-    c.that(rows >= 0 && D >= 1, "rows >= 0 and D >= 1 are needed");
+    c.that(rows >= 0 && D >= 1 && D <= kMostInt, "rows >= 0 and 1 <= D <= 2^31 - 65536 are needed");
     c.that(ldx >= 0 && lddy >= 0, "ldx and lddy must be >= 0");
     c.that(rows <= 1 || lddx >= D, "lddx must be >= D");
     SEQ_CHECKED();
@@ -293,7 +297,8 @@ extern "C" wm_status wm_seq_gated_scan(wm_seq *h, int dtype, long long T, int N,
                                        void *cuda_stream) {
     SEQ_BEGIN("wm_seq_gated_scan");
     SEQ_DTYPE();
-    c.that(T >= 0 && T < (1ll << 31) && N >= 0 && H >= 1, "0 <= T < 2^31, N >= 0 and H >= 1 are needed");
+    c.that(T >= 0 && T <= kMostInt && N >= 0 && H >= 1 && H <= kMostInt,
+           "0 <= T <= 2^31 - 65536, N >= 0 and 1 <= H <= 2^31 - 65536 are needed");
     c.that((long long)N * ((H + 31ll) / 32) < (1ll << 31), "N * ceil(H / 32) must be below 2^31");
     SEQ_CHECKED();
     const bool any = T > 0 && N > 0;
@@ -327,7 +332,8 @@ extern "C" wm_status wm_seq_gated_scan_backward(wm_seq *h, int dtype, long long 
                                                 void *cuda_stream) {
     SEQ_BEGIN("wm_seq_gated_scan_backward");
     SEQ_DTYPE();
-    c.that(T >= 0 && T < (1ll << 31) && N >= 0 && H >= 1, "0 <= T < 2^31, N >= 0 and H >= 1 are needed");
+    c.that(T >= 0 && T <= kMostInt && N >= 0 && H >= 1 && H <= kMostInt,
+           "0 <= T <= 2^31 - 65536, N >= 0 and 1 <= H <= 2^31 - 65536 are needed");
     c.that((long long)N * ((H + 31ll) / 32) < (1ll << 31), "N * ceil(H / 32) must be below 2^31");
     SEQ_CHECKED();
     const bool any = T > 0 && N > 0;

@@ -373,15 +373,16 @@ __global__ void __launch_bounds__(cta_threads<TPR>(), bwd_ctas<TPR>())
 constexpr int kSlices = 32;
 __global__ void __launch_bounds__(32 * kSlices) k_norm_cols(int parts, int D, const float *__restrict__ part, float *dw, float *db) {
     __shared__ float s[kSlices][33];
-    const int c = blockIdx.x * 32 + threadIdx.x % 32, q = threadIdx.x / 32;
+    const long long c = (long long)blockIdx.x * 32 + threadIdx.x % 32, columns = 2ll * D;
+    const int q = threadIdx.x / 32;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     float v = 0.f;
-    if (c < 2 * D)
+    if (c < columns)
 #pragma unroll 8
-        for (int i = q; i < parts; i += kSlices) v += part[(long long)i * 2 * D + c];
+        for (int i = q; i < parts; i += kSlices) v += part[i * columns + c];
     s[q][threadIdx.x % 32] = v;
     __syncthreads();
-    if (q || c >= 2 * D) return;
+    if (q || c >= columns) return;
 #pragma unroll
     for (int i = 1; i < kSlices; ++i) v += s[i][threadIdx.x];
     if (c < D) {
@@ -444,9 +445,11 @@ __global__ void __launch_bounds__(kLong) k_norm_bwd_long(long long rows, int D, 
                                                          const float *__restrict__ rstd, const T *dy, long long lddy,
                                                          T *dx, long long lddx, float *part) {
     __shared__ float2 red[kLong / 32];
+    float *part_w = nullptr, *part_b = nullptr;
     if (part) {
-        part += (long long)blockIdx.x * 2 * D;
-        for (int j = threadIdx.x; j < D; j += kLong) part[j] = part[D + j] = 0.f;
+        part_w = part + (long long)blockIdx.x * 2 * D;
+        part_b = part_w + D;
+        for (int j = threadIdx.x; j < D; j += kLong) part_w[j] = part_b[j] = 0.f;
     }
     for (long long r = blockIdx.x; r < rows; r += gridDim.x) {
         const T *px = x + r * ldx, *pd = dy + r * lddy;
@@ -461,9 +464,9 @@ __global__ void __launch_bounds__(kLong) k_norm_bwd_long(long long rows, int D, 
         const float m1 = s.x / (float)D, m2 = s.y / (float)D;
         for (int j = threadIdx.x; j < D; j += kLong) {
             const float xh = (seq_to_float(px[j]) - mu) * rs, d = seq_to_float(pd[j]), g = d * (w ? w[j] : 1.f);
-            if (part) {  // j and D + j are this thread's alone
-                part[j] = fmaf(d, xh, part[j]);
-                part[D + j] += d;
+            if (part) {  // column j is this thread's alone
+                part_w[j] = fmaf(d, xh, part_w[j]);
+                part_b[j] += d;
             }
             dx[r * lddx + j] = seq_from_float<T>(rs * (g - m1 - xh * m2));
         }

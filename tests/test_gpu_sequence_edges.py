@@ -40,3 +40,36 @@ def test_new_handle_beside_a_busy_default_stream(seq):
         torch.cuda._sleep(1_000_000)
         ops.sync()
         ref.check(norm, *ref.clip([g], 1e9)[:2], "norm")
+
+
+# ------------------------------------------------------------------ the ends of the range
+def test_norm_of_rows_past_2_30(ops):
+    """One row whose weight and bias gradients together pass 2^31 columns.  Whole numbers whose sums over the row are 0
+    (D is a multiple of 15): every gradient is exact."""
+    D = 2 ** 30 + 11
+    x, dy = ((torch.arange(15) % m - m // 2).to(torch.bfloat16).cuda().repeat(D // 15)[None] for m in (5, 3))
+    y, mean, rstd = ops.layer_norm(x, eps=0.0, want_stats=True)
+    assert float(mean) == 0.0 and abs(float(rstd) - 0.5 ** 0.5) <= 1e-6  # (the mean of 0, 1 and 4 squared: 2)
+    assert torch.equal(y[0, -15:], (x[0, -15:].float() * rstd).to(torch.bfloat16))
+    del y
+    one = torch.ones_like(rstd)
+    dx, dw, db = ops.layer_norm_backward(x, None, mean, one, dy)
+    assert torch.equal(dx, dy)
+    assert torch.equal(db, dy[0].float())
+    assert torch.equal(dw, (dy * x)[0].float())
+    ops.sync()
+
+
+def test_axes_that_the_kernels_cannot_index_are_refused(ops, seq):
+    """32-bit column and step indices go a little past the end: axes that end within that of 2^31 are refused."""
+    lib, h, p = seq._lib, ops.h, torch.empty(64, device="cuda").data_ptr()
+    for big in (2 ** 31 - 65535, 2 ** 31 - 1):
+        assert lib.wm_seq_embed(h, 0, 1, 1, big, p, p, 1.0, p, None) == 1
+        assert lib.wm_seq_embed_backward(h, 0, 1, 1, big, p, p, 1.0, p, None) == 1
+        assert lib.wm_seq_layer_norm(h, 0, 1, big, p, big, None, None, 0.1, p, big, None, None, None) == 1
+        assert lib.wm_seq_layer_norm_backward(h, 0, 1, big, p, big, None, p, p, p, big, p, big, None, None, None) == 1
+        for T, H in ((1, big), (big, 1)):
+            assert lib.wm_seq_gated_scan(h, 0, T, 1, H, *([None] * 8)) == 1
+            assert b"65536" in lib.wm_seq_last_error(h)
+            assert lib.wm_seq_gated_scan_backward(h, 0, T, 1, H, *([None] * 12)) == 1
+            assert b"65536" in lib.wm_seq_last_error(h)
