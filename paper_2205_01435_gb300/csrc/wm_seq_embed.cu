@@ -413,7 +413,8 @@ __global__ void __launch_bounds__(kSum, 6) k_embed_sum(const SumArgs<T> a) {
 
 // A run that crosses blocks: the CTAs of the block where it starts add its parts, a CTA four slices of
 // 128 columns.  A slice goes to a group of warps, whose warps take a stretch of the blocks each;
-// the stretches are added in order.
+// the stretches are added in order.  (CTAs are numbered blocks first, along x alone: rows may have
+// more slices than a grid's y holds.)
 constexpr int kJoin = 256, kJoinColumns = 128, kJoinSlices = 4;
 
 template <class T, int VEC>
@@ -421,7 +422,8 @@ __global__ void __launch_bounds__(kJoin) k_embed_join(const SumArgs<T> a) {
     constexpr int W = kJoin / 32, JV = VEC >= 4 ? 4 : 1, R = 4 / JV;  // a lane's columns: R times JV
     using F = seq_vec<float, JV>;
     __shared__ float s[W][R * JV][32];
-    const int b = blockIdx.x, lo = b * a.block, hi = lo + a.block;
+    const unsigned starts = (unsigned)a.blocks - 1;  // blocks that a run can leave
+    const int group = (int)(blockIdx.x / starts), b = (int)(blockIdx.x - group * starts), lo = b * a.block, hi = lo + a.block;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int k = a.key[hi - 1], k_next = a.key[hi], k_lo = a.key[lo], k_prev = lo > 0 ? a.key[lo - 1] : -1;
     if (k >= a.V || k_next != k || (k_lo == k && k_prev == k)) return;  // no run leaves, or it started before
@@ -434,7 +436,7 @@ __global__ void __launch_bounds__(kJoin) k_embed_join(const SumArgs<T> a) {
         last = q - 1 + (off ? __ffs(off) - 1 : 32);
         if (off) break;
     }
-    const int all = (a.D + kJoinColumns - 1) / kJoinColumns, first = blockIdx.y * kJoinSlices, slices = min(kJoinSlices, all - first);
+    const int all = (a.D + kJoinColumns - 1) / kJoinColumns, first = group * kJoinSlices, slices = min(kJoinSlices, all - first);
     const int warps = W / slices, share = (last - b + warps - 1) / warps;  // warps a slice; blocks a warp
     const int sl = w / warps, part = w % warps, from = b + 1 + part * share, to = min(last + 1, from + share);
     const int j0 = (first + sl) * kJoinColumns + lane * JV;
@@ -605,8 +607,8 @@ cudaError_t sums(wm_seq *h, SumArgs<T> a, cudaStream_t s) {
     if (e != cudaSuccess) return e;
     ++h->last_launches;
     if (a.blocks > 1) {
-        const unsigned columns = (unsigned)((a.D + kJoinColumns * kJoinSlices - 1) / (kJoinColumns * kJoinSlices));
-        e = follow(k_embed_join<T, VEC>, dim3((unsigned)(a.blocks - 1), columns), kJoin, s, a);
+        const unsigned groups = (unsigned)((a.D + kJoinColumns * kJoinSlices - 1) / (kJoinColumns * kJoinSlices));
+        e = follow(k_embed_join<T, VEC>, groups * (unsigned)(a.blocks - 1), kJoin, s, a);
         ++h->last_launches;
     }
     return e;

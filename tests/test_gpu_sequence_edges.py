@@ -73,3 +73,14 @@ def test_axes_that_the_kernels_cannot_index_are_refused(ops, seq):
             assert b"65536" in lib.wm_seq_last_error(h)
             assert lib.wm_seq_gated_scan_backward(h, 0, T, 1, H, *([None] * 12)) == 1
             assert b"65536" in lib.wm_seq_last_error(h)
+
+
+def test_embed_backward_of_wide_rows(ops):
+    """More than 65,535 times 512 columns, in runs that cross blocks of tokens (whole numbers: every sum is exact)."""
+    n, V, D = 260, 3, 33_554_432 + 40
+    t = (torch.arange(n, device="cuda") % (V + 1) - 1).to(torch.int32)
+    part = (torch.arange(n, device="cuda") % 7).to(torch.bfloat16)
+    got = ops.embed_backward(t, part[:, None].expand(n, D).contiguous(), V, scale=0.5)
+    want = torch.zeros(V + 1, device="cuda").index_add_(0, (t + 1).long(), part.float())[1:] * 0.5
+    assert torch.equal(got, want.to(torch.bfloat16)[:, None].expand(V, D))
+    ops.sync()
