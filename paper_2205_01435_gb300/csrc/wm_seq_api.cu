@@ -14,7 +14,9 @@ wm_status fail(wm_seq *h, wm_status st, const char *what, const char *why) {
     return st;
 }
 
+// (The runtime keeps a failing call's error until it is asked for: the next launch would report it again.)
 wm_status cuda_fail(wm_seq *h, cudaError_t e, const char *what) {
+    cudaGetLastError();
     return fail(h, e == cudaErrorMemoryAllocation ? WM_ERR_OOM : WM_ERR_CUDA, what, cudaGetErrorString(e));
 }
 
@@ -105,10 +107,7 @@ wm_status reserve(wm_seq *h, size_t need, cudaStream_t s, const char *what) {
         e = cudaMalloc(&p, n);
         if (e != cudaSuccess) {
             cudaGetLastError();
-            if ((e = cudaMalloc(&p, n = need)) != cudaSuccess) {
-                cudaGetLastError();
-                return cuda_fail(h, e, what);
-            }
+            if ((e = cudaMalloc(&p, n = need)) != cudaSuccess) return cuda_fail(h, e, what);
         }
         if (h->ws) {
             if (h->ws_captured)

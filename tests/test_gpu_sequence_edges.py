@@ -1,5 +1,7 @@
 """The sequence operators' handles, streams and ends of range: what a call leaves behind, what runs beside it, and the
 largest and smallest values and sizes."""
+import ctypes as C
+
 import pytest
 import torch
 
@@ -40,6 +42,29 @@ def test_new_handle_beside_a_busy_default_stream(seq):
         torch.cuda._sleep(1_000_000)
         ops.sync()
         ref.check(norm, *ref.clip([g], 1e9)[:2], "norm")
+
+
+def test_an_error_is_reported_once(seq):
+    """A CUDA call that fails inside a call is that call's error, and nobody else's: here the device cannot be waited
+    for, so that the workspace cannot grow, while a stream is being captured."""
+    rt = C.CDLL("libcudart.so.13")
+    stream, graph = C.c_void_p(), C.c_void_p()
+    assert rt.cudaStreamCreateWithFlags(C.byref(stream), 1) == 0
+    ops = seq.SequenceOps()
+    t = (torch.arange(3000, device="cuda") % 50).to(torch.int32)
+    dout, table = torch.ones(3000, 32, device="cuda"), torch.empty(50, 32, device="cuda")
+    torch.cuda.synchronize()
+    assert rt.cudaStreamBeginCapture(stream, 0) == 0
+    try:
+        with pytest.raises(seq.WMError) as e:
+            ops.embed_backward(t, dout, 50, out=table)
+        left = rt.cudaPeekAtLastError()
+    finally:
+        rt.cudaStreamEndCapture(stream, C.byref(graph))
+        rt.cudaGetLastError()
+    assert e.value.status == 2 and left == 0
+    assert torch.equal(ops.embed_backward(t, dout, 50, out=table), torch.full_like(table, 60.0))
+    rt.cudaStreamDestroy(stream)
 
 
 # ------------------------------------------------------------------ the ends of the range
