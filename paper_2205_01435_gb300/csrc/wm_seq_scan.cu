@@ -311,10 +311,11 @@ constexpr int kGroupBits = 4, kGroupOf = 1 << kGroupBits;
 constexpr unsigned kPolls = 1u << 20;  // a wait's limit: about a second
 
 struct SpanWork {
-    unsigned *ticket;
-    unsigned long long *chunk_ps, *group_ps;  // [tile][groups][kGroupOf][W], [tile][sections][kGroupOf][W]
-    unsigned long long *section;              // [tile][sections][W]: the state entering it
-    int chunks, groups, sections, tiles;      // chunks, groups, sections of a tile; tiles in all
+    unsigned *ticket;                         // (8 bytes on: a place that nothing sets)
+    // places for what is published, and no more: the last chunk of a tile publishes nothing, nor does what it ends
+    unsigned long long *chunk_ps, *group_ps;  // [tile][chunks - 1][W], [tile][groups][W]
+    unsigned long long *section;              // [tile][sections][W]: the state leaving it
+    int chunks, groups, sections, tiles;      // chunks of a tile, groups and sections with chunks after them; tiles in all
     int tiles_per_n;
     uint32_t test_wait;                       // > 0: the first chunk polls what nothing sets
 };
@@ -483,8 +484,8 @@ __global__ void __launch_bounds__(kSpanThreads, 4) k_scan_spans(const ScanParams
     if (DEEP) {
         const int group = chunk >> kGroupBits, in_group = chunk & (kGroupOf - 1);
         const int section = group >> kGroupBits, in_section = group & (kGroupOf - 1);
-        unsigned long long *cp = wk.chunk_ps + ((long long)tile * wk.groups + group) * kGroupOf * W + ch;
-        unsigned long long *gp = wk.group_ps + ((long long)tile * wk.sections + section) * kGroupOf * W + ch;
+        unsigned long long *cp = wk.chunk_ps + ((long long)tile * (wk.chunks - 1) + group * kGroupOf) * W + ch;
+        unsigned long long *gp = wk.group_ps + ((long long)tile * wk.groups + section * kGroupOf) * W + ch;
         unsigned long long *sp = wk.section + ((long long)tile * wk.sections + section) * W + ch;
         // h0 is read before the chunk publishes: `last` may be the same array, and the last chunk writes it
         // once all have published
@@ -498,14 +499,14 @@ __global__ void __launch_bounds__(kSpanThreads, 4) k_scan_spans(const ScanParams
         }
         if (wk.test_wait && ticket == 0 && threadIdx.x == 0) {
             unsigned left = wk.test_wait;
-            while (!is_set(peek(sp)) && left-- > 0) {}  // (nothing enters the first section)
+            while (!is_set(peek(reinterpret_cast<unsigned long long *>(wk.ticket) + 1)) && left-- > 0) {}
             seq_record(a.status + 1, WM_ERR_TIMEOUT);
         }
         const int from = part * EACH, n_near = min(EACH, in_group - from), n_far = min(EACH, in_section - from);
         Published<EACH> pub;
         unsigned long long s0 = 0;
         if (in_group) pub.ask(cp + from * W, W, n_near);
-        if (part == 0 && section > 0) s0 = peek(sp);
+        if (part == 0 && section > 0) s0 = peek(sp - W);
         if (in_group) {
             near[part][ch] = pub.joined(cp + from * W, W, n_near, a.status);
             if (in_group == kGroupOf - 1 && more) {  // the group's (P, S) goes out before anything else is waited for
@@ -526,7 +527,7 @@ __global__ void __launch_bounds__(kSpanThreads, 4) k_scan_spans(const ScanParams
         if (part == 0) {
             if (section > 0) {
                 Published<1> left{{s0}};
-                st = left.joined(sp, 0, 1, a.status).y;
+                st = left.joined(sp - W, 0, 1, a.status).y;
             }
             if (in_section)
 #pragma unroll
@@ -536,7 +537,7 @@ __global__ void __launch_bounds__(kSpanThreads, 4) k_scan_spans(const ScanParams
                 for (int q = 0; q < PARTS; ++q) st = through(near[q][ch], st);
             enter[ch] = st;
             st = through(own, st);
-            if (more && in_group == kGroupOf - 1 && in_section == kGroupOf - 1) publish(sp + W, make_float2(0.f, st));
+            if (more && in_group == kGroupOf - 1 && in_section == kGroupOf - 1) publish(sp, make_float2(0.f, st));
             if (!more && a.last && j0 + ch < a.H) a.last[(long long)n * a.H + j0 + ch] = st;
         }
     } else if (part == 0) {
@@ -690,12 +691,9 @@ Plan plan(const wm_seq *h, const seq_scan_args &a, bool bwd) {
         p.len = bwd ? kLenBwd : kLenFwd;
         if ((a.T + SUBS * p.len - 1) / (SUBS * p.len) * k.tiles < h->sms) p.len = kLenShort;
         k.chunks = (int)((a.T + SUBS * p.len - 1) / (SUBS * p.len));
-        k.groups = (k.chunks + kGroupOf - 1) / kGroupOf;
-        k.sections = (k.groups + kGroupOf - 1) / kGroupOf;
-        if (k.chunks > 1) {
-            const size_t t = (size_t)k.tiles * W * 8;
-            p.ws = 256 + t * kGroupOf * (k.groups + k.sections) + t * k.sections;
-        }
+        k.groups = (k.chunks - 1) / kGroupOf;
+        k.sections = k.groups / kGroupOf;
+        if (k.chunks > 1) p.ws = 256 + (size_t)k.tiles * W * 8 * (k.chunks - 1ll + k.groups + k.sections);
     }
     return p;
 }
@@ -709,8 +707,8 @@ cudaError_t spans(wm_seq *h, const seq_scan_args &a, const Plan &p, cudaStream_t
         const size_t t = (size_t)wk.tiles * 32 * VEC;
         wk.ticket = (unsigned *)h->ws;
         wk.chunk_ps = (unsigned long long *)((char *)h->ws + 256);
-        wk.group_ps = wk.chunk_ps + t * wk.groups * kGroupOf;
-        wk.section = wk.group_ps + t * wk.sections * kGroupOf;
+        wk.group_ps = wk.chunk_ps + t * (wk.chunks - 1);
+        wk.section = wk.group_ps + t * wk.groups;
         wk.test_wait = h->test_wait;
         h->test_wait = 0;
         const cudaError_t e = cudaMemsetAsync(h->ws, 0xff, p.ws, s);

@@ -67,6 +67,24 @@ def test_an_error_is_reported_once(seq):
     rt.cudaStreamDestroy(stream)
 
 
+@pytest.mark.parametrize("T,chunks", [(130, (2, 3)), (4100, (33, 65))])
+def test_scan_workspace(seq, T, chunks):
+    """Scratch of a scan in spans: 8 bytes a chunk and channel, a 16th more for groups of chunks, a 256th for theirs
+    (and an 8th of it in hand, in blocks of 2 MB), however few the chunks and narrow the rows."""
+    N, H, lanes = 200_000 // T * 40, 1, 32
+    v = [torch.randn(T, N, H, device="cuda").bfloat16() for _ in range(6)]
+    for k, call in enumerate((lambda o: o.gated_scan(v[0], v[1], out=v[2], want_last=False),
+                              lambda o: o.gated_scan_backward(v[0], v[1], v[2], v[3], dgate=v[4], dx=v[5], want_dh0=False))):
+        ops = seq.SequenceOps()
+        call(warm := seq.SequenceOps())
+        warm.sync()
+        free = torch.cuda.mem_get_info()[0]
+        call(ops)
+        ops.sync()
+        took = free - torch.cuda.mem_get_info()[0]
+        assert took <= N * lanes * 8 * chunks[k] * (1 + 1 / 16 + 1 / 256) * 1.125 + (4 << 20), took
+
+
 # ------------------------------------------------------------------ the ends of the range
 def test_norm_of_rows_past_2_30(ops):
     """One row whose weight and bias gradients together pass 2^31 columns.  Whole numbers whose sums over the row are 0
@@ -109,3 +127,9 @@ def test_embed_backward_of_wide_rows(ops):
     want = torch.zeros(V + 1, device="cuda").index_add_(0, (t + 1).long(), part.float())[1:] * 0.5
     assert torch.equal(got, want.to(torch.bfloat16)[:, None].expand(V, D))
     ops.sync()
+
+
+def test_scan_of_several_sections(ops):
+    """More than 256 chunks a tile, in both directions: a state published every 256 chunks."""
+    from test_gpu_sequence import check_scan, scan_inputs
+    check_scan(ops, scan_inputs(33_100, 1, 8, torch.bfloat16, seed=12, reset=True))
