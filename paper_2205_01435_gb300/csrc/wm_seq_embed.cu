@@ -511,8 +511,10 @@ __global__ void __launch_bounds__(kFewThreads) k_embed_few(int n, int V, int D, 
     const long long step = (long long)gridDim.x * (kFewThreads / 32);
     for (long long v = (long long)blockIdx.x * (kFewThreads / 32) + threadIdx.x / 32; v < V; v += step) {
         float acc[R][VEC] = {};
+        bool taken = false;
         for (int at = 0; at < n && marks[v % kMarks]; at += 32) {
             unsigned left = __ballot_sync(0xffffffffu, tok[at + lane] == v);
+            taken |= left != 0;
             while (left) {
                 seq_vec<T, VEC> x[U][R];
                 const int count = __popc(left);
@@ -537,7 +539,7 @@ __global__ void __launch_bounds__(kFewThreads) k_embed_few(int n, int V, int D, 
         }
 #pragma unroll
         for (int r = 0; r < R; ++r)
-            if (mine(r)) put_row<T, VEC>(dtable + v * D + j0 + r * 32 * VEC, acc[r], scale);
+            if (mine(r)) put_row<T, VEC>(dtable + v * D + j0 + r * 32 * VEC, acc[r], taken ? scale : 0.f);
     }
 }
 

@@ -133,3 +133,16 @@ def test_scan_of_several_sections(ops):
     """More than 256 chunks a tile, in both directions: a state published every 256 chunks."""
     from test_gpu_sequence import check_scan, scan_inputs
     check_scan(ops, scan_inputs(33_100, 1, 8, torch.bfloat16, seed=12, reset=True))
+
+
+@pytest.mark.parametrize("scale", [float("inf"), float("nan"), 3e38])
+@pytest.mark.parametrize("n", [3, 300])
+def test_embed_scale_reaches_taken_rows_only(ops, n, scale):
+    """Rows that no token took are 0 whatever the scale, with a sort and without."""
+    t = torch.tensor([1, -1, 3], dtype=torch.int32, device="cuda").repeat(n // 3)
+    g = ops.embed_backward(t, torch.full((n, 8), 100.0, device="cuda"), 5, scale=scale)
+    assert torch.equal(g[[0, 2, 4]], torch.zeros(3, 8, device="cuda"))
+    want = torch.full((2, 8), 100.0 * (n // 3), device="cuda") * torch.tensor(scale, dtype=torch.float32, device="cuda")
+    assert torch.equal(g[[1, 3]], want) or (scale != scale and g[[1, 3]].isnan().all())
+    table = torch.ones(5, 8, device="cuda")
+    assert torch.equal(ops.embed(table, t, scale=scale)[1], torch.zeros(8, device="cuda"))
