@@ -38,9 +38,10 @@ struct Table {
     int tile_end[SIZE];          // tiles of this and the tensors before
 };
 
-// What the first launches leave for the second ones.
-struct Result {
-    float scale;  // 1: leave the gradients as they are
+// What the gradients are multiplied by, and what the first launches leave for the second ones.
+struct Scale {
+    float by;    // 1: leave the gradients as they are
+    float then;  // 1 but where their product is below fp32's normal range
 };
 
 // A sum of fp32 values as hi + lo, and in fp64 what does not fit fp32.
@@ -242,9 +243,29 @@ __device__ __forceinline__ float norm_of(const double *part, int parts, double *
     __syncthreads();
     return *out;
 }
-// min(1, max_norm / norm); 1 where the norm is not finite.
-__device__ __forceinline__ float scale_of(float norm, float max_norm) {
-    return norm > max_norm && isfinite(norm) ? __fdiv_rn(max_norm, norm) : 1.f;
+// min(1, max_norm / norm); 1 where the norm is not finite.  A quotient below fp32's normal range has
+// lost bits that values of up to 1e38 would show: it is 2^-64 times one that has not.
+__device__ __forceinline__ Scale scale_of(float norm, float max_norm) {
+    if (!(norm > max_norm && isfinite(norm))) return {1.f, 1.f};
+    const float s = __fdiv_rn(max_norm, norm);
+    return s >= 0x1p-126f ? Scale{s, 1.f} : Scale{0x1p-64f, __fdiv_rn(max_norm * 0x1p64f, norm)};
+}
+// Tiles [first, end) by such a product.  (Apart from the tiles' loops, where a second product, met or
+// not, cost 12 registers a thread and 2% of the time of large gradients.)
+template <int SIZE>
+__device__ __noinline__ void scale_twice(const Table<SIZE> &t, int first, int end, Scale scale) {
+    Cursor<SIZE> c(t, first);
+    for (int tile = first; tile < end; ++tile, c.step(1)) {
+        Spot p;
+        p.find(c, true);
+        for (int i = threadIdx.x; i < p.n; i += kThreads) {
+            if (p.bf16)
+                reinterpret_cast<__nv_bfloat16 *>(p.dst)[i] = seq_from_float<__nv_bfloat16>(
+                    seq_to_float(reinterpret_cast<const __nv_bfloat16 *>(p.src)[i]) * scale.by * scale.then);
+            else
+                reinterpret_cast<float *>(p.dst)[i] = reinterpret_cast<const float *>(p.src)[i] * scale.by * scale.then;
+        }
+    }
 }
 
 // CTA b's tiles: [first, last) of an even split.
@@ -254,7 +275,7 @@ __device__ __forceinline__ int split(int tiles, int b) { return (int)((long long
 // last launch adds them, always in the same order, and leaves the norm and the scale.
 template <int SIZE>
 __global__ void __launch_bounds__(kThreads) k_clip_squares(const __grid_constant__ Table<SIZE> t, double *part, int parts_before,
-                                                           int last, float max_norm, Result *result, float *norm,
+                                                           int last, float max_norm, Scale *result, float *norm,
                                                            unsigned *arrived) {
     __shared__ double red[kThreads / 32];
     __shared__ float s_norm;
@@ -292,19 +313,20 @@ __global__ void __launch_bounds__(kThreads) k_clip_squares(const __grid_constant
     const float nrm = norm_of(part, parts_before + gridDim.x, red, &s_norm);
     if (threadIdx.x == 0) {
         *norm = nrm;
-        result->scale = scale_of(nrm, max_norm);
+        *result = scale_of(nrm, max_norm);
         *arrived = 0;
     }
 }
 
 template <int SIZE>
-__global__ void __launch_bounds__(kThreads) k_clip_scale(const __grid_constant__ Table<SIZE> t, const Result *result,
+__global__ void __launch_bounds__(kThreads) k_clip_scale(const __grid_constant__ Table<SIZE> t, const Scale *result,
                                                          int copies) {
     const int first = split(t.tiles, blockIdx.x), end = split(t.tiles, blockIdx.x + 1);
     Cursor<SIZE> c(t, end - 1);
     // launched while the first kernel still runs: its result is there after this
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const float scale = __ldcg(&result->scale);
+    const float scale = __ldcg(&result->by), then = __ldcg(&result->then);
+    if (then != 1.f) return scale_twice(t, first, end, {scale, then});
     if (scale == 1.f && !copies) return;  // (copies: some dst is not its src)
     Tile next;
     next.load(c, true);
@@ -382,7 +404,9 @@ __global__ void __launch_bounds__(kThreads, 2) k_clip_once(const __grid_constant
             meet->left = 0;
         }
     }
-    const float scale = scale_of(nrm, max_norm);
+    const Scale factor = scale_of(nrm, max_norm);
+    if (factor.then != 1.f) return scale_twice(t, first, end, factor);
+    const float scale = factor.by;
     if (scale == 1.f && !copies) return;
     Cursor<SIZE> c(t, first);
     for (int tile = first; tile < end; ++tile, c.step(1)) {
@@ -417,7 +441,7 @@ int fill(Table<SIZE> &t, const wm_seq_grad *g, int count, int from) {
 
 template <int SIZE>
 cudaError_t clip(wm_seq *h, int count, const wm_seq_grad *grads, float max_norm, float *norm, cudaStream_t s) {
-    Result *result = (Result *)h->ws;
+    Scale *result = (Scale *)h->ws;
     double *part = (double *)((char *)h->ws + 256);
     unsigned *arrived = (unsigned *)h->status + 8;
     Table<SIZE> t;
@@ -465,7 +489,7 @@ cudaError_t clip(wm_seq *h, int count, const wm_seq_grad *grads, float max_norm,
         cfg.stream = s;
         cfg.attrs = at;
         cfg.numAttrs = one;  // later tables follow a scale launch, whose end says nothing of the norm
-        const cudaError_t e = cudaLaunchKernelEx(&cfg, k_clip_scale<SIZE>, (const Table<SIZE>)t, (const Result *)result, (int)copies);
+        const cudaError_t e = cudaLaunchKernelEx(&cfg, k_clip_scale<SIZE>, (const Table<SIZE>)t, (const Scale *)result, (int)copies);
         if (e != cudaSuccess) return e;
         ++h->last_launches;
     }

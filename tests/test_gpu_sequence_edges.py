@@ -146,3 +146,15 @@ def test_embed_scale_reaches_taken_rows_only(ops, n, scale):
     assert torch.equal(g[[1, 3]], want) or (scale != scale and g[[1, 3]].isnan().all())
     table = torch.ones(5, 8, device="cuda")
     assert torch.equal(ops.embed(table, t, scale=scale)[1], torch.zeros(8, device="cuda"))
+
+
+@pytest.mark.parametrize("n", [5000, 9_000_000])
+@pytest.mark.parametrize("bound", [1e-12, 1e-9, 1e-42])
+def test_clip_by_more_than_fp32_holds(ops, n, bound):
+    """A factor below fp32's normal range: the clipped values keep their precision, in one launch and two."""
+    g = [torch.randn(n, generator=torch.Generator().manual_seed(n)).cuda() * 1e30, torch.ones(3, dtype=torch.bfloat16, device="cuda")]
+    norm, ne, want = ref.clip(g, bound)
+    out = [torch.empty_like(v) for v in g]
+    ref.check(ops.clip_grads(g, bound, out=out), norm, ne, "norm")
+    for o, (v, e) in zip(out, want):
+        ref.check(o, v, e, "out")
