@@ -284,7 +284,7 @@ extern "C" wm_status wm_seq_layer_norm_backward(wm_seq *h, int dtype, long long 
     c.that(dx != dy || lddx == lddy || rows <= 1, "dx may be dy with the same row stride only");
     c.that(dx != x || rows == 0, "dx must not be x");
     SEQ_CHECKED();
-    const wm_status st = reserve(h, wm_seq_norm_backward_ws(h, rows, D), s, kWhat);
+    const wm_status st = reserve(h, wm_seq_norm_backward_ws(h, dtype, rows, D, x, ldx, dy, lddy, dx, lddx), s, kWhat);
     if (st != WM_OK) return st;
     return launched(h, wm_seq_norm_backward_launch(h, dtype, rows, D, x, ldx, weight, mean, rstd, dy, lddy, dx, lddx,
                                                    dweight, dbias, s), kWhat);

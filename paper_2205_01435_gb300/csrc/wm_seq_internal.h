@@ -56,7 +56,8 @@ cudaError_t wm_seq_scan_launch(wm_seq *h, const seq_scan_args &a, bool backward,
 cudaError_t wm_seq_norm_launch(wm_seq *h, int dtype, long long rows, int D, const void *x, long long ldx,
                                const float *w, const float *b, float eps, void *y, long long ldy, float *mean,
                                float *rstd, cudaStream_t s);
-size_t wm_seq_norm_backward_ws(const wm_seq *h, long long rows, int D);
+size_t wm_seq_norm_backward_ws(const wm_seq *h, int dtype, long long rows, int D, const void *x, long long ldx, const void *dy,
+                               long long lddy, const void *dx, long long lddx);
 cudaError_t wm_seq_norm_backward_launch(wm_seq *h, int dtype, long long rows, int D, const void *x, long long ldx,
                                         const float *w, const float *mean, const float *rstd, const void *dy,
                                         long long lddy, void *dx, long long lddx, float *dw, float *db,

@@ -30,7 +30,7 @@ constexpr int kFwdMax = 16384, kBwdMax = 12288;
 // registers held by loads in flight).  bf16 rows that are not aligned to 4 bytes cannot be
 // copied so: their threads load a row when they come to it.
 template <int E, int ARRAYS, int THREADS>
-constexpr int ring_rows() {  // two rows and more on their way: 24 KB and more an SM in every variant, 192 KB at most
+constexpr int ring_rows() {  // two rows or more on their way, in 192 KB of a CTA at most
     const int rows = E == 8 ? 6 : E < 32 ? 4 : 3, room = (192 << 10) / (ARRAYS * THREADS * E * 4);
     return rows < room ? rows : room;
 }
@@ -178,7 +178,7 @@ constexpr int cta_threads() {
     return TPR < 128 ? 128 : TPR;
 }
 
-// CTAs of an SM at once: what the registers of the largest variants allow.
+// CTAs of an SM at once by their registers: what the launch bounds ask for.
 template <int TPR>
 constexpr int fwd_ctas() {
     return TPR == 32 ? 6 : TPR == 128 ? 4 : TPR == 256 ? 2 : 1;
@@ -186,6 +186,17 @@ constexpr int fwd_ctas() {
 template <int TPR>
 constexpr int bwd_ctas() {
     return TPR == 32 ? 4 : TPR == 128 ? 3 : 1;
+}
+
+// And by their shared memory too (an SM has 228 KB, and keeps 1 KB of it for every CTA): the grids' sizes.
+// Rows are split evenly over the CTAs, so those that do not run at once would run alone afterwards.
+template <class T, int VEC, int E, int TPR, bool BWD>
+constexpr int ctas_at_once() {
+    constexpr int THREADS = cta_threads<TPR>(), RPC = THREADS / TPR, by_registers = BWD ? bwd_ctas<TPR>() : fwd_ctas<TPR>();
+    constexpr size_t ring = Rows<T, VEC, E, TPR, BWD ? 2 : 1, THREADS>::bytes(), sums = BWD && RPC > 1 ? RPC * 8 * 32 * E : 0;
+    constexpr size_t weights = shared_weights<E, TPR>() ? (BWD ? 1 : 2) * 4096 : 0, fixed = weights + TPR / 32 * 16 + 1024;
+    constexpr size_t of_cta = ((ring > sums ? ring : sums) + fixed + 127) / 128 * 128, fit = (228 << 10) / of_cta;
+    return fit < by_registers ? (int)fit : by_registers;
 }
 
 template <class T, int VEC, int E, int TPR>
@@ -499,14 +510,6 @@ Shape shape(int D, int vec, bool bwd) {
     return {512, D <= 6144 && vec <= 4 ? 12 : D <= 8192 ? 16 : D <= 12288 ? 24 : 32};
 }
 
-int bwd_grid(const wm_seq *h, long long rows, int D) {
-    const int rpc = D <= 1024 ? 4 : 1, per_sm = D <= 1024 ? bwd_ctas<32>() : D <= 4096 ? bwd_ctas<128>() : bwd_ctas<512>();
-    const long long need = (rows + rpc - 1) / rpc, most = (long long)h->sms * per_sm;
-    // a few rows a warp: one CTA, which needs no second launch
-    if (need <= 4 && D <= 1024) return need > 0;
-    return (int)(need < most ? need : most);
-}
-
 // Launches with its dynamic shared memory (above 48 KB a kernel has to be told).
 template <class... P, class... A>
 cudaError_t launch(void (*k)(P...), int grid, int threads, size_t smem, cudaStream_t s, A... args) {
@@ -527,6 +530,30 @@ cudaError_t launch(void (*k)(P...), int grid, int threads, size_t smem, cudaStre
     if (sh.tpr == 128 && sh.e == 16) CALL(16, 128) \
     if (sh.tpr == 128) CALL(32, 128)
 
+// CTAs of an SM at once in the backward, for rows of D values in accesses of VEC.
+template <class T, int VEC>
+int bwd_per_sm(int D) {
+    const Shape sh = shape(D, VEC, true);
+#define CALL(E, TPR) return ctas_at_once<T, VEC, E, TPR, true>();
+    NORM_SHAPES(CALL)
+#undef CALL
+    return bwd_ctas<512>();
+}
+
+template <class T>
+int bwd_grid(const wm_seq *h, long long rows, int D, const void *x, long long ldx, const void *dy, long long lddy, const void *dx,
+             long long lddx) {
+    const int rpc = D <= 1024 ? 4 : 1;
+    const long long need = (rows + rpc - 1) / rpc;
+    // a few rows a warp: one CTA, which needs no second launch
+    if (need <= 4 && D <= 1024) return need > 0;
+    constexpr int VEC = 16 / sizeof(T);
+    const int v = width(VEC, sizeof(T), D, {{x, ldx}, {dy, lddy}, {dx, lddx}});
+    const int per_sm = v == VEC ? bwd_per_sm<T, VEC>(D) : v == 4 ? bwd_per_sm<T, 4>(D) : v == 2 ? bwd_per_sm<T, 2>(D) : bwd_per_sm<T, 1>(D);
+    const long long most = (long long)h->sms * per_sm;
+    return (int)(need < most ? need : most);
+}
+
 template <class T, int VEC>
 cudaError_t fwd(const wm_seq *h, long long rows, int D, const T *x, long long ldx, const float *w, const float *b, float eps,
                 T *y, long long ldy, float *mean, float *rstd, cudaStream_t s) {
@@ -534,7 +561,7 @@ cudaError_t fwd(const wm_seq *h, long long rows, int D, const T *x, long long ld
 #define CALL(E, TPR)                                                                                                     \
     {                                                                                                                    \
         constexpr int threads = cta_threads<TPR>(), rpc = threads / TPR;                                                 \
-        const long long need = (rows + rpc - 1) / rpc, most = (long long)h->sms * fwd_ctas<TPR>();                       \
+        const long long need = (rows + rpc - 1) / rpc, most = (long long)h->sms * ctas_at_once<T, VEC, E, TPR, false>(); \
         return launch(k_norm_fwd<T, VEC, E, TPR>, (int)(need < most ? need : most), threads,                             \
                       Rows<T, VEC, E, TPR, 1, threads>::bytes(), s, rows, D, x, ldx, w, b, eps, y, ldy, mean, rstd);     \
     }
@@ -604,8 +631,17 @@ cudaError_t wm_seq_norm_launch(wm_seq *h, int dtype, long long rows, int D, cons
     return fwd_any(h, rows, D, (const float *)x, ldx, w, b, eps, (float *)y, ldy, mean, rstd, s);
 }
 
-size_t wm_seq_norm_backward_ws(const wm_seq *h, long long rows, int D) {
-    return (size_t)bwd_grid(h, rows, D) * 2 * D * sizeof(float);
+namespace {
+int bwd_grid_of(const wm_seq *h, int dtype, long long rows, int D, const void *x, long long ldx, const void *dy, long long lddy,
+                const void *dx, long long lddx) {
+    return dtype == WM_BF16 ? bwd_grid<__nv_bfloat16>(h, rows, D, x, ldx, dy, lddy, dx, lddx)
+                            : bwd_grid<float>(h, rows, D, x, ldx, dy, lddy, dx, lddx);
+}
+}  // namespace
+
+size_t wm_seq_norm_backward_ws(const wm_seq *h, int dtype, long long rows, int D, const void *x, long long ldx, const void *dy,
+                               long long lddy, const void *dx, long long lddx) {
+    return (size_t)bwd_grid_of(h, dtype, rows, D, x, ldx, dy, lddy, dx, lddx) * 2 * D * sizeof(float);
 }
 
 cudaError_t wm_seq_norm_backward_launch(wm_seq *h, int dtype, long long rows, int D, const void *x, long long ldx,
@@ -613,7 +649,7 @@ cudaError_t wm_seq_norm_backward_launch(wm_seq *h, int dtype, long long rows, in
                                         long long lddy, void *dx, long long lddx, float *dw, float *db,
                                         cudaStream_t s) {
     using bf16 = __nv_bfloat16;
-    const int grid = bwd_grid(h, rows, D);
+    const int grid = bwd_grid_of(h, dtype, rows, D, x, ldx, dy, lddy, dx, lddx);
     float *part = dw || db ? (float *)h->ws : nullptr;
     h->last_launches = 0;
     if (grid > 0) {

@@ -85,6 +85,28 @@ def test_scan_workspace(seq, T, chunks):
         assert took <= N * lanes * 8 * chunks[k] * (1 + 1 / 16 + 1 / 256) * 1.125 + (4 << 20), took
 
 
+@pytest.mark.parametrize("D,rows_of_cta,at_once", [(500, 4, 3), (1000, 4, 2), (4096, 1, 2)])
+def test_norm_sums_of_ctas_that_run_at_once(seq, D, rows_of_cta, at_once):
+    """Partial column sums of as many CTAs as an SM's 228 KB hold (fp32: three to four rows of x and dy on their way in each),
+    and the gradients from them, with more rows than all CTAs take at a time."""
+    sms = torch.cuda.get_device_properties(0).multi_processor_count
+    rows = 4 * sms * rows_of_cta * 2 + 3
+    x, dy = (torch.randn(rows, D, generator=torch.Generator().manual_seed(i)).cuda() for i in (1, 2))
+    ops = seq.SequenceOps()
+    _, mean, rstd = ops.layer_norm(x, want_stats=True)
+    dx = torch.empty_like(x)
+    ops.layer_norm_backward(x, None, mean, rstd, dy, dx=dx)  # (the outputs' memory is in torch's hands from here on)
+    ops = seq.SequenceOps()
+    torch.cuda.synchronize()
+    free = torch.cuda.mem_get_info()[0]
+    got = ops.layer_norm_backward(x, None, mean, rstd, dy, dx=dx)
+    ops.sync()
+    assert free - torch.cuda.mem_get_info()[0] <= sms * at_once * 2 * D * 4 * 1.125 + (4 << 20)
+    want = ref.norm_backward(x, None, mean, rstd, dy)
+    for k, v in zip(("dx", "dw", "db"), got):
+        ref.check(v, *want[k], k)
+
+
 # ------------------------------------------------------------------ the ends of the range
 def test_norm_of_rows_past_2_30(ops):
     """One row whose weight and bias gradients together pass 2^31 columns.  Whole numbers whose sums over the row are 0
