@@ -456,11 +456,9 @@ __global__ void __launch_bounds__(kLong) k_norm_bwd_long(long long rows, int D, 
                                                          const float *__restrict__ rstd, const T *dy, long long lddy,
                                                          T *dx, long long lddx, float *part) {
     __shared__ float2 red[kLong / 32];
-    float *part_w = nullptr, *part_b = nullptr;
     if (part) {
-        part_w = part + (long long)blockIdx.x * 2 * D;
-        part_b = part_w + D;
-        for (int j = threadIdx.x; j < D; j += kLong) part_w[j] = part_b[j] = 0.f;
+        part += (long long)blockIdx.x * 2 * D;
+        for (int j = threadIdx.x; j < D; j += kLong) part[j] = part[D + (long long)j] = 0.f;
     }
     for (long long r = blockIdx.x; r < rows; r += gridDim.x) {
         const T *px = x + r * ldx, *pd = dy + r * lddy;
@@ -475,9 +473,9 @@ __global__ void __launch_bounds__(kLong) k_norm_bwd_long(long long rows, int D, 
         const float m1 = s.x / (float)D, m2 = s.y / (float)D;
         for (int j = threadIdx.x; j < D; j += kLong) {
             const float xh = (seq_to_float(px[j]) - mu) * rs, d = seq_to_float(pd[j]), g = d * (w ? w[j] : 1.f);
-            if (part) {  // column j is this thread's alone
-                part_w[j] = fmaf(d, xh, part_w[j]);
-                part_b[j] += d;
+            if (part) {  // j and D + j are this thread's alone (D + j in 64 bits)
+                part[j] = fmaf(d, xh, part[j]);
+                part[D + (long long)j] += d;
             }
             dx[r * lddx + j] = seq_from_float<T>(rs * (g - m1 - xh * m2));
         }
