@@ -201,7 +201,7 @@ constexpr int ctas_at_once() {
 
 template <class T, int VEC, int E, int TPR>
 __global__ void __launch_bounds__(cta_threads<TPR>(), fwd_ctas<TPR>())
-    k_norm_fwd(long long rows, int D, const T *__restrict__ x, long long ldx, const float *__restrict__ w,
+    k_norm_fwd(long long rows, int D, const T *x, long long ldx, const float *__restrict__ w,  // (y may be x)
                const float *__restrict__ b, float eps, T *y, long long ldy, float *__restrict__ mean, float *__restrict__ rstd) {
     constexpr int THREADS = cta_threads<TPR>(), RPC = THREADS / TPR;
     constexpr bool SHARED = shared_weights<E, TPR>();

@@ -107,6 +107,17 @@ def test_norm_sums_of_ctas_that_run_at_once(seq, D, rows_of_cta, at_once):
         ref.check(v, *want[k], k)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("D", [301, 1000, 1023, 4097, 9001, 16383, 20001])
+def test_norm_in_place_is_the_norm(ops, dtype, D):
+    """y over x gives the same bits, at every width of access, rows lying unaligned beside one another."""
+    x = torch.randn(700, D, generator=torch.Generator().manual_seed(D)).to(dtype).cuda()
+    w = torch.linspace(0.5, 1.5, D, device="cuda")
+    want, *stats = ops.layer_norm(x, w, w, want_stats=True)
+    y, *got = ops.layer_norm(x, w, w, out=x, want_stats=True)
+    assert y is x and torch.equal(x, want) and all(torch.equal(a, b) for a, b in zip(stats, got))
+
+
 # ------------------------------------------------------------------ the ends of the range
 def test_norm_of_rows_past_2_30(ops):
     """One row whose weight and bias gradients together pass 2^31 columns.  Whole numbers whose sums over the row are 0
