@@ -29,7 +29,8 @@
  *
  * Streams: calls are asynchronous on cuda_stream (a cudaStream_t; NULL = the legacy
  * default stream).  Calls on one handle share the workspace: issue them on one stream,
- * or order them between streams.  A handle is not thread-safe.
+ * or order them between streams.  Calls of several threads on one handle take turns; its
+ * message and launch count are those of the last.
  *
  * Errors: argument errors are returned at once and leave outputs untouched.  What only
  * the device can see (a token outside the table, a length outside [0, T]) is recorded in

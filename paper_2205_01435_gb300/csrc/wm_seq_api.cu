@@ -171,6 +171,7 @@ extern "C" void wm_seq_destroy(wm_seq *h) {
 
 extern "C" wm_status wm_seq_sync(wm_seq *h) {
     if (!h) return WM_ERR_INVALID_ARG;
+    const std::lock_guard<std::mutex> busy(h->busy);
     h->err[0] = 0;
     OnDevice on(h);
     int st[2] = {};
@@ -191,6 +192,7 @@ extern "C" int wm_seq_last_launches(const wm_seq *h) { return h ? h->last_launch
 
 extern "C" wm_status wm_seq_inject_wait_timeout(wm_seq *h, unsigned int polls) {
     if (!h) return WM_ERR_INVALID_ARG;
+    const std::lock_guard<std::mutex> busy(h->busy);
     h->err[0] = 0;
     h->test_wait = polls;
     return WM_OK;
@@ -198,6 +200,7 @@ extern "C" wm_status wm_seq_inject_wait_timeout(wm_seq *h, unsigned int polls) {
 
 #define SEQ_BEGIN(what)                                            \
     if (!h) return WM_ERR_INVALID_ARG;                             \
+    const std::lock_guard<std::mutex> busy(h->busy);               \
     h->err[0] = 0;                                                 \
     static const char *const kWhat = what;                         \
     OnDevice on(h);                                                \

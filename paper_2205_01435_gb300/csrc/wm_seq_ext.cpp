@@ -122,7 +122,14 @@ struct Call {
         if (v < 0) throw Failed{};
         return v;
     }
-    void done(wm_status st) const {
+    // The C call, without the interpreter's lock: it may wait for the device (a workspace that grows), and what it
+    // waits for may need another Python thread.  The arrays it takes are the caller's, who holds them meanwhile.
+    template <class F>
+    void run(F call) const {
+        wm_status st;
+        Py_BEGIN_ALLOW_THREADS;
+        st = call();
+        Py_END_ALLOW_THREADS;
         if (st == WM_OK) return;
         PyObject *args = Py_BuildValue("(is)", (int)st, wm_seq_last_error(h));
         if (args) {
@@ -170,8 +177,10 @@ PyObject *embed(const Call &c) {
     const void *tp = flat(&table, type, table.sizes(), "table");
     const int32_t *kp = flat<int32_t>(&tokens, at::kInt, tokens.sizes(), "tokens");
     if (!out) out = &(made = c.fresh(full, type));
-    c.done(wm_seq_embed(c.h, dt, tokens.numel(), size(table.size(0)), size(table.size(1)), tp, kp, scale, flat(out, type, full, "out"),
-                        c.stream()));
+    void *op = flat(out, type, full, "out"), *s = c.stream();
+    const long long n = tokens.numel();
+    const int V = size(table.size(0)), D = size(table.size(1));
+    c.run([&] { return wm_seq_embed(c.h, dt, n, V, D, tp, kp, scale, op, s); });
     return give(c.a[3], made);
 }
 
@@ -191,7 +200,10 @@ PyObject *embed_backward(const Call &c) {
     at::Tensor made;
     const at::Tensor *out = maybe(c.a[4], "out");
     if (!out) out = &(made = c.fresh(shape, type));
-    c.done(wm_seq_embed_backward(c.h, dt, tokens.numel(), (int)V, size(shape[1]), kp, dp, scale, flat(out, type, shape, "out"), c.stream()));
+    void *op = flat(out, type, shape, "out"), *s = c.stream();
+    const long long n = tokens.numel();
+    const int D = size(shape[1]);
+    c.run([&] { return wm_seq_embed_backward(c.h, dt, n, (int)V, D, kp, dp, scale, op, s); });
     return give(c.a[4], made);
 }
 
@@ -217,8 +229,12 @@ PyObject *layer_norm(const Call &c) {
         mean = c.fresh(lead, at::kFloat);
         rstd = c.fresh(lead, at::kFloat);
     }
-    c.done(wm_seq_layer_norm(c.h, dt, D ? x.numel() / D : 0, size(D), x.data_ptr(), ldx, wp, bp, eps, out->data_ptr(), ldy,
-                             stats ? (float *)mean.data_ptr() : nullptr, stats ? (float *)rstd.data_ptr() : nullptr, c.stream()));
+    const long long rows = D ? x.numel() / D : 0;
+    const int d = size(D);
+    const void *xp = x.data_ptr();
+    void *op = out->data_ptr(), *s = c.stream();
+    float *mp = stats ? (float *)mean.data_ptr() : nullptr, *rp = stats ? (float *)rstd.data_ptr() : nullptr;
+    c.run([&] { return wm_seq_layer_norm(c.h, dt, rows, d, xp, ldx, wp, bp, eps, op, ldy, mp, rp, s); });
     if (!stats) return give(c.a[5], made);
     return tuple({give(c.a[5], made), give(mean), give(rstd)});
 }
@@ -249,9 +265,12 @@ PyObject *layer_norm_backward(const Call &c) {
         dw = c.fresh(par, at::kFloat);
         db = c.fresh(par, at::kFloat);
     }
-    c.done(wm_seq_layer_norm_backward(c.h, dt, D ? x.numel() / D : 0, size(D), x.data_ptr(), ldx, wp, mp, rp, dy.data_ptr(), lddy,
-                                      dx->data_ptr(), lddx, params ? (float *)dw.data_ptr() : nullptr,
-                                      params ? (float *)db.data_ptr() : nullptr, c.stream()));
+    const long long rows = D ? x.numel() / D : 0;
+    const int d = size(D);
+    const void *xp = x.data_ptr(), *yp = dy.data_ptr();
+    void *op = dx->data_ptr(), *s = c.stream();
+    float *wo = params ? (float *)dw.data_ptr() : nullptr, *bo = params ? (float *)db.data_ptr() : nullptr;
+    c.run([&] { return wm_seq_layer_norm_backward(c.h, dt, rows, d, xp, ldx, wp, mp, rp, yp, lddy, op, lddx, wo, bo, s); });
     return tuple({give(c.a[5], made), params ? give(dw) : none(), params ? give(db) : none()});
 }
 
@@ -273,7 +292,10 @@ PyObject *scan(const Call &c) {
     if (!out) out = &(made = c.fresh(shape, type));
     const wm_seq_view vo = view(*out, type, shape, "out");
     if (!last && c.yes(6)) last = &(made_last = c.fresh(nh, at::kFloat));
-    c.done(wm_seq_gated_scan(c.h, dt, T, size(N), size(H), &vg, &vx, p0, pr, pl, &vo, flat<float>(last, at::kFloat, nh, "h_last"), c.stream()));
+    const int n = size(N), hh = size(H);
+    float *pe = flat<float>(last, at::kFloat, nh, "h_last");
+    void *s = c.stream();
+    c.run([&] { return wm_seq_gated_scan(c.h, dt, T, n, hh, &vg, &vx, p0, pr, pl, &vo, pe, s); });
     return tuple({give(c.a[5], made), last ? give(c.a[7], made_last) : none()});
 }
 
@@ -297,8 +319,11 @@ PyObject *scan_backward(const Call &c) {
     const wm_seq_view v0 = view(*dgate, type, shape, "dgate"), v1 = view(*dx, type, shape, "dx");
     const bool want = c.yes(10);
     if (want) m2 = c.fresh(nh, at::kFloat);
-    c.done(wm_seq_gated_scan_backward(c.h, dt, shape[0], size(N), size(H), &vg, &vx, p0, pr, pl, &vh, &vd, pd, &v0, &v1,
-                                      want ? (float *)m2.data_ptr() : nullptr, c.stream()));
+    const int n = size(N), hh = size(H);
+    float *pe = want ? (float *)m2.data_ptr() : nullptr;
+    void *s = c.stream();
+    const long long T = shape[0];
+    c.run([&] { return wm_seq_gated_scan_backward(c.h, dt, T, n, hh, &vg, &vx, p0, pr, pl, &vh, &vd, pd, &v0, &v1, pe, s); });
     return tuple({give(c.a[8], m0), give(c.a[9], m1), want ? give(m2) : none()});
 }
 
@@ -307,23 +332,27 @@ PyObject *clip(const Call &c) {
         PyObject *o;
         ~Ref() { Py_XDECREF(o); }
     };
-    const Ref grads{PySequence_Fast(c.a[0], "grads: a sequence of tensors is needed")};
+    // (tuples of their own: no other thread can take a tensor out of them while the lock is given up)
+    const Ref grads{PySequence_Tuple(c.a[0])};
     if (!grads.o) throw Failed{};
-    const Ref outs{c.a[2] == Py_None ? nullptr : PySequence_Fast(c.a[2], "out: a sequence of tensors is needed")};
+    const Ref outs{c.a[2] == Py_None ? nullptr : PySequence_Tuple(c.a[2])};
     if (PyErr_Occurred()) throw Failed{};
-    const Py_ssize_t n = PySequence_Fast_GET_SIZE(grads.o);
-    if (outs.o && PySequence_Fast_GET_SIZE(outs.o) != n) throw Refuse{"out needs a tensor for each gradient"};
+    const Py_ssize_t n = PyTuple_GET_SIZE(grads.o);
+    if (outs.o && PyTuple_GET_SIZE(outs.o) != n) throw Refuse{"out needs a tensor for each gradient"};
     std::vector<wm_seq_grad> table((size_t)n);
     for (Py_ssize_t i = 0; i < n; ++i) {
-        const at::Tensor &g = tensor(PySequence_Fast_GET_ITEM(grads.o, i), "grads");
-        const at::Tensor &o = outs.o ? tensor(PySequence_Fast_GET_ITEM(outs.o, i), "out") : g;
+        const at::Tensor &g = tensor(PyTuple_GET_ITEM(grads.o, i), "grads");
+        const at::Tensor &o = outs.o ? tensor(PyTuple_GET_ITEM(outs.o, i), "out") : g;
         if (!g.is_contiguous() || o.scalar_type() != g.scalar_type() || o.sizes() != g.sizes() || !o.is_contiguous())
             throw Refuse{"contiguous gradients, and out of the same shapes and types, are needed"};
         table[(size_t)i] = {g.data_ptr(), o.data_ptr(), g.numel(), dtype_of(g)};
     }
     const float max_norm = (float)c.number(1);
     at::Tensor norm = c.fresh({}, at::kFloat);
-    c.done(wm_seq_clip(c.h, size(n), table.data(), max_norm, (float *)norm.data_ptr(), c.stream()));
+    const int count = size(n);
+    float *np = (float *)norm.data_ptr();
+    void *s = c.stream();
+    c.run([&] { return wm_seq_clip(c.h, count, table.data(), max_norm, np, s); });
     return give(norm);
 }
 

@@ -6,9 +6,12 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <mutex>
+
 #include "wm_seq.h"
 
 struct wm_seq {
+    std::mutex busy;  // held by a call: the binding gives up the interpreter's lock, which kept threads apart
     int device = 0;
     int sms = 0;
     int sort_ranks = 0;  // CTAs of the embedding gradient's sorting cluster, at most

@@ -1,6 +1,8 @@
 """The sequence operators' handles, streams and ends of range: what a call leaves behind, what runs beside it, and the
 largest and smallest values and sizes."""
 import ctypes as C
+import threading
+import time
 
 import pytest
 import torch
@@ -116,6 +118,56 @@ def test_norm_in_place_is_the_norm(ops, dtype, D):
     want, *stats = ops.layer_norm(x, w, w, want_stats=True)
     y, *got = ops.layer_norm(x, w, w, out=x, want_stats=True)
     assert y is x and torch.equal(x, want) and all(torch.equal(a, b) for a, b in zip(stats, got))
+
+
+def test_other_threads_run_while_a_call_waits(seq):
+    """A call that waits for the device (its workspace grows) does not keep the interpreter's lock meanwhile."""
+    ops = seq.SequenceOps()
+    t = (torch.arange(3000, device="cuda") % 50).to(torch.int32)
+    dout, table = torch.ones(3000, 32, device="cuda"), torch.empty(50, 32, device="cuda")
+    torch.cuda.synchronize()
+    stop, ticks = threading.Event(), []
+
+    def other():
+        while not stop.wait(0.001):
+            ticks.append(time.perf_counter())
+
+    thread = threading.Thread(target=other)
+    thread.start()
+    try:
+        torch.cuda._sleep(600_000_000)  # about 0.3 s
+        start = time.perf_counter()
+        ops.embed_backward(t, dout, 50, out=table)
+        end = time.perf_counter()
+    finally:
+        stop.set()
+        thread.join()
+    assert end - start > 0.1  # (it did wait)
+    assert sum(start < v < end for v in ticks) > 20
+    assert torch.equal(table, torch.full_like(table, 60.0))
+
+
+def test_threads_take_turns_on_a_handle(seq):
+    """Several threads' calls on one handle and stream, with workspaces that grow between them."""
+    ops = seq.SequenceOps()
+    wrong = []
+
+    def work(k):
+        for i in range(12):
+            n, V = 300 + 700 * i * (k + 1), 17 + k
+            t = (torch.arange(n, device="cuda") % V).to(torch.int32)
+            g = ops.embed_backward(t, torch.full((n, 24), float(k + 1), device="cuda"), V)
+            want = torch.bincount(t, minlength=V)[:, None].float() * (k + 1)
+            if not torch.equal(g, want.expand(V, 24)):
+                wrong.append((k, i))
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    ops.sync()
+    assert not wrong
 
 
 # ------------------------------------------------------------------ the ends of the range
