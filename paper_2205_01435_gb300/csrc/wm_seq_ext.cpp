@@ -103,6 +103,7 @@ struct Call {
     PyObject *const *a;
     Call(PyObject *const *args, Py_ssize_t n, Py_ssize_t want) : a(args + 2) {
         if (n != want + 2) throw Refuse{"wrong number of arguments"};
+        if (args[0] == Py_None) throw Refuse{"the handle is closed"};
         h = static_cast<wm_seq *>(PyLong_AsVoidPtr(args[0]));
         index = (int)PyLong_AsLong(args[1]);
         if (PyErr_Occurred()) throw Failed{};

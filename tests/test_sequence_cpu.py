@@ -55,3 +55,16 @@ def test_the_references_agree_with_autograd():
     b = ref.norm_backward(x.detach(), w.detach(), f["mean"][0].detach(), f["rstd"][0].detach(), dy)
     for k, v in (("dx", x), ("dw", w), ("db", bias)):
         assert torch.allclose(b[k][0], v.grad, atol=1e-12), k
+
+
+def test_a_closed_handle_is_refused(seq):
+    """What a method of a closed SequenceOps comes to."""
+    import torch
+
+    x = torch.zeros(2, 3)
+    ops = seq.SequenceOps.__new__(seq.SequenceOps)
+    ops.h, ops._index = None, 0
+    for call in (lambda: ops.layer_norm(x), lambda: ops.gated_step(x, x, None), lambda: ops.clip_grads([x], 1.0),
+                 lambda: ops.embed(x, x)):
+        with pytest.raises(ValueError, match="closed"):
+            call()
