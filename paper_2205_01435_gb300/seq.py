@@ -161,8 +161,8 @@ class SequenceOps:
     def clip_grads(self, grads, max_norm: float, out=None, stream=None):
         """wm_seq_clip: the global norm [] of the gradients, which are scaled to it in place (or into `out`,
         tensors of the same sizes and types).  max_norm = inf only measures."""
-        if stream is not None:
-            return self._elsewhere(stream, self.clip_grads, grads, max_norm, out)
+        if stream is not None:  # (lists: what a view or a generator gives is to be kept until the call is done)
+            return self._elsewhere(stream, self.clip_grads, list(grads), max_norm, None if out is None else list(out))
         return _ext.clip_grads(self.h, self._index, grads, max_norm, out)
 
     # ------------------------------------------------------------- status

@@ -147,6 +147,24 @@ def test_other_threads_run_while_a_call_waits(seq):
     assert torch.equal(table, torch.full_like(table, 60.0))
 
 
+@pytest.mark.parametrize("kind", [list, tuple, dict.values, iter])
+def test_clip_on_another_stream_keeps_its_gradients(ops, kind):
+    """Gradients that the caller lets go of after a call on another stream are not used again before it is done, whatever
+    held them."""
+    n, side = 4_000_000, torch.cuda.Stream()
+    grads, out = {"a": torch.ones(n, device="cuda")}, [torch.empty(n, device="cuda")]
+    given = kind(grads) if kind is dict.values else kind(grads.values())
+    ops.clip_grads([out[0].fill_(1.0)], 1e9, out=out)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+    norm = ops.clip_grads(given, 1e9, out=out, stream=side)
+    del grads, given
+    other = torch.full((n,), 7.0, device="cuda")  # (the memory is free for it)
+    torch.cuda.synchronize()
+    assert float(norm) == 2000.0 and bool((out[0] == 1.0).all()) and bool((other == 7.0).all())
+
+
 def test_threads_take_turns_on_a_handle(seq):
     """Several threads' calls on one handle and stream, with workspaces that grow between them."""
     ops = seq.SequenceOps()
