@@ -94,6 +94,8 @@ class SequenceOps:
         """The call on another stream: its outputs are allocated there, and its inputs' memory is
         not used again before it is done."""
         s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream), device=self.device)
+        if s.device != self.device:  # (it would be current on its own device, and the call go to this one's current stream)
+            raise ValueError(f"a stream of {self.device} is needed, got one of {s.device}")
         with torch.cuda.stream(s):
             out = method(*args)
 

@@ -165,6 +165,13 @@ def test_clip_on_another_stream_keeps_its_gradients(ops, kind):
     assert float(norm) == 2000.0 and bool((out[0] == 1.0).all()) and bool((other == 7.0).all())
 
 
+def test_a_stream_of_another_device_is_refused(seq):
+    ops, x = seq.SequenceOps(), torch.ones(2, 8, device="cuda")
+    ops.device = torch.device("cuda", 1)  # as if the handle were there
+    with pytest.raises(ValueError, match="stream"):
+        ops.layer_norm(x, stream=torch.cuda.Stream(0))
+
+
 def test_threads_take_turns_on_a_handle(seq):
     """Several threads' calls on one handle and stream, with workspaces that grow between them."""
     ops = seq.SequenceOps()
