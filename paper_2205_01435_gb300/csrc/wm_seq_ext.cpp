@@ -303,7 +303,7 @@ PyObject *scan(const Call &c) {
 PyObject *scan_backward(const Call &c) {
     const at::Tensor &gate = tensor(c.a[0], "gate"), &x = tensor(c.a[1], "x"), &h = tensor(c.a[2], "h"), &dh = tensor(c.a[3], "dh"),
                      *dh_last = maybe(c.a[4], "dh_last"), *h0 = maybe(c.a[5], "h0"), *reset = maybe(c.a[6], "reset"),
-                     *lengths = maybe(c.a[7], "lengths"), *dgate = maybe(c.a[8], "dgate"), *dx = maybe(c.a[9], "dx");
+                     *lengths = maybe(c.a[7], "lengths"), *dgate = maybe(c.a[8], "dgate"), *dx = maybe(c.a[9], "dx"), *dh0 = maybe(c.a[11], "dh0");
     const auto type = gate.scalar_type();
     const int dt = dtype_of(gate);
     if (gate.dim() != 3) throw Refuse{"gate [T, N, H] is needed"};
@@ -318,14 +318,13 @@ PyObject *scan_backward(const Call &c) {
     if (!dgate) dgate = &(m0 = c.fresh(shape, type));
     if (!dx) dx = &(m1 = c.fresh(shape, type));
     const wm_seq_view v0 = view(*dgate, type, shape, "dgate"), v1 = view(*dx, type, shape, "dx");
-    const bool want = c.yes(10);
-    if (want) m2 = c.fresh(nh, at::kFloat);
+    if (!dh0 && c.yes(10)) dh0 = &(m2 = c.fresh(nh, at::kFloat));
     const int n = size(N), hh = size(H);
-    float *pe = want ? (float *)m2.data_ptr() : nullptr;
+    float *pe = flat<float>(dh0, at::kFloat, nh, "dh0");
     void *s = c.stream();
     const long long T = shape[0];
     c.run([&] { return wm_seq_gated_scan_backward(c.h, dt, T, n, hh, &vg, &vx, p0, pr, pl, &vh, &vd, pd, &v0, &v1, pe, s); });
-    return tuple({give(c.a[8], m0), give(c.a[9], m1), want ? give(m2) : none()});
+    return tuple({give(c.a[8], m0), give(c.a[9], m1), dh0 ? give(c.a[11], m2) : none()});
 }
 
 PyObject *clip(const Call &c) {
@@ -384,7 +383,7 @@ PyMethodDef g_methods[] = {
     SEQ_ENTRY("layer_norm_backward", layer_norm_backward, 7),
     SEQ_ENTRY("gated_scan", scan<false>, 8),
     SEQ_ENTRY("gated_step", scan<true>, 8),
-    SEQ_ENTRY("gated_scan_backward", scan_backward, 11),
+    SEQ_ENTRY("gated_scan_backward", scan_backward, 12),
     SEQ_ENTRY("clip_grads", clip, 3),
     {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},

@@ -152,12 +152,13 @@ class SequenceOps:
         return _ext.gated_step(self.h, self._index, gate, x, state, reset, None, out, True, out_state)
 
     def gated_scan_backward(self, gate, x, h, dh, dh_last=None, h0=None, reset=None, lengths=None, dgate=None, dx=None,
-                            want_dh0: bool = True, stream=None):
-        """wm_seq_gated_scan_backward: (dgate, dx, dh0); dgate and dx may be given, strided as in gated_scan."""
+                            want_dh0: bool = True, stream=None, dh0=None):
+        """wm_seq_gated_scan_backward: (dgate, dx, dh0); dgate and dx may be given, strided as in gated_scan, and dh0,
+        which may be dh_last."""
         if stream is not None:
             return self._elsewhere(stream, self.gated_scan_backward, gate, x, h, dh, dh_last, h0, reset, lengths, dgate, dx,
-                                   want_dh0)
-        return _ext.gated_scan_backward(self.h, self._index, gate, x, h, dh, dh_last, h0, reset, lengths, dgate, dx, want_dh0)
+                                   want_dh0, None, dh0)
+        return _ext.gated_scan_backward(self.h, self._index, gate, x, h, dh, dh_last, h0, reset, lengths, dgate, dx, want_dh0, dh0)
 
     # ------------------------------------------------------------- clipping
     def clip_grads(self, grads, max_norm: float, out=None, stream=None):

@@ -195,6 +195,24 @@ def test_threads_take_turns_on_a_handle(seq):
     assert not wrong
 
 
+@pytest.mark.parametrize("T,N,H", [(3, 2, 8), (40, 100, 512), (100, 2, 40), (20000, 1, 96), (5000, 4, 33)])
+def test_scan_backward_state_in_place(ops, T, N, H):
+    """dh0 may be dh_last, whichever kernel runs and however many CTAs read what enters the last step; on another stream too."""
+    from test_gpu_sequence import scan_inputs
+    s = scan_inputs(T, N, H, torch.bfloat16, seed=6)
+    h, _ = ops.gated_scan(s["gate"], s["x"], h0=s["h0"])
+    want = ops.gated_scan_backward(s["gate"], s["x"], h, s["dh"], dh_last=s["dh_last"], h0=s["h0"])
+    side = torch.cuda.Stream()
+    for stream in (None, None, side):
+        state = s["dh_last"].clone()
+        side.wait_stream(torch.cuda.current_stream())
+        got = ops.gated_scan_backward(s["gate"], s["x"], h, s["dh"], dh_last=state, h0=s["h0"], dh0=state, stream=stream)
+        torch.cuda.current_stream().wait_stream(side)
+        assert got[2] is state and all(torch.equal(a, b) for a, b in zip(want, got))
+    with pytest.raises(ValueError):
+        ops.gated_scan_backward(s["gate"], s["x"], h, s["dh"], dh0=s["h0"][:, :1])
+
+
 # ------------------------------------------------------------------ the ends of the range
 def test_norm_of_rows_past_2_30(ops):
     """One row whose weight and bias gradients together pass 2^31 columns.  Whole numbers whose sums over the row are 0
