@@ -16,6 +16,6 @@ def load():
 
 
 def load_seq():
-    """Imports the sequence operators' binding; raises ImportError if libwm.so has not been built."""
+    """Imports the sequence operators' binding; raises ImportError if libwm.so or _seq_ext.so has not been built."""
     from . import seq
     return seq
