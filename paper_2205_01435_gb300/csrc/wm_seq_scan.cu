@@ -51,14 +51,15 @@ struct ScanParams {
 
 // keep and write without cancellation in either.
 //   fp32: from exp(-|p|), which neither overflows nor cancels; the selects make saturated gates exact.
-//   bf16: from exp(-p), p held at -80 where write rounds to 1 (NaN stays): six instructions of the
-//   forward's 20 a value.  The hardware's exponential and reciprocal (2^-21, 2^-23) are far
-//   below the inputs' precision; results below fp32's normal range are 0.
+//   bf16: from exp(-p), p held at -87 (NaN stays): six instructions of the forward's 20 a value.
+//   There keep is 1.6e-38, the least that the reciprocal gives (results below fp32's normal range
+//   are 0), and write rounds to 1.  The hardware's exponential and reciprocal (2^-21, 2^-23) are
+//   far below the inputs' precision.
 template <class T>
 __device__ __forceinline__ void gates(float p, float &keep, float &write) {
     if constexpr (sizeof(T) == 2) {
         float e;
-        asm("max.NaN.f32 %0, %1, %2;" : "=f"(p) : "f"(p), "f"(-80.f));
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(p) : "f"(p), "f"(-87.f));
         asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(p * -1.4426950408889634f));
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(keep) : "f"(1.f + e));
         write = e * keep;

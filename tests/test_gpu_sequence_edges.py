@@ -286,3 +286,32 @@ def test_clip_by_more_than_fp32_holds(ops, n, bound):
     ref.check(ops.clip_grads(g, bound, out=out), norm, ne, "norm")
     for o, (v, e) in zip(out, want):
         ref.check(o, v, e, "out")
+
+
+@pytest.mark.parametrize("T,N,H", [(1, 2, 16), (200, 1, 16), (20, 100, 512)])
+@pytest.mark.parametrize("gate", [-79.0, -82.0, -84.0, -86.5])
+def test_scan_bf16_gates_near_the_range_of_fp32(ops, T, N, H, gate):
+    """Gates that keep 1e-35 of a state, and less: large states and gradients show it, forward and backward."""
+    g = torch.full((T, N, H), gate).bfloat16().cuda()
+    x = torch.zeros(T, N, H, dtype=torch.bfloat16, device="cuda")
+    h0 = torch.linspace(1e34, 3e36, N * H).view(N, H).cuda()
+    dh = torch.full((T, N, H), 1e25, dtype=torch.bfloat16, device="cuda")
+    h, last = ops.gated_scan(g, x, h0=h0)
+    f = ref.scan(g, x, h0)
+    ref.check(h, *f["h"], "h")
+    ref.check(last, *f["h_last"], "h_last")
+    got = ops.gated_scan_backward(g, x + 1, h, dh)
+    want = ref.scan_backward(g, x + 1, h, dh)
+    for k, v in zip(("dgate", "dx", "dh0"), got):
+        ref.check(v, *want[k], k)
+
+
+@pytest.mark.parametrize("T,N,H", [(3, 2, 16), (200, 1, 16), (20, 100, 512)])
+@pytest.mark.parametrize("gate", [-100.0, torch.finfo(torch.bfloat16).min, float("-inf")])
+def test_scan_bf16_gates_that_keep_nothing(ops, T, N, H, gate):
+    """A gate below that range takes the value and drops a large state."""
+    g = torch.full((T, N, H), gate, dtype=torch.bfloat16, device="cuda")
+    x = torch.linspace(1, 2, T * N * H).view(T, N, H).bfloat16().cuda()
+    h, last = ops.gated_scan(g, x, h0=torch.full((N, H), 1e30, device="cuda"))
+    assert torch.equal(h, x)
+    ref.check(last, x[-1].cpu().double(), torch.full((N, H), 2e-8, dtype=torch.float64), "h_last")
