@@ -88,8 +88,8 @@ wm_status wm_seq_embed(wm_seq *h, int dtype, long long n, int V, int D, const vo
 
 /* Its gradient: dtable[v, :] = scale * sum over i with tokens[i] = v of dout[i, :].
  *   tokens [n] int32;  dout [n, D] dtype, dense;  dtable [V, D] dtype, dense, overwritten
- * The tokens are sorted (stably, so the sums run in a fixed order) and every row is
- * written once; rows that no token took are 0.  Tokens outside [0, V) as above. */
+ * The tokens are sorted stably, so that the sums run in a fixed order; rows that no token took
+ * are 0, whatever the scale.  Tokens outside [0, V) as above. */
 wm_status wm_seq_embed_backward(wm_seq *h, int dtype, long long n, int V, int D, const int32_t *tokens, const void *dout,
                                 float scale, void *dtable, void *cuda_stream);
 
@@ -173,9 +173,11 @@ typedef struct {
  *   is not src);  norm [1] fp32 device, out
  * Gradients that are within the bound are not changed (dst != src: copied).  A norm that
  * is inf or NaN leaves them unchanged too: the caller reads `norm` and skips the update.
- * Squares are summed in fp64 across vectors of values, and values whose squares leave
- * fp32's range are squared in fp64: the norm of finite gradients is finite unless it
- * passes fp32's range itself.  Empty gradients are allowed; count = 0 gives norm 0.
+ * Squares are summed in fp32 within 16 bytes of values, in a pair of fp32 (a sum and its
+ * error) over a thread's and a warp's, in fp64 over all; values whose squares leave fp32's
+ * range are squared in fp64: the norm of finite gradients is finite unless it passes fp32's
+ * range itself.  A factor below fp32's normal range is applied as two.  Empty gradients are
+ * allowed; count = 0 gives norm 0.
  * count <= 65536. */
 wm_status wm_seq_clip(wm_seq *h, int count, const wm_seq_grad *grads, float max_norm, float *norm, void *cuda_stream);
 

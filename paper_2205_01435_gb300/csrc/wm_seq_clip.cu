@@ -10,8 +10,8 @@
 // through the runs backwards: what the first read last is still in L2.  Gradients of up to 30 MB
 // take one launch, which holds them in shared memory between the norm and the clipping.
 //
-// Measured (one GB300): 542 MB in 60 tensors 95 us for the norm (5.7 TB/s) and 160 us for the
-// clipping (6.8 TB/s); 8.8 MB in 4 tensors 10 us.
+// Measured (one GB300): 542 MB in 60 tensors 94 us for the norm (5.8 TB/s) and 161 us for the
+// clipping (6.7 TB/s); 8.8 MB in 4 tensors 10 us a call.
 //
 // Squares are summed in fp32 within a 16-byte vector (4 or 8 values) and from there on
 // without rounding error that matters: a thread adds the vectors' sums into an fp32 pair

@@ -3,8 +3,8 @@
 // A small CPython module: it checks types, shapes and strides, allocates outputs, takes the
 // current stream and calls the C entry.  A call of a few kernels costs about as much on the
 // host as on the device, and the same marshalling through ctypes took 15 us for one step of
-// a scan, most of it in Python; here it takes about 6.  That an array is memory of the
-// handle's device, and aligned, the C entries check.
+// a scan, most of it in Python; here it takes 3 with its outputs given.  That an array is memory
+// of the handle's device, and aligned, the C entries check.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 

@@ -10,9 +10,9 @@
 // backward each thread sums its columns' dw and db over the CTA's rows in fp32; the CTAs'
 // partial sums are added in a fixed order by a second, small launch.
 //
-// Measured (one GB300): 65,536 x 1024 bf16 46 us forward (5.8 TB/s), 80 us backward (5.0 TB/s: the
-// column sums leave 16 warps an SM, which issue half of the cycles) and 6 us for the column sums;
-// 20,000 x 301 fp32 12, 16 and 5 us.
+// Measured (one GB300, durations of the kernels alone): 65,536 x 1024 bf16 48 us forward (5.6 TB/s),
+// 81 us backward (5.0 TB/s: the column sums leave 16 warps an SM, which issue half of the cycles) and 7 us
+// for the column sums; 20,000 x 301 fp32 13, 18 and 7 us; 12,000 x 4096 fp32 69 (5.7 TB/s), 96 (6.1) and 7 us.
 #include <algorithm>
 #include <initializer_list>
 #include <utility>
@@ -494,8 +494,8 @@ int width(int vec, size_t es, int D, std::initializer_list<std::pair<const void 
 }
 
 // Threads per row and values per thread: the fewest of each that hold the row (a warp up to 1024
-// values, so that its sums need no barrier: 65536 x 1024 bf16 backward took 80 us so, and 90 us with
-// 128 threads a row).  From 4097 values the backward takes 512 threads where the forward takes 256: its column sums
+// values, so that its sums need no barrier: the kernel of 65536 x 1024 bf16 backward took 80 us so, and 90 us
+// with 128 threads a row).  From 4097 values the backward takes 512 threads where the forward takes 256: its column sums
 // would leave 256 threads an SM (8000 x 6001: fp32 144 us against 178, bf16 124 against 157; forward 84 against 80,
 // 106 against 92).
 struct Shape {

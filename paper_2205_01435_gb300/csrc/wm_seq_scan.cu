@@ -22,9 +22,10 @@
 //                  the (P, S) that the CTAs before it publish.  The spans' inputs stay in shared
 //                  memory between the two passes.
 //
-// Measured (bf16, one GB300): 128 steps x 512 x 1024 channels 59 us forward and 120 us backward, 6.8
-// TB/s, the rate of a copy; 65,536 steps x 256 channels 36 and 60 us (2.8 and 3.3 TB/s, bound by
-// instruction issue: 45 and 85 a value); one step of 16 x 256 channels 3 us.
+// Measured (bf16, one GB300, durations of the kernels alone): 128 steps x 512 x 1024 channels 61 us
+// forward and 120 us backward, 6.6 and 6.7 TB/s, nearly the rate of a copy (calls one after another: 66 and
+// 126); 65,536 steps x 256 channels 37 and 61 us (2.7 and 3.3 TB/s, bound by instruction issue: 45 and 85
+// a value); one step of 16 x 256 channels 4 us.
 #include <type_traits>
 
 #include "wm_seq_internal.h"
@@ -648,7 +649,7 @@ cudaError_t stream_launch(const ScanParams<T> &q, size_t step, cudaStream_t s) {
 }
 
 // A ring of 24 steps where all CTAs run at once with it, else of 12.  (512 x 1024 channels, bf16,
-// backward: 125 us with 12 steps and two CTAs an SM, 129 us with 6 steps and all at once.)
+// calls of the backward: 125 us with 12 steps and two CTAs an SM, 129 us with 6 steps and all at once.)
 template <class T, int VEC, bool BWD>
 cudaError_t stream(const wm_seq *h, const seq_scan_args &a, cudaStream_t s) {
     const ScanParams<T> q = params<T>(h, a, VEC, BWD);
@@ -674,8 +675,8 @@ Plan plan(const wm_seq *h, const seq_scan_args &a, bool bwd) {
     Plan p{};
     const int w4 = a.dtype == WM_BF16 ? 2 : 1;  // values in 4 bytes
     const long long C = (long long)a.N * a.H;
-    // 16-byte accesses where they leave an SM's 8 warps and more (512 x 1024, bf16: 66 and 125 us against 76
-    // and 145 with 8 bytes; 200 x 512: 78 and 151 against 70 and 128)
+    // 16-byte accesses where they leave an SM's 8 warps and more (calls of 512 x 1024 channels, bf16, no lengths: 66
+    // and 125 us against 76 and 145 with 8 bytes; 200 x 512: 78 and 151 against 70 and 128)
     p.vec = width(a, bwd, C >= h->sms * 1200ll && a.T > kWalk ? 4 * w4 : 2 * w4);
     if (a.T <= kWalk) {
         p.kind = Plan::WALK;

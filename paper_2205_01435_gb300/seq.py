@@ -5,6 +5,12 @@ in the compiled module ``_seq_ext``).
 their outputs unless given, and run on the current stream (or ``stream=``) without
 synchronising.  There is no CPU fallback.
 
+All calls of one object share its workspace: calls on several streams have to be ordered among
+them (``wait_stream``, events), or go through an object for each stream.  ``stream=`` makes that
+stream wait for nothing: what the inputs' own stream still has to do comes first by the caller's
+order.  Nothing is recorded for autograd: a tensor that requires a gradient is taken for its values,
+and the ``_backward`` methods are called by hand.
+
     ops = SequenceOps()
     e = ops.embed(table, actions, scale=32.0)
     y, mean, rstd = ops.layer_norm(e, weight, bias, want_stats=True)
