@@ -6,6 +6,8 @@
  *   wm_seq_embed, _backward        rows of a table by token, scaled; the table's gradient
  *   wm_seq_layer_norm, _backward   layer norm; input, weight and bias gradients
  *   wm_seq_gated_scan, _backward   a gated linear recurrence over time
+ *   wm_seq_head_norm, _backward    the norm of queries' and keys' heads, and their rotation by position
+ *   wm_seq_decay_attention, _backward  linear attention whose weights decay with the distance
  *   wm_seq_clip                    the global norm of many gradients, and clipping by it
  *
  * The LSTM of wm.h multiplies its state by W_h at every step, so its steps run one
@@ -157,6 +159,82 @@ wm_status wm_seq_gated_scan_backward(wm_seq *h, int dtype, long long T, int N, i
                                      const int32_t *lengths, const wm_seq_view *h_seq, const wm_seq_view *dh,
                                      const float *dh_last, const wm_seq_view *dgate, const wm_seq_view *dx, float *dh0,
                                      void *cuda_stream);
+
+/* An array [T, N, heads, D] of the call's dtype whose last axis is dense: element (t, n, h, j) is
+ * data[t * stride_t + n * stride_n + h * stride_h + j].  Inputs may have any strides >= 0 (0: an axis
+ * that is broadcast; gradients come for each of its places, and their sum is the caller's); an
+ * output's elements must be apart: of the axes longer than 1, in some order, each stride is at least
+ * the extent of the axes inside it. */
+typedef struct {
+    void *data;
+    long long stride_t, stride_n, stride_h;
+} wm_seq_heads;
+
+/* The norm of each head's vector and its rotation by position, of queries and keys in one pass:
+ *   y = x / sqrt(mean(x^2) + eps) * weight over the D values of a head, then of the first `rotary`
+ *   values the pairs (y_i, y_{i + rotary/2}), or with `interleaved` (y_{2i}, y_{2i+1}), turn by
+ *   positions[t, n] * freqs[i]:  (a, b) -> (a cos - b sin, b cos + a sin).
+ *   q [T, N, q_heads, D], k [T, N, k_heads, D] dtype (k_heads 0: no keys);  q_out, k_out alike; an
+ *   output may be its input with the same strides (in place)
+ *   q_weight, k_weight [D] fp32, either may be NULL (1)
+ *   positions [T, N] int32 dense;  freqs [rotary / 2] fp32: radians a position
+ * rotary is even, 0 <= rotary <= D <= 1024; with 0 positions and freqs are not read.  Positions may be
+ * negative.  An angle is taken as a fraction of a turn in 64-bit integers, so that it is as good at far
+ * positions as at near ones; its frequency is the fp32 value as it is.  eps >= 0. */
+wm_status wm_seq_head_norm(wm_seq *h, int dtype, long long T, int N, int D, int rotary, int interleaved, int q_heads,
+                           const wm_seq_heads *q, const float *q_weight, int k_heads, const wm_seq_heads *k,
+                           const float *k_weight, float eps, const int32_t *positions, const float *freqs,
+                           const wm_seq_heads *q_out, const wm_seq_heads *k_out, void *cuda_stream);
+
+/* Its gradients.  q, k, weights, eps, positions and freqs as in the forward call (the norms are taken again
+ * from q and k) and
+ *   dq_out, dk_out  the gradients with respect to q_out and k_out
+ *   dq, dk  out; each may be its dq_out or dk_out with the same strides (in place)
+ *   dq_weight, dk_weight [D] fp32, optional out
+ * with g = weight * (dy turned back), r = 1 / sqrt(mean(x^2) + eps), xhat = x r:
+ *   dx = r (g - xhat mean(g xhat)),  dweight = sum over all heads of (dy turned back) xhat. */
+wm_status wm_seq_head_norm_backward(wm_seq *h, int dtype, long long T, int N, int D, int rotary, int interleaved,
+                                    int q_heads, const wm_seq_heads *q, const float *q_weight, const wm_seq_heads *dq_out,
+                                    int k_heads, const wm_seq_heads *k, const float *k_weight, const wm_seq_heads *dk_out,
+                                    float eps, const int32_t *positions, const float *freqs, const wm_seq_heads *dq,
+                                    const wm_seq_heads *dk, float *dq_weight, float *dk_weight, void *cuda_stream);
+
+/* Linear attention whose weights decay with the distance, for N sequences of `heads` heads, all independent:
+ *   S_t = lambda S_{t-1} + k_t v_t^T,  o_t = scale * S_t^T q_t,  lambda = exp(log_decay[head])
+ * that is o_t = scale * sum over s <= t of lambda^(t-s) (q_t . k_s) v_s.
+ *   q, k     [T, N, heads, Dk] dtype;  v [T, N, heads, Dv] dtype;  1 <= Dk, Dv <= 256
+ *   log_decay [heads] fp32, <= 0 (-inf: only the token itself; 0: no decay).  A constant of the model:
+ *            it has no gradient here
+ *   s0       [N, heads, Dk, Dv] fp32 dense or NULL = zeros: the state entering the call
+ *   reset    [T, N] uint8 dense or NULL: nonzero = step t starts a new episode, nothing before it is seen
+ *            (also when that holds inf or NaN)
+ *   lengths  [N] int32 or NULL = T: steps t >= lengths[n] are padding: their inputs and reset are not read, their
+ *            outputs are 0 and the state is carried on.  A length outside [0, T] is recorded as
+ *            WM_ERR_INVALID_ARG and clamped.
+ *   out      [T, N, heads, Dv] dtype, out
+ *   s_last   [N, heads, Dk, Dv] fp32 dense, optional out: the state after the last step; may be s0
+ * What is not finite reaches the outputs that see it, and no others.  T = 1 is the single-token form.  A call of T
+ * steps and calls on its parts (each entering with the s_last before it) agree to rounding.
+ * In bf16 the products of queries and keys, and the state as the queries read it, are rounded to bf16 as factors of
+ * the tensor cores; sums and the state itself stay fp32. */
+wm_status wm_seq_decay_attention(wm_seq *h, int dtype, long long T, int N, int heads, int Dk, int Dv, const wm_seq_heads *q,
+                                 const wm_seq_heads *k, const wm_seq_heads *v, const float *log_decay, float scale,
+                                 const float *s0, const uint8_t *reset, const int32_t *lengths, const wm_seq_heads *out,
+                                 float *s_last, void *cuda_stream);
+
+/* Its gradients.  q, k, v, log_decay, scale, s0, reset, lengths as in the forward call and
+ *   dout     [T, N, heads, Dv] dtype: the gradient with respect to out, not read in padding
+ *   ds_last  [N, heads, Dk, Dv] fp32 dense or NULL: the gradient with respect to s_last
+ *   dq, dk, dv  like q, k, v, out (0 in padding)
+ *   ds0      [N, heads, Dk, Dv] fp32 dense, optional out; may be ds_last
+ * with G_t = scale q_t dout_t^T + lambda G_{t+1} (no second term into a reset step; ds_last enters after the last
+ * step): dq_t = scale * S_t dout_t, dk_t = G_t v_t, dv_t = G_t^T k_t, ds0 = lambda G_0. */
+wm_status wm_seq_decay_attention_backward(wm_seq *h, int dtype, long long T, int N, int heads, int Dk, int Dv,
+                                          const wm_seq_heads *q, const wm_seq_heads *k, const wm_seq_heads *v,
+                                          const float *log_decay, float scale, const float *s0, const uint8_t *reset,
+                                          const int32_t *lengths, const wm_seq_heads *dout, const float *ds_last,
+                                          const wm_seq_heads *dq, const wm_seq_heads *dk, const wm_seq_heads *dv,
+                                          float *ds0, void *cuda_stream);
 
 /* One gradient of a clipping call: n values at src, written (scaled) to dst, which may
  * be src.  Gradients must not overlap one another. */

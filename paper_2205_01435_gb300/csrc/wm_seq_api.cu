@@ -4,6 +4,7 @@
 #include <stdio.h>
 
 #include <new>
+#include <utility>
 
 #include "wm_seq_internal.h"
 
@@ -81,6 +82,39 @@ struct Check {
         that(t_outer || n_outer, "an output's elements overlap (strides)");
     }
 };
+
+// An array [T, N, heads, D] (see wm_seq_heads), its elements apart where it is an output.
+void heads_view(Check &c, const wm_seq_heads *v, long long T, int N, int H, int D, size_t esize, bool out, bool needed,
+                const char *msg) {
+    if (c.why) return;
+    if (!v) {
+        c.that(!needed, msg);
+        return;
+    }
+    c.array(v->data, esize, needed, msg);
+    c.that(v->stride_t >= 0 && v->stride_n >= 0 && v->stride_h >= 0, "strides must be >= 0");
+    if (c.why || !out) return;
+    // apart: from the smallest stride up, each steps over the extent of the axes before it
+    struct Axis {
+        __int128 stride;  // (products pass 64 bits for absurd strides)
+        long long n;
+    } ax[3] = {{v->stride_t, T}, {v->stride_n, N}, {v->stride_h, H}};
+    for (int i = 0; i < 2; ++i)
+        for (int j = 0; j < 2 - i; ++j)
+            if (ax[j].stride > ax[j + 1].stride) std::swap(ax[j], ax[j + 1]);
+    __int128 extent = D;
+    bool apart = true;
+    for (const Axis &a : ax) {
+        if (a.n <= 1) continue;
+        apart = apart && a.stride >= extent;
+        extent += (a.n - 1) * a.stride;
+    }
+    c.that(apart, "an output's elements overlap (strides)");
+}
+
+bool same_view(const wm_seq_heads &a, const wm_seq_heads &b) {
+    return a.stride_t == b.stride_t && a.stride_n == b.stride_n && a.stride_h == b.stride_h;
+}
 
 size_t esize(int dtype) { return dtype == WM_BF16 ? 2 : 4; }
 
@@ -363,6 +397,157 @@ extern "C" wm_status wm_seq_gated_scan_backward(wm_seq *h, int dtype, long long 
     const wm_status st = reserve(h, wm_seq_scan_ws(h, a, true), s, kWhat);
     if (st != WM_OK) return st;
     return launched(h, wm_seq_scan_launch(h, a, true, s), kWhat);
+}
+
+namespace {
+
+wm_status head_norm(wm_seq *h, bool backward, seq_heads_args a, const wm_seq_heads *const (&x)[2], const wm_seq_heads *const (&dy)[2],
+                    const wm_seq_heads *const (&out)[2], void *cuda_stream, const char *kWhat) {
+    const std::lock_guard<std::mutex> busy(h->busy);
+    h->err[0] = 0;
+    OnDevice on(h);
+    if (on.e != cudaSuccess) return cuda_fail(h, on.e, kWhat);
+    Check c{h};
+    const cudaStream_t s = (cudaStream_t)cuda_stream;
+    c.that(a.dtype == WM_FP32 || a.dtype == WM_BF16, "dtype must be WM_FP32 or WM_BF16");
+    c.that(a.T >= 0 && a.T <= kMostInt && a.N >= 0 && a.D >= 1 && a.D <= 1024,
+           "0 <= T <= 2^31 - 65536, N >= 0 and 1 <= D <= 1024 are needed");
+    c.that(a.rotary >= 0 && a.rotary <= a.D && a.rotary % 2 == 0, "rotary must be even and in [0, D]");
+    c.that(a.heads[0] >= 1 && a.heads[0] <= 65536 && a.heads[1] >= 0 && a.heads[1] <= 65536,
+           "1 <= q_heads <= 65536 and 0 <= k_heads <= 65536 are needed");
+    c.that(a.eps >= 0.f && !isinf(a.eps), "eps must be finite and >= 0");
+    SEQ_CHECKED();
+    const bool any = a.T > 0 && a.N > 0;
+    const size_t es = esize(a.dtype);
+    for (int i = 0; i < 2; ++i) {
+        const bool need = any && a.heads[i] > 0;
+        if (a.heads[i] == 0) continue;
+        heads_view(c, x[i], a.T, a.N, a.heads[i], a.D, es, false, need, i ? "k is NULL" : "q is NULL");
+        heads_view(c, out[i], a.T, a.N, a.heads[i], a.D, es, true, need, "an output is NULL");
+        if (backward) heads_view(c, dy[i], a.T, a.N, a.heads[i], a.D, es, false, need, "an output's gradient is NULL");
+        c.array(a.weight[i], 4, false, "");
+        c.array(a.dweight[i], 4, false, "");
+        if (c.why || !need) continue;
+        a.x[i] = *x[i];
+        a.out[i] = *out[i];
+        if (backward) a.dy[i] = *dy[i];
+        const wm_seq_heads &from = backward ? a.dy[i] : a.x[i];
+        c.that(from.data != a.out[i].data || same_view(from, a.out[i]), "an output may be its input with the same strides only");
+        if (backward) c.that(a.out[i].data != a.x[i].data, "a gradient must not be q or k");
+    }
+    if (a.rotary > 0) {
+        c.array(a.positions, 4, any, "positions is NULL");
+        c.array(a.freqs, 4, any, "freqs is NULL");
+    }
+    SEQ_CHECKED();
+    h->last_launches = 0;
+    if (!any && !(backward && (a.dweight[0] || a.dweight[1]))) return WM_OK;
+    if (backward) {
+        const wm_status st = reserve(h, wm_seq_heads_backward_ws(h, a), s, kWhat);
+        if (st != WM_OK) return st;
+    }
+    return launched(h, wm_seq_heads_launch(h, a, backward, s), kWhat);
+}
+
+}  // namespace
+
+extern "C" wm_status wm_seq_head_norm(wm_seq *h, int dtype, long long T, int N, int D, int rotary, int interleaved, int q_heads,
+                                      const wm_seq_heads *q, const float *q_weight, int k_heads, const wm_seq_heads *k,
+                                      const float *k_weight, float eps, const int32_t *positions, const float *freqs,
+                                      const wm_seq_heads *q_out, const wm_seq_heads *k_out, void *cuda_stream) {
+    if (!h) return WM_ERR_INVALID_ARG;
+    seq_heads_args a{};
+    a.dtype = dtype; a.T = T; a.N = N; a.D = D; a.rotary = rotary; a.interleaved = interleaved != 0;
+    a.heads[0] = q_heads; a.heads[1] = k_heads;
+    a.weight[0] = q_weight; a.weight[1] = k_weight;
+    a.eps = eps; a.positions = positions; a.freqs = freqs;
+    return head_norm(h, false, a, {q, k}, {nullptr, nullptr}, {q_out, k_out}, cuda_stream, "wm_seq_head_norm");
+}
+
+extern "C" wm_status wm_seq_head_norm_backward(wm_seq *h, int dtype, long long T, int N, int D, int rotary, int interleaved,
+                                               int q_heads, const wm_seq_heads *q, const float *q_weight,
+                                               const wm_seq_heads *dq_out, int k_heads, const wm_seq_heads *k,
+                                               const float *k_weight, const wm_seq_heads *dk_out, float eps,
+                                               const int32_t *positions, const float *freqs, const wm_seq_heads *dq,
+                                               const wm_seq_heads *dk, float *dq_weight, float *dk_weight, void *cuda_stream) {
+    if (!h) return WM_ERR_INVALID_ARG;
+    seq_heads_args a{};
+    a.dtype = dtype; a.T = T; a.N = N; a.D = D; a.rotary = rotary; a.interleaved = interleaved != 0;
+    a.heads[0] = q_heads; a.heads[1] = k_heads;
+    a.weight[0] = q_weight; a.weight[1] = k_weight;
+    a.dweight[0] = dq_weight; a.dweight[1] = k_heads ? dk_weight : nullptr;
+    a.eps = eps; a.positions = positions; a.freqs = freqs;
+    return head_norm(h, true, a, {q, k}, {dq_out, dk_out}, {dq, dk}, cuda_stream, "wm_seq_head_norm_backward");
+}
+
+// What both directions of the decayed attention check; what a NULL array is said to be.
+#define DECAY_CHECKS()                                                                                                       \
+    SEQ_DTYPE();                                                                                                             \
+    c.that(T >= 0 && T <= kMostInt && N >= 0 && heads >= 1 && Dk >= 1 && Dk <= 256 && Dv >= 1 && Dv <= 256,                    \
+           "0 <= T <= 2^31 - 65536, N >= 0, heads >= 1 and 1 <= Dk, Dv <= 256 are needed");                                   \
+    c.that((long long)N * heads <= (1ll << 27), "N * heads must be at most 2^27");                                           \
+    c.that(!isnan(scale) && !isinf(scale), "scale must be finite");                                                          \
+    SEQ_CHECKED();                                                                                                           \
+    const bool any = T > 0 && N > 0;                                                                                         \
+    const size_t es = esize(dtype);                                                                                          \
+    heads_view(c, q, T, N, heads, Dk, es, false, any, "q is NULL");                                                          \
+    heads_view(c, k, T, N, heads, Dk, es, false, any, "k is NULL");                                                          \
+    heads_view(c, v, T, N, heads, Dv, es, false, any, "v is NULL");                                                          \
+    c.array(log_decay, 4, any, "log_decay is NULL");                                                                         \
+    c.array(s0, 4, false, "");                                                                                               \
+    c.array(reset, 1, false, "");                                                                                            \
+    c.array(lengths, 4, false, "")
+
+extern "C" wm_status wm_seq_decay_attention(wm_seq *h, int dtype, long long T, int N, int heads, int Dk, int Dv,
+                                            const wm_seq_heads *q, const wm_seq_heads *k, const wm_seq_heads *v,
+                                            const float *log_decay, float scale, const float *s0, const uint8_t *reset,
+                                            const int32_t *lengths, const wm_seq_heads *out, float *s_last,
+                                            void *cuda_stream) {
+    SEQ_BEGIN("wm_seq_decay_attention");
+    DECAY_CHECKS();
+    heads_view(c, out, T, N, heads, Dv, es, true, any, "out is NULL");
+    c.array(s_last, 4, false, "");
+    SEQ_CHECKED();
+    h->last_launches = 0;
+    if (N == 0) return WM_OK;
+    seq_decay_args a{};
+    a.dtype = dtype; a.T = T; a.N = N; a.H = heads; a.Dk = Dk; a.Dv = Dv;
+    if (any) {
+        a.q = *q; a.k = *k; a.v = *v; a.o = *out;
+    }
+    a.log_decay = log_decay; a.scale = scale; a.s0 = s0; a.reset = reset; a.lengths = lengths; a.s_last = s_last;
+    const wm_status st = reserve(h, wm_seq_decay_ws(h, a, false), s, kWhat);
+    if (st != WM_OK) return st;
+    return launched(h, wm_seq_decay_launch(h, a, false, s), kWhat);
+}
+
+extern "C" wm_status wm_seq_decay_attention_backward(wm_seq *h, int dtype, long long T, int N, int heads, int Dk, int Dv,
+                                                     const wm_seq_heads *q, const wm_seq_heads *k, const wm_seq_heads *v,
+                                                     const float *log_decay, float scale, const float *s0,
+                                                     const uint8_t *reset, const int32_t *lengths, const wm_seq_heads *dout,
+                                                     const float *ds_last, const wm_seq_heads *dq, const wm_seq_heads *dk,
+                                                     const wm_seq_heads *dv, float *ds0, void *cuda_stream) {
+    SEQ_BEGIN("wm_seq_decay_attention_backward");
+    DECAY_CHECKS();
+    heads_view(c, dout, T, N, heads, Dv, es, false, any, "dout is NULL");
+    heads_view(c, dq, T, N, heads, Dk, es, true, any, "dq is NULL");
+    heads_view(c, dk, T, N, heads, Dk, es, true, any, "dk is NULL");
+    heads_view(c, dv, T, N, heads, Dv, es, true, any, "dv is NULL");
+    c.array(ds_last, 4, false, "");
+    c.array(ds0, 4, false, "");
+    SEQ_CHECKED();
+    h->last_launches = 0;
+    if (N == 0) return WM_OK;
+    seq_decay_args a{};
+    a.dtype = dtype; a.T = T; a.N = N; a.H = heads; a.Dk = Dk; a.Dv = Dv;
+    if (any) {
+        a.q = *q; a.k = *k; a.v = *v; a.dout = *dout; a.dq = *dq; a.dk = *dk; a.dv = *dv;
+    }
+    a.log_decay = log_decay; a.scale = scale; a.s0 = s0; a.reset = reset; a.lengths = lengths;
+    a.ds_last = ds_last; a.ds0 = ds0;
+    const wm_status st = reserve(h, wm_seq_decay_ws(h, a, true), s, kWhat);
+    if (st != WM_OK) return st;
+    return launched(h, wm_seq_decay_launch(h, a, true, s), kWhat);
 }
 
 extern "C" wm_status wm_seq_clip(wm_seq *h, int count, const wm_seq_grad *grads, float max_norm, float *norm,

@@ -1,0 +1,597 @@
+// wm_seq_decay.cu -- linear attention whose weights decay with the distance: fp32 kernels, single tokens, launches.
+//
+//   S_t = lambda S_{t-1} + k_t v_t^T,  o_t = scale S_t^T q_t
+//
+// Chunks of C tokens: within a chunk the products of queries and keys are formed, weighted by lambda^(i-j) and multiplied
+// by the values; what came before the chunk enters through the state X alone.  That is 2 C (Dk + Dv) operations a token
+// within the chunk and 4 Dk Dv with the state, where the recurrence takes 5 Dk Dv on a state that would have to be moved
+// for every token.
+//
+// The gradients are three passes of the same form.  With X the state, dq_t = scale X_t dout_t is the attention of queries
+// dout, keys v and values k (its state is X transposed).  Against the order of time, G_t = scale q_t dout_t^T +
+// lambda G_{t+1} is a state with keys q and values dout: dv_t = G_t^T k_t reads it with queries k, and dk_t = G_t v_t reads
+// its transpose with queries v.  One launch runs the three side by side, a sequence's three passes next to one another, so
+// that two of the three reads of an array come from L2.
+//
+// Few sequences: each is cut into spans of time that run side by side.  A first launch forms what each span's own tokens
+// give the state (no queries, no outputs), a second joins them along time, the third is the pass itself.
+#include <algorithm>
+
+#include "wm_seq_decay.cuh"
+
+namespace {
+
+constexpr int kChunk = 64, kSlice = 64, kPad = 4, kThreads = 256;
+
+__device__ __forceinline__ float4 ld4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
+
+// ------------------------------------------------------------------ chunks in fp32
+// A CTA: one sequence of one head, one job, kSlice values of c.  Tiles in shared memory as fp32, a thread 4 x 4 outputs.
+// STATE: only what the span's tokens give the state.
+struct ChunkTiles {
+    int ld;  // of a and b
+    float *a, *b, *c, *p, *x, *kept;
+    __device__ ChunkTiles(float *m, int da) {
+        const int dp = (da + 3) / 4 * 4;
+        ld = dp + kPad;
+        a = m;
+        b = a + kChunk * ld;
+        c = b + kChunk * ld;
+        p = c + kChunk * kSlice;
+        x = p + kChunk * kChunk;
+        kept = x + dp * kSlice;
+    }
+    static size_t bytes(int da) {
+        const int dp = (da + 3) / 4 * 4;
+        return sizeof(float) * (2 * kChunk * (dp + kPad) + kChunk * kSlice + kChunk * kChunk + dp * kSlice + kChunk);
+    }
+};
+
+// Rows [0, rows) of a chunk, D values from column col0, zeros up to D padded to 4 (and the rows behind); true if a value
+// is not finite.
+template <class T>
+__device__ __forceinline__ bool load_rows(float *dst, int ld, const decay_array &g, long long base, const decay_seq &q, long long s0, int rows,
+                                          int col0, int D, int Dp, int vec) {
+    bool odd = false;
+    if (vec > 1) {  // 16 bytes
+        constexpr int V = 16 / sizeof(T);
+        const int per = (Dp + V - 1) / V;
+        for (int i = threadIdx.x; i < kChunk * per; i += kThreads) {
+            const int r = i / per, d = (i - r * per) * V;
+            float f[V] = {};
+            if (r < rows && d < D)
+                seq_unpack<T, V>(seq_load<T, V>(static_cast<const T *>(g.p) + base + q.at(s0 + r) * g.t + col0 + d), f);
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                odd |= !(fabsf(f[k]) <= 3.4028235e38f);
+                if (d + k < Dp) dst[r * ld + d + k] = f[k];
+            }
+        }
+    } else {
+        for (int i = threadIdx.x; i < kChunk * Dp; i += kThreads) {
+            const int r = i / Dp, d = i - r * Dp;
+            float f = 0.f;
+            if (r < rows && d < D) f = seq_to_float(static_cast<const T *>(g.p)[base + q.at(s0 + r) * g.t + col0 + d]);
+            odd |= !(fabsf(f) <= 3.4028235e38f);
+            dst[r * ld + d] = f;
+        }
+    }
+    return odd;
+}
+
+template <class T, bool STATE>
+__global__ void __launch_bounds__(kThreads, 2) decay_chunk_kernel(const decay_pass p) {
+    extern __shared__ __align__(16) float smem[];
+    __shared__ unsigned cuts[2];  // the chunk's tokens that begin something new
+    int job = 0, slice = blockIdx.x;
+    long long pair = 0;
+    {
+        int per = 0, before[3];
+        for (int i = 0; i < p.jobs; ++i) {
+            before[i] = per;
+            per += STATE && p.job[i].spans_t ? 0 : (p.job[i].dc + kSlice - 1) / kSlice;
+        }
+        pair = slice / per;
+        slice -= (int)pair * per;
+        for (int i = 1; i < p.jobs; ++i)
+            if (slice >= before[i] && !(STATE && p.job[i].spans_t)) job = i;
+        slice -= before[job];
+    }
+    const decay_job &j = p.job[job];
+    if (p.only_redo && !p.redo[job * (long long)p.N * p.H + pair]) return;
+    const int n = (int)(pair / p.H), head = (int)(pair % p.H), span = blockIdx.y, da = j.da, dp = (da + 3) / 4 * 4;
+    const int col0 = slice * kSlice, cols = min(kSlice, j.dc - col0), colp = (cols + 3) / 4 * 4;
+    const ChunkTiles m(smem, da);
+    const decay_seq q = decay_open(p, j, n);
+    const float g = p.log_decay[head];
+    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+    const long long pairs = (long long)p.N * p.H, cells = (long long)da * j.dc;
+    const long long first = span * p.span_tokens, last = min(p.T, first + p.span_tokens);
+
+    // the entering state
+    const float *from = nullptr;
+    int from_t = 0;
+    float mul = 1.f;
+    if constexpr (!STATE) {
+        if (p.spans > 1) {
+            from = j.spans + (span * pairs + pair) * cells;
+            from_t = j.spans_t;
+        } else if (j.s_in) {
+            from = j.s_in + pair * cells;
+            from_t = j.in_t;
+            if (j.first && q.len > 0) mul = decay_power(g, 1);
+        }
+    }
+    for (int i = tid; i < dp * kSlice; i += kThreads) {
+        const int r = i / kSlice, c = i % kSlice;
+        float v = 0.f;
+        if (from && r < da && c < cols) v = (from_t ? from[(long long)(col0 + c) * da + r] : from[(long long)r * j.dc + col0 + c]);
+        m.x[i] = mul == 1.f ? v : v * mul;
+    }
+    float carry = 1.f;
+
+    const long long an = n * j.a.n + head * j.a.h, bn = n * j.b.n + head * j.b.h, cn = n * j.c.n + head * j.c.h;
+    for (long long s0 = first; s0 < last; s0 += kChunk) {
+        const int rows = (int)max(0ll, min((long long)kChunk, min(last, q.len) - s0));
+        if (rows == 0) {
+            if constexpr (STATE) break;
+            T *y = static_cast<T *>(const_cast<void *>(j.y.p)) + n * j.y.n + head * j.y.h + col0;
+            const int pad = (int)min((long long)kChunk, last - s0);
+            for (int i = tid; i < pad * cols; i += kThreads) y[(s0 + i / cols) * j.y.t + i % cols] = seq_from_float<T>(0.f);
+            continue;
+        }
+        __syncthreads();
+        bool odd = load_rows<T>(m.b, m.ld, j.b, bn, q, s0, rows, 0, da, dp, j.vec);
+        odd |= load_rows<T>(m.c, kSlice, j.c, cn, q, s0, rows, col0, cols, kSlice, j.vec);
+        if constexpr (!STATE) load_rows<T>(m.a, m.ld, j.a, an, q, s0, rows, 0, da, dp, j.vec);
+        if (tid < 64) {
+            const unsigned c = __ballot_sync(~0u, decay_cut(p, q, s0 + tid, n) && tid < rows);
+            if ((tid & 31) == 0) cuts[tid >> 5] = c;
+        }
+        const bool careful = __syncthreads_or(odd);  // (its zero weights would make NaN of what is not finite)
+        const unsigned long long cut = cuts[0] | (unsigned long long)cuts[1] << 32;
+        // the first token that token i sees; with none of the chunk cut before, the state too
+        auto start = [&](int i) {
+            const unsigned long long c = cut & (~0ull >> (63 - i));
+            return c ? 63 - __clzll((long long)c) : -1;
+        };
+        const int keep_from = start(rows - 1);
+        // (time's order, the last chunk of all: the state leaves as the last token wrote it)
+        const int less = j.first && p.span_tokens > 0 && s0 + rows == q.len && !STATE ? 1 : 0;
+        if (tid < kChunk) m.kept[tid] = tid < rows && tid >= keep_from ? j.up_scale * decay_power(g, rows - tid - less) : 0.f;
+
+        if constexpr (!STATE) {
+            int begin[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) begin[i] = start(ty * 4 + i);
+            // p = a b^T, weighted
+            const int nb = ty / 4 + 1;  // columns beyond the rows' own are not seen
+            float acc[4][4] = {};
+            for (int d = 0; d < dp; d += 4) {
+                float4 x[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = ld4(m.a + (ty * 4 + i) * m.ld + d);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (k >= nb) break;
+                    const float4 y = ld4(m.b + (tx + 16 * k) * m.ld + d);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[i][k] += x[i].x * y.x + x[i].y * y.y + x[i].z * y.z + x[i].w * y.w;
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = ty * 4 + i;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int c = tx + 16 * k;
+                    const bool seen = c <= r && c >= begin[i] && r < rows;
+                    m.p[r * kChunk + c] = seen ? acc[i][k] * (j.w_scale * decay_power(g, r - c)) : 0.f;
+                }
+            }
+            __syncthreads();
+            // y = p c + lambda^r X^T a
+            float y[4][4] = {};
+            if (tx * 4 < colp) {
+                if (!careful) {
+                    for (int k = 0; k < ty * 4 + 4; k += 4) {
+                        float4 w[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) w[i] = ld4(m.p + (ty * 4 + i) * kChunk + k);
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) {
+                            const float4 v = ld4(m.c + (k + h) * kSlice + tx * 4);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                const float f = h == 0 ? w[i].x : h == 1 ? w[i].y : h == 2 ? w[i].z : w[i].w;
+                                y[i][0] += f * v.x, y[i][1] += f * v.y, y[i][2] += f * v.z, y[i][3] += f * v.w;
+                            }
+                        }
+                    }
+                } else {
+                    for (int i = 0; i < 4; ++i)
+                        for (int k = max(begin[i], 0); k <= min(ty * 4 + i, rows - 1); ++k) {
+                            const float f = m.p[(ty * 4 + i) * kChunk + k];
+                            for (int h = 0; h < 4; ++h) y[i][h] += f * m.c[k * kSlice + tx * 4 + h];
+                        }
+                }
+                float in[4][4] = {};
+                for (int d = 0; d < dp; d += 4) {
+                    float4 x[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[i] = ld4(m.a + (ty * 4 + i) * m.ld + d);
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        const float4 v = ld4(m.x + (d + h) * kSlice + tx * 4);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float f = h == 0 ? x[i].x : h == 1 ? x[i].y : h == 2 ? x[i].z : x[i].w;
+                            in[i][0] += f * v.x, in[i][1] += f * v.y, in[i][2] += f * v.z, in[i][3] += f * v.w;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = ty * 4 + i;
+                    if (s0 + r >= last) continue;
+                    const float w = j.in_scale * decay_power(g, r);
+                    T *out = static_cast<T *>(const_cast<void *>(j.y.p)) + n * j.y.n + head * j.y.h + q.at(s0 + r) * j.y.t + col0 + tx * 4;
+#pragma unroll
+                    for (int h = 0; h < 4; ++h)
+                        if (tx * 4 + h < cols)
+                            out[h] = seq_from_float<T>(r >= rows ? 0.f : begin[i] < 0 ? y[i][h] + w * in[i][h] : y[i][h]);
+                }
+            }
+        }
+        __syncthreads();
+        // X = lambda^n X + b^T (kept c)
+        const float shrink = decay_power(g, rows - less);
+        const int from_row = careful ? max(keep_from, 0) : 0;
+        if (tx * 4 < colp) {
+            for (int r0 = ty * 4; r0 < dp; r0 += 64) {
+                float acc[4][4] = {};
+                for (int k = from_row; k < rows; ++k) {
+                    const float4 u = ld4(m.b + k * m.ld + r0), v = ld4(m.c + k * kSlice + tx * 4);
+                    const float w = m.kept[k], f[4] = {u.x * w, u.y * w, u.z * w, u.w * w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[i][0] += f[i] * v.x, acc[i][1] += f[i] * v.y, acc[i][2] += f[i] * v.z, acc[i][3] += f[i] * v.w;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float *x = m.x + (r0 + i) * kSlice + tx * 4;
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) x[h] = keep_from < 0 ? x[h] * shrink + acc[i][h] : acc[i][h];
+                }
+            }
+        }
+        carry = keep_from < 0 ? carry * shrink : 0.f;
+    }
+    __syncthreads();
+    // what leaves: the span's part, or the state itself (of the span that holds the sequence's end)
+    float *to = nullptr;
+    bool empty = false;
+    if constexpr (STATE) {
+        to = j.spans + (span * pairs + pair) * cells;
+        if (slice == 0 && tid == 0) p.carry[((long long)span * 2 + j.reverse) * pairs + pair] = carry;
+    } else if (j.s_out) {
+        const bool ends = q.len > first && q.len <= last;
+        if (ends || (q.len == 0 && span == 0)) to = j.s_out + pair * cells;
+        empty = j.out_zero && q.len > 0 && p.reset && p.reset[n] != 0;
+    }
+    if (to)
+        for (int i = tid; i < da * cols; i += kThreads) {
+            const int r = i / cols, c = i - r * cols;
+            to[(long long)r * j.dc + col0 + c] = empty ? 0.f : m.x[r * kSlice + c];
+        }
+}
+
+// Spans' own parts -> what enters each span, along time.  A thread takes one cell of a state; jobs that form the spans.
+__global__ void __launch_bounds__(256) decay_join_kernel(const decay_pass p) {
+    const decay_job &j = p.job[blockIdx.y];
+    if (j.spans_t) return;
+    const long long cells = (long long)j.da * j.dc, pairs = (long long)p.N * p.H, i = (long long)blockIdx.x * 256 + threadIdx.x;
+    if (i >= cells * pairs) return;
+    const long long pair = i / cells, cell = i % cells;
+    float x = 0.f;
+    if (j.s_in) {
+        const long long r = cell / j.dc, c = cell % j.dc;
+        x = j.s_in[pair * cells + (j.in_t ? c * j.da + r : cell)];
+        const int n = (int)(pair / p.H);
+        if (j.first && (!p.lengths || p.lengths[n] > 0)) x *= decay_power(p.log_decay[pair % p.H], 1);
+    }
+    for (int s = 0; s < p.spans; ++s) {
+        float *at = j.spans + s * pairs * cells + i;
+        const float own = *at, c = p.carry[((long long)s * 2 + j.reverse) * pairs + pair];
+        *at = x;
+        x = c == 0.f ? own : x * c + own;
+    }
+}
+
+// ------------------------------------------------------------------ token by token
+// Up to a few tokens: the state in registers, read and written once.  A CTA: one head of one sequence, 4 CT columns of its
+// state; thread (row group, column group) holds rows of 4 columns.
+struct StepArgs {
+    decay_array q, k, v, o;
+    int T, N, H, Dk, Dv, ct, slices, vec;
+    const float *log_decay, *s0;
+    const uint8_t *reset;
+    const int32_t *lengths;
+    float scale, *s_last;
+    int *status;
+};
+
+template <class T, int ROWS, bool VEC>
+__global__ void __launch_bounds__(256) decay_step_kernel(const StepArgs p) {
+    __shared__ float q[256], k[256], v[64];
+    __shared__ float part[8][64];
+    const long long pair = blockIdx.x / p.slices;
+    const int slice = blockIdx.x % p.slices, n = (int)(pair / p.H), head = (int)(pair % p.H), tid = threadIdx.x;
+    const int cg = tid & (p.ct - 1), rg = tid / p.ct, groups = 256 / p.ct, width = 4 * p.ct, col0 = slice * width, col = col0 + cg * 4;
+    int len = p.T;
+    if (p.lengths) {
+        len = p.lengths[n];
+        if (len < 0 || len > p.T) seq_record(p.status, WM_ERR_INVALID_ARG);
+        len = max(0, min(len, p.T));
+    }
+    float x[ROWS][4];
+    // (a first token that a reset begins does not see the state)
+    const bool read = p.s0 && !(len > 0 && p.reset && p.reset[n]);
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int r = rg + i * groups;
+#pragma unroll
+        for (int h = 0; h < 4; ++h) x[i][h] = 0.f;
+        if (!read || r >= p.Dk) continue;
+        const float *at = p.s0 + (pair * p.Dk + r) * p.Dv + col;
+        if constexpr (VEC) {
+            if (col < p.Dv) {
+                const float4 u = ld4(at);
+                x[i][0] = u.x, x[i][1] = u.y, x[i][2] = u.z, x[i][3] = u.w;
+            }
+        } else {
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+                if (col + h < p.Dv) x[i][h] = at[h];
+        }
+    }
+    const float keep = expf(p.log_decay[head]);
+    for (int t = 0; t < p.T; ++t) {
+        T *out = static_cast<T *>(const_cast<void *>(p.o.p)) + t * p.o.t + n * p.o.n + head * p.o.h;
+        if (t >= len) {
+            if (tid < width && col0 + tid < p.Dv) out[col0 + tid] = seq_from_float<T>(0.f);
+            continue;
+        }
+        if (tid < p.Dk) {
+            q[tid] = seq_to_float(static_cast<const T *>(p.q.p)[t * p.q.t + n * p.q.n + head * p.q.h + tid]);
+            k[tid] = seq_to_float(static_cast<const T *>(p.k.p)[t * p.k.t + n * p.k.n + head * p.k.h + tid]);
+        }
+        if (tid < width)
+            v[tid] = col0 + tid < p.Dv ? seq_to_float(static_cast<const T *>(p.v.p)[t * p.v.t + n * p.v.n + head * p.v.h + col0 + tid]) : 0.f;
+        const bool cut = p.reset && p.reset[(long long)t * p.N + n];
+        __syncthreads();
+        const float4 w = ld4(v + cg * 4);
+        float y[4] = {};
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            const int r = rg + i * groups;
+            if (r >= p.Dk) break;
+            const float a = k[r], b = q[r];
+            x[i][0] = (cut ? 0.f : keep * x[i][0]) + a * w.x;
+            x[i][1] = (cut ? 0.f : keep * x[i][1]) + a * w.y;
+            x[i][2] = (cut ? 0.f : keep * x[i][2]) + a * w.z;
+            x[i][3] = (cut ? 0.f : keep * x[i][3]) + a * w.w;
+#pragma unroll
+            for (int h = 0; h < 4; ++h) y[h] += b * x[i][h];
+        }
+        for (int o = 16; o >= p.ct; o >>= 1)
+#pragma unroll
+            for (int h = 0; h < 4; ++h) y[h] += __shfl_xor_sync(~0u, y[h], o);
+        if ((tid & 31) < p.ct)
+#pragma unroll
+            for (int h = 0; h < 4; ++h) part[tid >> 5][cg * 4 + h] = y[h];
+        __syncthreads();
+        if (tid < width && col0 + tid < p.Dv) {
+            float sum = part[0][tid];
+#pragma unroll
+            for (int g = 1; g < 8; ++g) sum += part[g][tid];
+            out[col0 + tid] = seq_from_float<T>(sum * p.scale);
+        }
+    }
+    if (!p.s_last) return;
+#pragma unroll
+    for (int i = 0; i < ROWS; ++i) {
+        const int r = rg + i * groups;
+        if (r >= p.Dk) break;
+        float *at = p.s_last + (pair * p.Dk + r) * p.Dv + col;
+        if constexpr (VEC) {
+            if (col < p.Dv) *reinterpret_cast<float4 *>(at) = make_float4(x[i][0], x[i][1], x[i][2], x[i][3]);
+        } else {
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+                if (col + h < p.Dv) at[h] = x[i][h];
+        }
+    }
+}
+
+// ------------------------------------------------------------------ launches
+decay_array array_of(const wm_seq_heads &v) { return {v.data, v.stride_t, v.stride_n, v.stride_h}; }
+
+bool aligned16(const decay_array &v, const seq_decay_args &a, int D) {
+    const long long es = a.dtype == WM_BF16 ? 2 : 4;
+    return (uintptr_t)v.p % 16 == 0 && D * es % 16 == 0 && (a.T == 1 || v.t * es % 16 == 0) && (a.N == 1 || v.n * es % 16 == 0) &&
+           (a.H == 1 || v.h * es % 16 == 0);
+}
+
+// The jobs of a call: the pass itself, or the gradients' three.
+decay_pass pass_of(const wm_seq *h, const seq_decay_args &a, bool backward) {
+    decay_pass p{};
+    p.T = a.T; p.N = a.N; p.H = a.H;
+    p.log_decay = a.log_decay; p.reset = a.reset; p.lengths = a.lengths;
+    p.status = h->status;
+    const decay_array q = array_of(a.q), k = array_of(a.k), v = array_of(a.v), o = array_of(a.o), dout = array_of(a.dout);
+    const auto job = [&](const decay_array &x, const decay_array &y, const decay_array &z, const decay_array &out, int da, int dc) {
+        decay_job j{};
+        j.a = x; j.b = y; j.c = z; j.y = out;
+        j.da = da; j.dc = dc;
+        j.w_scale = j.in_scale = a.scale;
+        j.up_scale = 1.f;
+        const int V = a.dtype == WM_BF16 ? 8 : 4;
+        j.vec = aligned16(x, a, da) && aligned16(y, a, da) && aligned16(z, a, dc) && aligned16(out, a, dc) ? V : 1;
+        return j;
+    };
+    if (!backward) {
+        p.jobs = 1;
+        decay_job &f = p.job[0] = job(q, k, v, o, a.Dk, a.Dv);
+        f.first = 1;
+        f.s_in = a.s0;
+        f.s_out = a.s_last;
+        return p;
+    }
+    p.jobs = 3;
+    decay_job &dq = p.job[0] = job(dout, v, k, array_of(a.dq), a.Dv, a.Dk);
+    dq.first = 1;
+    dq.s_in = a.s0;
+    dq.in_t = 1;
+    decay_job &dv = p.job[1] = job(k, q, dout, array_of(a.dv), a.Dk, a.Dv);
+    dv.reverse = 1;
+    dv.in_scale = 1.f;
+    dv.up_scale = a.scale;
+    dv.s_in = a.ds_last;
+    dv.s_out = a.ds0;
+    dv.out_zero = 1;
+    decay_job &dk = p.job[2] = job(v, dout, q, array_of(a.dk), a.Dv, a.Dk);
+    dk.reverse = 1;
+    dk.in_scale = 1.f;
+    dk.up_scale = a.scale;
+    dk.s_in = a.ds_last;
+    dk.in_t = 1;
+    dk.spans_t = 1;
+    return p;
+}
+
+int slices_of(int dc) { return (dc + kSlice - 1) / kSlice; }
+
+// Few sequences are cut in time so that every SM has two CTAs, into spans of at least 4 chunks: with fewer the two reads of
+// keys and values that forming the states takes cost more than the SMs they would fill.
+void split(const wm_seq *h, decay_pass &p, int chunk) {
+    long long ctas = 0;
+    for (int i = 0; i < p.jobs; ++i) ctas += slices_of(p.job[i].dc);
+    ctas *= (long long)p.N * p.H;
+    const long long chunks = (p.T + chunk - 1) / chunk;
+    long long spans = std::max(1ll, std::min({2ll * h->sms / std::max(1ll, ctas), chunks / 4, 65535ll}));
+    const long long per = std::max(1ll, (chunks + spans - 1) / spans);
+    p.span_tokens = per * chunk;
+    p.spans = (int)std::max(1ll, (chunks + per - 1) / per);
+}
+
+bool steps_take(const seq_decay_args &a, bool backward) { return !backward && a.T <= 8; }
+
+// Scratch of a pass: the spans' states and carries; a copy of ds_last where ds0 takes its place (two jobs read it, one writes).
+struct Scratch {
+    size_t spans[3] = {}, carry = 0, copy = 0, bytes = 0;
+    Scratch(const decay_pass &p, const seq_decay_args &a) {
+        const auto take = [&](size_t n) {
+            const size_t at = bytes;
+            bytes += (n + 255) / 256 * 256;
+            return at;
+        };
+        const size_t pairs = (size_t)p.N * p.H;
+        if (p.spans > 1) {
+            for (int i = 0; i < p.jobs; ++i)
+                if (!p.job[i].spans_t) spans[i] = take(pairs * p.spans * p.job[i].da * p.job[i].dc * 4);
+            carry = take(pairs * p.spans * 2 * 4);
+        }
+        if (p.jobs > 1 && a.ds0 && a.ds0 == a.ds_last) copy = take(pairs * a.Dk * a.Dv * 4);
+    }
+};
+
+template <class T, int ROWS>
+cudaError_t run_steps(wm_seq *h, const StepArgs &p, cudaStream_t s) {
+    const unsigned grid = (unsigned)((long long)p.N * p.H * p.slices);
+    ++h->last_launches;
+    if (p.vec) decay_step_kernel<T, ROWS, true><<<grid, 256, 0, s>>>(p);
+    else decay_step_kernel<T, ROWS, false><<<grid, 256, 0, s>>>(p);
+    return cudaGetLastError();
+}
+
+template <class T>
+cudaError_t steps(wm_seq *h, const seq_decay_args &a, cudaStream_t s) {
+    StepArgs p{};
+    p.q = array_of(a.q); p.k = array_of(a.k); p.v = array_of(a.v); p.o = array_of(a.o);
+    p.T = (int)a.T; p.N = a.N; p.H = a.H; p.Dk = a.Dk; p.Dv = a.Dv;
+    p.log_decay = a.log_decay; p.s0 = a.s0; p.reset = a.reset; p.lengths = a.lengths;
+    p.scale = a.scale; p.s_last = a.s_last; p.status = h->status;
+    // 64 columns a CTA, 32 where that leaves SMs without one
+    const long long pairs = (long long)a.N * a.H;
+    p.ct = a.Dv <= 32 || pairs * ((a.Dv + 63) / 64) < h->sms ? 8 : 16;
+    p.slices = (a.Dv + 4 * p.ct - 1) / (4 * p.ct);
+    p.vec = a.Dv % 4 == 0 && (uintptr_t)a.s0 % 16 == 0 && (uintptr_t)a.s_last % 16 == 0;
+    const int groups = 256 / p.ct, rows = (a.Dk + groups - 1) / groups;
+    if (rows <= 2) return run_steps<T, 2>(h, p, s);
+    if (rows <= 4) return run_steps<T, 4>(h, p, s);
+    if (rows <= 8) return run_steps<T, 8>(h, p, s);
+    return run_steps<T, 16>(h, p, s);
+}
+
+template <class T>
+cudaError_t chunks(wm_seq *h, const decay_pass &p, cudaStream_t s) {
+    const long long pairs = (long long)p.N * p.H;
+    int da = 0, out = 0, state = 0;
+    for (int i = 0; i < p.jobs; ++i) {
+        da = std::max(da, p.job[i].da);
+        out += slices_of(p.job[i].dc);
+        state += p.job[i].spans_t ? 0 : slices_of(p.job[i].dc);
+    }
+    const size_t bytes = ChunkTiles::bytes(da);
+    cudaError_t e = cudaFuncSetAttribute(decay_chunk_kernel<T, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != cudaSuccess) return e;
+    if (p.spans > 1) {
+        e = cudaFuncSetAttribute(decay_chunk_kernel<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+        if (e != cudaSuccess) return e;
+        decay_chunk_kernel<T, true><<<dim3((unsigned)(pairs * state), p.spans), kThreads, bytes, s>>>(p);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        long long cells = 0;
+        for (int i = 0; i < p.jobs; ++i) cells = std::max(cells, pairs * p.job[i].da * p.job[i].dc);
+        decay_join_kernel<<<dim3((unsigned)((cells + 255) / 256), p.jobs), 256, 0, s>>>(p);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+        h->last_launches += 2;
+    }
+    ++h->last_launches;
+    decay_chunk_kernel<T, false><<<dim3((unsigned)(pairs * out), p.spans), kThreads, bytes, s>>>(p);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t wm_seq_decay_ws(const wm_seq *h, const seq_decay_args &a, bool backward) {
+    if (a.T == 0 || steps_take(a, backward)) return 0;
+    decay_pass p = pass_of(h, a, backward);
+    split(h, p, kChunk);
+    return Scratch(p, a).bytes;
+}
+
+cudaError_t wm_seq_decay_launch(wm_seq *h, const seq_decay_args &a, bool backward, cudaStream_t s) {
+    h->last_launches = 0;
+    const size_t state = (size_t)a.N * a.H * a.Dk * a.Dv * 4;
+    if (a.T == 0) {  // the state, or its gradient, goes through
+        float *to = backward ? a.ds0 : a.s_last;
+        const float *from = backward ? a.ds_last : a.s0;
+        if (!to || to == from) return cudaSuccess;
+        return from ? cudaMemcpyAsync(to, from, state, cudaMemcpyDeviceToDevice, s) : cudaMemsetAsync(to, 0, state, s);
+    }
+    if (steps_take(a, backward)) return a.dtype == WM_BF16 ? steps<__nv_bfloat16>(h, a, s) : steps<float>(h, a, s);
+    decay_pass p = pass_of(h, a, backward);
+    split(h, p, kChunk);
+    const Scratch w(p, a);
+    unsigned char *ws = static_cast<unsigned char *>(h->ws);
+    for (int i = 0; i < p.jobs; ++i)
+        if (p.spans > 1) p.job[i].spans = reinterpret_cast<float *>(ws + w.spans[p.job[i].spans_t ? 1 : i]);
+    p.carry = reinterpret_cast<float *>(ws + w.carry);
+    if (backward && a.ds0 && a.ds0 == a.ds_last) {
+        float *copy = reinterpret_cast<float *>(ws + w.copy);
+        const cudaError_t e = cudaMemcpyAsync(copy, a.ds_last, state, cudaMemcpyDeviceToDevice, s);
+        if (e != cudaSuccess) return e;
+        p.job[1].s_in = p.job[2].s_in = copy;
+    }
+    return a.dtype == WM_BF16 ? chunks<__nv_bfloat16>(h, p, s) : chunks<float>(h, p, s);
+}

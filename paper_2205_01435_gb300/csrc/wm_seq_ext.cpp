@@ -77,6 +77,16 @@ wm_seq_view view(const at::Tensor &t, at::ScalarType type, at::IntArrayRef shape
     return {t.data_ptr(), shape.size() == 3 ? st[0] : 0, st[shape.size() - 2]};
 }
 
+// A [T, N, heads, D] (or, one step, [N, heads, D]) tensor whose last axis is dense.
+wm_seq_heads heads(const at::Tensor &t, at::ScalarType type, at::IntArrayRef shape, const char *what) {
+    const auto st = t.strides();
+    if (t.scalar_type() != type || t.sizes() != shape || (st.back() != 1 && shape.back() > 1))
+        throw Refuse{std::string(what) + ": a " + toString(type) + " tensor of shape " + text(shape) +
+                     " with a dense last axis is needed, got " + toString(t.scalar_type()) + " " + text(t.sizes())};
+    const size_t n = shape.size();
+    return {t.data_ptr(), n == 4 ? st[0] : 0, st[n - 3], st[n - 2]};
+}
+
 // The stride of a tensor's rows: its leading axes have to be one run of them.
 long long row_stride(const at::Tensor &t, const char *what) {
     const int64_t n = t.dim();
@@ -327,6 +337,158 @@ PyObject *scan_backward(const Call &c) {
     return tuple({give(c.a[8], m0), give(c.a[9], m1), dh0 ? give(c.a[11], m2) : none()});
 }
 
+// A side of the head norm: queries (0) or keys (1).
+struct Heads {
+    const at::Tensor *x = nullptr, *out = nullptr;
+    at::Tensor made;
+    wm_seq_heads vx{}, vo{}, vd{};
+    const float *w = nullptr;
+    int n = 0;
+};
+
+// q, k, q_weight, k_weight, positions, freqs, eps, interleaved, q_out, k_out; BACK: q_out, k_out are dq, dk, then dq_out, dk_out,
+// want_params.  Arrays [T, N, heads, D], or [N, heads, D] of one step.
+template <bool BACK>
+PyObject *head_norm(const Call &c) {
+    Heads s[2];
+    const char *const names[2] = {"q", "k"}, *const outs[2] = {BACK ? "dq" : "q_out", BACK ? "dk" : "k_out"}, *const grads[2] = {"dq_out", "dk_out"},
+                      *const ws[2] = {"q_weight", "k_weight"};
+    const at::Tensor &q = tensor(c.a[0], "q");
+    const auto type = q.scalar_type();
+    const int dt = dtype_of(q);
+    const int64_t dim = q.dim();
+    if (dim != 3 && dim != 4) throw Refuse{"q [T, N, heads, D] (or [N, heads, D]) is needed"};
+    const int64_t D = q.size(-1), par[1] = {D};
+    for (int i = 0; i < 2; ++i) {
+        const at::Tensor *x = s[i].x = maybe(c.a[i], names[i]), *w = maybe(c.a[2 + i], ws[i]), *dy = BACK ? maybe(c.a[10 + i], grads[i]) : nullptr;
+        const at::Tensor *out = maybe(c.a[8 + i], outs[i]);
+        if (!x) {
+            if (w || out || dy) throw Refuse{"without k its weight, its output and their gradients are none either"};
+            continue;
+        }
+        std::vector<int64_t> shape(q.sizes().begin(), q.sizes().end());
+        if (x->dim() != dim) throw Refuse{"k must have as many axes as q"};
+        shape[dim - 2] = x->size(dim - 2);
+        s[i].n = size(shape[dim - 2]);
+        s[i].vx = heads(*x, type, shape, names[i]);
+        s[i].w = flat<float>(w, at::kFloat, par, ws[i]);
+        if (!out) out = &(s[i].made = c.fresh(shape, type));
+        s[i].out = out;
+        s[i].vo = heads(*out, type, shape, outs[i]);
+        if (BACK) {
+            if (!dy) throw Refuse{std::string(grads[i]) + ": a tensor is needed"};
+            s[i].vd = heads(*dy, type, shape, grads[i]);
+        }
+    }
+    const at::Tensor *positions = maybe(c.a[4], "positions"), *freqs = maybe(c.a[5], "freqs");
+    if (!positions != !freqs) throw Refuse{"positions and freqs are given together"};
+    const int32_t *pp = flat<int32_t>(positions, at::kInt, q.sizes().slice(0, dim - 2), "positions");
+    if (freqs && freqs->dim() != 1) throw Refuse{"freqs [rotary / 2] is needed"};
+    const float *fp = freqs ? flat<float>(freqs, at::kFloat, freqs->sizes(), "freqs") : nullptr;
+    if (freqs && freqs->size(0) * 2 > D) throw Refuse{"freqs [rotary / 2] with rotary <= D is needed"};
+    const int rotary = freqs ? 2 * (int)freqs->size(0) : 0;
+    const float eps = (float)c.number(6);
+    const bool in = c.yes(7);
+    const long long T = dim == 4 ? q.size(0) : 1;
+    const int N = size(q.size(dim - 3)), d = size(D);
+    void *st = c.stream();
+    if (!BACK) {
+        c.run([&] {
+            return wm_seq_head_norm(c.h, dt, T, N, d, rotary, in, s[0].n, &s[0].vx, s[0].w, s[1].n, s[1].x ? &s[1].vx : nullptr, s[1].w, eps, pp,
+                                    fp, &s[0].vo, s[1].x ? &s[1].vo : nullptr, st);
+        });
+        PyObject *first = give(c.a[8], s[0].made);
+        return s[1].x ? tuple({first, give(c.a[9], s[1].made)}) : first;
+    }
+    at::Tensor dw[2];
+    float *wp[2] = {};
+    const bool params = c.yes(12);
+    for (int i = 0; i < 2 && params; ++i)
+        if (s[i].x) wp[i] = (float *)(dw[i] = c.fresh(par, at::kFloat)).data_ptr();
+    c.run([&] {
+        return wm_seq_head_norm_backward(c.h, dt, T, N, d, rotary, in, s[0].n, &s[0].vx, s[0].w, &s[0].vd, s[1].n, s[1].x ? &s[1].vx : nullptr,
+                                         s[1].w, s[1].x ? &s[1].vd : nullptr, eps, pp, fp, &s[0].vo, s[1].x ? &s[1].vo : nullptr, wp[0], wp[1],
+                                         st);
+    });
+    return tuple({give(c.a[8], s[0].made), s[1].x ? give(c.a[9], s[1].made) : none(), wp[0] ? give(dw[0]) : none(), wp[1] ? give(dw[1]) : none()});
+}
+
+// The shapes of a decayed attention: q, k [T, N, heads, Dk], v [T, N, heads, Dv]; STEP: without T.
+template <bool STEP>
+struct Decay {
+    const at::Tensor &q, &k, &v, &g;
+    at::ScalarType type;
+    int dt, N, H, Dk, Dv;
+    long long T;
+    std::vector<int64_t> sk, sv, state;
+    wm_seq_heads vq, vk, vv;
+    const float *pg, *p0;
+    const uint8_t *reset;
+    const int32_t *lengths;
+    // arguments q, k, v, log_decay at 0; s0, reset, lengths at `at`
+    Decay(const Call &c, int at) : q(tensor(c.a[0], "q")), k(tensor(c.a[1], "k")), v(tensor(c.a[2], "v")), g(tensor(c.a[3], "log_decay")) {
+        type = q.scalar_type();
+        dt = dtype_of(q);
+        const int64_t dim = STEP ? 3 : 4;
+        if (q.dim() != dim || v.dim() != dim) throw Refuse{STEP ? "q [N, heads, Dk] and v [N, heads, Dv] are needed" : "q [T, N, heads, Dk] and v [T, N, heads, Dv] are needed"};
+        sk.assign(q.sizes().begin(), q.sizes().end());
+        sv = sk;
+        sv.back() = v.size(-1);
+        T = STEP ? 1 : sk[0];
+        N = size(sk[dim - 3]); H = size(sk[dim - 2]); Dk = size(sk.back()); Dv = size(sv.back());
+        state = {N, H, Dk, Dv};
+        vq = heads(q, type, sk, "q");
+        vk = heads(k, type, sk, "k");
+        vv = heads(v, type, sv, "v");
+        const int64_t ph[1] = {H}, n1[1] = {N}, tn[2] = {T, N};
+        pg = flat<float>(&g, at::kFloat, ph, "log_decay");
+        p0 = flat<float>(maybe(c.a[at], "s0"), at::kFloat, state, "s0");
+        reset = flat<uint8_t>(maybe(c.a[at + 1], "reset"), at::kByte, STEP ? at::IntArrayRef(n1) : at::IntArrayRef(tn), "reset");
+        lengths = flat<int32_t>(maybe(c.a[at + 2], "lengths"), at::kInt, n1, "lengths");
+    }
+};
+
+// q, k, v, log_decay, scale, s0, reset, lengths, out, want_last, s_last
+template <bool STEP>
+PyObject *decay(const Call &c) {
+    const Decay<STEP> d(c, 5);
+    const float scale = (float)c.number(4);
+    at::Tensor made, made_last;
+    const at::Tensor *out = maybe(c.a[8], "out"), *last = maybe(c.a[10], "s_last");
+    if (!out) out = &(made = c.fresh(d.sv, d.type));
+    const wm_seq_heads vo = heads(*out, d.type, d.sv, "out");
+    if (!last && c.yes(9)) last = &(made_last = c.fresh(d.state, at::kFloat));
+    float *pe = flat<float>(last, at::kFloat, d.state, "s_last");
+    void *s = c.stream();
+    c.run([&] { return wm_seq_decay_attention(c.h, d.dt, d.T, d.N, d.H, d.Dk, d.Dv, &d.vq, &d.vk, &d.vv, d.pg, scale, d.p0, d.reset, d.lengths, &vo, pe, s); });
+    return tuple({give(c.a[8], made), last ? give(c.a[10], made_last) : none()});
+}
+
+// q, k, v, log_decay, scale, s0, reset, lengths, dout, ds_last, dq, dk, dv, want_ds0, ds0
+PyObject *decay_backward(const Call &c) {
+    const Decay<false> d(c, 5);
+    const float scale = (float)c.number(4);
+    const wm_seq_heads vd = heads(tensor(c.a[8], "dout"), d.type, d.sv, "dout");
+    const float *pl = flat<float>(maybe(c.a[9], "ds_last"), at::kFloat, d.state, "ds_last");
+    const at::Tensor *g[3] = {maybe(c.a[10], "dq"), maybe(c.a[11], "dk"), maybe(c.a[12], "dv")}, *ds0 = maybe(c.a[14], "ds0");
+    const char *const names[3] = {"dq", "dk", "dv"};
+    at::Tensor made[3], made0;
+    wm_seq_heads vg[3];
+    for (int i = 0; i < 3; ++i) {
+        const auto &shape = i == 2 ? d.sv : d.sk;
+        if (!g[i]) g[i] = &(made[i] = c.fresh(shape, d.type));
+        vg[i] = heads(*g[i], d.type, shape, names[i]);
+    }
+    if (!ds0 && c.yes(13)) ds0 = &(made0 = c.fresh(d.state, at::kFloat));
+    float *p0 = flat<float>(ds0, at::kFloat, d.state, "ds0");
+    void *s = c.stream();
+    c.run([&] {
+        return wm_seq_decay_attention_backward(c.h, d.dt, d.T, d.N, d.H, d.Dk, d.Dv, &d.vq, &d.vk, &d.vv, d.pg, scale, d.p0, d.reset, d.lengths, &vd, pl,
+                                               &vg[0], &vg[1], &vg[2], p0, s);
+    });
+    return tuple({give(c.a[10], made[0]), give(c.a[11], made[1]), give(c.a[12], made[2]), ds0 ? give(c.a[14], made0) : none()});
+}
+
 PyObject *clip(const Call &c) {
     struct Ref {
         PyObject *o;
@@ -384,6 +546,11 @@ PyMethodDef g_methods[] = {
     SEQ_ENTRY("gated_scan", scan<false>, 8),
     SEQ_ENTRY("gated_step", scan<true>, 8),
     SEQ_ENTRY("gated_scan_backward", scan_backward, 12),
+    SEQ_ENTRY("head_norm", head_norm<false>, 10),
+    SEQ_ENTRY("head_norm_backward", head_norm<true>, 13),
+    SEQ_ENTRY("decay_attention", decay<false>, 11),
+    SEQ_ENTRY("decay_step", decay<true>, 11),
+    SEQ_ENTRY("decay_attention_backward", decay_backward, 15),
     SEQ_ENTRY("clip_grads", clip, 3),
     {"set_error", set_error, METH_O, nullptr},
     {nullptr, nullptr, 0, nullptr},

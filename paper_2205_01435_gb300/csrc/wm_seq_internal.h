@@ -48,6 +48,31 @@ struct seq_scan_args {
     float *h_last, *dh0;
 };
 
+struct seq_heads_args {
+    int dtype;
+    long long T;
+    int N, D, rotary, interleaved;
+    int heads[2];  // of queries and of keys
+    wm_seq_heads x[2], dy[2], out[2];
+    const float *weight[2];
+    float *dweight[2];
+    float eps;
+    const int32_t *positions;
+    const float *freqs;
+};
+
+struct seq_decay_args {
+    int dtype;
+    long long T;
+    int N, H, Dk, Dv;
+    wm_seq_heads q, k, v, o, dout, dq, dk, dv;  // forward: o out; backward: dq, dk, dv out
+    const float *log_decay, *s0, *ds_last;
+    float scale;
+    const uint8_t *reset;
+    const int32_t *lengths;
+    float *s_last, *ds0;
+};
+
 // What the launchers ask the device for, once a handle.
 cudaError_t wm_seq_embed_prepare(wm_seq *h);
 cudaError_t wm_seq_clip_prepare(wm_seq *h);
@@ -71,6 +96,12 @@ cudaError_t wm_seq_embed_launch(wm_seq *h, int dtype, long long n, int V, int D,
 size_t wm_seq_embed_backward_ws(const wm_seq *h, int dtype, long long n, int V, int D, const void *dout, const void *dtable);
 cudaError_t wm_seq_embed_backward_launch(wm_seq *h, int dtype, long long n, int V, int D, const int32_t *tokens,
                                          const void *dout, float scale, void *dtable, cudaStream_t s);
+
+size_t wm_seq_heads_backward_ws(const wm_seq *h, const seq_heads_args &a);
+cudaError_t wm_seq_heads_launch(wm_seq *h, const seq_heads_args &a, bool backward, cudaStream_t s);
+
+size_t wm_seq_decay_ws(const wm_seq *h, const seq_decay_args &a, bool backward);
+cudaError_t wm_seq_decay_launch(wm_seq *h, const seq_decay_args &a, bool backward, cudaStream_t s);
 
 size_t wm_seq_clip_ws(const wm_seq *h);
 cudaError_t wm_seq_clip_launch(wm_seq *h, int count, const wm_seq_grad *grads, float max_norm, float *norm,

@@ -16,6 +16,9 @@ and the ``_backward`` methods are called by hand.
     y, mean, rstd = ops.layer_norm(e, weight, bias, want_stats=True)
     h, state = ops.gated_scan(gate, x, h0=state, reset=starts, lengths=lengths)
     dgate, dx, dh0 = ops.gated_scan_backward(gate, x, h, dh, h0=state)
+    q, k = ops.head_norm(q, k, q_weight, k_weight, positions=positions, freqs=freqs)
+    o, state = ops.decay_attention(q, k, v, log_decay, scale=0.125, s0=state, reset=starts)
+    dq, dk, dv, ds0 = ops.decay_attention_backward(q, k, v, log_decay, do, scale=0.125, s0=state)
     norm = ops.clip_grads(grads, max_norm=1.0)
     ops.sync()                               # raises WMError on a device-side error
 """
@@ -50,6 +53,10 @@ def _declare():
         "wm_seq_layer_norm_backward": [P, I, L, I, P, L, P, P, P, P, L, P, L, P, P, P],
         "wm_seq_gated_scan": [P, I, L, I, I, V, V, P, P, P, V, P, P],
         "wm_seq_gated_scan_backward": [P, I, L, I, I, V, V, P, P, P, V, V, P, V, V, P, P],
+        "wm_seq_head_norm": [P, I, L, I, I, I, I, I, V, P, I, V, P, F, P, P, V, V, P],
+        "wm_seq_head_norm_backward": [P, I, L, I, I, I, I, I, V, P, V, I, V, P, V, F, P, P, V, V, P, P, P],
+        "wm_seq_decay_attention": [P, I, L, I, I, I, I, V, V, V, P, F, P, P, P, V, P, P],
+        "wm_seq_decay_attention_backward": [P, I, L, I, I, I, I, V, V, V, P, F, P, P, P, V, P, V, V, V, P, P],
         "wm_seq_clip": [P, I, P, F, P, P],
     }
     for name, args in sig.items():
@@ -165,6 +172,51 @@ class SequenceOps:
             return self._elsewhere(stream, self.gated_scan_backward, gate, x, h, dh, dh_last, h0, reset, lengths, dgate, dx,
                                    want_dh0, None, dh0)
         return _ext.gated_scan_backward(self.h, self._index, gate, x, h, dh, dh_last, h0, reset, lengths, dgate, dx, want_dh0, dh0)
+
+    # ------------------------------------------------------------- head norm
+    def head_norm(self, q, k=None, q_weight=None, k_weight=None, positions=None, freqs=None, eps: float = 1e-6,
+                  interleaved: bool = False, q_out=None, k_out=None, stream=None):
+        """wm_seq_head_norm of queries [T, N, heads, D] (or [N, heads, D], one step) and keys, which may have another number
+        of heads: (q', k'), or q' without keys.  Without positions and freqs nothing is rotated; len(freqs) is half of the
+        rotated values.  q_out may be q, and k_out k."""
+        if stream is not None:
+            return self._elsewhere(stream, self.head_norm, q, k, q_weight, k_weight, positions, freqs, eps, interleaved, q_out, k_out)
+        return _ext.head_norm(self.h, self._index, q, k, q_weight, k_weight, positions, freqs, eps, interleaved, q_out, k_out)
+
+    def head_norm_backward(self, q, dq_out, k=None, dk_out=None, q_weight=None, k_weight=None, positions=None, freqs=None,
+                           eps: float = 1e-6, interleaved: bool = False, dq=None, dk=None, want_params: bool = True, stream=None):
+        """wm_seq_head_norm_backward: (dq, dk, dq_weight, dk_weight), those of the keys None without keys, the weights' None
+        without want_params.  dq may be dq_out, and dk dk_out."""
+        if stream is not None:
+            return self._elsewhere(stream, self.head_norm_backward, q, dq_out, k, dk_out, q_weight, k_weight, positions, freqs, eps,
+                                   interleaved, dq, dk, want_params)
+        return _ext.head_norm_backward(self.h, self._index, q, k, q_weight, k_weight, positions, freqs, eps, interleaved, dq, dk,
+                                       dq_out, dk_out, want_params)
+
+    # ------------------------------------------------------------- decayed attention
+    def decay_attention(self, q, k, v, log_decay, scale: float = 1.0, s0=None, reset=None, lengths=None, out=None,
+                        want_last: bool = True, s_last=None, stream=None):
+        """wm_seq_decay_attention over q, k [T, N, heads, Dk] and v [T, N, heads, Dv]: (o, s_last).  The arrays may be strided over
+        T, N and heads; s_last may be s0."""
+        if stream is not None:
+            return self._elsewhere(stream, self.decay_attention, q, k, v, log_decay, scale, s0, reset, lengths, out, want_last, s_last)
+        return _ext.decay_attention(self.h, self._index, q, k, v, log_decay, scale, s0, reset, lengths, out, want_last, s_last)
+
+    def decay_step(self, q, k, v, log_decay, state, scale: float = 1.0, reset=None, out=None, out_state=None, stream=None):
+        """One token of N sequences: q, k [N, heads, Dk], v [N, heads, Dv] and the state [N, heads, Dk, Dv] fp32 (or None) give
+        (o, state').  out_state may be the state itself."""
+        if stream is not None:
+            return self._elsewhere(stream, self.decay_step, q, k, v, log_decay, state, scale, reset, out, out_state)
+        return _ext.decay_step(self.h, self._index, q, k, v, log_decay, scale, state, reset, None, out, True, out_state)
+
+    def decay_attention_backward(self, q, k, v, log_decay, dout, scale: float = 1.0, ds_last=None, s0=None, reset=None, lengths=None,
+                                 dq=None, dk=None, dv=None, want_ds0: bool = True, ds0=None, stream=None):
+        """wm_seq_decay_attention_backward: (dq, dk, dv, ds0); each may be given, ds0 may be ds_last."""
+        if stream is not None:
+            return self._elsewhere(stream, self.decay_attention_backward, q, k, v, log_decay, dout, scale, ds_last, s0, reset, lengths,
+                                   dq, dk, dv, want_ds0, ds0)
+        return _ext.decay_attention_backward(self.h, self._index, q, k, v, log_decay, scale, s0, reset, lengths, dout, ds_last, dq, dk,
+                                             dv, want_ds0, ds0)
 
     # ------------------------------------------------------------- clipping
     def clip_grads(self, grads, max_norm: float, out=None, stream=None):
