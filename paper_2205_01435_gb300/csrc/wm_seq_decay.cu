@@ -80,10 +80,8 @@ __device__ __forceinline__ bool load_rows(float *dst, int ld, const decay_array 
 }
 
 template <class T, bool STATE>
-__global__ void __launch_bounds__(kThreads, 2) decay_chunk_kernel(const decay_pass p) {
-    extern __shared__ __align__(16) float smem[];
-    __shared__ unsigned cuts[2];  // the chunk's tokens that begin something new
-    int job = 0, slice = blockIdx.x;
+__device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, float *smem, unsigned (&cuts)[2]) {
+    int job = 0, slice = item;
     long long pair = 0;
     {
         int per = 0, before[3];
@@ -98,7 +96,8 @@ __global__ void __launch_bounds__(kThreads, 2) decay_chunk_kernel(const decay_pa
         slice -= before[job];
     }
     const decay_job &j = p.job[job];
-    if (p.only_redo && !p.redo[job * (long long)p.N * p.H + pair]) return;
+    if (p.only_redo && !p.redo[1 + job * (long long)p.N * p.H + pair]) return;
+    __syncthreads();  // (an item before this one is done with the shared memory)
     const int n = (int)(pair / p.H), head = (int)(pair % p.H), span = blockIdx.y, da = j.da, dp = (da + 3) / 4 * 4;
     const int col0 = slice * kSlice, cols = min(kSlice, j.dc - col0), colp = (cols + 3) / 4 * 4;
     const ChunkTiles m(smem, da);
@@ -283,6 +282,14 @@ __global__ void __launch_bounds__(kThreads, 2) decay_chunk_kernel(const decay_pa
             const int r = i / cols, c = i - r * cols;
             to[(long long)r * j.dc + col0 + c] = empty ? 0.f : m.x[r * kSlice + c];
         }
+}
+
+template <class T, bool STATE>
+__global__ void __launch_bounds__(kThreads, 2) decay_chunk_kernel(const decay_pass p, int items) {
+    extern __shared__ __align__(16) float smem[];
+    __shared__ unsigned cuts[2];  // the chunk's tokens that begin something new
+    if (p.only_redo && *p.redo == 0) return;
+    for (long long i = blockIdx.x; i < items; i += gridDim.x) decay_chunks<T, STATE>(p, (int)i, smem, cuts);
 }
 
 // Spans' own parts -> what enters each span, along time.  A thread takes one cell of a state; jobs that form the spans.
@@ -471,14 +478,15 @@ decay_pass pass_of(const wm_seq *h, const seq_decay_args &a, bool backward) {
 
 int slices_of(int dc) { return (dc + kSlice - 1) / kSlice; }
 
-// Few sequences are cut in time so that every SM has two CTAs, into spans of at least 4 chunks: with fewer the two reads of
-// keys and values that forming the states takes cost more than the SMs they would fill.
-void split(const wm_seq *h, decay_pass &p, int chunk) {
+// Few sequences are cut in time so that every SM has the CTAs it can hold, into spans of at least 4 chunks: with fewer the two
+// reads of keys and values that forming the states takes cost more than the SMs they would fill.
+void split(const wm_seq *h, decay_pass &p, const seq_decay_args &a, bool tc) {
     long long ctas = 0;
-    for (int i = 0; i < p.jobs; ++i) ctas += slices_of(p.job[i].dc);
+    for (int i = 0; i < p.jobs; ++i) ctas += tc ? 1 : slices_of(p.job[i].dc);
     ctas *= (long long)p.N * p.H;
+    const int chunk = tc ? kDecayTcChunk : kChunk, room = h->sms * (tc ? wm_seq_decay_tc_ctas(a.Dk, a.Dv) : 2);
     const long long chunks = (p.T + chunk - 1) / chunk;
-    long long spans = std::max(1ll, std::min({2ll * h->sms / std::max(1ll, ctas), chunks / 4, 65535ll}));
+    const long long spans = std::max(1ll, std::min({room / std::max(1ll, ctas), chunks / 4, 65535ll}));
     const long long per = std::max(1ll, (chunks + spans - 1) / spans);
     p.span_tokens = per * chunk;
     p.spans = (int)std::max(1ll, (chunks + per - 1) / per);
@@ -486,10 +494,15 @@ void split(const wm_seq *h, decay_pass &p, int chunk) {
 
 bool steps_take(const seq_decay_args &a, bool backward) { return !backward && a.T <= 8; }
 
-// Scratch of a pass: the spans' states and carries; a copy of ds_last where ds0 takes its place (two jobs read it, one writes).
+// Scratch of a pass: the spans' states and carries, the marks of what is taken again, a copy of an entering state whose place
+// the leaving one takes.
 struct Scratch {
-    size_t spans[3] = {}, carry = 0, copy = 0, bytes = 0;
-    Scratch(const decay_pass &p, const seq_decay_args &a) {
+    size_t spans[3] = {}, carry = 0, copy = 0, redo = 0, bytes = 0;
+    // (the gradients: two jobs read ds_last, one writes ds0; tensor cores: a sequence may be taken again from s0)
+    static bool copies(const seq_decay_args &a, bool backward, bool tc) {
+        return backward ? a.ds0 && a.ds0 == a.ds_last : tc && a.s_last && a.s_last == a.s0;
+    }
+    Scratch(const decay_pass &p, const seq_decay_args &a, bool backward, bool tc) {
         const auto take = [&](size_t n) {
             const size_t at = bytes;
             bytes += (n + 255) / 256 * 256;
@@ -501,7 +514,8 @@ struct Scratch {
                 if (!p.job[i].spans_t) spans[i] = take(pairs * p.spans * p.job[i].da * p.job[i].dc * 4);
             carry = take(pairs * p.spans * 2 * 4);
         }
-        if (p.jobs > 1 && a.ds0 && a.ds0 == a.ds_last) copy = take(pairs * a.Dk * a.Dv * 4);
+        if (copies(a, backward, tc)) copy = take(pairs * a.Dk * a.Dv * 4);
+        if (tc) redo = take((1 + p.jobs * pairs) * 4);
     }
 };
 
@@ -533,41 +547,58 @@ cudaError_t steps(wm_seq *h, const seq_decay_args &a, cudaStream_t s) {
     return run_steps<T, 16>(h, p, s);
 }
 
-template <class T>
-cudaError_t chunks(wm_seq *h, const decay_pass &p, cudaStream_t s) {
-    const long long pairs = (long long)p.N * p.H;
-    int da = 0, out = 0, state = 0;
-    for (int i = 0; i < p.jobs; ++i) {
-        da = std::max(da, p.job[i].da);
-        out += slices_of(p.job[i].dc);
-        state += p.job[i].spans_t ? 0 : slices_of(p.job[i].dc);
-    }
+int items_of(const decay_pass &p, bool state) {
+    int n = 0;
+    for (int i = 0; i < p.jobs; ++i) n += state && p.job[i].spans_t ? 0 : slices_of(p.job[i].dc);
+    return (int)((long long)p.N * p.H * n);
+}
+
+template <class T, bool STATE>
+cudaError_t chunk_launch(wm_seq *h, const decay_pass &p, cudaStream_t s) {
+    int da = 0;
+    for (int i = 0; i < p.jobs; ++i) da = std::max(da, p.job[i].da);
     const size_t bytes = ChunkTiles::bytes(da);
-    cudaError_t e = cudaFuncSetAttribute(decay_chunk_kernel<T, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    const cudaError_t e = cudaFuncSetAttribute(decay_chunk_kernel<T, STATE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
     if (e != cudaSuccess) return e;
-    if (p.spans > 1) {
-        e = cudaFuncSetAttribute(decay_chunk_kernel<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-        if (e != cudaSuccess) return e;
-        decay_chunk_kernel<T, true><<<dim3((unsigned)(pairs * state), p.spans), kThreads, bytes, s>>>(p);
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
-        long long cells = 0;
-        for (int i = 0; i < p.jobs; ++i) cells = std::max(cells, pairs * p.job[i].da * p.job[i].dc);
-        decay_join_kernel<<<dim3((unsigned)((cells + 255) / 256), p.jobs), 256, 0, s>>>(p);
-        if ((e = cudaGetLastError()) != cudaSuccess) return e;
-        h->last_launches += 2;
-    }
+    const int items = items_of(p, STATE);
     ++h->last_launches;
-    decay_chunk_kernel<T, false><<<dim3((unsigned)(pairs * out), p.spans), kThreads, bytes, s>>>(p);
+    decay_chunk_kernel<T, STATE><<<dim3((unsigned)(p.only_redo ? std::min(items, h->sms) : items), p.spans), kThreads, bytes, s>>>(p, items);
     return cudaGetLastError();
 }
+
+// The pass, on tensor cores or in fp32; in spans, what each gives the state and the joins first.
+template <class T>
+cudaError_t run_pass(wm_seq *h, decay_pass &p, bool tc, cudaStream_t s) {
+    const long long pairs = (long long)p.N * p.H;
+    cudaError_t e;
+    if (tc && (e = cudaMemsetAsync(p.redo, 0, (size_t)(1 + p.jobs * pairs) * 4, s)) != cudaSuccess) return e;
+    if (p.spans > 1) {
+        e = tc ? wm_seq_decay_tc_launch(h, p, true, s) : chunk_launch<T, true>(h, p, s);
+        if (e != cudaSuccess) return e;
+        long long cells = 0;
+        for (int i = 0; i < p.jobs; ++i) cells = std::max(cells, pairs * p.job[i].da * p.job[i].dc);
+        ++h->last_launches;
+        decay_join_kernel<<<dim3((unsigned)((cells + 255) / 256), p.jobs), 256, 0, s>>>(p);
+        if ((e = cudaGetLastError()) != cudaSuccess) return e;
+    }
+    if (!tc) return chunk_launch<T, false>(h, p, s);
+    if ((e = wm_seq_decay_tc_launch(h, p, false, s)) != cudaSuccess) return e;
+    p.only_redo = 1;
+    p.spans = 1;
+    p.span_tokens = (p.T + kChunk - 1) / kChunk * kChunk;
+    return chunk_launch<T, false>(h, p, s);
+}
+
+// Tensor cores: bf16, heads of up to 128 values, and more tokens than go one by one.
+bool tc_takes(const seq_decay_args &a) { return a.dtype == WM_BF16 && a.Dk <= kDecayTcMost && a.Dv <= kDecayTcMost; }
 
 }  // namespace
 
 size_t wm_seq_decay_ws(const wm_seq *h, const seq_decay_args &a, bool backward) {
     if (a.T == 0 || steps_take(a, backward)) return 0;
     decay_pass p = pass_of(h, a, backward);
-    split(h, p, kChunk);
-    return Scratch(p, a).bytes;
+    split(h, p, a, tc_takes(a));
+    return Scratch(p, a, backward, tc_takes(a)).bytes;
 }
 
 cudaError_t wm_seq_decay_launch(wm_seq *h, const seq_decay_args &a, bool backward, cudaStream_t s) {
@@ -580,18 +611,21 @@ cudaError_t wm_seq_decay_launch(wm_seq *h, const seq_decay_args &a, bool backwar
         return from ? cudaMemcpyAsync(to, from, state, cudaMemcpyDeviceToDevice, s) : cudaMemsetAsync(to, 0, state, s);
     }
     if (steps_take(a, backward)) return a.dtype == WM_BF16 ? steps<__nv_bfloat16>(h, a, s) : steps<float>(h, a, s);
+    const bool tc = tc_takes(a);
     decay_pass p = pass_of(h, a, backward);
-    split(h, p, kChunk);
-    const Scratch w(p, a);
+    split(h, p, a, tc);
+    const Scratch w(p, a, backward, tc);
     unsigned char *ws = static_cast<unsigned char *>(h->ws);
     for (int i = 0; i < p.jobs; ++i)
         if (p.spans > 1) p.job[i].spans = reinterpret_cast<float *>(ws + w.spans[p.job[i].spans_t ? 1 : i]);
     p.carry = reinterpret_cast<float *>(ws + w.carry);
-    if (backward && a.ds0 && a.ds0 == a.ds_last) {
+    p.redo = reinterpret_cast<int *>(ws + w.redo);
+    if (Scratch::copies(a, backward, tc)) {
         float *copy = reinterpret_cast<float *>(ws + w.copy);
-        const cudaError_t e = cudaMemcpyAsync(copy, a.ds_last, state, cudaMemcpyDeviceToDevice, s);
+        const cudaError_t e = cudaMemcpyAsync(copy, backward ? a.ds_last : a.s0, state, cudaMemcpyDeviceToDevice, s);
         if (e != cudaSuccess) return e;
-        p.job[1].s_in = p.job[2].s_in = copy;
+        (backward ? p.job[1].s_in : p.job[0].s_in) = copy;
+        if (backward) p.job[2].s_in = copy;
     }
-    return a.dtype == WM_BF16 ? chunks<__nv_bfloat16>(h, p, s) : chunks<float>(h, p, s);
+    return a.dtype == WM_BF16 ? run_pass<__nv_bfloat16>(h, p, tc, s) : run_pass<float>(h, p, tc, s);
 }

@@ -39,16 +39,24 @@ struct decay_pass {
     float *carry;            // [spans][2][N, H]: what a span multiplies the state by, by direction
     int spans;               // of each sequence
     long long span_tokens;   // a multiple of the chunk
-    int *redo;               // [jobs][N, H]: a chunk met what is not finite (tensor-core pass)
+    int *redo;               // tensor-core pass: how many marks, then [jobs][N, H] marks: a chunk met what is not finite
     int only_redo;           // work on those alone
 };
 
-// Tensor-core pass in bf16 (wm_seq_decay_tc.cu).
-bool wm_seq_decay_tc_takes(const seq_decay_args &a);
+// The tensor-core pass in bf16 (wm_seq_decay_tc.cu): its launch (state: only what the spans' tokens give the state), and the
+// CTAs an SM holds.
+constexpr int kDecayTcChunk = 128, kDecayTcMost = 128;  // tokens; values of a head
+cudaError_t wm_seq_decay_tc_launch(wm_seq *h, const decay_pass &p, bool state, cudaStream_t s);
+int wm_seq_decay_tc_ctas(int Dk, int Dv);
 
 #ifdef __CUDACC__
 // lambda^n: 1 for n = 0 whatever lambda is.
 __device__ __forceinline__ float decay_power(float log_decay, long long n) { return n <= 0 ? 1.f : expf((float)n * log_decay); }
+
+// Marks a job of a head of a sequence to be taken again.
+__device__ __forceinline__ void decay_mark(const decay_pass &p, int job, long long pair) {
+    if (atomicExch(p.redo + 1 + job * (long long)p.N * p.H + pair, 1) == 0) atomicAdd(p.redo, 1);
+}
 
 // A sequence as a pass sees it: step s of it is token at(s); steps from len on are padding.
 struct decay_seq {
