@@ -53,7 +53,7 @@ struct Plan {
     // (b's tiles and lo are read as operands 128 values wide: with D = 64 the second half is what lies behind them, and unused)
     static constexpr int xb = 0, lo = xb + D * 128 * (D / 64), b = lo + tile, a = b + 2 * tile, c = a + 2 * tile, end = c + tile;
     static constexpr int small = end;  // tables and barriers
-    static constexpr int bytes = small + 4 * (132 + 128) + 64 + 64 + 1024;
+    static constexpr int bytes = small + 4 * 132 + 8 * 128 + 48 + 32 + 1024;
     // P lies over A's first columns; with D = 64 O2 over A's others
     static constexpr int tA = 0, tO1 = 128, tO2 = D == 64 ? 64 : 256, tX = D == 64 ? 192 : 384, columns = D == 64 ? 256 : 512;
 };
@@ -85,23 +85,57 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&v);
 }
-__device__ __forceinline__ float low(uint32_t v) { return __uint_as_float(v << 16); }
-__device__ __forceinline__ float high(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+// Two fp32 values at a time.
+union Pair {
+    unsigned long long u;
+    float2 f;
+};
+__device__ __forceinline__ Pair pair_of(uint32_t a, uint32_t b) {
+    Pair p;
+    p.f = make_float2(__uint_as_float(a), __uint_as_float(b));
+    return p;
+}
+__device__ __forceinline__ Pair twice(float v) {
+    Pair p;
+    p.f = make_float2(v, v);
+    return p;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u));
+    return r;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.u) : "l"(a.u), "l"(b.u), "l"(c.u));
+    return r;
+}
+// Two bf16 values at a time.
+__device__ __forceinline__ uint32_t hmul(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t hfma(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
 
 // 128 tokens of an array as swizzled panels.  `at` is the first token's row, step the elements to the next one; rows and values
-// that are not there are zeros.  16-byte copies where vec > 1.
-template <int D>
-__device__ __forceinline__ void load_tile(uint32_t dst, const bf16 *at, long long step, int rows, int dim, int vec) {
+// that are not there are zeros.  VEC: 16-byte copies.
+template <int D, bool VEC>
+__device__ __forceinline__ void load_tile(uint32_t dst, const bf16 *at, long long step, int rows, int dim) {
     constexpr int per = D / 8, stride = kThreads / per;
     const int ch = threadIdx.x % per, row0 = threadIdx.x / per, left = dim - ch * 8;
     const bf16 *p = at + row0 * step + ch * 8;
+    const uint32_t to = dst + (ch / 8) * kPanel + row0 * 128 + (((ch & 7) ^ (row0 & 7)) << 4);  // (stride is a multiple of 8)
+    if (left <= 0) rows = 0;
 #pragma unroll
     for (int k = 0; k < kChunk / stride; ++k) {
-        const int row = row0 + k * stride;
-        const uint32_t to = dst + (ch / 8) * kPanel + row * 128 + (((ch & 7) ^ (row & 7)) << 4);
-        const bool on = row < rows && left > 0;
-        if (vec > 1) {
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(on ? p : at), "r"(on ? 16 : 0) : "memory");
+        const bool on = row0 + k * stride < rows;
+        if constexpr (VEC) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + k * stride * 128), "l"(on ? p : at), "r"(on ? 16 : 0) : "memory");
         } else {
             uint32_t v[4] = {};
             const unsigned short *u = reinterpret_cast<const unsigned short *>(p);
@@ -110,24 +144,25 @@ __device__ __forceinline__ void load_tile(uint32_t dst, const bf16 *at, long lon
                 for (int h = 0; h < 8; ++h)
                     if (h < left) v[h / 2] |= (uint32_t)u[h] << (16 * (h & 1));
             }
-            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to + k * stride * 128), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
         }
         p += stride * step;
     }
 }
 
-template <int D, bool STATE>
+// VEC: 16-byte accesses; CUT: there may be resets.
+template <int D, bool STATE, bool VEC, bool CUT>
 __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(const decay_pass p) {
     using L = Plan<D>;
     extern __shared__ unsigned char raw[];
     unsigned char *smem = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
     const uint32_t base = tc::smem_u32(smem);
     float *const power = reinterpret_cast<float *>(smem + L::small);        // lambda^0 .. lambda^128
-    float *const kept = power + 132;                                        // the tokens' weights in the next state
+    uint2 *const kept = reinterpret_cast<uint2 *>(power + 132);             // the tokens' weights in the next state: two bf16, each twice
     uint32_t *const cuts = reinterpret_cast<uint32_t *>(kept + 128);        // [2][4]: tokens that begin something new
     int *const late = reinterpret_cast<int *>(cuts + 8);                    // a wait gave up
     uint32_t *const tmem_at = cuts + 9;
-    const uint32_t bars = base + L::small + 4 * (132 + 128) + 64, barA = bars, barO = bars + 8, barX = bars + 16;
+    const uint32_t bars = tc::smem_u32(cuts + 12), barA = bars, barO = bars + 8, barX = bars + 16;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quad = warp & 3, wg = warp >> 2;
     int jobs = 0, at[3] = {};
@@ -152,20 +187,20 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
         if (c < chunks) {
             const long long s0 = first + (long long)c * kChunk;
             const int rows = (int)min((long long)kChunk, stop - s0), slot = c & 1;
-            load_tile<D>(base + L::b + slot * L::tile, pb + q.at(s0) * j.b.t, dir * j.b.t, rows, da, j.vec);
-            if constexpr (!STATE) load_tile<D>(base + L::a + slot * L::tile, pa + q.at(s0) * j.a.t, dir * j.a.t, rows, da, j.vec);
+            load_tile<D, VEC>(base + L::b + slot * L::tile, pb + q.at(s0) * j.b.t, dir * j.b.t, rows, da);
+            if constexpr (!STATE) load_tile<D, VEC>(base + L::a + slot * L::tile, pa + q.at(s0) * j.a.t, dir * j.a.t, rows, da);
         }
         copy_commit();
     };
     const auto load_c = [&](int c) {
         if (c < chunks) {
             const long long s0 = first + (long long)c * kChunk;
-            load_tile<D>(base + L::c, pc + q.at(s0) * j.c.t, dir * j.c.t, (int)min((long long)kChunk, stop - s0), dc, j.vec);
+            load_tile<D, VEC>(base + L::c, pc + q.at(s0) * j.c.t, dir * j.c.t, (int)min((long long)kChunk, stop - s0), dc);
         }
         copy_commit();
     };
     const auto find_cuts = [&](int c) {
-        if (p.reset && warp < 4) {
+        if (CUT && warp < 4) {
             const int r = warp * 32 + lane;
             const long long s = first + (long long)c * kChunk + r;
             const unsigned m = __ballot_sync(~0u, c < chunks && s < stop && decay_cut(p, q, s, n));
@@ -197,7 +232,9 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
         tc::fence_after_sync();
     };
 
-    // the entering state: fp32, row a thread's lane, half of the columns a warpgroup
+    // the entering state into TMEM: row a thread's lane, half of the columns a warpgroup
+    constexpr int W = D / 2;  // columns of X and of the outputs that a thread takes
+    const int xrow = quad * 32 + lane, col0 = wg * W;
     const float *from = nullptr;
     int from_t = 0;
     float mul = 1.f;
@@ -212,11 +249,26 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
         }
     }
     bool has_x = from != nullptr && chunks > 0;  // X is not 0
-    constexpr int W = D / 2;                     // columns of X and of the outputs that a thread takes
-    const int xrow = quad * 32 + lane, col0 = wg * W;
-    float odd = 0.f;                             // NaN once a value was not finite
-    bool keeps = true;                           // (STATE) no cut so far
+    if (has_x && quad * 32 < D) {
+#pragma unroll 1
+        for (int h = 0; h < W; h += 32) {
+            uint32_t r[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const int col = col0 + h + i;
+                float v = 0.f;
+                if (xrow < da && col < dc) v = from_t ? from[(long long)col * da + xrow] : from[(long long)xrow * dc + col];
+                r[i] = __float_as_uint(mul == 1.f ? v : v * mul);
+            }
+            __syncwarp();
+            TC_ST32(mine + L::tX + col0 + h, r);
+        }
+        tmem_st_wait();
+    }
+    uint32_t odd = 0;   // two bf16: NaN once an output was not finite
+    bool keeps = true;  // (STATE) no cut so far
 
+#pragma unroll 1
     for (int c = 0; c < chunks; ++c) {
         const long long s0 = first + (long long)c * kChunk;
         const int rows = (int)min((long long)kChunk, stop - s0), slot = c & 1;
@@ -234,54 +286,47 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
                                  tc::idesc_bf16_f32(128, 128), k > 0);
                 tc::mma_commit(barA);
             }
+            __syncwarp();
         }
         // tokens that begin something new: what a token sees begins with the last of them up to it
-        uint32_t cut[4] = {};
-        if (p.reset) {
+        int keep_from = -1, begin = -1;
+        bool any_cut = false;
+        if constexpr (CUT) {
+            uint32_t cut[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) cut[i] = cuts[slot * 4 + i];
-        }
-        const bool any_cut = (cut[0] | cut[1] | cut[2] | cut[3]) != 0;
-        const auto start = [&](int r) {
-            int b = -1;
+            any_cut = (cut[0] | cut[1] | cut[2] | cut[3]) != 0;
+            if (any_cut) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t m = r >= 32 * i + 31 ? cut[i] : r < 32 * i ? 0u : cut[i] & (~0u >> (31 - (r - 32 * i)));
-                if (m) b = 32 * i + 31 - __clz(m);
+                for (int i = 0; i < 4; ++i) {
+                    if (cut[i]) keep_from = 32 * i + 31 - __clz(cut[i]);  // (no cuts behind the last row)
+                    const uint32_t m = quad > i ? cut[i] : quad < i ? 0u : cut[i] & (~0u >> (31 - lane));
+                    if (m) begin = 32 * i + 31 - __clz(m);
+                }
             }
-            return b;
-        };
-        const int keep_from = any_cut ? start(rows - 1) : -1;
+        }
         // (time's order, the last token of all: the state leaves as that token wrote it)
         const int less = !STATE && j.first && s0 + rows == q.len ? 1 : 0;
-        if (tid < kChunk) {
+        if (tid < kChunk && (CUT || STATE || c == 0 || rows < kChunk || less)) {
             float w = 0.f;
             if (tid < rows && tid >= keep_from) {
                 if constexpr (STATE) w = decay_power(g, stop - s0 - tid);  // up to the span's end
                 else w = power[rows - tid - less];
             }
-            kept[tid] = j.up_scale * w;
+            w *= j.up_scale;
+            const float w1 = __bfloat162float(__float2bfloat16_rn(w));
+            kept[tid] = make_uint2(pack2(w1, w1), pack2(w - w1, w - w1));
         }
         if constexpr (!STATE) {
             // X -> Xb, and X to what the next state keeps of it
-            if (has_x && xrow < D) {
-                const float shrink = power[rows - less];
+            if (has_x && quad * 32 < D) {
+                const Pair shrink = twice(power[rows - less]);
 #pragma unroll
                 for (int h = 0; h < W; h += 32) {
                     uint32_t r[32];
                     const int col = col0 + h;
-                    if (c == 0) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            float v = 0.f;
-                            if (xrow < da && col + i < dc) v = from_t ? from[(long long)(col + i) * da + xrow] : from[(long long)xrow * dc + col + i];
-                            r[i] = __float_as_uint(mul == 1.f ? v : v * mul);
-                        }
-                    } else {
-                        TC_LD32(mine + L::tX + col, r);
-                        tc::tmem_ld_wait();
-                    }
-                    __syncwarp();
+                    TC_LD32(mine + L::tX + col, r);
+                    tc::tmem_ld_wait();
 #pragma unroll
                     for (int i = 0; i < 32; i += 8) {
                         const float *f = reinterpret_cast<const float *>(r + i);
@@ -289,23 +334,19 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
                         asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(pack2(f[0], f[1])), "r"(pack2(f[2], f[3])),
                                      "r"(pack2(f[4], f[5])), "r"(pack2(f[6], f[7])) : "memory");
                     }
-                    if (keep_from < 0) {
+                    if (!CUT || keep_from < 0) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const float v = __uint_as_float(r[i]);
-                            odd += v * 0.f;
-                            r[i] = __float_as_uint(v * shrink);
+                        for (int i = 0; i < 32; i += 2) {
+                            const Pair v = mul2(pair_of(r[i], r[i + 1]), shrink);
+                            r[i] = __float_as_uint(v.f.x);
+                            r[i + 1] = __float_as_uint(v.f.y);
                         }
                         TC_ST32(mine + L::tX + col, r);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) odd += __uint_as_float(r[i]) * 0.f;
                     }
                 }
                 tmem_st_wait();
             }
-            // A -> P: row r = xrow, 64 columns a warpgroup, in blocks of 32
-            const int r = xrow, begin = any_cut ? start(r) : -1;
+            // A -> P: row xrow, 64 columns a warpgroup, in blocks of 32
             wait(barA, c);
             uint32_t packed[32];
 #pragma unroll
@@ -319,27 +360,32 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
                 uint32_t v[32];
                 TC_LD32(mine + L::tA + j0, v);
                 tc::tmem_ld_wait();
-                float f[32];
                 if (block == quad) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) f[i] = i <= lane ? __uint_as_float(v[i]) * (j.w_scale * power[max(lane - i, 0)]) : 0.f;
-                } else {
-                    const float w = j.w_scale * power[r - j0 - 31];
+                    for (int i = 0; i < 32; ++i) {
+                        const float f = __uint_as_float(v[i]) * (j.w_scale * power[max(lane - i, 0)]);
+                        v[i] = i <= lane ? __float_as_uint(f) : 0u;
+                    }
+                } else {  // lambda^(xrow - j0 - 31) lambda^(31 - i): neither is above 1
+                    const Pair w = twice(j.w_scale * power[xrow - j0 - 31]);
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) {
-                        const float4 t = *reinterpret_cast<const float4 *>(power + 28 - i);  // lambda^(31 - i - ...): backwards
-                        f[i] = __uint_as_float(v[i]) * (w * t.w);
-                        f[i + 1] = __uint_as_float(v[i + 1]) * (w * t.z);
-                        f[i + 2] = __uint_as_float(v[i + 2]) * (w * t.y);
-                        f[i + 3] = __uint_as_float(v[i + 3]) * (w * t.x);
+                        const float4 t = *reinterpret_cast<const float4 *>(power + 28 - i);
+                        Pair t0, t1;
+                        t0.f = make_float2(t.w, t.z);
+                        t1.f = make_float2(t.y, t.x);
+                        t0 = mul2(pair_of(v[i], v[i + 1]), mul2(t0, w));
+                        t1 = mul2(pair_of(v[i + 2], v[i + 3]), mul2(t1, w));
+                        v[i] = __float_as_uint(t0.f.x), v[i + 1] = __float_as_uint(t0.f.y);
+                        v[i + 2] = __float_as_uint(t1.f.x), v[i + 3] = __float_as_uint(t1.f.y);
                     }
                 }
-                if (any_cut) {
+                if (CUT && any_cut) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) f[i] = j0 + i >= begin ? f[i] : 0.f;
+                    for (int i = 0; i < 32; ++i) v[i] = j0 + i >= begin ? v[i] : 0u;
                 }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) packed[h * 16 + i] = pack2(f[2 * i], f[2 * i + 1]);
+                for (int i = 0; i < 16; ++i) packed[h * 16 + i] = pack2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
             }
             tc::fence_proxy_async_smem();  // Xb
             tc::fence_before_sync();
@@ -353,31 +399,31 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
             }
             __syncwarp();
             TC_ST32(mine + L::tA + wg * 32, packed);
-            tmem_st_wait();
         } else {
             __syncthreads();  // kept
         }
-        // b -> b w as two bf16 values, the first in b's place
+        // b -> b w as two bf16 values, the first in b's place: with w = w1 + w2, hi = b w1 rounded, lo = (b w1 - hi) + b w2,
+        // where b w1 - hi is exact (16 bits of a product, the first 8 taken away)
         {
             constexpr int per = D / 8, stride = kThreads / per;
             const int ch = tid % per, row0 = tid / per;
+            const uint32_t off = (ch / 8) * kPanel + row0 * 128 + (((ch & 7) ^ (row0 & 7)) << 4);
 #pragma unroll
             for (int k = 0; k < kChunk / stride; ++k) {
-                const int row = row0 + k * stride;
-                const uint32_t off = (ch / 8) * kPanel + row * 128 + (((ch & 7) ^ (row & 7)) << 4);
+                const uint32_t to = off + k * stride * 128;
                 uint32_t v[4], hi[4], lo[4];
-                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(tb + off));
-                const float w = kept[row];
+                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(tb + to));
+                const uint2 w = kept[row0 + k * stride];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float x = low(v[i]) * w, y = high(v[i]) * w;
-                    hi[i] = pack2(x, y);
-                    lo[i] = pack2(x - low(hi[i]), y - high(hi[i]));
+                    hi[i] = hmul(v[i], w.x);
+                    lo[i] = hfma(v[i], w.y, hfma(v[i], w.x, hi[i] ^ 0x80008000u));
                 }
-                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(tb + off), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
-                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(base + L::lo + off), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
+                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(tb + to), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
+                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(base + L::lo + to), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
             }
         }
+        if constexpr (!STATE) tmem_st_wait();
         copy_wait<1>();
         tc::fence_proxy_async_smem();
         tc::fence_before_sync();
@@ -404,11 +450,10 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
         find_cuts(c + 1);
         if constexpr (!STATE) {
             // y = O1 + in_scale lambda^r O2
-            const int r = xrow, begin = any_cut ? start(r) : -1;
-            const float w = j.in_scale * power[r];
-            const bool sees = has_x && begin < 0;
+            const Pair w = twice(j.in_scale * power[xrow]);
+            const bool sees = !CUT || begin < 0;
+            bf16 *const out = py + q.at(s0 + min(xrow, rows - 1)) * j.y.t + col0;
             wait(barO, c);
-            bf16 *const out = py + q.at(s0 + min(r, rows - 1)) * j.y.t + col0;
 #pragma unroll
             for (int h = 0; h < W; h += 32) {
                 uint32_t o1[32];
@@ -420,26 +465,28 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
                     tc::tmem_ld_wait();
                     if (sees) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) o1[i] = __float_as_uint(__uint_as_float(o1[i]) + w * __uint_as_float(o2[i]));
+                        for (int i = 0; i < 32; i += 2) {
+                            const Pair v = fma2(pair_of(o2[i], o2[i + 1]), w, pair_of(o1[i], o1[i + 1]));
+                            o1[i] = __float_as_uint(v.f.x), o1[i + 1] = __float_as_uint(v.f.y);
+                        }
                     }
                 } else {
                     tc::tmem_ld_wait();
                 }
-                if (r < rows) {
+                if (xrow < rows) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) odd += __uint_as_float(o1[i]) * 0.f;
+                    for (int i = 0; i < 16; ++i) {
+                        o1[i] = pack2(__uint_as_float(o1[2 * i]), __uint_as_float(o1[2 * i + 1]));
+                        odd = hfma(o1[i], 0u, odd);
+                    }
+                    if constexpr (VEC) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 8) {
-                        const float *f = reinterpret_cast<const float *>(o1 + i);
-                        if (j.vec > 1) {
-                            if (col0 + h + i < dc)
-                                *reinterpret_cast<uint4 *>(out + h + i) =
-                                    make_uint4(pack2(f[0], f[1]), pack2(f[2], f[3]), pack2(f[4], f[5]), pack2(f[6], f[7]));
-                        } else {
+                        for (int i = 0; i < 16; i += 4)
+                            if (col0 + h + 2 * i < dc) *reinterpret_cast<uint4 *>(out + h + 2 * i) = make_uint4(o1[i], o1[i + 1], o1[i + 2], o1[i + 3]);
+                    } else {
 #pragma unroll
-                            for (int m = 0; m < 8; ++m)
-                                if (col0 + h + i + m < dc) out[h + i + m] = __float2bfloat16_rn(f[m]);
-                        }
+                        for (int i = 0; i < 32; ++i)
+                            if (col0 + h + i < dc) reinterpret_cast<unsigned short *>(out)[h + i] = (unsigned short)(o1[i / 2] >> (16 * (i & 1)));
                     }
                 }
             }
@@ -453,7 +500,12 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
     // outputs of padding
     if constexpr (!STATE) {
         const long long pad = max(first, min(q.len, last));
-        for (long long i = tid; i < (last - pad) * dc; i += kThreads) py[(pad + i / dc) * j.y.t + i % dc] = __float2bfloat16_rn(0.f);
+        const int per = VEC ? dc / 8 : dc, at_once = max(1, kThreads / per), r0 = tid / per, c0 = tid - r0 * per;
+        if (r0 < at_once)
+            for (long long r = pad + r0; r < last; r += at_once) {
+                if constexpr (VEC) *reinterpret_cast<uint4 *>(py + r * j.y.t + c0 * 8) = make_uint4(0, 0, 0, 0);
+                else py[r * j.y.t + c0] = __float2bfloat16_rn(0.f);
+            }
     }
     // what leaves: the span's part, or the state itself (of the span that holds the sequence's end)
     float *to = nullptr;
@@ -466,8 +518,9 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
         empty = j.out_zero && q.len > 0 && p.reset && p.reset[n] != 0;
     }
     if (chunks > 0) {
-        if (xrow < D) {
-#pragma unroll
+        bool bad = (odd & 0x7fff7fffu) != 0;  // (a product with 0 is 0 or NaN)
+        if (quad * 32 < D) {
+#pragma unroll 1
             for (int h = 0; h < W; h += 32) {
                 uint32_t r[32];
                 __syncwarp();
@@ -479,14 +532,14 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
                         const int col = col0 + h + i;
                         const float v = __uint_as_float(r[i]);
                         if (col < dc) {
-                            odd += v * 0.f;
+                            bad |= !(fabsf(v) <= 3.4028235e38f);
                             if (to) to[(long long)xrow * dc + col] = empty ? 0.f : v;
                         }
                     }
                 }
             }
         }
-        if (!(odd == 0.f)) {
+        if (bad) {
             decay_mark(p, job, pair);
             if constexpr (STATE)
                 for (int i = 0; i < p.jobs; ++i)  // (another job may read this state)
@@ -509,12 +562,19 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
 int wm_seq_decay_tc_ctas(int Dk, int Dv) { return Dk <= 64 && Dv <= 64 ? 2 : 1; }
 
 namespace {
+template <int D, bool STATE, bool VEC, bool CUT>
+cudaError_t launch(const decay_pass &p, unsigned grid, cudaStream_t s) {
+    const cudaError_t e = cudaFuncSetAttribute(decay_tc_kernel<D, STATE, VEC, CUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan<D>::bytes);
+    if (e != cudaSuccess) return e;
+    decay_tc_kernel<D, STATE, VEC, CUT><<<dim3(grid, p.spans), kThreads, Plan<D>::bytes, s>>>(p);
+    return cudaGetLastError();
+}
 template <int D, bool STATE>
 cudaError_t launch(const decay_pass &p, unsigned grid, cudaStream_t s) {
-    const cudaError_t e = cudaFuncSetAttribute(decay_tc_kernel<D, STATE>, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan<D>::bytes);
-    if (e != cudaSuccess) return e;
-    decay_tc_kernel<D, STATE><<<dim3(grid, p.spans), kThreads, Plan<D>::bytes, s>>>(p);
-    return cudaGetLastError();
+    bool vec = true;
+    for (int i = 0; i < p.jobs; ++i) vec = vec && p.job[i].vec > 1;
+    if (vec) return p.reset ? launch<D, STATE, true, true>(p, grid, s) : launch<D, STATE, true, false>(p, grid, s);
+    return p.reset ? launch<D, STATE, false, true>(p, grid, s) : launch<D, STATE, false, false>(p, grid, s);
 }
 }  // namespace
 
