@@ -436,9 +436,12 @@ decay_pass pass_of(const wm_seq *h, const seq_decay_args &a, bool backward) {
     p.log_decay = a.log_decay; p.reset = a.reset; p.lengths = a.lengths;
     p.status = h->status;
     const decay_array q = array_of(a.q), k = array_of(a.k), v = array_of(a.v), o = array_of(a.o), dout = array_of(a.dout);
-    const auto job = [&](const decay_array &x, const decay_array &y, const decay_array &z, const decay_array &out, int da, int dc) {
+    const decay_array in[4] = {q, k, v, dout};
+    const auto job = [&](int ia, int ib, int ic, const decay_array &out, int da, int dc) {
         decay_job j{};
+        const decay_array &x = in[ia], &y = in[ib], &z = in[ic];
         j.a = x; j.b = y; j.c = z; j.y = out;
+        j.map[0] = ia; j.map[1] = ib; j.map[2] = ic;
         j.da = da; j.dc = dc;
         j.w_scale = j.in_scale = a.scale;
         j.up_scale = 1.f;
@@ -448,25 +451,25 @@ decay_pass pass_of(const wm_seq *h, const seq_decay_args &a, bool backward) {
     };
     if (!backward) {
         p.jobs = 1;
-        decay_job &f = p.job[0] = job(q, k, v, o, a.Dk, a.Dv);
+        decay_job &f = p.job[0] = job(0, 1, 2, o, a.Dk, a.Dv);
         f.first = 1;
         f.s_in = a.s0;
         f.s_out = a.s_last;
         return p;
     }
     p.jobs = 3;
-    decay_job &dq = p.job[0] = job(dout, v, k, array_of(a.dq), a.Dv, a.Dk);
+    decay_job &dq = p.job[0] = job(3, 2, 1, array_of(a.dq), a.Dv, a.Dk);
     dq.first = 1;
     dq.s_in = a.s0;
     dq.in_t = 1;
-    decay_job &dv = p.job[1] = job(k, q, dout, array_of(a.dv), a.Dk, a.Dv);
+    decay_job &dv = p.job[1] = job(1, 0, 3, array_of(a.dv), a.Dk, a.Dv);
     dv.reverse = 1;
     dv.in_scale = 1.f;
     dv.up_scale = a.scale;
     dv.s_in = a.ds_last;
     dv.s_out = a.ds0;
     dv.out_zero = 1;
-    decay_job &dk = p.job[2] = job(v, dout, q, array_of(a.dk), a.Dv, a.Dk);
+    decay_job &dk = p.job[2] = job(2, 3, 0, array_of(a.dk), a.Dv, a.Dk);
     dk.reverse = 1;
     dk.in_scale = 1.f;
     dk.up_scale = a.scale;
@@ -568,12 +571,14 @@ cudaError_t chunk_launch(wm_seq *h, const decay_pass &p, cudaStream_t s) {
 
 // The pass, on tensor cores or in fp32; in spans, what each gives the state and the joins first.
 template <class T>
-cudaError_t run_pass(wm_seq *h, decay_pass &p, bool tc, cudaStream_t s) {
+cudaError_t run_pass(wm_seq *h, const seq_decay_args &a, decay_pass &p, bool tc, cudaStream_t s) {
     const long long pairs = (long long)p.N * p.H;
     cudaError_t e;
+    decay_maps maps;
+    if (tc) wm_seq_decay_tc_maps(a, p, maps);
     if (tc && (e = cudaMemsetAsync(p.redo, 0, (size_t)(1 + p.jobs * pairs) * 4, s)) != cudaSuccess) return e;
     if (p.spans > 1) {
-        e = tc ? wm_seq_decay_tc_launch(h, p, true, s) : chunk_launch<T, true>(h, p, s);
+        e = tc ? wm_seq_decay_tc_launch(h, p, maps, true, s) : chunk_launch<T, true>(h, p, s);
         if (e != cudaSuccess) return e;
         long long cells = 0;
         for (int i = 0; i < p.jobs; ++i) cells = std::max(cells, pairs * p.job[i].da * p.job[i].dc);
@@ -582,7 +587,7 @@ cudaError_t run_pass(wm_seq *h, decay_pass &p, bool tc, cudaStream_t s) {
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
     }
     if (!tc) return chunk_launch<T, false>(h, p, s);
-    if ((e = wm_seq_decay_tc_launch(h, p, false, s)) != cudaSuccess) return e;
+    if ((e = wm_seq_decay_tc_launch(h, p, maps, false, s)) != cudaSuccess) return e;
     p.only_redo = 1;
     p.spans = 1;
     p.span_tokens = (p.T + kChunk - 1) / kChunk * kChunk;
@@ -627,5 +632,5 @@ cudaError_t wm_seq_decay_launch(wm_seq *h, const seq_decay_args &a, bool backwar
         (backward ? p.job[1].s_in : p.job[0].s_in) = copy;
         if (backward) p.job[2].s_in = copy;
     }
-    return a.dtype == WM_BF16 ? run_pass<__nv_bfloat16>(h, p, tc, s) : run_pass<float>(h, p, tc, s);
+    return a.dtype == WM_BF16 ? run_pass<__nv_bfloat16>(h, a, p, tc, s) : run_pass<float>(h, a, p, tc, s);
 }

@@ -1,6 +1,8 @@
 // wm_seq_decay.cuh -- what the kernels of the decayed linear attention share (see wm_seq_decay.cu).
 // Not part of the public interface.
 #pragma once
+#include <cuda.h>
+
 #include "wm_seq_internal.h"
 
 // One array [T, N, H, D] of a call, strides in elements.
@@ -25,6 +27,7 @@ struct decay_job {
     float *spans;            // split over time: [spans][N, H, da, dc], what a span's tokens give, then what enters it
     int spans_t;             // those are another job's: [dc, da], and that one forms them
     int vec;                 // values of a, b, c and y that one access may move (alignment)
+    int map[3];              // which of q, k, v, dout a, b and c are
 };
 
 struct decay_pass {
@@ -46,7 +49,12 @@ struct decay_pass {
 // The tensor-core pass in bf16 (wm_seq_decay_tc.cu): its launch (state: only what the spans' tokens give the state), and the
 // CTAs an SM holds.
 constexpr int kDecayTcChunk = 128, kDecayTcMost = 128;  // tokens; values of a head
-cudaError_t wm_seq_decay_tc_launch(wm_seq *h, const decay_pass &p, bool state, cudaStream_t s);
+struct decay_maps {
+    CUtensorMap m[4];  // of q, k, v, dout
+    int use;           // all have one
+};
+void wm_seq_decay_tc_maps(const seq_decay_args &a, const decay_pass &p, decay_maps &maps);
+cudaError_t wm_seq_decay_tc_launch(wm_seq *h, const decay_pass &p, const decay_maps &maps, bool state, cudaStream_t s);
 int wm_seq_decay_tc_ctas(int Dk, int Dv);
 
 #ifdef __CUDACC__

@@ -50,10 +50,10 @@ constexpr uint32_t kWait = 1u << 22;                                // polls of 
 template <int D>
 struct Plan {
     static constexpr int tile = kPanel * (D / 64);
-    // (b's tiles and lo are read as operands 128 values wide: with D = 64 the second half is what lies behind them, and unused)
-    static constexpr int xb = 0, lo = xb + D * 128 * (D / 64), b = lo + tile, a = b + 2 * tile, c = a + 2 * tile, end = c + tile;
+    // (lo lies behind b: with D = 64 both are one operand of 128 rows)
+    static constexpr int xb = 0, b = xb + D * 128 * (D / 64), lo = b + 2 * tile, a = lo + tile, c = a + 2 * tile, end = c + tile;
     static constexpr int small = end;  // tables and barriers
-    static constexpr int bytes = small + 4 * 132 + 8 * 128 + 48 + 32 + 1024;
+    static constexpr int bytes = small + 4 * (132 + 32) + 8 * 128 + 48 + 48 + 1024;
     // P lies over A's first columns; with D = 64 O2 over A's others
     static constexpr int tA = 0, tO1 = 128, tO2 = D == 64 ? 64 : 256, tX = D == 64 ? 192 : 384, columns = D == 64 ? 256 : 512;
 };
@@ -122,20 +122,21 @@ __device__ __forceinline__ uint32_t hfma(uint32_t a, uint32_t b, uint32_t c) {
     return r;
 }
 
-// 128 tokens of an array as swizzled panels.  `at` is the first token's row, step the elements to the next one; rows and values
-// that are not there are zeros.  VEC: 16-byte copies.
-template <int D, bool VEC>
-__device__ __forceinline__ void load_tile(uint32_t dst, const bf16 *at, long long step, int rows, int dim) {
+// 128 tokens of an array as swizzled panels, by the CTA's threads.  `at` is the first row, step the elements to the next one;
+// rows outside [lo, hi) and values that are not there are zeros.
+template <int D>
+__device__ __forceinline__ void load_tile(uint32_t dst, const bf16 *at, long long step, int lo, int hi, int dim, int vec) {
     constexpr int per = D / 8, stride = kThreads / per;
     const int ch = threadIdx.x % per, row0 = threadIdx.x / per, left = dim - ch * 8;
     const bf16 *p = at + row0 * step + ch * 8;
     const uint32_t to = dst + (ch / 8) * kPanel + row0 * 128 + (((ch & 7) ^ (row0 & 7)) << 4);  // (stride is a multiple of 8)
-    if (left <= 0) rows = 0;
-#pragma unroll
+#pragma unroll 1
     for (int k = 0; k < kChunk / stride; ++k) {
-        const bool on = row0 + k * stride < rows;
-        if constexpr (VEC) {
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + k * stride * 128), "l"(on ? p : at), "r"(on ? 16 : 0) : "memory");
+        const int row = row0 + k * stride;
+        const bool on = row >= lo && row < hi && left > 0;
+        if (vec > 1) {
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + k * stride * 128), "l"(on ? p : at + lo * step), "r"(on ? 16 : 0)
+                         : "memory");
         } else {
             uint32_t v[4] = {};
             const unsigned short *u = reinterpret_cast<const unsigned short *>(p);
@@ -150,19 +151,27 @@ __device__ __forceinline__ void load_tile(uint32_t dst, const bf16 *at, long lon
     }
 }
 
-// VEC: 16-byte accesses; CUT: there may be resets.
-template <int D, bool STATE, bool VEC, bool CUT>
-__global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(const decay_pass p) {
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map, int d, int t, int n, int h, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+                 "l"(map), "r"(d), "r"(t), "r"(n), "r"(h), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void pair_barrier(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
+
+// TMA: the arrays have tensor maps; CUT: there may be resets.
+template <int D, bool STATE, bool TMA, bool CUT>
+__global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(const decay_pass p, const __grid_constant__ decay_maps maps) {
     using L = Plan<D>;
     extern __shared__ unsigned char raw[];
     unsigned char *smem = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
     const uint32_t base = tc::smem_u32(smem);
     float *const power = reinterpret_cast<float *>(smem + L::small);        // lambda^0 .. lambda^128
-    uint2 *const kept = reinterpret_cast<uint2 *>(power + 132);             // the tokens' weights in the next state: two bf16, each twice
+    float *const fall = power + 132;                                        // a block's columns: lambda^(31-i), or lambda^i in reverse
+    uint2 *const kept = reinterpret_cast<uint2 *>(fall + 32);               // the tokens' weights in the next state: two bf16, each twice
     uint32_t *const cuts = reinterpret_cast<uint32_t *>(kept + 128);        // [2][4]: tokens that begin something new
     int *const late = reinterpret_cast<int *>(cuts + 8);                    // a wait gave up
     uint32_t *const tmem_at = cuts + 9;
-    const uint32_t bars = tc::smem_u32(cuts + 12), barA = bars, barO = bars + 8, barX = bars + 16;
+    const uint32_t bars = tc::smem_u32(cuts + 12), barA = bars, barO = bars + 8, barX = bars + 16, barV = bars + 24, barQK = bars + 32;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quad = warp & 3, wg = warp >> 2;
     int jobs = 0, at[3] = {};
@@ -173,66 +182,94 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
     const decay_job &j = p.job[job];
     const int n = (int)(pair / p.H), head = (int)(pair % p.H), da = j.da, dc = j.dc;
     const decay_seq q = decay_open(p, j, n);
-    const float g = p.log_decay[head];
+    const bool rev = q.reverse;
     const long long pairs = (long long)p.N * p.H, cells = (long long)da * dc;
     const long long first = span * p.span_tokens, last = min(p.T, first + p.span_tokens), stop = min(last, q.len);
     const int chunks = stop > first ? (int)((stop - first + kChunk - 1) / kChunk) : 0;
+    // Row r of a tile is token begin(c) + r; counted along the pass it is step step_of(r) of the chunk.
+    const auto begin_of = [&](int c) { return rev ? q.len - first - (long long)(c + 1) * kChunk : first + (long long)c * kChunk; };
+    const auto step_of = [&](int r) { return rev ? kChunk - 1 - r : r; };
 
-    const bf16 *const pa = static_cast<const bf16 *>(j.a.p) + n * j.a.n + head * j.a.h;
-    const bf16 *const pb = static_cast<const bf16 *>(j.b.p) + n * j.b.n + head * j.b.h;
-    const bf16 *const pc = static_cast<const bf16 *>(j.c.p) + n * j.c.n + head * j.c.h;
     bf16 *const py = static_cast<bf16 *>(const_cast<void *>(j.y.p)) + n * j.y.n + head * j.y.h;
-    const int dir = q.reverse ? -1 : 1;
-    const auto load_ab = [&](int c) {  // keys, and queries, of a chunk
-        if (c < chunks) {
-            const long long s0 = first + (long long)c * kChunk;
-            const int rows = (int)min((long long)kChunk, stop - s0), slot = c & 1;
-            load_tile<D, VEC>(base + L::b + slot * L::tile, pb + q.at(s0) * j.b.t, dir * j.b.t, rows, da);
-            if constexpr (!STATE) load_tile<D, VEC>(base + L::a + slot * L::tile, pa + q.at(s0) * j.a.t, dir * j.a.t, rows, da);
+    const auto load = [&](uint32_t dst, const decay_array &g, int map, int dim, int c, uint32_t bar) {
+        const long long t0 = begin_of(c);
+        if constexpr (TMA) {
+#pragma unroll
+            for (int k = 0; k < D / 64; ++k) tma_load_4d(dst + k * kPanel, &maps.m[map], k * 64, (int)t0, n, head, bar);
+        } else {
+            const int rows = (int)min((long long)kChunk, stop - first - (long long)c * kChunk);
+            load_tile<D>(dst, static_cast<const bf16 *>(g.p) + n * g.n + head * g.h + t0 * g.t, g.t, rev ? kChunk - rows : 0, rev ? kChunk : rows, dim,
+                         j.vec);
         }
-        copy_commit();
+    };
+    // Loads of a chunk: by one thread of warp 0 where TMA does them, by all threads otherwise.
+    const auto load_ab = [&](int c) {  // keys, and queries
+        const int slot = c & 1;
+        if constexpr (TMA) {
+            if (c < chunks && warp == 0 && tc::elect_one()) {
+                tc::mbar_arrive_expect_tx(barQK + 8 * slot, (STATE ? 1 : 2) * L::tile);
+                load(base + L::b + slot * L::tile, j.b, j.map[1], da, c, barQK + 8 * slot);
+                if constexpr (!STATE) load(base + L::a + slot * L::tile, j.a, j.map[0], da, c, barQK + 8 * slot);
+            }
+            __syncwarp();
+        } else {
+            if (c < chunks) {
+                load(base + L::b + slot * L::tile, j.b, 0, da, c, 0);
+                if constexpr (!STATE) load(base + L::a + slot * L::tile, j.a, 0, da, c, 0);
+            }
+            copy_commit();
+        }
     };
     const auto load_c = [&](int c) {
-        if (c < chunks) {
-            const long long s0 = first + (long long)c * kChunk;
-            load_tile<D, VEC>(base + L::c, pc + q.at(s0) * j.c.t, dir * j.c.t, (int)min((long long)kChunk, stop - s0), dc);
+        if constexpr (TMA) {
+            if (c < chunks && warp == 0 && tc::elect_one()) {
+                tc::mbar_arrive_expect_tx(barV, L::tile);
+                load(base + L::c, j.c, j.map[2], dc, c, barV);
+            }
+            __syncwarp();
+        } else {
+            if (c < chunks) load(base + L::c, j.c, 0, dc, c, 0);
+            copy_commit();
         }
-        copy_commit();
     };
     const auto find_cuts = [&](int c) {
         if (CUT && warp < 4) {
-            const int r = warp * 32 + lane;
-            const long long s = first + (long long)c * kChunk + r;
+            const long long s = first + (long long)c * kChunk + warp * 32 + lane;
             const unsigned m = __ballot_sync(~0u, c < chunks && s < stop && decay_cut(p, q, s, n));
             if (lane == 0) cuts[(c & 1) * 4 + warp] = m;
         }
     };
+    if (warp == 0) {
+        if (tc::elect_one()) {
+            for (int i = 0; i < 6; ++i) tc::mbar_init(bars + 8 * i, 1);
+            tc::fence_mbar_init();
+            *late = 0;
+        }
+        __syncwarp();
+        tc::fence_proxy_async_smem();
+    }
     load_ab(0);
     load_c(0);
     load_ab(1);
+    if (warp == 1) tc::tmem_alloc(tc::smem_u32(tmem_at), L::columns);
+    const float g = p.log_decay[head];
     find_cuts(0);
     if (tid <= kChunk) power[tid] = decay_power(g, tid);
-    if (warp == 0) tc::tmem_alloc(tc::smem_u32(tmem_at), L::columns);
-    if (tid == 32) {
-        tc::mbar_init(barA, 1);
-        tc::mbar_init(barO, 1);
-        tc::mbar_init(barX, 1);
-        tc::fence_mbar_init();
-        *late = 0;
-    }
+    if (tid >= kThreads - 32) fall[lane] = decay_power(g, rev ? lane : 31 - lane);
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
     const uint32_t tmem = *tmem_at, mine = tmem + ((uint32_t)(quad * 32) << 16);
-    const auto wait = [&](uint32_t bar, int c) {
-        if (!*(volatile int *)late && !tc::mbar_wait_bounded(bar, (uint32_t)c & 1u, kWait)) {
+    const auto wait = [&](uint32_t bar, int phase) {
+        if (!*(volatile int *)late && !tc::mbar_wait_bounded(bar, (uint32_t)phase & 1u, kWait)) {
             *late = 1;
             seq_record(p.status + 1, WM_ERR_TIMEOUT);
         }
         tc::fence_after_sync();
     };
 
-    // the entering state into TMEM: row a thread's lane, half of the columns a warpgroup
+    // The entering state into TMEM: row a thread's lane, half of the columns a warpgroup.  With D = 64 the state is the sum of
+    // lanes 0 to 63 (sums of the first bf16 parts) and 64 to 127 (of the second).
     constexpr int W = D / 2;  // columns of X and of the outputs that a thread takes
     const int xrow = quad * 32 + lane, col0 = wg * W;
     const float *from = nullptr;
@@ -249,7 +286,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
         }
     }
     bool has_x = from != nullptr && chunks > 0;  // X is not 0
-    if (has_x && quad * 32 < D) {
+    if (has_x) {
 #pragma unroll 1
         for (int h = 0; h < W; h += 32) {
             uint32_t r[32];
@@ -267,16 +304,18 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
     }
     uint32_t odd = 0;   // two bf16: NaN once an output was not finite
     bool keeps = true;  // (STATE) no cut so far
+    const int step = step_of(xrow), slope = rev ? -1 : 1;
 
 #pragma unroll 1
     for (int c = 0; c < chunks; ++c) {
-        const long long s0 = first + (long long)c * kChunk;
+        const long long s0 = first + (long long)c * kChunk, t0 = begin_of(c);
         const int rows = (int)min((long long)kChunk, stop - s0), slot = c & 1;
         const uint32_t ta = base + L::a + slot * L::tile, tb = base + L::b + slot * L::tile, tv = base + L::c;
-        copy_wait<2>();
+        if constexpr (TMA) wait(barQK + 8 * slot, c >> 1);
+        else copy_wait<1>();
         tc::fence_proxy_async_smem();
         tc::fence_before_sync();
-        __syncthreads();
+        __syncthreads();  // the chunk before is read out
         if constexpr (!STATE) {
             if (warp == 0 && tc::elect_one()) {
                 tc::fence_after_sync();
@@ -288,7 +327,8 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
             }
             __syncwarp();
         }
-        // tokens that begin something new: what a token sees begins with the last of them up to it
+        if (c > 0) load_ab(c + 1);
+        // tokens that begin something new: what a token sees begins with the last of them up to it (counted in steps)
         int keep_from = -1, begin = -1;
         bool any_cut = false;
         if constexpr (CUT) {
@@ -299,8 +339,8 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
             if (any_cut) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    if (cut[i]) keep_from = 32 * i + 31 - __clz(cut[i]);  // (no cuts behind the last row)
-                    const uint32_t m = quad > i ? cut[i] : quad < i ? 0u : cut[i] & (~0u >> (31 - lane));
+                    if (cut[i]) keep_from = 32 * i + 31 - __clz(cut[i]);  // (no cuts behind the last step)
+                    const uint32_t m = step / 32 > i ? cut[i] : step / 32 < i ? 0u : cut[i] & (~0u >> (31 - step % 32));
                     if (m) begin = 32 * i + 31 - __clz(m);
                 }
             }
@@ -309,9 +349,10 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
         const int less = !STATE && j.first && s0 + rows == q.len ? 1 : 0;
         if (tid < kChunk && (CUT || STATE || c == 0 || rows < kChunk || less)) {
             float w = 0.f;
-            if (tid < rows && tid >= keep_from) {
-                if constexpr (STATE) w = decay_power(g, stop - s0 - tid);  // up to the span's end
-                else w = power[rows - tid - less];
+            const int s = step_of(tid);
+            if (s < rows && s >= keep_from) {
+                if constexpr (STATE) w = decay_power(g, stop - s0 - s);  // up to the span's end
+                else w = power[rows - s - less];
             }
             w *= j.up_scale;
             const float w1 = __bfloat162float(__float2bfloat16_rn(w));
@@ -319,20 +360,47 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
         }
         if constexpr (!STATE) {
             // X -> Xb, and X to what the next state keeps of it
-            if (has_x && quad * 32 < D) {
+            if (has_x) {
                 const Pair shrink = twice(power[rows - less]);
 #pragma unroll
                 for (int h = 0; h < W; h += 32) {
                     uint32_t r[32];
-                    const int col = col0 + h;
+                    const int col = col0 + h, row = D == 64 ? xrow & 63 : xrow;
+                    const uint32_t to = base + L::xb + (col / 64) * (D * 128) + row * 128;
+                    const auto place = [&](int i) { return to + (((((col + i) % 64) / 8) ^ (row & 7)) << 4); };
                     TC_LD32(mine + L::tX + col, r);
                     tc::tmem_ld_wait();
+                    if constexpr (D == 64) {  // the second parts come by way of Xb's place
+                        if (quad >= 2) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 8) {
-                        const float *f = reinterpret_cast<const float *>(r + i);
-                        const uint32_t to = base + L::xb + ((col + i) / 64) * (D * 128) + xrow * 128 + (((((col + i) % 64) / 8) ^ (xrow & 7)) << 4);
-                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(pack2(f[0], f[1])), "r"(pack2(f[2], f[3])),
-                                     "r"(pack2(f[4], f[5])), "r"(pack2(f[6], f[7])) : "memory");
+                            for (int i = 0; i < 32; i += 8) {
+                                const float *f = reinterpret_cast<const float *>(r + i);
+                                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(place(i)), "r"(pack2(f[0], f[1])), "r"(pack2(f[2], f[3])),
+                                             "r"(pack2(f[4], f[5])), "r"(pack2(f[6], f[7])) : "memory");
+                            }
+                        }
+                        pair_barrier(1 + wg * 2 + (quad & 1));
+                    }
+                    if (D == 128 || quad < 2) {
+#pragma unroll
+                        for (int i = 0; i < 32; i += 8) {
+                            const float *f = reinterpret_cast<const float *>(r + i);
+                            float x[8];
+                            if constexpr (D == 64) {
+                                uint32_t e[4];
+                                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(e[0]), "=r"(e[1]), "=r"(e[2]), "=r"(e[3]) : "r"(place(i)) : "memory");
+#pragma unroll
+                                for (int m = 0; m < 4; ++m) {
+                                    x[2 * m] = f[2 * m] + __uint_as_float(e[m] << 16);
+                                    x[2 * m + 1] = f[2 * m + 1] + __uint_as_float(e[m] & 0xffff0000u);
+                                }
+                            } else {
+#pragma unroll
+                                for (int m = 0; m < 8; ++m) x[m] = f[m];
+                            }
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(place(i)), "r"(pack2(x[0], x[1])), "r"(pack2(x[2], x[3])),
+                                         "r"(pack2(x[4], x[5])), "r"(pack2(x[6], x[7])) : "memory");
+                        }
                     }
                     if (!CUT || keep_from < 0) {
 #pragma unroll
@@ -341,6 +409,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
                             r[i] = __float_as_uint(v.f.x);
                             r[i + 1] = __float_as_uint(v.f.y);
                         }
+                        __syncwarp();
                         TC_ST32(mine + L::tX + col, r);
                     }
                 }
@@ -352,7 +421,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int block = wg * 2 + h, j0 = block * 32;
-                if (block > quad) {  // above the diagonal
+                if (rev ? block < quad : block > quad) {  // not seen
 #pragma unroll
                     for (int i = 0; i < 16; ++i) packed[h * 16 + i] = 0u;
                     continue;
@@ -363,17 +432,18 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
                 if (block == quad) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
-                        const float f = __uint_as_float(v[i]) * (j.w_scale * power[max(lane - i, 0)]);
-                        v[i] = i <= lane ? __float_as_uint(f) : 0u;
+                        const int away = slope * (lane - i);
+                        const float f = __uint_as_float(v[i]) * (j.w_scale * power[max(away, 0)]);
+                        v[i] = away >= 0 ? __float_as_uint(f) : 0u;
                     }
-                } else {  // lambda^(xrow - j0 - 31) lambda^(31 - i): neither is above 1
-                    const Pair w = twice(j.w_scale * power[xrow - j0 - 31]);
+                } else {  // lambda^away in two factors, neither above 1
+                    const Pair w = twice(j.w_scale * power[rev ? j0 - xrow : xrow - j0 - 31]);
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) {
-                        const float4 t = *reinterpret_cast<const float4 *>(power + 28 - i);
+                        const float4 t = *reinterpret_cast<const float4 *>(fall + i);
                         Pair t0, t1;
-                        t0.f = make_float2(t.w, t.z);
-                        t1.f = make_float2(t.y, t.x);
+                        t0.f = make_float2(t.x, t.y);
+                        t1.f = make_float2(t.z, t.w);
                         t0 = mul2(pair_of(v[i], v[i + 1]), mul2(t0, w));
                         t1 = mul2(pair_of(v[i + 2], v[i + 3]), mul2(t1, w));
                         v[i] = __float_as_uint(t0.f.x), v[i + 1] = __float_as_uint(t0.f.y);
@@ -382,7 +452,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
                 }
                 if (CUT && any_cut) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = j0 + i >= begin ? v[i] : 0u;
+                    for (int i = 0; i < 32; ++i) v[i] = step_of(j0 + i) >= begin ? v[i] : 0u;
                 }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) packed[h * 16 + i] = pack2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
@@ -412,8 +482,9 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
             for (int k = 0; k < kChunk / stride; ++k) {
                 const uint32_t to = off + k * stride * 128;
                 uint32_t v[4], hi[4], lo[4];
-                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(tb + to));
+                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(tb + to) : "memory");
                 const uint2 w = kept[row0 + k * stride];
+                if (TMA && rows < kChunk && step_of(row0 + k * stride) >= rows) v[0] = v[1] = v[2] = v[3] = 0u;  // (whatever lies there)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     hi[i] = hmul(v[i], w.x);
@@ -423,8 +494,21 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
                 asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(base + L::lo + to), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
             }
         }
+        if constexpr (TMA) {
+            if (rows < kChunk) {  // values of steps that are not there: whatever lies there times 0 is to be 0
+                wait(barV, c);
+                constexpr int per = D / 8;
+                for (int i = tid; i < (kChunk - rows) * per; i += kThreads) {
+                    const int s = rows + i / per, ch = i % per, row = step_of(s);
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(tv + (ch / 8) * kPanel + row * 128 + (((ch & 7) ^ (row & 7)) << 4)), "r"(0) : "memory");
+                }
+            } else if (warp == 0) {
+                wait(barV, c);
+            }
+        } else {
+            copy_wait<1>();
+        }
         if constexpr (!STATE) tmem_st_wait();
-        copy_wait<1>();
         tc::fence_proxy_async_smem();
         tc::fence_before_sync();
         __syncthreads();
@@ -437,22 +521,22 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
                     mma_bf16_ts(tmem + L::tO1, tmem + L::tA + k * 8, desc_mn(tv + k * 2048, kPanel), tc::idesc_bf16_f32(128, D) | kBmn, k > 0);
                 tc::mma_commit(barO);
             }
+            // (D = 64: both parts as one operand of 128 rows)
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+            for (int part = 0; part < D / 64; ++part)
 #pragma unroll
                 for (int k = 0; k < kChunk / 16; ++k)
-                    tc::mma_bf16(tmem + L::tX, desc_mn((half ? base + L::lo : tb) + k * 2048, kPanel), desc_mn(tv + k * 2048, kPanel),
-                                 tc::idesc_bf16_f32(128, D) | kAmn | kBmn, half > 0 || k > 0 || onto);
+                    tc::mma_bf16(tmem + L::tX, desc_mn((part ? base + L::lo : tb) + k * 2048, D == 64 ? base + L::lo - tb : kPanel),
+                                 desc_mn(tv + k * 2048, kPanel), tc::idesc_bf16_f32(128, D) | kAmn | kBmn, part > 0 || k > 0 || onto);
             tc::mma_commit(barX);
         }
         __syncwarp();
         if constexpr (STATE) keeps = keeps && keep_from < 0;
         find_cuts(c + 1);
         if constexpr (!STATE) {
-            // y = O1 + in_scale lambda^r O2
-            const Pair w = twice(j.in_scale * power[xrow]);
-            const bool sees = !CUT || begin < 0;
-            bf16 *const out = py + q.at(s0 + min(xrow, rows - 1)) * j.y.t + col0;
+            // y = O1 + in_scale lambda^step O2, by way of a's tile to whole rows
+            const Pair w = twice(j.in_scale * power[step]);
+            const bool sees = !CUT || begin < 0, there = step < rows;
             wait(barO, c);
 #pragma unroll
             for (int h = 0; h < W; h += 32) {
@@ -473,20 +557,37 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
                 } else {
                     tc::tmem_ld_wait();
                 }
-                if (xrow < rows) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        o1[i] = pack2(__uint_as_float(o1[2 * i]), __uint_as_float(o1[2 * i + 1]));
-                        odd = hfma(o1[i], 0u, odd);
-                    }
-                    if constexpr (VEC) {
+                for (int i = 0; i < 16; ++i) o1[i] = pack2(__uint_as_float(o1[2 * i]), __uint_as_float(o1[2 * i + 1]));
+                if (there) {
 #pragma unroll
-                        for (int i = 0; i < 16; i += 4)
-                            if (col0 + h + 2 * i < dc) *reinterpret_cast<uint4 *>(out + h + 2 * i) = make_uint4(o1[i], o1[i + 1], o1[i + 2], o1[i + 3]);
+                    for (int i = 0; i < 16; ++i) odd = hfma(o1[i], 0u, odd);
+                }
+#pragma unroll
+                for (int i = 0; i < 16; i += 4) {
+                    const int col = col0 + h + 2 * i;
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(ta + (col / 64) * kPanel + xrow * 128 + ((((col % 64) / 8) ^ (xrow & 7)) << 4)),
+                                 "r"(o1[i]), "r"(o1[i + 1]), "r"(o1[i + 2]), "r"(o1[i + 3]) : "memory");
+                }
+            }
+            __syncwarp();
+            // a warp's 32 rows, W / 8 pieces of 16 bytes each
+            constexpr int per = W / 8, at_once = 32 / per;
+            const int ch = col0 / 8 + lane % per, left = dc - ch * 8;
+#pragma unroll
+            for (int k = 0; k < 32 / at_once; ++k) {
+                const int row = quad * 32 + k * at_once + lane / per;
+                uint32_t v[4];
+                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                             : "r"(ta + (ch / 8) * kPanel + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) : "memory");
+                if (step_of(row) < rows && left > 0) {
+                    bf16 *const out = py + (t0 + row) * j.y.t + ch * 8;
+                    if (TMA || j.vec > 1) {
+                        *reinterpret_cast<uint4 *>(out) = make_uint4(v[0], v[1], v[2], v[3]);
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (col0 + h + i < dc) reinterpret_cast<unsigned short *>(out)[h + i] = (unsigned short)(o1[i / 2] >> (16 * (i & 1)));
+                        for (int m = 0; m < 8; ++m)
+                            if (m < left) reinterpret_cast<unsigned short *>(out)[m] = (unsigned short)(v[m / 2] >> (16 * (m & 1)));
                     }
                 }
             }
@@ -494,16 +595,16 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
         wait(barX, c);
         has_x = true;
         load_c(c + 1);
-        load_ab(c + 2);
     }
 
     // outputs of padding
     if constexpr (!STATE) {
         const long long pad = max(first, min(q.len, last));
-        const int per = VEC ? dc / 8 : dc, at_once = max(1, kThreads / per), r0 = tid / per, c0 = tid - r0 * per;
+        const bool wide = TMA || j.vec > 1;
+        const int per = wide ? dc / 8 : dc, at_once = kThreads / per, r0 = tid / per, c0 = tid - r0 * per;
         if (r0 < at_once)
             for (long long r = pad + r0; r < last; r += at_once) {
-                if constexpr (VEC) *reinterpret_cast<uint4 *>(py + r * j.y.t + c0 * 8) = make_uint4(0, 0, 0, 0);
+                if (wide) *reinterpret_cast<uint4 *>(py + r * j.y.t + c0 * 8) = make_uint4(0, 0, 0, 0);
                 else py[r * j.y.t + c0] = __float2bfloat16_rn(0.f);
             }
     }
@@ -517,28 +618,35 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
         if ((q.len > first && q.len <= last) || (q.len == 0 && span == 0)) to = j.s_out + pair * cells;
         empty = j.out_zero && q.len > 0 && p.reset && p.reset[n] != 0;
     }
+    if constexpr (!TMA) copy_wait<0>();
     if (chunks > 0) {
+        // by way of shared memory (a's tiles, and c's behind them, are done with) to whole rows
         bool bad = (odd & 0x7fff7fffu) != 0;  // (a product with 0 is 0 or NaN)
-        if (quad * 32 < D) {
+        float *const x = reinterpret_cast<float *>(smem + L::a);
+        constexpr int ld = D + 1;
+        __syncthreads();
 #pragma unroll 1
-            for (int h = 0; h < W; h += 32) {
-                uint32_t r[32];
-                __syncwarp();
-                TC_LD32(mine + L::tX + col0 + h, r);
-                tc::tmem_ld_wait();
-                if (xrow < da) {
+        for (int part = D == 64; part >= 0; --part) {  // D = 64: lanes 64 and up, then the others onto them
+            if (D == 128 || (quad >= 2) == (part == 1)) {
+#pragma unroll 1
+                for (int h = 0; h < W; h += 32) {
+                    uint32_t r[32];
+                    __syncwarp();
+                    TC_LD32(mine + L::tX + col0 + h, r);
+                    tc::tmem_ld_wait();
+                    float *const at = x + (D == 64 ? xrow & 63 : xrow) * ld + col0 + h;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const int col = col0 + h + i;
-                        const float v = __uint_as_float(r[i]);
-                        if (col < dc) {
-                            bad |= !(fabsf(v) <= 3.4028235e38f);
-                            if (to) to[(long long)xrow * dc + col] = empty ? 0.f : v;
-                        }
-                    }
+                    for (int i = 0; i < 32; ++i) at[i] = __uint_as_float(r[i]) + (D == 64 && part == 0 ? at[i] : 0.f);
                 }
             }
+            __syncthreads();
         }
+        for (int r = warp; r < da; r += kThreads / 32)
+            for (int k = lane; k < dc; k += 32) {
+                const float v = x[r * ld + k];
+                bad |= !(fabsf(v) <= 3.4028235e38f);
+                if (to) to[(long long)r * dc + k] = empty ? 0.f : v;
+            }
         if (bad) {
             decay_mark(p, job, pair);
             if constexpr (STATE)
@@ -551,38 +659,72 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
             to[i] = empty || !from ? 0.f : from_t ? from[k * da + r] : from[i];
         }
     }
-    copy_wait<0>();
     tc::fence_before_sync();
     __syncthreads();
-    if (warp == 0) tc::tmem_dealloc(tmem, L::columns);
+    if (warp == 1) tc::tmem_dealloc(tmem, L::columns);
+}
+
+typedef CUresult (*encode_fn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                              const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+encode_fn encoder() {
+    static const encode_fn fn = [] {
+        void *f = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q);
+        return e == cudaSuccess && q == cudaDriverEntryPointSuccess ? (encode_fn)f : nullptr;
+    }();
+    return fn;
+}
+
+// A map of [T, N, H, dim] whose box is 128 tokens x 64 values of one head; false where a map cannot say it (an axis that is
+// broadcast, strides that are not multiples of 16 bytes).
+bool make_map(CUtensorMap *m, const decay_array &v, long long T, int N, int H, int dim) {
+    const long long sizes[3] = {T, N, H}, strides[3] = {v.t, v.n, v.h};
+    cuuint64_t dims[4] = {(cuuint64_t)dim, (cuuint64_t)T, (cuuint64_t)N, (cuuint64_t)H}, bytes[3];
+    for (int i = 0; i < 3; ++i) {
+        bytes[i] = sizes[i] == 1 ? 16 : (cuuint64_t)strides[i] * 2;
+        if (sizes[i] > 1 && (strides[i] == 0 || strides[i] >= (1ll << 38) || bytes[i] % 16)) return false;
+    }
+    if ((uintptr_t)v.p % 16 || !encoder()) return false;
+    const cuuint32_t box[4] = {64, kChunk, 1, 1}, one[4] = {1, 1, 1, 1};
+    return encoder()(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(v.p), dims, bytes, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace
 
 int wm_seq_decay_tc_ctas(int Dk, int Dv) { return Dk <= 64 && Dv <= 64 ? 2 : 1; }
 
+void wm_seq_decay_tc_maps(const seq_decay_args &a, const decay_pass &p, decay_maps &maps) {
+    const wm_seq_heads *const arrays[4] = {&a.q, &a.k, &a.v, &a.dout};
+    maps.use = 1;
+    for (int i = 0; i < p.jobs; ++i) maps.use = maps.use && p.job[i].vec > 1;
+    for (int i = 0; i < (p.jobs > 1 ? 4 : 3) && maps.use; ++i) {
+        const wm_seq_heads &v = *arrays[i];
+        maps.use = make_map(&maps.m[i], {v.data, v.stride_t, v.stride_n, v.stride_h}, a.T, a.N, a.H, i < 2 ? a.Dk : a.Dv);
+    }
+}
+
 namespace {
-template <int D, bool STATE, bool VEC, bool CUT>
-cudaError_t launch(const decay_pass &p, unsigned grid, cudaStream_t s) {
-    const cudaError_t e = cudaFuncSetAttribute(decay_tc_kernel<D, STATE, VEC, CUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan<D>::bytes);
+template <int D, bool STATE, bool TMA, bool CUT>
+cudaError_t launch(const decay_pass &p, const decay_maps &maps, unsigned grid, cudaStream_t s) {
+    const cudaError_t e = cudaFuncSetAttribute(decay_tc_kernel<D, STATE, TMA, CUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan<D>::bytes);
     if (e != cudaSuccess) return e;
-    decay_tc_kernel<D, STATE, VEC, CUT><<<dim3(grid, p.spans), kThreads, Plan<D>::bytes, s>>>(p);
+    decay_tc_kernel<D, STATE, TMA, CUT><<<dim3(grid, p.spans), kThreads, Plan<D>::bytes, s>>>(p, maps);
     return cudaGetLastError();
 }
 template <int D, bool STATE>
-cudaError_t launch(const decay_pass &p, unsigned grid, cudaStream_t s) {
-    bool vec = true;
-    for (int i = 0; i < p.jobs; ++i) vec = vec && p.job[i].vec > 1;
-    if (vec) return p.reset ? launch<D, STATE, true, true>(p, grid, s) : launch<D, STATE, true, false>(p, grid, s);
-    return p.reset ? launch<D, STATE, false, true>(p, grid, s) : launch<D, STATE, false, false>(p, grid, s);
+cudaError_t launch(const decay_pass &p, const decay_maps &maps, unsigned grid, cudaStream_t s) {
+    if (maps.use) return p.reset ? launch<D, STATE, true, true>(p, maps, grid, s) : launch<D, STATE, true, false>(p, maps, grid, s);
+    return p.reset ? launch<D, STATE, false, true>(p, maps, grid, s) : launch<D, STATE, false, false>(p, maps, grid, s);
 }
 }  // namespace
 
-cudaError_t wm_seq_decay_tc_launch(wm_seq *h, const decay_pass &p, bool state, cudaStream_t s) {
+cudaError_t wm_seq_decay_tc_launch(wm_seq *h, const decay_pass &p, const decay_maps &maps, bool state, cudaStream_t s) {
     int jobs = 0;
     for (int i = 0; i < p.jobs; ++i) jobs += !(state && p.job[i].spans_t);
     const unsigned grid = (unsigned)((long long)p.N * p.H * jobs);
     ++h->last_launches;
-    if (std::max(p.job[0].da, p.job[0].dc) <= 64) return state ? launch<64, true>(p, grid, s) : launch<64, false>(p, grid, s);
-    return state ? launch<128, true>(p, grid, s) : launch<128, false>(p, grid, s);
+    if (std::max(p.job[0].da, p.job[0].dc) <= 64) return state ? launch<64, true>(p, maps, grid, s) : launch<64, false>(p, maps, grid, s);
+    return state ? launch<128, true>(p, maps, grid, s) : launch<128, false>(p, maps, grid, s);
 }
