@@ -50,8 +50,8 @@ struct decay_pass {
 // CTAs an SM holds.
 constexpr int kDecayTcChunk = 128, kDecayTcMost = 128;  // tokens; values of a head
 struct decay_maps {
-    CUtensorMap m[4];  // of q, k, v, dout
-    int use;           // all have one
+    CUtensorMap in[4], out[3];  // of q, k, v, dout; of the jobs' outputs
+    int use, stores;            // all inputs, all outputs have one
 };
 void wm_seq_decay_tc_maps(const seq_decay_args &a, const decay_pass &p, decay_maps &maps);
 cudaError_t wm_seq_decay_tc_launch(wm_seq *h, const decay_pass &p, const decay_maps &maps, bool state, cudaStream_t s);

@@ -1,6 +1,7 @@
 // wm_seq_decay_tc.cu -- the decayed linear attention's passes in bf16 on the tensor cores (see wm_seq_decay.cu).
 //
-// Chunks of 128 tokens, one CTA a job of a head of a sequence (or of a span of it), 256 threads.  For each chunk
+// Chunks of 128 tokens, one CTA a job of a head of a sequence (or of a span of it): 8 warps for heads of up to 64 values (two
+// such CTAs an SM), 16 for up to 128, and one more that issues copies and products.  For each chunk
 //   A = a b^T                     128 x 128, both K-major as they lie in memory
 //   P = A * weights               TMEM -> registers -> TMEM as bf16, where the next product reads it
 //   O2 = a Xb                     Xb: the state X, fp32 in TMEM, as a bf16 tile
@@ -39,16 +40,23 @@
                    "r"((r)[24]), "r"((r)[25]), "r"((r)[26]), "r"((r)[27]), "r"((r)[28]), "r"((r)[29]), "r"((r)[30]), "r"((r)[31]), \
                    "r"((uint32_t)(taddr)) : "memory")
 
+#define TC_ST16(taddr, r)                                                                                                        \
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"         \
+                 ::"r"((r)[0]), "r"((r)[1]), "r"((r)[2]), "r"((r)[3]), "r"((r)[4]), "r"((r)[5]), "r"((r)[6]), "r"((r)[7]),         \
+                   "r"((r)[8]), "r"((r)[9]), "r"((r)[10]), "r"((r)[11]), "r"((r)[12]), "r"((r)[13]), "r"((r)[14]), "r"((r)[15]),   \
+                   "r"((uint32_t)(taddr)) : "memory")
+
 namespace {
 
 using bf16 = __nv_bfloat16;
 
-constexpr int kChunk = kDecayTcChunk, kThreads = 256, kPanel = kChunk * 128;  // bytes of 128 tokens x 64 values
+constexpr int kChunk = kDecayTcChunk, kPanel = kChunk * 128;  // bytes of 128 tokens x 64 values
 constexpr uint32_t kWait = 1u << 22;                                // polls of a wait (each about 20 ns or more)
 
 // What a CTA of head width D (64 or 128) holds: shared memory and TMEM columns.
 template <int D>
 struct Plan {
+    static constexpr int workers = 4 * D, threads = workers + 32;  // 32 columns of the state and of the outputs a thread
     static constexpr int tile = kPanel * (D / 64);
     // (lo lies behind b: with D = 64 both are one operand of 128 rows)
     static constexpr int xb = 0, b = xb + D * 128 * (D / 64), lo = b + 2 * tile, a = lo + tile, c = a + 2 * tile, end = c + tile;
@@ -126,7 +134,7 @@ __device__ __forceinline__ uint32_t hfma(uint32_t a, uint32_t b, uint32_t c) {
 // rows outside [lo, hi) and values that are not there are zeros.
 template <int D>
 __device__ __forceinline__ void load_tile(uint32_t dst, const bf16 *at, long long step, int lo, int hi, int dim, int vec) {
-    constexpr int per = D / 8, stride = kThreads / per;
+    constexpr int per = D / 8, stride = Plan<D>::workers / per;
     const int ch = threadIdx.x % per, row0 = threadIdx.x / per, left = dim - ch * 8;
     const bf16 *p = at + row0 * step + ch * 8;
     const uint32_t to = dst + (ch / 8) * kPanel + row0 * 128 + (((ch & 7) ^ (row0 & 7)) << 4);  // (stride is a multiple of 8)
@@ -156,12 +164,20 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *map
                  "l"(map), "r"(d), "r"(t), "r"(n), "r"(h), "r"(bar)
                  : "memory");
 }
+__device__ __forceinline__ void tma_store_4d(const CUtensorMap *map, uint32_t src, int d, int t, int n, int h) {
+    asm volatile("cp.async.bulk.tensor.4d.global.shared::cta.bulk_group [%0, {%1, %2, %3, %4}], [%5];" ::"l"(map), "r"(d), "r"(t), "r"(n), "r"(h),
+                 "r"(src)
+                 : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void tma_store_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void pair_barrier(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
 
-// TMA: the arrays have tensor maps; CUT: there may be resets.
+// TMA: the inputs have tensor maps; CUT: there may be resets.
 template <int D, bool STATE, bool TMA, bool CUT>
-__global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(const decay_pass p, const __grid_constant__ decay_maps maps) {
+__global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_kernel(const decay_pass p, const __grid_constant__ decay_maps maps) {
     using L = Plan<D>;
+    constexpr bool early = TMA && !STATE && D == 128;  // A of the next chunk is formed as soon as P is read (O2 has a place of its own)
     extern __shared__ unsigned char raw[];
     unsigned char *smem = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
     const uint32_t base = tc::smem_u32(smem);
@@ -169,11 +185,12 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
     float *const fall = power + 132;                                        // a block's columns: lambda^(31-i), or lambda^i in reverse
     uint2 *const kept = reinterpret_cast<uint2 *>(fall + 32);               // the tokens' weights in the next state: two bf16, each twice
     uint32_t *const cuts = reinterpret_cast<uint32_t *>(kept + 128);        // [2][4]: tokens that begin something new
-    int *const late = reinterpret_cast<int *>(cuts + 8);                    // a wait gave up
+    volatile int *const late = reinterpret_cast<int *>(cuts + 8);           // a wait gave up
     uint32_t *const tmem_at = cuts + 9;
     const uint32_t bars = tc::smem_u32(cuts + 12), barA = bars, barO = bars + 8, barX = bars + 16, barV = bars + 24, barQK = bars + 32;
 
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quad = warp & 3, wg = warp >> 2;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quad = warp & 3;
+    const bool worker = tid < L::workers;
     int jobs = 0, at[3] = {};
     for (int i = 0; i < p.jobs; ++i)
         if (!(STATE && p.job[i].spans_t)) at[jobs++] = i;
@@ -186,27 +203,27 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
     const long long pairs = (long long)p.N * p.H, cells = (long long)da * dc;
     const long long first = span * p.span_tokens, last = min(p.T, first + p.span_tokens), stop = min(last, q.len);
     const int chunks = stop > first ? (int)((stop - first + kChunk - 1) / kChunk) : 0;
-    // Row r of a tile is token begin(c) + r; counted along the pass it is step step_of(r) of the chunk.
+    // Row r of a tile is token begin_of(c) + r; counted along the pass it is step step_of(r) of the chunk.
     const auto begin_of = [&](int c) { return rev ? q.len - first - (long long)(c + 1) * kChunk : first + (long long)c * kChunk; };
     const auto step_of = [&](int r) { return rev ? kChunk - 1 - r : r; };
 
     bf16 *const py = static_cast<bf16 *>(const_cast<void *>(j.y.p)) + n * j.y.n + head * j.y.h;
+    // Loads of a chunk: by the issuing warp's one thread where TMA does them, by the workers otherwise.
     const auto load = [&](uint32_t dst, const decay_array &g, int map, int dim, int c, uint32_t bar) {
         const long long t0 = begin_of(c);
         if constexpr (TMA) {
 #pragma unroll
-            for (int k = 0; k < D / 64; ++k) tma_load_4d(dst + k * kPanel, &maps.m[map], k * 64, (int)t0, n, head, bar);
+            for (int k = 0; k < D / 64; ++k) tma_load_4d(dst + k * kPanel, &maps.in[map], k * 64, (int)t0, n, head, bar);
         } else {
             const int rows = (int)min((long long)kChunk, stop - first - (long long)c * kChunk);
             load_tile<D>(dst, static_cast<const bf16 *>(g.p) + n * g.n + head * g.h + t0 * g.t, g.t, rev ? kChunk - rows : 0, rev ? kChunk : rows, dim,
                          j.vec);
         }
     };
-    // Loads of a chunk: by one thread of warp 0 where TMA does them, by all threads otherwise.
     const auto load_ab = [&](int c) {  // keys, and queries
         const int slot = c & 1;
         if constexpr (TMA) {
-            if (c < chunks && warp == 0 && tc::elect_one()) {
+            if (c < chunks && tc::elect_one()) {
                 tc::mbar_arrive_expect_tx(barQK + 8 * slot, (STATE ? 1 : 2) * L::tile);
                 load(base + L::b + slot * L::tile, j.b, j.map[1], da, c, barQK + 8 * slot);
                 if constexpr (!STATE) load(base + L::a + slot * L::tile, j.a, j.map[0], da, c, barQK + 8 * slot);
@@ -222,7 +239,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
     };
     const auto load_c = [&](int c) {
         if constexpr (TMA) {
-            if (c < chunks && warp == 0 && tc::elect_one()) {
+            if (c < chunks && tc::elect_one()) {
                 tc::mbar_arrive_expect_tx(barV, L::tile);
                 load(base + L::c, j.c, j.map[2], dc, c, barV);
             }
@@ -239,7 +256,17 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
             if (lane == 0) cuts[(c & 1) * 4 + warp] = m;
         }
     };
-    if (warp == 0) {
+    const auto wait = [&](uint32_t bar, int phase) {
+        for (uint32_t i = 0; !tc::mbar_try_wait(bar, (uint32_t)phase & 1u); ++i) {
+            if (*late || i == kWait) {  // (what follows goes on with what there is)
+                *late = 1;
+                seq_record(p.status + 1, WM_ERR_TIMEOUT);
+                break;
+            }
+        }
+        tc::fence_after_sync();
+    };
+    if (!worker) {
         if (tc::elect_one()) {
             for (int i = 0; i < 6; ++i) tc::mbar_init(bars + 8 * i, 1);
             tc::fence_mbar_init();
@@ -248,33 +275,23 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
         __syncwarp();
         tc::fence_proxy_async_smem();
     }
-    load_ab(0);
-    load_c(0);
-    load_ab(1);
+    if (TMA != worker) {
+        load_ab(0);
+        load_c(0);
+        load_ab(1);
+    }
     if (warp == 1) tc::tmem_alloc(tc::smem_u32(tmem_at), L::columns);
     const float g = p.log_decay[head];
     find_cuts(0);
     if (tid <= kChunk) power[tid] = decay_power(g, tid);
-    if (tid >= kThreads - 32) fall[lane] = decay_power(g, rev ? lane : 31 - lane);
+    if (warp == 7) fall[lane] = decay_power(g, rev ? lane : 31 - lane);
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
-    const uint32_t tmem = *tmem_at, mine = tmem + ((uint32_t)(quad * 32) << 16);
-    const auto wait = [&](uint32_t bar, int phase) {
-        if (!*(volatile int *)late && !tc::mbar_wait_bounded(bar, (uint32_t)phase & 1u, kWait)) {
-            *late = 1;
-            seq_record(p.status + 1, WM_ERR_TIMEOUT);
-        }
-        tc::fence_after_sync();
-    };
+    const uint32_t tmem = *tmem_at;
 
-    // The entering state into TMEM: row a thread's lane, half of the columns a warpgroup.  With D = 64 the state is the sum of
-    // lanes 0 to 63 (sums of the first bf16 parts) and 64 to 127 (of the second).
-    constexpr int W = D / 2;  // columns of X and of the outputs that a thread takes
-    const int xrow = quad * 32 + lane, col0 = wg * W;
-    const float *from = nullptr;
+    const float *from = nullptr;  // the entering state
     int from_t = 0;
-    float mul = 1.f;
     if constexpr (!STATE) {
         if (p.spans > 1) {
             from = j.spans + (span * pairs + pair) * cells;
@@ -282,43 +299,17 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
         } else if (j.s_in) {
             from = j.s_in + pair * cells;
             from_t = j.in_t;
-            if (j.first && q.len > 0) mul = power[1];
         }
     }
-    bool has_x = from != nullptr && chunks > 0;  // X is not 0
-    if (has_x) {
-#pragma unroll 1
-        for (int h = 0; h < W; h += 32) {
-            uint32_t r[32];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                const int col = col0 + h + i;
-                float v = 0.f;
-                if (xrow < da && col < dc) v = from_t ? from[(long long)col * da + xrow] : from[(long long)xrow * dc + col];
-                r[i] = __float_as_uint(mul == 1.f ? v : v * mul);
-            }
-            __syncwarp();
-            TC_ST32(mine + L::tX + col0 + h, r);
-        }
-        tmem_st_wait();
-    }
-    uint32_t odd = 0;   // two bf16: NaN once an output was not finite
+    const bool enters = from != nullptr;
+    bool bad = false;   // something was not finite
     bool keeps = true;  // (STATE) no cut so far
-    const int step = step_of(xrow), slope = rev ? -1 : 1;
 
-#pragma unroll 1
-    for (int c = 0; c < chunks; ++c) {
-        const long long s0 = first + (long long)c * kChunk, t0 = begin_of(c);
-        const int rows = (int)min((long long)kChunk, stop - s0), slot = c & 1;
-        const uint32_t ta = base + L::a + slot * L::tile, tb = base + L::b + slot * L::tile, tv = base + L::c;
-        if constexpr (TMA) wait(barQK + 8 * slot, c >> 1);
-        else copy_wait<1>();
-        tc::fence_proxy_async_smem();
-        tc::fence_before_sync();
-        __syncthreads();  // the chunk before is read out
-        if constexpr (!STATE) {
-            if (warp == 0 && tc::elect_one()) {
-                tc::fence_after_sync();
+    if (!worker) {
+        // ---- one thread issues the products, and the copies
+        const auto form_a = [&](int c) {
+            const uint32_t ta = base + L::a + (c & 1) * L::tile, tb = base + L::b + (c & 1) * L::tile;
+            if (tc::elect_one()) {
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k)
                     tc::mma_bf16(tmem + L::tA, tc::desc_sw128(ta + (k / 4) * kPanel + (k % 4) * 32), tc::desc_sw128(tb + (k / 4) * kPanel + (k % 4) * 32),
@@ -326,49 +317,138 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
                 tc::mma_commit(barA);
             }
             __syncwarp();
-        }
-        if (c > 0) load_ab(c + 1);
-        // tokens that begin something new: what a token sees begins with the last of them up to it (counted in steps)
-        int keep_from = -1, begin = -1;
-        bool any_cut = false;
-        if constexpr (CUT) {
-            uint32_t cut[4];
+        };
+#pragma unroll 1
+        for (int c = 0; c < chunks; ++c) {
+            const int slot = c & 1;
+            const uint32_t ta = base + L::a + slot * L::tile, tb = base + L::b + slot * L::tile, tv = base + L::c;
+            const bool has_x = enters || c > 0;
+            if (TMA && !(early && c > 0)) wait(barQK + 8 * slot, c >> 1);
+            tc::fence_before_sync();
+            __syncthreads();  // 1: the chunk before is read out
+            tc::fence_after_sync();
+            if (!STATE && !(early && c > 0)) form_a(c);
+            if (TMA && c > 0) load_ab(c + 1);
+            tc::fence_before_sync();
+            __syncthreads();  // 2: A is read, Xb there
+            tc::fence_after_sync();
+            if (!STATE && has_x && tc::elect_one()) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) cut[i] = cuts[slot * 4 + i];
-            any_cut = (cut[0] | cut[1] | cut[2] | cut[3]) != 0;
-            if (any_cut) {
+                for (int k = 0; k < D / 16; ++k)
+                    tc::mma_bf16(tmem + L::tO2, tc::desc_sw128(ta + (k / 4) * kPanel + (k % 4) * 32), desc_mn(base + L::xb + k * 2048, D * 128),
+                                 tc::idesc_bf16_f32(128, D) | kBmn, k > 0);
+            }
+            __syncwarp();
+            bool keeps_x = true;
+            if constexpr (CUT) keeps_x = (cuts[slot * 4] | cuts[slot * 4 + 1] | cuts[slot * 4 + 2] | cuts[slot * 4 + 3]) == 0;
+            if constexpr (TMA) wait(barV, c);
+            tc::fence_before_sync();
+            __syncthreads();  // 3: P and the keys' parts are there
+            tc::fence_after_sync();
+            const bool onto = (STATE ? c > 0 : has_x) && keeps_x;
+            if (tc::elect_one()) {
+                if constexpr (!STATE) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (cut[i]) keep_from = 32 * i + 31 - __clz(cut[i]);  // (no cuts behind the last step)
-                    const uint32_t m = step / 32 > i ? cut[i] : step / 32 < i ? 0u : cut[i] & (~0u >> (31 - step % 32));
-                    if (m) begin = 32 * i + 31 - __clz(m);
+                    for (int k = 0; k < kChunk / 16; ++k)
+                        mma_bf16_ts(tmem + L::tO1, tmem + L::tA + k * 8, desc_mn(tv + k * 2048, kPanel), tc::idesc_bf16_f32(128, D) | kBmn, k > 0);
+                    tc::mma_commit(barO);
                 }
-            }
-        }
-        // (time's order, the last token of all: the state leaves as that token wrote it)
-        const int less = !STATE && j.first && s0 + rows == q.len ? 1 : 0;
-        if (tid < kChunk && (CUT || STATE || c == 0 || rows < kChunk || less)) {
-            float w = 0.f;
-            const int s = step_of(tid);
-            if (s < rows && s >= keep_from) {
-                if constexpr (STATE) w = decay_power(g, stop - s0 - s);  // up to the span's end
-                else w = power[rows - s - less];
-            }
-            w *= j.up_scale;
-            const float w1 = __bfloat162float(__float2bfloat16_rn(w));
-            kept[tid] = make_uint2(pack2(w1, w1), pack2(w - w1, w - w1));
-        }
-        if constexpr (!STATE) {
-            // X -> Xb, and X to what the next state keeps of it
-            if (has_x) {
-                const Pair shrink = twice(power[rows - less]);
+                // (D = 64: both parts as one operand of 128 rows)
 #pragma unroll
-                for (int h = 0; h < W; h += 32) {
+                for (int part = 0; part < D / 64; ++part)
+#pragma unroll
+                    for (int k = 0; k < kChunk / 16; ++k)
+                        tc::mma_bf16(tmem + L::tX, desc_mn((part ? base + L::lo : tb) + k * 2048, D == 64 ? base + L::lo - tb : kPanel),
+                                     desc_mn(tv + k * 2048, kPanel), tc::idesc_bf16_f32(128, D) | kAmn | kBmn, part > 0 || k > 0 || onto);
+                tc::mma_commit(barX);
+            }
+            __syncwarp();
+            if (early && c + 1 < chunks) {
+                wait(barQK + 8 * (slot ^ 1), (c + 1) >> 1);
+                form_a(c + 1);
+            }
+            if (TMA) {
+                wait(barX, c);
+                load_c(c + 1);
+            }
+        }
+    } else {
+        const uint32_t mine = tmem + ((uint32_t)(quad * 32) << 16);
+        // The entering state into TMEM: row a thread's lane, 32 columns a thread.  With D = 64 the state is the sum of lanes 0
+        // to 63 (sums of the keys' first parts) and 64 to 127 (of the second).
+        const int xrow = quad * 32 + lane, group = warp >> 2, col0 = group * 32;
+        if (enters && chunks > 0) {
+            const float mul = p.spans == 1 && j.first ? power[1] : 1.f;
+            uint32_t r[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) {
+                const int col = col0 + i;
+                float v = 0.f;
+                if (xrow < da && col < dc) v = from_t ? from[(long long)col * da + xrow] : from[(long long)xrow * dc + col];
+                r[i] = __float_as_uint(mul == 1.f ? v : v * mul);
+            }
+            __syncwarp();
+            TC_ST32(mine + L::tX + col0, r);
+            tmem_st_wait();
+        }
+        uint32_t odd = 0;  // two bf16: NaN once an output was not finite
+        const int step = step_of(xrow), slope = rev ? -1 : 1;
+
+#pragma unroll 1
+        for (int c = 0; c < chunks; ++c) {
+            const long long s0 = first + (long long)c * kChunk, t0 = begin_of(c);
+            const int rows = (int)min((long long)kChunk, stop - s0), slot = c & 1;
+            const uint32_t ta = base + L::a + slot * L::tile, tb = base + L::b + slot * L::tile, tv = base + L::c;
+            const bool has_x = enters || c > 0;
+            if constexpr (!TMA) copy_wait<1>();
+            if constexpr (!STATE) tma_store_read();  // (the outputs' copies have read a's tile, which is filled again)
+            tc::fence_proxy_async_smem();
+            tc::fence_before_sync();
+            __syncthreads();  // 1
+            tc::fence_after_sync();
+            if (!TMA && c > 0) load_ab(c + 1);
+            // tokens that begin something new: what a token sees begins with the last of them up to it (counted in steps)
+            int keep_from = -1, begin = -1;
+            bool any_cut = false;
+            if constexpr (CUT) {
+                uint32_t cut[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) cut[i] = cuts[slot * 4 + i];
+                any_cut = (cut[0] | cut[1] | cut[2] | cut[3]) != 0;
+                if (any_cut) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (cut[i]) keep_from = 32 * i + 31 - __clz(cut[i]);  // (no cuts behind the last step)
+                        const uint32_t m = step / 32 > i ? cut[i] : step / 32 < i ? 0u : cut[i] & (~0u >> (31 - step % 32));
+                        if (m) begin = 32 * i + 31 - __clz(m);
+                    }
+                }
+                if constexpr (STATE) keeps = keeps && keep_from < 0;
+            }
+            // (time's order, the last token of all: the state leaves as that token wrote it)
+            const int less = !STATE && j.first && s0 + rows == q.len ? 1 : 0;
+            if (tid < kChunk && (CUT || STATE || c == 0 || rows < kChunk || less)) {
+                float w = 0.f;
+                const int s = step_of(tid);
+                if (s < rows && s >= keep_from) {
+                    if constexpr (STATE) w = decay_power(g, stop - s0 - s);  // up to the span's end
+                    else w = power[rows - s - less];
+                }
+                w *= j.up_scale;
+                const float w1 = __bfloat162float(__float2bfloat16_rn(w));
+                kept[tid] = make_uint2(pack2(w1, w1), pack2(w - w1, w - w1));
+            }
+            constexpr int cols = 128 / (D / 32);  // of A, a thread
+            uint32_t packed[cols / 2];
+            if constexpr (!STATE) {
+                // X -> Xb, and X to what the next state keeps of it
+                if (has_x) {
+                    const Pair shrink = twice(power[rows - less]);
                     uint32_t r[32];
-                    const int col = col0 + h, row = D == 64 ? xrow & 63 : xrow;
-                    const uint32_t to = base + L::xb + (col / 64) * (D * 128) + row * 128;
-                    const auto place = [&](int i) { return to + (((((col + i) % 64) / 8) ^ (row & 7)) << 4); };
-                    TC_LD32(mine + L::tX + col, r);
+                    const int row = D == 64 ? xrow & 63 : xrow;
+                    const uint32_t to = base + L::xb + (col0 / 64) * (D * 128) + row * 128;
+                    const auto place = [&](int i) { return to + ((((col0 % 64 + i) / 8) ^ (row & 7)) << 4); };
+                    TC_LD32(mine + L::tX + col0, r);
                     tc::tmem_ld_wait();
                     if constexpr (D == 64) {  // the second parts come by way of Xb's place
                         if (quad >= 2) {
@@ -379,7 +459,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
                                              "r"(pack2(f[4], f[5])), "r"(pack2(f[6], f[7])) : "memory");
                             }
                         }
-                        pair_barrier(1 + wg * 2 + (quad & 1));
+                        pair_barrier(1 + group * 2 + (quad & 1));
                     }
                     if (D == 128 || quad < 2) {
 #pragma unroll
@@ -410,142 +490,110 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
                             r[i + 1] = __float_as_uint(v.f.y);
                         }
                         __syncwarp();
-                        TC_ST32(mine + L::tX + col, r);
+                        TC_ST32(mine + L::tX + col0, r);
                     }
+                    tmem_st_wait();
                 }
-                tmem_st_wait();
-            }
-            // A -> P: row xrow, 64 columns a warpgroup, in blocks of 32
-            wait(barA, c);
-            uint32_t packed[32];
+                // A -> P: row xrow, blocks of 32 columns
+                wait(barA, c);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int block = wg * 2 + h, j0 = block * 32;
-                if (rev ? block < quad : block > quad) {  // not seen
+                for (int h = 0; h < cols / 32; ++h) {
+                    const int block = group * (cols / 32) + h, j0 = block * 32;
+                    if (rev ? block < quad : block > quad) {  // not seen
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) packed[h * 16 + i] = 0u;
-                    continue;
-                }
-                uint32_t v[32];
-                TC_LD32(mine + L::tA + j0, v);
-                tc::tmem_ld_wait();
-                if (block == quad) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        const int away = slope * (lane - i);
-                        const float f = __uint_as_float(v[i]) * (j.w_scale * power[max(away, 0)]);
-                        v[i] = away >= 0 ? __float_as_uint(f) : 0u;
+                        for (int i = 0; i < 16; ++i) packed[h * 16 + i] = 0u;
+                        continue;
                     }
-                } else {  // lambda^away in two factors, neither above 1
-                    const Pair w = twice(j.w_scale * power[rev ? j0 - xrow : xrow - j0 - 31]);
+                    uint32_t v[32];
+                    TC_LD32(mine + L::tA + j0, v);
+                    tc::tmem_ld_wait();
+                    if (block == quad) {
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        const float4 t = *reinterpret_cast<const float4 *>(fall + i);
-                        Pair t0, t1;
-                        t0.f = make_float2(t.x, t.y);
-                        t1.f = make_float2(t.z, t.w);
-                        t0 = mul2(pair_of(v[i], v[i + 1]), mul2(t0, w));
-                        t1 = mul2(pair_of(v[i + 2], v[i + 3]), mul2(t1, w));
-                        v[i] = __float_as_uint(t0.f.x), v[i + 1] = __float_as_uint(t0.f.y);
-                        v[i + 2] = __float_as_uint(t1.f.x), v[i + 3] = __float_as_uint(t1.f.y);
+                        for (int i = 0; i < 32; ++i) {
+                            const int away = slope * (lane - i);
+                            const float f = __uint_as_float(v[i]) * (j.w_scale * power[max(away, 0)]);
+                            v[i] = away >= 0 ? __float_as_uint(f) : 0u;
+                        }
+                    } else {  // lambda^away in two factors, neither above 1
+                        const Pair w = twice(j.w_scale * power[rev ? j0 - xrow : xrow - j0 - 31]);
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) {
+                            const float4 t = *reinterpret_cast<const float4 *>(fall + i);
+                            Pair t0, t1;
+                            t0.f = make_float2(t.x, t.y);
+                            t1.f = make_float2(t.z, t.w);
+                            t0 = mul2(pair_of(v[i], v[i + 1]), mul2(t0, w));
+                            t1 = mul2(pair_of(v[i + 2], v[i + 3]), mul2(t1, w));
+                            v[i] = __float_as_uint(t0.f.x), v[i + 1] = __float_as_uint(t0.f.y);
+                            v[i + 2] = __float_as_uint(t1.f.x), v[i + 3] = __float_as_uint(t1.f.y);
+                        }
                     }
-                }
-                if (CUT && any_cut) {
+                    if (CUT && any_cut) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = step_of(j0 + i) >= begin ? v[i] : 0u;
-                }
+                        for (int i = 0; i < 32; ++i) v[i] = step_of(j0 + i) >= begin ? v[i] : 0u;
+                    }
 #pragma unroll
-                for (int i = 0; i < 16; ++i) packed[h * 16 + i] = pack2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+                    for (int i = 0; i < 16; ++i) packed[h * 16 + i] = pack2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+                }
             }
             tc::fence_proxy_async_smem();  // Xb
             tc::fence_before_sync();
-            __syncthreads();               // A is read: P and O2 may take its place
-            tc::fence_after_sync();
-            if (has_x && warp == 0 && tc::elect_one()) {
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k)
-                    tc::mma_bf16(tmem + L::tO2, tc::desc_sw128(ta + (k / 4) * kPanel + (k % 4) * 32), desc_mn(base + L::xb + k * 2048, D * 128),
-                                 tc::idesc_bf16_f32(128, D) | kBmn, k > 0);
-            }
-            __syncwarp();
-            TC_ST32(mine + L::tA + wg * 32, packed);
-        } else {
-            __syncthreads();  // kept
-        }
-        // b -> b w as two bf16 values, the first in b's place: with w = w1 + w2, hi = b w1 rounded, lo = (b w1 - hi) + b w2,
-        // where b w1 - hi is exact (16 bits of a product, the first 8 taken away)
-        {
-            constexpr int per = D / 8, stride = kThreads / per;
-            const int ch = tid % per, row0 = tid / per;
-            const uint32_t off = (ch / 8) * kPanel + row0 * 128 + (((ch & 7) ^ (row0 & 7)) << 4);
-#pragma unroll
-            for (int k = 0; k < kChunk / stride; ++k) {
-                const uint32_t to = off + k * stride * 128;
-                uint32_t v[4], hi[4], lo[4];
-                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(tb + to) : "memory");
-                const uint2 w = kept[row0 + k * stride];
-                if (TMA && rows < kChunk && step_of(row0 + k * stride) >= rows) v[0] = v[1] = v[2] = v[3] = 0u;  // (whatever lies there)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    hi[i] = hmul(v[i], w.x);
-                    lo[i] = hfma(v[i], w.y, hfma(v[i], w.x, hi[i] ^ 0x80008000u));
-                }
-                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(tb + to), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
-                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(base + L::lo + to), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
-            }
-        }
-        if constexpr (TMA) {
-            if (rows < kChunk) {  // values of steps that are not there: whatever lies there times 0 is to be 0
-                wait(barV, c);
-                constexpr int per = D / 8;
-                for (int i = tid; i < (kChunk - rows) * per; i += kThreads) {
-                    const int s = rows + i / per, ch = i % per, row = step_of(s);
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(tv + (ch / 8) * kPanel + row * 128 + (((ch & 7) ^ (row & 7)) << 4)), "r"(0) : "memory");
-                }
-            } else if (warp == 0) {
-                wait(barV, c);
-            }
-        } else {
-            copy_wait<1>();
-        }
-        if constexpr (!STATE) tmem_st_wait();
-        tc::fence_proxy_async_smem();
-        tc::fence_before_sync();
-        __syncthreads();
-        const bool onto = STATE ? c > 0 && keep_from < 0 : has_x && keep_from < 0;
-        if (warp == 0 && tc::elect_one()) {
+            __syncthreads();  // 2: A is read, P and O2 may take its place (STATE: kept is there)
             tc::fence_after_sync();
             if constexpr (!STATE) {
-#pragma unroll
-                for (int k = 0; k < kChunk / 16; ++k)
-                    mma_bf16_ts(tmem + L::tO1, tmem + L::tA + k * 8, desc_mn(tv + k * 2048, kPanel), tc::idesc_bf16_f32(128, D) | kBmn, k > 0);
-                tc::mma_commit(barO);
+                if constexpr (cols == 64) TC_ST32(mine + L::tA + group * 32, packed);
+                else TC_ST16(mine + L::tA + group * 16, packed);
             }
-            // (D = 64: both parts as one operand of 128 rows)
+            // b -> b w as two bf16 values, the first in b's place: with w = w1 + w2, hi = b w1 rounded, lo = (b w1 - hi) + b w2,
+            // where b w1 - hi is exact (16 bits of a product, the first 8 taken away)
+            {
+                constexpr int per = D / 8, stride = L::workers / per;
+                const int ch = tid % per, row0 = tid / per;
+                const uint32_t off = (ch / 8) * kPanel + row0 * 128 + (((ch & 7) ^ (row0 & 7)) << 4);
 #pragma unroll
-            for (int part = 0; part < D / 64; ++part)
+                for (int k = 0; k < kChunk / stride; ++k) {
+                    const uint32_t to = off + k * stride * 128;
+                    uint32_t v[4], hi[4], lo[4];
+                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(tb + to) : "memory");
+                    const uint2 w = kept[row0 + k * stride];
+                    if (TMA && rows < kChunk && step_of(row0 + k * stride) >= rows) v[0] = v[1] = v[2] = v[3] = 0u;  // (whatever lies there)
 #pragma unroll
-                for (int k = 0; k < kChunk / 16; ++k)
-                    tc::mma_bf16(tmem + L::tX, desc_mn((part ? base + L::lo : tb) + k * 2048, D == 64 ? base + L::lo - tb : kPanel),
-                                 desc_mn(tv + k * 2048, kPanel), tc::idesc_bf16_f32(128, D) | kAmn | kBmn, part > 0 || k > 0 || onto);
-            tc::mma_commit(barX);
-        }
-        __syncwarp();
-        if constexpr (STATE) keeps = keeps && keep_from < 0;
-        find_cuts(c + 1);
-        if constexpr (!STATE) {
-            // y = O1 + in_scale lambda^step O2, by way of a's tile to whole rows
-            const Pair w = twice(j.in_scale * power[step]);
-            const bool sees = !CUT || begin < 0, there = step < rows;
-            wait(barO, c);
-#pragma unroll
-            for (int h = 0; h < W; h += 32) {
+                    for (int i = 0; i < 4; ++i) {
+                        hi[i] = hmul(v[i], w.x);
+                        lo[i] = hfma(v[i], w.y, hfma(v[i], w.x, hi[i] ^ 0x80008000u));
+                    }
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(tb + to), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(base + L::lo + to), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
+                }
+            }
+            if constexpr (TMA) {
+                if (rows < kChunk) {  // values of steps that are not there: whatever lies there times 0 is to be 0
+                    wait(barV, c);
+                    constexpr int per = D / 8;
+                    for (int i = tid; i < (kChunk - rows) * per; i += L::workers) {
+                        const int s = rows + i / per, ch = i % per, row = step_of(s);
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(tv + (ch / 8) * kPanel + row * 128 + (((ch & 7) ^ (row & 7)) << 4)), "r"(0) : "memory");
+                    }
+                }
+            } else {
+                copy_wait<1>();
+            }
+            if constexpr (!STATE) tmem_st_wait();
+            tc::fence_proxy_async_smem();
+            tc::fence_before_sync();
+            __syncthreads();  // 3
+            find_cuts(c + 1);
+            if constexpr (!STATE) {
+                // y = O1 + in_scale lambda^step O2, by way of a's tile (32 rows of 64 bytes a warp, 64-byte swizzle) to whole rows
+                const Pair w = twice(j.in_scale * power[step]);
+                const bool sees = !CUT || begin < 0;
+                const uint32_t stage = ta + warp * 2048, own = stage + lane * 64, turn = (lane >> 1) & 3;
+                wait(barO, c);
                 uint32_t o1[32];
-                __syncwarp();
-                TC_LD32(mine + L::tO1 + col0 + h, o1);
+                TC_LD32(mine + L::tO1 + col0, o1);
                 if (has_x) {
                     uint32_t o2[32];
-                    TC_LD32(mine + L::tO2 + col0 + h, o2);
+                    TC_LD32(mine + L::tO2 + col0, o2);
                     tc::tmem_ld_wait();
                     if (sees) {
 #pragma unroll
@@ -559,49 +607,53 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
                 }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) o1[i] = pack2(__uint_as_float(o1[2 * i]), __uint_as_float(o1[2 * i + 1]));
-                if (there) {
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(own + (((i / 4) ^ turn) << 4)), "r"(o1[i]), "r"(o1[i + 1]), "r"(o1[i + 2]),
+                                 "r"(o1[i + 3]) : "memory");
+                if (step < rows) {
 #pragma unroll
                     for (int i = 0; i < 16; ++i) odd = hfma(o1[i], 0u, odd);
                 }
+                if (maps.stores && rows == kChunk) {
+                    tc::fence_proxy_async_smem();
+                    __syncwarp();
+                    if (lane == 0 && col0 < dc) tma_store_4d(&maps.out[job], stage, col0, (int)t0 + quad * 32, n, head);
+                } else {
+                    __syncwarp();
+                    const int left = dc - col0 - lane % 4 * 8;
+#pragma unroll 1
+                    for (int k = 0; k < 4; ++k) {
+                        const int r = k * 8 + lane / 4, row = quad * 32 + r;
+                        uint32_t v[4];
+                        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                                     : "r"(stage + r * 64 + (((lane % 4) ^ ((r >> 1) & 3)) << 4)) : "memory");
+                        if (step_of(row) < rows && left > 0) {
+                            bf16 *const out = py + (t0 + row) * j.y.t + col0 + lane % 4 * 8;
+                            if (j.vec > 1) {
+                                *reinterpret_cast<uint4 *>(out) = make_uint4(v[0], v[1], v[2], v[3]);
+                            } else {
 #pragma unroll
-                for (int i = 0; i < 16; i += 4) {
-                    const int col = col0 + h + 2 * i;
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(ta + (col / 64) * kPanel + xrow * 128 + ((((col % 64) / 8) ^ (xrow & 7)) << 4)),
-                                 "r"(o1[i]), "r"(o1[i + 1]), "r"(o1[i + 2]), "r"(o1[i + 3]) : "memory");
-                }
-            }
-            __syncwarp();
-            // a warp's 32 rows, W / 8 pieces of 16 bytes each
-            constexpr int per = W / 8, at_once = 32 / per;
-            const int ch = col0 / 8 + lane % per, left = dc - ch * 8;
-#pragma unroll
-            for (int k = 0; k < 32 / at_once; ++k) {
-                const int row = quad * 32 + k * at_once + lane / per;
-                uint32_t v[4];
-                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
-                             : "r"(ta + (ch / 8) * kPanel + row * 128 + (((ch & 7) ^ (row & 7)) << 4)) : "memory");
-                if (step_of(row) < rows && left > 0) {
-                    bf16 *const out = py + (t0 + row) * j.y.t + ch * 8;
-                    if (TMA || j.vec > 1) {
-                        *reinterpret_cast<uint4 *>(out) = make_uint4(v[0], v[1], v[2], v[3]);
-                    } else {
-#pragma unroll
-                        for (int m = 0; m < 8; ++m)
-                            if (m < left) reinterpret_cast<unsigned short *>(out)[m] = (unsigned short)(v[m / 2] >> (16 * (m & 1)));
+                                for (int m = 0; m < 8; ++m)
+                                    if (m < left) reinterpret_cast<unsigned short *>(out)[m] = (unsigned short)(v[m / 2] >> (16 * (m & 1)));
+                            }
+                        }
                     }
                 }
             }
+            wait(barX, c);
+            if (!TMA) load_c(c + 1);
         }
-        wait(barX, c);
-        has_x = true;
-        load_c(c + 1);
+        bad = (odd & 0x7fff7fffu) != 0;  // (a product with 0 is 0 or NaN)
+        if constexpr (!STATE) tma_store_read();
+        if constexpr (!TMA) copy_wait<0>();
     }
 
     // outputs of padding
     if constexpr (!STATE) {
         const long long pad = max(first, min(q.len, last));
-        const bool wide = TMA || j.vec > 1;
-        const int per = wide ? dc / 8 : dc, at_once = kThreads / per, r0 = tid / per, c0 = tid - r0 * per;
+        const bool wide = j.vec > 1;
+        const int per = wide ? dc / 8 : dc, at_once = L::threads / per, r0 = tid / per, c0 = tid - r0 * per;
         if (r0 < at_once)
             for (long long r = pad + r0; r < last; r += at_once) {
                 if (wide) *reinterpret_cast<uint4 *>(py + r * j.y.t + c0 * 8) = make_uint4(0, 0, 0, 0);
@@ -618,30 +670,27 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
         if ((q.len > first && q.len <= last) || (q.len == 0 && span == 0)) to = j.s_out + pair * cells;
         empty = j.out_zero && q.len > 0 && p.reset && p.reset[n] != 0;
     }
-    if constexpr (!TMA) copy_wait<0>();
     if (chunks > 0) {
         // by way of shared memory (a's tiles, and c's behind them, are done with) to whole rows
-        bool bad = (odd & 0x7fff7fffu) != 0;  // (a product with 0 is 0 or NaN)
         float *const x = reinterpret_cast<float *>(smem + L::a);
         constexpr int ld = D + 1;
+        const int xrow = quad * 32 + lane, col0 = (warp >> 2) * 32;
+        tc::fence_before_sync();
         __syncthreads();
+        tc::fence_after_sync();
 #pragma unroll 1
         for (int part = D == 64; part >= 0; --part) {  // D = 64: lanes 64 and up, then the others onto them
-            if (D == 128 || (quad >= 2) == (part == 1)) {
-#pragma unroll 1
-                for (int h = 0; h < W; h += 32) {
-                    uint32_t r[32];
-                    __syncwarp();
-                    TC_LD32(mine + L::tX + col0 + h, r);
-                    tc::tmem_ld_wait();
-                    float *const at = x + (D == 64 ? xrow & 63 : xrow) * ld + col0 + h;
+            if (worker && (D == 128 || (quad >= 2) == (part == 1))) {
+                uint32_t r[32];
+                TC_LD32(tmem + ((uint32_t)(quad * 32) << 16) + L::tX + col0, r);
+                tc::tmem_ld_wait();
+                float *const at = x + (D == 64 ? xrow & 63 : xrow) * ld + col0;
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) at[i] = __uint_as_float(r[i]) + (D == 64 && part == 0 ? at[i] : 0.f);
-                }
+                for (int i = 0; i < 32; ++i) at[i] = __uint_as_float(r[i]) + (D == 64 && part == 0 ? at[i] : 0.f);
             }
             __syncthreads();
         }
-        for (int r = warp; r < da; r += kThreads / 32)
+        for (int r = warp; r < da; r += L::threads / 32)
             for (int k = lane; k < dc; k += 32) {
                 const float v = x[r * ld + k];
                 bad |= !(fabsf(v) <= 3.4028235e38f);
@@ -654,7 +703,7 @@ __global__ void __launch_bounds__(kThreads, D == 64 ? 2 : 1) decay_tc_kernel(con
                     if (p.job[i].spans_t) decay_mark(p, i, pair);
         }
     } else if (to) {
-        for (long long i = tid; i < cells; i += kThreads) {
+        for (long long i = tid; i < cells; i += L::threads) {
             const long long r = i / dc, k = i % dc;
             to[i] = empty || !from ? 0.f : from_t ? from[k * da + r] : from[i];
         }
@@ -676,9 +725,9 @@ encode_fn encoder() {
     return fn;
 }
 
-// A map of [T, N, H, dim] whose box is 128 tokens x 64 values of one head; false where a map cannot say it (an axis that is
-// broadcast, strides that are not multiples of 16 bytes).
-bool make_map(CUtensorMap *m, const decay_array &v, long long T, int N, int H, int dim) {
+// A map of [T, N, H, dim] whose box is 128 tokens x 64 values of one head (of outputs, 32 x 32); false where a map cannot say it
+// (an axis that is broadcast, strides that are not multiples of 16 bytes).
+bool make_map(CUtensorMap *m, const decay_array &v, long long T, int N, int H, int dim, bool out) {
     const long long sizes[3] = {T, N, H}, strides[3] = {v.t, v.n, v.h};
     cuuint64_t dims[4] = {(cuuint64_t)dim, (cuuint64_t)T, (cuuint64_t)N, (cuuint64_t)H}, bytes[3];
     for (int i = 0; i < 3; ++i) {
@@ -686,9 +735,9 @@ bool make_map(CUtensorMap *m, const decay_array &v, long long T, int N, int H, i
         if (sizes[i] > 1 && (strides[i] == 0 || strides[i] >= (1ll << 38) || bytes[i] % 16)) return false;
     }
     if ((uintptr_t)v.p % 16 || !encoder()) return false;
-    const cuuint32_t box[4] = {64, kChunk, 1, 1}, one[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {out ? 32u : 64u, out ? 32u : (cuuint32_t)kChunk, 1, 1}, one[4] = {1, 1, 1, 1};
     return encoder()(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(v.p), dims, bytes, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                     CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+                     out ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 }  // namespace
@@ -701,8 +750,11 @@ void wm_seq_decay_tc_maps(const seq_decay_args &a, const decay_pass &p, decay_ma
     for (int i = 0; i < p.jobs; ++i) maps.use = maps.use && p.job[i].vec > 1;
     for (int i = 0; i < (p.jobs > 1 ? 4 : 3) && maps.use; ++i) {
         const wm_seq_heads &v = *arrays[i];
-        maps.use = make_map(&maps.m[i], {v.data, v.stride_t, v.stride_n, v.stride_h}, a.T, a.N, a.H, i < 2 ? a.Dk : a.Dv);
+        maps.use = make_map(&maps.in[i], {v.data, v.stride_t, v.stride_n, v.stride_h}, a.T, a.N, a.H, i < 2 ? a.Dk : a.Dv, false);
     }
+    maps.stores = 1;
+    for (int i = 0; i < p.jobs && maps.stores; ++i)
+        maps.stores = p.job[i].vec > 1 && make_map(&maps.out[i], p.job[i].y, a.T, a.N, a.H, p.job[i].dc, true);
 }
 
 namespace {
@@ -710,7 +762,7 @@ template <int D, bool STATE, bool TMA, bool CUT>
 cudaError_t launch(const decay_pass &p, const decay_maps &maps, unsigned grid, cudaStream_t s) {
     const cudaError_t e = cudaFuncSetAttribute(decay_tc_kernel<D, STATE, TMA, CUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan<D>::bytes);
     if (e != cudaSuccess) return e;
-    decay_tc_kernel<D, STATE, TMA, CUT><<<dim3(grid, p.spans), kThreads, Plan<D>::bytes, s>>>(p, maps);
+    decay_tc_kernel<D, STATE, TMA, CUT><<<dim3(grid, p.spans), Plan<D>::threads, Plan<D>::bytes, s>>>(p, maps);
     return cudaGetLastError();
 }
 template <int D, bool STATE>
