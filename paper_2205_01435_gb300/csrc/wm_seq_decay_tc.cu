@@ -61,7 +61,7 @@ struct Plan {
     // (lo lies behind b: with D = 64 both are one operand of 128 rows)
     static constexpr int xb = 0, b = xb + D * 128 * (D / 64), lo = b + 2 * tile, a = lo + tile, c = a + 2 * tile, end = c + tile;
     static constexpr int small = end;  // tables and barriers
-    static constexpr int bytes = small + 4 * (132 + 32) + 8 * 128 + 48 + 48 + 1024;
+    static constexpr int bytes = small + 4 * 132 + 8 * 128 + 48 + 48 + 1024;
     // P lies over A's first columns; with D = 64 O2 over A's others
     static constexpr int tA = 0, tO1 = 128, tO2 = D == 64 ? 64 : 256, tX = D == 64 ? 192 : 384, columns = D == 64 ? 256 : 512;
 };
@@ -181,9 +181,9 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
     extern __shared__ unsigned char raw[];
     unsigned char *smem = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
     const uint32_t base = tc::smem_u32(smem);
-    float *const power = reinterpret_cast<float *>(smem + L::small);        // lambda^0 .. lambda^128
-    float *const fall = power + 132;                                        // a block's columns: lambda^(31-i), or lambda^i in reverse
-    uint2 *const kept = reinterpret_cast<uint2 *>(fall + 32);               // the tokens' weights in the next state: two bf16, each twice
+    float *const power = reinterpret_cast<float *>(smem + L::small);         // lambda^0 .. lambda^128
+    float *const scales = power + 129;                                       // of products, of the entering state, of its update
+    uint2 *const kept = reinterpret_cast<uint2 *>(power + 132);              // the tokens' weights in the next state: two bf16, each twice
     uint32_t *const cuts = reinterpret_cast<uint32_t *>(kept + 128);        // [2][4]: tokens that begin something new
     volatile int *const late = reinterpret_cast<int *>(cuts + 8);           // a wait gave up
     uint32_t *const tmem_at = cuts + 9;
@@ -200,22 +200,24 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
     const int n = (int)(pair / p.H), head = (int)(pair % p.H), da = j.da, dc = j.dc;
     const decay_seq q = decay_open(p, j, n);
     const bool rev = q.reverse;
-    const long long pairs = (long long)p.N * p.H, cells = (long long)da * dc;
-    const long long first = span * p.span_tokens, last = min(p.T, first + p.span_tokens), stop = min(last, q.len);
-    const int chunks = stop > first ? (int)((stop - first + kChunk - 1) / kChunk) : 0;
+    const long long pairs = (long long)p.N * p.H;
+    const int cells = da * dc;
+    // (T is below 2^31 - 65536: tokens, and the ends of chunks and spans, are ints)
+    const int len = (int)q.len, first = (int)(span * p.span_tokens), last = (int)min(p.T, span * p.span_tokens + p.span_tokens), stop = min(last, len);
+    const int chunks = stop > first ? (stop - first + kChunk - 1) / kChunk : 0;
     // Row r of a tile is token begin_of(c) + r; counted along the pass it is step step_of(r) of the chunk.
-    const auto begin_of = [&](int c) { return rev ? q.len - first - (long long)(c + 1) * kChunk : first + (long long)c * kChunk; };
+    const auto begin_of = [&](int c) { return rev ? len - first - (c + 1) * kChunk : first + c * kChunk; };
     const auto step_of = [&](int r) { return rev ? kChunk - 1 - r : r; };
 
     bf16 *const py = static_cast<bf16 *>(const_cast<void *>(j.y.p)) + n * j.y.n + head * j.y.h;
     // Loads of a chunk: by the issuing warp's one thread where TMA does them, by the workers otherwise.
     const auto load = [&](uint32_t dst, const decay_array &g, int map, int dim, int c, uint32_t bar) {
-        const long long t0 = begin_of(c);
+        const int t0 = begin_of(c);
         if constexpr (TMA) {
 #pragma unroll
-            for (int k = 0; k < D / 64; ++k) tma_load_4d(dst + k * kPanel, &maps.in[map], k * 64, (int)t0, n, head, bar);
+            for (int k = 0; k < D / 64; ++k) tma_load_4d(dst + k * kPanel, &maps.in[map], k * 64, t0, n, head, bar);
         } else {
-            const int rows = (int)min((long long)kChunk, stop - first - (long long)c * kChunk);
+            const int rows = min(kChunk, stop - first - c * kChunk);
             load_tile<D>(dst, static_cast<const bf16 *>(g.p) + n * g.n + head * g.h + t0 * g.t, g.t, rev ? kChunk - rows : 0, rev ? kChunk : rows, dim,
                          j.vec);
         }
@@ -251,7 +253,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
     };
     const auto find_cuts = [&](int c) {
         if (CUT && warp < 4) {
-            const long long s = first + (long long)c * kChunk + warp * 32 + lane;
+            const int s = first + c * kChunk + warp * 32 + lane;
             const unsigned m = __ballot_sync(~0u, c < chunks && s < stop && decay_cut(p, q, s, n));
             if (lane == 0) cuts[(c & 1) * 4 + warp] = m;
         }
@@ -284,7 +286,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
     const float g = p.log_decay[head];
     find_cuts(0);
     if (tid <= kChunk) power[tid] = decay_power(g, tid);
-    if (warp == 7) fall[lane] = decay_power(g, rev ? lane : 31 - lane);
+    if (tid < 3) scales[tid] = tid == 0 ? j.w_scale : tid == 1 ? j.in_scale : j.up_scale;
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
@@ -384,7 +386,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             for (int i = 0; i < 32; ++i) {
                 const int col = col0 + i;
                 float v = 0.f;
-                if (xrow < da && col < dc) v = from_t ? from[(long long)col * da + xrow] : from[(long long)xrow * dc + col];
+                if (xrow < da && col < dc) v = from_t ? from[col * da + xrow] : from[xrow * dc + col];
                 r[i] = __float_as_uint(mul == 1.f ? v : v * mul);
             }
             __syncwarp();
@@ -392,12 +394,11 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             tmem_st_wait();
         }
         uint32_t odd = 0;  // two bf16: NaN once an output was not finite
-        const int step = step_of(xrow), slope = rev ? -1 : 1;
+        const int step = step_of(xrow);
 
 #pragma unroll 1
         for (int c = 0; c < chunks; ++c) {
-            const long long s0 = first + (long long)c * kChunk, t0 = begin_of(c);
-            const int rows = (int)min((long long)kChunk, stop - s0), slot = c & 1;
+            const int s0 = first + c * kChunk, t0 = begin_of(c), rows = min(kChunk, stop - s0), slot = c & 1;
             const uint32_t ta = base + L::a + slot * L::tile, tb = base + L::b + slot * L::tile, tv = base + L::c;
             const bool has_x = enters || c > 0;
             if constexpr (!TMA) copy_wait<1>();
@@ -426,7 +427,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 if constexpr (STATE) keeps = keeps && keep_from < 0;
             }
             // (time's order, the last token of all: the state leaves as that token wrote it)
-            const int less = !STATE && j.first && s0 + rows == q.len ? 1 : 0;
+            const int less = !STATE && j.first && s0 + rows == len ? 1 : 0;
             if (tid < kChunk && (CUT || STATE || c == 0 || rows < kChunk || less)) {
                 float w = 0.f;
                 const int s = step_of(tid);
@@ -434,7 +435,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                     if constexpr (STATE) w = decay_power(g, stop - s0 - s);  // up to the span's end
                     else w = power[rows - s - less];
                 }
-                w *= j.up_scale;
+                w *= scales[2];
                 const float w1 = __bfloat162float(__float2bfloat16_rn(w));
                 kept[tid] = make_uint2(pack2(w1, w1), pack2(w - w1, w - w1));
             }
@@ -462,17 +463,21 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                         pair_barrier(1 + group * 2 + (quad & 1));
                     }
                     if (D == 128 || quad < 2) {
+                        uint32_t e[16];
+                        if constexpr (D == 64) {
+#pragma unroll
+                            for (int i = 0; i < 16; i += 4)
+                                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(e[i]), "=r"(e[i + 1]), "=r"(e[i + 2]), "=r"(e[i + 3]) : "r"(place(2 * i)) : "memory");
+                        }
 #pragma unroll
                         for (int i = 0; i < 32; i += 8) {
                             const float *f = reinterpret_cast<const float *>(r + i);
                             float x[8];
                             if constexpr (D == 64) {
-                                uint32_t e[4];
-                                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(e[0]), "=r"(e[1]), "=r"(e[2]), "=r"(e[3]) : "r"(place(i)) : "memory");
 #pragma unroll
                                 for (int m = 0; m < 4; ++m) {
-                                    x[2 * m] = f[2 * m] + __uint_as_float(e[m] << 16);
-                                    x[2 * m + 1] = f[2 * m + 1] + __uint_as_float(e[m] & 0xffff0000u);
+                                    x[2 * m] = f[2 * m] + __uint_as_float(e[i / 2 + m] << 16);
+                                    x[2 * m + 1] = f[2 * m + 1] + __uint_as_float(e[i / 2 + m] & 0xffff0000u);
                                 }
                             } else {
 #pragma unroll
@@ -494,46 +499,70 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                     }
                     tmem_st_wait();
                 }
-                // A -> P: row xrow, blocks of 32 columns
+                // A -> P: row xrow, 16 columns at a time.  Weights lambda^away by products from the nearest column on: up to 16
+                // roundings of 2^-24, before one of 2^-8
                 wait(barA, c);
+                const float w_scale = scales[0], lambda = power[1];
 #pragma unroll
-                for (int h = 0; h < cols / 32; ++h) {
-                    const int block = group * (cols / 32) + h, j0 = block * 32;
+                for (int h = 0; h < cols / 16; ++h) {
+                    const int j0 = group * cols + h * 16, block = j0 / 32, i0 = j0 % 32;
                     if (rev ? block < quad : block > quad) {  // not seen
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) packed[h * 16 + i] = 0u;
+                        for (int i = 0; i < 8; ++i) packed[h * 8 + i] = 0u;
                         continue;
                     }
-                    uint32_t v[32];
-                    TC_LD32(mine + L::tA + j0, v);
+                    uint32_t v[16];
+                    TC_LD16(mine + L::tA + j0, v);
+                    const auto weigh = [&](int i, float a, float b) {
+                        Pair w;
+                        w.f = make_float2(a, b);
+                        w = mul2(pair_of(v[i], v[i + 1]), w);
+                        packed[h * 8 + i / 2] = pack2(w.f.x, w.f.y);
+                    };
+                    // (the weight of the column before the first of these, in the order they are taken)
+                    const int before = rev ? j0 - 1 - xrow : xrow - j0 - 16;
+                    float w = before >= 0 ? w_scale * power[before] : 0.f;
                     tc::tmem_ld_wait();
                     if (block == quad) {
+                        const int own = lane - i0;  // the token itself; columns behind it are not seen, whatever they hold
+                        if (!rev) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const int away = slope * (lane - i);
-                            const float f = __uint_as_float(v[i]) * (j.w_scale * power[max(away, 0)]);
-                            v[i] = away >= 0 ? __float_as_uint(f) : 0u;
+                            for (int i = 14; i >= 0; i -= 2) {
+                                const float b = i + 1 == own ? w_scale : w * lambda;
+                                w = i == own ? w_scale : b * lambda;
+                                v[i + 1] = i + 1 <= own ? v[i + 1] : 0u;
+                                v[i] = i <= own ? v[i] : 0u;
+                                weigh(i, w, b);
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 16; i += 2) {
+                                const float a = i == own ? w_scale : w * lambda;
+                                w = i + 1 == own ? w_scale : a * lambda;
+                                v[i] = i >= own ? v[i] : 0u;
+                                v[i + 1] = i + 1 >= own ? v[i + 1] : 0u;
+                                weigh(i, a, w);
+                            }
                         }
-                    } else {  // lambda^away in two factors, neither above 1
-                        const Pair w = twice(j.w_scale * power[rev ? j0 - xrow : xrow - j0 - 31]);
+                    } else {
+                        const Pair lambda2 = twice(lambda * lambda);
+                        Pair t;
+                        w *= lambda;
+                        if (!rev) {
+                            t.f = make_float2(w * lambda, w);
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4) {
-                            const float4 t = *reinterpret_cast<const float4 *>(fall + i);
-                            Pair t0, t1;
-                            t0.f = make_float2(t.x, t.y);
-                            t1.f = make_float2(t.z, t.w);
-                            t0 = mul2(pair_of(v[i], v[i + 1]), mul2(t0, w));
-                            t1 = mul2(pair_of(v[i + 2], v[i + 3]), mul2(t1, w));
-                            v[i] = __float_as_uint(t0.f.x), v[i + 1] = __float_as_uint(t0.f.y);
-                            v[i + 2] = __float_as_uint(t1.f.x), v[i + 3] = __float_as_uint(t1.f.y);
+                            for (int i = 14; i >= 0; i -= 2, t = mul2(t, lambda2)) weigh(i, t.f.x, t.f.y);
+                        } else {
+                            t.f = make_float2(w, w * lambda);
+#pragma unroll
+                            for (int i = 0; i < 16; i += 2, t = mul2(t, lambda2)) weigh(i, t.f.x, t.f.y);
                         }
                     }
                     if (CUT && any_cut) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = step_of(j0 + i) >= begin ? v[i] : 0u;
+                        for (int i = 0; i < 8; ++i)
+                            packed[h * 8 + i] &= (step_of(j0 + 2 * i) >= begin ? 0xffffu : 0u) | (step_of(j0 + 2 * i + 1) >= begin ? 0xffff0000u : 0u);
                     }
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) packed[h * 16 + i] = pack2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
                 }
             }
             tc::fence_proxy_async_smem();  // Xb
@@ -550,17 +579,23 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 constexpr int per = D / 8, stride = L::workers / per;
                 const int ch = tid % per, row0 = tid / per;
                 const uint32_t off = (ch / 8) * kPanel + row0 * 128 + (((ch & 7) ^ (row0 & 7)) << 4);
+                constexpr int turns = kChunk / stride;
+                uint32_t v[turns][4];
+                uint2 w[turns];
 #pragma unroll
-                for (int k = 0; k < kChunk / stride; ++k) {
+                for (int k = 0; k < turns; ++k) {
+                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[k][0]), "=r"(v[k][1]), "=r"(v[k][2]), "=r"(v[k][3]) : "r"(tb + off + k * stride * 128) : "memory");
+                    w[k] = kept[row0 + k * stride];
+                }
+#pragma unroll
+                for (int k = 0; k < turns; ++k) {
                     const uint32_t to = off + k * stride * 128;
-                    uint32_t v[4], hi[4], lo[4];
-                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(tb + to) : "memory");
-                    const uint2 w = kept[row0 + k * stride];
-                    if (TMA && rows < kChunk && step_of(row0 + k * stride) >= rows) v[0] = v[1] = v[2] = v[3] = 0u;  // (whatever lies there)
+                    uint32_t hi[4], lo[4];
+                    if (TMA && rows < kChunk && step_of(row0 + k * stride) >= rows) v[k][0] = v[k][1] = v[k][2] = v[k][3] = 0u;  // (whatever lies there)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        hi[i] = hmul(v[i], w.x);
-                        lo[i] = hfma(v[i], w.y, hfma(v[i], w.x, hi[i] ^ 0x80008000u));
+                        hi[i] = hmul(v[k][i], w[k].x);
+                        lo[i] = hfma(v[k][i], w[k].y, hfma(v[k][i], w[k].x, hi[i] ^ 0x80008000u));
                     }
                     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(tb + to), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
                     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(base + L::lo + to), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
@@ -585,9 +620,9 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             find_cuts(c + 1);
             if constexpr (!STATE) {
                 // y = O1 + in_scale lambda^step O2, by way of a's tile (32 rows of 64 bytes a warp, 64-byte swizzle) to whole rows
-                const Pair w = twice(j.in_scale * power[step]);
                 const bool sees = !CUT || begin < 0;
                 const uint32_t stage = ta + warp * 2048, own = stage + lane * 64, turn = (lane >> 1) & 3;
+                const Pair w = twice(scales[1] * power[step]);
                 wait(barO, c);
                 uint32_t o1[32];
                 TC_LD32(mine + L::tO1 + col0, o1);
@@ -611,14 +646,10 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 for (int i = 0; i < 16; i += 4)
                     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(own + (((i / 4) ^ turn) << 4)), "r"(o1[i]), "r"(o1[i + 1]), "r"(o1[i + 2]),
                                  "r"(o1[i + 3]) : "memory");
-                if (step < rows) {
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) odd = hfma(o1[i], 0u, odd);
-                }
                 if (maps.stores && rows == kChunk) {
                     tc::fence_proxy_async_smem();
                     __syncwarp();
-                    if (lane == 0 && col0 < dc) tma_store_4d(&maps.out[job], stage, col0, (int)t0 + quad * 32, n, head);
+                    if (lane == 0 && col0 < dc) tma_store_4d(&maps.out[job], stage, col0, t0 + quad * 32, n, head);
                 } else {
                     __syncwarp();
                     const int left = dc - col0 - lane % 4 * 8;
@@ -629,7 +660,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                         asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
                                      : "r"(stage + r * 64 + (((lane % 4) ^ ((r >> 1) & 3)) << 4)) : "memory");
                         if (step_of(row) < rows && left > 0) {
-                            bf16 *const out = py + (t0 + row) * j.y.t + col0 + lane % 4 * 8;
+                            bf16 *const out = py + (long long)(t0 + row) * j.y.t + col0 + lane % 4 * 8;
                             if (j.vec > 1) {
                                 *reinterpret_cast<uint4 *>(out) = make_uint4(v[0], v[1], v[2], v[3]);
                             } else {
@@ -639,6 +670,10 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                             }
                         }
                     }
+                }
+                if (step < rows) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) odd = hfma(o1[i], 0u, odd);
                 }
             }
             wait(barX, c);
@@ -651,13 +686,13 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
 
     // outputs of padding
     if constexpr (!STATE) {
-        const long long pad = max(first, min(q.len, last));
+        const int pad = max(first, stop);
         const bool wide = j.vec > 1;
         const int per = wide ? dc / 8 : dc, at_once = L::threads / per, r0 = tid / per, c0 = tid - r0 * per;
         if (r0 < at_once)
-            for (long long r = pad + r0; r < last; r += at_once) {
-                if (wide) *reinterpret_cast<uint4 *>(py + r * j.y.t + c0 * 8) = make_uint4(0, 0, 0, 0);
-                else py[r * j.y.t + c0] = __float2bfloat16_rn(0.f);
+            for (int r = pad + r0; r < last; r += at_once) {
+                if (wide) *reinterpret_cast<uint4 *>(py + (long long)r * j.y.t + c0 * 8) = make_uint4(0, 0, 0, 0);
+                else py[(long long)r * j.y.t + c0] = __float2bfloat16_rn(0.f);
             }
     }
     // what leaves: the span's part, or the state itself (of the span that holds the sequence's end)
@@ -665,10 +700,10 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
     bool empty = false;
     if constexpr (STATE) {
         to = j.spans + (span * pairs + pair) * cells;
-        if (tid == 0) p.carry[((long long)span * 2 + j.reverse) * pairs + pair] = !keeps ? 0.f : decay_power(g, max(0ll, stop - first));
+        if (tid == 0) p.carry[((long long)span * 2 + j.reverse) * pairs + pair] = !keeps ? 0.f : decay_power(g, max(0, stop - first));
     } else if (j.s_out) {
-        if ((q.len > first && q.len <= last) || (q.len == 0 && span == 0)) to = j.s_out + pair * cells;
-        empty = j.out_zero && q.len > 0 && p.reset && p.reset[n] != 0;
+        if ((len > first && len <= last) || (len == 0 && span == 0)) to = j.s_out + pair * cells;
+        empty = j.out_zero && len > 0 && p.reset && p.reset[n] != 0;
     }
     if (chunks > 0) {
         // by way of shared memory (a's tiles, and c's behind them, are done with) to whole rows
@@ -694,7 +729,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             for (int k = lane; k < dc; k += 32) {
                 const float v = x[r * ld + k];
                 bad |= !(fabsf(v) <= 3.4028235e38f);
-                if (to) to[(long long)r * dc + k] = empty ? 0.f : v;
+                if (to) to[r * dc + k] = empty ? 0.f : v;
             }
         if (bad) {
             decay_mark(p, job, pair);
@@ -703,8 +738,8 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                     if (p.job[i].spans_t) decay_mark(p, i, pair);
         }
     } else if (to) {
-        for (long long i = tid; i < cells; i += L::threads) {
-            const long long r = i / dc, k = i % dc;
+        for (int i = tid; i < cells; i += L::threads) {
+            const int r = i / dc, k = i % dc;
             to[i] = empty || !from ? 0.f : from_t ? from[k * da + r] : from[i];
         }
     }
