@@ -292,25 +292,48 @@ __global__ void __launch_bounds__(kThreads, 2) decay_chunk_kernel(const decay_pa
     for (long long i = blockIdx.x; i < items; i += gridDim.x) decay_chunks<T, STATE>(p, (int)i, smem, cuts);
 }
 
-// Spans' own parts -> what enters each span, along time.  A thread takes one cell of a state; jobs that form the spans.
+// Spans' own parts -> what enters each span, along time.  A thread takes one cell of a state (QUAD: four), the parts of 8
+// spans on their way at a time; jobs that form the spans.
+template <int QUAD>
 __global__ void __launch_bounds__(256) decay_join_kernel(const decay_pass p) {
     const decay_job &j = p.job[blockIdx.y];
     if (j.spans_t) return;
-    const long long cells = (long long)j.da * j.dc, pairs = (long long)p.N * p.H, i = (long long)blockIdx.x * 256 + threadIdx.x;
+    const long long cells = (long long)j.da * j.dc, pairs = (long long)p.N * p.H, i = ((long long)blockIdx.x * 256 + threadIdx.x) * QUAD;
     if (i >= cells * pairs) return;
     const long long pair = i / cells, cell = i % cells;
-    float x = 0.f;
+    float x[QUAD] = {};
     if (j.s_in) {
-        const long long r = cell / j.dc, c = cell % j.dc;
-        x = j.s_in[pair * cells + (j.in_t ? c * j.da + r : cell)];
         const int n = (int)(pair / p.H);
-        if (j.first && (!p.lengths || p.lengths[n] > 0)) x *= decay_power(p.log_decay[pair % p.H], 1);
+        const float mul = j.first && (!p.lengths || p.lengths[n] > 0) ? decay_power(p.log_decay[pair % p.H], 1) : 1.f;
+#pragma unroll
+        for (int k = 0; k < QUAD; ++k) {
+            const long long r = (cell + k) / j.dc, c = (cell + k) % j.dc;
+            x[k] = j.s_in[pair * cells + (j.in_t ? c * j.da + r : cell + k)];
+            if (mul != 1.f) x[k] *= mul;
+        }
     }
-    for (int s = 0; s < p.spans; ++s) {
-        float *at = j.spans + s * pairs * cells + i;
-        const float own = *at, c = p.carry[((long long)s * 2 + j.reverse) * pairs + pair];
-        *at = x;
-        x = c == 0.f ? own : x * c + own;
+    using V = seq_vec<float, QUAD>;
+    const float *const carry = p.carry + (long long)j.reverse * pairs + pair;
+    for (int s = 0; s < p.spans; s += 8) {
+        V own[8];
+        float c[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (s + k < p.spans) {
+                own[k] = seq_load<float, QUAD>(j.spans + (s + k) * pairs * cells + i);
+                c[k] = carry[(s + k) * 2 * pairs];
+            }
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (s + k < p.spans) {
+                V v;
+#pragma unroll
+                for (int h = 0; h < QUAD; ++h) {
+                    v.v[h] = x[h];
+                    x[h] = c[k] == 0.f ? own[k].v[h] : x[h] * c[k] + own[k].v[h];
+                }
+                seq_store<float, QUAD>(j.spans + (s + k) * pairs * cells + i, v);
+            }
     }
 }
 
@@ -580,10 +603,10 @@ cudaError_t run_pass(wm_seq *h, const seq_decay_args &a, decay_pass &p, bool tc,
     if (p.spans > 1) {
         e = tc ? wm_seq_decay_tc_launch(h, p, maps, true, s) : chunk_launch<T, true>(h, p, s);
         if (e != cudaSuccess) return e;
-        long long cells = 0;
-        for (int i = 0; i < p.jobs; ++i) cells = std::max(cells, pairs * p.job[i].da * p.job[i].dc);
+        const long long cells = pairs * a.Dk * a.Dv;
         ++h->last_launches;
-        decay_join_kernel<<<dim3((unsigned)((cells + 255) / 256), p.jobs), 256, 0, s>>>(p);
+        if ((long long)a.Dk * a.Dv % 4 == 0) decay_join_kernel<4><<<dim3((unsigned)((cells / 4 + 255) / 256), p.jobs), 256, 0, s>>>(p);
+        else decay_join_kernel<1><<<dim3((unsigned)((cells + 255) / 256), p.jobs), 256, 0, s>>>(p);
         if ((e = cudaGetLastError()) != cudaSuccess) return e;
     }
     if (!tc) return chunk_launch<T, false>(h, p, s);

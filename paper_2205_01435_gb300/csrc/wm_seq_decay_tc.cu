@@ -58,8 +58,8 @@ template <int D>
 struct Plan {
     static constexpr int workers = 4 * D, threads = workers + 32;  // 32 columns of the state and of the outputs a thread
     static constexpr int tile = kPanel * (D / 64);
-    // (lo lies behind b: with D = 64 both are one operand of 128 rows)
-    static constexpr int xb = 0, b = xb + D * 128 * (D / 64), lo = b + 2 * tile, a = lo + tile, c = a + 2 * tile, end = c + tile;
+    // (lo lies behind b: with D = 64 both are one operand of 128 rows; lo and xb also hold the state on its way in and out)
+    static constexpr int b = 0, lo = b + 2 * tile, xb = lo + tile, a = xb + D * 128 * (D / 64), c = a + 2 * tile, end = c + tile;
     static constexpr int small = end;  // tables and barriers
     static constexpr int bytes = small + 4 * 132 + 8 * 128 + 48 + 48 + 1024;
     // P lies over A's first columns; with D = 64 O2 over A's others
@@ -172,6 +172,36 @@ __device__ __forceinline__ void tma_store_4d(const CUtensorMap *map, uint32_t sr
 }
 __device__ __forceinline__ void tma_store_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void pair_barrier(int id) { asm volatile("bar.sync %0, 64;" ::"r"(id) : "memory"); }
+
+// A state in shared memory: rows of D / 4 quads, turned so that 8 rows' quads of one column lie in 8 places.
+template <int D>
+__device__ __forceinline__ int state_at(int r, int quad) {
+    return r * (D / 4) + (quad ^ (r & 7));
+}
+// A state [da, dc] of values (or, where rows and address allow, quads) into it, zeros around, by the workers.
+template <int D, class One, class Four>
+__device__ __forceinline__ void state_rows(float4 *x, int da, int dc, One one, Four four, bool aligned) {
+    for (int i = threadIdx.x; i < D * D / 4; i += Plan<D>::workers) {
+        const int r = i / (D / 4), k = i % (D / 4);
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (r < da && 4 * k < dc) {
+            const int at = r * dc + 4 * k;
+            if (aligned && dc % 4 == 0) {
+                v = four(at);
+            } else {
+                v.x = one(at);
+                if (4 * k + 1 < dc) v.y = one(at + 1);
+                if (4 * k + 2 < dc) v.z = one(at + 2);
+                if (4 * k + 3 < dc) v.w = one(at + 3);
+            }
+        }
+        x[state_at<D>(r, k)] = v;
+    }
+}
+template <int D>
+__device__ __forceinline__ void worker_barrier() {
+    asm volatile("bar.sync 5, %0;" ::"n"(Plan<D>::workers) : "memory");
+}
 
 // TMA: the inputs have tensor maps; CUT: there may be resets.
 template <int D, bool STATE, bool TMA, bool CUT>
@@ -304,6 +334,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
         }
     }
     const bool enters = from != nullptr;
+    float4 *const x = reinterpret_cast<float4 *>(smem + L::lo);  // a state on its way
     bool bad = false;   // something was not finite
     bool keeps = true;  // (STATE) no cut so far
 
@@ -382,12 +413,24 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
         if (enters && chunks > 0) {
             const float mul = p.spans == 1 && j.first ? power[1] : 1.f;
             uint32_t r[32];
+            if (from_t) {  // (a row of the state is a column there: lanes read side by side)
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                const int col = col0 + i;
-                float v = 0.f;
-                if (xrow < da && col < dc) v = from_t ? from[col * da + xrow] : from[xrow * dc + col];
-                r[i] = __float_as_uint(mul == 1.f ? v : v * mul);
+                for (int i = 0; i < 32; ++i) r[i] = xrow < da && col0 + i < dc ? __float_as_uint(from[(col0 + i) * da + xrow]) : 0u;
+            } else {
+                state_rows<D>(x, da, dc, [&](int at) { return from[at]; }, [&](int at) { return *reinterpret_cast<const float4 *>(from + at); },
+                              (uintptr_t)from % 16 == 0);
+                worker_barrier<D>();
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                    const float4 v = x[state_at<D>(xrow & (D - 1), (col0 + i) / 4)];
+                    const bool on = xrow < D;
+                    r[i] = on ? __float_as_uint(v.x) : 0u, r[i + 1] = on ? __float_as_uint(v.y) : 0u;
+                    r[i + 2] = on ? __float_as_uint(v.z) : 0u, r[i + 3] = on ? __float_as_uint(v.w) : 0u;
+                }
+            }
+            if (mul != 1.f) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * mul);
             }
             __syncwarp();
             TC_ST32(mine + L::tX + col0, r);
@@ -706,9 +749,6 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
         empty = j.out_zero && len > 0 && p.reset && p.reset[n] != 0;
     }
     if (chunks > 0) {
-        // by way of shared memory (a's tiles, and c's behind them, are done with) to whole rows
-        float *const x = reinterpret_cast<float *>(smem + L::a);
-        constexpr int ld = D + 1;
         const int xrow = quad * 32 + lane, col0 = (warp >> 2) * 32;
         tc::fence_before_sync();
         __syncthreads();
@@ -719,18 +759,34 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 uint32_t r[32];
                 TC_LD32(tmem + ((uint32_t)(quad * 32) << 16) + L::tX + col0, r);
                 tc::tmem_ld_wait();
-                float *const at = x + (D == 64 ? xrow & 63 : xrow) * ld + col0;
 #pragma unroll
-                for (int i = 0; i < 32; ++i) at[i] = __uint_as_float(r[i]) + (D == 64 && part == 0 ? at[i] : 0.f);
+                for (int i = 0; i < 32; i += 4) {
+                    float4 *const at = x + state_at<D>(xrow & (D - 1), (col0 + i) / 4);
+                    float4 v = make_float4(__uint_as_float(r[i]), __uint_as_float(r[i + 1]), __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
+                    if (D == 64 && part == 0) {
+                        const float4 o = *at;
+                        v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
+                    }
+                    *at = v;
+                }
             }
             __syncthreads();
         }
-        for (int r = warp; r < da; r += L::threads / 32)
-            for (int k = lane; k < dc; k += 32) {
-                const float v = x[r * ld + k];
-                bad |= !(fabsf(v) <= 3.4028235e38f);
-                if (to) to[r * dc + k] = empty ? 0.f : v;
+        if (dc % 4 == 0 && (uintptr_t)to % 16 == 0) {
+            for (int i = tid; i < da * (dc / 4); i += L::threads) {
+                const int r = i / (dc / 4), k = i - r * (dc / 4);
+                const float4 v = x[state_at<D>(r, k)];
+                bad |= !(fabsf(v.x) <= 3.4028235e38f && fabsf(v.y) <= 3.4028235e38f && fabsf(v.z) <= 3.4028235e38f && fabsf(v.w) <= 3.4028235e38f);
+                if (to) reinterpret_cast<float4 *>(to)[i] = empty ? make_float4(0.f, 0.f, 0.f, 0.f) : v;
             }
+        } else {
+            for (int i = tid; i < cells; i += L::threads) {
+                const int r = i / dc, k = i - r * dc;
+                const float v = reinterpret_cast<const float *>(x + state_at<D>(r, k / 4))[k % 4];
+                bad |= !(fabsf(v) <= 3.4028235e38f);
+                if (to) to[i] = empty ? 0.f : v;
+            }
+        }
         if (bad) {
             decay_mark(p, job, pair);
             if constexpr (STATE)
