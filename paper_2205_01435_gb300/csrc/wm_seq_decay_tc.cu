@@ -178,25 +178,69 @@ template <int D>
 __device__ __forceinline__ int state_at(int r, int quad) {
     return r * (D / 4) + (quad ^ (r & 7));
 }
-// A state [da, dc] of values (or, where rows and address allow, quads) into it, zeros around, by the workers.
-template <int D, class One, class Four>
-__device__ __forceinline__ void state_rows(float4 *x, int da, int dc, One one, Four four, bool aligned) {
-    for (int i = threadIdx.x; i < D * D / 4; i += Plan<D>::workers) {
-        const int r = i / (D / 4), k = i % (D / 4);
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (r < da && 4 * k < dc) {
-            const int at = r * dc + 4 * k;
-            if (aligned && dc % 4 == 0) {
-                v = four(at);
+// Its quads in the workers' hands: quad k of rows row0, row0 + 16, ...; 4 or 8 of them a thread.
+template <int D>
+struct Quads {
+    static constexpr int per = D / 4, turns = D * per / Plan<D>::workers, rows = Plan<D>::workers / per;
+    const int k = threadIdx.x % per, row0 = threadIdx.x / per;
+};
+// A state [da, dc] from memory, zeros around.  Whole quads where rows and address allow.
+template <int D>
+__device__ __forceinline__ void state_in(float4 *x, const float *from, int da, int dc) {
+    using Q = Quads<D>;
+    const Q q;
+    const bool wide = dc % 4 == 0 && (uintptr_t)from % 16 == 0;
+    float4 v[Q::turns];
+#pragma unroll
+    for (int i = 0; i < Q::turns; ++i) {
+        const int r = q.row0 + i * Q::rows, left = dc - 4 * q.k;
+        const float *const at = from + r * dc + 4 * q.k;
+        v[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (r < da && left > 0) {
+            if (wide) {
+                v[i] = *reinterpret_cast<const float4 *>(at);
             } else {
-                v.x = one(at);
-                if (4 * k + 1 < dc) v.y = one(at + 1);
-                if (4 * k + 2 < dc) v.z = one(at + 2);
-                if (4 * k + 3 < dc) v.w = one(at + 3);
+                v[i].x = at[0];
+                if (left > 1) v[i].y = at[1];
+                if (left > 2) v[i].z = at[2];
+                if (left > 3) v[i].w = at[3];
             }
         }
-        x[state_at<D>(r, k)] = v;
     }
+#pragma unroll
+    for (int i = 0; i < Q::turns; ++i) x[state_at<D>(q.row0 + i * Q::rows, q.k)] = v[i];
+}
+// And to memory (to = NULL: nowhere; empty: as zeros); true if a value is not finite.
+template <int D>
+__device__ __forceinline__ bool state_out(const float4 *x, float *to, int da, int dc, bool empty) {
+    using Q = Quads<D>;
+    const Q q;
+    const bool wide = dc % 4 == 0 && (uintptr_t)to % 16 == 0;
+    float odd = 0.f;
+#pragma unroll
+    for (int i = 0; i < Q::turns; ++i) {
+        const int r = q.row0 + i * Q::rows, left = dc - 4 * q.k;
+        if (r < da && left > 0) {
+            float4 v = x[state_at<D>(r, q.k)];
+            odd += v.x * 0.f;  // (values beyond the state's may be what they like)
+            if (left > 1) odd += v.y * 0.f;
+            if (left > 2) odd += v.z * 0.f;
+            if (left > 3) odd += v.w * 0.f;
+            if (to) {
+                if (empty) v = make_float4(0.f, 0.f, 0.f, 0.f);
+                float *const at = to + r * dc + 4 * q.k;
+                if (wide) {
+                    *reinterpret_cast<float4 *>(at) = v;
+                } else {
+                    at[0] = v.x;
+                    if (left > 1) at[1] = v.y;
+                    if (left > 2) at[2] = v.z;
+                    if (left > 3) at[3] = v.w;
+                }
+            }
+        }
+    }
+    return !(odd == 0.f);
 }
 template <int D>
 __device__ __forceinline__ void worker_barrier() {
@@ -221,73 +265,39 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quad = warp & 3;
     const bool worker = tid < L::workers;
-    int jobs = 0, at[3] = {};
+    int jobs = 0, job_at[3] = {};
     for (int i = 0; i < p.jobs; ++i)
-        if (!(STATE && p.job[i].spans_t)) at[jobs++] = i;
-    const int job = at[blockIdx.x % jobs], span = blockIdx.y;
-    const long long pair = blockIdx.x / jobs;
-    const decay_job &j = p.job[job];
-    const int n = (int)(pair / p.H), head = (int)(pair % p.H), da = j.da, dc = j.dc;
-    const decay_seq q = decay_open(p, j, n);
-    const bool rev = q.reverse;
-    const long long pairs = (long long)p.N * p.H;
-    const int cells = da * dc;
-    // (T is below 2^31 - 65536: tokens, and the ends of chunks and spans, are ints)
-    const int len = (int)q.len, first = (int)(span * p.span_tokens), last = (int)min(p.T, span * p.span_tokens + p.span_tokens), stop = min(last, len);
-    const int chunks = stop > first ? (stop - first + kChunk - 1) / kChunk : 0;
-    // Row r of a tile is token begin_of(c) + r; counted along the pass it is step step_of(r) of the chunk.
-    const auto begin_of = [&](int c) { return rev ? len - first - (c + 1) * kChunk : first + c * kChunk; };
-    const auto step_of = [&](int r) { return rev ? kChunk - 1 - r : r; };
+        if (!(STATE && p.job[i].spans_t)) job_at[jobs++] = i;
+    const int pairs = p.N * p.H, items = pairs * jobs * p.spans;
 
-    bf16 *const py = static_cast<bf16 *>(const_cast<void *>(j.y.p)) + n * j.y.n + head * j.y.h;
-    // Loads of a chunk: by the issuing warp's one thread where TMA does them, by the workers otherwise.
-    const auto load = [&](uint32_t dst, const decay_array &g, int map, int dim, int c, uint32_t bar) {
-        const int t0 = begin_of(c);
-        if constexpr (TMA) {
-#pragma unroll
-            for (int k = 0; k < D / 64; ++k) tma_load_4d(dst + k * kPanel, &maps.in[map], k * 64, t0, n, head, bar);
-        } else {
-            const int rows = min(kChunk, stop - first - c * kChunk);
-            load_tile<D>(dst, static_cast<const bf16 *>(g.p) + n * g.n + head * g.h + t0 * g.t, g.t, rev ? kChunk - rows : 0, rev ? kChunk : rows, dim,
-                         j.vec);
-        }
+    // A CTA takes items (a job of a head of a sequence, or of a span of it) one after the other.
+    // (T is below 2^31 - 65536: tokens, and the ends of chunks and spans, are ints)
+    struct Item {
+        int at, job, pair, n, head, span, len, first, last, stop, chunks;
+        bool rev;
     };
-    const auto load_ab = [&](int c) {  // keys, and queries
-        const int slot = c & 1;
-        if constexpr (TMA) {
-            if (c < chunks && tc::elect_one()) {
-                tc::mbar_arrive_expect_tx(barQK + 8 * slot, (STATE ? 1 : 2) * L::tile);
-                load(base + L::b + slot * L::tile, j.b, j.map[1], da, c, barQK + 8 * slot);
-                if constexpr (!STATE) load(base + L::a + slot * L::tile, j.a, j.map[0], da, c, barQK + 8 * slot);
-            }
-            __syncwarp();
-        } else {
-            if (c < chunks) {
-                load(base + L::b + slot * L::tile, j.b, 0, da, c, 0);
-                if constexpr (!STATE) load(base + L::a + slot * L::tile, j.a, 0, da, c, 0);
-            }
-            copy_commit();
-        }
+    const auto open = [&](int at) {
+        Item m{};
+        m.at = at;
+        if (at >= items) return m;
+        m.span = at / (pairs * jobs);
+        const int k = at - m.span * pairs * jobs;
+        m.pair = k / jobs;
+        m.job = job_at[k - m.pair * jobs];
+        m.n = m.pair / p.H;
+        m.head = m.pair - m.n * p.H;
+        const decay_seq q = decay_open(p, p.job[m.job], m.n);
+        m.rev = q.reverse;
+        m.len = (int)q.len;
+        m.first = (int)(m.span * p.span_tokens);
+        m.last = (int)min(p.T, m.span * p.span_tokens + p.span_tokens);
+        m.stop = min(m.last, m.len);
+        m.chunks = m.stop > m.first ? (m.stop - m.first + kChunk - 1) / kChunk : 0;
+        return m;
     };
-    const auto load_c = [&](int c) {
-        if constexpr (TMA) {
-            if (c < chunks && tc::elect_one()) {
-                tc::mbar_arrive_expect_tx(barV, L::tile);
-                load(base + L::c, j.c, j.map[2], dc, c, barV);
-            }
-            __syncwarp();
-        } else {
-            if (c < chunks) load(base + L::c, j.c, 0, dc, c, 0);
-            copy_commit();
-        }
-    };
-    const auto find_cuts = [&](int c) {
-        if (CUT && warp < 4) {
-            const int s = first + c * kChunk + warp * 32 + lane;
-            const unsigned m = __ballot_sync(~0u, c < chunks && s < stop && decay_cut(p, q, s, n));
-            if (lane == 0) cuts[(c & 1) * 4 + warp] = m;
-        }
-    };
+    // Row r of a chunk's tiles is token begin_of(c) + r; counted along the pass it is step step_of(r) of the chunk.
+    const auto begin_of = [](const Item &m, int c) { return m.rev ? m.len - m.first - (c + 1) * kChunk : m.first + c * kChunk; };
+
     const auto wait = [&](uint32_t bar, int phase) {
         for (uint32_t i = 0; !tc::mbar_try_wait(bar, (uint32_t)phase & 1u); ++i) {
             if (*late || i == kWait) {  // (what follows goes on with what there is)
@@ -307,41 +317,61 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
         __syncwarp();
         tc::fence_proxy_async_smem();
     }
-    if (TMA != worker) {
-        load_ab(0);
-        load_c(0);
-        load_ab(1);
-    }
     if (warp == 1) tc::tmem_alloc(tc::smem_u32(tmem_at), L::columns);
-    const float g = p.log_decay[head];
-    find_cuts(0);
-    if (tid <= kChunk) power[tid] = decay_power(g, tid);
-    if (tid < 3) scales[tid] = tid == 0 ? j.w_scale : tid == 1 ? j.in_scale : j.up_scale;
     tc::fence_before_sync();
     __syncthreads();
     tc::fence_after_sync();
     const uint32_t tmem = *tmem_at;
 
-    const float *from = nullptr;  // the entering state
-    int from_t = 0;
-    if constexpr (!STATE) {
-        if (p.spans > 1) {
-            from = j.spans + (span * pairs + pair) * cells;
-            from_t = j.spans_t;
-        } else if (j.s_in) {
-            from = j.s_in + pair * cells;
-            from_t = j.in_t;
-        }
-    }
-    const bool enters = from != nullptr;
-    float4 *const x = reinterpret_cast<float4 *>(smem + L::lo);  // a state on its way
-    bool bad = false;   // something was not finite
-    bool keeps = true;  // (STATE) no cut so far
-
     if (!worker) {
-        // ---- one thread issues the products, and the copies
-        const auto form_a = [&](int c) {
-            const uint32_t ta = base + L::a + (c & 1) * L::tile, tb = base + L::b + (c & 1) * L::tile;
+        // ---- one thread issues the products, and the copies: keys and queries a chunk ahead, of the next item too
+        struct Cursor {  // a chunk: of item `at`, the c-th of its `chunks`, from token t0
+            int at, c, chunks, t0, dt, n, head, maps;
+            bool enters;
+        };
+        const auto find = [&](Cursor &k, int at) {  // the first chunk of item `at`, or of the next one that has any
+            for (;; at += gridDim.x) {
+                const Item m = open(at);
+                const decay_job &j = p.job[m.job];
+                k = {at, 0, m.chunks, begin_of(m, 0), m.rev ? -kChunk : kChunk, m.n, m.head, j.map[0] | j.map[1] << 2 | j.map[2] << 4,
+                     !STATE && (p.spans > 1 || j.s_in)};
+                if (m.chunks > 0 || at >= items) return;
+            }
+        };
+        const auto step = [&](Cursor &k) {
+            k.t0 += k.dt;
+            if (++k.c >= k.chunks && k.at < items) find(k, k.at + (int)gridDim.x);
+        };
+        const auto load = [&](const Cursor &k, uint32_t dst, int map, uint32_t bar) {
+#pragma unroll
+            for (int i = 0; i < D / 64; ++i) tma_load_4d(dst + i * kPanel, &maps.in[map], i * 64, k.t0, k.n, k.head, bar);
+        };
+        const auto load_ab = [&](const Cursor &k, int slot) {  // keys, and queries
+            if (k.at < items && tc::elect_one()) {
+                tc::mbar_arrive_expect_tx(barQK + 8 * slot, (STATE ? 1 : 2) * L::tile);
+                load(k, base + L::b + slot * L::tile, k.maps >> 2 & 3, barQK + 8 * slot);
+                if constexpr (!STATE) load(k, base + L::a + slot * L::tile, k.maps & 3, barQK + 8 * slot);
+            }
+            __syncwarp();
+        };
+        const auto load_c = [&](const Cursor &k) {
+            if (k.at < items && tc::elect_one()) {
+                tc::mbar_arrive_expect_tx(barV, L::tile);
+                load(k, base + L::c, k.maps >> 4, barV);
+            }
+            __syncwarp();
+        };
+        Cursor now;
+        find(now, blockIdx.x);
+        Cursor ahead = now;
+        if constexpr (TMA) {
+            load_ab(ahead, 0);
+            load_c(ahead);
+            step(ahead);
+            load_ab(ahead, 1);
+        }
+        const auto form_a = [&](int slot) {
+            const uint32_t ta = base + L::a + slot * L::tile, tb = base + L::b + slot * L::tile;
             if (tc::elect_one()) {
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k)
@@ -352,16 +382,19 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             __syncwarp();
         };
 #pragma unroll 1
-        for (int c = 0; c < chunks; ++c) {
-            const int slot = c & 1;
+        for (int done = 0; now.at < items; ++done) {  // chunks
+            const bool has_x = now.enters || now.c > 0, fresh = STATE && now.c == 0;
+            const int slot = done & 1;
             const uint32_t ta = base + L::a + slot * L::tile, tb = base + L::b + slot * L::tile, tv = base + L::c;
-            const bool has_x = enters || c > 0;
-            if (TMA && !(early && c > 0)) wait(barQK + 8 * slot, c >> 1);
+            if (TMA && !(early && done > 0)) wait(barQK + 8 * slot, done >> 1);
             tc::fence_before_sync();
             __syncthreads();  // 1: the chunk before is read out
             tc::fence_after_sync();
-            if (!STATE && !(early && c > 0)) form_a(c);
-            if (TMA && c > 0) load_ab(c + 1);
+            if (!STATE && !(early && done > 0)) form_a(slot);
+            if (TMA && done > 0) {
+                step(ahead);
+                load_ab(ahead, slot ^ 1);
+            }
             tc::fence_before_sync();
             __syncthreads();  // 2: A is read, Xb there
             tc::fence_after_sync();
@@ -374,11 +407,11 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             __syncwarp();
             bool keeps_x = true;
             if constexpr (CUT) keeps_x = (cuts[slot * 4] | cuts[slot * 4 + 1] | cuts[slot * 4 + 2] | cuts[slot * 4 + 3]) == 0;
-            if constexpr (TMA) wait(barV, c);
+            if constexpr (TMA) wait(barV, done);
             tc::fence_before_sync();
             __syncthreads();  // 3: P and the keys' parts are there
             tc::fence_after_sync();
-            const bool onto = (STATE ? c > 0 : has_x) && keeps_x;
+            const bool onto = (STATE ? !fresh : has_x) && keeps_x;
             if (tc::elect_one()) {
                 if constexpr (!STATE) {
 #pragma unroll
@@ -396,407 +429,464 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 tc::mma_commit(barX);
             }
             __syncwarp();
-            if (early && c + 1 < chunks) {
-                wait(barQK + 8 * (slot ^ 1), (c + 1) >> 1);
-                form_a(c + 1);
+            step(now);
+            if (early && now.at < items) {
+                wait(barQK + 8 * (slot ^ 1), (done + 1) >> 1);
+                form_a(slot ^ 1);
             }
             if (TMA) {
-                wait(barX, c);
-                load_c(c + 1);
+                wait(barX, done);
+                load_c(now);
             }
         }
     } else {
         const uint32_t mine = tmem + ((uint32_t)(quad * 32) << 16);
-        // The entering state into TMEM: row a thread's lane, 32 columns a thread.  With D = 64 the state is the sum of lanes 0
-        // to 63 (sums of the keys' first parts) and 64 to 127 (of the second).
         const int xrow = quad * 32 + lane, group = warp >> 2, col0 = group * 32;
-        if (enters && chunks > 0) {
-            const float mul = p.spans == 1 && j.first ? power[1] : 1.f;
-            uint32_t r[32];
-            if (from_t) {  // (a row of the state is a column there: lanes read side by side)
-#pragma unroll
-                for (int i = 0; i < 32; ++i) r[i] = xrow < da && col0 + i < dc ? __float_as_uint(from[(col0 + i) * da + xrow]) : 0u;
-            } else {
-                state_rows<D>(x, da, dc, [&](int at) { return from[at]; }, [&](int at) { return *reinterpret_cast<const float4 *>(from + at); },
-                              (uintptr_t)from % 16 == 0);
-                worker_barrier<D>();
-#pragma unroll
-                for (int i = 0; i < 32; i += 4) {
-                    const float4 v = x[state_at<D>(xrow & (D - 1), (col0 + i) / 4)];
-                    const bool on = xrow < D;
-                    r[i] = on ? __float_as_uint(v.x) : 0u, r[i + 1] = on ? __float_as_uint(v.y) : 0u;
-                    r[i + 2] = on ? __float_as_uint(v.z) : 0u, r[i + 3] = on ? __float_as_uint(v.w) : 0u;
+        float4 *const x = reinterpret_cast<float4 *>(smem + L::lo);  // a state on its way
+        int done = 0;                                                // chunks
+        Item m = open(blockIdx.x);
+        float g = p.log_decay[m.head];
+        while (m.at < items) {
+            const decay_job &j = p.job[m.job];
+            const int da = j.da, dc = j.dc, len = m.len, first = m.first, last = m.last, stop = m.stop, chunks = m.chunks;
+            const bool rev = m.rev;
+            const decay_seq q{p.T, len, rev};
+            const int cells = da * dc;
+            bf16 *const py = static_cast<bf16 *>(const_cast<void *>(j.y.p)) + m.n * j.y.n + m.head * j.y.h;
+            const auto step_of = [&](int r) { return rev ? kChunk - 1 - r : r; };
+            const auto find_cuts = [&](int c) {
+                if (CUT && warp < 4) {
+                    const int s = first + c * kChunk + warp * 32 + lane;
+                    const unsigned bits = __ballot_sync(~0u, c < chunks && s < stop && decay_cut(p, q, s, m.n));
+                    if (lane == 0) cuts[((done + c) & 1) * 4 + warp] = bits;
+                }
+            };
+            const float *from = nullptr;  // the entering state
+            int from_t = 0;
+            if constexpr (!STATE) {
+                if (p.spans > 1) {
+                    from = j.spans + ((long long)m.span * pairs + m.pair) * cells;
+                    from_t = j.spans_t;
+                } else if (j.s_in) {
+                    from = j.s_in + (long long)m.pair * cells;
+                    from_t = j.in_t;
                 }
             }
-            if (mul != 1.f) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * mul);
+            const bool enters = from != nullptr;
+            bool bad = false;   // something was not finite
+            bool keeps = true;  // (STATE) no cut so far
+            // (without TMA the workers load: keys and queries a chunk ahead within an item)
+            const auto load = [&](int c, uint32_t dst, const decay_array &g, int dim) {
+                const int n = min(kChunk, stop - first - c * kChunk);
+                load_tile<D>(dst, static_cast<const bf16 *>(g.p) + m.n * g.n + m.head * g.h + begin_of(m, c) * g.t, g.t, rev ? kChunk - n : 0, rev ? kChunk : n,
+                             dim, j.vec);
+            };
+            const auto load_ab = [&](int c) {
+                const int slot = (done + c) & 1;
+                if (c < chunks) {
+                    load(c, base + L::b + slot * L::tile, j.b, da);
+                    if constexpr (!STATE) load(c, base + L::a + slot * L::tile, j.a, da);
+                }
+                copy_commit();
+            };
+            const auto load_c = [&](int c) {
+                if (c < chunks) load(c, base + L::c, j.c, dc);
+                copy_commit();
+            };
+            if constexpr (!TMA) {
+                load_ab(0);
+                load_c(0);
+                load_ab(1);
             }
-            __syncwarp();
-            TC_ST32(mine + L::tX + col0, r);
-            tmem_st_wait();
-        }
-        uint32_t odd = 0;  // two bf16: NaN once an output was not finite
-        const int step = step_of(xrow);
-
-#pragma unroll 1
-        for (int c = 0; c < chunks; ++c) {
-            const int s0 = first + c * kChunk, t0 = begin_of(c), rows = min(kChunk, stop - s0), slot = c & 1;
-            const uint32_t ta = base + L::a + slot * L::tile, tb = base + L::b + slot * L::tile, tv = base + L::c;
-            const bool has_x = enters || c > 0;
-            if constexpr (!TMA) copy_wait<1>();
-            if constexpr (!STATE) tma_store_read();  // (the outputs' copies have read a's tile, which is filled again)
-            tc::fence_proxy_async_smem();
-            tc::fence_before_sync();
-            __syncthreads();  // 1
-            tc::fence_after_sync();
-            if (!TMA && c > 0) load_ab(c + 1);
-            // tokens that begin something new: what a token sees begins with the last of them up to it (counted in steps)
-            int keep_from = -1, begin = -1;
-            bool any_cut = false;
-            if constexpr (CUT) {
-                uint32_t cut[4];
+            find_cuts(0);
+            if (tid <= kChunk) power[tid] = decay_power(g, tid);
+            if (tid < 3) scales[tid] = tid == 0 ? j.w_scale : tid == 1 ? j.in_scale : j.up_scale;
+            worker_barrier<D>();
+            // The entering state into TMEM: row a thread's lane, 32 columns a thread.  With D = 64 the state is the sum of lanes 0
+            // to 63 (sums of the keys' first parts) and 64 to 127 (of the second).
+            if (enters && chunks > 0) {
+                const float mul = p.spans == 1 && j.first ? power[1] : 1.f;
+                uint32_t r[32];
+                if (from_t) {  // (a row of the state is a column there: lanes read side by side)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) cut[i] = cuts[slot * 4 + i];
-                any_cut = (cut[0] | cut[1] | cut[2] | cut[3]) != 0;
-                if (any_cut) {
+                    for (int i = 0; i < 32; ++i) r[i] = xrow < da && col0 + i < dc ? __float_as_uint(from[(col0 + i) * da + xrow]) : 0u;
+                } else {
+                    state_in<D>(x, from, da, dc);
+                    worker_barrier<D>();
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if (cut[i]) keep_from = 32 * i + 31 - __clz(cut[i]);  // (no cuts behind the last step)
-                        const uint32_t m = step / 32 > i ? cut[i] : step / 32 < i ? 0u : cut[i] & (~0u >> (31 - step % 32));
-                        if (m) begin = 32 * i + 31 - __clz(m);
+                    for (int i = 0; i < 32; i += 4) {
+                        const float4 v = x[state_at<D>(xrow & (D - 1), (col0 + i) / 4)];
+                        const bool on = xrow < D;
+                        r[i] = on ? __float_as_uint(v.x) : 0u, r[i + 1] = on ? __float_as_uint(v.y) : 0u;
+                        r[i + 2] = on ? __float_as_uint(v.z) : 0u, r[i + 3] = on ? __float_as_uint(v.w) : 0u;
                     }
                 }
-                if constexpr (STATE) keeps = keeps && keep_from < 0;
-            }
-            // (time's order, the last token of all: the state leaves as that token wrote it)
-            const int less = !STATE && j.first && s0 + rows == len ? 1 : 0;
-            if (tid < kChunk && (CUT || STATE || c == 0 || rows < kChunk || less)) {
-                float w = 0.f;
-                const int s = step_of(tid);
-                if (s < rows && s >= keep_from) {
-                    if constexpr (STATE) w = decay_power(g, stop - s0 - s);  // up to the span's end
-                    else w = power[rows - s - less];
+                if (mul != 1.f) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * mul);
                 }
-                w *= scales[2];
-                const float w1 = __bfloat162float(__float2bfloat16_rn(w));
-                kept[tid] = make_uint2(pack2(w1, w1), pack2(w - w1, w - w1));
+                __syncwarp();
+                TC_ST32(mine + L::tX + col0, r);
+                tmem_st_wait();
             }
-            constexpr int cols = 128 / (D / 32);  // of A, a thread
-            uint32_t packed[cols / 2];
-            if constexpr (!STATE) {
-                // X -> Xb, and X to what the next state keeps of it
-                if (has_x) {
-                    const Pair shrink = twice(power[rows - less]);
-                    uint32_t r[32];
-                    const int row = D == 64 ? xrow & 63 : xrow;
-                    const uint32_t to = base + L::xb + (col0 / 64) * (D * 128) + row * 128;
-                    const auto place = [&](int i) { return to + ((((col0 % 64 + i) / 8) ^ (row & 7)) << 4); };
-                    TC_LD32(mine + L::tX + col0, r);
-                    tc::tmem_ld_wait();
-                    if constexpr (D == 64) {  // the second parts come by way of Xb's place
-                        if (quad >= 2) {
+            uint32_t odd = 0;  // two bf16: NaN once an output was not finite
+            const int step = step_of(xrow);
+
+#pragma unroll 1
+            for (int c = 0; c < chunks; ++c) {
+                const int s0 = first + c * kChunk, t0 = begin_of(m, c), rows = min(kChunk, stop - s0), slot = (done + c) & 1, phase = done + c;
+                const uint32_t ta = base + L::a + slot * L::tile, tb = base + L::b + slot * L::tile, tv = base + L::c;
+                const bool has_x = enters || c > 0;
+                if constexpr (!TMA) copy_wait<1>();
+                if constexpr (!STATE) tma_store_read();  // (the outputs' copies have read a's tile, which is filled again)
+                tc::fence_proxy_async_smem();
+                tc::fence_before_sync();
+                __syncthreads();  // 1
+                tc::fence_after_sync();
+                if (!TMA && c > 0) load_ab(c + 1);
+                // tokens that begin something new: what a token sees begins with the last of them up to it (counted in steps)
+                int keep_from = -1, begin = -1;
+                bool any_cut = false;
+                if constexpr (CUT) {
+                    uint32_t cut[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) cut[i] = cuts[slot * 4 + i];
+                    any_cut = (cut[0] | cut[1] | cut[2] | cut[3]) != 0;
+                    if (any_cut) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if (cut[i]) keep_from = 32 * i + 31 - __clz(cut[i]);  // (no cuts behind the last step)
+                            const uint32_t m = step / 32 > i ? cut[i] : step / 32 < i ? 0u : cut[i] & (~0u >> (31 - step % 32));
+                            if (m) begin = 32 * i + 31 - __clz(m);
+                        }
+                    }
+                    if constexpr (STATE) keeps = keeps && keep_from < 0;
+                }
+                // (time's order, the last token of all: the state leaves as that token wrote it)
+                const int less = !STATE && j.first && s0 + rows == len ? 1 : 0;
+                if (tid < kChunk && (CUT || STATE || c == 0 || rows < kChunk || less)) {
+                    float w = 0.f;
+                    const int s = step_of(tid);
+                    if (s < rows && s >= keep_from) {
+                        if constexpr (STATE) w = decay_power(g, stop - s0 - s);  // up to the span's end
+                        else w = power[rows - s - less];
+                    }
+                    w *= scales[2];
+                    const float w1 = __bfloat162float(__float2bfloat16_rn(w));
+                    kept[tid] = make_uint2(pack2(w1, w1), pack2(w - w1, w - w1));
+                }
+                constexpr int cols = 128 / (D / 32);  // of A, a thread
+                uint32_t packed[cols / 2];
+                if constexpr (!STATE) {
+                    // X -> Xb, and X to what the next state keeps of it
+                    if (has_x) {
+                        const Pair shrink = twice(power[rows - less]);
+                        uint32_t r[32];
+                        const int row = D == 64 ? xrow & 63 : xrow;
+                        const uint32_t to = base + L::xb + (col0 / 64) * (D * 128) + row * 128;
+                        const auto place = [&](int i) { return to + ((((col0 % 64 + i) / 8) ^ (row & 7)) << 4); };
+                        TC_LD32(mine + L::tX + col0, r);
+                        tc::tmem_ld_wait();
+                        if constexpr (D == 64) {  // the second parts come by way of Xb's place
+                            if (quad >= 2) {
+#pragma unroll
+                                for (int i = 0; i < 32; i += 8) {
+                                    const float *f = reinterpret_cast<const float *>(r + i);
+                                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(place(i)), "r"(pack2(f[0], f[1])), "r"(pack2(f[2], f[3])),
+                                                 "r"(pack2(f[4], f[5])), "r"(pack2(f[6], f[7])) : "memory");
+                                }
+                            }
+                            pair_barrier(1 + group * 2 + (quad & 1));
+                        }
+                        if (D == 128 || quad < 2) {
+                            uint32_t e[16];
+                            if constexpr (D == 64) {
+#pragma unroll
+                                for (int i = 0; i < 16; i += 4)
+                                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(e[i]), "=r"(e[i + 1]), "=r"(e[i + 2]), "=r"(e[i + 3]) : "r"(place(2 * i)) : "memory");
+                            }
 #pragma unroll
                             for (int i = 0; i < 32; i += 8) {
                                 const float *f = reinterpret_cast<const float *>(r + i);
-                                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(place(i)), "r"(pack2(f[0], f[1])), "r"(pack2(f[2], f[3])),
-                                             "r"(pack2(f[4], f[5])), "r"(pack2(f[6], f[7])) : "memory");
+                                float x[8];
+                                if constexpr (D == 64) {
+#pragma unroll
+                                    for (int m = 0; m < 4; ++m) {
+                                        x[2 * m] = f[2 * m] + __uint_as_float(e[i / 2 + m] << 16);
+                                        x[2 * m + 1] = f[2 * m + 1] + __uint_as_float(e[i / 2 + m] & 0xffff0000u);
+                                    }
+                                } else {
+#pragma unroll
+                                    for (int m = 0; m < 8; ++m) x[m] = f[m];
+                                }
+                                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(place(i)), "r"(pack2(x[0], x[1])), "r"(pack2(x[2], x[3])),
+                                             "r"(pack2(x[4], x[5])), "r"(pack2(x[6], x[7])) : "memory");
                             }
                         }
-                        pair_barrier(1 + group * 2 + (quad & 1));
-                    }
-                    if (D == 128 || quad < 2) {
-                        uint32_t e[16];
-                        if constexpr (D == 64) {
+                        if (!CUT || keep_from < 0) {
 #pragma unroll
-                            for (int i = 0; i < 16; i += 4)
-                                asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(e[i]), "=r"(e[i + 1]), "=r"(e[i + 2]), "=r"(e[i + 3]) : "r"(place(2 * i)) : "memory");
+                            for (int i = 0; i < 32; i += 2) {
+                                const Pair v = mul2(pair_of(r[i], r[i + 1]), shrink);
+                                r[i] = __float_as_uint(v.f.x);
+                                r[i + 1] = __float_as_uint(v.f.y);
+                            }
+                            __syncwarp();
+                            TC_ST32(mine + L::tX + col0, r);
                         }
+                        tmem_st_wait();
+                    }
+                    // A -> P: row xrow, 16 columns at a time.  Weights lambda^away by products from the nearest column on: up to 16
+                    // roundings of 2^-24, before one of 2^-8
+                    wait(barA, phase);
+                    const float w_scale = scales[0], lambda = power[1];
 #pragma unroll
-                        for (int i = 0; i < 32; i += 8) {
-                            const float *f = reinterpret_cast<const float *>(r + i);
-                            float x[8];
-                            if constexpr (D == 64) {
+                    for (int h = 0; h < cols / 16; ++h) {
+                        const int j0 = group * cols + h * 16, block = j0 / 32, i0 = j0 % 32;
+                        if (rev ? block < quad : block > quad) {  // not seen
 #pragma unroll
-                                for (int m = 0; m < 4; ++m) {
-                                    x[2 * m] = f[2 * m] + __uint_as_float(e[i / 2 + m] << 16);
-                                    x[2 * m + 1] = f[2 * m + 1] + __uint_as_float(e[i / 2 + m] & 0xffff0000u);
+                            for (int i = 0; i < 8; ++i) packed[h * 8 + i] = 0u;
+                            continue;
+                        }
+                        uint32_t v[16];
+                        TC_LD16(mine + L::tA + j0, v);
+                        const auto weigh = [&](int i, float a, float b) {
+                            Pair w;
+                            w.f = make_float2(a, b);
+                            w = mul2(pair_of(v[i], v[i + 1]), w);
+                            packed[h * 8 + i / 2] = pack2(w.f.x, w.f.y);
+                        };
+                        // (the weight of the column before the first of these, in the order they are taken)
+                        const int before = rev ? j0 - 1 - xrow : xrow - j0 - 16;
+                        float w = before >= 0 ? w_scale * power[before] : 0.f;
+                        tc::tmem_ld_wait();
+                        if (block == quad) {
+                            const int own = lane - i0;  // the token itself; columns behind it are not seen, whatever they hold
+                            if (!rev) {
+#pragma unroll
+                                for (int i = 14; i >= 0; i -= 2) {
+                                    const float b = i + 1 == own ? w_scale : w * lambda;
+                                    w = i == own ? w_scale : b * lambda;
+                                    v[i + 1] = i + 1 <= own ? v[i + 1] : 0u;
+                                    v[i] = i <= own ? v[i] : 0u;
+                                    weigh(i, w, b);
                                 }
                             } else {
 #pragma unroll
-                                for (int m = 0; m < 8; ++m) x[m] = f[m];
-                            }
-                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(place(i)), "r"(pack2(x[0], x[1])), "r"(pack2(x[2], x[3])),
-                                         "r"(pack2(x[4], x[5])), "r"(pack2(x[6], x[7])) : "memory");
-                        }
-                    }
-                    if (!CUT || keep_from < 0) {
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            const Pair v = mul2(pair_of(r[i], r[i + 1]), shrink);
-                            r[i] = __float_as_uint(v.f.x);
-                            r[i + 1] = __float_as_uint(v.f.y);
-                        }
-                        __syncwarp();
-                        TC_ST32(mine + L::tX + col0, r);
-                    }
-                    tmem_st_wait();
-                }
-                // A -> P: row xrow, 16 columns at a time.  Weights lambda^away by products from the nearest column on: up to 16
-                // roundings of 2^-24, before one of 2^-8
-                wait(barA, c);
-                const float w_scale = scales[0], lambda = power[1];
-#pragma unroll
-                for (int h = 0; h < cols / 16; ++h) {
-                    const int j0 = group * cols + h * 16, block = j0 / 32, i0 = j0 % 32;
-                    if (rev ? block < quad : block > quad) {  // not seen
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) packed[h * 8 + i] = 0u;
-                        continue;
-                    }
-                    uint32_t v[16];
-                    TC_LD16(mine + L::tA + j0, v);
-                    const auto weigh = [&](int i, float a, float b) {
-                        Pair w;
-                        w.f = make_float2(a, b);
-                        w = mul2(pair_of(v[i], v[i + 1]), w);
-                        packed[h * 8 + i / 2] = pack2(w.f.x, w.f.y);
-                    };
-                    // (the weight of the column before the first of these, in the order they are taken)
-                    const int before = rev ? j0 - 1 - xrow : xrow - j0 - 16;
-                    float w = before >= 0 ? w_scale * power[before] : 0.f;
-                    tc::tmem_ld_wait();
-                    if (block == quad) {
-                        const int own = lane - i0;  // the token itself; columns behind it are not seen, whatever they hold
-                        if (!rev) {
-#pragma unroll
-                            for (int i = 14; i >= 0; i -= 2) {
-                                const float b = i + 1 == own ? w_scale : w * lambda;
-                                w = i == own ? w_scale : b * lambda;
-                                v[i + 1] = i + 1 <= own ? v[i + 1] : 0u;
-                                v[i] = i <= own ? v[i] : 0u;
-                                weigh(i, w, b);
+                                for (int i = 0; i < 16; i += 2) {
+                                    const float a = i == own ? w_scale : w * lambda;
+                                    w = i + 1 == own ? w_scale : a * lambda;
+                                    v[i] = i >= own ? v[i] : 0u;
+                                    v[i + 1] = i + 1 >= own ? v[i + 1] : 0u;
+                                    weigh(i, a, w);
+                                }
                             }
                         } else {
+                            const Pair lambda2 = twice(lambda * lambda);
+                            Pair t;
+                            w *= lambda;
+                            if (!rev) {
+                                t.f = make_float2(w * lambda, w);
 #pragma unroll
-                            for (int i = 0; i < 16; i += 2) {
-                                const float a = i == own ? w_scale : w * lambda;
-                                w = i + 1 == own ? w_scale : a * lambda;
-                                v[i] = i >= own ? v[i] : 0u;
-                                v[i + 1] = i + 1 >= own ? v[i + 1] : 0u;
-                                weigh(i, a, w);
+                                for (int i = 14; i >= 0; i -= 2, t = mul2(t, lambda2)) weigh(i, t.f.x, t.f.y);
+                            } else {
+                                t.f = make_float2(w, w * lambda);
+#pragma unroll
+                                for (int i = 0; i < 16; i += 2, t = mul2(t, lambda2)) weigh(i, t.f.x, t.f.y);
+                            }
+                        }
+                        if (CUT && any_cut) {
+#pragma unroll
+                            for (int i = 0; i < 8; ++i)
+                                packed[h * 8 + i] &= (step_of(j0 + 2 * i) >= begin ? 0xffffu : 0u) | (step_of(j0 + 2 * i + 1) >= begin ? 0xffff0000u : 0u);
+                        }
+                    }
+                }
+                tc::fence_proxy_async_smem();  // Xb
+                tc::fence_before_sync();
+                __syncthreads();  // 2: A is read, P and O2 may take its place (STATE: kept is there)
+                tc::fence_after_sync();
+                if constexpr (!STATE) {
+                    if constexpr (cols == 64) TC_ST32(mine + L::tA + group * 32, packed);
+                    else TC_ST16(mine + L::tA + group * 16, packed);
+                }
+                // b -> b w as two bf16 values, the first in b's place: with w = w1 + w2, hi = b w1 rounded, lo = (b w1 - hi) + b w2,
+                // where b w1 - hi is exact (16 bits of a product, the first 8 taken away)
+                {
+                    constexpr int per = D / 8, stride = L::workers / per;
+                    const int ch = tid % per, row0 = tid / per;
+                    const uint32_t off = (ch / 8) * kPanel + row0 * 128 + (((ch & 7) ^ (row0 & 7)) << 4);
+                    constexpr int turns = kChunk / stride;
+                    uint32_t v[turns][4];
+                    uint2 w[turns];
+#pragma unroll
+                    for (int k = 0; k < turns; ++k) {
+                        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[k][0]), "=r"(v[k][1]), "=r"(v[k][2]), "=r"(v[k][3]) : "r"(tb + off + k * stride * 128) : "memory");
+                        w[k] = kept[row0 + k * stride];
+                    }
+#pragma unroll
+                    for (int k = 0; k < turns; ++k) {
+                        const uint32_t to = off + k * stride * 128;
+                        uint32_t hi[4], lo[4];
+                        if (TMA && rows < kChunk && step_of(row0 + k * stride) >= rows) v[k][0] = v[k][1] = v[k][2] = v[k][3] = 0u;  // (whatever lies there)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            hi[i] = hmul(v[k][i], w[k].x);
+                            lo[i] = hfma(v[k][i], w[k].y, hfma(v[k][i], w[k].x, hi[i] ^ 0x80008000u));
+                        }
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(tb + to), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(base + L::lo + to), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
+                    }
+                }
+                if constexpr (TMA) {
+                    if (rows < kChunk) {  // values of steps that are not there: whatever lies there times 0 is to be 0
+                        wait(barV, phase);
+                        constexpr int per = D / 8;
+                        for (int i = tid; i < (kChunk - rows) * per; i += L::workers) {
+                            const int s = rows + i / per, ch = i % per, row = step_of(s);
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(tv + (ch / 8) * kPanel + row * 128 + (((ch & 7) ^ (row & 7)) << 4)), "r"(0) : "memory");
+                        }
+                    }
+                } else {
+                    copy_wait<1>();
+                }
+                if constexpr (!STATE) tmem_st_wait();
+                tc::fence_proxy_async_smem();
+                tc::fence_before_sync();
+                __syncthreads();  // 3
+                find_cuts(c + 1);
+                if constexpr (!STATE) {
+                    // y = O1 + in_scale lambda^step O2, by way of a's tile (32 rows of 64 bytes a warp, 64-byte swizzle) to whole rows
+                    const bool sees = !CUT || begin < 0;
+                    const uint32_t stage = ta + warp * 2048, own = stage + lane * 64, turn = (lane >> 1) & 3;
+                    const Pair w = twice(scales[1] * power[step]);
+                    wait(barO, phase);
+                    uint32_t o1[32];
+                    TC_LD32(mine + L::tO1 + col0, o1);
+                    if (has_x) {
+                        uint32_t o2[32];
+                        TC_LD32(mine + L::tO2 + col0, o2);
+                        tc::tmem_ld_wait();
+                        if (sees) {
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2) {
+                                const Pair v = fma2(pair_of(o2[i], o2[i + 1]), w, pair_of(o1[i], o1[i + 1]));
+                                o1[i] = __float_as_uint(v.f.x), o1[i + 1] = __float_as_uint(v.f.y);
                             }
                         }
                     } else {
-                        const Pair lambda2 = twice(lambda * lambda);
-                        Pair t;
-                        w *= lambda;
-                        if (!rev) {
-                            t.f = make_float2(w * lambda, w);
-#pragma unroll
-                            for (int i = 14; i >= 0; i -= 2, t = mul2(t, lambda2)) weigh(i, t.f.x, t.f.y);
-                        } else {
-                            t.f = make_float2(w, w * lambda);
-#pragma unroll
-                            for (int i = 0; i < 16; i += 2, t = mul2(t, lambda2)) weigh(i, t.f.x, t.f.y);
-                        }
+                        tc::tmem_ld_wait();
                     }
-                    if (CUT && any_cut) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            packed[h * 8 + i] &= (step_of(j0 + 2 * i) >= begin ? 0xffffu : 0u) | (step_of(j0 + 2 * i + 1) >= begin ? 0xffff0000u : 0u);
-                    }
-                }
-            }
-            tc::fence_proxy_async_smem();  // Xb
-            tc::fence_before_sync();
-            __syncthreads();  // 2: A is read, P and O2 may take its place (STATE: kept is there)
-            tc::fence_after_sync();
-            if constexpr (!STATE) {
-                if constexpr (cols == 64) TC_ST32(mine + L::tA + group * 32, packed);
-                else TC_ST16(mine + L::tA + group * 16, packed);
-            }
-            // b -> b w as two bf16 values, the first in b's place: with w = w1 + w2, hi = b w1 rounded, lo = (b w1 - hi) + b w2,
-            // where b w1 - hi is exact (16 bits of a product, the first 8 taken away)
-            {
-                constexpr int per = D / 8, stride = L::workers / per;
-                const int ch = tid % per, row0 = tid / per;
-                const uint32_t off = (ch / 8) * kPanel + row0 * 128 + (((ch & 7) ^ (row0 & 7)) << 4);
-                constexpr int turns = kChunk / stride;
-                uint32_t v[turns][4];
-                uint2 w[turns];
+                    for (int i = 0; i < 16; ++i) o1[i] = pack2(__uint_as_float(o1[2 * i]), __uint_as_float(o1[2 * i + 1]));
 #pragma unroll
-                for (int k = 0; k < turns; ++k) {
-                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[k][0]), "=r"(v[k][1]), "=r"(v[k][2]), "=r"(v[k][3]) : "r"(tb + off + k * stride * 128) : "memory");
-                    w[k] = kept[row0 + k * stride];
-                }
-#pragma unroll
-                for (int k = 0; k < turns; ++k) {
-                    const uint32_t to = off + k * stride * 128;
-                    uint32_t hi[4], lo[4];
-                    if (TMA && rows < kChunk && step_of(row0 + k * stride) >= rows) v[k][0] = v[k][1] = v[k][2] = v[k][3] = 0u;  // (whatever lies there)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        hi[i] = hmul(v[k][i], w[k].x);
-                        lo[i] = hfma(v[k][i], w[k].y, hfma(v[k][i], w[k].x, hi[i] ^ 0x80008000u));
-                    }
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(tb + to), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(base + L::lo + to), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
-                }
-            }
-            if constexpr (TMA) {
-                if (rows < kChunk) {  // values of steps that are not there: whatever lies there times 0 is to be 0
-                    wait(barV, c);
-                    constexpr int per = D / 8;
-                    for (int i = tid; i < (kChunk - rows) * per; i += L::workers) {
-                        const int s = rows + i / per, ch = i % per, row = step_of(s);
-                        asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(tv + (ch / 8) * kPanel + row * 128 + (((ch & 7) ^ (row & 7)) << 4)), "r"(0) : "memory");
-                    }
-                }
-            } else {
-                copy_wait<1>();
-            }
-            if constexpr (!STATE) tmem_st_wait();
-            tc::fence_proxy_async_smem();
-            tc::fence_before_sync();
-            __syncthreads();  // 3
-            find_cuts(c + 1);
-            if constexpr (!STATE) {
-                // y = O1 + in_scale lambda^step O2, by way of a's tile (32 rows of 64 bytes a warp, 64-byte swizzle) to whole rows
-                const bool sees = !CUT || begin < 0;
-                const uint32_t stage = ta + warp * 2048, own = stage + lane * 64, turn = (lane >> 1) & 3;
-                const Pair w = twice(scales[1] * power[step]);
-                wait(barO, c);
-                uint32_t o1[32];
-                TC_LD32(mine + L::tO1 + col0, o1);
-                if (has_x) {
-                    uint32_t o2[32];
-                    TC_LD32(mine + L::tO2 + col0, o2);
-                    tc::tmem_ld_wait();
-                    if (sees) {
-#pragma unroll
-                        for (int i = 0; i < 32; i += 2) {
-                            const Pair v = fma2(pair_of(o2[i], o2[i + 1]), w, pair_of(o1[i], o1[i + 1]));
-                            o1[i] = __float_as_uint(v.f.x), o1[i + 1] = __float_as_uint(v.f.y);
-                        }
-                    }
-                } else {
-                    tc::tmem_ld_wait();
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o1[i] = pack2(__uint_as_float(o1[2 * i]), __uint_as_float(o1[2 * i + 1]));
-#pragma unroll
-                for (int i = 0; i < 16; i += 4)
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(own + (((i / 4) ^ turn) << 4)), "r"(o1[i]), "r"(o1[i + 1]), "r"(o1[i + 2]),
-                                 "r"(o1[i + 3]) : "memory");
-                if (maps.stores && rows == kChunk) {
-                    tc::fence_proxy_async_smem();
-                    __syncwarp();
-                    if (lane == 0 && col0 < dc) tma_store_4d(&maps.out[job], stage, col0, t0 + quad * 32, n, head);
-                } else {
-                    __syncwarp();
-                    const int left = dc - col0 - lane % 4 * 8;
+                    for (int i = 0; i < 16; i += 4)
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(own + (((i / 4) ^ turn) << 4)), "r"(o1[i]), "r"(o1[i + 1]), "r"(o1[i + 2]),
+                                     "r"(o1[i + 3]) : "memory");
+                    if (maps.stores && rows == kChunk) {
+                        tc::fence_proxy_async_smem();
+                        __syncwarp();
+                        if (lane == 0 && col0 < dc) tma_store_4d(&maps.out[m.job], stage, col0, t0 + quad * 32, m.n, m.head);
+                    } else {
+                        __syncwarp();
+                        const int left = dc - col0 - lane % 4 * 8;
 #pragma unroll 1
-                    for (int k = 0; k < 4; ++k) {
-                        const int r = k * 8 + lane / 4, row = quad * 32 + r;
-                        uint32_t v[4];
-                        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
-                                     : "r"(stage + r * 64 + (((lane % 4) ^ ((r >> 1) & 3)) << 4)) : "memory");
-                        if (step_of(row) < rows && left > 0) {
-                            bf16 *const out = py + (long long)(t0 + row) * j.y.t + col0 + lane % 4 * 8;
-                            if (j.vec > 1) {
-                                *reinterpret_cast<uint4 *>(out) = make_uint4(v[0], v[1], v[2], v[3]);
-                            } else {
+                        for (int k = 0; k < 4; ++k) {
+                            const int r = k * 8 + lane / 4, row = quad * 32 + r;
+                            uint32_t v[4];
+                            asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3])
+                                         : "r"(stage + r * 64 + (((lane % 4) ^ ((r >> 1) & 3)) << 4)) : "memory");
+                            if (step_of(row) < rows && left > 0) {
+                                bf16 *const out = py + (long long)(t0 + row) * j.y.t + col0 + lane % 4 * 8;
+                                if (j.vec > 1) {
+                                    *reinterpret_cast<uint4 *>(out) = make_uint4(v[0], v[1], v[2], v[3]);
+                                } else {
 #pragma unroll
-                                for (int m = 0; m < 8; ++m)
-                                    if (m < left) reinterpret_cast<unsigned short *>(out)[m] = (unsigned short)(v[m / 2] >> (16 * (m & 1)));
+                                    for (int m = 0; m < 8; ++m)
+                                        if (m < left) reinterpret_cast<unsigned short *>(out)[m] = (unsigned short)(v[m / 2] >> (16 * (m & 1)));
+                                }
                             }
                         }
                     }
-                }
-                if (step < rows) {
+                    if (step < rows) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) odd = hfma(o1[i], 0u, odd);
-                }
-            }
-            wait(barX, c);
-            if (!TMA) load_c(c + 1);
-        }
-        bad = (odd & 0x7fff7fffu) != 0;  // (a product with 0 is 0 or NaN)
-        if constexpr (!STATE) tma_store_read();
-        if constexpr (!TMA) copy_wait<0>();
-    }
-
-    // outputs of padding
-    if constexpr (!STATE) {
-        const int pad = max(first, stop);
-        const bool wide = j.vec > 1;
-        const int per = wide ? dc / 8 : dc, at_once = L::threads / per, r0 = tid / per, c0 = tid - r0 * per;
-        if (r0 < at_once)
-            for (int r = pad + r0; r < last; r += at_once) {
-                if (wide) *reinterpret_cast<uint4 *>(py + (long long)r * j.y.t + c0 * 8) = make_uint4(0, 0, 0, 0);
-                else py[(long long)r * j.y.t + c0] = __float2bfloat16_rn(0.f);
-            }
-    }
-    // what leaves: the span's part, or the state itself (of the span that holds the sequence's end)
-    float *to = nullptr;
-    bool empty = false;
-    if constexpr (STATE) {
-        to = j.spans + (span * pairs + pair) * cells;
-        if (tid == 0) p.carry[((long long)span * 2 + j.reverse) * pairs + pair] = !keeps ? 0.f : decay_power(g, max(0, stop - first));
-    } else if (j.s_out) {
-        if ((len > first && len <= last) || (len == 0 && span == 0)) to = j.s_out + pair * cells;
-        empty = j.out_zero && len > 0 && p.reset && p.reset[n] != 0;
-    }
-    if (chunks > 0) {
-        const int xrow = quad * 32 + lane, col0 = (warp >> 2) * 32;
-        tc::fence_before_sync();
-        __syncthreads();
-        tc::fence_after_sync();
-#pragma unroll 1
-        for (int part = D == 64; part >= 0; --part) {  // D = 64: lanes 64 and up, then the others onto them
-            if (worker && (D == 128 || (quad >= 2) == (part == 1))) {
-                uint32_t r[32];
-                TC_LD32(tmem + ((uint32_t)(quad * 32) << 16) + L::tX + col0, r);
-                tc::tmem_ld_wait();
-#pragma unroll
-                for (int i = 0; i < 32; i += 4) {
-                    float4 *const at = x + state_at<D>(xrow & (D - 1), (col0 + i) / 4);
-                    float4 v = make_float4(__uint_as_float(r[i]), __uint_as_float(r[i + 1]), __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
-                    if (D == 64 && part == 0) {
-                        const float4 o = *at;
-                        v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
+                        for (int i = 0; i < 16; ++i) odd = hfma(o1[i], 0u, odd);
                     }
-                    *at = v;
+                }
+                wait(barX, phase);
+                if (!TMA) load_c(c + 1);
+            }
+            bad = (odd & 0x7fff7fffu) != 0;  // (a product with 0 is 0 or NaN)
+            if constexpr (!STATE) tma_store_read();
+            if constexpr (!TMA) copy_wait<0>();
+            // the next item's marks, and its state on the way to L2, while this one's state leaves
+            const Item next = open(m.at + (int)gridDim.x);
+            float g_next = 0.f;
+            if (next.at < items) {
+                g_next = p.log_decay[next.head];
+                if constexpr (!STATE) {
+                    const decay_job &k = p.job[next.job];
+                    const float *const s = p.spans > 1 ? k.spans + (long long)next.span * pairs * cells : k.s_in;
+                    if (s && tid * 32 < cells)  // (a state is as large in every job)
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"(s + (long long)next.pair * cells + tid * 32));
                 }
             }
-            __syncthreads();
-        }
-        if (dc % 4 == 0 && (uintptr_t)to % 16 == 0) {
-            for (int i = tid; i < da * (dc / 4); i += L::threads) {
-                const int r = i / (dc / 4), k = i - r * (dc / 4);
-                const float4 v = x[state_at<D>(r, k)];
-                bad |= !(fabsf(v.x) <= 3.4028235e38f && fabsf(v.y) <= 3.4028235e38f && fabsf(v.z) <= 3.4028235e38f && fabsf(v.w) <= 3.4028235e38f);
-                if (to) reinterpret_cast<float4 *>(to)[i] = empty ? make_float4(0.f, 0.f, 0.f, 0.f) : v;
+            // outputs of padding
+            if (!STATE && max(first, stop) < last) {
+                const bool wide = j.vec > 1;
+                const int per = wide ? dc / 8 : dc, at_once = L::workers / per, r0 = tid / per, c0 = tid - r0 * per;
+                if (r0 < at_once)
+                    for (int r = max(first, stop) + r0; r < last; r += at_once) {
+                        if (wide) *reinterpret_cast<uint4 *>(py + (long long)r * j.y.t + c0 * 8) = make_uint4(0, 0, 0, 0);
+                        else py[(long long)r * j.y.t + c0] = __float2bfloat16_rn(0.f);
+                    }
             }
-        } else {
-            for (int i = tid; i < cells; i += L::threads) {
-                const int r = i / dc, k = i - r * dc;
-                const float v = reinterpret_cast<const float *>(x + state_at<D>(r, k / 4))[k % 4];
-                bad |= !(fabsf(v) <= 3.4028235e38f);
-                if (to) to[i] = empty ? 0.f : v;
+            // what leaves: the span's part, or the state itself (of the span that holds the sequence's end)
+            float *to = nullptr;
+            bool empty = false;
+            if constexpr (STATE) {
+                to = j.spans + ((long long)m.span * pairs + m.pair) * cells;
+                if (tid == 0) p.carry[((long long)m.span * 2 + j.reverse) * pairs + m.pair] = !keeps ? 0.f : decay_power(g, max(0, stop - first));
+            } else if (j.s_out) {
+                if ((len > first && len <= last) || (len == 0 && m.span == 0)) to = j.s_out + (long long)m.pair * cells;
+                empty = j.out_zero && len > 0 && p.reset && p.reset[m.n] != 0;
             }
-        }
-        if (bad) {
-            decay_mark(p, job, pair);
-            if constexpr (STATE)
-                for (int i = 0; i < p.jobs; ++i)  // (another job may read this state)
-                    if (p.job[i].spans_t) decay_mark(p, i, pair);
-        }
-    } else if (to) {
-        for (int i = tid; i < cells; i += L::threads) {
-            const int r = i / dc, k = i % dc;
-            to[i] = empty || !from ? 0.f : from_t ? from[k * da + r] : from[i];
+            if (chunks > 0) {
+#pragma unroll 1
+                for (int part = D == 64; part >= 0; --part) {  // D = 64: lanes 64 and up, then the others onto them
+                    if (D == 128 || (quad >= 2) == (part == 1)) {
+                        uint32_t r[32];
+                        TC_LD32(tmem + ((uint32_t)(quad * 32) << 16) + L::tX + col0, r);
+                        tc::tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 32; i += 4) {
+                            float4 *const at = x + state_at<D>(xrow & (D - 1), (col0 + i) / 4);
+                            float4 v = make_float4(__uint_as_float(r[i]), __uint_as_float(r[i + 1]), __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
+                            if (D == 64 && part == 0) {
+                                const float4 o = *at;
+                                v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
+                            }
+                            *at = v;
+                        }
+                    }
+                    worker_barrier<D>();
+                }
+                bad |= state_out<D>(x, to, da, dc, empty);
+                if (bad) {
+                    decay_mark(p, m.job, m.pair);
+                    if constexpr (STATE)
+                        for (int i = 0; i < p.jobs; ++i)  // (another job may read this state)
+                            if (p.job[i].spans_t) decay_mark(p, i, m.pair);
+                }
+            } else if (to) {
+                for (int i = tid; i < cells; i += L::workers) {
+                    const int r = i / dc, k = i % dc;
+                    to[i] = empty || !from ? 0.f : from_t ? from[k * da + r] : from[i];
+                }
+            }
+            done += chunks;
+            m = next;
+            g = g_next;
+            worker_barrier<D>();  // (tables and places are free)
         }
     }
     tc::fence_before_sync();
@@ -853,7 +943,7 @@ template <int D, bool STATE, bool TMA, bool CUT>
 cudaError_t launch(const decay_pass &p, const decay_maps &maps, unsigned grid, cudaStream_t s) {
     const cudaError_t e = cudaFuncSetAttribute(decay_tc_kernel<D, STATE, TMA, CUT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Plan<D>::bytes);
     if (e != cudaSuccess) return e;
-    decay_tc_kernel<D, STATE, TMA, CUT><<<dim3(grid, p.spans), Plan<D>::threads, Plan<D>::bytes, s>>>(p, maps);
+    decay_tc_kernel<D, STATE, TMA, CUT><<<grid, Plan<D>::threads, Plan<D>::bytes, s>>>(p, maps);
     return cudaGetLastError();
 }
 template <int D, bool STATE>
@@ -866,8 +956,10 @@ cudaError_t launch(const decay_pass &p, const decay_maps &maps, unsigned grid, c
 cudaError_t wm_seq_decay_tc_launch(wm_seq *h, const decay_pass &p, const decay_maps &maps, bool state, cudaStream_t s) {
     int jobs = 0;
     for (int i = 0; i < p.jobs; ++i) jobs += !(state && p.job[i].spans_t);
-    const unsigned grid = (unsigned)((long long)p.N * p.H * jobs);
+    const int D = std::max(p.job[0].da, p.job[0].dc) <= 64 ? 64 : 128;
+    const long long items = (long long)p.N * p.H * jobs * p.spans;
+    const unsigned grid = (unsigned)std::min(items, (long long)h->sms * (D == 64 ? 2 : 1));
     ++h->last_launches;
-    if (std::max(p.job[0].da, p.job[0].dc) <= 64) return state ? launch<64, true>(p, maps, grid, s) : launch<64, false>(p, maps, grid, s);
+    if (D == 64) return state ? launch<64, true>(p, maps, grid, s) : launch<64, false>(p, maps, grid, s);
     return state ? launch<128, true>(p, maps, grid, s) : launch<128, false>(p, maps, grid, s);
 }
