@@ -62,8 +62,12 @@ struct Plan {
     static constexpr int b = 0, lo = b + 2 * tile, xb = lo + tile, a = xb + D * 128 * (D / 64), c = a + 2 * tile, end = c + tile;
     static constexpr int small = end;  // tables and barriers
     static constexpr int bytes = small + 4 * 132 + 8 * 128 + 48 + 48 + 1024;
-    // P lies over A's first columns; with D = 64 O2 over A's others
-    static constexpr int tA = 0, tO1 = 128, tO2 = D == 64 ? 64 : 256, tX = D == 64 ? 192 : 384, columns = D == 64 ? 256 : 512;
+    // P lies over A: 16 tokens' column pairs where their warps read them, in blocks of `own` columns of A; with D = 64 O2, in two
+    // halves, over the rest of each block
+    static constexpr int own = 128 / (D / 32);
+    static constexpr int tA = 0, tO1 = 128, tX = D == 64 ? 192 : 384, columns = D == 64 ? 256 : 512;
+    static constexpr int p_at(int k) { return tA + k * 16 / own * own + k * 16 % own / 2; }     // of tokens 16 k and on
+    static constexpr int o2_at(int group) { return D == 64 ? 32 + 64 * group : 256 + 32 * group; }  // of 32 outputs
 };
 
 // MN-major operand, 128-byte swizzle: 64 values a row of 128 bytes; `panel` bytes to the next 64 values, 1024 to the next
@@ -242,6 +246,17 @@ __device__ __forceinline__ bool state_out(const float4 *x, float *to, int da, in
     }
     return !(odd == 0.f);
 }
+// What the workers hand to the issuing warp: they arrive and go on, it waits.  (No worker arrives twice before it has waited:
+// in between each waits for a product that was issued after.)
+enum { kRead = 6, kScaled = 7, kReady = 8 };
+template <int D>
+__device__ __forceinline__ void hand_over(int id) {
+    asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(Plan<D>::threads) : "memory");
+}
+template <int D>
+__device__ __forceinline__ void take_over(int id) {
+    asm volatile("bar.sync %0, %1;" ::"r"(id), "n"(Plan<D>::threads) : "memory");
+}
 template <int D>
 __device__ __forceinline__ void worker_barrier() {
     asm volatile("bar.sync 5, %0;" ::"n"(Plan<D>::workers) : "memory");
@@ -387,36 +402,38 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             const int slot = done & 1;
             const uint32_t ta = base + L::a + slot * L::tile, tb = base + L::b + slot * L::tile, tv = base + L::c;
             if (TMA && !(early && done > 0)) wait(barQK + 8 * slot, done >> 1);
-            tc::fence_before_sync();
-            __syncthreads();  // 1: the chunk before is read out
+            take_over<D>(kRead);  // the chunk before is read out
             tc::fence_after_sync();
             if (!STATE && !(early && done > 0)) form_a(slot);
             if (TMA && done > 0) {
                 step(ahead);
                 load_ab(ahead, slot ^ 1);
             }
-            tc::fence_before_sync();
-            __syncthreads();  // 2: A is read, Xb there
-            tc::fence_after_sync();
+            if (!STATE) {
+                take_over<D>(kScaled);  // A is read, Xb there
+                tc::fence_after_sync();
+            }
             if (!STATE && has_x && tc::elect_one()) {
+                constexpr int parts = D == 64 ? 2 : 1;
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k)
-                    tc::mma_bf16(tmem + L::tO2, tc::desc_sw128(ta + (k / 4) * kPanel + (k % 4) * 32), desc_mn(base + L::xb + k * 2048, D * 128),
-                                 tc::idesc_bf16_f32(128, D) | kBmn, k > 0);
+                for (int part = 0; part < parts; ++part)
+#pragma unroll
+                    for (int k = 0; k < D / 16; ++k)
+                        tc::mma_bf16(tmem + L::o2_at(part), tc::desc_sw128(ta + (k / 4) * kPanel + (k % 4) * 32),
+                                     desc_mn(base + L::xb + k * 2048 + part * 64, D * 128), tc::idesc_bf16_f32(128, D / parts) | kBmn, k > 0);
             }
             __syncwarp();
+            if constexpr (TMA) wait(barV, done);
+            take_over<D>(kReady);  // P and the keys' parts are there
+            tc::fence_after_sync();
             bool keeps_x = true;
             if constexpr (CUT) keeps_x = (cuts[slot * 4] | cuts[slot * 4 + 1] | cuts[slot * 4 + 2] | cuts[slot * 4 + 3]) == 0;
-            if constexpr (TMA) wait(barV, done);
-            tc::fence_before_sync();
-            __syncthreads();  // 3: P and the keys' parts are there
-            tc::fence_after_sync();
             const bool onto = (STATE ? !fresh : has_x) && keeps_x;
             if (tc::elect_one()) {
                 if constexpr (!STATE) {
 #pragma unroll
                     for (int k = 0; k < kChunk / 16; ++k)
-                        mma_bf16_ts(tmem + L::tO1, tmem + L::tA + k * 8, desc_mn(tv + k * 2048, kPanel), tc::idesc_bf16_f32(128, D) | kBmn, k > 0);
+                        mma_bf16_ts(tmem + L::tO1, tmem + L::p_at(k), desc_mn(tv + k * 2048, kPanel), tc::idesc_bf16_f32(128, D) | kBmn, k > 0);
                     tc::mma_commit(barO);
                 }
                 // (D = 64: both parts as one operand of 128 rows)
@@ -541,8 +558,8 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 if constexpr (!STATE) tma_store_read();  // (the outputs' copies have read a's tile, which is filled again)
                 tc::fence_proxy_async_smem();
                 tc::fence_before_sync();
-                __syncthreads();  // 1
-                tc::fence_after_sync();
+                if (CUT || !TMA) worker_barrier<D>();  // the chunk's cuts, or its tiles, are there
+                hand_over<D>(kRead);
                 if (!TMA && c > 0) load_ab(c + 1);
                 // tokens that begin something new: what a token sees begins with the last of them up to it (counted in steps)
                 int keep_from = -1, begin = -1;
@@ -564,7 +581,10 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 }
                 // (time's order, the last token of all: the state leaves as that token wrote it)
                 const int less = !STATE && j.first && s0 + rows == len ? 1 : 0;
-                if (tid < kChunk && (CUT || STATE || c == 0 || rows < kChunk || less)) {
+                if (STATE && TMA) wait(barQK + 8 * slot, phase >> 1);
+                const bool weigh_again = CUT || STATE || c == 0 || rows < kChunk || less;
+                if (weigh_again && c > 0) worker_barrier<D>();  // (the chunk before has its weights)
+                if (weigh_again && tid < kChunk) {
                     float w = 0.f;
                     const int s = step_of(tid);
                     if (s < rows && s >= keep_from) {
@@ -575,6 +595,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                     const float w1 = __bfloat162float(__float2bfloat16_rn(w));
                     kept[tid] = make_uint2(pack2(w1, w1), pack2(w - w1, w - w1));
                 }
+                if (weigh_again) worker_barrier<D>();
                 constexpr int cols = 128 / (D / 32);  // of A, a thread
                 uint32_t packed[cols / 2];
                 if constexpr (!STATE) {
@@ -701,13 +722,12 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                         }
                     }
                 }
-                tc::fence_proxy_async_smem();  // Xb
-                tc::fence_before_sync();
-                __syncthreads();  // 2: A is read, P and O2 may take its place (STATE: kept is there)
-                tc::fence_after_sync();
                 if constexpr (!STATE) {
-                    if constexpr (cols == 64) TC_ST32(mine + L::tA + group * 32, packed);
-                    else TC_ST16(mine + L::tA + group * 16, packed);
+                    tc::fence_proxy_async_smem();  // Xb
+                    tc::fence_before_sync();
+                    hand_over<D>(kScaled);
+                    if constexpr (cols == 64) TC_ST32(mine + L::tA + group * 64, packed);
+                    else TC_ST16(mine + L::tA + group * 32, packed);
                 }
                 // b -> b w as two bf16 values, the first in b's place: with w = w1 + w2, hi = b w1 rounded, lo = (b w1 - hi) + b w2,
                 // where b w1 - hi is exact (16 bits of a product, the first 8 taken away)
@@ -752,7 +772,8 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 if constexpr (!STATE) tmem_st_wait();
                 tc::fence_proxy_async_smem();
                 tc::fence_before_sync();
-                __syncthreads();  // 3
+                if (!TMA) worker_barrier<D>();  // (their tiles' copies, by all of them)
+                hand_over<D>(kReady);
                 find_cuts(c + 1);
                 if constexpr (!STATE) {
                     // y = O1 + in_scale lambda^step O2, by way of a's tile (32 rows of 64 bytes a warp, 64-byte swizzle) to whole rows
@@ -764,7 +785,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                     TC_LD32(mine + L::tO1 + col0, o1);
                     if (has_x) {
                         uint32_t o2[32];
-                        TC_LD32(mine + L::tO2 + col0, o2);
+                        TC_LD32(mine + L::o2_at(group), o2);
                         tc::tmem_ld_wait();
                         if (sees) {
 #pragma unroll
