@@ -42,43 +42,68 @@ struct HeadArgs {
     const float *freqs;
 };
 
-// How a row is cut: vectors of VEC values; IN: pairs are neighbours within a vector.
+// Rows that a thread has on their way: so many that their loads come to about 32 values.
+constexpr int rows_of(int lane_values, bool bwd) { return lane_values <= 4 ? 4 : lane_values <= (bwd ? 8 : 16) ? 2 : 1; }
+
+// The columns' weights of a thread: in registers, or read when they are needed.
+template <int VEC, int UPL>
+constexpr bool held() {
+    return VEC * UPL <= 8;
+}
+
+struct TileRow {  // where a token's rows begin
+    long long x, y, o;
+};
+// Shared memory: phases, two tiles' angles and rows, weights (and, for their gradient, a row of sums a warp).
+struct HeadsSmem {
+    size_t turn, row, weight, bytes;
+    __host__ __device__ HeadsSmem(int half, int tile, int D, bool backward) {
+        turn = ((size_t)half * 8 + 15) / 16 * 16;
+        row = (turn + (size_t)2 * tile * half * 8 + 15) / 16 * 16;
+        weight = row + (size_t)2 * tile * sizeof(TileRow);
+        bytes = weight + (size_t)(backward ? kThreads / 32 : 1) * ((D + 7) / 8 * 8) * 4;
+    }
+};
+
+// VEC values a vector, UPL units a lane; IN: pairs are neighbours within a vector.
 template <class T, int VEC, bool IN, int UPL, bool BWD>
-__global__ void __launch_bounds__(kThreads, UPL *VEC >= 16 ? 1 : BWD ? 2 : 4) heads_kernel(const HeadArgs p) {
+__global__ void __launch_bounds__(kThreads, UPL *VEC > 8 ? 1 : BWD ? 2 : 4) heads_kernel(const __grid_constant__ HeadArgs p) {
+    constexpr int R = rows_of(2 * VEC * UPL, BWD);
+    constexpr bool HELD = held<VEC, UPL>();
     extern __shared__ __align__(16) unsigned char smem[];
     const int half = p.rotary / 2;
+    const HeadsSmem at(half, p.tile, p.D, BWD);
     unsigned long long *phase = reinterpret_cast<unsigned long long *>(smem);
-    float2 *turn = reinterpret_cast<float2 *>(phase + half);                    // [tile][half]: cos, sin
-    float *weight = reinterpret_cast<float *>(turn + (size_t)p.tile * half);    // [D], padded to whole vectors
+    float2 *const turns = reinterpret_cast<float2 *>(smem + at.turn);     // [2][tile][half]: cos, sin
+    TileRow *const starts = reinterpret_cast<TileRow *>(smem + at.row);   // [2][tile]
+    float *const weight = reinterpret_cast<float *>(smem + at.weight);
     const bool keys = blockIdx.x >= (unsigned)p.side[0].ctas;
     const Side &sd = p.side[keys];
-    const int cta = blockIdx.x - (keys ? p.side[0].ctas : 0);
+    const int cta = blockIdx.x - (keys ? p.side[0].ctas : 0), heads = sd.heads;
+    const long long stride = (long long)sd.ctas * p.tile;
     for (int i = threadIdx.x; i < half; i += kThreads) {
-        const double turns = (double)p.freqs[i] * 0.15915494309189533577;
-        phase[i] = __double2ull_rz((turns - floor(turns)) * 18446744073709551616.0);
+        const double t = (double)p.freqs[i] * 0.15915494309189533577;
+        phase[i] = __double2ull_rz((t - floor(t)) * 18446744073709551616.0);
     }
     for (int j = threadIdx.x; j < p.D; j += kThreads) weight[j] = sd.w ? sd.w[j] : 1.f;
 
     const int lane = threadIdx.x & (p.group - 1), row0 = threadIdx.x / p.group, rows_at_once = kThreads / p.group;
     const int nv = (p.D + VEC - 1) / VEC;
-    int va[UPL], vb[UPL];  // the unit's vectors; -1: none
+    int va[UPL], vb[UPL];  // the unit's vectors: their first values
+    bool ha[UPL], hb[UPL], turns_here[UPL];
 #pragma unroll
     for (int i = 0; i < UPL; ++i) {
         const int u = lane + i * p.group;
-        va[i] = vb[i] = -1;
-        if (u < p.units) {
-            va[i] = u < p.hc ? u * p.sa : 2 * p.hc + 2 * (u - p.hc);
-            vb[i] = u < p.hc ? va[i] + p.sb : va[i] + 1;
-            if (vb[i] >= nv) vb[i] = -1;
-        }
+        const int a = u < p.hc ? u * p.sa : 2 * p.hc + 2 * (u - p.hc), b = u < p.hc ? a + p.sb : a + 1;
+        ha[i] = u < p.units;
+        hb[i] = ha[i] && b < nv;
+        turns_here[i] = u < p.hc;
+        va[i] = ha[i] ? a * VEC : 0;
+        vb[i] = hb[i] ? b * VEC : 0;
     }
-    float dwa[BWD ? UPL : 1][VEC] = {}, dwb[BWD ? UPL : 1][VEC] = {};
-    const float inv_d = 1.f / (float)p.D;
-    const bool sums = BWD && sd.part;
-
-    for (long long tok0 = (long long)cta * p.tile; tok0 < p.tokens; tok0 += (long long)sd.ctas * p.tile) {
+    // a tile's angles and rows, into the places of even or odd tiles
+    const auto prepare = [&](long long tok0, int slot) {
         const int tile = (int)min((long long)p.tile, p.tokens - tok0);
-        __syncthreads();  // the angles of the tile before are read; weights and phases are there
         for (int i = threadIdx.x; i < tile * half; i += kThreads) {
             const int k = i / half, j = i - k * half;
             const unsigned long long ph = phase[j] * (unsigned long long)(long long)p.positions[tok0 + k];
@@ -86,152 +111,212 @@ __global__ void __launch_bounds__(kThreads, UPL *VEC >= 16 ? 1 : BWD ? 2 : 4) he
             sincospif((float)(int)((ph + (1ull << 31)) >> 32) * 0x1p-31f, &sn, &cs);
             const float f = p.freqs[j];
             if (!(fabsf(f) <= 3.4028235e38f)) sn = cs = f - f;  // NaN: no angle of a frequency that is none
-            turn[i] = make_float2(cs, sn);
+            turns[slot * p.tile * half + i] = make_float2(cs, sn);
         }
-        __syncthreads();
-        const int rows = tile * sd.heads;
-        for (int r0 = 0; r0 < rows; r0 += rows_at_once) {  // (all lanes walk along: they sum over the group)
-            const int r = r0 + row0;
-            const bool on = r < rows;
-            const int k = on ? r / sd.heads : 0, head = on ? r - k * sd.heads : 0;
+        const int k = (int)threadIdx.x - (kThreads - 32);  // (the last warp: it has the fewest angles)
+        if (k >= 0 && k < tile) {
             const long long tok = tok0 + k, t = tok / p.N, n = tok - t * p.N;
-            const T *x = static_cast<const T *>(sd.x) + t * sd.xt + n * sd.xn + head * sd.xh;
-            const T *dy = BWD ? static_cast<const T *>(sd.dy) + t * sd.yt + n * sd.yn + head * sd.yh : nullptr;
-            T *out = static_cast<T *>(sd.out) + t * sd.ot + n * sd.on + head * sd.oh;
-            const float2 *tw = turn + k * half;
-            seq_vec<T, VEC> xa[UPL], xb[UPL], ya[BWD ? UPL : 1], yb[BWD ? UPL : 1];
+            starts[slot * p.tile + k] = {t * sd.xt + n * sd.xn, t * sd.yt + n * sd.yn, t * sd.ot + n * sd.on};
+        }
+    };
+    __syncthreads();
+    long long tok0 = (long long)cta * p.tile;
+    if (tok0 < p.tokens) prepare(tok0, 0);
+    float wa[HELD ? UPL : 1][VEC], wb[HELD ? UPL : 1][VEC];
+    const auto weights_of = [&](int i, float(&a)[VEC], float(&b)[VEC]) {
 #pragma unroll
-            for (int i = 0; i < UPL; ++i) {
-                const bool a = on && va[i] >= 0, b = on && vb[i] >= 0;
-                xa[i] = a ? seq_load<T, VEC>(x + va[i] * VEC) : seq_vec<T, VEC>{};
-                xb[i] = b ? seq_load<T, VEC>(x + vb[i] * VEC) : seq_vec<T, VEC>{};
-                if constexpr (BWD) {
-                    ya[i] = a ? seq_load<T, VEC>(dy + va[i] * VEC) : seq_vec<T, VEC>{};
-                    yb[i] = b ? seq_load<T, VEC>(dy + vb[i] * VEC) : seq_vec<T, VEC>{};
-                }
-            }
-            // turns a unit's values in place, by sign * angle
-            auto rotate = [&](int i, float(&a)[VEC], float(&b)[VEC], float sign) {
-                if constexpr (IN) {
+        for (int m = 0; m < VEC; ++m) a[m] = weight[va[i] + m], b[m] = weight[vb[i] + m];
+    };
+    if constexpr (HELD) {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        float(&v)[VEC] = h ? b : a;
-                        const int at = (h ? vb[i] : va[i]) * VEC;
-                        if (at < 0 || at >= p.rotary) continue;
+        for (int i = 0; i < UPL; ++i) weights_of(i, wa[i], wb[i]);
+    }
+    float dwa[BWD ? UPL : 1][VEC] = {}, dwb[BWD ? UPL : 1][VEC] = {};
+    const float inv_d = 1.f / (float)p.D;
+    const int down = rows_at_once / heads, across = rows_at_once - down * heads;  // from a row to the thread's next
+    __syncthreads();
+
+    for (int slot = 0; tok0 < p.tokens; tok0 += stride, slot ^= 1) {
+        if (tok0 + stride < p.tokens) prepare(tok0 + stride, slot ^ 1);
+        const int tile = (int)min((long long)p.tile, p.tokens - tok0), rows = tile * heads;
+        const float2 *const turn = turns + slot * p.tile * half;
+        const TileRow *const start = starts + slot * p.tile;
+        int token = row0 / heads, head = row0 - token * heads;
+        for (int r = row0; r - row0 < rows; r += R * rows_at_once) {  // (all lanes walk along: they sum over the group)
+            seq_vec<T, VEC> xa[R][UPL], xb[R][UPL], ya[BWD ? R : 1][UPL], yb[BWD ? R : 1][UPL];
+            T *out[R];
+            const float2 *tw[R];
 #pragma unroll
-                        for (int m = 0; m + 1 < VEC; m += 2) {
-                            const float2 cs = tw[(at + m) / 2];
-                            const float s = sign * cs.y, u = v[m], w = v[m + 1];
-                            v[m] = u * cs.x - w * s;
-                            v[m + 1] = w * cs.x + u * s;
-                        }
+            for (int q = 0; q < R; ++q) {
+                const bool on = r + q * rows_at_once < rows;
+                const TileRow s = start[on ? token : 0];
+                const T *const x = static_cast<const T *>(sd.x) + s.x + (on ? head : 0) * sd.xh;
+                const T *const dy = BWD ? static_cast<const T *>(sd.dy) + s.y + (on ? head : 0) * sd.yh : nullptr;
+                out[q] = static_cast<T *>(sd.out) + s.o + (on ? head : 0) * sd.oh;
+                tw[q] = turn + (on ? token : 0) * half;
+#pragma unroll
+                for (int i = 0; i < UPL; ++i) {
+                    xa[q][i] = on && ha[i] ? seq_load<T, VEC>(x + va[i]) : seq_vec<T, VEC>{};
+                    xb[q][i] = on && hb[i] ? seq_load<T, VEC>(x + vb[i]) : seq_vec<T, VEC>{};
+                    if constexpr (BWD) {
+                        ya[q][i] = on && ha[i] ? seq_load<T, VEC>(dy + va[i]) : seq_vec<T, VEC>{};
+                        yb[q][i] = on && hb[i] ? seq_load<T, VEC>(dy + vb[i]) : seq_vec<T, VEC>{};
                     }
-                } else {
-                    const int u = lane + i * p.group;
-                    if (u < p.hc) {
+                }
+                token += down;
+                head += across;
+                if (head >= heads) head -= heads, ++token;
+            }
+#pragma unroll
+            for (int q = 0; q < R; ++q) {
+                const bool on = r + q * rows_at_once < rows;
+                // turns a unit's values in place, by sign * angle
+                const auto rotate = [&](int i, float(&a)[VEC], float(&b)[VEC], float sign) {
+                    if constexpr (IN) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            float(&v)[VEC] = h ? b : a;
+                            const int from = h ? vb[i] : va[i];
+                            if (from >= p.rotary) continue;
+                            float c[VEC];  // cos, sin, cos, sin ...
+#pragma unroll
+                            for (int m = 0; m < VEC; m += VEC < 4 ? 2 : 4) {
+                                if constexpr (VEC < 4) {
+                                    const float2 t = tw[q][from / 2];
+                                    c[0] = t.x, c[1] = t.y;
+                                } else {
+                                    const float4 t = *reinterpret_cast<const float4 *>(tw[q] + (from + m) / 2);
+                                    c[m] = t.x, c[m + 1] = t.y, c[m + 2] = t.z, c[m + 3] = t.w;
+                                }
+                            }
+#pragma unroll
+                            for (int m = 0; m < VEC; m += 2) {
+                                const float s = sign * c[m + 1], u = v[m], w = v[m + 1];
+                                v[m] = u * c[m] - w * s;
+                                v[m + 1] = w * c[m] + u * s;
+                            }
+                        }
+                    } else if (turns_here[i]) {
+                        const float2 *const t = tw[q] + (lane + i * p.group) * VEC;
+                        float c[VEC], s[VEC];
+                        if constexpr (VEC == 1) {
+                            c[0] = t->x, s[0] = t->y;
+                        } else {
+#pragma unroll
+                            for (int m = 0; m < VEC; m += 2) {
+                                const float4 two = *reinterpret_cast<const float4 *>(t + m);
+                                c[m] = two.x, s[m] = two.y, c[m + 1] = two.z, s[m + 1] = two.w;
+                            }
+                        }
 #pragma unroll
                         for (int m = 0; m < VEC; ++m) {
-                            const float2 cs = tw[u * VEC + m];
-                            const float s = sign * cs.y, q = a[m], w = b[m];
-                            a[m] = q * cs.x - w * s;
-                            b[m] = w * cs.x + q * s;
+                            const float n = sign * s[m], u = a[m], w = b[m];
+                            a[m] = u * c[m] - w * n;
+                            b[m] = w * c[m] + u * n;
                         }
                     }
-                }
-            };
-            float ss = 0.f, gx = 0.f;
-            float fa[UPL][VEC], fb[UPL][VEC], da[BWD ? UPL : 1][VEC], db[BWD ? UPL : 1][VEC];
+                };
+                float ss = 0.f, gx = 0.f;
+                float fa[UPL][VEC], fb[UPL][VEC], da[BWD ? UPL : 1][VEC], db[BWD ? UPL : 1][VEC];
 #pragma unroll
-            for (int i = 0; i < UPL; ++i) {
-                seq_unpack<T, VEC>(xa[i], fa[i]);
-                seq_unpack<T, VEC>(xb[i], fb[i]);
+                for (int i = 0; i < UPL; ++i) {
+                    seq_unpack<T, VEC>(xa[q][i], fa[i]);
+                    seq_unpack<T, VEC>(xb[q][i], fb[i]);
 #pragma unroll
-                for (int m = 0; m < VEC; ++m) ss += fa[i][m] * fa[i][m] + fb[i][m] * fb[i][m];
-                if constexpr (BWD) {
-                    seq_unpack<T, VEC>(ya[i], da[i]);
-                    seq_unpack<T, VEC>(yb[i], db[i]);
-                    rotate(i, da[i], db[i], -1.f);
+                    for (int m = 0; m < VEC; ++m) ss += fa[i][m] * fa[i][m] + fb[i][m] * fb[i][m];
+                    if constexpr (BWD) {
+                        float ua[VEC], ub[VEC];
+                        if constexpr (!HELD) weights_of(i, ua, ub);
+                        seq_unpack<T, VEC>(ya[q][i], da[i]);
+                        seq_unpack<T, VEC>(yb[q][i], db[i]);
+                        rotate(i, da[i], db[i], -1.f);
 #pragma unroll
-                    for (int m = 0; m < VEC; ++m) {
-                        const float wa = va[i] >= 0 ? weight[va[i] * VEC + m] : 0.f, wb = vb[i] >= 0 ? weight[vb[i] * VEC + m] : 0.f;
-                        gx += da[i][m] * wa * fa[i][m] + db[i][m] * wb * fb[i][m];
+                        for (int m = 0; m < VEC; ++m)
+                            gx += da[i][m] * (HELD ? wa[HELD ? i : 0][m] : ua[m]) * fa[i][m] + db[i][m] * (HELD ? wb[HELD ? i : 0][m] : ub[m]) * fb[i][m];
                     }
                 }
-            }
-            for (int o = p.group / 2; o > 0; o >>= 1) {
-                ss += __shfl_xor_sync(~0u, ss, o);
-                if constexpr (BWD) gx += __shfl_xor_sync(~0u, gx, o);
-            }
-            const float rs = 1.f / sqrtf(ss * inv_d + p.eps);
-            const float back = BWD ? rs * rs * (gx * inv_d) : 0.f;
+                for (int o = p.group / 2; o > 0; o >>= 1) {
+                    ss += __shfl_xor_sync(~0u, ss, o);
+                    if constexpr (BWD) gx += __shfl_xor_sync(~0u, gx, o);
+                }
+                const float rs = 1.f / sqrtf(ss * inv_d + p.eps);
+                const float back = BWD ? rs * rs * (gx * inv_d) : 0.f;
 #pragma unroll
-            for (int i = 0; i < UPL; ++i) {
-                if constexpr (BWD) {
-                    if (sums && on) {
+                for (int i = 0; i < UPL; ++i) {
+                    float ua[VEC], ub[VEC];
+                    if constexpr (!HELD) weights_of(i, ua, ub);
+                    if constexpr (BWD) {
+                        if (on) {  // (of rows that are there: what a thread without one holds may be what it likes)
+#pragma unroll
+                            for (int m = 0; m < VEC; ++m) {
+                                dwa[i][m] += da[i][m] * (fa[i][m] * rs);
+                                dwb[i][m] += db[i][m] * (fb[i][m] * rs);
+                            }
+                        }
 #pragma unroll
                         for (int m = 0; m < VEC; ++m) {
-                            dwa[i][m] += da[i][m] * (fa[i][m] * rs);
-                            dwb[i][m] += db[i][m] * (fb[i][m] * rs);
+                            fa[i][m] = rs * (da[i][m] * (HELD ? wa[HELD ? i : 0][m] : ua[m]) - fa[i][m] * back);
+                            fb[i][m] = rs * (db[i][m] * (HELD ? wb[HELD ? i : 0][m] : ub[m]) - fb[i][m] * back);
                         }
-                    }
+                    } else {
 #pragma unroll
-                    for (int m = 0; m < VEC; ++m) {
-                        const float wa = va[i] >= 0 ? weight[va[i] * VEC + m] : 0.f, wb = vb[i] >= 0 ? weight[vb[i] * VEC + m] : 0.f;
-                        fa[i][m] = rs * (da[i][m] * wa - fa[i][m] * back);
-                        fb[i][m] = rs * (db[i][m] * wb - fb[i][m] * back);
+                        for (int m = 0; m < VEC; ++m) {
+                            fa[i][m] = fa[i][m] * rs * (HELD ? wa[HELD ? i : 0][m] : ua[m]);
+                            fb[i][m] = fb[i][m] * rs * (HELD ? wb[HELD ? i : 0][m] : ub[m]);
+                        }
+                        rotate(i, fa[i], fb[i], 1.f);
                     }
-                } else {
-#pragma unroll
-                    for (int m = 0; m < VEC; ++m) {
-                        const float wa = va[i] >= 0 ? weight[va[i] * VEC + m] : 0.f, wb = vb[i] >= 0 ? weight[vb[i] * VEC + m] : 0.f;
-                        fa[i][m] = fa[i][m] * rs * wa;
-                        fb[i][m] = fb[i][m] * rs * wb;
-                    }
-                    rotate(i, fa[i], fb[i], 1.f);
+                    if (on && ha[i]) seq_store<T, VEC>(out[q] + va[i], seq_pack<T, VEC>(fa[i]));
+                    if (on && hb[i]) seq_store<T, VEC>(out[q] + vb[i], seq_pack<T, VEC>(fb[i]));
                 }
-                if (on && va[i] >= 0) seq_store<T, VEC>(out + va[i] * VEC, seq_pack<T, VEC>(fa[i]));
-                if (on && vb[i] >= 0) seq_store<T, VEC>(out + vb[i] * VEC, seq_pack<T, VEC>(fb[i]));
             }
         }
+        __syncthreads();  // this tile's places are free, the next one's are there
     }
     if constexpr (BWD) {
-        if (!sums) return;
-        // the row groups' sums, added in their order
-        __syncthreads();
-        float *acc = weight;  // [rows_at_once][D] would not fit for all: one group after another adds its own
-        for (int j = threadIdx.x; j < p.D; j += kThreads) acc[j] = 0.f;
-        for (int g = 0; g < rows_at_once; ++g) {
-            __syncthreads();
-            if (row0 != g) continue;
+        if (!sd.part) return;
+        // over a warp's row groups by halves, then the warps one after the other
+        float *const sums = weight + (threadIdx.x >> 5) * ((p.D + 7) / 8 * 8);
 #pragma unroll
-            for (int i = 0; i < UPL; ++i)
+        for (int i = 0; i < UPL; ++i)
 #pragma unroll
-                for (int m = 0; m < VEC; ++m) {
-                    if (va[i] >= 0) acc[va[i] * VEC + m] += dwa[i][m];
-                    if (vb[i] >= 0) acc[vb[i] * VEC + m] += dwb[i][m];
+            for (int m = 0; m < VEC; ++m) {
+                for (int o = 16; o >= p.group; o >>= 1) {
+                    dwa[i][m] += __shfl_xor_sync(~0u, dwa[i][m], o);
+                    dwb[i][m] += __shfl_xor_sync(~0u, dwb[i][m], o);
                 }
-        }
+                if ((threadIdx.x & 31) < p.group) {
+                    if (ha[i]) sums[va[i] + m] = dwa[i][m];
+                    if (hb[i]) sums[vb[i] + m] = dwb[i][m];
+                }
+            }
         __syncthreads();
-        for (int j = threadIdx.x; j < p.D; j += kThreads) sd.part[(long long)cta * p.D + j] = acc[j];
+        for (int j = threadIdx.x; j < p.D; j += kThreads) {
+            float v = weight[j];
+            for (int w = 1; w < kThreads / 32; ++w) v += weight[w * ((p.D + 7) / 8 * 8) + j];
+            sd.part[(long long)cta * p.D + j] = v;
+        }
     }
 }
 
-// dweight[j] = sum of the CTAs' parts, 32 columns a block and 8 stretches of CTAs.
+// dweight[j] = sum of the CTAs' parts: 8 columns a block, 32 stretches of CTAs.
 __global__ void __launch_bounds__(256) heads_weight_kernel(const float *part0, const float *part1, int ctas0, int ctas1, int D,
                                                            float *dw0, float *dw1) {
-    __shared__ float sum[8][32];
+    __shared__ float sum[32][8];
     const bool keys = blockIdx.y;
     const float *part = keys ? part1 : part0;
     float *dw = keys ? dw1 : dw0;
-    const int ctas = keys ? ctas1 : ctas0, x = threadIdx.x & 31, y = threadIdx.x >> 5, j = blockIdx.x * 32 + x;
+    const int ctas = keys ? ctas1 : ctas0, x = threadIdx.x & 7, y = threadIdx.x >> 3, j = blockIdx.x * 8 + x;
     if (!dw) return;
     float v = 0.f;
-    if (j < D)
-        for (int c = y; c < ctas; c += 8) v += part[(long long)c * D + j];
+    if (j < D) {
+#pragma unroll 4
+        for (int c = y; c < ctas; c += 32) v += part[(long long)c * D + j];
+    }
     sum[y][x] = v;
     __syncthreads();
     if (y == 0 && j < D) {
-        for (int k = 1; k < 8; ++k) v += sum[k][x];
+        for (int k = 1; k < 32; ++k) v += sum[k][x];
         dw[j] = v;
     }
 }
@@ -255,25 +340,32 @@ int vector_of(const seq_heads_args &a, bool backward) {
     return 1;
 }
 
-// CTAs of queries and keys: 4 an SM over both, by their heads, no more than there are tiles.
-void ctas_of(const wm_seq *h, const seq_heads_args &a, long long tiles, int (&ctas)[2]) {
-    const int all = a.heads[0] + a.heads[1], room = 8 * h->sms;
+// CTAs of queries and keys: as many as run at once, shared by their heads, no more than there are tiles.
+void ctas_of(const wm_seq *h, const seq_heads_args &a, bool backward, long long tiles, int (&ctas)[2]) {
+    const int all = a.heads[0] + a.heads[1], room = (backward ? 2 : 4) * h->sms;
     for (int i = 0; i < 2; ++i) {
         const long long share = a.heads[i] ? std::max(1ll, (long long)room * a.heads[i] / all) : 0;
         ctas[i] = (int)std::min(share, std::max(a.heads[i] ? 1ll : 0, tiles));
     }
 }
 
-int tile_of(const wm_seq *h, const seq_heads_args &a) {
-    const long long tokens = a.T * a.N;
-    // about an angle a thread, and no fewer tiles than CTAs
-    const long long want = a.rotary ? std::max(1, 512 / a.rotary) : 16, fair = tokens / (8ll * h->sms);
-    return (int)std::max(1ll, std::min({want, fair, 16ll}));
+// Tokens of a tile: about 8 rows a thread group between two barriers, as long as every CTA has one.
+int tile_of(const wm_seq *h, const seq_heads_args &a, bool backward) {
+    const long long tokens = a.T * a.N, fair = tokens * (a.heads[1] ? 2 : 1) / ((backward ? 2ll : 4ll) * h->sms);
+    const int heads = std::max(a.heads[0], a.heads[1]);
+    const long long want = std::max(1, 8 * 64 * 64 / (heads * std::max(a.D, 64)));
+    const long long room = a.rotary ? 8192 / a.rotary : 32;  // 64 KB of angles
+    return (int)std::max(1ll, std::min({want, fair, room, 32ll}));
 }
 
 template <class T, int VEC, bool IN, int UPL>
 cudaError_t run(wm_seq *h, const HeadArgs &p, bool backward, cudaStream_t s) {
-    const size_t bytes = (size_t)p.rotary / 2 * 8 * (1 + p.tile) + (size_t)((p.D + VEC - 1) / VEC * VEC) * 4;
+    const size_t bytes = HeadsSmem(p.rotary / 2, p.tile, p.D, backward).bytes;
+    cudaError_t e = cudaSuccess;
+    if (bytes > 48 << 10)
+        e = backward ? cudaFuncSetAttribute(heads_kernel<T, VEC, IN, UPL, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes)
+                     : cudaFuncSetAttribute(heads_kernel<T, VEC, IN, UPL, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (e != cudaSuccess) return e;
     const unsigned grid = (unsigned)(p.side[0].ctas + p.side[1].ctas);
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(grid);
@@ -328,8 +420,8 @@ cudaError_t run_type(wm_seq *h, HeadArgs &p, const seq_heads_args &a, bool backw
 size_t wm_seq_heads_backward_ws(const wm_seq *h, const seq_heads_args &a) {
     if (!a.dweight[0] && !a.dweight[1]) return 0;
     int ctas[2];
-    const int tile = tile_of(h, a);
-    ctas_of(h, a, (a.T * a.N + tile - 1) / tile, ctas);
+    const int tile = tile_of(h, a, true);
+    ctas_of(h, a, true, (a.T * a.N + tile - 1) / tile, ctas);
     return (size_t)(ctas[0] + ctas[1]) * a.D * 4;
 }
 
@@ -339,9 +431,9 @@ cudaError_t wm_seq_heads_launch(wm_seq *h, const seq_heads_args &a, bool backwar
     p.tokens = a.T * a.N;
     p.N = a.N; p.D = a.D; p.rotary = a.rotary; p.eps = a.eps;
     p.positions = a.positions; p.freqs = a.freqs;
-    p.tile = tile_of(h, a);
+    p.tile = tile_of(h, a, backward);
     int ctas[2];
-    ctas_of(h, a, (p.tokens + p.tile - 1) / p.tile, ctas);
+    ctas_of(h, a, backward, (p.tokens + p.tile - 1) / p.tile, ctas);
     for (int i = 0; i < 2; ++i) {
         Side &d = p.side[i];
         d.heads = a.heads[i];
@@ -357,7 +449,7 @@ cudaError_t wm_seq_heads_launch(wm_seq *h, const seq_heads_args &a, bool backwar
     if (e != cudaSuccess || !backward || (!a.dweight[0] && !a.dweight[1])) return e;
     if (p.tokens == 0) ctas[0] = ctas[1] = 0;  // (no rows: sums of nothing)
     ++h->last_launches;
-    heads_weight_kernel<<<dim3((a.D + 31) / 32, 2), 256, 0, s>>>(p.side[0].part, p.side[1].part, ctas[0], ctas[1], a.D, a.dweight[0],
+    heads_weight_kernel<<<dim3((a.D + 7) / 8, 2), 256, 0, s>>>(p.side[0].part, p.side[1].part, ctas[0], ctas[1], a.D, a.dweight[0],
                                                                  a.dweight[1]);
     return cudaGetLastError();
 }
