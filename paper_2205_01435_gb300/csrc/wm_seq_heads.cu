@@ -36,7 +36,7 @@ struct HeadArgs {
     int N, D, rotary;
     int hc, sa, sb;    // units below hc: vectors u sa and u sa + sb turn into one another; the others are two in a row
     int units, group;  // of a row; lanes a row
-    int tile;          // tokens
+    int tile;          // tokens that a warp takes at once
     float eps;
     const int32_t *positions;
     const float *freqs;
@@ -54,40 +54,45 @@ constexpr bool held() {
 struct TileRow {  // where a token's rows begin
     long long x, y, o;
 };
-// Shared memory: phases, two tiles' angles and rows, weights (and, for their gradient, a row of sums a warp).
+// Shared memory: phases, two tiles' angles and rows for each warp, weights (and, for their gradient, a row of sums a warp).
+constexpr int kWarps = kThreads / 32;
 struct HeadsSmem {
     size_t turn, row, weight, bytes;
     __host__ __device__ HeadsSmem(int half, int tile, int D, bool backward) {
         turn = ((size_t)half * 8 + 15) / 16 * 16;
-        row = (turn + (size_t)2 * tile * half * 8 + 15) / 16 * 16;
-        weight = row + (size_t)2 * tile * sizeof(TileRow);
-        bytes = weight + (size_t)(backward ? kThreads / 32 : 1) * ((D + 7) / 8 * 8) * 4;
+        row = (turn + (size_t)kWarps * 2 * tile * half * 8 + 15) / 16 * 16;
+        weight = row + (size_t)kWarps * 2 * tile * sizeof(TileRow);
+        bytes = weight + (size_t)(backward ? kWarps : 1) * ((D + 7) / 8 * 8) * 4;
     }
 };
 
 // VEC values a vector, UPL units a lane; IN: pairs are neighbours within a vector.
 template <class T, int VEC, bool IN, int UPL, bool BWD>
-__global__ void __launch_bounds__(kThreads, UPL *VEC > 8 ? 1 : BWD ? 2 : 4) heads_kernel(const __grid_constant__ HeadArgs p) {
+__global__ void __launch_bounds__(kThreads, UPL *VEC > 8 ? 1 : BWD ? 2 : 3) heads_kernel(const __grid_constant__ HeadArgs p) {
     constexpr int R = rows_of(2 * VEC * UPL, BWD);
     constexpr bool HELD = held<VEC, UPL>();
     extern __shared__ __align__(16) unsigned char smem[];
     const int half = p.rotary / 2;
     const HeadsSmem at(half, p.tile, p.D, BWD);
     unsigned long long *phase = reinterpret_cast<unsigned long long *>(smem);
-    float2 *const turns = reinterpret_cast<float2 *>(smem + at.turn);     // [2][tile][half]: cos, sin
-    TileRow *const starts = reinterpret_cast<TileRow *>(smem + at.row);   // [2][tile]
+    const int warp = threadIdx.x >> 5, wl = threadIdx.x & 31;
+    float2 *const turns = reinterpret_cast<float2 *>(smem + at.turn) + (size_t)warp * 2 * p.tile * half;  // [2][tile][half]: cos, sin
+    TileRow *const starts = reinterpret_cast<TileRow *>(smem + at.row) + warp * 2 * p.tile;               // [2][tile]
     float *const weight = reinterpret_cast<float *>(smem + at.weight);
     const bool keys = blockIdx.x >= (unsigned)p.side[0].ctas;
     const Side &sd = p.side[keys];
     const int cta = blockIdx.x - (keys ? p.side[0].ctas : 0), heads = sd.heads;
-    const long long stride = (long long)sd.ctas * p.tile;
+    // the warp's tokens
+    const long long w0 = (long long)cta * kWarps + warp, all = (long long)sd.ctas * kWarps;
+    long long tok0 = p.tokens * w0 / all;
+    const long long end = p.tokens * (w0 + 1) / all;
     for (int i = threadIdx.x; i < half; i += kThreads) {
         const double t = (double)p.freqs[i] * 0.15915494309189533577;
         phase[i] = __double2ull_rz((t - floor(t)) * 18446744073709551616.0);
     }
     for (int j = threadIdx.x; j < p.D; j += kThreads) weight[j] = sd.w ? sd.w[j] : 1.f;
 
-    const int lane = threadIdx.x & (p.group - 1), row0 = threadIdx.x / p.group, rows_at_once = kThreads / p.group;
+    const int lane = wl & (p.group - 1), row0 = wl / p.group, rows_at_once = 32 / p.group;
     const int nv = (p.D + VEC - 1) / VEC;
     int va[UPL], vb[UPL];  // the unit's vectors: their first values
     bool ha[UPL], hb[UPL], turns_here[UPL];
@@ -103,25 +108,24 @@ __global__ void __launch_bounds__(kThreads, UPL *VEC > 8 ? 1 : BWD ? 2 : 4) head
     }
     // a tile's angles and rows, into the places of even or odd tiles
     const auto prepare = [&](long long tok0, int slot) {
-        const int tile = (int)min((long long)p.tile, p.tokens - tok0);
-        for (int i = threadIdx.x; i < tile * half; i += kThreads) {
-            const int k = i / half, j = i - k * half;
-            const unsigned long long ph = phase[j] * (unsigned long long)(long long)p.positions[tok0 + k];
-            float sn, cs;
-            sincospif((float)(int)((ph + (1ull << 31)) >> 32) * 0x1p-31f, &sn, &cs);
-            const float f = p.freqs[j];
-            if (!(fabsf(f) <= 3.4028235e38f)) sn = cs = f - f;  // NaN: no angle of a frequency that is none
-            turns[slot * p.tile * half + i] = make_float2(cs, sn);
+        const int tile = (int)min((long long)p.tile, end - tok0);
+        for (int k = 0; k < tile; ++k) {
+            const unsigned long long pos = half ? (unsigned long long)(long long)p.positions[tok0 + k] : 0;
+            for (int j = wl; j < half; j += 32) {
+                float sn, cs;
+                sincospif((float)(int)((phase[j] * pos + (1ull << 31)) >> 32) * 0x1p-31f, &sn, &cs);
+                const float f = p.freqs[j];
+                if (!(fabsf(f) <= 3.4028235e38f)) sn = cs = f - f;  // NaN: no angle of a frequency that is none
+                turns[(slot * p.tile + k) * half + j] = make_float2(cs, sn);
+            }
         }
-        const int k = (int)threadIdx.x - (kThreads - 32);  // (the last warp: it has the fewest angles)
-        if (k >= 0 && k < tile) {
-            const long long tok = tok0 + k, t = tok / p.N, n = tok - t * p.N;
-            starts[slot * p.tile + k] = {t * sd.xt + n * sd.xn, t * sd.yt + n * sd.yn, t * sd.ot + n * sd.on};
+        if (wl < tile) {
+            const long long tok = tok0 + wl, t = tok / p.N, n = tok - t * p.N;
+            starts[slot * p.tile + wl] = {t * sd.xt + n * sd.xn, t * sd.yt + n * sd.yn, t * sd.ot + n * sd.on};
         }
     };
     __syncthreads();
-    long long tok0 = (long long)cta * p.tile;
-    if (tok0 < p.tokens) prepare(tok0, 0);
+    if (tok0 < end) prepare(tok0, 0);
     float wa[HELD ? UPL : 1][VEC], wb[HELD ? UPL : 1][VEC];
     const auto weights_of = [&](int i, float(&a)[VEC], float(&b)[VEC]) {
 #pragma unroll
@@ -134,11 +138,11 @@ __global__ void __launch_bounds__(kThreads, UPL *VEC > 8 ? 1 : BWD ? 2 : 4) head
     float dwa[BWD ? UPL : 1][VEC] = {}, dwb[BWD ? UPL : 1][VEC] = {};
     const float inv_d = 1.f / (float)p.D;
     const int down = rows_at_once / heads, across = rows_at_once - down * heads;  // from a row to the thread's next
-    __syncthreads();
+    __syncwarp();
 
-    for (int slot = 0; tok0 < p.tokens; tok0 += stride, slot ^= 1) {
-        if (tok0 + stride < p.tokens) prepare(tok0 + stride, slot ^ 1);
-        const int tile = (int)min((long long)p.tile, p.tokens - tok0), rows = tile * heads;
+    for (int slot = 0; tok0 < end; tok0 += p.tile, slot ^= 1) {
+        if (tok0 + p.tile < end) prepare(tok0 + p.tile, slot ^ 1);
+        const int tile = (int)min((long long)p.tile, end - tok0), rows = tile * heads;
         const float2 *const turn = turns + slot * p.tile * half;
         const TileRow *const start = starts + slot * p.tile;
         int token = row0 / heads, head = row0 - token * heads;
@@ -271,12 +275,13 @@ __global__ void __launch_bounds__(kThreads, UPL *VEC > 8 ? 1 : BWD ? 2 : 4) head
                 }
             }
         }
-        __syncthreads();  // this tile's places are free, the next one's are there
+        __syncwarp();  // this tile's places are free, the next one's are there
     }
     if constexpr (BWD) {
         if (!sd.part) return;
-        // over a warp's row groups by halves, then the warps one after the other
-        float *const sums = weight + (threadIdx.x >> 5) * ((p.D + 7) / 8 * 8);
+        // over a warp's row groups by halves, then the warps one after the other (in the weights' place)
+        __syncthreads();
+        float *const sums = weight + warp * ((p.D + 7) / 8 * 8);
 #pragma unroll
         for (int i = 0; i < UPL; ++i)
 #pragma unroll
@@ -285,7 +290,7 @@ __global__ void __launch_bounds__(kThreads, UPL *VEC > 8 ? 1 : BWD ? 2 : 4) head
                     dwa[i][m] += __shfl_xor_sync(~0u, dwa[i][m], o);
                     dwb[i][m] += __shfl_xor_sync(~0u, dwb[i][m], o);
                 }
-                if ((threadIdx.x & 31) < p.group) {
+                if (wl < p.group) {
                     if (ha[i]) sums[va[i] + m] = dwa[i][m];
                     if (hb[i]) sums[vb[i] + m] = dwb[i][m];
                 }
@@ -340,22 +345,21 @@ int vector_of(const seq_heads_args &a, bool backward) {
     return 1;
 }
 
-// CTAs of queries and keys: as many as run at once, shared by their heads, no more than there are tiles.
-void ctas_of(const wm_seq *h, const seq_heads_args &a, bool backward, long long tiles, int (&ctas)[2]) {
-    const int all = a.heads[0] + a.heads[1], room = (backward ? 2 : 4) * h->sms;
+// CTAs of queries and keys: as many as run at once, shared by their heads, no more than their warps have tokens.
+void ctas_of(const wm_seq *h, const seq_heads_args &a, bool backward, int (&ctas)[2]) {
+    const int all = a.heads[0] + a.heads[1], room = (backward ? 2 : 3) * h->sms;
+    const long long tokens = a.T * a.N;
     for (int i = 0; i < 2; ++i) {
         const long long share = a.heads[i] ? std::max(1ll, (long long)room * a.heads[i] / all) : 0;
-        ctas[i] = (int)std::min(share, std::max(a.heads[i] ? 1ll : 0, tiles));
+        ctas[i] = (int)std::min(share, std::max(a.heads[i] ? 1ll : 0, (tokens + kWarps - 1) / kWarps));
     }
 }
 
-// Tokens of a tile: about 8 rows a thread group between two barriers, as long as every CTA has one.
-int tile_of(const wm_seq *h, const seq_heads_args &a, bool backward) {
-    const long long tokens = a.T * a.N, fair = tokens * (a.heads[1] ? 2 : 1) / ((backward ? 2ll : 4ll) * h->sms);
-    const int heads = std::max(a.heads[0], a.heads[1]);
-    const long long want = std::max(1, 8 * 64 * 64 / (heads * std::max(a.D, 64)));
-    const long long room = a.rotary ? 8192 / a.rotary : 32;  // 64 KB of angles
-    return (int)std::max(1ll, std::min({want, fair, room, 32ll}));
+// Tokens a warp takes at once: about 4 turns of two rows a lane group.
+int tile_of(const seq_heads_args &a, int group) {
+    const int heads = std::max(a.heads[0], a.heads[1]), want = std::max(1, 8 * (32 / group) / heads);
+    const int room = a.rotary ? std::max(1, 1024 / a.rotary) : 32;  // 64 KB of angles
+    return std::min({want, room, 32});
 }
 
 template <class T, int VEC, bool IN, int UPL>
@@ -378,14 +382,20 @@ cudaError_t run(wm_seq *h, const HeadArgs &p, bool backward, cudaStream_t s) {
 }
 
 template <class T, int VEC, bool IN>
-cudaError_t run_units(wm_seq *h, HeadArgs &p, bool backward, cudaStream_t s) {
+cudaError_t run_units(wm_seq *h, HeadArgs &p, const seq_heads_args &a, bool backward, cudaStream_t s) {
+    // (a lane holds up to 8 values of each of a unit's vectors, 4 where it loads them one by one)
+    constexpr int most = VEC >= 8 ? 1 : VEC == 4 ? 2 : 4;
     int g = 1;
-    while (g < 32 && g < p.units) g <<= 1;
+    while (g < 32 && p.units > most * g) g <<= 1;
     p.group = g;
+    p.tile = tile_of(a, g);
     const int upl = (p.units + g - 1) / g;
     if (upl <= 1) return run<T, VEC, IN, 1>(h, p, backward, s);
     if constexpr (VEC <= 4 || sizeof(T) == 2) {
         if (upl <= 2) return run<T, VEC, IN, 2>(h, p, backward, s);
+    }
+    if constexpr (VEC <= 2) {
+        if (upl <= 3) return run<T, VEC, IN, 3>(h, p, backward, s);
     }
     if constexpr (VEC <= 4) {
         if (upl <= 4) return run<T, VEC, IN, 4>(h, p, backward, s);
@@ -408,11 +418,11 @@ cudaError_t run_type(wm_seq *h, HeadArgs &p, const seq_heads_args &a, bool backw
     p.sb = a.interleaved ? 1 : p.hc;
     p.units = p.hc + (nv - 2 * p.hc + 1) / 2;
     if constexpr (sizeof(T) == 2) {
-        if (vec == 8) return in ? run_units<T, 8, true>(h, p, backward, s) : run_units<T, 8, false>(h, p, backward, s);
+        if (vec == 8) return in ? run_units<T, 8, true>(h, p, a, backward, s) : run_units<T, 8, false>(h, p, a, backward, s);
     }
-    if (vec == 4) return in ? run_units<T, 4, true>(h, p, backward, s) : run_units<T, 4, false>(h, p, backward, s);
-    if (vec == 2) return in ? run_units<T, 2, true>(h, p, backward, s) : run_units<T, 2, false>(h, p, backward, s);
-    return run_units<T, 1, false>(h, p, backward, s);
+    if (vec == 4) return in ? run_units<T, 4, true>(h, p, a, backward, s) : run_units<T, 4, false>(h, p, a, backward, s);
+    if (vec == 2) return in ? run_units<T, 2, true>(h, p, a, backward, s) : run_units<T, 2, false>(h, p, a, backward, s);
+    return run_units<T, 1, false>(h, p, a, backward, s);
 }
 
 }  // namespace
@@ -420,8 +430,7 @@ cudaError_t run_type(wm_seq *h, HeadArgs &p, const seq_heads_args &a, bool backw
 size_t wm_seq_heads_backward_ws(const wm_seq *h, const seq_heads_args &a) {
     if (!a.dweight[0] && !a.dweight[1]) return 0;
     int ctas[2];
-    const int tile = tile_of(h, a, true);
-    ctas_of(h, a, true, (a.T * a.N + tile - 1) / tile, ctas);
+    ctas_of(h, a, true, ctas);
     return (size_t)(ctas[0] + ctas[1]) * a.D * 4;
 }
 
@@ -431,9 +440,8 @@ cudaError_t wm_seq_heads_launch(wm_seq *h, const seq_heads_args &a, bool backwar
     p.tokens = a.T * a.N;
     p.N = a.N; p.D = a.D; p.rotary = a.rotary; p.eps = a.eps;
     p.positions = a.positions; p.freqs = a.freqs;
-    p.tile = tile_of(h, a, backward);
     int ctas[2];
-    ctas_of(h, a, backward, (p.tokens + p.tile - 1) / p.tile, ctas);
+    ctas_of(h, a, backward, ctas);
     for (int i = 0; i < 2; ++i) {
         Side &d = p.side[i];
         d.heads = a.heads[i];
