@@ -21,65 +21,103 @@
 
 namespace {
 
-constexpr int kChunk = 64, kSlice = 64, kPad = 4, kThreads = 256;
+constexpr int kChunk = 64, kSlice = 64, kThreads = 256;
 
 __device__ __forceinline__ float4 ld4(const float *p) { return *reinterpret_cast<const float4 *>(p); }
 
 // ------------------------------------------------------------------ chunks in fp32
-// A CTA: one sequence of one head, one job, kSlice values of c.  Tiles in shared memory as fp32, a thread 4 x 4 outputs.
-// STATE: only what the span's tokens give the state.
+// A CTA: one sequence of one head, one job, kSlice values of c.  Every product sums over the quads of two tiles' rows, so that a
+// thread's 4 x 4 outputs take 8 quads from shared memory and 32 instructions of two multiply-adds for 64 of them: c and the
+// weighted b are turned over on the way, the state is held as [values of c][values of a].  (128 x 128 x 8 x 64, forward: 205 us
+// with one multiply-add an instruction and rows read across.)
+// A tile: rows of ld floats (a multiple of 32), the quads of row r turned by r & 7: 8 rows' quads of one column lie in 8 places.
+__device__ __forceinline__ int quad_at(int r, int quad, int ld) { return r * ld + ((quad ^ (r & 7)) << 2); }
+__device__ __forceinline__ int cell_at(int r, int c, int ld) { return quad_at(r, c >> 2, ld) + (c & 3); }
+
+template <int LD>  // values of a row of a, b and x: 64, 128 or 256
 struct ChunkTiles {
-    int ld;  // of a and b
-    float *a, *b, *c, *p, *x, *kept;
-    __device__ ChunkTiles(float *m, int da) {
-        const int dp = (da + 3) / 4 * 4;
-        ld = dp + kPad;
-        a = m;
-        b = a + kChunk * ld;
-        c = b + kChunk * ld;
-        p = c + kChunk * kSlice;
-        x = p + kChunk * kChunk;
-        kept = x + dp * kSlice;
+    float *a, *b, *c, *p, *x, *kept, *power;
+    __device__ explicit ChunkTiles(float *m) {
+        a = m;                      // [64][LD]; the weighted b turned over, [LD][64], once a is read
+        b = a + kChunk * LD;        // [64][LD]
+        c = b + kChunk * LD;        // turned over: [64 values][64 tokens]
+        p = c + kSlice * kChunk;    // [64][64]: c as it comes, then the products
+        x = p + kChunk * kChunk;    // [64 values of c][LD]
+        kept = x + kSlice * LD;
+        power = kept + kChunk;      // lambda^0 .. lambda^64
     }
-    static size_t bytes(int da) {
-        const int dp = (da + 3) / 4 * 4;
-        return sizeof(float) * (2 * kChunk * (dp + kPad) + kChunk * kSlice + kChunk * kChunk + dp * kSlice + kChunk);
-    }
+    static constexpr size_t bytes = sizeof(float) * (2 * kChunk * LD + kSlice * kChunk + kChunk * kChunk + kSlice * LD + kChunk + kChunk + 4);
 };
 
-// Rows [0, rows) of a chunk, D values from column col0, zeros up to D padded to 4 (and the rows behind); true if a value
-// is not finite.
-template <class T>
-__device__ __forceinline__ bool load_rows(float *dst, int ld, const decay_array &g, long long base, const decay_seq &q, long long s0, int rows,
-                                          int col0, int D, int Dp, int vec) {
-    bool odd = false;
+// Rows [0, rows) of a chunk, D values from column col0, zeros around; true if a value is not finite.
+template <class T, int ld>
+__device__ __forceinline__ bool load_rows(float *dst, const decay_array &g, long long base, const decay_seq &q, long long s0, int rows,
+                                          int col0, int D, int vec) {
+    float odd = 0.f;
+    const int step = q.reverse ? -1 : 1;
+    const T *const first = static_cast<const T *>(g.p) + base + q.at(s0) * g.t + col0;
     if (vec > 1) {  // 16 bytes
         constexpr int V = 16 / sizeof(T);
-        const int per = (Dp + V - 1) / V;
+        constexpr int per = ld / V;
         for (int i = threadIdx.x; i < kChunk * per; i += kThreads) {
             const int r = i / per, d = (i - r * per) * V;
             float f[V] = {};
-            if (r < rows && d < D)
-                seq_unpack<T, V>(seq_load<T, V>(static_cast<const T *>(g.p) + base + q.at(s0 + r) * g.t + col0 + d), f);
+            if (r < rows && d < D) seq_unpack<T, V>(seq_load<T, V>(first + (long long)(step * r) * g.t + d), f);
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                odd |= !(fabsf(f[k]) <= 3.4028235e38f);
-                if (d + k < Dp) dst[r * ld + d + k] = f[k];
+            for (int k = 0; k < V; k += 4) {
+                odd += f[k] * 0.f + f[k + 1] * 0.f + f[k + 2] * 0.f + f[k + 3] * 0.f;
+                *reinterpret_cast<float4 *>(dst + quad_at(r, (d + k) / 4, ld)) = make_float4(f[k], f[k + 1], f[k + 2], f[k + 3]);
             }
         }
     } else {
-        for (int i = threadIdx.x; i < kChunk * Dp; i += kThreads) {
-            const int r = i / Dp, d = i - r * Dp;
-            float f = 0.f;
-            if (r < rows && d < D) f = seq_to_float(static_cast<const T *>(g.p)[base + q.at(s0 + r) * g.t + col0 + d]);
-            odd |= !(fabsf(f) <= 3.4028235e38f);
-            dst[r * ld + d] = f;
-        }
+        for (int r = threadIdx.x >> 5; r < kChunk; r += kThreads / 32)
+            for (int d = threadIdx.x & 31; d < ld; d += 32) {
+                float f = 0.f;
+                if (r < rows && d < D) f = seq_to_float(first[(long long)(step * r) * g.t + d]);
+                odd += f * 0.f;
+                dst[cell_at(r, d, ld)] = f;
+            }
     }
-    return odd;
+    return !(odd == 0.f);
 }
 
-template <class T, bool STATE>
+// acc[i][k] += sums over `quads` quads of rows r0 + i of u and rows c0 + 16 k of v, for k < B.  (r0 a multiple of 4.  The quads of
+// rows 16 apart are turned alike: one address for all k, the rest in the instructions; quads are taken 4 at a time, those behind
+// the last are zeros.)
+template <int LDU, int LDV, int B>
+__device__ __forceinline__ void products(seq_pair (&acc)[4][4], const float *u, int r0, const float *v, int c0, int quads) {
+    const char *const ub = reinterpret_cast<const char *>(u + r0 * LDU), *const vb = reinterpret_cast<const char *>(v + c0 * LDV);
+    const int ut = (r0 & 7) << 4, vt = (c0 & 7) << 4;
+#pragma unroll 1
+    for (int d0 = 0; d0 < quads << 4; d0 += 64) {
+#pragma unroll
+        for (int e = 0; e < 64; e += 16) {
+            float4 x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const float4 *>(ub + ((d0 | e) ^ ut ^ (i << 4)) + i * LDU * 4);
+            const char *const y0 = vb + ((d0 | e) ^ vt);
+#pragma unroll
+            for (int k = 0; k < B; ++k) {
+                const float4 y = *reinterpret_cast<const float4 *>(y0 + k * 16 * LDV * 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    acc[i][k] = seq_fma2(seq_pair_of(x[i].x, x[i].y), seq_pair_of(y.x, y.y), acc[i][k]);
+                    acc[i][k] = seq_fma2(seq_pair_of(x[i].z, x[i].w), seq_pair_of(y.z, y.w), acc[i][k]);
+                }
+            }
+        }
+    }
+}
+template <int LDU, int LDV>
+__device__ __forceinline__ void products(seq_pair (&acc)[4][4], const float *u, int r0, const float *v, int c0, int quads, int blocks) {
+    if (blocks == 4) products<LDU, LDV, 4>(acc, u, r0, v, c0, quads);
+    else if (blocks == 3) products<LDU, LDV, 3>(acc, u, r0, v, c0, quads);
+    else if (blocks == 2) products<LDU, LDV, 2>(acc, u, r0, v, c0, quads);
+    else products<LDU, LDV, 1>(acc, u, r0, v, c0, quads);
+}
+
+// STATE: only what the span's tokens give the state.
+template <class T, bool STATE, int LD>
 __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, float *smem, unsigned (&cuts)[2]) {
     int job = 0, slice = item;
     long long pair = 0;
@@ -98,14 +136,15 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
     const decay_job &j = p.job[job];
     if (p.only_redo && !p.redo[1 + job * (long long)p.N * p.H + pair]) return;
     __syncthreads();  // (an item before this one is done with the shared memory)
-    const int n = (int)(pair / p.H), head = (int)(pair % p.H), span = blockIdx.y, da = j.da, dp = (da + 3) / 4 * 4;
-    const int col0 = slice * kSlice, cols = min(kSlice, j.dc - col0), colp = (cols + 3) / 4 * 4;
-    const ChunkTiles m(smem, da);
+    const int n = (int)(pair / p.H), head = (int)(pair % p.H), span = blockIdx.y, da = j.da, dq = (da + 3) / 4;
+    const int col0 = slice * kSlice, cols = min(kSlice, j.dc - col0);
+    const ChunkTiles<LD> m(smem);
     const decay_seq q = decay_open(p, j, n);
     const float g = p.log_decay[head];
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
     const long long pairs = (long long)p.N * p.H, cells = (long long)da * j.dc;
     const long long first = span * p.span_tokens, last = min(p.T, first + p.span_tokens);
+    const int cblocks = (cols + 15) / 16;  // of 16 values of c
 
     // the entering state
     const float *from = nullptr;
@@ -121,12 +160,13 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
             if (j.first && q.len > 0) mul = decay_power(g, 1);
         }
     }
-    for (int i = tid; i < dp * kSlice; i += kThreads) {
-        const int r = i / kSlice, c = i % kSlice;
+    for (int i = tid; i < LD * kSlice; i += kThreads) {
+        const int r = i / kSlice, c = i % kSlice;  // (value of a, of c)
         float v = 0.f;
         if (from && r < da && c < cols) v = (from_t ? from[(long long)(col0 + c) * da + r] : from[(long long)r * j.dc + col0 + c]);
-        m.x[i] = mul == 1.f ? v : v * mul;
+        m.x[cell_at(c, r, LD)] = mul == 1.f ? v : v * mul;
     }
+    if (tid <= kChunk) m.power[tid] = decay_power(g, tid);
     float carry = 1.f;
 
     const long long an = n * j.a.n + head * j.a.h, bn = n * j.b.n + head * j.b.h, cn = n * j.c.n + head * j.c.h;
@@ -140,14 +180,14 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
             continue;
         }
         __syncthreads();
-        bool odd = load_rows<T>(m.b, m.ld, j.b, bn, q, s0, rows, 0, da, dp, j.vec);
-        odd |= load_rows<T>(m.c, kSlice, j.c, cn, q, s0, rows, col0, cols, kSlice, j.vec);
-        if constexpr (!STATE) load_rows<T>(m.a, m.ld, j.a, an, q, s0, rows, 0, da, dp, j.vec);
+        bool odd = load_rows<T, LD>(m.b, j.b, bn, q, s0, rows, 0, da, j.vec);
+        odd |= load_rows<T, kSlice>(m.p, j.c, cn, q, s0, rows, col0, cols, j.vec);
+        if constexpr (!STATE) load_rows<T, LD>(m.a, j.a, an, q, s0, rows, 0, da, j.vec);
         if (tid < 64) {
             const unsigned c = __ballot_sync(~0u, decay_cut(p, q, s0 + tid, n) && tid < rows);
             if ((tid & 31) == 0) cuts[tid >> 5] = c;
         }
-        const bool careful = __syncthreads_or(odd);  // (its zero weights would make NaN of what is not finite)
+        const bool careful = __syncthreads_or(odd);  // (zero weights would make NaN of what is not finite)
         const unsigned long long cut = cuts[0] | (unsigned long long)cuts[1] << 32;
         // the first token that token i sees; with none of the chunk cut before, the state too
         auto start = [&](int i) {
@@ -156,28 +196,33 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
         };
         const int keep_from = start(rows - 1);
         // (time's order, the last chunk of all: the state leaves as the last token wrote it)
-        const int less = j.first && p.span_tokens > 0 && s0 + rows == q.len && !STATE ? 1 : 0;
-        if (tid < kChunk) m.kept[tid] = tid < rows && tid >= keep_from ? j.up_scale * decay_power(g, rows - tid - less) : 0.f;
+        const int less = j.first && s0 + rows == q.len && !STATE ? 1 : 0;
+        if (tid < kChunk) m.kept[tid] = tid < rows && tid >= keep_from ? j.up_scale * m.power[rows - tid - less] : 0.f;
+        // rows [64][ld] -> [ld][64], each row times its weight (0: nothing of it); a thread takes whole quads of a row
+        const auto turn = [&](float *to, const float *rowsm, int ld, int quads, const float *w) {
+            for (int i = tid; i < kChunk * quads; i += kThreads) {
+                const int r = i % kChunk, d = i / kChunk;
+                float4 v = ld4(rowsm + quad_at(r, d, ld));
+                if (w) {
+                    const float f = w[r];
+                    v = f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+                }
+                to[cell_at(4 * d, r, kChunk)] = v.x;
+                to[cell_at(4 * d + 1, r, kChunk)] = v.y;
+                to[cell_at(4 * d + 2, r, kChunk)] = v.z;
+                to[cell_at(4 * d + 3, r, kChunk)] = v.w;
+            }
+        };
+        turn(m.c, m.p, kSlice, kSlice / 4, nullptr);
 
         if constexpr (!STATE) {
             int begin[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) begin[i] = start(ty * 4 + i);
-            // p = a b^T, weighted
-            const int nb = ty / 4 + 1;  // columns beyond the rows' own are not seen
-            float acc[4][4] = {};
-            for (int d = 0; d < dp; d += 4) {
-                float4 x[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = ld4(m.a + (ty * 4 + i) * m.ld + d);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if (k >= nb) break;
-                    const float4 y = ld4(m.b + (tx + 16 * k) * m.ld + d);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[i][k] += x[i].x * y.x + x[i].y * y.y + x[i].z * y.z + x[i].w * y.w;
-                }
-            }
+            // p = a b^T, weighted; columns beyond the rows' own are not seen
+            seq_pair acc[4][4] = {};
+            products<LD, LD>(acc, m.a, ty * 4, m.b, tx, dq, ty / 4 + 1);
+            __syncthreads();  // (c is turned over: p's place is free)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = ty * 4 + i;
@@ -185,84 +230,84 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
                 for (int k = 0; k < 4; ++k) {
                     const int c = tx + 16 * k;
                     const bool seen = c <= r && c >= begin[i] && r < rows;
-                    m.p[r * kChunk + c] = seen ? acc[i][k] * (j.w_scale * decay_power(g, r - c)) : 0.f;
+                    m.p[cell_at(r, c, kChunk)] = seen ? (acc[i][k].f.x + acc[i][k].f.y) * (j.w_scale * m.power[r - c]) : 0.f;
                 }
             }
             __syncthreads();
-            // y = p c + lambda^r X^T a
-            float y[4][4] = {};
-            if (tx * 4 < colp) {
-                if (!careful) {
-                    for (int k = 0; k < ty * 4 + 4; k += 4) {
-                        float4 w[4];
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) w[i] = ld4(m.p + (ty * 4 + i) * kChunk + k);
-#pragma unroll
-                        for (int h = 0; h < 4; ++h) {
-                            const float4 v = ld4(m.c + (k + h) * kSlice + tx * 4);
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const float f = h == 0 ? w[i].x : h == 1 ? w[i].y : h == 2 ? w[i].z : w[i].w;
-                                y[i][0] += f * v.x, y[i][1] += f * v.y, y[i][2] += f * v.z, y[i][3] += f * v.w;
-                            }
-                        }
-                    }
-                } else {
-                    for (int i = 0; i < 4; ++i)
-                        for (int k = max(begin[i], 0); k <= min(ty * 4 + i, rows - 1); ++k) {
-                            const float f = m.p[(ty * 4 + i) * kChunk + k];
-                            for (int h = 0; h < 4; ++h) y[i][h] += f * m.c[k * kSlice + tx * 4 + h];
-                        }
-                }
-                float in[4][4] = {};
-                for (int d = 0; d < dp; d += 4) {
-                    float4 x[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) x[i] = ld4(m.a + (ty * 4 + i) * m.ld + d);
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        const float4 v = ld4(m.x + (d + h) * kSlice + tx * 4);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float f = h == 0 ? x[i].x : h == 1 ? x[i].y : h == 2 ? x[i].z : x[i].w;
-                            in[i][0] += f * v.x, in[i][1] += f * v.y, in[i][2] += f * v.z, in[i][3] += f * v.w;
-                        }
-                    }
-                }
+            // y = lambda^r X^T a + p c
+            float y[4][4];
+            {
+                seq_pair in[4][4] = {};
+                products<LD, LD>(in, m.a, ty * 4, m.x, tx, dq, cblocks);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const int r = ty * 4 + i;
-                    if (s0 + r >= last) continue;
-                    const float w = j.in_scale * decay_power(g, r);
-                    T *out = static_cast<T *>(const_cast<void *>(j.y.p)) + n * j.y.n + head * j.y.h + q.at(s0 + r) * j.y.t + col0 + tx * 4;
+                    const float w = j.in_scale * m.power[ty * 4 + i];
 #pragma unroll
-                    for (int h = 0; h < 4; ++h)
-                        if (tx * 4 + h < cols)
-                            out[h] = seq_from_float<T>(r >= rows ? 0.f : begin[i] < 0 ? y[i][h] + w * in[i][h] : y[i][h]);
+                    for (int h = 0; h < 4; ++h) y[i][h] = begin[i] < 0 ? w * (in[i][h].f.x + in[i][h].f.y) : 0.f;
                 }
+            }
+            if (!careful) {
+                seq_pair own[4][4] = {};
+                products<kChunk, kChunk>(own, m.p, ty * 4, m.c, tx, ty + 1, cblocks);
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) y[i][h] += own[i][h].f.x + own[i][h].f.y;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    for (int k = max(begin[i], 0); k <= min(ty * 4 + i, rows - 1); ++k) {
+                        const float w = m.p[cell_at(ty * 4 + i, k, kChunk)];
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) y[i][h] += w * m.c[cell_at(tx + 16 * h, k, kChunk)];
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = ty * 4 + i;
+                if (s0 + r >= last) continue;
+                T *out = static_cast<T *>(const_cast<void *>(j.y.p)) + n * j.y.n + head * j.y.h + q.at(s0 + r) * j.y.t + col0 + tx;
+#pragma unroll
+                for (int h = 0; h < 4; ++h)
+                    if (tx + 16 * h < cols) out[16 * h] = seq_from_float<T>(r >= rows ? 0.f : y[i][h]);
             }
         }
         __syncthreads();
-        // X = lambda^n X + b^T (kept c)
-        const float shrink = decay_power(g, rows - less);
-        const int from_row = careful ? max(keep_from, 0) : 0;
-        if (tx * 4 < colp) {
-            for (int r0 = ty * 4; r0 < dp; r0 += 64) {
-                float acc[4][4] = {};
-                for (int k = from_row; k < rows; ++k) {
-                    const float4 u = ld4(m.b + k * m.ld + r0), v = ld4(m.c + k * kSlice + tx * 4);
-                    const float w = m.kept[k], f[4] = {u.x * w, u.y * w, u.z * w, u.w * w};
+        float *const bt = m.a;
+        turn(bt, m.b, LD, LD / 4, m.kept);
+        __syncthreads();
+        // X = lambda^n X + (kept b)^T c
+        const float shrink = m.power[rows - less];
+        if (ty * 4 < cols)
+            for (int r0 = 0; r0 < da; r0 += 64) {
+                seq_pair acc[4][4] = {};
+                const int blocks = min(4, (da - r0 + 15) / 16);
+                if (!careful) {
+                    products<kChunk, kChunk>(acc, m.c, ty * 4, bt + r0 * kChunk, tx, (rows + 3) / 4, blocks);
+                } else {
+                    for (int k = max(keep_from, 0); k < rows; ++k) {
+                        float v[4];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[i][0] += f[i] * v.x, acc[i][1] += f[i] * v.y, acc[i][2] += f[i] * v.z, acc[i][3] += f[i] * v.w;
+                        for (int h = 0; h < 4; ++h) v[h] = h < blocks ? bt[cell_at(r0 + tx + 16 * h, k, kChunk)] : 0.f;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const float u = m.c[cell_at(ty * 4 + i, k, kChunk)];
+#pragma unroll
+                            for (int h = 0; h < 4; ++h) acc[i][h].f.x += u * v[h];
+                        }
+                    }
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float *x = m.x + (r0 + i) * kSlice + tx * 4;
+                for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int h = 0; h < 4; ++h) x[h] = keep_from < 0 ? x[h] * shrink + acc[i][h] : acc[i][h];
-                }
+                    for (int h = 0; h < 4; ++h) {
+                        const int r = r0 + tx + 16 * h;
+                        if (r >= LD) break;
+                        float *const x = m.x + cell_at(ty * 4 + i, r, LD);
+                        const float v = acc[i][h].f.x + acc[i][h].f.y;
+                        *x = keep_from < 0 ? *x * shrink + v : v;
+                    }
             }
-        }
         carry = keep_from < 0 ? carry * shrink : 0.f;
     }
     __syncthreads();
@@ -278,18 +323,18 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
         empty = j.out_zero && q.len > 0 && p.reset && p.reset[n] != 0;
     }
     if (to)
-        for (int i = tid; i < da * cols; i += kThreads) {
-            const int r = i / cols, c = i - r * cols;
-            to[(long long)r * j.dc + col0 + c] = empty ? 0.f : m.x[r * kSlice + c];
+        for (int i = tid; i < da * kSlice; i += kThreads) {
+            const int r = i / kSlice, c = i % kSlice;
+            if (c < cols) to[(long long)r * j.dc + col0 + c] = empty ? 0.f : m.x[cell_at(c, r, LD)];
         }
 }
 
-template <class T, bool STATE>
-__global__ void __launch_bounds__(kThreads, 2) decay_chunk_kernel(const decay_pass p, int items) {
+template <class T, bool STATE, int LD>
+__global__ void __launch_bounds__(kThreads, LD == 64 ? 2 : 1) decay_chunk_kernel(const __grid_constant__ decay_pass p, int items) {
     extern __shared__ __align__(16) float smem[];
     __shared__ unsigned cuts[2];  // the chunk's tokens that begin something new
     if (p.only_redo && *p.redo == 0) return;
-    for (long long i = blockIdx.x; i < items; i += gridDim.x) decay_chunks<T, STATE>(p, (int)i, smem, cuts);
+    for (long long i = blockIdx.x; i < items; i += gridDim.x) decay_chunks<T, STATE, LD>(p, (int)i, smem, cuts);
 }
 
 // Spans' own parts -> what enters each span, along time.  A thread takes one cell of a state (QUAD: four), the parts of 8
@@ -579,17 +624,22 @@ int items_of(const decay_pass &p, bool state) {
     return (int)((long long)p.N * p.H * n);
 }
 
+template <class T, bool STATE, int LD>
+cudaError_t chunk_launch(wm_seq *h, const decay_pass &p, cudaStream_t s) {
+    constexpr int bytes = (int)ChunkTiles<LD>::bytes;
+    const cudaError_t e = cudaFuncSetAttribute(decay_chunk_kernel<T, STATE, LD>, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e != cudaSuccess) return e;
+    const int items = items_of(p, STATE);
+    ++h->last_launches;
+    decay_chunk_kernel<T, STATE, LD><<<dim3((unsigned)(p.only_redo ? std::min(items, h->sms) : items), p.spans), kThreads, bytes, s>>>(p, items);
+    return cudaGetLastError();
+}
 template <class T, bool STATE>
 cudaError_t chunk_launch(wm_seq *h, const decay_pass &p, cudaStream_t s) {
     int da = 0;
     for (int i = 0; i < p.jobs; ++i) da = std::max(da, p.job[i].da);
-    const size_t bytes = ChunkTiles::bytes(da);
-    const cudaError_t e = cudaFuncSetAttribute(decay_chunk_kernel<T, STATE>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    if (e != cudaSuccess) return e;
-    const int items = items_of(p, STATE);
-    ++h->last_launches;
-    decay_chunk_kernel<T, STATE><<<dim3((unsigned)(p.only_redo ? std::min(items, h->sms) : items), p.spans), kThreads, bytes, s>>>(p, items);
-    return cudaGetLastError();
+    if (da <= 64) return chunk_launch<T, STATE, 64>(h, p, s);
+    return da <= 128 ? chunk_launch<T, STATE, 128>(h, p, s) : chunk_launch<T, STATE, 256>(h, p, s);
 }
 
 // The pass, on tensor cores or in fp32; in spans, what each gives the state and the joins first.

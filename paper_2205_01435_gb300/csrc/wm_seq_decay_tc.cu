@@ -97,31 +97,11 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&v);
 }
-// Two fp32 values at a time.
-union Pair {
-    unsigned long long u;
-    float2 f;
-};
-__device__ __forceinline__ Pair pair_of(uint32_t a, uint32_t b) {
-    Pair p;
-    p.f = make_float2(__uint_as_float(a), __uint_as_float(b));
-    return p;
-}
-__device__ __forceinline__ Pair twice(float v) {
-    Pair p;
-    p.f = make_float2(v, v);
-    return p;
-}
-__device__ __forceinline__ Pair mul2(Pair a, Pair b) {
-    Pair r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u));
-    return r;
-}
-__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) {
-    Pair r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.u) : "l"(a.u), "l"(b.u), "l"(c.u));
-    return r;
-}
+using Pair = seq_pair;
+__device__ __forceinline__ Pair pair_of(uint32_t a, uint32_t b) { return seq_pair_of(__uint_as_float(a), __uint_as_float(b)); }
+__device__ __forceinline__ Pair twice(float v) { return seq_pair_of(v, v); }
+__device__ __forceinline__ Pair mul2(Pair a, Pair b) { return seq_mul2(a, b); }
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c) { return seq_fma2(a, b, c); }
 // Two bf16 values at a time.
 __device__ __forceinline__ uint32_t hmul(uint32_t a, uint32_t b) {
     uint32_t r;

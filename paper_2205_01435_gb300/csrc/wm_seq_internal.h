@@ -167,6 +167,27 @@ __device__ __forceinline__ void seq_store(T *p, const seq_vec<T, VEC> &v) {
     *reinterpret_cast<seq_vec<T, VEC> *>(p) = v;
 }
 
+// Two fp32 values at a time, in one instruction.
+union seq_pair {
+    unsigned long long u;
+    float2 f;
+};
+__device__ __forceinline__ seq_pair seq_pair_of(float a, float b) {
+    seq_pair p;
+    p.f = make_float2(a, b);
+    return p;
+}
+__device__ __forceinline__ seq_pair seq_mul2(seq_pair a, seq_pair b) {
+    seq_pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.u) : "l"(a.u), "l"(b.u));
+    return r;
+}
+__device__ __forceinline__ seq_pair seq_fma2(seq_pair a, seq_pair b, seq_pair c) {
+    seq_pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.u) : "l"(a.u), "l"(b.u), "l"(c.u));
+    return r;
+}
+
 // ---- asynchronous copies into a thread's own places of shared memory (4, 8 or 16 bytes) ----
 template <int BYTES>
 __device__ __forceinline__ void copy_async(uint32_t dst, const void *src) {
