@@ -36,49 +36,61 @@ __device__ __forceinline__ int cell_at(int r, int c, int ld) { return quad_at(r,
 
 template <int LD>  // values of a row of a, b and x: 64, 128 or 256
 struct ChunkTiles {
-    float *a, *b, *c, *p, *x, *kept, *power;
+    static constexpr bool apart = LD < 256;  // the weighted b has a place of its own, and the next chunk comes while the state is formed
+    float *a, *b, *bt, *c, *p, *x, *kept, *power;
     __device__ explicit ChunkTiles(float *m) {
-        a = m;                      // [64][LD]; the weighted b turned over, [LD][64], once a is read
-        b = a + kChunk * LD;        // [64][LD]
-        c = b + kChunk * LD;        // turned over: [64 values][64 tokens]
-        p = c + kSlice * kChunk;    // [64][64]: c as it comes, then the products
-        x = p + kChunk * kChunk;    // [64 values of c][LD]
+        a = m;                                // [64][LD]
+        b = a + kChunk * LD;                  // [64][LD]
+        c = b + kChunk * LD;                  // turned over: [64 values][64 tokens]
+        p = c + kSlice * kChunk;              // [64][64]: c as it comes, then the products
+        x = p + kChunk * kChunk;              // [64 values of c][LD]
         kept = x + kSlice * LD;
-        power = kept + kChunk;      // lambda^0 .. lambda^64
+        power = kept + kChunk;                // lambda^0 .. lambda^64
+        bt = apart ? power + kChunk + 4 : a;  // the weighted b turned over, [LD][64]; or, once a is read, in its place
     }
-    static constexpr size_t bytes = sizeof(float) * (2 * kChunk * LD + kSlice * kChunk + kChunk * kChunk + kSlice * LD + kChunk + kChunk + 4);
+    static constexpr size_t bytes =
+        sizeof(float) * (2 * kChunk * LD + kSlice * kChunk + kChunk * kChunk + kSlice * LD + kChunk + kChunk + 4 + (apart ? kChunk * LD : 0));
 };
 
-// Rows [0, rows) of a chunk, D values from column col0, zeros around; true if a value is not finite.
+// Rows [0, rows) of a chunk, D values from column col0, zeros around: on their way in fp32 (copy_commit, copy_wait), there in bf16.
 template <class T, int ld>
-__device__ __forceinline__ bool load_rows(float *dst, const decay_array &g, long long base, const decay_seq &q, long long s0, int rows,
-                                          int col0, int D, int vec) {
-    float odd = 0.f;
-    const int step = q.reverse ? -1 : 1;
+__device__ __forceinline__ void load_rows(float *dst, const decay_array &g, long long base, const decay_seq &q, long long s0, int rows, int col0, int D,
+                                          int vec) {
     const T *const first = static_cast<const T *>(g.p) + base + q.at(s0) * g.t + col0;
+    const long long next = q.reverse ? -g.t : g.t;
+    constexpr bool fp32 = sizeof(T) == 4;
     if (vec > 1) {  // 16 bytes
-        constexpr int V = 16 / sizeof(T);
-        constexpr int per = ld / V;
-        for (int i = threadIdx.x; i < kChunk * per; i += kThreads) {
-            const int r = i / per, d = (i - r * per) * V;
-            float f[V] = {};
-            if (r < rows && d < D) seq_unpack<T, V>(seq_load<T, V>(first + (long long)(step * r) * g.t + d), f);
+        constexpr int V = 16 / sizeof(T), per = ld / V, turns = kChunk * per / kThreads, at_once = kThreads / per;
+        const int d = threadIdx.x % per * V, r0 = threadIdx.x / per;
+#pragma unroll 4
+        for (int i = 0; i < turns; ++i) {
+            const int r = r0 + i * at_once;
+            const bool on = r < rows && d < D;
+            const T *const at = first + (on ? r * next + d : 0);
+            if constexpr (fp32) {
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst + quad_at(r, d / 4, ld))), "l"(at),
+                             "r"(on ? 16 : 0) : "memory");
+            } else {
+                float f[V] = {};
+                if (on) seq_unpack<T, V>(seq_load<T, V>(at), f);
 #pragma unroll
-            for (int k = 0; k < V; k += 4) {
-                odd += f[k] * 0.f + f[k + 1] * 0.f + f[k + 2] * 0.f + f[k + 3] * 0.f;
-                *reinterpret_cast<float4 *>(dst + quad_at(r, (d + k) / 4, ld)) = make_float4(f[k], f[k + 1], f[k + 2], f[k + 3]);
+                for (int k = 0; k < V; k += 4) *reinterpret_cast<float4 *>(dst + quad_at(r, (d + k) / 4, ld)) = make_float4(f[k], f[k + 1], f[k + 2], f[k + 3]);
             }
         }
     } else {
-        for (int r = threadIdx.x >> 5; r < kChunk; r += kThreads / 32)
+        for (int r = threadIdx.x >> 5; r < kChunk; r += kThreads / 32) {
+#pragma unroll
             for (int d = threadIdx.x & 31; d < ld; d += 32) {
-                float f = 0.f;
-                if (r < rows && d < D) f = seq_to_float(first[(long long)(step * r) * g.t + d]);
-                odd += f * 0.f;
-                dst[cell_at(r, d, ld)] = f;
+                const bool on = r < rows && d < D;
+                const T *const at = first + (on ? r * next + d : 0);
+                if constexpr (fp32)
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst + cell_at(r, d, ld))), "l"(at),
+                                 "r"(on ? 4 : 0) : "memory");
+                else
+                    dst[cell_at(r, d, ld)] = on ? seq_to_float(*at) : 0.f;
             }
+        }
     }
-    return !(odd == 0.f);
 }
 
 // acc[i][k] += sums over `quads` quads of rows r0 + i of u and rows c0 + 16 k of v, for k < B.  (r0 a multiple of 4.  The quads of
@@ -160,34 +172,50 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
             if (j.first && q.len > 0) mul = decay_power(g, 1);
         }
     }
-    for (int i = tid; i < LD * kSlice; i += kThreads) {
-        const int r = i / kSlice, c = i % kSlice;  // (value of a, of c)
-        float v = 0.f;
-        if (from && r < da && c < cols) v = (from_t ? from[(long long)(col0 + c) * da + r] : from[(long long)r * j.dc + col0 + c]);
-        m.x[cell_at(c, r, LD)] = mul == 1.f ? v : v * mul;
+    if (!from) {
+        for (int i = tid; i < LD * kSlice / 4; i += kThreads) reinterpret_cast<float4 *>(m.x)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    } else {
+#pragma unroll 8
+        for (int i = tid; i < LD * kSlice; i += kThreads) {
+            // (value of a, of c: lanes along what lies side by side)
+            const int r = from_t ? i % LD : i / kSlice, c = from_t ? i / LD : i % kSlice;
+            float v = 0.f;
+            if (r < da && c < cols) v = (from_t ? from[(long long)(col0 + c) * da + r] : from[(long long)r * j.dc + col0 + c]);
+            m.x[cell_at(c, r, LD)] = mul == 1.f ? v : v * mul;
+        }
     }
     if (tid <= kChunk) m.power[tid] = decay_power(g, tid);
     float carry = 1.f;
 
     const long long an = n * j.a.n + head * j.a.h, bn = n * j.b.n + head * j.b.h, cn = n * j.c.n + head * j.c.h;
+    const auto rows_of = [&](long long s0) { return (int)max(0ll, min((long long)kChunk, min(last, q.len) - s0)); };
+    const auto load = [&](long long s0) {
+        const int rows = rows_of(s0);
+        if (rows > 0) {
+            load_rows<T, LD>(m.b, j.b, bn, q, s0, rows, 0, da, j.vec);
+            load_rows<T, kSlice>(m.p, j.c, cn, q, s0, rows, col0, cols, j.vec);
+            if constexpr (!STATE) load_rows<T, LD>(m.a, j.a, an, q, s0, rows, 0, da, j.vec);
+        }
+        copy_commit();
+    };
+    load(first);
+    const float w_scale = j.w_scale, in_scale = j.in_scale, up_scale = j.up_scale;
+    T *const y0 = static_cast<T *>(const_cast<void *>(j.y.p)) + n * j.y.n + head * j.y.h + col0;
     for (long long s0 = first; s0 < last; s0 += kChunk) {
-        const int rows = (int)max(0ll, min((long long)kChunk, min(last, q.len) - s0));
+        const int rows = rows_of(s0);
         if (rows == 0) {
             if constexpr (STATE) break;
-            T *y = static_cast<T *>(const_cast<void *>(j.y.p)) + n * j.y.n + head * j.y.h + col0;
             const int pad = (int)min((long long)kChunk, last - s0);
-            for (int i = tid; i < pad * cols; i += kThreads) y[(s0 + i / cols) * j.y.t + i % cols] = seq_from_float<T>(0.f);
+            for (int r = tid >> 5; r < pad; r += kThreads / 32)
+                for (int c = tid & 31; c < cols; c += 32) y0[(s0 + r) * j.y.t + c] = seq_from_float<T>(0.f);
             continue;
         }
-        __syncthreads();
-        bool odd = load_rows<T, LD>(m.b, j.b, bn, q, s0, rows, 0, da, j.vec);
-        odd |= load_rows<T, kSlice>(m.p, j.c, cn, q, s0, rows, col0, cols, j.vec);
-        if constexpr (!STATE) load_rows<T, LD>(m.a, j.a, an, q, s0, rows, 0, da, j.vec);
         if (tid < 64) {
             const unsigned c = __ballot_sync(~0u, decay_cut(p, q, s0 + tid, n) && tid < rows);
             if ((tid & 31) == 0) cuts[tid >> 5] = c;
         }
-        const bool careful = __syncthreads_or(odd);  // (zero weights would make NaN of what is not finite)
+        copy_wait<0>();
+        __syncthreads();  // 1: the tiles are there
         const unsigned long long cut = cuts[0] | (unsigned long long)cuts[1] << 32;
         // the first token that token i sees; with none of the chunk cut before, the state too
         auto start = [&](int i) {
@@ -197,23 +225,25 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
         const int keep_from = start(rows - 1);
         // (time's order, the last chunk of all: the state leaves as the last token wrote it)
         const int less = j.first && s0 + rows == q.len && !STATE ? 1 : 0;
-        if (tid < kChunk) m.kept[tid] = tid < rows && tid >= keep_from ? j.up_scale * m.power[rows - tid - less] : 0.f;
-        // rows [64][ld] -> [ld][64], each row times its weight (0: nothing of it); a thread takes whole quads of a row
-        const auto turn = [&](float *to, const float *rowsm, int ld, int quads, const float *w) {
-            for (int i = tid; i < kChunk * quads; i += kThreads) {
-                const int r = i % kChunk, d = i / kChunk;
+        if (tid < kChunk) m.kept[tid] = tid < rows && tid >= keep_from ? up_scale * m.power[rows - tid - less] : 0.f;
+        // rows [64][ld] -> [ld][64], each row times its weight (0: nothing of it); true if a value is not finite
+        const auto turn = [&](float *to, const float *rowsm, int ld, const float *w) {
+            float odd = 0.f;
+            const int r = tid % kChunk;
+            const float f = w ? w[r] : 1.f;
+#pragma unroll 4
+            for (int d = tid / kChunk; d < ld / 4; d += kThreads / kChunk) {
                 float4 v = ld4(rowsm + quad_at(r, d, ld));
-                if (w) {
-                    const float f = w[r];
-                    v = f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
-                }
+                odd += v.x * 0.f + v.y * 0.f + v.z * 0.f + v.w * 0.f;
+                if (w) v = f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
                 to[cell_at(4 * d, r, kChunk)] = v.x;
                 to[cell_at(4 * d + 1, r, kChunk)] = v.y;
                 to[cell_at(4 * d + 2, r, kChunk)] = v.z;
                 to[cell_at(4 * d + 3, r, kChunk)] = v.w;
             }
+            return !(odd == 0.f);
         };
-        turn(m.c, m.p, kSlice, kSlice / 4, nullptr);
+        bool careful = turn(m.c, m.p, kSlice, nullptr);  // (zero weights would make NaN of what is not finite)
 
         if constexpr (!STATE) {
             int begin[4];
@@ -222,7 +252,8 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
             // p = a b^T, weighted; columns beyond the rows' own are not seen
             seq_pair acc[4][4] = {};
             products<LD, LD>(acc, m.a, ty * 4, m.b, tx, dq, ty / 4 + 1);
-            __syncthreads();  // (c is turned over: p's place is free)
+            careful = __syncthreads_or(careful);  // 2: c is turned over, and p's place free
+            if constexpr (m.apart) careful |= turn(m.bt, m.b, LD, m.kept);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = ty * 4 + i;
@@ -230,10 +261,10 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
                 for (int k = 0; k < 4; ++k) {
                     const int c = tx + 16 * k;
                     const bool seen = c <= r && c >= begin[i] && r < rows;
-                    m.p[cell_at(r, c, kChunk)] = seen ? (acc[i][k].f.x + acc[i][k].f.y) * (j.w_scale * m.power[r - c]) : 0.f;
+                    m.p[cell_at(r, c, kChunk)] = seen ? (acc[i][k].f.x + acc[i][k].f.y) * (w_scale * m.power[r - c]) : 0.f;
                 }
             }
-            __syncthreads();
+            careful = __syncthreads_or(careful);  // 3
             // y = lambda^r X^T a + p c
             float y[4][4];
             {
@@ -241,7 +272,7 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
                 products<LD, LD>(in, m.a, ty * 4, m.x, tx, dq, cblocks);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float w = j.in_scale * m.power[ty * 4 + i];
+                    const float w = in_scale * m.power[ty * 4 + i];
 #pragma unroll
                     for (int h = 0; h < 4; ++h) y[i][h] = begin[i] < 0 ? w * (in[i][h].f.x + in[i][h].f.y) : 0.f;
                 }
@@ -266,16 +297,20 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
             for (int i = 0; i < 4; ++i) {
                 const int r = ty * 4 + i;
                 if (s0 + r >= last) continue;
-                T *out = static_cast<T *>(const_cast<void *>(j.y.p)) + n * j.y.n + head * j.y.h + q.at(s0 + r) * j.y.t + col0 + tx;
+                T *const out = y0 + q.at(s0 + r) * j.y.t + tx;
 #pragma unroll
                 for (int h = 0; h < 4; ++h)
                     if (tx + 16 * h < cols) out[16 * h] = seq_from_float<T>(r >= rows ? 0.f : y[i][h]);
             }
         }
-        __syncthreads();
-        float *const bt = m.a;
-        turn(bt, m.b, LD, LD / 4, m.kept);
-        __syncthreads();
+        if constexpr (STATE || !m.apart) {
+            __syncthreads();  // (kept is there, a and p are read)
+            const bool odd = turn(m.bt, m.b, LD, m.kept) || careful;
+            careful = __syncthreads_or(odd);
+        } else {
+            __syncthreads();  // 4: the state is read
+        }
+        if constexpr (m.apart) load(s0 + kChunk);
         // X = lambda^n X + (kept b)^T c
         const float shrink = m.power[rows - less];
         if (ty * 4 < cols)
@@ -283,12 +318,12 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
                 seq_pair acc[4][4] = {};
                 const int blocks = min(4, (da - r0 + 15) / 16);
                 if (!careful) {
-                    products<kChunk, kChunk>(acc, m.c, ty * 4, bt + r0 * kChunk, tx, (rows + 3) / 4, blocks);
+                    products<kChunk, kChunk>(acc, m.c, ty * 4, m.bt + r0 * kChunk, tx, (rows + 3) / 4, blocks);
                 } else {
                     for (int k = max(keep_from, 0); k < rows; ++k) {
                         float v[4];
 #pragma unroll
-                        for (int h = 0; h < 4; ++h) v[h] = h < blocks ? bt[cell_at(r0 + tx + 16 * h, k, kChunk)] : 0.f;
+                        for (int h = 0; h < 4; ++h) v[h] = h < blocks ? m.bt[cell_at(r0 + tx + 16 * h, k, kChunk)] : 0.f;
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const float u = m.c[cell_at(ty * 4 + i, k, kChunk)];
@@ -309,7 +344,12 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
                     }
             }
         carry = keep_from < 0 ? carry * shrink : 0.f;
+        if constexpr (!m.apart) {
+            __syncthreads();
+            load(s0 + kChunk);
+        }
     }
+    copy_wait<0>();
     __syncthreads();
     // what leaves: the span's part, or the state itself (of the span that holds the sequence's end)
     float *to = nullptr;
@@ -323,9 +363,10 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
         empty = j.out_zero && q.len > 0 && p.reset && p.reset[n] != 0;
     }
     if (to)
-        for (int i = tid; i < da * kSlice; i += kThreads) {
+#pragma unroll 8
+        for (int i = tid; i < LD * kSlice; i += kThreads) {
             const int r = i / kSlice, c = i % kSlice;
-            if (c < cols) to[(long long)r * j.dc + col0 + c] = empty ? 0.f : m.x[cell_at(c, r, LD)];
+            if (r < da && c < cols) to[(long long)r * j.dc + col0 + c] = empty ? 0.f : m.x[cell_at(c, r, LD)];
         }
 }
 
