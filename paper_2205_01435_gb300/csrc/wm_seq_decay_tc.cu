@@ -6,7 +6,7 @@
 //   P = A * weights               TMEM -> registers -> TMEM as bf16, where the next product reads it
 //   O2 = a Xb                     Xb: the state X, fp32 in TMEM, as a bf16 tile
 //   O1 = P c,  y = O1 + in_scale lambda^r O2
-//   X = lambda^n X + (b w)^T c    in place in TMEM; b w as two bf16 values, so that X is as good as 2^-17 of its terms
+//   X = lambda^n X + (b w)^T c    in place in TMEM; b w as three bf16 values, all 24 bits of it: the state is as good as in fp32
 // a, b and c lie as [128 tokens][64 values] panels of 128-byte rows in the 128-byte swizzle, which serve as K-major operands
 // (a, b in A and O2) and as MN-major ones (c, and b transposed, where the tokens are summed over).  Rows come by asynchronous
 // 16-byte copies that a padded token or value leaves as zeros: lengths, strides and either direction of time cost nothing extra.
@@ -58,10 +58,11 @@ template <int D>
 struct Plan {
     static constexpr int workers = 4 * D, threads = workers + 32;  // 32 columns of the state and of the outputs a thread
     static constexpr int tile = kPanel * (D / 64);
-    // (lo lies behind b: with D = 64 both are one operand of 128 rows; lo and xb also hold the state on its way in and out)
-    static constexpr int b = 0, lo = b + 2 * tile, xb = lo + tile, a = xb + D * 128 * (D / 64), c = a + 2 * tile, end = c + tile;
+    // (lo lies behind b: with D = 64 both are one operand of 128 rows; lo and xb, whose place the outputs take on their way out,
+    // also hold the state on its way in and out)
+    static constexpr int b = 0, lo = b + 2 * tile, xb = lo + tile, a = xb + tile, c = a + 2 * tile, end = c + tile;
     static constexpr int small = end;  // tables and barriers
-    static constexpr int bytes = small + 4 * 132 + 8 * 128 + 48 + 48 + 1024;
+    static constexpr int bytes = small + 4 * 132 + 48 + 48;
     // P lies over A: 16 tokens' column pairs where their warps read them, in blocks of `own` columns of A; with D = 64 O2, in two
     // halves, over the rest of each block
     static constexpr int own = 128 / (D / 32);
@@ -228,7 +229,7 @@ __device__ __forceinline__ bool state_out(const float4 *x, float *to, int da, in
 }
 // What the workers hand to the issuing warp: they arrive and go on, it waits.  (No worker arrives twice before it has waited:
 // in between each waits for a product that was issued after.)
-enum { kRead = 6, kScaled = 7, kReady = 8 };
+enum { kRead = 6, kScaled = 7, kWeighted = 8, kReady = 9 };
 template <int D>
 __device__ __forceinline__ void hand_over(int id) {
     asm volatile("bar.arrive %0, %1;" ::"r"(id), "n"(Plan<D>::threads) : "memory");
@@ -247,13 +248,11 @@ template <int D, bool STATE, bool TMA, bool CUT>
 __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_kernel(const decay_pass p, const __grid_constant__ decay_maps maps) {
     using L = Plan<D>;
     constexpr bool early = TMA && !STATE && D == 128;  // A of the next chunk is formed as soon as P is read (O2 has a place of its own)
-    extern __shared__ unsigned char raw[];
-    unsigned char *smem = raw + ((1024u - (tc::smem_u32(raw) & 1023u)) & 1023u);
+    extern __shared__ __align__(1024) unsigned char smem[];
     const uint32_t base = tc::smem_u32(smem);
     float *const power = reinterpret_cast<float *>(smem + L::small);         // lambda^0 .. lambda^128
     float *const scales = power + 129;                                       // of products, of the entering state, of its update
-    uint2 *const kept = reinterpret_cast<uint2 *>(power + 132);              // the tokens' weights in the next state: two bf16, each twice
-    uint32_t *const cuts = reinterpret_cast<uint32_t *>(kept + 128);        // [2][4]: tokens that begin something new
+    uint32_t *const cuts = reinterpret_cast<uint32_t *>(power + 132);       // [2][4]: tokens that begin something new
     volatile int *const late = reinterpret_cast<int *>(cuts + 8);           // a wait gave up
     uint32_t *const tmem_at = cuts + 9;
     const uint32_t bars = tc::smem_u32(cuts + 12), barA = bars, barO = bars + 8, barX = bars + 16, barV = bars + 24, barQK = bars + 32;
@@ -404,25 +403,33 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             }
             __syncwarp();
             if constexpr (TMA) wait(barV, done);
-            take_over<D>(kReady);  // P and the keys' parts are there
-            tc::fence_after_sync();
-            bool keeps_x = true;
-            if constexpr (CUT) keeps_x = (cuts[slot * 4] | cuts[slot * 4 + 1] | cuts[slot * 4 + 2] | cuts[slot * 4 + 3]) == 0;
-            const bool onto = (STATE ? !fresh : has_x) && keeps_x;
-            if (tc::elect_one()) {
-                if constexpr (!STATE) {
+            if constexpr (!STATE) {
+                take_over<D>(kWeighted);  // P is there
+                tc::fence_after_sync();
+                if (tc::elect_one()) {
 #pragma unroll
                     for (int k = 0; k < kChunk / 16; ++k)
                         mma_bf16_ts(tmem + L::tO1, tmem + L::p_at(k), desc_mn(tv + k * 2048, kPanel), tc::idesc_bf16_f32(128, D) | kBmn, k > 0);
                     tc::mma_commit(barO);
                 }
-                // (D = 64: both parts as one operand of 128 rows)
+                __syncwarp();
+            }
+            take_over<D>(kReady);  // the keys' parts are there
+            tc::fence_after_sync();
+            bool keeps_x = true;
+            if constexpr (CUT) keeps_x = (cuts[slot * 4] | cuts[slot * 4 + 1] | cuts[slot * 4 + 2] | cuts[slot * 4 + 3]) == 0;
+            const bool onto = (STATE ? !fresh : has_x) && keeps_x;
+            if (tc::elect_one()) {
+                // (D = 64: two operands of 128 rows, the first two parts and half of the third twice)
+                constexpr int parts = D == 64 ? 2 : 3;
 #pragma unroll
-                for (int part = 0; part < D / 64; ++part)
+                for (int part = 0; part < parts; ++part) {
+                    const uint32_t at = part == 0 ? tb : part == parts - 1 ? ta : base + L::lo, panel = D == 128 ? kPanel : part == 0 ? base + L::lo - tb : 0;
 #pragma unroll
                     for (int k = 0; k < kChunk / 16; ++k)
-                        tc::mma_bf16(tmem + L::tX, desc_mn((part ? base + L::lo : tb) + k * 2048, D == 64 ? base + L::lo - tb : kPanel),
-                                     desc_mn(tv + k * 2048, kPanel), tc::idesc_bf16_f32(128, D) | kAmn | kBmn, part > 0 || k > 0 || onto);
+                        tc::mma_bf16(tmem + L::tX, desc_mn(at + k * 2048, panel), desc_mn(tv + k * 2048, kPanel),
+                                     tc::idesc_bf16_f32(128, D) | kAmn | kBmn, part > 0 || k > 0 || onto);
+                }
                 tc::mma_commit(barX);
             }
             __syncwarp();
@@ -535,10 +542,10 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 const uint32_t ta = base + L::a + slot * L::tile, tb = base + L::b + slot * L::tile, tv = base + L::c;
                 const bool has_x = enters || c > 0;
                 if constexpr (!TMA) copy_wait<1>();
-                if constexpr (!STATE) tma_store_read();  // (the outputs' copies have read a's tile, which is filled again)
+                if constexpr (!STATE) tma_store_read();
                 tc::fence_proxy_async_smem();
                 tc::fence_before_sync();
-                if (CUT || !TMA) worker_barrier<D>();  // the chunk's cuts, or its tiles, are there
+                worker_barrier<D>();  // the outputs' place is free (CUT: and the chunk's cuts there)
                 hand_over<D>(kRead);
                 if (!TMA && c > 0) load_ab(c + 1);
                 // tokens that begin something new: what a token sees begins with the last of them up to it (counted in steps)
@@ -562,20 +569,6 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 // (time's order, the last token of all: the state leaves as that token wrote it)
                 const int less = !STATE && j.first && s0 + rows == len ? 1 : 0;
                 if (STATE && TMA) wait(barQK + 8 * slot, phase >> 1);
-                const bool weigh_again = CUT || STATE || c == 0 || rows < kChunk || less;
-                if (weigh_again && c > 0) worker_barrier<D>();  // (the chunk before has its weights)
-                if (weigh_again && tid < kChunk) {
-                    float w = 0.f;
-                    const int s = step_of(tid);
-                    if (s < rows && s >= keep_from) {
-                        if constexpr (STATE) w = decay_power(g, stop - s0 - s);  // up to the span's end
-                        else w = power[rows - s - less];
-                    }
-                    w *= scales[2];
-                    const float w1 = __bfloat162float(__float2bfloat16_rn(w));
-                    kept[tid] = make_uint2(pack2(w1, w1), pack2(w - w1, w - w1));
-                }
-                if (weigh_again) worker_barrier<D>();
                 constexpr int cols = 128 / (D / 32);  // of A, a thread
                 uint32_t packed[cols / 2];
                 if constexpr (!STATE) {
@@ -709,34 +702,6 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                     if constexpr (cols == 64) TC_ST32(mine + L::tA + group * 64, packed);
                     else TC_ST16(mine + L::tA + group * 32, packed);
                 }
-                // b -> b w as two bf16 values, the first in b's place: with w = w1 + w2, hi = b w1 rounded, lo = (b w1 - hi) + b w2,
-                // where b w1 - hi is exact (16 bits of a product, the first 8 taken away)
-                {
-                    constexpr int per = D / 8, stride = L::workers / per;
-                    const int ch = tid % per, row0 = tid / per;
-                    const uint32_t off = (ch / 8) * kPanel + row0 * 128 + (((ch & 7) ^ (row0 & 7)) << 4);
-                    constexpr int turns = kChunk / stride;
-                    uint32_t v[turns][4];
-                    uint2 w[turns];
-#pragma unroll
-                    for (int k = 0; k < turns; ++k) {
-                        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[k][0]), "=r"(v[k][1]), "=r"(v[k][2]), "=r"(v[k][3]) : "r"(tb + off + k * stride * 128) : "memory");
-                        w[k] = kept[row0 + k * stride];
-                    }
-#pragma unroll
-                    for (int k = 0; k < turns; ++k) {
-                        const uint32_t to = off + k * stride * 128;
-                        uint32_t hi[4], lo[4];
-                        if (TMA && rows < kChunk && step_of(row0 + k * stride) >= rows) v[k][0] = v[k][1] = v[k][2] = v[k][3] = 0u;  // (whatever lies there)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            hi[i] = hmul(v[k][i], w[k].x);
-                            lo[i] = hfma(v[k][i], w[k].y, hfma(v[k][i], w[k].x, hi[i] ^ 0x80008000u));
-                        }
-                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(tb + to), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
-                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(base + L::lo + to), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
-                    }
-                }
                 if constexpr (TMA) {
                     if (rows < kChunk) {  // values of steps that are not there: whatever lies there times 0 is to be 0
                         wait(barV, phase);
@@ -749,18 +714,59 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 } else {
                     copy_wait<1>();
                 }
-                if constexpr (!STATE) tmem_st_wait();
+                if constexpr (!STATE) {
+                    tmem_st_wait();
+                    if (!TMA || rows < kChunk) tc::fence_proxy_async_smem();
+                    tc::fence_before_sync();
+                    hand_over<D>(kWeighted);
+                }
+                // b -> b w as three bf16 values, what each leaves rounded to the next: in b's place, in lo, and (once the products with a
+                // are done) in a's place
+                {
+                    constexpr int per = D / 8, stride = L::workers / per, turns = kChunk / stride;
+                    const int ch = tid % per, row0 = tid / per;
+                    const uint32_t off = (ch / 8) * kPanel + row0 * 128 + (((ch & 7) ^ (row0 & 7)) << 4);
+                    uint32_t v[turns][4];
+#pragma unroll
+                    for (int k = 0; k < turns; ++k)
+                        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[k][0]), "=r"(v[k][1]), "=r"(v[k][2]), "=r"(v[k][3]) : "r"(tb + off + k * stride * 128) : "memory");
+#pragma unroll
+                    for (int k = 0; k < turns; ++k) {
+                        const uint32_t to = off + k * stride * 128;
+                        const int s = step_of(row0 + k * stride);  // its weight in the next state (STATE: in the span's)
+                        const bool counts = s < rows && s >= keep_from;
+                        const float f = !counts ? 0.f : scales[2] * (STATE ? decay_power(g, stop - s0 - s) : power[rows - s - less]);
+                        const Pair w = twice(f), minus = twice(-1.f);
+                        uint32_t hi[4], lo[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if (TMA && !counts) v[k][i] = 0u;  // (whatever lies there)
+                            Pair x = mul2(pair_of(v[k][i] << 16, v[k][i] & 0xffff0000u), w);
+                            hi[i] = pack2(x.f.x, x.f.y);
+                            x = fma2(pair_of(hi[i] << 16, hi[i] & 0xffff0000u), minus, x);
+                            lo[i] = pack2(x.f.x, x.f.y);
+                            x = fma2(pair_of(lo[i] << 16, lo[i] & 0xffff0000u), minus, x);
+                            v[k][i] = pack2(x.f.x, x.f.y);
+                            if constexpr (D == 64) v[k][i] = hmul(v[k][i], 0x3f003f00u);  // (it is added twice)
+                        }
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(tb + to), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(base + L::lo + to), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
+                    }
+                    if constexpr (!STATE) wait(barO, phase);
+#pragma unroll
+                    for (int k = 0; k < turns; ++k)
+                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(ta + off + k * stride * 128), "r"(v[k][0]), "r"(v[k][1]), "r"(v[k][2]), "r"(v[k][3]) : "memory");
+                }
                 tc::fence_proxy_async_smem();
                 tc::fence_before_sync();
                 if (!TMA) worker_barrier<D>();  // (their tiles' copies, by all of them)
                 hand_over<D>(kReady);
                 find_cuts(c + 1);
                 if constexpr (!STATE) {
-                    // y = O1 + in_scale lambda^step O2, by way of a's tile (32 rows of 64 bytes a warp, 64-byte swizzle) to whole rows
+                    // y = O1 + in_scale lambda^step O2, by way of Xb's place (32 rows of 64 bytes a warp, 64-byte swizzle) to whole rows
                     const bool sees = !CUT || begin < 0;
-                    const uint32_t stage = ta + warp * 2048, own = stage + lane * 64, turn = (lane >> 1) & 3;
+                    const uint32_t stage = base + L::xb + warp * 2048, own = stage + lane * 64, turn = (lane >> 1) & 3;
                     const Pair w = twice(scales[1] * power[step]);
-                    wait(barO, phase);
                     uint32_t o1[32];
                     TC_LD32(mine + L::tO1 + col0, o1);
                     if (has_x) {
@@ -819,6 +825,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             bad = (odd & 0x7fff7fffu) != 0;  // (a product with 0 is 0 or NaN)
             if constexpr (!STATE) tma_store_read();
             if constexpr (!TMA) copy_wait<0>();
+            if constexpr (!STATE) worker_barrier<D>();  // (the outputs' place is free: the state leaves by it)
             // the next item's marks, and its state on the way to L2, while this one's state leaves
             const Item next = open(m.at + (int)gridDim.x);
             float g_next = 0.f;

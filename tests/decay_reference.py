@@ -46,8 +46,7 @@ def _walk(a, b, c, g, keep, live, state, order, factors):
         if factors:  # (or the rounded state)
             bound = bound + 1.01 * B * (prod[i] + (R * at.abs()).sum(-2))
         yb[t] = torch.where(on[..., 0], bound, 0.0)
-    # (bf16 keys times their weight are taken as two bf16 values: 2^-17)
-    return y, yb, F, (n * U + (2.0 ** -17 if factors else 0.0)) * M
+    return y, yb, F, n * U * M
 
 
 def _marks(T, N, H, g, reset, lengths):
