@@ -561,7 +561,7 @@ decay_pass pass_of(const wm_seq *h, const seq_decay_args &a, bool backward) {
     if (!backward) {
         p.jobs = 1;
         decay_job &f = p.job[0] = job(0, 1, 2, o, a.Dk, a.Dv);
-        f.first = 1;
+        f.first = f.fine = 1;
         f.s_in = a.s0;
         f.s_out = a.s_last;
         return p;
@@ -572,7 +572,7 @@ decay_pass pass_of(const wm_seq *h, const seq_decay_args &a, bool backward) {
     dq.s_in = a.s0;
     dq.in_t = 1;
     decay_job &dv = p.job[1] = job(1, 0, 3, array_of(a.dv), a.Dk, a.Dv);
-    dv.reverse = 1;
+    dv.reverse = dv.fine = 1;
     dv.in_scale = 1.f;
     dv.up_scale = a.scale;
     dv.s_in = a.ds_last;

@@ -20,6 +20,7 @@ struct decay_job {
     int da, dc;              // values of a and b; of c and y
     int reverse;             // the tokens from the last to the first
     int first;               // the entering state has not decayed yet (time's order): X = lambda s_in; and it leaves so too
+    int fine;                // the state is one that a call gives out: as good as in fp32 (whether it is asked for or not: outputs do not depend on that)
     int in_t, out_zero;      // s_in is [dc, da]; a reset of the token that comes last here empties s_out
     float w_scale, in_scale, up_scale;
     const float *s_in;       // [N, H, da, dc], or NULL = 0

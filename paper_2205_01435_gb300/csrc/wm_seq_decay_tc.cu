@@ -6,7 +6,8 @@
 //   P = A * weights               TMEM -> registers -> TMEM as bf16, where the next product reads it
 //   O2 = a Xb                     Xb: the state X, fp32 in TMEM, as a bf16 tile
 //   O1 = P c,  y = O1 + in_scale lambda^r O2
-//   X = lambda^n X + (b w)^T c    in place in TMEM; b w as three bf16 values, all 24 bits of it: the state is as good as in fp32
+//   X = lambda^n X + (b w)^T c    in place in TMEM; b w as three bf16 values, all 24 bits of it, where the state leaves: it is as
+//                                 good as in fp32; as two where only Xb is read from it
 // a, b and c lie as [128 tokens][64 values] panels of 128-byte rows in the 128-byte swizzle, which serve as K-major operands
 // (a, b in A and O2) and as MN-major ones (c, and b transposed, where the tokens are summed over).  Rows come by asynchronous
 // 16-byte copies that a padded token or value leaves as zeros: lengths, strides and either direction of time cost nothing extra.
@@ -58,8 +59,8 @@ template <int D>
 struct Plan {
     static constexpr int workers = 4 * D, threads = workers + 32;  // 32 columns of the state and of the outputs a thread
     static constexpr int tile = kPanel * (D / 64);
-    // (lo lies behind b: with D = 64 both are one operand of 128 rows; lo and xb, whose place the outputs take on their way out,
-    // also hold the state on its way in and out)
+    // (lo lies behind b: with D = 64 both are one operand of 128 rows; xb's place is a tile, for the third part;
+    // both also hold the state on its way in and out)
     static constexpr int b = 0, lo = b + 2 * tile, xb = lo + tile, a = xb + tile, c = a + 2 * tile, end = c + tile;
     static constexpr int small = end;  // tables and barriers
     static constexpr int bytes = small + 4 * 132 + 48 + 48;
@@ -321,14 +322,14 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
         // ---- one thread issues the products, and the copies: keys and queries a chunk ahead, of the next item too
         struct Cursor {  // a chunk: of item `at`, the c-th of its `chunks`, from token t0
             int at, c, chunks, t0, dt, n, head, maps;
-            bool enters;
+            bool enters, fine;
         };
         const auto find = [&](Cursor &k, int at) {  // the first chunk of item `at`, or of the next one that has any
             for (;; at += gridDim.x) {
                 const Item m = open(at);
                 const decay_job &j = p.job[m.job];
                 k = {at, 0, m.chunks, begin_of(m, 0), m.rev ? -kChunk : kChunk, m.n, m.head, j.map[0] | j.map[1] << 2 | j.map[2] << 4,
-                     !STATE && (p.spans > 1 || j.s_in)};
+                     !STATE && (p.spans > 1 || j.s_in), j.fine != 0};
                 if (m.chunks > 0 || at >= items) return;
             }
         };
@@ -377,7 +378,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
         };
 #pragma unroll 1
         for (int done = 0; now.at < items; ++done) {  // chunks
-            const bool has_x = now.enters || now.c > 0, fresh = STATE && now.c == 0;
+            const bool has_x = now.enters || now.c > 0, fresh = STATE && now.c == 0, fine = now.fine;
             const int slot = done & 1;
             const uint32_t ta = base + L::a + slot * L::tile, tb = base + L::b + slot * L::tile, tv = base + L::c;
             if (TMA && !(early && done > 0)) wait(barQK + 8 * slot, done >> 1);
@@ -421,15 +422,15 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             const bool onto = (STATE ? !fresh : has_x) && keeps_x;
             if (tc::elect_one()) {
                 // (D = 64: two operands of 128 rows, the first two parts and half of the third twice)
-                constexpr int parts = D == 64 ? 2 : 3;
-#pragma unroll
-                for (int part = 0; part < parts; ++part) {
-                    const uint32_t at = part == 0 ? tb : part == parts - 1 ? ta : base + L::lo, panel = D == 128 ? kPanel : part == 0 ? base + L::lo - tb : 0;
+                const auto update = [&](uint32_t at, uint32_t panel, bool more) {
 #pragma unroll
                     for (int k = 0; k < kChunk / 16; ++k)
                         tc::mma_bf16(tmem + L::tX, desc_mn(at + k * 2048, panel), desc_mn(tv + k * 2048, kPanel),
-                                     tc::idesc_bf16_f32(128, D) | kAmn | kBmn, part > 0 || k > 0 || onto);
-                }
+                                     tc::idesc_bf16_f32(128, D) | kAmn | kBmn, more || k > 0);
+                };
+                update(tb, D == 128 ? kPanel : base + L::lo - tb, onto);
+                if (D == 128) update(base + L::lo, kPanel, true);
+                if (fine) update(base + L::xb, D == 128 ? kPanel : 0, true);
                 tc::mma_commit(barX);
             }
             __syncwarp();
@@ -476,7 +477,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                     from_t = j.in_t;
                 }
             }
-            const bool enters = from != nullptr;
+            const bool enters = from != nullptr, fine = j.fine != 0;
             bool bad = false;   // something was not finite
             bool keeps = true;  // (STATE) no cut so far
             // (without TMA the workers load: keys and queries a chunk ahead within an item)
@@ -542,10 +543,10 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 const uint32_t ta = base + L::a + slot * L::tile, tb = base + L::b + slot * L::tile, tv = base + L::c;
                 const bool has_x = enters || c > 0;
                 if constexpr (!TMA) copy_wait<1>();
-                if constexpr (!STATE) tma_store_read();
+                if constexpr (!STATE) tma_store_read();  // (the outputs' copies have read a's tile, which is filled again)
                 tc::fence_proxy_async_smem();
                 tc::fence_before_sync();
-                worker_barrier<D>();  // the outputs' place is free (CUT: and the chunk's cuts there)
+                if (CUT || !TMA) worker_barrier<D>();  // the chunk's cuts, or its tiles, are there
                 hand_over<D>(kRead);
                 if (!TMA && c > 0) load_ab(c + 1);
                 // tokens that begin something new: what a token sees begins with the last of them up to it (counted in steps)
@@ -720,8 +721,9 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                     tc::fence_before_sync();
                     hand_over<D>(kWeighted);
                 }
-                // b -> b w as three bf16 values, what each leaves rounded to the next: in b's place, in lo, and (once the products with a
-                // are done) in a's place
+                // b -> b w as bf16 values.  Where the state leaves, as three, what each leaves rounded to the next: in b's place, in lo, and
+                // (once the products with Xb are done) in Xb's place.  Where only Xb is read from it, as two (2^-17): with w = w1 + w2,
+                // hi = b w1 rounded, lo = (b w1 - hi) + b w2, where b w1 - hi is exact (16 bits of a product, the first 8 taken away)
                 {
                     constexpr int per = D / 8, stride = L::workers / per, turns = kChunk / stride;
                     const int ch = tid % per, row0 = tid / per;
@@ -736,26 +738,39 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                         const int s = step_of(row0 + k * stride);  // its weight in the next state (STATE: in the span's)
                         const bool counts = s < rows && s >= keep_from;
                         const float f = !counts ? 0.f : scales[2] * (STATE ? decay_power(g, stop - s0 - s) : power[rows - s - less]);
-                        const Pair w = twice(f), minus = twice(-1.f);
                         uint32_t hi[4], lo[4];
+                        if (TMA && !counts) v[k][0] = v[k][1] = v[k][2] = v[k][3] = 0u;  // (whatever lies there)
+                        if (fine) {
+                            const Pair w = twice(f), minus = twice(-1.f);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            if (TMA && !counts) v[k][i] = 0u;  // (whatever lies there)
-                            Pair x = mul2(pair_of(v[k][i] << 16, v[k][i] & 0xffff0000u), w);
-                            hi[i] = pack2(x.f.x, x.f.y);
-                            x = fma2(pair_of(hi[i] << 16, hi[i] & 0xffff0000u), minus, x);
-                            lo[i] = pack2(x.f.x, x.f.y);
-                            x = fma2(pair_of(lo[i] << 16, lo[i] & 0xffff0000u), minus, x);
-                            v[k][i] = pack2(x.f.x, x.f.y);
-                            if constexpr (D == 64) v[k][i] = hmul(v[k][i], 0x3f003f00u);  // (it is added twice)
+                            for (int i = 0; i < 4; ++i) {
+                                Pair x = mul2(pair_of(v[k][i] << 16, v[k][i] & 0xffff0000u), w);
+                                hi[i] = pack2(x.f.x, x.f.y);
+                                x = fma2(pair_of(hi[i] << 16, hi[i] & 0xffff0000u), minus, x);
+                                lo[i] = pack2(x.f.x, x.f.y);
+                                x = fma2(pair_of(lo[i] << 16, lo[i] & 0xffff0000u), minus, x);
+                                v[k][i] = pack2(x.f.x, x.f.y);
+                                if constexpr (D == 64) v[k][i] = hmul(v[k][i], 0x3f003f00u);  // (it is added twice)
+                            }
+                        } else {
+                            const uint32_t w1 = pack2(f, f);
+                            const float rest = f - __uint_as_float(w1 << 16);
+                            const uint32_t w2 = pack2(rest, rest);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                hi[i] = hmul(v[k][i], w1);
+                                lo[i] = hfma(v[k][i], w2, hfma(v[k][i], w1, hi[i] ^ 0x80008000u));
+                            }
                         }
                         asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(tb + to), "r"(hi[0]), "r"(hi[1]), "r"(hi[2]), "r"(hi[3]) : "memory");
                         asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(base + L::lo + to), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
                     }
-                    if constexpr (!STATE) wait(barO, phase);
+                    if (fine) {
+                        if constexpr (!STATE) wait(barO, phase);
 #pragma unroll
-                    for (int k = 0; k < turns; ++k)
-                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(ta + off + k * stride * 128), "r"(v[k][0]), "r"(v[k][1]), "r"(v[k][2]), "r"(v[k][3]) : "memory");
+                        for (int k = 0; k < turns; ++k)
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(base + L::xb + off + k * stride * 128), "r"(v[k][0]), "r"(v[k][1]), "r"(v[k][2]), "r"(v[k][3]) : "memory");
+                    }
                 }
                 tc::fence_proxy_async_smem();
                 tc::fence_before_sync();
@@ -763,10 +778,11 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 hand_over<D>(kReady);
                 find_cuts(c + 1);
                 if constexpr (!STATE) {
-                    // y = O1 + in_scale lambda^step O2, by way of Xb's place (32 rows of 64 bytes a warp, 64-byte swizzle) to whole rows
+                    // y = O1 + in_scale lambda^step O2, by way of a's tile (32 rows of 64 bytes a warp, 64-byte swizzle) to whole rows
                     const bool sees = !CUT || begin < 0;
-                    const uint32_t stage = base + L::xb + warp * 2048, own = stage + lane * 64, turn = (lane >> 1) & 3;
+                    const uint32_t stage = ta + warp * 2048, own = stage + lane * 64, turn = (lane >> 1) & 3;
                     const Pair w = twice(scales[1] * power[step]);
+                    if (!fine) wait(barO, phase);
                     uint32_t o1[32];
                     TC_LD32(mine + L::tO1 + col0, o1);
                     if (has_x) {
@@ -825,7 +841,6 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             bad = (odd & 0x7fff7fffu) != 0;  // (a product with 0 is 0 or NaN)
             if constexpr (!STATE) tma_store_read();
             if constexpr (!TMA) copy_wait<0>();
-            if constexpr (!STATE) worker_barrier<D>();  // (the outputs' place is free: the state leaves by it)
             // the next item's marks, and its state on the way to L2, while this one's state leaves
             const Item next = open(m.at + (int)gridDim.x);
             float g_next = 0.f;
