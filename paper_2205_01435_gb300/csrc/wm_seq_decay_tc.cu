@@ -6,8 +6,8 @@
 //   P = A * weights               TMEM -> registers -> TMEM as bf16, where the next product reads it
 //   O2 = a Xb                     Xb: the state X, fp32 in TMEM, as a bf16 tile
 //   O1 = P c,  y = O1 + in_scale lambda^r O2
-//   X = lambda^n X + (b w)^T c    in place in TMEM; b w as three bf16 values, all 24 bits of it, where the state leaves: it is as
-//                                 good as in fp32; as two where only Xb is read from it
+//   X = lambda^n X + (b w)^T c    in place in TMEM; b w as three bf16 values, all 24 bits of it, where the state leaves and the chunk
+//                                 still counts in it: it is as good as in fp32; else as two
 // a, b and c lie as [128 tokens][64 values] panels of 128-byte rows in the 128-byte swizzle, which serve as K-major operands
 // (a, b in A and O2) and as MN-major ones (c, and b transposed, where the tokens are summed over).  Rows come by asynchronous
 // 16-byte copies that a padded token or value leaves as zeros: lengths, strides and either direction of time cost nothing extra.
@@ -228,6 +228,10 @@ __device__ __forceinline__ bool state_out(const float4 *x, float *to, int da, in
     }
     return !(odd == 0.f);
 }
+// Are a chunk's keys taken in three parts?  Where the state leaves, unless what the chunk gives it is down to 1/16 by then: two parts'
+// 2^-17 of that is 2^-21, below what fp32 sums of hundreds of terms are off by.
+__device__ __forceinline__ bool in_three(float log_decay, int tokens_left) { return tokens_left <= 0 || (float)tokens_left * log_decay > -2.7725887f; }
+
 // What the workers hand to the issuing warp: they arrive and go on, it waits.  (No worker arrives twice before it has waited:
 // in between each waits for a product that was issued after.)
 enum { kRead = 6, kScaled = 7, kWeighted = 8, kReady = 9 };
@@ -321,7 +325,8 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
     if (!worker) {
         // ---- one thread issues the products, and the copies: keys and queries a chunk ahead, of the next item too
         struct Cursor {  // a chunk: of item `at`, the c-th of its `chunks`, from token t0
-            int at, c, chunks, t0, dt, n, head, maps;
+            int at, c, chunks, t0, dt, n, head, maps, left;  // left: tokens of the sequence from this chunk's end on
+            float g;
             bool enters, fine;
         };
         const auto find = [&](Cursor &k, int at) {  // the first chunk of item `at`, or of the next one that has any
@@ -329,12 +334,13 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 const Item m = open(at);
                 const decay_job &j = p.job[m.job];
                 k = {at, 0, m.chunks, begin_of(m, 0), m.rev ? -kChunk : kChunk, m.n, m.head, j.map[0] | j.map[1] << 2 | j.map[2] << 4,
-                     !STATE && (p.spans > 1 || j.s_in), j.fine != 0};
+                     m.len - m.first - kChunk, at < items ? p.log_decay[m.head] : 0.f, !STATE && (p.spans > 1 || j.s_in), j.fine != 0};
                 if (m.chunks > 0 || at >= items) return;
             }
         };
         const auto step = [&](Cursor &k) {
             k.t0 += k.dt;
+            k.left -= kChunk;
             if (++k.c >= k.chunks && k.at < items) find(k, k.at + (int)gridDim.x);
         };
         const auto load = [&](const Cursor &k, uint32_t dst, int map, uint32_t bar) {
@@ -378,7 +384,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
         };
 #pragma unroll 1
         for (int done = 0; now.at < items; ++done) {  // chunks
-            const bool has_x = now.enters || now.c > 0, fresh = STATE && now.c == 0, fine = now.fine;
+            const bool has_x = now.enters || now.c > 0, fresh = STATE && now.c == 0, fine = now.fine && in_three(now.g, now.left);
             const int slot = done & 1;
             const uint32_t ta = base + L::a + slot * L::tile, tb = base + L::b + slot * L::tile, tv = base + L::c;
             if (TMA && !(early && done > 0)) wait(barQK + 8 * slot, done >> 1);
@@ -477,7 +483,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                     from_t = j.in_t;
                 }
             }
-            const bool enters = from != nullptr, fine = j.fine != 0;
+            const bool enters = from != nullptr;
             bool bad = false;   // something was not finite
             bool keeps = true;  // (STATE) no cut so far
             // (without TMA the workers load: keys and queries a chunk ahead within an item)
@@ -540,6 +546,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
 #pragma unroll 1
             for (int c = 0; c < chunks; ++c) {
                 const int s0 = first + c * kChunk, t0 = begin_of(m, c), rows = min(kChunk, stop - s0), slot = (done + c) & 1, phase = done + c;
+                const bool fine = j.fine && in_three(g, len - s0 - kChunk);
                 const uint32_t ta = base + L::a + slot * L::tile, tb = base + L::b + slot * L::tile, tv = base + L::c;
                 const bool has_x = enters || c > 0;
                 if constexpr (!TMA) copy_wait<1>();
