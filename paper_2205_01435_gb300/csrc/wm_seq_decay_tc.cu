@@ -63,7 +63,7 @@ struct Plan {
     // both also hold the state on its way in and out)
     static constexpr int b = 0, lo = b + 2 * tile, xb = lo + tile, a = xb + tile, c = a + 2 * tile, end = c + tile;
     static constexpr int small = end;  // tables and barriers
-    static constexpr int bytes = small + 4 * 132 + 48 + 48;
+    static constexpr int bytes = small + 48 + 48;
     // P lies over A: 16 tokens' column pairs where their warps read them, in blocks of `own` columns of A; with D = 64 O2, in two
     // halves, over the rest of each block
     static constexpr int own = 128 / (D / 32);
@@ -232,6 +232,14 @@ __device__ __forceinline__ bool state_out(const float4 *x, float *to, int da, in
 // 2^-17 of that is 2^-21, below what fp32 sums of hundreds of terms are off by.
 __device__ __forceinline__ bool in_three(float log_decay, int tokens_left) { return tokens_left <= 0 || (float)tokens_left * log_decay > -2.7725887f; }
 
+// 2^(rate n), rate = log2 lambda and not -inf, as good as 2^-22: for what is rounded to 2^-8.  (In registers: a look at a table in
+// shared memory takes some 250 cycles beside the tensor cores' own.)
+__device__ __forceinline__ float power_of(float rate, int n) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(rate * (float)n));
+    return r;
+}
+
 // What the workers hand to the issuing warp: they arrive and go on, it waits.  (No worker arrives twice before it has waited:
 // in between each waits for a product that was issued after.)
 enum { kRead = 6, kScaled = 7, kWeighted = 8, kReady = 9 };
@@ -255,9 +263,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
     constexpr bool early = TMA && !STATE && D == 128;  // A of the next chunk is formed as soon as P is read (O2 has a place of its own)
     extern __shared__ __align__(1024) unsigned char smem[];
     const uint32_t base = tc::smem_u32(smem);
-    float *const power = reinterpret_cast<float *>(smem + L::small);         // lambda^0 .. lambda^128
-    float *const scales = power + 129;                                       // of products, of the entering state, of its update
-    uint32_t *const cuts = reinterpret_cast<uint32_t *>(power + 132);       // [2][4]: tokens that begin something new
+    uint32_t *const cuts = reinterpret_cast<uint32_t *>(smem + L::small);    // [2][4]: tokens that begin something new
     volatile int *const late = reinterpret_cast<int *>(cuts + 8);           // a wait gave up
     uint32_t *const tmem_at = cuts + 9;
     const uint32_t bars = tc::smem_u32(cuts + 12), barA = bars, barO = bars + 8, barX = bars + 16, barV = bars + 24, barQK = bars + 32;
@@ -281,8 +287,15 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
         if (at >= items) return m;
         m.span = at / (pairs * jobs);
         const int k = at - m.span * pairs * jobs;
-        m.pair = k / jobs;
-        m.job = job_at[k - m.pair * jobs];
+        if (jobs == 3) {
+            // the pass in time's order first, then the two against it side by side (they read the same arrays; all CTAs run the same
+            // code at a time: 1024 x 64 x 16 x 64 backward 390 -> 381 us)
+            m.pair = k < pairs ? k : (k - pairs) / 2;
+            m.job = k < pairs ? 0 : 1 + (k - pairs) % 2;
+        } else {
+            m.pair = k / jobs;
+            m.job = job_at[k - m.pair * jobs];
+        }
         m.n = m.pair / p.H;
         m.head = m.pair - m.n * p.H;
         const decay_seq q = decay_open(p, p.job[m.job], m.n);
@@ -510,13 +523,12 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 load_ab(1);
             }
             find_cuts(0);
-            if (tid <= kChunk) power[tid] = decay_power(g, tid);
-            if (tid < 3) scales[tid] = tid == 0 ? j.w_scale : tid == 1 ? j.in_scale : j.up_scale;
+            const float rate = fmaxf(g * 1.4426950408889634f, -1e4f), w_scale = j.w_scale, in_scale = j.in_scale, up_scale = j.up_scale;
             worker_barrier<D>();
             // The entering state into TMEM: row a thread's lane, 32 columns a thread.  With D = 64 the state is the sum of lanes 0
             // to 63 (sums of the keys' first parts) and 64 to 127 (of the second).
             if (enters && chunks > 0) {
-                const float mul = p.spans == 1 && j.first ? power[1] : 1.f;
+                const float mul = p.spans == 1 && j.first ? decay_power(g, 1) : 1.f;
                 uint32_t r[32];
                 if (from_t) {  // (a row of the state is a column there: lanes read side by side)
 #pragma unroll
@@ -578,11 +590,10 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 const int less = !STATE && j.first && s0 + rows == len ? 1 : 0;
                 if (STATE && TMA) wait(barQK + 8 * slot, phase >> 1);
                 constexpr int cols = 128 / (D / 32);  // of A, a thread
-                uint32_t packed[cols / 2];
                 if constexpr (!STATE) {
                     // X -> Xb, and X to what the next state keeps of it
                     if (has_x) {
-                        const Pair shrink = twice(power[rows - less]);
+                        const Pair shrink = twice(decay_power(g, rows - less));
                         uint32_t r[32];
                         const int row = D == 64 ? xrow & 63 : xrow;
                         const uint32_t to = base + L::xb + (col0 / 64) * (D * 128) + row * 128;
@@ -637,78 +648,73 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                         }
                         tmem_st_wait();
                     }
-                    // A -> P: row xrow, 16 columns at a time.  Weights lambda^away by products from the nearest column on: up to 16
-                    // roundings of 2^-24, before one of 2^-8
+                    // A -> P: row xrow, 32 columns at a time, P over columns that are read.  Weights lambda^away by products from the
+                    // nearest column on: up to 32 roundings of 2^-24, before one of 2^-8
                     wait(barA, phase);
-                    const float w_scale = scales[0], lambda = power[1];
 #pragma unroll
-                    for (int h = 0; h < cols / 16; ++h) {
-                        const int j0 = group * cols + h * 16, block = j0 / 32, i0 = j0 % 32;
+                    for (int h = 0; h < cols / 32; ++h) {
+                        const int block = group * (cols / 32) + h, j0 = block * 32;
+                        uint32_t v[32];
                         if (rev ? block < quad : block > quad) {  // not seen
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) packed[h * 8 + i] = 0u;
-                            continue;
-                        }
-                        uint32_t v[16];
-                        TC_LD16(mine + L::tA + j0, v);
-                        const auto weigh = [&](int i, float a, float b) {
-                            Pair w;
-                            w.f = make_float2(a, b);
-                            w = mul2(pair_of(v[i], v[i + 1]), w);
-                            packed[h * 8 + i / 2] = pack2(w.f.x, w.f.y);
-                        };
-                        // (the weight of the column before the first of these, in the order they are taken)
-                        const int before = rev ? j0 - 1 - xrow : xrow - j0 - 16;
-                        float w = before >= 0 ? w_scale * power[before] : 0.f;
-                        tc::tmem_ld_wait();
-                        if (block == quad) {
-                            const int own = lane - i0;  // the token itself; columns behind it are not seen, whatever they hold
-                            if (!rev) {
-#pragma unroll
-                                for (int i = 14; i >= 0; i -= 2) {
-                                    const float b = i + 1 == own ? w_scale : w * lambda;
-                                    w = i == own ? w_scale : b * lambda;
-                                    v[i + 1] = i + 1 <= own ? v[i + 1] : 0u;
-                                    v[i] = i <= own ? v[i] : 0u;
-                                    weigh(i, w, b);
-                                }
-                            } else {
-#pragma unroll
-                                for (int i = 0; i < 16; i += 2) {
-                                    const float a = i == own ? w_scale : w * lambda;
-                                    w = i + 1 == own ? w_scale : a * lambda;
-                                    v[i] = i >= own ? v[i] : 0u;
-                                    v[i + 1] = i + 1 >= own ? v[i + 1] : 0u;
-                                    weigh(i, a, w);
-                                }
-                            }
+                            for (int i = 0; i < 16; ++i) v[i] = 0u;
                         } else {
-                            const Pair lambda2 = twice(lambda * lambda);
-                            Pair t;
-                            w *= lambda;
-                            if (!rev) {
-                                t.f = make_float2(w * lambda, w);
+                            TC_LD32(mine + L::tA + j0, v);
+                            const float lambda = power_of(rate, 1);
+                            const auto weigh = [&](int i, float a, float b) {
+                                const Pair w = mul2(pair_of(v[i], v[i + 1]), seq_pair_of(a, b));
+                                v[i] = __float_as_uint(w.f.x), v[i + 1] = __float_as_uint(w.f.y);
+                            };
+                            if (block == quad) {  // columns behind the token itself are not seen, whatever they hold
+                                float w = 0.f;
+                                tc::tmem_ld_wait();
+                                if (!rev) {
 #pragma unroll
-                                for (int i = 14; i >= 0; i -= 2, t = mul2(t, lambda2)) weigh(i, t.f.x, t.f.y);
+                                    for (int i = 30; i >= 0; i -= 2) {
+                                        const float b = i + 1 == lane ? w_scale : w * lambda;
+                                        w = i == lane ? w_scale : b * lambda;
+                                        v[i + 1] = i + 1 <= lane ? v[i + 1] : 0u;
+                                        v[i] = i <= lane ? v[i] : 0u;
+                                        weigh(i, w, b);
+                                    }
+                                } else {
+#pragma unroll
+                                    for (int i = 0; i < 32; i += 2) {
+                                        const float a = i == lane ? w_scale : w * lambda;
+                                        w = i + 1 == lane ? w_scale : a * lambda;
+                                        v[i] = i >= lane ? v[i] : 0u;
+                                        v[i + 1] = i + 1 >= lane ? v[i + 1] : 0u;
+                                        weigh(i, a, w);
+                                    }
+                                }
                             } else {
-                                t.f = make_float2(w, w * lambda);
+                                const float w = w_scale * power_of(rate, rev ? j0 - xrow : xrow - j0 - 31);
+                                const Pair lambda2 = twice(lambda * lambda);
+                                Pair t = rev ? seq_pair_of(w, w * lambda) : seq_pair_of(w * lambda, w);
+                                tc::tmem_ld_wait();
+                                if (!rev) {
 #pragma unroll
-                                for (int i = 0; i < 16; i += 2, t = mul2(t, lambda2)) weigh(i, t.f.x, t.f.y);
+                                    for (int i = 30; i >= 0; i -= 2, t = mul2(t, lambda2)) weigh(i, t.f.x, t.f.y);
+                                } else {
+#pragma unroll
+                                    for (int i = 0; i < 32; i += 2, t = mul2(t, lambda2)) weigh(i, t.f.x, t.f.y);
+                                }
                             }
-                        }
-                        if (CUT && any_cut) {
+                            if (CUT && any_cut) {
 #pragma unroll
-                            for (int i = 0; i < 8; ++i)
-                                packed[h * 8 + i] &= (step_of(j0 + 2 * i) >= begin ? 0xffffu : 0u) | (step_of(j0 + 2 * i + 1) >= begin ? 0xffff0000u : 0u);
+                                for (int i = 0; i < 32; ++i) v[i] = step_of(j0 + i) >= begin ? v[i] : 0u;
+                            }
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) v[i] = pack2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
                         }
+                        __syncwarp();
+                        TC_ST16(mine + L::tA + group * cols + h * 16, v);
                     }
                 }
                 if constexpr (!STATE) {
                     tc::fence_proxy_async_smem();  // Xb
                     tc::fence_before_sync();
                     hand_over<D>(kScaled);
-                    if constexpr (cols == 64) TC_ST32(mine + L::tA + group * 64, packed);
-                    else TC_ST16(mine + L::tA + group * 32, packed);
                 }
                 if constexpr (TMA) {
                     if (rows < kChunk) {  // values of steps that are not there: whatever lies there times 0 is to be 0
@@ -744,7 +750,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                         const uint32_t to = off + k * stride * 128;
                         const int s = step_of(row0 + k * stride);  // its weight in the next state (STATE: in the span's)
                         const bool counts = s < rows && s >= keep_from;
-                        const float f = !counts ? 0.f : scales[2] * (STATE ? decay_power(g, stop - s0 - s) : power[rows - s - less]);
+                        const float f = !counts ? 0.f : up_scale * decay_power(g, STATE ? stop - s0 - s : rows - s - less);
                         uint32_t hi[4], lo[4];
                         if (TMA && !counts) v[k][0] = v[k][1] = v[k][2] = v[k][3] = 0u;  // (whatever lies there)
                         if (fine) {
@@ -788,7 +794,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                     // y = O1 + in_scale lambda^step O2, by way of a's tile (32 rows of 64 bytes a warp, 64-byte swizzle) to whole rows
                     const bool sees = !CUT || begin < 0;
                     const uint32_t stage = ta + warp * 2048, own = stage + lane * 64, turn = (lane >> 1) & 3;
-                    const Pair w = twice(scales[1] * power[step]);
+                    const Pair w = twice(in_scale * power_of(rate, step));
                     if (!fine) wait(barO, phase);
                     uint32_t o1[32];
                     TC_LD32(mine + L::tO1 + col0, o1);
