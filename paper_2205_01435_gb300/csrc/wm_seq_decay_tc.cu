@@ -779,7 +779,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                         asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(base + L::lo + to), "r"(lo[0]), "r"(lo[1]), "r"(lo[2]), "r"(lo[3]) : "memory");
                     }
                     if (fine) {
-                        if constexpr (!STATE) wait(barO, phase);
+                        if (!STATE && has_x) wait(barO, phase);
 #pragma unroll
                         for (int k = 0; k < turns; ++k)
                             asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(base + L::xb + off + k * stride * 128), "r"(v[k][0]), "r"(v[k][1]), "r"(v[k][2]), "r"(v[k][3]) : "memory");
@@ -795,7 +795,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                     const bool sees = !CUT || begin < 0;
                     const uint32_t stage = ta + warp * 2048, own = stage + lane * 64, turn = (lane >> 1) & 3;
                     const Pair w = twice(in_scale * power_of(rate, step));
-                    if (!fine) wait(barO, phase);
+                    if (!fine || !has_x) wait(barO, phase);
                     uint32_t o1[32];
                     TC_LD32(mine + L::tO1 + col0, o1);
                     if (has_x) {

@@ -1,7 +1,7 @@
 // wm_seq_heads.cu -- the norm of each head's vector and its rotation by position, forward and backward.
 //
 //   y = x r w, r = 1 / sqrt(mean(x^2) + eps); pairs (a, b) of y turn: (a cos - b sin, b cos + a sin)
-//   backward, with d = dy turned back and g = d w: dx = r (g - x r^2 mean(g x)), dw = sum d x r
+//   backward, with d = dy turned back and g = d w: dx = r (g - xhat mean(g xhat)), xhat = x r, dw = sum d xhat
 //
 // Bound by memory: forward moves 2 values per element, backward 3.  A row (one head of one token) lives in the
 // registers of G lanes, each with units of two vectors that hold the two sides of its pairs, so that a rotation
@@ -51,16 +51,74 @@ constexpr bool held() {
     return VEC * UPL <= 8;
 }
 
+// Vectors of fp32, two values an instruction where there are two.
+template <int N>
+__device__ __forceinline__ void times(float (&r)[N], const float (&a)[N], const float (&b)[N]) {
+    if constexpr (N % 2 == 0) {
+#pragma unroll
+        for (int m = 0; m < N; m += 2) {
+            const seq_pair p = seq_mul2(seq_pair_of(a[m], a[m + 1]), seq_pair_of(b[m], b[m + 1]));
+            r[m] = p.f.x, r[m + 1] = p.f.y;
+        }
+    } else {
+#pragma unroll
+        for (int m = 0; m < N; ++m) r[m] = a[m] * b[m];
+    }
+}
+template <int N>
+__device__ __forceinline__ void times_plus(float (&r)[N], const float (&a)[N], const float (&b)[N], const float (&c)[N]) {  // r = a b + c
+    if constexpr (N % 2 == 0) {
+#pragma unroll
+        for (int m = 0; m < N; m += 2) {
+            const seq_pair p = seq_fma2(seq_pair_of(a[m], a[m + 1]), seq_pair_of(b[m], b[m + 1]), seq_pair_of(c[m], c[m + 1]));
+            r[m] = p.f.x, r[m + 1] = p.f.y;
+        }
+    } else {
+#pragma unroll
+        for (int m = 0; m < N; ++m) r[m] = a[m] * b[m] + c[m];
+    }
+}
+template <int N>
+__device__ __forceinline__ void all_of(float (&r)[N], float v) {
+#pragma unroll
+    for (int m = 0; m < N; ++m) r[m] = v;
+}
+// Sums of products, in two halves.
+template <int N>
+__device__ __forceinline__ void dot(seq_pair &sum, const float (&a)[N], const float (&b)[N]) {
+    if constexpr (N % 2 == 0) {
+#pragma unroll
+        for (int m = 0; m < N; m += 2) sum = seq_fma2(seq_pair_of(a[m], a[m + 1]), seq_pair_of(b[m], b[m + 1]), sum);
+    } else {
+#pragma unroll
+        for (int m = 0; m < N; ++m) sum.f.x += a[m] * b[m];
+    }
+}
+
+// N values that lie side by side, aligned to as many as one access takes.
+template <int N>
+__device__ __forceinline__ void quads(float (&r)[N], const float *p) {
+    constexpr int V = N % 4 == 0 ? 4 : N;
+#pragma unroll
+    for (int m = 0; m < N; m += V) {
+        const seq_vec<float, V> v = seq_load<float, V>(p + m);
+#pragma unroll
+        for (int k = 0; k < V; ++k) r[m + k] = v.v[k];
+    }
+}
+
 struct TileRow {  // where a token's rows begin
     long long x, y, o;
 };
 // Shared memory: phases, two tiles' angles and rows for each warp, weights (and, for their gradient, a row of sums a warp).
 constexpr int kWarps = kThreads / 32;
+// A token's angles: cosines, sines (as the direction turns), minus those; each a whole number of quads.
+__host__ __device__ constexpr int angles(int half) { return 3 * ((half + 3) / 4 * 4); }
 struct HeadsSmem {
     size_t turn, row, weight, bytes;
     __host__ __device__ HeadsSmem(int half, int tile, int D, bool backward) {
         turn = ((size_t)half * 8 + 15) / 16 * 16;
-        row = (turn + (size_t)kWarps * 2 * tile * half * 8 + 15) / 16 * 16;
+        row = (turn + (size_t)kWarps * 2 * tile * angles(half) * 4 + 15) / 16 * 16;
         weight = row + (size_t)kWarps * 2 * tile * sizeof(TileRow);
         bytes = weight + (size_t)(backward ? kWarps : 1) * ((D + 7) / 8 * 8) * 4;
     }
@@ -76,7 +134,8 @@ __global__ void __launch_bounds__(kThreads, UPL *VEC > 8 ? 1 : BWD ? 2 : 3) head
     const HeadsSmem at(half, p.tile, p.D, BWD);
     unsigned long long *phase = reinterpret_cast<unsigned long long *>(smem);
     const int warp = threadIdx.x >> 5, wl = threadIdx.x & 31;
-    float2 *const turns = reinterpret_cast<float2 *>(smem + at.turn) + (size_t)warp * 2 * p.tile * half;  // [2][tile][half]: cos, sin
+    const int each = angles(half) / 3;
+    float *const turns = reinterpret_cast<float *>(smem + at.turn) + (size_t)warp * 2 * p.tile * 3 * each;  // [2][tile][3][each]
     TileRow *const starts = reinterpret_cast<TileRow *>(smem + at.row) + warp * 2 * p.tile;               // [2][tile]
     float *const weight = reinterpret_cast<float *>(smem + at.weight);
     const bool keys = blockIdx.x >= (unsigned)p.side[0].ctas;
@@ -107,16 +166,22 @@ __global__ void __launch_bounds__(kThreads, UPL *VEC > 8 ? 1 : BWD ? 2 : 3) head
         vb[i] = hb[i] ? b * VEC : 0;
     }
     // a tile's angles and rows, into the places of even or odd tiles
+    // (the positions of the tile after it are on their way meanwhile, a lane each)
+    int ahead = half && tok0 + wl < end && wl < p.tile ? p.positions[tok0 + wl] : 0;
     const auto prepare = [&](long long tok0, int slot) {
-        const int tile = (int)min((long long)p.tile, end - tok0);
+        const int tile = (int)min((long long)p.tile, end - tok0), now = ahead;
+        ahead = half && tok0 + p.tile + wl < end && wl < p.tile ? p.positions[tok0 + p.tile + wl] : 0;
         for (int k = 0; k < tile; ++k) {
-            const unsigned long long pos = half ? (unsigned long long)(long long)p.positions[tok0 + k] : 0;
+            const unsigned long long pos = (unsigned long long)(long long)__shfl_sync(~0u, now, k);
             for (int j = wl; j < half; j += 32) {
                 float sn, cs;
                 sincospif((float)(int)((phase[j] * pos + (1ull << 31)) >> 32) * 0x1p-31f, &sn, &cs);
                 const float f = p.freqs[j];
                 if (!(fabsf(f) <= 3.4028235e38f)) sn = cs = f - f;  // NaN: no angle of a frequency that is none
-                turns[(slot * p.tile + k) * half + j] = make_float2(cs, sn);
+                float *const t = turns + (slot * p.tile + k) * 3 * each + j;
+                t[0] = cs;
+                t[each] = BWD ? -sn : sn;
+                t[2 * each] = BWD ? sn : -sn;
             }
         }
         if (wl < tile) {
@@ -143,13 +208,13 @@ __global__ void __launch_bounds__(kThreads, UPL *VEC > 8 ? 1 : BWD ? 2 : 3) head
     for (int slot = 0; tok0 < end; tok0 += p.tile, slot ^= 1) {
         if (tok0 + p.tile < end) prepare(tok0 + p.tile, slot ^ 1);
         const int tile = (int)min((long long)p.tile, end - tok0), rows = tile * heads;
-        const float2 *const turn = turns + slot * p.tile * half;
+        const float *const turn = turns + slot * p.tile * 3 * each;
         const TileRow *const start = starts + slot * p.tile;
         int token = row0 / heads, head = row0 - token * heads;
         for (int r = row0; r - row0 < rows; r += R * rows_at_once) {  // (all lanes walk along: they sum over the group)
             seq_vec<T, VEC> xa[R][UPL], xb[R][UPL], ya[BWD ? R : 1][UPL], yb[BWD ? R : 1][UPL];
             T *out[R];
-            const float2 *tw[R];
+            const float *tw[R];
 #pragma unroll
             for (int q = 0; q < R; ++q) {
                 const bool on = r + q * rows_at_once < rows;
@@ -157,7 +222,7 @@ __global__ void __launch_bounds__(kThreads, UPL *VEC > 8 ? 1 : BWD ? 2 : 3) head
                 const T *const x = static_cast<const T *>(sd.x) + s.x + (on ? head : 0) * sd.xh;
                 const T *const dy = BWD ? static_cast<const T *>(sd.dy) + s.y + (on ? head : 0) * sd.yh : nullptr;
                 out[q] = static_cast<T *>(sd.out) + s.o + (on ? head : 0) * sd.oh;
-                tw[q] = turn + (on ? token : 0) * half;
+                tw[q] = turn + (on ? token : 0) * 3 * each;
 #pragma unroll
                 for (int i = 0; i < UPL; ++i) {
                     xa[q][i] = on && ha[i] ? seq_load<T, VEC>(x + va[i]) : seq_vec<T, VEC>{};
@@ -174,101 +239,99 @@ __global__ void __launch_bounds__(kThreads, UPL *VEC > 8 ? 1 : BWD ? 2 : 3) head
 #pragma unroll
             for (int q = 0; q < R; ++q) {
                 const bool on = r + q * rows_at_once < rows;
-                // turns a unit's values in place, by sign * angle
-                const auto rotate = [&](int i, float(&a)[VEC], float(&b)[VEC], float sign) {
+                // turns a unit's values in place
+                const auto rotate = [&](int i, float(&a)[VEC], float(&b)[VEC]) {
                     if constexpr (IN) {
+                        constexpr int C = VEC / 2;
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
                             float(&v)[VEC] = h ? b : a;
                             const int from = h ? vb[i] : va[i];
                             if (from >= p.rotary) continue;
-                            float c[VEC];  // cos, sin, cos, sin ...
+                            float c[C], s[C];
+                            quads(c, tw[q] + from / 2);
+                            quads(s, tw[q] + each + from / 2);
 #pragma unroll
-                            for (int m = 0; m < VEC; m += VEC < 4 ? 2 : 4) {
-                                if constexpr (VEC < 4) {
-                                    const float2 t = tw[q][from / 2];
-                                    c[0] = t.x, c[1] = t.y;
-                                } else {
-                                    const float4 t = *reinterpret_cast<const float4 *>(tw[q] + (from + m) / 2);
-                                    c[m] = t.x, c[m + 1] = t.y, c[m + 2] = t.z, c[m + 3] = t.w;
-                                }
-                            }
-#pragma unroll
-                            for (int m = 0; m < VEC; m += 2) {
-                                const float s = sign * c[m + 1], u = v[m], w = v[m + 1];
-                                v[m] = u * c[m] - w * s;
-                                v[m + 1] = w * c[m] + u * s;
+                            for (int m = 0; m < C; ++m) {
+                                const float u = v[2 * m], w = v[2 * m + 1];
+                                v[2 * m] = u * c[m] - w * s[m];
+                                v[2 * m + 1] = w * c[m] + u * s[m];
                             }
                         }
                     } else if (turns_here[i]) {
-                        const float2 *const t = tw[q] + (lane + i * p.group) * VEC;
-                        float c[VEC], s[VEC];
-                        if constexpr (VEC == 1) {
-                            c[0] = t->x, s[0] = t->y;
-                        } else {
-#pragma unroll
-                            for (int m = 0; m < VEC; m += 2) {
-                                const float4 two = *reinterpret_cast<const float4 *>(t + m);
-                                c[m] = two.x, s[m] = two.y, c[m + 1] = two.z, s[m + 1] = two.w;
-                            }
-                        }
-#pragma unroll
-                        for (int m = 0; m < VEC; ++m) {
-                            const float n = sign * s[m], u = a[m], w = b[m];
-                            a[m] = u * c[m] - w * n;
-                            b[m] = w * c[m] + u * n;
-                        }
+                        const float *const t = tw[q] + (lane + i * p.group) * VEC;
+                        float c[VEC], s[VEC], n[VEC], p1[VEC], p2[VEC];
+                        quads(c, t);
+                        quads(s, t + each);
+                        quads(n, t + 2 * each);
+                        times(p1, b, n);
+                        times(p2, a, s);
+                        times_plus(a, a, c, p1);
+                        times_plus(b, b, c, p2);
                     }
                 };
-                float ss = 0.f, gx = 0.f;
+                seq_pair s2 = seq_pair_of(0.f, 0.f), g2 = s2;
                 float fa[UPL][VEC], fb[UPL][VEC], da[BWD ? UPL : 1][VEC], db[BWD ? UPL : 1][VEC];
+                float ga[BWD ? UPL : 1][VEC], gb[BWD ? UPL : 1][VEC];  // the turned gradient times the weight
 #pragma unroll
                 for (int i = 0; i < UPL; ++i) {
                     seq_unpack<T, VEC>(xa[q][i], fa[i]);
                     seq_unpack<T, VEC>(xb[q][i], fb[i]);
-#pragma unroll
-                    for (int m = 0; m < VEC; ++m) ss += fa[i][m] * fa[i][m] + fb[i][m] * fb[i][m];
+                    dot(s2, fa[i], fa[i]);
+                    dot(s2, fb[i], fb[i]);
                     if constexpr (BWD) {
-                        float ua[VEC], ub[VEC];
-                        if constexpr (!HELD) weights_of(i, ua, ub);
                         seq_unpack<T, VEC>(ya[q][i], da[i]);
                         seq_unpack<T, VEC>(yb[q][i], db[i]);
-                        rotate(i, da[i], db[i], -1.f);
-#pragma unroll
-                        for (int m = 0; m < VEC; ++m)
-                            gx += da[i][m] * (HELD ? wa[HELD ? i : 0][m] : ua[m]) * fa[i][m] + db[i][m] * (HELD ? wb[HELD ? i : 0][m] : ub[m]) * fb[i][m];
+                        rotate(i, da[i], db[i]);
+                        if constexpr (HELD) {
+                            times(ga[i], da[i], wa[i]);
+                            times(gb[i], db[i], wb[i]);
+                        } else {
+                            float ua[VEC], ub[VEC];
+                            weights_of(i, ua, ub);
+                            times(ga[i], da[i], ua);
+                            times(gb[i], db[i], ub);
+                        }
+                        dot(g2, ga[i], fa[i]);
+                        dot(g2, gb[i], fb[i]);
                     }
                 }
+                float ss = s2.f.x + s2.f.y, gx = g2.f.x + g2.f.y;
                 for (int o = p.group / 2; o > 0; o >>= 1) {
                     ss += __shfl_xor_sync(~0u, ss, o);
                     if constexpr (BWD) gx += __shfl_xor_sync(~0u, gx, o);
                 }
                 const float rs = 1.f / sqrtf(ss * inv_d + p.eps);
-                const float back = BWD ? rs * rs * (gx * inv_d) : 0.f;
+                float r[VEC], back[VEC];
+                all_of(r, rs);
+                all_of(back, BWD ? -rs * (gx * inv_d) : 0.f);
 #pragma unroll
                 for (int i = 0; i < UPL; ++i) {
-                    float ua[VEC], ub[VEC];
-                    if constexpr (!HELD) weights_of(i, ua, ub);
                     if constexpr (BWD) {
+                        float ta[VEC], tb[VEC];
+                        times(ta, fa[i], r);
+                        times(tb, fb[i], r);
                         if (on) {  // (of rows that are there: what a thread without one holds may be what it likes)
-#pragma unroll
-                            for (int m = 0; m < VEC; ++m) {
-                                dwa[i][m] += da[i][m] * (fa[i][m] * rs);
-                                dwb[i][m] += db[i][m] * (fb[i][m] * rs);
-                            }
+                            times_plus(dwa[i], da[i], ta, dwa[i]);
+                            times_plus(dwb[i], db[i], tb, dwb[i]);
                         }
-#pragma unroll
-                        for (int m = 0; m < VEC; ++m) {
-                            fa[i][m] = rs * (da[i][m] * (HELD ? wa[HELD ? i : 0][m] : ua[m]) - fa[i][m] * back);
-                            fb[i][m] = rs * (db[i][m] * (HELD ? wb[HELD ? i : 0][m] : ub[m]) - fb[i][m] * back);
-                        }
+                        times_plus(fa[i], ta, back, ga[i]);
+                        times_plus(fb[i], tb, back, gb[i]);
+                        times(fa[i], fa[i], r);
+                        times(fb[i], fb[i], r);
                     } else {
-#pragma unroll
-                        for (int m = 0; m < VEC; ++m) {
-                            fa[i][m] = fa[i][m] * rs * (HELD ? wa[HELD ? i : 0][m] : ua[m]);
-                            fb[i][m] = fb[i][m] * rs * (HELD ? wb[HELD ? i : 0][m] : ub[m]);
+                        times(fa[i], fa[i], r);
+                        times(fb[i], fb[i], r);
+                        if constexpr (HELD) {
+                            times(fa[i], fa[i], wa[i]);
+                            times(fb[i], fb[i], wb[i]);
+                        } else {
+                            float ua[VEC], ub[VEC];
+                            weights_of(i, ua, ub);
+                            times(fa[i], fa[i], ua);
+                            times(fb[i], fb[i], ub);
                         }
-                        rotate(i, fa[i], fb[i], 1.f);
+                        rotate(i, fa[i], fb[i]);
                     }
                     if (on && ha[i]) seq_store<T, VEC>(out[q] + va[i], seq_pack<T, VEC>(fa[i]));
                     if (on && hb[i]) seq_store<T, VEC>(out[q] + vb[i], seq_pack<T, VEC>(fb[i]));
@@ -355,10 +418,10 @@ void ctas_of(const wm_seq *h, const seq_heads_args &a, bool backward, int (&ctas
     }
 }
 
-// Tokens a warp takes at once: about 4 turns of two rows a lane group.
+// Tokens a warp takes at once: about 16 rows a lane group.
 int tile_of(const seq_heads_args &a, int group) {
-    const int heads = std::max(a.heads[0], a.heads[1]), want = std::max(1, 8 * (32 / group) / heads);
-    const int room = a.rotary ? std::max(1, 1024 / a.rotary) : 32;  // 64 KB of angles
+    const int heads = std::max(a.heads[0], a.heads[1]), want = std::max(1, 16 * (32 / group) / heads);
+    const int room = a.rotary ? std::max(1, 1024 / a.rotary) : 32;  // 100 KB of angles
     return std::min({want, room, 32});
 }
 
