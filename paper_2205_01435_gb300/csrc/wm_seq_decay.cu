@@ -437,12 +437,14 @@ struct StepArgs {
 };
 
 template <class T, int ROWS, bool VEC>
-__global__ void __launch_bounds__(256) decay_step_kernel(const StepArgs p) {
+__global__ void __launch_bounds__(256, ROWS <= 4 ? 6 : ROWS <= 8 ? 4 : 2) decay_step_kernel(const __grid_constant__ StepArgs p) {
     __shared__ float q[256], k[256], v[64];
     __shared__ float part[8][64];
-    const long long pair = blockIdx.x / p.slices;
-    const int slice = blockIdx.x % p.slices, n = (int)(pair / p.H), head = (int)(pair % p.H), tid = threadIdx.x;
-    const int cg = tid & (p.ct - 1), rg = tid / p.ct, groups = 256 / p.ct, width = 4 * p.ct, col0 = slice * width, col = col0 + cg * 4;
+    const int item = (int)blockIdx.x, at_pair = p.slices == 1 ? item : item / p.slices, slice = item - at_pair * p.slices;  // (below 2^30)
+    const int n = at_pair / p.H, head = at_pair - n * p.H, tid = threadIdx.x;
+    const long long pair = at_pair;
+    const int shift = p.ct == 16 ? 4 : 3, cg = tid & (p.ct - 1), rg = tid >> shift, groups = 256 >> shift, width = 4 << shift, col0 = slice * width,
+              col = col0 + cg * 4;
     int len = p.T;
     if (p.lengths) {
         len = p.lengths[n];
