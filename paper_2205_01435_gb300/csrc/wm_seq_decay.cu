@@ -251,7 +251,8 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
             for (int i = 0; i < 4; ++i) begin[i] = start(ty * 4 + i);
             // p = a b^T, weighted; columns beyond the rows' own are not seen
             seq_pair acc[4][4] = {};
-            products<LD, LD>(acc, m.a, ty * 4, m.b, tx, dq, ty / 4 + 1);
+            const bool live = ty * 4 < rows;  // (of four rows, any)
+            if (live) products<LD, LD>(acc, m.a, ty * 4, m.b, tx, dq, ty / 4 + 1);
             careful = __syncthreads_or(careful);  // 2: c is turned over, and p's place free
             if constexpr (m.apart) careful |= turn(m.bt, m.b, LD, m.kept);
 #pragma unroll
@@ -269,7 +270,7 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
             float y[4][4];
             {
                 seq_pair in[4][4] = {};
-                products<LD, LD>(in, m.a, ty * 4, m.x, tx, dq, cblocks);
+                if (live) products<LD, LD>(in, m.a, ty * 4, m.x, tx, dq, cblocks);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const float w = in_scale * m.power[ty * 4 + i];
@@ -279,7 +280,7 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
             }
             if (!careful) {
                 seq_pair own[4][4] = {};
-                products<kChunk, kChunk>(own, m.p, ty * 4, m.c, tx, ty + 1, cblocks);
+                if (live) products<kChunk, kChunk>(own, m.p, ty * 4, m.c, tx, ty + 1, cblocks);
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -606,7 +607,15 @@ void split(const wm_seq *h, decay_pass &p, const seq_decay_args &a, bool tc) {
     p.spans = (int)std::max(1ll, (chunks + per - 1) / per);
 }
 
-bool steps_take(const seq_decay_args &a, bool backward) { return !backward && a.T <= 8; }
+// Tensor cores: bf16, heads of up to 128 values.
+bool tc_takes(const seq_decay_args &a) { return a.dtype == WM_BF16 && a.Dk <= kDecayTcMost && a.Dv <= kDecayTcMost; }
+
+// Up to how many tokens go one by one (both ways measured, us, state in place).  bf16 on tensor cores: 256 heads x 64 x 64, 12 tokens:
+// steps 25, chunks 25; 16: 31 and 25; 16,384 heads, 12: 422 and 466; 16: 548 and 461.  fp32, 4096 heads, 32: 292 and 316; 256 heads,
+// 12: 27 and 29; 16: 31 and 29.
+bool steps_take(const wm_seq *h, const seq_decay_args &a, bool backward) {
+    return !backward && a.T <= (tc_takes(a) ? 12 : (long long)a.N * a.H >= 2ll * h->sms ? 32 : 14);
+}
 
 // Scratch of a pass: the spans' states and carries, the marks of what is taken again, a copy of an entering state whose place
 // the leaving one takes.
@@ -710,13 +719,11 @@ cudaError_t run_pass(wm_seq *h, const seq_decay_args &a, decay_pass &p, bool tc,
     return chunk_launch<T, false>(h, p, s);
 }
 
-// Tensor cores: bf16, heads of up to 128 values, and more tokens than go one by one.
-bool tc_takes(const seq_decay_args &a) { return a.dtype == WM_BF16 && a.Dk <= kDecayTcMost && a.Dv <= kDecayTcMost; }
 
 }  // namespace
 
 size_t wm_seq_decay_ws(const wm_seq *h, const seq_decay_args &a, bool backward) {
-    if (a.T == 0 || steps_take(a, backward)) return 0;
+    if (a.T == 0 || steps_take(h, a, backward)) return 0;
     decay_pass p = pass_of(h, a, backward);
     split(h, p, a, tc_takes(a));
     return Scratch(p, a, backward, tc_takes(a)).bytes;
@@ -731,7 +738,7 @@ cudaError_t wm_seq_decay_launch(wm_seq *h, const seq_decay_args &a, bool backwar
         if (!to || to == from) return cudaSuccess;
         return from ? cudaMemcpyAsync(to, from, state, cudaMemcpyDeviceToDevice, s) : cudaMemsetAsync(to, 0, state, s);
     }
-    if (steps_take(a, backward)) return a.dtype == WM_BF16 ? steps<__nv_bfloat16>(h, a, s) : steps<float>(h, a, s);
+    if (steps_take(h, a, backward)) return a.dtype == WM_BF16 ? steps<__nv_bfloat16>(h, a, s) : steps<float>(h, a, s);
     const bool tc = tc_takes(a);
     decay_pass p = pass_of(h, a, backward);
     split(h, p, a, tc);
