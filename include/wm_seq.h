@@ -208,22 +208,23 @@ wm_status wm_seq_head_norm_backward(wm_seq *h, int dtype, long long T, int N, in
  *   s0       [N, heads, Dk, Dv] fp32 dense or NULL = zeros: the state entering the call
  *   reset    [T, N] uint8 dense or NULL: nonzero = step t starts a new episode, nothing before it is seen
  *            (also when that holds inf or NaN)
- *   lengths  [N] int32 or NULL = T: steps t >= lengths[n] are padding: their inputs and reset are not read, their
+ *   lengths  [N] int32 or NULL = T: steps t >= lengths[n] are padding: whatever their inputs and reset hold, their
  *            outputs are 0 and the state is carried on.  A length outside [0, T] is recorded as
  *            WM_ERR_INVALID_ARG and clamped.
  *   out      [T, N, heads, Dv] dtype, out
  *   s_last   [N, heads, Dk, Dv] fp32 dense, optional out: the state after the last step; may be s0
- * What is not finite reaches the outputs that see it, and no others.  T = 1 is the single-token form.  A call of T
- * steps and calls on its parts (each entering with the s_last before it) agree to rounding.
+ * What is not finite reaches the outputs that see it, and no others (a sequence that holds such values is taken again
+ * in fp32, which takes longer).  T = 1 is the single-token form.  A call of T steps and calls on its parts (each
+ * entering with the s_last before it) agree to rounding.
  * In bf16 the products of queries and keys, and the state as the queries read it, are rounded to bf16 as factors of
- * the tensor cores; sums and the state itself stay fp32. */
+ * the tensor cores (heads of up to 128 values and more than 12 tokens); sums stay fp32, and so does s_last. */
 wm_status wm_seq_decay_attention(wm_seq *h, int dtype, long long T, int N, int heads, int Dk, int Dv, const wm_seq_heads *q,
                                  const wm_seq_heads *k, const wm_seq_heads *v, const float *log_decay, float scale,
                                  const float *s0, const uint8_t *reset, const int32_t *lengths, const wm_seq_heads *out,
                                  float *s_last, void *cuda_stream);
 
 /* Its gradients.  q, k, v, log_decay, scale, s0, reset, lengths as in the forward call and
- *   dout     [T, N, heads, Dv] dtype: the gradient with respect to out, not read in padding
+ *   dout     [T, N, heads, Dv] dtype: the gradient with respect to out; padding may hold anything
  *   ds_last  [N, heads, Dk, Dv] fp32 dense or NULL: the gradient with respect to s_last
  *   dq, dk, dv  like q, k, v, out (0 in padding)
  *   ds0      [N, heads, Dk, Dv] fp32 dense, optional out; may be ds_last

@@ -564,6 +564,61 @@ def test_graph_capture(seq):
     ops.sync()
 
 
+def test_two_graphs_share_a_workspace(seq):
+    """Captured on one handle and replayed in turn: neither reads what the other left."""
+    ops = seq.SequenceOps()
+    a, b = (inputs(1500, 1, 2, D, D, torch.bfloat16, seed=85 + D) for D in (64, 128))
+
+    def calls(s):
+        return ops.decay_attention(s["q"], s["k"], s["v"], s["g"], s0=s["s0"]) + ops.decay_attention_backward(s["q"], s["k"], s["v"], s["g"], s["do"])
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        want = [calls(s) for s in (b, a)]
+    side.synchronize()
+    graphs, outs = [], []
+    for s in (b, a):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            outs.append(calls(s))
+        graphs.append(g)
+    for i in (0, 1, 1, 0, 1):
+        for v in outs[i]:
+            v.fill_(float("nan"))
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(outs[i], want[i]))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [11, 13, 20, 32, 33])
+def test_many_sequences_of_few_tokens(ops, dtype, T):
+    """Token by token, or in chunks: by type and by how many there are."""
+    check_all(ops, inputs(T, 110, 3, 16, 24, DT[dtype], seed=T, reset=True, lengths=True))
+
+
+def test_threads_take_turns(ops):
+    """Two threads on one handle: each call whole."""
+    import threading
+    s = inputs(300, 2, 2, 64, 64, torch.bfloat16, seed=33)
+    want = ops.decay_attention(s["q"], s["k"], s["v"], s["g"], s0=s["s0"])
+    bad = []
+
+    def work():
+        for _ in range(20):
+            got = ops.decay_attention(s["q"], s["k"], s["v"], s["g"], s0=s["s0"])
+            if not all(torch.equal(x, y) for x, y in zip(got, want)):
+                bad.append(1)
+
+    threads = [threading.Thread(target=work) for _ in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not bad
+
+
 def test_capture_needs_a_workspace(seq):
     ops = seq.SequenceOps()
     s = inputs(3000, 1, 1, 64, 64, torch.bfloat16, seed=83)
