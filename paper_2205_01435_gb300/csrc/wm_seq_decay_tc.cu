@@ -63,7 +63,7 @@ struct Plan {
     // both also hold the state on its way in and out)
     static constexpr int b = 0, lo = b + 2 * tile, xb = lo + tile, a = xb + tile, c = a + 2 * tile, end = c + tile;
     static constexpr int small = end;  // tables and barriers
-    static constexpr int bytes = small + 48 + 48;
+    static constexpr int notes = small + 96, bytes = notes + 128;
     // P lies over A: 16 tokens' column pairs where their warps read them, in blocks of `own` columns of A; with D = 64 O2, in two
     // halves, over the rest of each block
     static constexpr int own = 128 / (D / 32);
@@ -208,6 +208,10 @@ __device__ __forceinline__ bool state_out(const float4 *x, float *to, int da, in
         const int r = q.row0 + i * Q::rows, left = dc - 4 * q.k;
         if (r < da && left > 0) {
             float4 v = x[state_at<D>(r, q.k)];
+            if constexpr (D == 64) {
+                const float4 o = x[D * D / 4 + state_at<D>(r, q.k)];
+                v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
+            }
             odd += v.x * 0.f;  // (values beyond the state's may be what they like)
             if (left > 1) odd += v.y * 0.f;
             if (left > 2) odd += v.z * 0.f;
@@ -278,9 +282,10 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
     // A CTA takes items (a job of a head of a sequence, or of a span of it) one after the other.
     // (T is below 2^31 - 65536: tokens, and the ends of chunks and spans, are ints)
     struct Item {
-        int at, job, pair, n, head, span, len, first, last, stop, chunks;
-        bool rev;
+        int at, job, pair, n, head, span, len, first, last, stop, chunks, rev;
+        float g;
     };
+    volatile int *const notes = reinterpret_cast<volatile int *>(smem + L::notes);  // [2][16]: items that the issuing warp has opened
     const auto open = [&](int at) {
         Item m{};
         m.at = at;
@@ -300,6 +305,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
         m.head = m.pair - m.n * p.H;
         const decay_seq q = decay_open(p, p.job[m.job], m.n);
         m.rev = q.reverse;
+        m.g = p.log_decay[m.head];
         m.len = (int)q.len;
         m.first = (int)(m.span * p.span_tokens);
         m.last = (int)min(p.T, m.span * p.span_tokens + p.span_tokens);
@@ -325,6 +331,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             for (int i = 0; i < 6; ++i) tc::mbar_init(bars + 8 * i, 1);
             tc::fence_mbar_init();
             *late = 0;
+            notes[0] = notes[16] = -1;
         }
         __syncwarp();
         tc::fence_proxy_async_smem();
@@ -342,12 +349,25 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             float g;
             bool enters, fine;
         };
+        int opened = 0;
         const auto find = [&](Cursor &k, int at) {  // the first chunk of item `at`, or of the next one that has any
             for (;; at += gridDim.x) {
                 const Item m = open(at);
+                if (TMA && m.chunks > 0) {
+                    // for the workers, who are at the item before (and past the one before that, whose place this is): what opening it
+                    // takes, looks at memory among it, is done when they come to it
+                    if (lane == 0) {
+                        volatile int *const note = notes + (opened & 1) * 16;
+                        note[1] = m.job, note[2] = m.pair, note[3] = m.n, note[4] = m.head, note[5] = m.span, note[6] = m.len, note[7] = m.first;
+                        note[8] = m.last, note[9] = m.stop, note[10] = m.chunks, note[11] = m.rev, note[12] = __float_as_int(m.g);
+                        __threadfence_block();
+                        note[0] = m.at;
+                    }
+                    ++opened;
+                }
                 const decay_job &j = p.job[m.job];
                 k = {at, 0, m.chunks, begin_of(m, 0), m.rev ? -kChunk : kChunk, m.n, m.head, j.map[0] | j.map[1] << 2 | j.map[2] << 4,
-                     m.len - m.first - kChunk, at < items ? p.log_decay[m.head] : 0.f, !STATE && (p.spans > 1 || j.s_in), j.fine != 0};
+                     m.len - m.first - kChunk, m.g, !STATE && (p.spans > 1 || j.s_in), j.fine != 0};
                 if (m.chunks > 0 || at >= items) return;
             }
         };
@@ -453,7 +473,8 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 tc::mma_commit(barX);
             }
             __syncwarp();
-            step(now);
+            if constexpr (TMA) now = ahead;
+            else step(now);
             if (early && now.at < items) {
                 wait(barQK + 8 * (slot ^ 1), (done + 1) >> 1);
                 form_a(slot ^ 1);
@@ -468,12 +489,13 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
         const int xrow = quad * 32 + lane, group = warp >> 2, col0 = group * 32;
         float4 *const x = reinterpret_cast<float4 *>(smem + L::lo);  // a state on its way
         int done = 0;                                                // chunks
+        int taken = 0;                                               // items that had any
         Item m = open(blockIdx.x);
-        float g = p.log_decay[m.head];
         while (m.at < items) {
             const decay_job &j = p.job[m.job];
             const int da = j.da, dc = j.dc, len = m.len, first = m.first, last = m.last, stop = m.stop, chunks = m.chunks;
             const bool rev = m.rev;
+            const float g = m.g;
             const decay_seq q{p.T, len, rev};
             const int cells = da * dc;
             bf16 *const py = static_cast<bf16 *>(const_cast<void *>(j.y.p)) + m.n * j.y.n + m.head * j.y.h;
@@ -854,17 +876,24 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             bad = (odd & 0x7fff7fffu) != 0;  // (a product with 0 is 0 or NaN)
             if constexpr (!STATE) tma_store_read();
             if constexpr (!TMA) copy_wait<0>();
-            // the next item's marks, and its state on the way to L2, while this one's state leaves
-            const Item next = open(m.at + (int)gridDim.x);
-            float g_next = 0.f;
-            if (next.at < items) {
-                g_next = p.log_decay[next.head];
-                if constexpr (!STATE) {
-                    const decay_job &k = p.job[next.job];
-                    const float *const s = p.spans > 1 ? k.spans + (long long)next.span * pairs * cells : k.s_in;
-                    if (s && tid * 32 < cells)  // (a state is as large in every job)
-                        asm volatile("prefetch.global.L2 [%0];" ::"l"(s + (long long)next.pair * cells + tid * 32));
-                }
+            // the next item, as the issuing warp noted it (it notes none that is empty), and its state on the way to L2
+            taken += chunks > 0;
+            Item next{};
+            next.at = m.at + (int)gridDim.x;
+            if (TMA && notes[(taken & 1) * 16] == next.at) {
+                const volatile int *const note = notes + (taken & 1) * 16;
+                __threadfence_block();
+                next.job = note[1], next.pair = note[2], next.n = note[3], next.head = note[4], next.span = note[5], next.len = note[6];
+                next.first = note[7], next.last = note[8], next.stop = note[9], next.chunks = note[10], next.rev = note[11];
+                next.g = __int_as_float(note[12]);
+            } else {
+                next = open(next.at);
+            }
+            if (!STATE && next.at < items) {
+                const decay_job &k = p.job[next.job];
+                const float *const s = p.spans > 1 ? k.spans + (long long)next.span * pairs * cells : k.s_in;
+                if (s && tid * 32 < cells)  // (a state is as large in every job)
+                    asm volatile("prefetch.global.L2 [%0];" ::"l"(s + (long long)next.pair * cells + tid * 32));
             }
             // outputs of padding
             if (!STATE && max(first, stop) < last) {
@@ -887,26 +916,18 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 empty = j.out_zero && len > 0 && p.reset && p.reset[m.n] != 0;
             }
             if (chunks > 0) {
-#pragma unroll 1
-                for (int part = D == 64; part >= 0; --part) {  // D = 64: lanes 64 and up, then the others onto them
-                    if (D == 128 || (quad >= 2) == (part == 1)) {
-                        uint32_t r[32];
-                        TC_LD32(tmem + ((uint32_t)(quad * 32) << 16) + L::tX + col0, r);
-                        tc::tmem_ld_wait();
+                if (to) {  // by way of shared memory to whole rows; D = 64: lanes 64 and up beside the others, added there
+                    uint32_t r[32];
+                    TC_LD32(tmem + ((uint32_t)(quad * 32) << 16) + L::tX + col0, r);
+                    tc::tmem_ld_wait();
+                    float4 *const half = x + (D == 64 && quad >= 2 ? D * D / 4 : 0);
 #pragma unroll
-                        for (int i = 0; i < 32; i += 4) {
-                            float4 *const at = x + state_at<D>(xrow & (D - 1), (col0 + i) / 4);
-                            float4 v = make_float4(__uint_as_float(r[i]), __uint_as_float(r[i + 1]), __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
-                            if (D == 64 && part == 0) {
-                                const float4 o = *at;
-                                v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
-                            }
-                            *at = v;
-                        }
-                    }
+                    for (int i = 0; i < 32; i += 4)
+                        half[state_at<D>(xrow & (D - 1), (col0 + i) / 4)] =
+                            make_float4(__uint_as_float(r[i]), __uint_as_float(r[i + 1]), __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
                     worker_barrier<D>();
+                    bad |= state_out<D>(x, to, da, dc, empty);
                 }
-                bad |= state_out<D>(x, to, da, dc, empty);
                 if (bad) {
                     decay_mark(p, m.job, m.pair);
                     if constexpr (STATE)
@@ -921,7 +942,6 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             }
             done += chunks;
             m = next;
-            g = g_next;
             worker_barrier<D>();  // (tables and places are free)
         }
     }
