@@ -4,9 +4,9 @@
 // such CTAs an SM), 16 for up to 128, and one more that issues copies and products.  For each chunk
 //   A = a b^T                     128 x 128, both K-major as they lie in memory
 //   P = A * weights               TMEM -> registers -> TMEM as bf16, where the next product reads it
-//   O2 = a Xb                     Xb: the state X, fp32 in TMEM, as a bf16 tile
+//   O2 = a Xb                     Xb: the state X as a bf16 tile
 //   O1 = P c,  y = O1 + in_scale lambda^r O2
-//   X = lambda^n X + (b w)^T c    in place in TMEM; b w as three bf16 values, all 24 bits of it, where the state leaves and the chunk
+//   X = lambda^n X + (b w)^T c    X in fp32 in registers; b w as three bf16 values, all 24 bits of it, where the state leaves and the chunk
 //                                 still counts in it: it is as good as in fp32; else as two
 // a, b and c lie as [128 tokens][64 values] panels of 128-byte rows in the 128-byte swizzle, which serve as K-major operands
 // (a, b in A and O2) and as MN-major ones (c, and b transposed, where the tokens are summed over).  Rows come by asynchronous
@@ -32,19 +32,9 @@
                    "=r"((r)[24]), "=r"((r)[25]), "=r"((r)[26]), "=r"((r)[27]), "=r"((r)[28]), "=r"((r)[29]), "=r"((r)[30]), "=r"((r)[31]) \
                  : "r"((uint32_t)(taddr)))
 
-#define TC_ST32(taddr, r)                                                                                                        \
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "                                                                \
-                 "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" \
+#define TC_ST8(taddr, r)                                                                                                         \
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};"                                        \
                  ::"r"((r)[0]), "r"((r)[1]), "r"((r)[2]), "r"((r)[3]), "r"((r)[4]), "r"((r)[5]), "r"((r)[6]), "r"((r)[7]),         \
-                   "r"((r)[8]), "r"((r)[9]), "r"((r)[10]), "r"((r)[11]), "r"((r)[12]), "r"((r)[13]), "r"((r)[14]), "r"((r)[15]),   \
-                   "r"((r)[16]), "r"((r)[17]), "r"((r)[18]), "r"((r)[19]), "r"((r)[20]), "r"((r)[21]), "r"((r)[22]), "r"((r)[23]), \
-                   "r"((r)[24]), "r"((r)[25]), "r"((r)[26]), "r"((r)[27]), "r"((r)[28]), "r"((r)[29]), "r"((r)[30]), "r"((r)[31]), \
-                   "r"((uint32_t)(taddr)) : "memory")
-
-#define TC_ST16(taddr, r)                                                                                                        \
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};"         \
-                 ::"r"((r)[0]), "r"((r)[1]), "r"((r)[2]), "r"((r)[3]), "r"((r)[4]), "r"((r)[5]), "r"((r)[6]), "r"((r)[7]),         \
-                   "r"((r)[8]), "r"((r)[9]), "r"((r)[10]), "r"((r)[11]), "r"((r)[12]), "r"((r)[13]), "r"((r)[14]), "r"((r)[15]),   \
                    "r"((uint32_t)(taddr)) : "memory")
 
 namespace {
@@ -208,10 +198,6 @@ __device__ __forceinline__ bool state_out(const float4 *x, float *to, int da, in
         const int r = q.row0 + i * Q::rows, left = dc - 4 * q.k;
         if (r < da && left > 0) {
             float4 v = x[state_at<D>(r, q.k)];
-            if constexpr (D == 64) {
-                const float4 o = x[D * D / 4 + state_at<D>(r, q.k)];
-                v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
-            }
             odd += v.x * 0.f;  // (values beyond the state's may be what they like)
             if (left > 1) odd += v.y * 0.f;
             if (left > 2) odd += v.z * 0.f;
@@ -417,7 +403,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
         };
 #pragma unroll 1
         for (int done = 0; now.at < items; ++done) {  // chunks
-            const bool has_x = now.enters || now.c > 0, fresh = STATE && now.c == 0, fine = now.fine && in_three(now.g, now.left);
+            const bool has_x = now.enters || now.c > 0, fine = now.fine && in_three(now.g, now.left);
             const int slot = done & 1;
             const uint32_t ta = base + L::a + slot * L::tile, tb = base + L::b + slot * L::tile, tv = base + L::c;
             if (TMA && !(early && done > 0)) wait(barQK + 8 * slot, done >> 1);
@@ -456,9 +442,6 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             }
             take_over<D>(kReady);  // the keys' parts are there
             tc::fence_after_sync();
-            bool keeps_x = true;
-            if constexpr (CUT) keeps_x = (cuts[slot * 4] | cuts[slot * 4 + 1] | cuts[slot * 4 + 2] | cuts[slot * 4 + 3]) == 0;
-            const bool onto = (STATE ? !fresh : has_x) && keeps_x;
             if (tc::elect_one()) {
                 // (D = 64: two operands of 128 rows, the first two parts and half of the third twice)
                 const auto update = [&](uint32_t at, uint32_t panel, bool more) {
@@ -467,9 +450,10 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                         tc::mma_bf16(tmem + L::tX, desc_mn(at + k * 2048, panel), desc_mn(tv + k * 2048, kPanel),
                                      tc::idesc_bf16_f32(128, D) | kAmn | kBmn, more || k > 0);
                 };
-                update(tb, D == 128 ? kPanel : base + L::lo - tb, onto);
-                if (D == 128) update(base + L::lo, kPanel, true);
-                if (fine) update(base + L::xb, D == 128 ? kPanel : 0, true);
+                // the smallest first: what the tensor cores' sums lose, by cutting them off at 24 bits, is a part of what is there
+                if (fine) update(base + L::xb, D == 128 ? kPanel : 0, false);
+                if (D == 128) update(base + L::lo, kPanel, fine);
+                update(tb, D == 128 ? kPanel : base + L::lo - tb, fine || D == 128);
                 tc::mma_commit(barX);
             }
             __syncwarp();
@@ -547,33 +531,85 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             find_cuts(0);
             const float rate = fmaxf(g * 1.4426950408889634f, -1e4f), w_scale = j.w_scale, in_scale = j.in_scale, up_scale = j.up_scale;
             worker_barrier<D>();
-            // The entering state into TMEM: row a thread's lane, 32 columns a thread.  With D = 64 the state is the sum of lanes 0
-            // to 63 (sums of the keys' first parts) and 64 to 127 (of the second).
+            // The state, in registers: of row xr, columns xc and on.  The products of a chunk come by TMEM, fresh each time: the tensor
+            // cores' sums are cut off, not rounded, which a state that they ran on over a long sequence would feel (the state's
+            // gradient after 16,384 tokens of 8 heads of 128: 2e-7 off in the norm, by sums in place in TMEM 1e-6; that is what it
+            // costs: 479 -> 547 us backward there, 371 -> 389 at 1024 x 64 x 16 x 64).
+            constexpr int XN = D == 64 ? 16 : 32;
+            const int xr = D == 64 ? xrow & 63 : xrow, xc = col0 + (D == 64 && quad >= 2 ? 16 : 0);
+            float X[XN];
+#pragma unroll
+            for (int i = 0; i < XN; ++i) X[i] = 0.f;
             if (enters && chunks > 0) {
                 const float mul = p.spans == 1 && j.first ? decay_power(g, 1) : 1.f;
-                uint32_t r[32];
                 if (from_t) {  // (a row of the state is a column there: lanes read side by side)
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) r[i] = xrow < da && col0 + i < dc ? __float_as_uint(from[(col0 + i) * da + xrow]) : 0u;
+                    for (int i = 0; i < XN; ++i) X[i] = xr < da && xc + i < dc ? from[(xc + i) * da + xr] : 0.f;
                 } else {
                     state_in<D>(x, from, da, dc);
                     worker_barrier<D>();
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        const float4 v = x[state_at<D>(xrow & (D - 1), (col0 + i) / 4)];
-                        const bool on = xrow < D;
-                        r[i] = on ? __float_as_uint(v.x) : 0u, r[i + 1] = on ? __float_as_uint(v.y) : 0u;
-                        r[i + 2] = on ? __float_as_uint(v.z) : 0u, r[i + 3] = on ? __float_as_uint(v.w) : 0u;
+                    for (int i = 0; i < XN; i += 4) {
+                        const float4 v = x[state_at<D>(xr, (xc + i) / 4)];
+                        X[i] = v.x, X[i + 1] = v.y, X[i + 2] = v.z, X[i + 3] = v.w;
                     }
                 }
                 if (mul != 1.f) {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * mul);
+                    for (int i = 0; i < XN; ++i) X[i] *= mul;
                 }
-                __syncwarp();
-                TC_ST32(mine + L::tX + col0, r);
-                tmem_st_wait();
             }
+            // X <- shrink X (keep) + the last chunk's products.  D = 64: those are the sums of lanes 0 to 63 (of the keys' first parts) and
+            // 64 to 127 (of the second); two threads share a row's 32 columns and send each other what the other one adds, one by way of
+            // their own places in Xb, one by the places behind it.
+            const auto fold = [&](float shrink, bool keep) {
+                if constexpr (D == 128) {
+#pragma unroll
+                    for (int h = 0; h < 32; h += 16) {
+                        uint32_t r[16];
+                        __syncwarp();
+                        TC_LD16(mine + L::tX + col0 + h, r);
+                        tc::tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) X[h + i] = keep ? X[h + i] * shrink + __uint_as_float(r[i]) : __uint_as_float(r[i]);
+                    }
+                } else {
+                    uint32_t r[32];
+                    __syncwarp();
+                    TC_LD32(mine + L::tX + col0, r);
+                    tc::tmem_ld_wait();
+                    const uint32_t row = base + L::xb + xr * 128, far = base + L::xb + 8192 + (group * 64 + xr) * 64;
+                    const auto near_at = [&](int i) { return row + (((group * 4 + i / 4) ^ (xr & 7)) << 4); };
+                    const auto far_at = [&](int i) { return far + (((i / 4) ^ ((xr >> 1) & 3)) << 4); };
+                    const bool low = quad < 2;
+                    if (low) {
+#pragma unroll
+                        for (int i = 0; i < 16; i += 4)
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(far_at(i)), "r"(r[16 + i]), "r"(r[17 + i]), "r"(r[18 + i]), "r"(r[19 + i]) : "memory");
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; i += 4)
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(near_at(i)), "r"(r[i]), "r"(r[i + 1]), "r"(r[i + 2]), "r"(r[i + 3]) : "memory");
+                    }
+                    pair_barrier(1 + group * 2 + (quad & 1));
+                    uint32_t e[16];
+#pragma unroll
+                    for (int i = 0; i < 16; i += 4)
+                        asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(e[i]), "=r"(e[i + 1]), "=r"(e[i + 2]), "=r"(e[i + 3]) : "r"(low ? near_at(i) : far_at(i)) : "memory");
+                    if (!low) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) r[i] = r[16 + i];
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) + __uint_as_float(e[i]));
+                    pair_barrier(1 + group * 2 + (quad & 1));  // (both have read: Xb may take its place)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) X[i] = keep ? X[i] * shrink + __uint_as_float(r[i]) : __uint_as_float(r[i]);
+                }
+            };
+            const float whole = STATE ? 1.f : decay_power(g, kChunk);  // (STATE: weights up to the span's end)
+            bool kept = true;   // no cut in the last chunk
+            float shrink = 1.f;
             uint32_t odd = 0;  // two bf16: NaN once an output was not finite
             const int step = step_of(xrow);
 
@@ -611,126 +647,82 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 // (time's order, the last token of all: the state leaves as that token wrote it)
                 const int less = !STATE && j.first && s0 + rows == len ? 1 : 0;
                 if (STATE && TMA) wait(barQK + 8 * slot, phase >> 1);
+                if (c > 0) fold(whole, kept);
+                kept = keep_from < 0;
+                shrink = STATE ? 1.f : decay_power(g, rows - less);
+                if (STATE && c > 0) worker_barrier<D>();  // (what they sent each other is read: the third parts take its place)
                 constexpr int cols = 128 / (D / 32);  // of A, a thread
                 if constexpr (!STATE) {
-                    // X -> Xb, and X to what the next state keeps of it
-                    if (has_x) {
-                        const Pair shrink = twice(decay_power(g, rows - less));
-                        uint32_t r[32];
-                        const int row = D == 64 ? xrow & 63 : xrow;
-                        const uint32_t to = base + L::xb + (col0 / 64) * (D * 128) + row * 128;
-                        const auto place = [&](int i) { return to + ((((col0 % 64 + i) / 8) ^ (row & 7)) << 4); };
-                        TC_LD32(mine + L::tX + col0, r);
-                        tc::tmem_ld_wait();
-                        if constexpr (D == 64) {  // the second parts come by way of Xb's place
-                            if (quad >= 2) {
+                    if (has_x) {  // X -> Xb
+                        const uint32_t to = base + L::xb + (xc / 64) * (D * 128) + xr * 128;
 #pragma unroll
-                                for (int i = 0; i < 32; i += 8) {
-                                    const float *f = reinterpret_cast<const float *>(r + i);
-                                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(place(i)), "r"(pack2(f[0], f[1])), "r"(pack2(f[2], f[3])),
-                                                 "r"(pack2(f[4], f[5])), "r"(pack2(f[6], f[7])) : "memory");
-                                }
-                            }
-                            pair_barrier(1 + group * 2 + (quad & 1));
-                        }
-                        if (D == 128 || quad < 2) {
-                            uint32_t e[16];
-                            if constexpr (D == 64) {
-#pragma unroll
-                                for (int i = 0; i < 16; i += 4)
-                                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(e[i]), "=r"(e[i + 1]), "=r"(e[i + 2]), "=r"(e[i + 3]) : "r"(place(2 * i)) : "memory");
-                            }
-#pragma unroll
-                            for (int i = 0; i < 32; i += 8) {
-                                const float *f = reinterpret_cast<const float *>(r + i);
-                                float x[8];
-                                if constexpr (D == 64) {
-#pragma unroll
-                                    for (int m = 0; m < 4; ++m) {
-                                        x[2 * m] = f[2 * m] + __uint_as_float(e[i / 2 + m] << 16);
-                                        x[2 * m + 1] = f[2 * m + 1] + __uint_as_float(e[i / 2 + m] & 0xffff0000u);
-                                    }
-                                } else {
-#pragma unroll
-                                    for (int m = 0; m < 8; ++m) x[m] = f[m];
-                                }
-                                asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(place(i)), "r"(pack2(x[0], x[1])), "r"(pack2(x[2], x[3])),
-                                             "r"(pack2(x[4], x[5])), "r"(pack2(x[6], x[7])) : "memory");
-                            }
-                        }
-                        if (!CUT || keep_from < 0) {
-#pragma unroll
-                            for (int i = 0; i < 32; i += 2) {
-                                const Pair v = mul2(pair_of(r[i], r[i + 1]), shrink);
-                                r[i] = __float_as_uint(v.f.x);
-                                r[i + 1] = __float_as_uint(v.f.y);
-                            }
-                            __syncwarp();
-                            TC_ST32(mine + L::tX + col0, r);
-                        }
-                        tmem_st_wait();
+                        for (int i = 0; i < XN; i += 8)
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to + ((((xc % 64 + i) / 8) ^ (xr & 7)) << 4)), "r"(pack2(X[i], X[i + 1])),
+                                         "r"(pack2(X[i + 2], X[i + 3])), "r"(pack2(X[i + 4], X[i + 5])), "r"(pack2(X[i + 6], X[i + 7])) : "memory");
                     }
-                    // A -> P: row xrow, 32 columns at a time, P over columns that are read.  Weights lambda^away by products from the
-                    // nearest column on: up to 32 roundings of 2^-24, before one of 2^-8
+                    // A -> P: row xrow, 16 columns at a time, P over columns that are read.  Weights lambda^away by products from the
+                    // nearest column on: up to 16 roundings of 2^-24, before one of 2^-8
                     wait(barA, phase);
 #pragma unroll
-                    for (int h = 0; h < cols / 32; ++h) {
-                        const int block = group * (cols / 32) + h, j0 = block * 32;
-                        uint32_t v[32];
+                    for (int h = 0; h < cols / 16; ++h) {
+                        const int j0 = group * cols + h * 16, block = j0 / 32;
+                        uint32_t v[16];
                         if (rev ? block < quad : block > quad) {  // not seen
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) v[i] = 0u;
+                            for (int i = 0; i < 8; ++i) v[i] = 0u;
                         } else {
-                            TC_LD32(mine + L::tA + j0, v);
+                            TC_LD16(mine + L::tA + j0, v);
                             const float lambda = power_of(rate, 1);
+                            // (the weight of the column before the first of these, in the order they are taken)
+                            const int before = rev ? j0 - 1 - xrow : xrow - j0 - 16;
+                            float w = before >= 0 ? w_scale * power_of(rate, before) : 0.f;
                             const auto weigh = [&](int i, float a, float b) {
-                                const Pair w = mul2(pair_of(v[i], v[i + 1]), seq_pair_of(a, b));
-                                v[i] = __float_as_uint(w.f.x), v[i + 1] = __float_as_uint(w.f.y);
+                                const Pair t = mul2(pair_of(v[i], v[i + 1]), seq_pair_of(a, b));
+                                v[i] = __float_as_uint(t.f.x), v[i + 1] = __float_as_uint(t.f.y);
                             };
+                            tc::tmem_ld_wait();
                             if (block == quad) {  // columns behind the token itself are not seen, whatever they hold
-                                float w = 0.f;
-                                tc::tmem_ld_wait();
+                                const int own = lane - j0 % 32;
                                 if (!rev) {
 #pragma unroll
-                                    for (int i = 30; i >= 0; i -= 2) {
-                                        const float b = i + 1 == lane ? w_scale : w * lambda;
-                                        w = i == lane ? w_scale : b * lambda;
-                                        v[i + 1] = i + 1 <= lane ? v[i + 1] : 0u;
-                                        v[i] = i <= lane ? v[i] : 0u;
+                                    for (int i = 14; i >= 0; i -= 2) {
+                                        const float b = i + 1 == own ? w_scale : w * lambda;
+                                        w = i == own ? w_scale : b * lambda;
+                                        v[i + 1] = i + 1 <= own ? v[i + 1] : 0u;
+                                        v[i] = i <= own ? v[i] : 0u;
                                         weigh(i, w, b);
                                     }
                                 } else {
 #pragma unroll
-                                    for (int i = 0; i < 32; i += 2) {
-                                        const float a = i == lane ? w_scale : w * lambda;
-                                        w = i + 1 == lane ? w_scale : a * lambda;
-                                        v[i] = i >= lane ? v[i] : 0u;
-                                        v[i + 1] = i + 1 >= lane ? v[i + 1] : 0u;
+                                    for (int i = 0; i < 16; i += 2) {
+                                        const float a = i == own ? w_scale : w * lambda;
+                                        w = i + 1 == own ? w_scale : a * lambda;
+                                        v[i] = i >= own ? v[i] : 0u;
+                                        v[i + 1] = i + 1 >= own ? v[i + 1] : 0u;
                                         weigh(i, a, w);
                                     }
                                 }
                             } else {
-                                const float w = w_scale * power_of(rate, rev ? j0 - xrow : xrow - j0 - 31);
                                 const Pair lambda2 = twice(lambda * lambda);
+                                w *= lambda;
                                 Pair t = rev ? seq_pair_of(w, w * lambda) : seq_pair_of(w * lambda, w);
-                                tc::tmem_ld_wait();
                                 if (!rev) {
 #pragma unroll
-                                    for (int i = 30; i >= 0; i -= 2, t = mul2(t, lambda2)) weigh(i, t.f.x, t.f.y);
+                                    for (int i = 14; i >= 0; i -= 2, t = mul2(t, lambda2)) weigh(i, t.f.x, t.f.y);
                                 } else {
 #pragma unroll
-                                    for (int i = 0; i < 32; i += 2, t = mul2(t, lambda2)) weigh(i, t.f.x, t.f.y);
+                                    for (int i = 0; i < 16; i += 2, t = mul2(t, lambda2)) weigh(i, t.f.x, t.f.y);
                                 }
                             }
                             if (CUT && any_cut) {
 #pragma unroll
-                                for (int i = 0; i < 32; ++i) v[i] = step_of(j0 + i) >= begin ? v[i] : 0u;
+                                for (int i = 0; i < 16; ++i) v[i] = step_of(j0 + i) >= begin ? v[i] : 0u;
                             }
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) v[i] = pack2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+                            for (int i = 0; i < 8; ++i) v[i] = pack2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
                         }
                         __syncwarp();
-                        TC_ST16(mine + L::tA + group * cols + h * 16, v);
+                        TC_ST8(mine + L::tA + group * cols + h * 8, v);
                     }
                 }
                 if constexpr (!STATE) {
@@ -818,28 +810,35 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                     const uint32_t stage = ta + warp * 2048, own = stage + lane * 64, turn = (lane >> 1) & 3;
                     const Pair w = twice(in_scale * power_of(rate, step));
                     if (!fine || !has_x) wait(barO, phase);
-                    uint32_t o1[32];
-                    TC_LD32(mine + L::tO1 + col0, o1);
-                    if (has_x) {
-                        uint32_t o2[32];
-                        TC_LD32(mine + L::o2_at(group), o2);
-                        tc::tmem_ld_wait();
-                        if (sees) {
 #pragma unroll
-                            for (int i = 0; i < 32; i += 2) {
-                                const Pair v = fma2(pair_of(o2[i], o2[i + 1]), w, pair_of(o1[i], o1[i + 1]));
-                                o1[i] = __float_as_uint(v.f.x), o1[i + 1] = __float_as_uint(v.f.y);
+                    for (int h = 0; h < 32; h += 16) {
+                        uint32_t o1[16];
+                        __syncwarp();
+                        TC_LD16(mine + L::tO1 + col0 + h, o1);
+                        if (has_x) {
+                            uint32_t o2[16];
+                            TC_LD16(mine + L::o2_at(group) + h, o2);
+                            tc::tmem_ld_wait();
+                            if (sees) {
+#pragma unroll
+                                for (int i = 0; i < 16; i += 2) {
+                                    const Pair v = fma2(pair_of(o2[i], o2[i + 1]), w, pair_of(o1[i], o1[i + 1]));
+                                    o1[i] = __float_as_uint(v.f.x), o1[i + 1] = __float_as_uint(v.f.y);
+                                }
                             }
+                        } else {
+                            tc::tmem_ld_wait();
                         }
-                    } else {
-                        tc::tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            o1[i] = pack2(__uint_as_float(o1[2 * i]), __uint_as_float(o1[2 * i + 1]));
+                            if (step < rows) odd = hfma(o1[i], 0u, odd);
+                        }
+#pragma unroll
+                        for (int i = 0; i < 8; i += 4)
+                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(own + (((h / 8 + i / 4) ^ turn) << 4)), "r"(o1[i]), "r"(o1[i + 1]),
+                                         "r"(o1[i + 2]), "r"(o1[i + 3]) : "memory");
                     }
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o1[i] = pack2(__uint_as_float(o1[2 * i]), __uint_as_float(o1[2 * i + 1]));
-#pragma unroll
-                    for (int i = 0; i < 16; i += 4)
-                        asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(own + (((i / 4) ^ turn) << 4)), "r"(o1[i]), "r"(o1[i + 1]), "r"(o1[i + 2]),
-                                     "r"(o1[i + 3]) : "memory");
                     if (maps.stores && rows == kChunk) {
                         tc::fence_proxy_async_smem();
                         __syncwarp();
@@ -864,10 +863,6 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                                 }
                             }
                         }
-                    }
-                    if (step < rows) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) odd = hfma(o1[i], 0u, odd);
                     }
                 }
                 wait(barX, phase);
@@ -916,15 +911,10 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 empty = j.out_zero && len > 0 && p.reset && p.reset[m.n] != 0;
             }
             if (chunks > 0) {
-                if (to) {  // by way of shared memory to whole rows; D = 64: lanes 64 and up beside the others, added there
-                    uint32_t r[32];
-                    TC_LD32(tmem + ((uint32_t)(quad * 32) << 16) + L::tX + col0, r);
-                    tc::tmem_ld_wait();
-                    float4 *const half = x + (D == 64 && quad >= 2 ? D * D / 4 : 0);
+                if (to) {  // by way of shared memory to whole rows
+                    fold(shrink, kept);
 #pragma unroll
-                    for (int i = 0; i < 32; i += 4)
-                        half[state_at<D>(xrow & (D - 1), (col0 + i) / 4)] =
-                            make_float4(__uint_as_float(r[i]), __uint_as_float(r[i + 1]), __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
+                    for (int i = 0; i < XN; i += 4) x[state_at<D>(xr, (xc + i) / 4)] = make_float4(X[i], X[i + 1], X[i + 2], X[i + 3]);
                     worker_barrier<D>();
                     bad |= state_out<D>(x, to, da, dc, empty);
                 }

@@ -314,6 +314,24 @@ def test_same_bits_again(ops, dtype):
         assert all(torch.equal(x, y) for x, y in zip(r, runs[0]))
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("heads", [1, 304])
+def test_a_state_of_many_tokens(ops, D, heads):
+    """A state that forgets nothing, of 16,384 products that are all positive: what is lost on the way adds up.  Each chunk of 128
+    tokens is 24 sums of 16 products and the sum so far, each of the 17 off by less than the last place of it (2^-23 of a chunk's
+    state, of half of one in the mean of positive sums): 24 * 17 * 2^-24; adding the chunks up is 128 roundings of 2^-24 of half the
+    state in the mean; the products' factors are exact to 2^-24.  (With a head for every place of 152 processors the sequences are
+    not split.)"""
+    T = 16384
+    k = (0.5 + torch.rand(T, 1, 1, D, generator=torch.Generator().manual_seed(1))).bfloat16().cuda().expand(T, 1, heads, D)
+    v = (0.5 + torch.rand(T, 1, 1, D, generator=torch.Generator().manual_seed(2))).bfloat16().cuda().expand(T, 1, heads, D)
+    _, last = ops.decay_attention(k, k, v, torch.zeros(heads, device="cuda"))
+    value = torch.einsum("tk,tv->kv", k[:, 0, 0].double(), v[:, 0, 0].double())
+    off = float(((last[0].double() - value) / value).abs().max())
+    assert off <= (24 * 17 + 64 + 1) * 2.0 ** -24, off
+    ops.sync()
+
+
 def test_offsets_past_32_bits(ops):
     """A view of an array of more than 2^32 values."""
     T, N, H, D = 130, 2, 2, 64
