@@ -30,6 +30,10 @@ __device__ __forceinline__ float4 ld4(const float *p) { return *reinterpret_cast
 // thread's 4 x 4 outputs take 8 quads from shared memory and 32 instructions of two multiply-adds for 64 of them: c and the
 // weighted b are turned over on the way, the state is held as [values of c][values of a].  (128 x 128 x 8 x 64, forward: 205 us
 // with one multiply-add an instruction and rows read across.)
+// What bounds it (128 x 128 x 8 x 64: 135 us forward, 362 backward; 100 x 200 x 7 x 43 ragged 109 and 281): reads of shared memory
+// (57% of its cycles), instructions (50%) and multiply-adds (39%) together, at the 16 warps that two CTAs of 100 KB hold.  More warps
+// with smaller blocks read more: 512 threads of 4 x 2 outputs 152 and 422 us.  Taking both products with a's rows at once saves
+// reads, but not registers: 141 and 372.
 // A tile: rows of ld floats (a multiple of 32), the quads of row r turned by r & 7: 8 rows' quads of one column lie in 8 places.
 __device__ __forceinline__ int quad_at(int r, int quad, int ld) { return r * ld + ((quad ^ (r & 7)) << 2); }
 __device__ __forceinline__ int cell_at(int r, int c, int ld) { return quad_at(r, c >> 2, ld) + (c & 3); }
@@ -153,7 +157,9 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
     const ChunkTiles<LD> m(smem);
     const decay_seq q = decay_open(p, j, n);
     const float g = p.log_decay[head];
-    const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
+    // Rows 4 ty and on, columns tx and on by 16.  Later rows see more tokens: a quarter of the processor, which has warps w and w + 4,
+    // takes 8 rows of the first half and the 8 as far from the end (128 x 128 x 8 x 64: forward 141 -> 135 us, backward 381 -> 362).
+    const int tid = threadIdx.x, wy = tid & 128 ? 11 - (tid >> 5) : tid >> 5, tx = tid & 15, ty = wy * 2 + (tid >> 4 & 1);
     const long long pairs = (long long)p.N * p.H, cells = (long long)da * j.dc;
     const long long first = span * p.span_tokens, last = min(p.T, first + p.span_tokens);
     const int cblocks = (cols + 15) / 16;  // of 16 values of c

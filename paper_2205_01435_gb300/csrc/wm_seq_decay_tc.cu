@@ -16,6 +16,14 @@
 // Rounded to bf16: P (each weight of a value by at most 2^-8 of itself, as the output is) and Xb (the state as the queries see
 // it); A, O1, O2 and X are fp32.
 //
+// What bounds it: not the products (20% of the tensor cores' cycles for heads of 64, 35% for 128) nor memory, but
+// the chain copies - A - P - O1 - update that a chunk walks, each link with its latency, and the workers' instructions between them
+// (50% of the issue slots at 1024 x 64 x 16 x 64).  Hence two CTAs an SM where a head has up to 64 values (96 registers a thread are
+// all that 18 warps can have), hand-overs after which the workers go on, and chunks of 128: fewer would leave half of the tensor
+// cores' rows empty.  Times: 128 x 512 x 16 x 64 ragged forward 205 us (2.3 TB/s of the tokens that are there);
+// 1024 x 64 x 16 x 64 forward 152 us (3.5 TB/s), backward 389 (2.4 TB/s); 8192 x 2 x 8 x 128 forward 87; 65,536 x 1 x 8 x 128 x 64
+// forward 201, backward 547.
+//
 // Masked places hold zeros, and zero times what is not finite is NaN: a chunk whose outputs or state are not finite marks its
 // sequence, and the fp32 kernel, which skips what is masked, takes it again.
 #include <algorithm>
