@@ -20,9 +20,9 @@
 // the chain copies - A - P - O1 - update that a chunk walks, each link with its latency, and the workers' instructions between them
 // (50% of the issue slots at 1024 x 64 x 16 x 64).  Hence two CTAs an SM where a head has up to 64 values (96 registers a thread are
 // all that 18 warps can have), hand-overs after which the workers go on, and chunks of 128: fewer would leave half of the tensor
-// cores' rows empty.  Times: 128 x 512 x 16 x 64 ragged forward 205 us (2.3 TB/s of the tokens that are there);
-// 1024 x 64 x 16 x 64 forward 152 us (3.5 TB/s), backward 389 (2.4 TB/s); 8192 x 2 x 8 x 128 forward 87; 65,536 x 1 x 8 x 128 x 64
-// forward 201, backward 547.
+// cores' rows empty.  Times: 128 x 512 x 16 x 64 ragged forward 199 us (2.4 TB/s of the tokens that are there);
+// 1024 x 64 x 16 x 64 forward 150 us (3.6 TB/s), backward 359 (2.6 TB/s); 8192 x 2 x 8 x 128 forward 88; 65,536 x 1 x 8 x 128 x 64
+// forward 196, backward 542.
 //
 // Masked places hold zeros, and zero times what is not finite is NaN: a chunk whose outputs or state are not finite marks its
 // sequence, and the fp32 kernel, which skips what is masked, takes it again.
@@ -542,7 +542,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             // The state, in registers: of row xr, columns xc and on.  The products of a chunk come by TMEM, fresh each time: the tensor
             // cores' sums are cut off, not rounded, which a state that they ran on over a long sequence would feel (the state's
             // gradient after 16,384 tokens of 8 heads of 128: 2e-7 off in the norm, by sums in place in TMEM 1e-6; that is what it
-            // costs: 479 -> 547 us backward there, 371 -> 389 at 1024 x 64 x 16 x 64).
+            // costs: 479 -> 547 us backward there when it was built, 371 -> 389 at 1024 x 64 x 16 x 64).
             constexpr int XN = D == 64 ? 16 : 32;
             const int xr = D == 64 ? xrow & 63 : xrow, xc = col0 + (D == 64 && quad >= 2 ? 16 : 0);
             float X[XN];
@@ -615,9 +615,8 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                     for (int i = 0; i < 16; ++i) X[i] = keep ? X[i] * shrink + __uint_as_float(r[i]) : __uint_as_float(r[i]);
                 }
             };
-            const float whole = STATE ? 1.f : decay_power(g, kChunk);  // (STATE: weights up to the span's end)
-            bool kept = true;   // no cut in the last chunk
-            float shrink = 1.f;
+            bool kept = true;    // no cut in the last chunk
+            float shrink = 1.f;  // what the state keeps over it (STATE: weights are up to the span's end)
             uint32_t odd = 0;  // two bf16: NaN once an output was not finite
             const int step = step_of(xrow);
 
@@ -655,7 +654,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 // (time's order, the last token of all: the state leaves as that token wrote it)
                 const int less = !STATE && j.first && s0 + rows == len ? 1 : 0;
                 if (STATE && TMA) wait(barQK + 8 * slot, phase >> 1);
-                if (c > 0) fold(whole, kept);
+                if (c > 0) fold(shrink, kept);
                 kept = keep_from < 0;
                 shrink = STATE ? 1.f : decay_power(g, rows - less);
                 if (STATE && c > 0) worker_barrier<D>();  // (what they sent each other is read: the third parts take its place)
@@ -669,9 +668,10 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                                          "r"(pack2(X[i + 2], X[i + 3])), "r"(pack2(X[i + 4], X[i + 5])), "r"(pack2(X[i + 6], X[i + 7])) : "memory");
                     }
                     // A -> P: row xrow, 16 columns at a time, P over columns that are read.  Weights lambda^away by products from the
-                    // nearest column on: up to 16 roundings of 2^-24, before one of 2^-8
+                    // nearest column on: up to 16 roundings of 2^-24, before one of 2^-8.  (A loop, for the instructions' cache: 1024 x 64 x 16 x 64
+                    // backward 389 -> 359 us, unrolled against not; 65,536 x 1 x 8 x 128 x 64 forward 201 -> 196)
                     wait(barA, phase);
-#pragma unroll
+#pragma unroll 1
                     for (int h = 0; h < cols / 16; ++h) {
                         const int j0 = group * cols + h * 16, block = j0 / 32;
                         uint32_t v[16];
