@@ -599,18 +599,40 @@ decay_pass pass_of(const wm_seq *h, const seq_decay_args &a, bool backward) {
 
 int slices_of(int dc) { return (dc + kSlice - 1) / kSlice; }
 
-// Few sequences are cut in time so that every SM has the CTAs it can hold, into spans of at least 4 chunks: with fewer the two
-// reads of keys and values that forming the states takes cost more than the SMs they would fill.
+// Few sequences are cut into spans of time, of at least 4 chunks, as many as take the least time by this count.  A launch takes
+// (chunks of a span + what opening and leaving one takes) for each round of CTAs that the SMs hold, in fp32 0.6 of it for a last
+// round of one CTA an SM where two fit; with spans the launch that forms their states comes on top, at 0.57 of a pass (0.4 in fp32).
+// Measured, us, spans in brackets, the chosen one first.  bf16: 65,536 x 1 x 8 x 128 x 64, forward 198 (19), 460 (6), 213 (38), backward
+// 432 (19), 480 (6), 470 (38); 8192 x 4 x 16 x 64, forward 135 (4), 202 (1), 137 (8), backward 254 (1), 282 (3); 16,384 x 1 x 16 x 64,
+// backward 149 (19), 153 (6), 165 (12).  fp32: 4096 x 24 x 8 x 64, forward 981 (3), 1073 (1), 1020 (8), backward 2104 (1), 2575 (3);
+// 8192 x 1 x 4 x 128, forward 195 (19), 232 (32), backward 481 (19), 535 (12).
 void split(const wm_seq *h, decay_pass &p, const seq_decay_args &a, bool tc) {
-    long long ctas = 0;
-    for (int i = 0; i < p.jobs; ++i) ctas += tc ? 1 : slices_of(p.job[i].dc);
+    long long ctas = 0, state_ctas = 0;
+    int da = 0;
+    for (int i = 0; i < p.jobs; ++i) {
+        const int n = tc ? 1 : slices_of(p.job[i].dc);
+        ctas += n;
+        if (!p.job[i].spans_t) state_ctas += n;
+        da = std::max(da, p.job[i].da);
+    }
     ctas *= (long long)p.N * p.H;
-    const int chunk = tc ? kDecayTcChunk : kChunk, room = h->sms * (tc ? wm_seq_decay_tc_ctas(a.Dk, a.Dv) : 2);
-    const long long chunks = (p.T + chunk - 1) / chunk;
-    const long long spans = std::max(1ll, std::min({room / std::max(1ll, ctas), chunks / 4, 65535ll}));
-    const long long per = std::max(1ll, (chunks + spans - 1) / spans);
+    state_ctas *= (long long)p.N * p.H;
+    const int chunk = tc ? kDecayTcChunk : kChunk, held = tc ? wm_seq_decay_tc_ctas(a.Dk, a.Dv) : da <= 64 ? 2 : 1, room = h->sms * held;
+    const double opening = tc ? 2.0 : 0.5, of_a_pass = tc ? 0.57 : 0.4;
+    const auto rounds = [&](long long n) {
+        const long long rest = n % room;
+        return (double)(n / room) + (rest == 0 ? 0.0 : !tc && held == 2 && rest <= h->sms ? 0.6 : 1.0);
+    };
+    const long long chunks = (p.T + chunk - 1) / chunk, most = std::min({chunks / 4, 4 * room / std::max(1ll, ctas) + 1, 65535ll});
+    long long spans = 1, per = std::max(1ll, chunks);
+    double least = rounds(ctas) * (double)(chunks + opening);
+    for (long long s = 2; s <= most; ++s) {
+        const long long chunks_of = (chunks + s - 1) / s, n = (chunks + chunks_of - 1) / chunks_of;
+        const double time = (rounds(ctas * n) + of_a_pass * rounds(state_ctas * n)) * ((double)chunks_of + opening);
+        if (time < least) least = time, spans = n, per = chunks_of;
+    }
     p.span_tokens = per * chunk;
-    p.spans = (int)std::max(1ll, (chunks + per - 1) / per);
+    p.spans = (int)spans;
 }
 
 // Tensor cores: bf16, heads of up to 128 values.

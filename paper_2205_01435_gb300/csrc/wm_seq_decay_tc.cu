@@ -22,7 +22,7 @@
 // all that 18 warps can have), hand-overs after which the workers go on, and chunks of 128: fewer would leave half of the tensor
 // cores' rows empty.  Times: 128 x 512 x 16 x 64 ragged forward 199 us (2.4 TB/s of the tokens that are there);
 // 1024 x 64 x 16 x 64 forward 150 us (3.6 TB/s), backward 359 (2.6 TB/s); 8192 x 2 x 8 x 128 forward 88; 65,536 x 1 x 8 x 128 x 64
-// forward 196, backward 542.
+// forward 196, backward 470.
 //
 // Masked places hold zeros, and zero times what is not finite is NaN: a chunk whose outputs or state are not finite marks its
 // sequence, and the fp32 kernel, which skips what is masked, takes it again.

@@ -332,6 +332,28 @@ def test_a_state_of_many_tokens(ops, D, heads):
     ops.sync()
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_split_into_more_spans_than_run_at_once(ops, dtype):
+    """The gradients of 16 heads of 16,384 tokens, and of the same sequence twenty times over, which are too many to split: each is as
+    far from the exact value as near() allows, so that the two are apart by at most twice that."""
+    T, H, D = 16384, 16, 64
+    s = inputs(T, 1, H, D, D, DT[dtype], seed=40, reset=True)
+    one = lambda v: v
+    many = lambda v: None if v is None else v.expand(-1, 20, *v.shape[2:]) if v.shape[0] == T else v.expand(20, *v.shape[1:]).contiguous()
+    results = []
+    for of in (one, many):
+        m = {key: of(s[key]) for key in ("q", "k", "v", "do", "s0", "ds_last")}
+        reset = of(s["reset"]).contiguous()
+        o, last = ops.decay_attention(m["q"], m["k"], m["v"], s["g"], scale=s["scale"], s0=m["s0"], reset=reset)
+        dq, dk, dv, ds0 = ops.decay_attention_backward(m["q"], m["k"], m["v"], s["g"], m["do"], scale=s["scale"], s0=m["s0"], reset=reset,
+                                                       ds_last=m["ds_last"])
+        results.append([o[:, 19 if of is many else 0], dq[:, -1], dk[:, -1], dv[:, -1], last[-1], ds0[-1]])
+    for name, a, b in zip(("o", "dq", "dk", "dv", "s_last", "ds0"), *results):
+        off = float((a.double() - b.double()).norm() / b.double().norm())
+        assert off <= 2 * (1.25 * 2.0 ** -8 if a.dtype == torch.bfloat16 else 32 * ref.U), f"{name}: {off}"
+    ops.sync()
+
+
 def test_offsets_past_32_bits(ops):
     """A view of an array of more than 2^32 values."""
     T, N, H, D = 130, 2, 2, 64
