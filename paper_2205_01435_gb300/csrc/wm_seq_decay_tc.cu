@@ -20,9 +20,9 @@
 // the chain copies - A - P - O1 - update that a chunk walks, each link with its latency, and the workers' instructions between them
 // (50% of the issue slots at 1024 x 64 x 16 x 64).  Hence two CTAs an SM where a head has up to 64 values (96 registers a thread are
 // all that 18 warps can have), hand-overs after which the workers go on, and chunks of 128: fewer would leave half of the tensor
-// cores' rows empty.  Times: 128 x 512 x 16 x 64 ragged forward 199 us (2.4 TB/s of the tokens that are there);
-// 1024 x 64 x 16 x 64 forward 150 us (3.6 TB/s), backward 359 (2.6 TB/s); 8192 x 2 x 8 x 128 forward 88; 65,536 x 1 x 8 x 128 x 64
-// forward 196, backward 470.
+// cores' rows empty.  Times: 128 x 512 x 16 x 64 ragged forward 193 us (2.4 TB/s of the tokens that are there);
+// 1024 x 64 x 16 x 64 forward 146 us (3.7 TB/s), backward 353 (2.7 TB/s); 8192 x 2 x 8 x 128 forward 86; 65,536 x 1 x 8 x 128 x 64
+// forward 201, backward 479.
 //
 // Masked places hold zeros, and zero times what is not finite is NaN: a chunk whose outputs or state are not finite marks its
 // sequence, and the fp32 kernel, which skips what is masked, takes it again.
@@ -659,6 +659,9 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 shrink = STATE ? 1.f : decay_power(g, rows - less);
                 if (STATE && c > 0) worker_barrier<D>();  // (what they sent each other is read: the third parts take its place)
                 constexpr int cols = 128 / (D / 32);  // of A, a thread
+                // Is any of the warp's 32 rows there?  (Those that are not keep what A left, which reaches no row but their own.
+                // 128 x 512 x 16 x 64 ragged 199 -> 193 us, 65,536 x 1 x 8 x 128 x 64 forward 196 -> 201, for its spilled registers.)
+                const bool live = rev ? quad * 32 + 32 > kChunk - rows : quad * 32 < rows;
                 if constexpr (!STATE) {
                     if (has_x) {  // X -> Xb
                         const uint32_t to = base + L::xb + (xc / 64) * (D * 128) + xr * 128;
@@ -672,7 +675,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                     // backward 389 -> 359 us, unrolled against not; 65,536 x 1 x 8 x 128 x 64 forward 201 -> 196)
                     wait(barA, phase);
 #pragma unroll 1
-                    for (int h = 0; h < cols / 16; ++h) {
+                    for (int h = 0; h < (live ? cols / 16 : 0); ++h) {
                         const int j0 = group * cols + h * 16, block = j0 / 32;
                         uint32_t v[16];
                         if (rev ? block < quad : block > quad) {  // not seen
@@ -819,7 +822,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                     const Pair w = twice(in_scale * power_of(rate, step));
                     if (!fine || !has_x) wait(barO, phase);
 #pragma unroll
-                    for (int h = 0; h < 32; h += 16) {
+                    for (int h = 0; h < (live ? 32 : 0); h += 16) {
                         uint32_t o1[16];
                         __syncwarp();
                         TC_LD16(mine + L::tO1 + col0 + h, o1);
@@ -851,7 +854,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                         tc::fence_proxy_async_smem();
                         __syncwarp();
                         if (lane == 0 && col0 < dc) tma_store_4d(&maps.out[m.job], stage, col0, t0 + quad * 32, m.n, m.head);
-                    } else {
+                    } else if (live) {
                         __syncwarp();
                         const int left = dc - col0 - lane % 4 * 8;
 #pragma unroll 1
