@@ -561,6 +561,9 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                         const float4 v = x[state_at<D>(xr, (xc + i) / 4)];
                         X[i] = v.x, X[i + 1] = v.y, X[i + 2] = v.z, X[i + 3] = v.w;
                     }
+                    // (all have read it: with D = 128 the state lies over lo and xb, and xb is written before the workers meet again,
+                    // lo after a product that may have been formed ahead; where there are cuts to find they meet at the chunk's head)
+                    if constexpr (D == 128 && TMA && !CUT) worker_barrier<D>();
                 }
                 if (mul != 1.f) {
 #pragma unroll

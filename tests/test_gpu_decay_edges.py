@@ -1,0 +1,50 @@
+"""Decayed linear attention: what runs side by side in its kernels, states at the edge of their precision, decays and values that
+are not finite, waits that give up, calls that are refused."""
+import pytest
+import torch
+
+import decay_reference as ref
+from seq_reference import check
+from test_gpu_decay import DT, decays, inputs, masks, near, ops, rnd, seq  # noqa: F401  (fixtures among them)
+
+pytestmark = pytest.mark.gpu
+
+
+def both_ways(ops, s):
+    """Outputs and gradients of a call, by name."""
+    o, last = ops.decay_attention(s["q"], s["k"], s["v"], s["g"], scale=s["scale"], **masks(s))
+    g = ops.decay_attention_backward(s["q"], s["k"], s["v"], s["g"], s["do"], scale=s["scale"], ds_last=s["ds_last"], **masks(s))
+    return dict(zip(("o", "s_last", "dq", "dk", "dv", "ds0"), (o, last, *g)))
+
+
+def copies(s, n):
+    """The same sequence n times over (N = 1)."""
+    out = dict(s)
+    for key in ("q", "k", "v", "do"):
+        out[key] = s[key].expand(-1, n, -1, -1).contiguous()
+    for key in ("s0", "ds_last"):
+        out[key] = s[key].expand(n, -1, -1, -1).contiguous()
+    return out
+
+
+# ------------------------------------------------------------------ side by side
+@pytest.mark.parametrize("T,H,Dk,Dv,n", [(130, 8, 128, 128, 60), (13, 8, 128, 128, 60), (300, 4, 128, 64, 100), (200, 4, 72, 128, 100),
+                                         (1100, 2, 128, 128, 1), (2600, 1, 96, 128, 1)])
+def test_wide_heads_take_their_states_whole(ops, T, H, Dk, Dv, n):
+    """States of more than 64 values that enter without resets, more heads of sequences than run at once or spans of time: each copy of
+    a sequence, and each call again, gives the same bits, and what the definition gives."""
+    s = inputs(T, 1, H, Dk, Dv, torch.bfloat16, seed=T)
+    got = both_ways(ops, copies(s, n))
+    f = ref.attend(s["q"], s["k"], s["v"], s["g"], s["scale"], **masks(s))
+    b = ref.attend_backward(s["q"], s["k"], s["v"], s["g"], s["scale"], s["do"], s["ds_last"], **masks(s))
+    for name, value in got.items():
+        axis = 0 if name in ("s_last", "ds0") else 1
+        first = value.narrow(axis, 0, 1)
+        assert torch.equal(value, first.expand_as(value)), name
+        check(first, *{**f, **b}[name], name)
+        near(first, {**f, **b}[name][0], name, value.dtype)
+    for _ in range(3 if n > 1 else 12):
+        again = both_ways(ops, copies(s, n))
+        for name, value in got.items():
+            assert torch.equal(value, again[name]), name
+    ops.sync()
