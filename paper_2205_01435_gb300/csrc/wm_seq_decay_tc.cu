@@ -770,6 +770,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                     const int ch = tid % per, row0 = tid / per;
                     const uint32_t off = (ch / 8) * kPanel + row0 * 128 + (((ch & 7) ^ (row0 & 7)) << 4);
                     uint32_t v[turns][4];
+                    if (TMA && !STATE) wait(barQK + 8 * slot, phase >> 1);  // (over since A was formed; but it is this wait that shows a thread the copies)
 #pragma unroll
                     for (int k = 0; k < turns; ++k)
                         asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v[k][0]), "=r"(v[k][1]), "=r"(v[k][2]), "=r"(v[k][3]) : "r"(tb + off + k * stride * 128) : "memory");

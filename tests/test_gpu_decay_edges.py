@@ -48,3 +48,28 @@ def test_wide_heads_take_their_states_whole(ops, T, H, Dk, Dv, n):
         for name, value in got.items():
             assert torch.equal(value, again[name]), name
     ops.sync()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("T,state", [(14, False), (128, True), (257, False)])
+def test_keys_are_there_when_they_are_weighted(ops, D, T, state):
+    """Items of one to three chunks, one after the other on each processor: what the keys give the states (and, by them, the outputs)
+    is the same in each copy of a sequence and in each call, and what the definition gives."""
+    s = inputs(T, 1, 4, D, D, torch.bfloat16, seed=100 + T, state=state)
+    if not state:
+        s["s0"] = s["ds_last"] = torch.zeros(1, 4, D, D, device="cuda")
+    c = copies(s, 300)
+    if not state:
+        for v in (s, c):
+            v["s0"] = v["ds_last"] = None
+    got = both_ways(ops, c)
+    f = ref.attend(s["q"], s["k"], s["v"], s["g"], s["scale"], **masks(s))
+    b = ref.attend_backward(s["q"], s["k"], s["v"], s["g"], s["scale"], s["do"], s["ds_last"], **masks(s))
+    for name, value in got.items():
+        first = value.narrow(0 if name in ("s_last", "ds0") else 1, 0, 1)
+        assert torch.equal(value, first.expand_as(value)), name
+        check(first, *{**f, **b}[name], name)
+        near(first, {**f, **b}[name][0], name, value.dtype)
+    again = both_ways(ops, c)
+    assert all(torch.equal(v, again[name]) for name, v in got.items())
+    ops.sync()
