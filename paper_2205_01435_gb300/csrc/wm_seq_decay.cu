@@ -445,7 +445,9 @@ struct StepArgs {
 
 template <class T, int ROWS, bool VEC>
 __global__ void __launch_bounds__(256, ROWS <= 4 ? 6 : ROWS <= 8 ? 4 : 2) decay_step_kernel(const __grid_constant__ StepArgs p) {
-    __shared__ float q[256], k[256], v[64];
+    __shared__ float4 quads[16];  // of the values, which are read four at a time
+    __shared__ float q[256], k[256];
+    float *const v = reinterpret_cast<float *>(quads);
     __shared__ float part[8][64];
     const int item = (int)blockIdx.x, at_pair = p.slices == 1 ? item : item / p.slices, slice = item - at_pair * p.slices;  // (below 2^30)
     const int n = at_pair / p.H, head = at_pair - n * p.H, tid = threadIdx.x;
@@ -494,7 +496,7 @@ __global__ void __launch_bounds__(256, ROWS <= 4 ? 6 : ROWS <= 8 ? 4 : 2) decay_
             v[tid] = col0 + tid < p.Dv ? seq_to_float(static_cast<const T *>(p.v.p)[t * p.v.t + n * p.v.n + head * p.v.h + col0 + tid]) : 0.f;
         const bool cut = p.reset && p.reset[(long long)t * p.N + n];
         __syncthreads();
-        const float4 w = ld4(v + cg * 4);
+        const float4 w = quads[cg];
         float y[4] = {};
 #pragma unroll
         for (int i = 0; i < ROWS; ++i) {

@@ -73,3 +73,17 @@ def test_keys_are_there_when_they_are_weighted(ops, D, T, state):
     again = both_ways(ops, c)
     assert all(torch.equal(v, again[name]) for name, v in got.items())
     ops.sync()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("N,Dk,Dv", [(1, 1, 1), (2, 3, 5), (3, 43, 43), (1, 256, 31), (2, 33, 64), (200, 20, 66), (400, 64, 72), (1, 7, 256)])
+def test_steps_of_any_width(ops, dtype, N, Dk, Dv):
+    """Single tokens whose values fill a CTA's columns in part, 32 and 64 columns wide, with the state in place."""
+    s = inputs(3, N, 2, Dk, Dv, DT[dtype], seed=Dk + Dv)
+    f = ref.attend(s["q"], s["k"], s["v"], s["g"], s["scale"], s["s0"], factors=False)
+    state = s["s0"].clone()
+    for t in range(3):
+        o, _ = ops.decay_step(s["q"][t], s["k"][t], s["v"][t], s["g"], state, scale=s["scale"], out_state=state)
+        check(o, f["o"][0][t], f["o"][1][t], "o")
+    check(state, *f["s_last"], "state")
+    ops.sync()
