@@ -730,11 +730,16 @@ cudaError_t run_pass(wm_seq *h, const seq_decay_args &a, decay_pass &p, bool tc,
     const long long pairs = (long long)p.N * p.H;
     cudaError_t e;
     decay_maps maps;
-    if (tc) wm_seq_decay_tc_maps(a, p, maps);
+    if (tc) {
+        wm_seq_decay_tc_maps(a, p, maps);
+        p.test_wait = h->test_wait;  // (an injected wait goes to the call's first such launch)
+        h->test_wait = 0;
+    }
     if (tc && (e = cudaMemsetAsync(p.redo, 0, (size_t)(1 + p.jobs * pairs) * 4, s)) != cudaSuccess) return e;
     if (p.spans > 1) {
         e = tc ? wm_seq_decay_tc_launch(h, p, maps, true, s) : chunk_launch<T, true>(h, p, s);
         if (e != cudaSuccess) return e;
+        p.test_wait = 0;
         const long long cells = pairs * a.Dk * a.Dv;
         ++h->last_launches;
         if ((long long)a.Dk * a.Dv % 4 == 0) decay_join_kernel<4><<<dim3((unsigned)((cells / 4 + 255) / 256), p.jobs), 256, 0, s>>>(p);

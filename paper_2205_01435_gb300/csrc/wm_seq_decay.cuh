@@ -45,6 +45,7 @@ struct decay_pass {
     long long span_tokens;   // a multiple of the chunk
     int *redo;               // tensor-core pass: how many marks, then [jobs][N, H] marks: a chunk met what is not finite
     int only_redo;           // work on those alone
+    uint32_t test_wait;      // > 0: the tensor-core pass's first CTA polls, that often, what nothing sets
 };
 
 // The tensor-core pass in bf16 (wm_seq_decay_tc.cu): its launch (state: only what the spans' tokens give the state), and the

@@ -61,7 +61,7 @@ struct Plan {
     // both also hold the state on its way in and out)
     static constexpr int b = 0, lo = b + 2 * tile, xb = lo + tile, a = xb + tile, c = a + 2 * tile, end = c + tile;
     static constexpr int small = end;  // tables and barriers
-    static constexpr int notes = small + 96, bytes = notes + 128;
+    static constexpr int notes = small + 112, bytes = notes + 128;
     // P lies over A: 16 tokens' column pairs where their warps read them, in blocks of `own` columns of A; with D = 64 O2, in two
     // halves, over the rest of each block
     static constexpr int own = 128 / (D / 32);
@@ -239,7 +239,7 @@ __device__ __forceinline__ float power_of(float rate, int n) {
 }
 
 // What the workers hand to the issuing warp: they arrive and go on, it waits.  (No worker arrives twice before it has waited:
-// in between each waits for a product that was issued after.)
+// in between each waits for a product that was issued after, or, where a wait gave up, for the issuing warp's count of chunks.)
 enum { kRead = 6, kScaled = 7, kWeighted = 8, kReady = 9 };
 template <int D>
 __device__ __forceinline__ void hand_over(int id) {
@@ -264,7 +264,9 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
     uint32_t *const cuts = reinterpret_cast<uint32_t *>(smem + L::small);    // [2][4]: tokens that begin something new
     volatile int *const late = reinterpret_cast<int *>(cuts + 8);           // a wait gave up
     uint32_t *const tmem_at = cuts + 9;
-    const uint32_t bars = tc::smem_u32(cuts + 12), barA = bars, barO = bars + 8, barX = bars + 16, barV = bars + 24, barQK = bars + 32;
+    volatile int *const passed = reinterpret_cast<int *>(cuts + 10);         // chunks of which the issuing warp took over all that is handed over
+    const uint32_t bars = tc::smem_u32(cuts + 12), barA = bars, barO = bars + 8, barX = bars + 16, barV = bars + 24, barQK = bars + 32,
+                   barEnd = bars + 48;
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, quad = warp & 3;
     const bool worker = tid < L::workers;
@@ -310,21 +312,27 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
     // Row r of a chunk's tiles is token begin_of(c) + r; counted along the pass it is step step_of(r) of the chunk.
     const auto begin_of = [](const Item &m, int c) { return m.rev ? m.len - m.first - (c + 1) * kChunk : m.first + c * kChunk; };
 
+    // Once a wait has given up, here or in another warp, those after it look once: the CTA walks to its end with what there is.
+    // Its warps stay in step (see in_step), nothing more is issued, and what was is waited for at the end.
     const auto wait = [&](uint32_t bar, int phase) {
+        bool there = true;
         for (uint32_t i = 0; !tc::mbar_try_wait(bar, (uint32_t)phase & 1u); ++i) {
-            if (*late || i == kWait) {  // (what follows goes on with what there is)
+            if (*late || i == kWait) {
                 *late = 1;
                 seq_record(p.status + 1, WM_ERR_TIMEOUT);
+                there = false;
                 break;
             }
         }
         tc::fence_after_sync();
+        return there;
     };
+    int asked_ab = 0, asked_c = 0;  // chunks whose copies the issuing warp asked for
     if (!worker) {
         if (tc::elect_one()) {
-            for (int i = 0; i < 6; ++i) tc::mbar_init(bars + 8 * i, 1);
+            for (int i = 0; i < 7; ++i) tc::mbar_init(bars + 8 * i, 1);
             tc::fence_mbar_init();
-            *late = 0;
+            *late = *passed = 0;
             notes[0] = notes[16] = -1;
         }
         __syncwarp();
@@ -344,6 +352,8 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             bool enters, fine;
         };
         int opened = 0;
+        bool goes = true;  // no wait of this warp has given up: what it issues finds its operands, and its barriers in step
+        const auto await = [&](uint32_t bar, int phase) { goes = __all_sync(~0u, wait(bar, phase)) && goes; };
         const auto find = [&](Cursor &k, int at) {  // the first chunk of item `at`, or of the next one that has any
             for (;; at += gridDim.x) {
                 const Item m = open(at);
@@ -375,7 +385,9 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             for (int i = 0; i < D / 64; ++i) tma_load_4d(dst + i * kPanel, &maps.in[map], i * 64, k.t0, k.n, k.head, bar);
         };
         const auto load_ab = [&](const Cursor &k, int slot) {  // keys, and queries
-            if (k.at < items && tc::elect_one()) {
+            if (k.at >= items || !goes) return;
+            ++asked_ab;
+            if (tc::elect_one()) {
                 tc::mbar_arrive_expect_tx(barQK + 8 * slot, (STATE ? 1 : 2) * L::tile);
                 load(k, base + L::b + slot * L::tile, k.maps >> 2 & 3, barQK + 8 * slot);
                 if constexpr (!STATE) load(k, base + L::a + slot * L::tile, k.maps & 3, barQK + 8 * slot);
@@ -383,7 +395,9 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             __syncwarp();
         };
         const auto load_c = [&](const Cursor &k) {
-            if (k.at < items && tc::elect_one()) {
+            if (k.at >= items || !goes) return;
+            ++asked_c;
+            if (tc::elect_one()) {
                 tc::mbar_arrive_expect_tx(barV, L::tile);
                 load(k, base + L::c, k.maps >> 4, barV);
             }
@@ -400,7 +414,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
         }
         const auto form_a = [&](int slot) {
             const uint32_t ta = base + L::a + slot * L::tile, tb = base + L::b + slot * L::tile;
-            if (tc::elect_one()) {
+            if (goes && tc::elect_one()) {
 #pragma unroll
                 for (int k = 0; k < D / 16; ++k)
                     tc::mma_bf16(tmem + L::tA, tc::desc_sw128(ta + (k / 4) * kPanel + (k % 4) * 32), tc::desc_sw128(tb + (k / 4) * kPanel + (k % 4) * 32),
@@ -409,12 +423,22 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             }
             __syncwarp();
         };
+        const auto test = [&]() {  // (a test's wait, for what nothing sets)
+            if (!p.test_wait || blockIdx.x != 0) return;
+            if (!tc::mbar_wait_bounded(barEnd, 0, p.test_wait)) {
+                *late = 1;
+                seq_record(p.status + 1, WM_ERR_TIMEOUT);
+            }
+            goes = false;
+        };
+        if (now.at >= items) test();
 #pragma unroll 1
         for (int done = 0; now.at < items; ++done) {  // chunks
             const bool has_x = now.enters || now.c > 0, fine = now.fine && in_three(now.g, now.left);
             const int slot = done & 1;
             const uint32_t ta = base + L::a + slot * L::tile, tb = base + L::b + slot * L::tile, tv = base + L::c;
-            if (TMA && !(early && done > 0)) wait(barQK + 8 * slot, done >> 1);
+            if (done == (TMA && ahead.at < items ? 1 : 0)) test();  // (where there is a second chunk, with copies and products on their way)
+            if (TMA && !(early && done > 0)) await(barQK + 8 * slot, done >> 1);
             take_over<D>(kRead);  // the chunk before is read out
             tc::fence_after_sync();
             if (!STATE && !(early && done > 0)) form_a(slot);
@@ -426,7 +450,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 take_over<D>(kScaled);  // A is read, Xb there
                 tc::fence_after_sync();
             }
-            if (!STATE && has_x && tc::elect_one()) {
+            if (!STATE && has_x && goes && tc::elect_one()) {
                 constexpr int parts = D == 64 ? 2 : 1;
 #pragma unroll
                 for (int part = 0; part < parts; ++part)
@@ -436,11 +460,11 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                                      desc_mn(base + L::xb + k * 2048 + part * 64, D * 128), tc::idesc_bf16_f32(128, D / parts) | kBmn, k > 0);
             }
             __syncwarp();
-            if constexpr (TMA) wait(barV, done);
+            if constexpr (TMA) await(barV, done);
             if constexpr (!STATE) {
                 take_over<D>(kWeighted);  // P is there
                 tc::fence_after_sync();
-                if (tc::elect_one()) {
+                if (goes && tc::elect_one()) {
 #pragma unroll
                     for (int k = 0; k < kChunk / 16; ++k)
                         mma_bf16_ts(tmem + L::tO1, tmem + L::p_at(k), desc_mn(tv + k * 2048, kPanel), tc::idesc_bf16_f32(128, D) | kBmn, k > 0);
@@ -450,7 +474,8 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             }
             take_over<D>(kReady);  // the keys' parts are there
             tc::fence_after_sync();
-            if (tc::elect_one()) {
+            if (lane == 0) *passed = done + 1;
+            if (goes && tc::elect_one()) {
                 // (D = 64: two operands of 128 rows, the first two parts and half of the third twice)
                 const auto update = [&](uint32_t at, uint32_t panel, bool more) {
 #pragma unroll
@@ -468,11 +493,11 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             if constexpr (TMA) now = ahead;
             else step(now);
             if (early && now.at < items) {
-                wait(barQK + 8 * (slot ^ 1), (done + 1) >> 1);
+                await(barQK + 8 * (slot ^ 1), (done + 1) >> 1);
                 form_a(slot ^ 1);
             }
             if (TMA) {
-                wait(barX, done);
+                await(barX, done);
                 load_c(now);
             }
         }
@@ -480,6 +505,11 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
         const uint32_t mine = tmem + ((uint32_t)(quad * 32) << 16);
         const int xrow = quad * 32 + lane, group = warp >> 2, col0 = group * 32;
         float4 *const x = reinterpret_cast<float4 *>(smem + L::lo);  // a state on its way
+        // (The products that the workers wait for are what keeps them from arriving twice at what the issuing warp has not taken over.
+        // Without them its count of chunks does.  It gets there: no worker waits for it on the way but in bounded waits and here.)
+        const auto in_step = [&](int phase) {
+            for (uint32_t i = 0; *passed <= phase && i < (1u << 26); ++i) __nanosleep(100);
+        };
         int done = 0;                                                // chunks
         int taken = 0;                                               // items that had any
         Item m = open(blockIdx.x);
@@ -881,6 +911,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                     }
                 }
                 wait(barX, phase);
+                if (*late) in_step(phase);
                 if (!TMA) load_c(c + 1);
             }
             bad = (odd & 0x7fff7fffu) != 0;  // (a product with 0 is 0 or NaN)
@@ -951,6 +982,14 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
         }
     }
     tc::fence_before_sync();
+    __syncthreads();
+    if (!worker && *late) {  // copies and products that were not waited for end before the CTA does
+        if (tc::elect_one()) tc::mma_commit(barEnd);
+        __syncwarp();
+        for (int k = max(0, asked_ab - 2); k < asked_ab; ++k) tc::mbar_wait_bounded(barQK + 8 * (k & 1), (uint32_t)(k >> 1) & 1u, kWait);
+        if (asked_c > 0) tc::mbar_wait_bounded(barV, (uint32_t)(asked_c - 1) & 1u, kWait);
+        tc::mbar_wait_bounded(barEnd, 0, kWait);
+    }
     __syncthreads();
     if (warp == 1) tc::tmem_dealloc(tmem, L::columns);
 }

@@ -87,3 +87,27 @@ def test_steps_of_any_width(ops, dtype, N, Dk, Dv):
         check(o, f["o"][0][t], f["o"][1][t], "o")
     check(state, *f["s_last"], "state")
     ops.sync()
+
+
+# ------------------------------------------------------------------ waits that give up
+@pytest.mark.parametrize("layout,masked", [("plain", False), ("plain", True), ("shifted", False), ("shifted", True)])
+@pytest.mark.parametrize("T,N,H,D", [(70, 3, 2, 64), (300, 2, 2, 64), (500, 1, 3, 128), (300, 250, 2, 128), (2000, 1, 2, 64), (1500, 1, 1, 128)])
+def test_a_wait_gives_up(seq, T, N, H, D, layout, masked):
+    """A wait that nothing completes, with copies and products on their way: the call ends by its limit with all its warps, the
+    timeout is reported once, and the same call then gives what it gave before.  Copies and plain loads, one span and several."""
+    ops = seq.SequenceOps()
+    s = inputs(T, N, H, D, D, torch.bfloat16, layout, seed=T + D, reset=masked, lengths=masked and N > 1)
+    want = both_ways(ops, s)
+    ops.sync()
+    calls = (lambda: ops.decay_attention(s["q"], s["k"], s["v"], s["g"], **masks(s)),
+             lambda: ops.decay_attention_backward(s["q"], s["k"], s["v"], s["g"], s["do"], ds_last=s["ds_last"], **masks(s)))
+    for call in calls:
+        ops.inject_wait_timeout(1000)
+        call()
+        with pytest.raises(seq.WMError) as e:
+            ops.sync()
+        assert e.value.status == 4
+        ops.sync()
+    got = both_ways(ops, s)
+    ops.sync()
+    assert all(torch.equal(v, got[name]) for name, v in want.items())
