@@ -567,7 +567,8 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
                 load_ab(1);
             }
             find_cuts(0);
-            const float rate = fmaxf(g * 1.4426950408889634f, -1e4f), w_scale = j.w_scale, in_scale = j.in_scale, up_scale = j.up_scale;
+            const float log2_lambda = g * 1.4426950408889634f, rate = log2_lambda < -1e4f ? -1e4f : log2_lambda;  // (NaN stays NaN)
+            const float w_scale = j.w_scale, in_scale = j.in_scale, up_scale = j.up_scale;
             worker_barrier<D>();
             // The state, in registers: of row xr, columns xc and on.  The products of a chunk come by TMEM, fresh each time: the tensor
             // cores' sums are cut off, not rounded, which a state that they ran on over a long sequence would feel (the state's

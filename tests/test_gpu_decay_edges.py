@@ -111,3 +111,20 @@ def test_a_wait_gives_up(seq, T, N, H, D, layout, masked):
     got = both_ways(ops, s)
     ops.sync()
     assert all(torch.equal(v, got[name]) for name, v in want.items())
+
+
+# ------------------------------------------------------------------ decays and values that are not finite
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [5, 20, 100, 300, 1500])
+def test_a_decay_that_is_no_number(ops, dtype, T):
+    """It spoils all tokens of its head that see another one, with states and without, and no other head."""
+    s = inputs(T, 2, 2, 64, 64, DT[dtype], seed=50, state=False)
+    args = s["q"], s["k"], s["v"]
+    want = ops.decay_attention(*args, s["g"], want_last=False)[0], *ops.decay_attention_backward(*args, s["g"], s["do"], want_ds0=False)[:3]
+    g = s["g"].clone()
+    g[0] = float("nan")
+    got = ops.decay_attention(*args, g, want_last=False)[0], *ops.decay_attention_backward(*args, g, s["do"], want_ds0=False)[:3]
+    for name, value, clean in zip(("o", "dq", "dk", "dv"), got, want):
+        assert torch.isnan(value[:-1, :, 0] if name in ("dk", "dv") else value[1:, :, 0]).all(), name
+        assert torch.equal(value[:, :, 1], clean[:, :, 1]), name
+    ops.sync()
