@@ -217,7 +217,7 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
             continue;
         }
         if (tid < 64) {
-            const unsigned c = __ballot_sync(~0u, decay_cut(p, q, s0 + tid, n) && tid < rows);
+            const unsigned c = __ballot_sync(~0u, decay_cut(p, q, s0 + tid, n, g) && tid < rows);
             if ((tid & 31) == 0) cuts[tid >> 5] = c;
         }
         copy_wait<0>();
@@ -367,7 +367,7 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
     } else if (j.s_out) {
         const bool ends = q.len > first && q.len <= last;
         if (ends || (q.len == 0 && span == 0)) to = j.s_out + pair * cells;
-        empty = j.out_zero && q.len > 0 && p.reset && p.reset[n] != 0;
+        empty = j.out_zero && q.len > 0 && ((p.reset && p.reset[n] != 0) || decay_keeps_none(g));
     }
     if (to)
 #pragma unroll 8
@@ -482,6 +482,7 @@ __global__ void __launch_bounds__(256, ROWS <= 4 ? 6 : ROWS <= 8 ? 4 : 2) decay_
         }
     }
     const float keep = expf(p.log_decay[head]);
+    const bool alone = decay_keeps_none(p.log_decay[head]);
     for (int t = 0; t < p.T; ++t) {
         T *out = static_cast<T *>(const_cast<void *>(p.o.p)) + t * p.o.t + n * p.o.n + head * p.o.h;
         if (t >= len) {
@@ -494,7 +495,7 @@ __global__ void __launch_bounds__(256, ROWS <= 4 ? 6 : ROWS <= 8 ? 4 : 2) decay_
         }
         if (tid < width)
             v[tid] = col0 + tid < p.Dv ? seq_to_float(static_cast<const T *>(p.v.p)[t * p.v.t + n * p.v.n + head * p.v.h + col0 + tid]) : 0.f;
-        const bool cut = p.reset && p.reset[(long long)t * p.N + n];
+        const bool cut = alone || (p.reset && p.reset[(long long)t * p.N + n]);
         __syncthreads();
         const float4 w = quads[cg];
         float y[4] = {};

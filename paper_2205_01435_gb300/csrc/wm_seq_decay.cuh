@@ -83,9 +83,13 @@ __device__ __forceinline__ decay_seq decay_open(const decay_pass &p, const decay
     }
     return {p.T, len, j.reverse};
 }
+// A head that keeps nothing: each of its tokens begins something new (0 times a state that is not finite would be NaN).
+__device__ __forceinline__ bool decay_keeps_none(float log_decay) { return log_decay == -INFINITY; }
 // Does step s begin something new, seen in the pass's direction?
-__device__ __forceinline__ bool decay_cut(const decay_pass &p, const decay_seq &q, long long s, int n) {
-    if (!p.reset || s >= q.len) return false;
+__device__ __forceinline__ bool decay_cut(const decay_pass &p, const decay_seq &q, long long s, int n, float log_decay) {
+    if (s >= q.len) return false;
+    if (decay_keeps_none(log_decay)) return !q.reverse || s > 0;
+    if (!p.reset) return false;
     if (!q.reverse) return p.reset[s * p.N + n] != 0;
     return s > 0 && p.reset[(q.len - s) * p.N + n] != 0;  // (the token after this one, in time, begins an episode)
 }

@@ -24,7 +24,7 @@
 // 1024 x 64 x 16 x 64 forward 146 us (3.7 TB/s), backward 353 (2.7 TB/s); 8192 x 2 x 8 x 128 forward 86; 65,536 x 1 x 8 x 128 x 64
 // forward 201, backward 479.
 //
-// Masked places hold zeros, and zero times what is not finite is NaN: a chunk whose outputs or state are not finite marks its
+// Masked places hold zeros, and zero times what is not finite is NaN (so is lambda = 0 times it, of log_decay = -inf): a chunk whose outputs or state are not finite marks its
 // sequence, and the fp32 kernel, which skips what is masked, takes it again.
 #include <algorithm>
 
@@ -525,7 +525,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             const auto find_cuts = [&](int c) {
                 if (CUT && warp < 4) {
                     const int s = first + c * kChunk + warp * 32 + lane;
-                    const unsigned bits = __ballot_sync(~0u, c < chunks && s < stop && decay_cut(p, q, s, m.n));
+                    const unsigned bits = __ballot_sync(~0u, c < chunks && s < stop && decay_cut(p, q, s, m.n, g));
                     if (lane == 0) cuts[((done + c) & 1) * 4 + warp] = bits;
                 }
             };

@@ -128,3 +128,54 @@ def test_a_decay_that_is_no_number(ops, dtype, T):
         assert torch.isnan(value[:-1, :, 0] if name in ("dk", "dv") else value[1:, :, 0]).all(), name
         assert torch.equal(value[:, :, 1], clean[:, :, 1]), name
     ops.sync()
+
+
+def same(got, want, what, dtype):
+    """As good as equal: what is not finite is taken again another way, with roundings of its own."""
+    if got.numel():
+        assert torch.isfinite(got).all(), what
+        off = float((got.double() - want.double()).abs().max())
+        assert off <= (4.0 * ref.B if dtype == torch.bfloat16 else 1e-5) * float(want.double().abs().max()), f"{what}: {off}"
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T", [2, 5, 40, 300, 1500])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("reset", [False, True])
+def test_only_the_token_itself(ops, dtype, T, bad, reset):
+    """A head that keeps nothing (log_decay = -inf): a token's bad values, and a bad state, reach no other token."""
+    dt = DT[dtype]
+    s = inputs(T, 2, 2, 64, 64, dt, seed=51, reset=reset)
+    s["g"] = torch.tensor([-float("inf"), -0.01], device="cuda")
+    want, at = both_ways(ops, s), T // 3
+    assert (want["ds0"][:, 0] == 0).all()
+    others, not_last = torch.arange(T) != at, torch.arange(T) != T - 1
+
+    def spoiled(name, *where):
+        t = dict(s)
+        t[name] = s[name].clone()
+        t[name][where] = bad
+        return both_ways(ops, t)
+
+    for name, alone in (("q", ("o", "dk")), ("k", ("o", "dq", "dv")), ("v", ("o", "dq", "dk")), ("do", ("dq", "dk", "dv"))):
+        got = spoiled(name, at, 0, 0, 3)
+        for out in ("o", "dq", "dk", "dv"):
+            same(got[out][others, 0, 0], want[out][others, 0, 0], f"{out} of {name}", dt)
+            same(got[out][:, 1], want[out][:, 1], f"{out} of {name}, another sequence", dt)
+            if out in alone:
+                assert not torch.isfinite(got[out][at, 0, 0]).all(), f"{out} of {name}"
+        if at < T - 1:
+            same(got["s_last"][:, 0], want["s_last"][:, 0], f"s_last of {name}", torch.float32)
+        assert (got["ds0"][:, 0] == 0).all(), name
+    got = spoiled("s0", 0, 0)
+    for out in ("o", "s_last", "dq", "dk", "dv"):
+        axis = 1 if out == "s_last" else 2
+        same(got[out].select(axis, 0), want[out].select(axis, 0), f"{out} of s0", dt)
+    got = spoiled("ds_last", 0, 0)
+    for out in ("o", "dq"):
+        same(got[out][:, :, 0], want[out][:, :, 0], f"{out} of ds_last", dt)
+    for out in ("dk", "dv"):
+        same(got[out][not_last, :, 0], want[out][not_last, :, 0], f"{out} of ds_last", dt)
+        assert not torch.isfinite(got[out][T - 1, 0, 0]).any(), out
+    assert (got["ds0"][:, 0] == 0).all()
+    ops.sync()
