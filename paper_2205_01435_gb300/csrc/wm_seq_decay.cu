@@ -232,16 +232,18 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
         // (time's order, the last chunk of all: the state leaves as the last token wrote it)
         const int less = j.first && s0 + rows == q.len && !STATE ? 1 : 0;
         if (tid < kChunk) m.kept[tid] = tid < rows && tid >= keep_from ? up_scale * m.power[rows - tid - less] : 0.f;
-        // rows [64][ld] -> [ld][64], each row times its weight (0: nothing of it); true if a value is not finite
+        // rows [64][ld] -> [ld][64], each row times its weight (rows that are not there or cut off: zeros, whatever they hold; a weight
+        // that has become 0 keeps what is not finite); true if a value is not finite
         const auto turn = [&](float *to, const float *rowsm, int ld, const float *w) {
             float odd = 0.f;
             const int r = tid % kChunk;
             const float f = w ? w[r] : 1.f;
+            const bool none = w && !(r < rows && r >= keep_from);
 #pragma unroll 4
             for (int d = tid / kChunk; d < ld / 4; d += kThreads / kChunk) {
                 float4 v = ld4(rowsm + quad_at(r, d, ld));
                 odd += v.x * 0.f + v.y * 0.f + v.z * 0.f + v.w * 0.f;
-                if (w) v = f == 0.f ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
+                if (w) v = none ? make_float4(0.f, 0.f, 0.f, 0.f) : make_float4(v.x * f, v.y * f, v.z * f, v.w * f);
                 to[cell_at(4 * d, r, kChunk)] = v.x;
                 to[cell_at(4 * d + 1, r, kChunk)] = v.y;
                 to[cell_at(4 * d + 2, r, kChunk)] = v.z;
@@ -350,7 +352,7 @@ __device__ __forceinline__ void decay_chunks(const decay_pass &p, int item, floa
                         *x = keep_from < 0 ? *x * shrink + v : v;
                     }
             }
-        carry = keep_from < 0 ? carry * shrink : 0.f;
+        carry = keep_from >= 0 || carry < 0.f ? -1.f : carry * shrink;
         if constexpr (!m.apart) {
             __syncthreads();
             load(s0 + kChunk);
@@ -423,7 +425,7 @@ __global__ void __launch_bounds__(256) decay_join_kernel(const decay_pass p) {
 #pragma unroll
                 for (int h = 0; h < QUAD; ++h) {
                     v.v[h] = x[h];
-                    x[h] = c[k] == 0.f ? own[k].v[h] : x[h] * c[k] + own[k].v[h];
+                    x[h] = c[k] < 0.f ? own[k].v[h] : x[h] * c[k] + own[k].v[h];
                 }
                 seq_store<float, QUAD>(j.spans + (s + k) * pairs * cells + i, v);
             }

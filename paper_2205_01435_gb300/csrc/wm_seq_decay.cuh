@@ -40,7 +40,7 @@ struct decay_pass {
     const uint8_t *reset;
     const int32_t *lengths;
     int *status;
-    float *carry;            // [spans][2][N, H]: what a span multiplies the state by, by direction
+    float *carry;            // [spans][2][N, H]: what a span multiplies the state by, by direction; < 0: it sees nothing before a cut
     int spans;               // of each sequence
     long long span_tokens;   // a multiple of the chunk
     int *redo;               // tensor-core pass: how many marks, then [jobs][N, H] marks: a chunk met what is not finite

@@ -952,7 +952,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             bool empty = false;
             if constexpr (STATE) {
                 to = j.spans + ((long long)m.span * pairs + m.pair) * cells;
-                if (tid == 0) p.carry[((long long)m.span * 2 + j.reverse) * pairs + m.pair] = !keeps ? 0.f : decay_power(g, max(0, stop - first));
+                if (tid == 0) p.carry[((long long)m.span * 2 + j.reverse) * pairs + m.pair] = !keeps ? -1.f : decay_power(g, max(0, stop - first));
             } else if (j.s_out) {
                 if ((len > first && len <= last) || (len == 0 && m.span == 0)) to = j.s_out + (long long)m.pair * cells;
                 empty = j.out_zero && len > 0 && p.reset && p.reset[m.n] != 0;

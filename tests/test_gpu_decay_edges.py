@@ -179,3 +179,48 @@ def test_only_the_token_itself(ops, dtype, T, bad, reset):
         assert not torch.isfinite(got[out][T - 1, 0, 0]).any(), out
     assert (got["ds0"][:, 0] == 0).all()
     ops.sync()
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("T,N", [(5, 2), (40, 2), (200, 2), (2600, 1)])
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+def test_what_is_not_finite_does_not_wear_off(ops, dtype, T, N, bad):
+    """However small its weight has become (0 in fp32): what is not finite reaches all that sees it, and the state."""
+    s = inputs(T, N, 2, 64, 64, DT[dtype], seed=52)
+    s["g"] = torch.tensor([-2.0, -30.0], device="cuda")
+
+    def spoiled(name, *where):
+        t = dict(s)
+        t[name] = s[name].clone()
+        t[name][where] = bad
+        return both_ways(ops, t)
+
+    def none(x, what):
+        assert not torch.isfinite(x).any(), what
+
+    for h in range(2):
+        got = spoiled("k", 1, 0, h, 3)
+        none(got["o"][1:, 0, h], "o of k")
+        none(got["s_last"][0, h, 3], "s_last of k")
+        none(got["dq"][1:, 0, h, 3], "dq of k")
+        got = spoiled("v", 1, 0, h, 3)
+        none(got["o"][1:, 0, h, 3], "o of v")
+        none(got["s_last"][0, h, :, 3], "s_last of v")
+        none(got["dq"][1:, 0, h], "dq of v")
+        got = spoiled("s0", 0, h, 3, 3)
+        none(got["o"][:, 0, h, 3], "o of s0")
+        none(got["s_last"][0, h, 3, 3], "s_last of s0")
+        none(got["dq"][:, 0, h, 3], "dq of s0")
+        got = spoiled("do", T - 2, 0, h, 3)
+        none(got["dk"][:T - 1, 0, h], "dk of do")
+        none(got["dv"][:T - 1, 0, h, 3], "dv of do")
+        none(got["ds0"][0, h, :, 3], "ds0 of do")
+        got = spoiled("q", T - 2, 0, h, 3)
+        none(got["dk"][:T - 1, 0, h, 3], "dk of q")
+        none(got["dv"][:T - 1, 0, h], "dv of q")
+        none(got["ds0"][0, h, 3], "ds0 of q")
+        got = spoiled("ds_last", 0, h, 3, 3)
+        none(got["dk"][:, 0, h, 3], "dk of ds_last")
+        none(got["dv"][:, 0, h, 3], "dv of ds_last")
+        none(got["ds0"][0, h, 3, 3], "ds0 of ds_last")
+    ops.sync()
