@@ -226,9 +226,10 @@ __device__ __forceinline__ bool state_out(const float4 *x, float *to, int da, in
     }
     return !(odd == 0.f);
 }
-// Are a chunk's keys taken in three parts?  Where the state leaves, unless what the chunk gives it is down to 1/16 by then: two parts'
-// 2^-17 of that is 2^-21, below what fp32 sums of hundreds of terms are off by.
-__device__ __forceinline__ bool in_three(float log_decay, int tokens_left) { return tokens_left <= 0 || (float)tokens_left * log_decay > -2.7725887f; }
+// Are a chunk's keys taken in three parts?  Where the state leaves, unless nothing of what the chunk gives it is there by then: tokens
+// after it may write nothing, so that a chunk's part, and two parts' 2^-17 of it, can be all there is.  (2^-277: of fp32's largest value
+// less than its smallest.)
+__device__ __forceinline__ bool in_three(float log_decay, int tokens_left) { return tokens_left <= 0 || (float)tokens_left * log_decay > -192.f; }
 
 // 2^(rate n), rate = log2 lambda and not -inf, as good as 2^-22: for what is rounded to 2^-8.  (In registers: a look at a table in
 // shared memory takes some 250 cycles beside the tensor cores' own.)

@@ -224,3 +224,31 @@ def test_what_is_not_finite_does_not_wear_off(ops, dtype, T, N, bad):
         none(got["dv"][:, 0, h, 3], "dv of ds_last")
         none(got["ds0"][0, h, 3, 3], "ds0 of ds_last")
     ops.sync()
+
+
+# ------------------------------------------------------------------ the state's precision
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("T,tail,rate", [(192, 64, -0.05), (320, 190, -0.05), (384, 128, -0.5), (2000, 300, -0.02)])
+def test_a_state_after_tokens_that_write_nothing(ops, dtype, D, T, tail, rate):
+    """Keys that are zeros at the end (and queries at the start, for the gradient of the entering state): the state that leaves has decayed
+    and is as good as it was.  Beside what near() allows it its factors are off by U / 2 of their exponents, which are rate * tail in all,
+    and the exponential and the product by 3 U each of the chunks that it lay still: of 64 tokens at least.  One call, and two that are cut
+    where the keys end, are each as good as that."""
+    N, H = 1, 2
+    s = inputs(T, N, H, D, D, DT[dtype], seed=53, state=False)
+    s["g"] = torch.tensor([rate, rate / 3], device="cuda")
+    s["k"][T - tail:] = 0
+    s["q"][:tail] = 0
+    s["ds_last"] = None
+    f = ref.attend(s["q"], s["k"], s["v"], s["g"], s["scale"], **masks(s))["s_last"][0]
+    b = ref.attend_backward(s["q"], s["k"], s["v"], s["g"], s["scale"], s["do"], **masks(s))["ds0"][0]
+    got = both_ways(ops, s)
+    _, first = ops.decay_attention(s["q"][:T - tail], s["k"][:T - tail], s["v"][:T - tail], s["g"])
+    _, parts = ops.decay_attention(s["q"][T - tail:], s["k"][T - tail:], s["v"][T - tail:], s["g"], s0=first)
+    for h in range(H):
+        most = (32 + 0.5 * abs(float(s["g"][h])) * (tail + 128) + 3 * (tail // 64 + 2)) * ref.U
+        for what, value, exact in (("s_last", got["s_last"], f), ("s_last of parts", parts, f), ("ds0", got["ds0"], b)):
+            off = float((value[:, h].cpu().double() - exact[:, h]).norm() / exact[:, h].norm())
+            assert off <= most, f"{what}, head {h}: {off} of {most}"
+    ops.sync()
