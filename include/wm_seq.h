@@ -24,7 +24,8 @@
  *
  * Memory: every array is device or managed memory of the handle's device; host memory
  * is an argument error (nothing is staged).  Outputs must not overlap inputs or each
- * other except where a declaration says so.  Arrays of zero elements may be NULL.
+ * other except where a declaration says so (the head norm and the decayed attention refuse
+ * an output that begins where another array of the call does).  Arrays of zero elements may be NULL.
  * Scratch is a workspace of the handle, grown when a call needs more than any before it
  * (that synchronises the device; under stream capture it is an error: make a call of
  * the same size first).  Graphs captured earlier stay valid when it grows.

@@ -3,6 +3,7 @@
 #include <math.h>
 #include <stdio.h>
 
+#include <initializer_list>
 #include <new>
 #include <utility>
 
@@ -110,6 +111,12 @@ void heads_view(Check &c, const wm_seq_heads *v, long long T, int N, int H, int 
         extent += (a.n - 1) * a.stride;
     }
     c.that(apart, "an output's elements overlap (strides)");
+}
+
+// An output that is another array of the call.  (What overlaps in part is the caller's to know: views of one buffer may lie in one
+// another's gaps.)
+void not_another(Check &c, const void *out, std::initializer_list<const void *> others) {
+    for (const void *o : others) c.that(!out || out != o, "an output must not be another array of the call");
 }
 
 bool same_view(const wm_seq_heads &a, const wm_seq_heads &b) {
@@ -435,6 +442,11 @@ wm_status head_norm(wm_seq *h, bool backward, seq_heads_args a, const wm_seq_hea
         c.that(from.data != a.out[i].data || same_view(from, a.out[i]), "an output may be its input with the same strides only");
         if (backward) c.that(a.out[i].data != a.x[i].data, "a gradient must not be q or k");
     }
+    if (any && a.heads[1] > 0 && !c.why) {  // (an output may be its own side's input)
+        not_another(c, a.out[0].data, {a.out[1].data, a.x[1].data, backward ? a.dy[1].data : nullptr});
+        not_another(c, a.out[1].data, {a.x[0].data, backward ? a.dy[0].data : nullptr});
+    }
+    not_another(c, a.dweight[0], {a.dweight[1]});
     if (a.rotary > 0) {
         c.array(a.positions, 4, any, "positions is NULL");
         c.array(a.freqs, 4, any, "freqs is NULL");
@@ -507,6 +519,10 @@ extern "C" wm_status wm_seq_decay_attention(wm_seq *h, int dtype, long long T, i
     DECAY_CHECKS();
     heads_view(c, out, T, N, heads, Dv, es, true, any, "out is NULL");
     c.array(s_last, 4, false, "");
+    if (any && !c.why) {
+        not_another(c, out->data, {q->data, k->data, v->data, s0, s_last});
+        not_another(c, s_last, {q->data, k->data, v->data});
+    }
     SEQ_CHECKED();
     h->last_launches = 0;
     if (N == 0) return WM_OK;
@@ -535,6 +551,12 @@ extern "C" wm_status wm_seq_decay_attention_backward(wm_seq *h, int dtype, long 
     heads_view(c, dv, T, N, heads, Dv, es, true, any, "dv is NULL");
     c.array(ds_last, 4, false, "");
     c.array(ds0, 4, false, "");
+    if (any && !c.why) {
+        not_another(c, dq->data, {q->data, k->data, v->data, dout->data, s0, ds_last, dk->data, dv->data, ds0});
+        not_another(c, dk->data, {q->data, k->data, v->data, dout->data, s0, ds_last, dv->data, ds0});
+        not_another(c, dv->data, {q->data, k->data, v->data, dout->data, s0, ds_last, ds0});
+        not_another(c, ds0, {q->data, k->data, v->data, dout->data, s0});
+    }
     SEQ_CHECKED();
     h->last_launches = 0;
     if (N == 0) return WM_OK;

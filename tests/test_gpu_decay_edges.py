@@ -252,3 +252,46 @@ def test_a_state_after_tokens_that_write_nothing(ops, dtype, D, T, tail, rate):
             off = float((value[:, h].cpu().double() - exact[:, h]).norm() / exact[:, h].norm())
             assert off <= most, f"{what}, head {h}: {off} of {most}"
     ops.sync()
+
+
+# ------------------------------------------------------------------ refusals
+def test_an_output_is_no_other_array(ops, seq):
+    """Three passes read what one writes, and a sequence may be taken again: refused, with the outputs as they were."""
+    for T, dtype in ((8, torch.float32), (40, torch.bfloat16)):
+        s = inputs(T, 2, 2, 8, 8, dtype, seed=70)
+        q, k, v, do, g = s["q"], s["k"], s["v"], s["do"], s["g"]
+        given = {name: x.clone() for name, x in s.items() if torch.is_tensor(x)}
+        for x in (q, k, v):
+            with pytest.raises(seq.WMError, match="another array"):
+                ops.decay_attention(q, k, v, g, out=x)
+        if dtype == torch.float32:
+            with pytest.raises(seq.WMError, match="another array"):
+                ops.decay_attention(q, k, v, g, s_last=q.flatten()[:256].view(2, 2, 8, 8))
+        for x in (q, k, v, do):
+            for name in ("dq", "dk", "dv"):
+                with pytest.raises(seq.WMError, match="another array"):
+                    ops.decay_attention_backward(q, k, v, g, do, **{name: x})
+        x = torch.empty_like(q)
+        for a, b in (("dq", "dk"), ("dq", "dv"), ("dk", "dv")):
+            with pytest.raises(seq.WMError, match="another array"):
+                ops.decay_attention_backward(q, k, v, g, do, **{a: x, b: x})
+        with pytest.raises(seq.WMError, match="another array"):
+            ops.decay_attention_backward(q, k, v, g, do, s0=s["s0"], ds_last=s["ds_last"], ds0=s["s0"])
+        for name, x in given.items():
+            assert torch.equal(s[name], x), name
+        # side by side in one buffer is not the same array
+        wide = torch.empty(T, 2, 2, 24, dtype=dtype, device="cuda")
+        dq, dk, dv = wide.split(8, -1)
+        got = ops.decay_attention_backward(q, k, v, g, do, dq=dq, dk=dk, dv=dv)
+        assert all(torch.equal(a, b) for a, b in zip(got[:3], ops.decay_attention_backward(q, k, v, g, do)))
+    x, y, dx, dy = (rnd(4, 2, 2, 8, seed=71 + i) for i in range(4))
+    given = [t.clone() for t in (x, y, dx, dy)]
+    z = torch.empty_like(x)
+    for kw in (dict(q_out=y), dict(k_out=x), dict(q_out=z, k_out=z), dict(q_out=x, k_out=x)):
+        with pytest.raises(seq.WMError, match="another array"):
+            ops.head_norm(x, y, **kw)
+    for kw in (dict(dq=y), dict(dk=x), dict(dq=dy), dict(dk=dx), dict(dq=z, dk=z)):
+        with pytest.raises(seq.WMError, match="another array|must not be"):
+            ops.head_norm_backward(x, dx, y, dy, **kw)
+    assert all(torch.equal(a, b) for a, b in zip((x, y, dx, dy), given))
+    ops.sync()
