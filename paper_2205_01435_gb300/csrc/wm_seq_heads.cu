@@ -146,8 +146,9 @@ __global__ void __launch_bounds__(kThreads, UPL *VEC > 8 ? 1 : BWD ? 2 : 3) head
     long long tok0 = p.tokens * w0 / all;
     const long long end = p.tokens * (w0 + 1) / all;
     for (int i = threadIdx.x; i < half; i += kThreads) {
-        const double t = (double)p.freqs[i] * 0.15915494309189533577;
-        phase[i] = __double2ull_rz((t - floor(t)) * 18446744073709551616.0);
+        const double t = fabs((double)p.freqs[i]) * 0.15915494309189533577;
+        const unsigned long long u = __double2ull_rz((t - floor(t)) * 18446744073709551616.0);
+        phase[i] = p.freqs[i] < 0.f ? 0ull - u : u;  // (just below a whole turn a small frequency would lose its last bits)
     }
     for (int j = threadIdx.x; j < p.D; j += kThreads) weight[j] = sd.w ? sd.w[j] : 1.f;
 

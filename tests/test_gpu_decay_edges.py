@@ -1,5 +1,5 @@
 """Decayed linear attention: what runs side by side in its kernels, states at the edge of their precision, decays and values that
-are not finite, waits that give up, calls that are refused."""
+are not finite, waits that give up, calls that are refused; angles of the head norm."""
 import pytest
 import torch
 
@@ -295,3 +295,21 @@ def test_an_output_is_no_other_array(ops, seq):
             ops.head_norm_backward(x, dx, y, dy, **kw)
     assert all(torch.equal(a, b) for a, b in zip((x, y, dx, dy), given))
     ops.sync()
+
+
+# ------------------------------------------------------------------ head norm
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_angles_of_negative_frequencies(ops, dtype, interleaved):
+    """A turn back is a turn by the negative position: the same bits, at any position and frequency."""
+    T, N, H, D = 40, 3, 2, 64
+    q, dy = rnd(T, N, H, D, seed=60, dtype=DT[dtype]), rnd(T, N, H, D, seed=61, dtype=DT[dtype])
+    pos = torch.randint(-2 ** 31 + 1, 2 ** 31 - 1, (T, N), generator=torch.Generator().manual_seed(62), dtype=torch.int32).cuda()
+    pos[0] = 2 ** 31 - 1
+    f = (10.0 ** -torch.linspace(0, 12, D // 2, dtype=torch.float64)).float().cuda()
+    a = ops.head_norm(q, positions=pos, freqs=-f, interleaved=interleaved)
+    b = ops.head_norm(q, positions=-pos, freqs=f, interleaved=interleaved)
+    assert torch.equal(a, b)
+    a = ops.head_norm_backward(q, dy, positions=pos, freqs=-f, interleaved=interleaved)
+    b = ops.head_norm_backward(q, dy, positions=-pos, freqs=f, interleaved=interleaved)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[2], b[2])
