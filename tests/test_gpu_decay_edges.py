@@ -313,3 +313,29 @@ def test_angles_of_negative_frequencies(ops, dtype, interleaved):
     a = ops.head_norm_backward(q, dy, positions=pos, freqs=-f, interleaved=interleaved)
     b = ops.head_norm_backward(q, dy, positions=-pos, freqs=f, interleaved=interleaved)
     assert torch.equal(a[0], b[0]) and torch.equal(a[2], b[2])
+
+
+def test_angles_next_to_a_quarter_turn(ops):
+    """Where a cosine or a sine is below 1e-4 its error is the angle's: |position * frequency| 2^-53 by the frequency as a fraction of a turn,
+    2^-33 turns of fixed point, and in all 16 U of the value itself by the functions, the norm and the products (the other side of
+    the pair is 0, so that there is one product)."""
+    import math
+    pos, near_0 = [], []
+    for p in range(1, 400000):
+        for k, f in enumerate((math.cos, math.sin)):
+            if abs(f(float(p))) < 1e-4:
+                pos.append(p)
+                near_0.append(k)
+    pos, near_0 = torch.tensor(pos, dtype=torch.int32), torch.tensor(near_0)
+    assert len(pos) > 40 and 0 < int(near_0.sum()) < len(pos)
+    x = torch.zeros(len(pos), 1, 1, 2, device="cuda")
+    x[..., 0] = 1.0
+    for sign in (1.0, -1.0):
+        y = ops.head_norm(x, positions=pos[:, None].cuda(), freqs=torch.full((1,), sign, device="cuda"), eps=0.0).cpu().double()[:, 0, 0]
+        # (x / sqrt(1 / 2): off by 4 U)
+        got = torch.where(near_0 == 0, y[:, 0], y[:, 1]) / math.sqrt(2.0)
+        want = torch.where(near_0 == 0, torch.cos(pos.double()), sign * torch.sin(pos.double()))
+        most = pos.double() * 2.0 ** -53 + 2 * math.pi * 2.0 ** -33 + 16 * ref.U * want.abs() + 1e-11  # (cosines of 64 bits in the last)
+        off = (got - want).abs()
+        assert (off <= most).all(), float((off / most).max())
+    ops.sync()
