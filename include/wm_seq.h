@@ -17,7 +17,8 @@
  *
  * Types: `dtype` is WM_FP32 or WM_BF16 and holds for the arrays declared `void *`;
  * arithmetic, states, statistics and sums are fp32 (or wider), rounded once when an
- * output is written.
+ * output is written.  The decayed attention rounds factors of the tensor cores to bf16
+ * besides, as its declaration says.
  *
  * Sizes: D, H, T and the tokens of a gradient are at most 2^31 - 65536; what a declaration
  * gives as long long may be larger.
@@ -181,7 +182,8 @@ typedef struct {
  *   positions [T, N] int32 dense;  freqs [rotary / 2] fp32: radians a position
  * rotary is even, 0 <= rotary <= D <= 1024; with 0 positions and freqs are not read.  Positions may be
  * negative.  An angle is taken as a fraction of a turn in 64-bit integers, so that it is as good at far
- * positions as at near ones; its frequency is the fp32 value as it is.  eps >= 0. */
+ * positions as at near ones; its frequency is the fp32 value as it is.  eps >= 0.  Squares are summed in fp32: a row
+ * whose sum of squares leaves fp32's range (values of 10^18 and more) gives zeros. */
 wm_status wm_seq_head_norm(wm_seq *h, int dtype, long long T, int N, int D, int rotary, int interleaved, int q_heads,
                            const wm_seq_heads *q, const float *q_weight, int k_heads, const wm_seq_heads *k,
                            const float *k_weight, float eps, const int32_t *positions, const float *freqs,
@@ -215,10 +217,13 @@ wm_status wm_seq_head_norm_backward(wm_seq *h, int dtype, long long T, int N, in
  *   out      [T, N, heads, Dv] dtype, out
  *   s_last   [N, heads, Dk, Dv] fp32 dense, optional out: the state after the last step; may be s0
  * What is not finite reaches the outputs that see it, and no others (a sequence that holds such values is taken again
- * in fp32, which takes longer).  T = 1 is the single-token form.  A call of T steps and calls on its parts (each
+ * in fp32, which takes longer): with a finite log_decay every later token sees it, however far, with -inf none does.
+ * A log_decay of NaN makes NaN of what it weighs.  T = 1 is the single-token form.  A call of T steps and calls on its parts (each
  * entering with the s_last before it) agree to rounding.
  * In bf16 the products of queries and keys, and the state as the queries read it, are rounded to bf16 as factors of
- * the tensor cores (heads of up to 128 values and more than 12 tokens); sums stay fp32, and so does s_last. */
+ * the tensor cores (heads of up to 128 values and more than 12 tokens); sums stay fp32, and s_last is as good as in fp32.
+ * Wider heads take the fp32 kernel, at its speed; rows that are not whole 16 bytes, or not aligned to them, are read value
+ * by value. */
 wm_status wm_seq_decay_attention(wm_seq *h, int dtype, long long T, int N, int heads, int Dk, int Dv, const wm_seq_heads *q,
                                  const wm_seq_heads *k, const wm_seq_heads *v, const float *log_decay, float scale,
                                  const float *s0, const uint8_t *reset, const int32_t *lengths, const wm_seq_heads *out,

@@ -607,10 +607,11 @@ int slices_of(int dc) { return (dc + kSlice - 1) / kSlice; }
 // Few sequences are cut into spans of time, of at least 4 chunks, as many as take the least time by this count.  A launch takes
 // (chunks of a span + what opening and leaving one takes) for each round of CTAs that the SMs hold, in fp32 0.6 of it for a last
 // round of one CTA an SM where two fit; with spans the launch that forms their states comes on top, at 0.57 of a pass (0.4 in fp32).
-// Measured, us, spans in brackets, the chosen one first.  bf16: 65,536 x 1 x 8 x 128 x 64, forward 198 (19), 460 (6), 213 (38), backward
-// 432 (19), 480 (6), 470 (38); 8192 x 4 x 16 x 64, forward 135 (4), 202 (1), 137 (8), backward 254 (1), 282 (3); 16,384 x 1 x 16 x 64,
-// backward 149 (19), 153 (6), 165 (12).  fp32: 4096 x 24 x 8 x 64, forward 981 (3), 1073 (1), 1020 (8), backward 2104 (1), 2575 (3);
-// 8192 x 1 x 4 x 128, forward 195 (19), 232 (32), backward 481 (19), 535 (12).
+// Measured, us, spans in brackets, the chosen one first (no resets, heads that lose 1/8 to 1/1024 a token).  bf16: 65,536 x 1 x 8 x 128 x 64,
+// forward 213 (19), 587 (6), 232 (38), backward 487 (19), 589 (6), 507 (38); 8192 x 2 x 8 x 128, forward 92 (9), 100 (16), 137 (4);
+// 8192 x 4 x 16 x 64, forward 143 (4), 222 (1), 147 (8), backward 284 (1), 309 (3); 16,384 x 1 x 16 x 64, backward 163 (19), 176 (6), 178 (12).
+// fp32: 4096 x 24 x 8 x 64, forward 981 (3), 1068 (1), 1020 (8), backward 2092 (1), 2571 (3); 8192 x 1 x 4 x 128, forward 195 (19), 233 (32),
+// backward 485 (19), 542 (12).
 void split(const wm_seq *h, decay_pass &p, const seq_decay_args &a, bool tc) {
     long long ctas = 0, state_ctas = 0;
     int da = 0;

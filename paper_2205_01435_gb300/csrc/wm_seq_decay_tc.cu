@@ -6,8 +6,8 @@
 //   P = A * weights               TMEM -> registers -> TMEM as bf16, where the next product reads it
 //   O2 = a Xb                     Xb: the state X as a bf16 tile
 //   O1 = P c,  y = O1 + in_scale lambda^r O2
-//   X = lambda^n X + (b w)^T c    X in fp32 in registers; b w as three bf16 values, all 24 bits of it, where the state leaves and the chunk
-//                                 still counts in it: it is as good as in fp32; else as two
+//   X = lambda^n X + (b w)^T c    X in fp32 in registers; b w as three bf16 values, all 24 bits of it, where the state leaves and anything of
+//                                 the chunk can be left in it: it is as good as in fp32; else as two
 // a, b and c lie as [128 tokens][64 values] panels of 128-byte rows in the 128-byte swizzle, which serve as K-major operands
 // (a, b in A and O2) and as MN-major ones (c, and b transposed, where the tokens are summed over).  Rows come by asynchronous
 // 16-byte copies that a padded token or value leaves as zeros: lengths, strides and either direction of time cost nothing extra.
@@ -20,9 +20,9 @@
 // the chain copies - A - P - O1 - update that a chunk walks, each link with its latency, and the workers' instructions between them
 // (50% of the issue slots at 1024 x 64 x 16 x 64).  Hence two CTAs an SM where a head has up to 64 values (96 registers a thread are
 // all that 18 warps can have), hand-overs after which the workers go on, and chunks of 128: fewer would leave half of the tensor
-// cores' rows empty.  Times: 128 x 512 x 16 x 64 ragged forward 193 us (2.4 TB/s of the tokens that are there);
-// 1024 x 64 x 16 x 64 forward 146 us (3.7 TB/s), backward 353 (2.7 TB/s); 8192 x 2 x 8 x 128 forward 86; 65,536 x 1 x 8 x 128 x 64
-// forward 201, backward 479.
+// cores' rows empty.  Times: 128 x 512 x 16 x 64 ragged forward 199 us (2.3 TB/s of the tokens that are there);
+// 1024 x 64 x 16 x 64 forward 156 us (3.4 TB/s), backward 381 (2.5 TB/s); 8192 x 2 x 8 x 128 forward 90; 65,536 x 1 x 8 x 128 x 64
+// with resets forward 235, backward 534.
 //
 // Masked places hold zeros, and zero times what is not finite is NaN (so is lambda = 0 times it, of log_decay = -inf): a chunk whose outputs or state are not finite marks its
 // sequence, and the fp32 kernel, which skips what is masked, takes it again.
@@ -228,7 +228,8 @@ __device__ __forceinline__ bool state_out(const float4 *x, float *to, int da, in
 }
 // Are a chunk's keys taken in three parts?  Where the state leaves, unless nothing of what the chunk gives it is there by then: tokens
 // after it may write nothing, so that a chunk's part, and two parts' 2^-17 of it, can be all there is.  (2^-277: of fp32's largest value
-// less than its smallest.)
+// less than its smallest.  Against two parts once 1/16 is left, both directions: 1024 x 64 x 16 x 64 510 -> 532 us, 65,536 x 1 x 8 x 128 x 64
+// 687 -> 763.)
 __device__ __forceinline__ bool in_three(float log_decay, int tokens_left) { return tokens_left <= 0 || (float)tokens_left * log_decay > -192.f; }
 
 // 2^(rate n), rate = log2 lambda and not -inf, as good as 2^-22: for what is rounded to 2^-8.  (In registers: a look at a table in
@@ -574,7 +575,7 @@ __global__ void __launch_bounds__(Plan<D>::threads, D == 64 ? 2 : 1) decay_tc_ke
             // The state, in registers: of row xr, columns xc and on.  The products of a chunk come by TMEM, fresh each time: the tensor
             // cores' sums are cut off, not rounded, which a state that they ran on over a long sequence would feel (the state's
             // gradient after 16,384 tokens of 8 heads of 128: 2e-7 off in the norm, by sums in place in TMEM 1e-6; that is what it
-            // costs: 479 -> 547 us backward there when it was built, 371 -> 389 at 1024 x 64 x 16 x 64).
+            // costs, when it was built: 65,536 x 1 x 8 x 128 x 64 479 -> 547 us backward, 1024 x 64 x 16 x 64 371 -> 389).
             constexpr int XN = D == 64 ? 16 : 32;
             const int xr = D == 64 ? xrow & 63 : xrow, xc = col0 + (D == 64 && quad >= 2 ? 16 : 0);
             float X[XN];
