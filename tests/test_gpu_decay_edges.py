@@ -5,7 +5,7 @@ import torch
 
 import decay_reference as ref
 from seq_reference import check
-from test_gpu_decay import DT, decays, inputs, masks, near, ops, rnd, seq  # noqa: F401  (fixtures among them)
+from test_gpu_decay import DT, inputs, masks, near, ops, rnd, seq  # noqa: F401  (fixtures among them)
 
 pytestmark = pytest.mark.gpu
 
